@@ -335,6 +335,150 @@ int32_t mikv_budget(int32_t T, double ratio);
 /* Bytes of one retained row (codes + parameters, K or V) and of one important row (K or V). */
 size_t mikv_retained_row_bytes(int32_t bits, int32_t group, int32_t head_dim);
 
+/* ------------------------------------------------------------------ prompts: positions, attention, shared prefixes
+ *
+ * What stands on either side of the mixed-precision cache: rotary positions for queries and keys, the attention of
+ * a prompt's own tokens, and single-token attention over a prefix whose keys and values several requests share
+ * (joined with what each request's own cache gave). The conventions are those of the entry points above. Tensors
+ * are views with strides, so the token-major rows a projection leaves and the head-major rows the cache is built
+ * from are taken alike. */
+
+/* Element types of these entry points. */
+enum { MIKV_BF16 = 0, MIKV_F16 = 1, MIKV_F32 = 2 };
+
+/* A tensor [batch][heads][tokens][d] in device memory: element strides of its first three dimensions (the channels
+ * are dense). The stride of a dimension of size 1 is not used. */
+typedef struct {
+  void* data;
+  int64_t stride_batch, stride_head, stride_token;
+} mikv_view;
+
+/* Which channels of a head turn together: i and i + rot / 2, or 2 i and 2 i + 1 (i < rot / 2). */
+enum { MIKV_ROTARY_HALF = 0, MIKV_ROTARY_INTERLEAVED = 1 };
+
+typedef struct {
+  int32_t dtype;      /* of both tensors: MIKV_BF16, MIKV_F16 or MIKV_F32 */
+  int32_t batch;
+  int32_t tokens;
+  int32_t heads_q;    /* heads of the first tensor */
+  int32_t heads_k;    /* heads of the second tensor, 0 = there is none */
+  int32_t head_dim;   /* d, must be 128 */
+  int32_t rot;        /* channels that turn, even, 2 <= rot <= d; the others are copied */
+  int32_t layout;     /* MIKV_ROTARY_HALF or MIKV_ROTARY_INTERLEAVED */
+  int32_t inverse;    /* 0: turn by the angle; 1: by minus the angle (the transposed map: the gradient's) */
+  float amplitude;    /* factor on the turned channels (1 unless long-context scaling asks for one) */
+} mikv_rotary_desc;
+
+/*
+ * Phases of the rotary frequencies: phases[i] = the fraction of a turn that frequency i (radians per position,
+ * freq[i] >= 0) advances per position, modulo 1, in units of 2^-64. Position times phase in 64-bit integer
+ * arithmetic is then the angle modulo a turn, without the loss that a 32-bit product has at long positions.
+ * Host-only, pure; n values each. Returns MIKV_ERR_ARG for a negative or non-finite frequency.
+ */
+mikv_status mikv_rotary_phases(const double* freq, int32_t n, uint64_t* phases);
+
+/*
+ * Rotary positions of a query tensor and (optionally, in the same launch) a key tensor: every pair (x, x') of
+ * channels named by `layout` becomes amplitude * (x cos a - x' sin a, x sin a + x' cos a), a = 2 pi pos phase_i,
+ * the other channels are copied; fp32 arithmetic, one rounding to `dtype`.
+ *   q_in, q_out, k_in, k_out  views [batch][heads][tokens][d]; an output may be its own input (in place), and may
+ *              have other strides than it (e.g. token-major in, head-major out). Any alignment of the elements.
+ *   phases     uint64 [rot / 2] (device), see mikv_rotary_phases
+ *   positions  int32 [batch][tokens] (device), or NULL: token t has position `start` + t. Negative positions turn
+ *              the other way.
+ */
+mikv_status mikv_rotary(const mikv_rotary_desc* desc, const mikv_view* q_in, const mikv_view* q_out,
+                        const mikv_view* k_in, const mikv_view* k_out, const uint64_t* phases,
+                        const int32_t* positions, int32_t start, void* stream);
+
+/*
+ * The keys that each query of a prompt sees, as half-open spans: spans[b][i] = [lo, hi). Query i stands at position
+ * p = q_start + i among the tk keys. It starts from [0, causal ? p + 1 : tk); then
+ *   docs    int32 [batch][n_docs + 1] or NULL: ascending offsets of the documents packed into the row. lo becomes
+ *           the start of the document that holds p, hi is cut at its end; a p in no document (padding) sees nothing
+ *   prefix  int32 [batch][max(n_docs, 1)] or NULL: the first prefix[d] keys of p's document (of the row without
+ *           `docs`) are seen by all of its queries
+ *   key_len int32 [batch] or NULL: keys from key_len[b] on are seen by nobody
+ * An empty span is written as [0, 0). One launch; the result serves every layer of the batch.
+ *   spans   int32 [batch][tq][2] (device), 8-byte aligned
+ */
+mikv_status mikv_mask_spans(int32_t* spans, int32_t batch, int32_t tq, int32_t tk, int32_t q_start, int32_t causal,
+                            const int32_t* docs, int32_t n_docs, const int32_t* prefix, const int32_t* key_len,
+                            void* stream);
+
+typedef struct {
+  int32_t dtype;      /* of q, k, v: MIKV_BF16 or MIKV_F16 */
+  int32_t out_dtype;  /* of out: the same, or MIKV_F32 */
+  int32_t batch;
+  int32_t heads_q;
+  int32_t heads_kv;   /* heads_q / heads_kv in {1, 2, 4, 8} */
+  int32_t head_dim;   /* d, must be 128 */
+  int32_t tq;         /* queries per row of the batch */
+  int32_t tk;         /* keys per row of the batch */
+  int32_t causal;     /* without spans: 1 = query i sees the keys up to its own position, 0 = all keys */
+  int32_t q_start;    /* position of query 0 among the keys (tk - tq when the queries are the last tokens) */
+  float sm_scale;     /* > 0 */
+  float softcap;      /* 0 = none; c > 0: scores become c tanh(score / c) */
+} mikv_prompt_desc;
+
+/*
+ * Attention of a prompt's queries over its keys:
+ *   s_ij = sm_scale * q_i . k_j;  softcap c: s_ij = c tanh(s_ij / c);  slopes: s_ij -= slope_h |p_i - j|
+ *   out_i = sum_j softmax_j(s_i) v_j over the keys j that query i sees,  lse_i = ln sum_j exp(s_ij)
+ * with p_i = q_start + i. A query that sees no key gives out = 0 and lse = -inf. Keys that no query sees may hold
+ * any bits. A query that sees an infinity or NaN in V gets NaN in the channels concerned (in tiles that a mask
+ * cuts, in all channels); other queries are not touched by it.
+ * Scores and sums are fp32 (exact products, fp32 accumulation); the probabilities enter the product with V rounded
+ * to the input type.
+ *   q, k, v, out  views; 16-byte aligned data, strides multiples of 16 bytes. k and v may have a zero batch or head
+ *                 stride (one set of keys for several)
+ *   spans     int32 [batch][tq][2] from mikv_mask_spans, or NULL (then `causal` decides); lo < 0 counts as 0 and
+ *             hi > tk as tk
+ *   slopes    fp32 [heads_q] or NULL
+ *   lse       fp32 [batch][heads_q][tq] or NULL
+ *   workspace >= mikv_prompt_workspace_bytes(desc) bytes, 256-byte aligned, status word as in the entry points above
+ */
+size_t mikv_prompt_workspace_bytes(const mikv_prompt_desc* desc);
+mikv_status mikv_prompt_attention(const mikv_prompt_desc* desc, const mikv_view* q, const mikv_view* k,
+                                  const mikv_view* v, const mikv_view* out, const int32_t* spans,
+                                  const float* slopes, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+typedef struct {
+  int32_t dtype;      /* of q, k, v: MIKV_BF16 or MIKV_F16 */
+  int32_t out_dtype;  /* of out: the same, or MIKV_F32 */
+  int32_t batch;      /* requests, one query token each */
+  int32_t groups;     /* prefixes; requests b of the batch share prefix b div (batch / groups) */
+  int32_t heads_q;
+  int32_t heads_kv;   /* heads_q / heads_kv in {1, 2, 4, 8} */
+  int32_t head_dim;   /* d, must be 128 */
+  int32_t length;     /* keys per prefix (the longest, with `lens`) */
+  float sm_scale;     /* > 0 */
+  float softcap;      /* as in mikv_prompt_desc */
+} mikv_prefix_desc;
+
+/*
+ * Single-token attention over prefixes that requests share: every key and value of a prefix is read once for all
+ * its requests and their query heads. groups = batch gives each request keys of its own (a plain bf16 / fp16
+ * cache); groups = 1 one prefix for all. Scores as in mikv_prompt_attention with p = q_pos[b].
+ * With own_out and own_ml the result is joined with attention over other keys of the same query, as
+ * mikv_decode_attention leaves it for the request's own cache (fp32 output, (max, sum)): the softmax runs over both.
+ *   q         [batch][heads_q][d] dense, 16-byte aligned
+ *   k, v      views [groups][heads_kv][length][d] as in mikv_prompt_attention
+ *   lens      int32 [groups] (device) or NULL: keys of each prefix, 0 <= lens <= length; later rows may hold any bits
+ *   q_pos     int32 [batch] (device) or NULL: position of each query, for the distance (NULL: the prefix's length)
+ *   slopes    fp32 [heads_q] or NULL
+ *   own_out   fp32 [batch][heads_q][d], own_ml fp32 [batch][heads_q][2], or both NULL
+ *   out       [batch][heads_q][d] dense, 16-byte aligned; 0 where there is no key at all
+ *   ml        fp32 [batch][heads_q][2] or NULL: (ln sum exp(s), 1) over all keys, (-inf, 0) where there is none: a
+ *             (reference, sum) pair like mikv_decode_attention's, for mikv_update_importance or a further join
+ *   workspace >= mikv_prefix_workspace_bytes(desc) bytes, 256-byte aligned
+ */
+size_t mikv_prefix_workspace_bytes(const mikv_prefix_desc* desc);
+mikv_status mikv_prefix_attention(const mikv_prefix_desc* desc, const void* q, const mikv_view* k,
+                                  const mikv_view* v, const int32_t* lens, const int32_t* q_pos,
+                                  const float* slopes, const float* own_out, const float* own_ml, void* out,
+                                  float* ml, void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

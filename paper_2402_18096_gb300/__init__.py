@@ -24,6 +24,8 @@ __all__ = [
     "mikv_gather_hi", "mikv_decode_step", "mikv_cache_fraction", "mikv_retained_row_bytes",
     "mikv_decode_attention_noalloc", "mikv_noalloc_check", "NOALLOC_SCRATCH_BYTES", "mikv_prefill_scores",
     "mikv_budget", "shape_for_context", "mikv_debug_check", "debug_build",
+    "RotaryTable", "mikv_rotary_phases", "mikv_rotary", "mikv_mask_spans", "mikv_prompt_workspace_bytes",
+    "mikv_prompt_attention", "mikv_prefix_workspace_bytes", "mikv_prefix_attention",
     "WS_ATTENTION", "WS_BALANCER", "WS_STEP", "WS_PREFILL", "OUT_BF16", "OUT_F32", "HEAD_DIM",
 ]
 
@@ -52,6 +54,29 @@ class _Cache(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("k_hi", "v_hi", "hi_tok", "acc", "k_codes", "v_codes", "k_params", "v_params", "lo_tok",
                  "balancer", "k_hi_params", "v_hi_params")]
+
+
+class _View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_batch", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+                ("stride_token", ctypes.c_int64)]
+
+
+class _RotaryDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("dtype", "batch", "tokens", "heads_q", "heads_k", "head_dim", "rot", "layout", "inverse")]
+    _fields_ += [("amplitude", ctypes.c_float)]
+
+
+class _PromptDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("dtype", "out_dtype", "batch", "heads_q", "heads_kv", "head_dim", "tq", "tk", "causal", "q_start")]
+    _fields_ += [("sm_scale", ctypes.c_float), ("softcap", ctypes.c_float)]
+
+
+class _PrefixDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("dtype", "out_dtype", "batch", "groups", "heads_q", "heads_kv", "head_dim", "length")]
+    _fields_ += [("sm_scale", ctypes.c_float), ("softcap", ctypes.c_float)]
 
 
 _lib = None
@@ -95,6 +120,13 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
                 "mikv_prefill_scores": (I, [SP, P, P, I, F, P, P, Z, P]),
                 "mikv_cache_fraction": (ctypes.c_double, [I, I, ctypes.c_double, I]),
                 "mikv_retained_row_bytes": (Z, [I, I, I]),
+                "mikv_rotary_phases": (I, [P, I, P]),
+                "mikv_rotary": (I, [P, P, P, P, P, P, P, I, P]),
+                "mikv_mask_spans": (I, [P, I, I, I, I, I, P, I, P, P, P]),
+                "mikv_prompt_workspace_bytes": (Z, [P]),
+                "mikv_prompt_attention": (I, [P, P, P, P, P, P, P, P, P, Z, P]),
+                "mikv_prefix_workspace_bytes": (Z, [P]),
+                "mikv_prefix_attention": (I, [P, P, P, P, P, P, P, P, P, P, P, P, Z, P]),
             }
             for name, (res, args) in sig.items():
                 fn = getattr(lib, name)
@@ -336,3 +368,8 @@ def mikv_budget(T: int, ratio: float) -> int:
 
 def mikv_retained_row_bytes(bits: int, group: int, head_dim: int = HEAD_DIM) -> int:
     return int(load(build_if_missing=False).mikv_retained_row_bytes(bits, group, head_dim))
+
+
+from .prompt import (RotaryTable, mikv_mask_spans, mikv_prefix_attention,  # noqa: E402
+                     mikv_prefix_workspace_bytes, mikv_prompt_attention, mikv_prompt_workspace_bytes, mikv_rotary,
+                     mikv_rotary_phases)

@@ -9,35 +9,12 @@
 
 #include <mutex>
 
-#ifndef MIKV_NVTX
-#define MIKV_NVTX 1
-#endif
-#if MIKV_NVTX
-#include <nvtx3/nvToolsExt.h>
-#endif
-
 #include "mikv_device.cuh"
 #include "mikv_internal.h"
+#include "mikv_nvtx.h"
 #include "mikv_prefill.h"
 
 using namespace mikv;
-
-namespace {
-// One NVTX range per compute entry point, named after the call, around its validation and launches (host time:
-// the kernels run later on the stream). Without a tool attached, push and pop return at once; -DMIKV_NVTX=0
-// leaves them out.
-struct CallRange {
-#if MIKV_NVTX
-  explicit CallRange(const char* name) { nvtxRangePushA(name); }
-  ~CallRange() { nvtxRangePop(); }
-#else
-  explicit CallRange(const char*) {}
-#endif
-  CallRange(const CallRange&) = delete;
-  CallRange& operator=(const CallRange&) = delete;
-};
-}  // namespace
-#define MIKV_CALL_RANGE() const CallRange mikv_call_range_(__func__)
 
 // The library's own status word for the index checks of debug builds (-DMIKV_DEBUG) in the entry points that take
 // no workspace (insertion, gather, quantize/pack). Looked up in the current context on every use.

@@ -1,0 +1,39 @@
+// mikv_flash.h — arguments of the attention kernels over bf16 / fp16 keys (mikv_flash.cu): prompts and shared
+// prefixes.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "mikv_device.cuh"
+
+namespace mikv {
+
+// Both entry points are one problem to the kernels: `batch` sets of keys, each attended by tq "tokens" of G query
+// heads per KV head. For a prompt a token is a query position; for a shared prefix it is one of its requests.
+struct FlashArgs {
+  const void *q, *k, *v;
+  long long q_b, q_h, q_t, k_b, k_h, k_t, v_b, v_h, v_t;  // element strides
+  void* out;
+  long long o_b, o_h, o_t;
+  float* stat;                 // log-sum-exp (stat_pair 0), or (log-sum-exp, 1) pairs (stat_pair 1), or nullptr
+  long long s_b, s_h, s_t;     // strides of stat in entries
+  int stat_pair;
+  const float* own_out;        // join: [batch * tq][heads_q][128] with its (max, sum), or nullptr
+  const float* own_ml;
+  const int2* spans;           // [batch][tq], or nullptr
+  const int32_t* lens;         // [batch] visible keys, or nullptr
+  const int32_t* pos;          // [batch][tq] query positions, or nullptr
+  const float* slopes;         // [heads_q] or nullptr
+  int batch, tq, tk, heads_q, heads_kv, G;
+  int causal, q_start;
+  int pos_at_len;              // without `pos`: 1 = a query stands at its set's length, 0 = at q_start + token
+  float sm_scale, softcap;
+  int* status;
+};
+
+size_t flash_workspace_bytes(int batch, int heads_kv, int G, int tq, int tk, int num_sms);
+cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, int num_sms, cudaStream_t st);
+
+}  // namespace mikv
