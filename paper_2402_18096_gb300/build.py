@@ -22,7 +22,7 @@ LIB_DEBUG = os.path.join(OUT_DIR_DEBUG, "libmikv_debug.so")
 SOURCES = ["mikv_attn_h16.cu", "mikv_attn_h8.cu", "mikv_attn_h4.cu", "mikv_attn_h2.cu", "mikv_attn_kch.cu",
            "mikv_attention.cu",
            "mikv_quant.cu", "mikv_policy.cu", "mikv_step.cu", "mikv_prefill.cu", "mikv_abi.cu",
-           "mikv_rotary.cu", "mikv_flash.cu", "mikv_abi_prompt.cu"]
+           "mikv_rotary.cu", "mikv_flash.cu", "mikv_flash_bf16.cu", "mikv_flash_f16.cu", "mikv_abi_prompt.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

@@ -1,115 +1,174 @@
-// mikv_flash.cu — attention over bf16 / fp16 keys (sm_103a): prompts, and single tokens over a shared prefix.
-//
-// One block per (set of keys, query head, token): 128 keys at a time, a thread per key for the scores and a thread
-// per channel for the output, online softmax in fp32. Masked keys are never read.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-#include <math.h>
+// mikv_flash.cu — attention over bf16 / fp16 keys: work plan, tensor maps, merge of split parts and dispatch (the
+// kernels are in mikv_flash.cuh).
+#include <string.h>
 
-#include "mikv_flash.h"
+#include <mutex>
+
+#include "mikv_flash.cuh"
+#include "mikv_internal.h"
 
 namespace mikv {
 namespace {
 
-constexpr float kLn2 = 0.6931471805599453f;
+using flash::kTile;
 
-template <bool F16>
-__device__ __forceinline__ float load16(const void* p, long long i) {
-  return F16 ? __half2float(static_cast<const __half*>(p)[i]) : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeTiledFn>(p);
+  });
+  return fn;
 }
 
-template <bool F16, bool OUT32>
-__global__ void __launch_bounds__(128) flash_rows_kernel(const __grid_constant__ FlashArgs a) {
-  __shared__ float s_q[128], s_p[128], s_red[4];
-  const int tid = threadIdx.x, t = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-  const int kv = h / a.G;
-  int lo = 0, hi = a.tk, len = a.tk;
-  if (a.lens) len = hi = max(0, min(a.lens[b], a.tk));
-  if (a.spans) {
-    const int2 s = a.spans[(size_t)b * a.tq + t];
-    lo = max(s.x, 0);
-    hi = min(s.y, a.tk);
-  } else if (a.causal) {
-    hi = (int)min((long long)a.tk, max(0ll, (long long)a.q_start + t + 1));
+// Map of a 16-bit tensor of 128 channels and three more dimensions (element strides; a zero stride makes the
+// dimension one entry long: its coordinate is then 0).
+bool encode_rows(CUtensorMap* map, bool f16, const void* data, const long long (&n)[3], const long long (&stride)[3],
+                 const uint32_t (&box)[3]) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return false;
+  cuuint64_t dims[4] = {kHeadDim, 1, 1, 1};
+  cuuint64_t strides[3];
+  cuuint32_t boxes[4] = {64, box[0], box[1], box[2]};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 3; ++i) {
+    dims[i + 1] = stride[i] ? (cuuint64_t)n[i] : 1;
+    strides[i] = stride[i] ? 2 * (cuuint64_t)stride[i] : 2 * kHeadDim;
   }
-  const int pos = a.pos ? a.pos[(size_t)b * a.tq + t] : a.pos_at_len ? len : a.q_start + t;
-  const float slope = a.slopes ? a.slopes[h] : 0.f;
-  s_q[tid] = load16<F16>(a.q, b * a.q_b + h * a.q_h + t * a.q_t + tid);
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  __syncthreads();
-  for (int j0 = lo; j0 < hi; j0 += 128) {
-    const int j = j0 + tid;
-    float s = -INFINITY;
-    if (j < hi) {
-      float acc = 0.f;
-      const long long base = b * a.k_b + kv * a.k_h + (long long)j * a.k_t;
-      for (int c = 0; c < 128; ++c) acc = fmaf(s_q[c], load16<F16>(a.k, base + c), acc);
-      s = acc * a.sm_scale;
-      if (a.softcap > 0.f) s = a.softcap * tanhf(s / a.softcap);
-      s -= slope * fabsf((float)(pos - j));
-    }
-    float mx = s;
-    for (int off = 16; off; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-    if ((tid & 31) == 0) s_red[tid >> 5] = mx;
-    __syncthreads();
-    const float mn = fmaxf(m, fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])));
-    const float ref = mn == -INFINITY ? 0.f : mn;
-    const float p = j < hi ? expf(s - ref) : 0.f;
-    s_p[tid] = p;
-    const float c = m == -INFINITY ? 0.f : expf(m - ref);
-    m = mn;
-    __syncthreads();
-    float sum = 0.f, acc = 0.f;
-    const int n = min(128, hi - j0);
-    const long long base = b * a.v_b + kv * a.v_h + (long long)j0 * a.v_t + tid;
-    for (int i = 0; i < n; ++i) {
-      sum += s_p[i];
-      acc = fmaf(s_p[i], load16<F16>(a.v, base + i * a.v_t), acc);
-    }
-    l = l * c + sum;
-    o = o * c + acc;
-    __syncthreads();
+  return enc(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(data),
+             dims, strides, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Plan {
+  bool pair;
+  int m_blocks, n_splits;
+};
+
+// Splits a row block's key tiles may be cut into: enough that two rounds of CTAs could be filled, at least two tiles
+// each (so that both streams of a CTA have one).
+int most_splits(long long base, int tiles, int num_sms) {
+  const long long by_sms = 2ll * num_sms / base;
+  const long long s = by_sms < tiles / 2 ? by_sms : tiles / 2;
+  return s < 1 ? 1 : (int)s;
+}
+
+Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
+  Plan p;
+  const long long rows = (long long)tq * G;
+  p.pair = rows > kTile;
+  p.m_blocks = (int)(p.pair ? (rows + 2 * kTile - 1) / (2 * kTile) : 1);
+  const long long base = (long long)batch * heads_kv * p.m_blocks;
+  const int tiles = (int)(((long long)tk + kTile - 1) / kTile);
+  // rounds of CTAs times the length of one: its tiles plus about four tiles' time of start and end
+  p.n_splits = 1;
+  double best = 1e300;
+  for (int s = 1; s <= most_splits(base, tiles, num_sms); ++s) {
+    const double rounds = (double)((base * s + num_sms - 1) / num_sms);
+    const double cost = rounds * ((tiles + s - 1) / s + 4.0 + (s > 1 ? 1.0 : 0.0));
+    if (cost < best) best = cost, p.n_splits = s;
   }
-  float lse = l == 0.f ? -INFINITY : m + logf(l);
-  float r = l == 0.f ? 0.f : o / l;
-  if (a.own_out) {
-    const size_t row = ((size_t)b * a.tq + t) * a.heads_q + h;
-    const float om = a.own_ml[2 * row], ol = a.own_ml[2 * row + 1];
-    const float mine = ol == 0.f ? -INFINITY : om + logf(ol);
-    const float top = fmaxf(lse, mine);
-    if (mine != -INFINITY) {
-      const float w0 = expf(lse - top), w1 = expf(mine - top);
-      r = (r * w0 + a.own_out[row * 128 + tid] * w1) / (w0 + w1);
-      lse = top + logf(w0 + w1);
-    }
+  return p;
+}
+
+struct MergePartsArgs {
+  FlashArgs a;
+  const float* part_o;
+  const float* part_lse;
+  long long part_rows;
+  int n_splits, out_kind;
+};
+
+// One warp per output row: the parts weighted by 2^(lse - largest), then the join with the request's own part.
+__global__ void __launch_bounds__(128) merge_parts_kernel(const __grid_constant__ MergePartsArgs m) {
+  const FlashArgs& a = m.a;
+  const long long row = blockIdx.x * 4ll + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  grid_dependency_wait();
+  if (row >= m.part_rows) return;
+  float top = -INFINITY;
+  for (int s = lane; s < m.n_splits; s += 32) top = fmaxf(top, m.part_lse[s * m.part_rows + row]);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < m.n_splits; ++s) {
+    const float e = m.part_lse[s * m.part_rows + row];
+    if (e == -INFINITY) continue;  // nothing seen
+    const float w = fast_exp2(e - top);
+    const float4 o = reinterpret_cast<const float4*>(m.part_o + (s * m.part_rows + row) * kHeadDim)[lane];
+    sum += w;
+    acc.x = fmaf(o.x, w, acc.x);
+    acc.y = fmaf(o.y, w, acc.y);
+    acc.z = fmaf(o.z, w, acc.z);
+    acc.w = fmaf(o.w, w, acc.w);
   }
-  const long long at = b * a.o_b + h * a.o_h + t * a.o_t + tid;
-  if (OUT32)
-    static_cast<float*>(a.out)[at] = r;
-  else if (F16)
-    static_cast<__half*>(a.out)[at] = __float2half_rn(r);
+  float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
+  float f0 = sum == 0.f ? 0.f : 1.f / sum, f1 = 0.f;
+  if (a.own_out) flash::join_own(a, row, lse2, f0, f1);
+  float v[4] = {acc.x * f0, acc.y * f0, acc.z * f0, acc.w * f0};
+  if (f1 != 0.f) {
+    const float4 o = reinterpret_cast<const float4*>(a.own_out + row * kHeadDim)[lane];
+    v[0] = fmaf(o.x, f1, v[0]);
+    v[1] = fmaf(o.y, f1, v[1]);
+    v[2] = fmaf(o.z, f1, v[2]);
+    v[3] = fmaf(o.w, f1, v[3]);
+  }
+  const int head = (int)(row % a.heads_q);
+  const long long bt = row / a.heads_q;
+  const int token = (int)(bt % a.tq), b = (int)(bt / a.tq);
+  const long long at = b * a.o_b + head * a.o_h + token * a.o_t + 4 * lane;
+  if (m.out_kind == 2)
+    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
   else
-    static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(r);
-  if (a.stat && tid == 0) {
-    const long long i = b * a.s_b + h * a.s_h + t * a.s_t;
-    if (a.stat_pair) {
-      a.stat[2 * i] = lse;
-      a.stat[2 * i + 1] = lse == -INFINITY ? 0.f : 1.f;
-    } else {
-      a.stat[i] = lse;
-    }
-  }
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) =
+        m.out_kind == 1 ? make_uint2(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]))
+                        : make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+  if (lane == 0) flash::store_stat(a, b * a.s_b + head * a.s_h + token * a.s_t, lse2);
 }
 
 }  // namespace
 
-size_t flash_workspace_bytes(int, int, int, int, int, int) { return kWsHeader; }
+size_t flash_workspace_bytes(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
+  const Plan p = plan_flash(batch, heads_kv, G, tq, tk, num_sms);
+  const long long base = (long long)batch * heads_kv * p.m_blocks;
+  const int tiles = (int)(((long long)tk + kTile - 1) / kTile);
+  const int s = most_splits(base, tiles, num_sms);
+  const size_t rows = (size_t)batch * tq * heads_kv * G;
+  return kWsHeader + (s > 1 ? (size_t)s * rows * (kHeadDim + 1) * sizeof(float) : 0);
+}
 
-cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void*, int, cudaStream_t st) {
-  auto k = f16 ? (out_f32 ? flash_rows_kernel<true, true> : flash_rows_kernel<true, false>)
-               : (out_f32 ? flash_rows_kernel<false, true> : flash_rows_kernel<false, false>);
-  k<<<dim3(a.tq, a.heads_q, a.batch), 128, 0, st>>>(a);
-  return cudaGetLastError();
+cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, int num_sms, cudaStream_t st) {
+  const Plan plan = plan_flash(a.batch, a.heads_kv, a.G, a.tq, a.tk, num_sms);
+  FlashKernelArgs p;
+  memset(&p, 0, sizeof p);
+  p.a = a;
+  p.n_splits = plan.n_splits;
+  p.out_kind = out_f32 ? 2 : f16 ? 1 : 0;
+  p.part_rows = (long long)a.batch * a.tq * a.heads_q;
+  p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + kWsHeader);
+  p.part_lse = p.part_o + (size_t)plan.n_splits * p.part_rows * kHeadDim;
+  if (a.tk > 0) {
+    p.k_batch = a.k_b != 0, p.k_head = a.k_h != 0, p.v_batch = a.v_b != 0, p.v_head = a.v_h != 0;
+    const uint32_t box_q[3] = {(uint32_t)a.G, (uint32_t)(kTile / a.G), 1}, box_k[3] = {(uint32_t)kTile, 1, 1};
+    if (!encode_rows(&p.map_q, f16, a.q, {a.heads_q, a.tq, a.batch}, {a.q_h, a.q_t, a.q_b}, box_q) ||
+        !encode_rows(&p.map_k, f16, a.k, {a.tk, a.heads_kv, a.batch}, {a.k_t, a.k_h, a.k_b}, box_k) ||
+        !encode_rows(&p.map_v, f16, a.v, {a.tk, a.heads_kv, a.batch}, {a.v_t, a.v_h, a.v_b}, box_k))
+      return cudaErrorInvalidValue;
+  }
+  const dim3 grid(plan.m_blocks * plan.n_splits, a.heads_kv, a.batch);
+  cudaError_t e = f16 ? launch_flash_kernel<true>(p, plan.pair, grid, st) : launch_flash_kernel<false>(p, plan.pair, grid, st);
+  if (e != cudaSuccess || plan.n_splits == 1) return e;
+  const MergePartsArgs m = {a, p.part_o, p.part_lse, p.part_rows, plan.n_splits, p.out_kind};
+  return launch_chained(merge_parts_kernel, dim3((unsigned)((p.part_rows + 3) / 4)), dim3(128), 0, st, m);
 }
 
 }  // namespace mikv

@@ -1,0 +1,694 @@
+// mikv_flash.cuh — attention over bf16 / fp16 keys on the fifth-generation tensor cores (sm_103a): the kernel
+// template of the prompt and shared-prefix entry points. mikv_flash_bf16.cu and mikv_flash_f16.cu instantiate it for
+// one operand type each; mikv_flash.cu holds the work plan, the merge of split parts and the dispatch.
+//
+// Problem. `batch` sets of keys; each set is attended by tq tokens of G query heads per KV head (a prompt's tokens are
+// its positions, a shared prefix's tokens are its requests). The tq * G query rows of one KV head are packed into
+// tiles of 128 rows, row R = token * G + head, so that all heads and tokens that share keys share their loads.
+//
+// One CTA works on two streams, each with a score tile S (128 x 128 fp32) and an output tile O (128 x 128 fp32) in
+// TMEM, over 128-key tiles of K and V that TMA stages in a ring:
+//   PAIR    two row tiles (256 rows) over the same key tiles: a K or V tile is loaded once for both.
+//   !PAIR   one row tile (up to 128 rows) over alternating key tiles; the streams' results are joined at the end.
+//           The second stream's loads and softmax overlap the first's, which keeps HBM busy when rows are few.
+// Roles: warps 0-3 and 4-7 are the streams' softmax warpgroups (thread = row = TMEM lane), warp 8 issues the copies,
+// warp 9 the MMAs, warps 10-11 guard masked tiles (below). Per stream and tile: S = Q K^T (8 MMAs of K = 16), softmax
+// to P (16-bit, written over S in TMEM), O += P V (8 MMAs with A in TMEM). The MMA warp alternates streams, so one
+// stream's softmax runs under the other's products.
+//
+// Softmax. Weights are 2^(x - r) with x the score in log2 units and r a reference of the row: the largest x of the
+// first tile the row sees (less kRefDrop), moved only when a tile's sum of weights passes kSumMax, which rescales O. The
+// weights' 16-bit types hold that range without loss of relative precision, so most tiles need no maximum at all. Key
+// tiles are visited from the last to the first: with a causal mask or a distance bias the largest scores then
+// tend to come first. Sums are fp32 over the unrounded weights; rounding the weights to 16 bits is what the tensor
+// cores take, and perturbs each weight by at most half a unit in its last place.
+//
+// Masks. Every row sees one span of keys [lo, hi). Tiles outside the union of the CTA's spans are not visited; tiles
+// inside every span are not masked. In the tiles between, a weight of 0 does not stop an infinity or NaN in V from
+// entering O (0 * inf), so the guard warps look through the V tile first: rows with such a value are set to 0 and
+// their keys reported to the softmax threads, which mark the output rows that do see them.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <limits.h>
+#include <math.h>
+
+#include "mikv_device.cuh"
+#include "mikv_flash.h"
+#include "mikv_tcgen05.cuh"
+
+namespace mikv {
+
+template <bool F16>
+cudaError_t launch_flash_kernel(const FlashKernelArgs& p, bool pair, dim3 grid, cudaStream_t st);
+
+namespace flash {
+
+constexpr int kTile = 128;                     // query rows of a tile, keys of a tile
+constexpr int kTileBytes = kTile * kHeadDim * 2;
+constexpr int kHalfBytes = kTileBytes / 2;     // one 64-channel box
+constexpr int kSoftThreads = 256;
+constexpr int kCopyWarp = 8, kMmaWarp = 9, kGuardWarp = 10;
+constexpr int kThreads = 384;
+constexpr int kTmemCols = 512;                 // S0, S1, O0, O1
+constexpr int kVRing = 8;                      // guard results in flight (more than V tiles can be in the ring)
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <bool PAIR>
+struct Layout {
+  static constexpr int kQ = PAIR ? 2 : 1;          // query tiles in shared memory
+  static constexpr int kStages = PAIR ? 5 : 6;     // K / V tiles in the ring
+  static constexpr int kBars = 1 + 2 * kStages + 3 * 2 + kVRing + 1;
+  static constexpr int kSmem = 1024 + (kQ + kStages) * kTileBytes + 8 * kBars;
+  static_assert(kSmem <= 227 * 1024, "shared memory of one CTA");
+  uint32_t base;
+  __device__ uint32_t q(int m) const { return base + m * kTileBytes; }
+  __device__ uint32_t stage(int s) const { return base + (kQ + s) * kTileBytes; }
+  __device__ uint32_t bar(int i) const { return base + (kQ + kStages) * kTileBytes + 8 * i; }
+  __device__ uint32_t qfull() const { return bar(0); }
+  __device__ uint32_t full(int s) const { return bar(1 + s); }               // a copy landed
+  __device__ uint32_t empty(int s) const { return bar(1 + kStages + s); }    // its MMAs have read it
+  __device__ uint32_t sfull(int w) const { return bar(1 + 2 * kStages + w); }       // scores of stream w
+  __device__ uint32_t pready(int w) const { return bar(1 + 2 * kStages + 2 + w); }  // weights written (and O rescaled)
+  __device__ uint32_t odone(int w) const { return bar(1 + 2 * kStages + 4 + w); }   // O += P V done
+  __device__ uint32_t vsafe(int u) const { return bar(1 + 2 * kStages + 6 + u); }   // V tile u looked through
+  __device__ uint32_t drain() const { return bar(kBars - 1); }
+};
+
+// What the weights may grow to before the reference moves, and how far below the first tile's largest score the
+// reference starts (log2). bf16 weights have fp32's range, so the reference is that largest score and the sums
+// may grow far; fp16 weights hold 2^-24 .. 2^16, so they start at 2^8 and move before the sum can pass 2^16.
+template <bool F16>
+__device__ constexpr float ref_drop() { return F16 ? 8.f : 0.f; }
+template <bool F16>
+__device__ constexpr float sum_max() { return F16 ? 0x1.fep15f : 0x1p20f; }
+
+// Above this size of the reference, scores are rounded before it is taken off: the fused form keeps the product's
+// rounding error, up to 2^-24 of it, which would be a factor of the weights.
+constexpr float kRefExact = 0x1p22f;
+
+// The scores of one row in log2 units: x = cap(v * scale) - slope |pos - j|, times log2 e.
+struct Row {
+  int lo, hi;        // keys the row sees
+  float pos;         // its position, as far as the bias needs it (exact below 2^24)
+  float slope;       // slope of its head times log2 e
+};
+
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+struct Score {
+  float scale;     // uncapped: sm_scale log2 e; capped: 2 log2 e sm_scale / cap
+  float cap;       // cap log2 e
+};
+
+// 32 scores (columns col0 .. col0 + 31 of the tile at key k0) less `ref`, in place; masked ones become -inf.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ void row_scores(float (&v)[32], const Score& sc, const Row& row, int k0, int col0, float ref,
+                                           bool masked) {
+  if constexpr (!CAP && !BIAS) {
+    const uint64_t s2 = f32x2(sc.scale, sc.scale), r2 = f32x2(-ref, -ref);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) f32x2_split(fma_f32x2(f32x2(v[i], v[i + 1]), s2, r2), v[i], v[i + 1]);
+  } else {
+    const float e0 = (float)(k0 + col0) - row.pos;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      float r = -ref;
+      if constexpr (BIAS) r = fmaf(-row.slope, fabsf(e0 + (float)i), -ref);
+      if constexpr (CAP)  // tanh(y) = 1 - 2 / (1 + e^2y)
+        v[i] = fmaf(fmaf(-2.f, rcp_approx(1.f + fast_exp2(v[i] * sc.scale)), 1.f), sc.cap, r);
+      else
+        v[i] = fmaf(v[i], sc.scale, r);
+    }
+  }
+  if (masked) {
+    const int first = row.lo - k0 - col0, n = row.hi - row.lo;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if ((unsigned)(i - first) >= (unsigned)n) v[i] = -INFINITY;
+  }
+}
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack16(float a, float b) {
+  return F16 ? pack_f16(a, b) : pack_bf16(a, b);
+}
+
+// Whether one of the eight 16-bit values is an infinity or NaN (its exponent bits all ones).
+template <bool F16>
+__device__ __forceinline__ bool any_nonfinite(const uint4& x) {
+  constexpr uint32_t one = F16 ? 0x04000400u : 0x00800080u;  // carries into the sign bit from an all-ones exponent
+  const uint32_t r = ((x.x & 0x7FFF7FFFu) + one) | ((x.y & 0x7FFF7FFFu) + one) | ((x.z & 0x7FFF7FFFu) + one) |
+                     ((x.w & 0x7FFF7FFFu) + one);
+  return (r & 0x80008000u) != 0;
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 r;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr)
+               : "memory");
+  return r;
+}
+__device__ __forceinline__ void sts128_zero(uint32_t addr) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0u) : "memory");
+}
+
+// S (128 x 128) = query tile x key tile^T.
+template <bool F16>
+__device__ __forceinline__ void mma_scores(uint32_t d, uint32_t q, uint32_t k) {
+  constexpr uint32_t idesc = umma_idesc_16(F16, kTile, kTile, false);
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) {
+    const uint32_t off = (ks >> 2) * kHalfBytes + (ks & 3) * 32;
+    umma_bf16(d, umma_desc_sw128(q + off), umma_desc_sw128(k + off), idesc, ks > 0 ? 1u : 0u);
+  }
+}
+
+// O (128 x 128) += P (TMEM, 128 x 128) x V tile.
+template <bool F16>
+__device__ __forceinline__ void mma_values(uint32_t d, uint32_t p, uint32_t v, bool accumulate) {
+  constexpr uint32_t idesc = umma_idesc_16(F16, kTile, kTile, true);
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks)
+    umma_16_ts(d, p + 8 * ks, umma_desc_rows_sw128(v + ks * 16 * 128, kHalfBytes), idesc,
+               (ks > 0 || accumulate) ? 1u : 0u);
+}
+
+// Four packed outputs at element i of an output row (16-byte stores for a caller that walks 8 / 4 elements).
+__device__ __forceinline__ void store_out8(void* row, int out_kind, int i, const float* v) {
+  if (out_kind == 2) {
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + i);
+    o[0] = make_float4(v[0], v[1], v[2], v[3]);
+    o[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else if (out_kind == 1) {
+    *reinterpret_cast<uint4*>(static_cast<__half*>(row) + i) =
+        make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+  } else {
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(row) + i) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  }
+}
+
+__device__ __forceinline__ void store_stat(const FlashArgs& a, long long i, float lse2) {
+  if (!a.stat) return;
+  if (a.stat_pair) {
+    a.stat[2 * i] = lse2 * kLn2;
+    a.stat[2 * i + 1] = lse2 == -INFINITY ? 0.f : 1.f;
+  } else {
+    a.stat[i] = lse2 * kLn2;
+  }
+}
+
+// Join of a part (log2 of its sum: lse2) with the request's own part: factors of both outputs, and the joint lse2.
+__device__ __forceinline__ void join_own(const FlashArgs& a, size_t row, float& lse2, float& f0, float& f1) {
+  const float m = a.own_ml[2 * row], l = a.own_ml[2 * row + 1];
+  const float mine = l == 0.f ? -INFINITY : fmaf(m, kLog2e, log2f(l));
+  f1 = 0.f;
+  if (mine == -INFINITY) return;
+  const float top = fmaxf(lse2, mine);
+  const float w0 = fast_exp2(lse2 - top), w1 = fast_exp2(mine - top), inv = 1.f / (w0 + w1);
+  f0 *= w0 * inv;
+  f1 = w1 * inv;
+  lse2 = top + log2f(w0 + w1);
+}
+
+template <bool F16, bool PAIR, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constant__ FlashKernelArgs p) {
+  using L = Layout<PAIR>;
+  const FlashArgs& a = p.a;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_fail;
+  __shared__ int s_range[8][4];
+  __shared__ uint32_t s_bad[kVRing][4];  // keys of a guarded V tile that hold infinities or NaN
+  __shared__ float s_join[2][kTile];     // !PAIR: the second stream's reference and sum
+  __shared__ int s_join_bad[kTile];
+  volatile int* fail = &s_fail;
+  L sm;
+  sm.base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int split = blockIdx.x % p.n_splits;
+  const int m_blocks = gridDim.x / p.n_splits;
+  const int m_block = m_blocks - 1 - (int)(blockIdx.x / p.n_splits);  // a causal prompt's longest rows first
+
+  if (tid == 0) {
+    s_fail = 0;
+    mbar_init(sm.qfull(), 1);
+    for (int s = 0; s < L::kStages; ++s) {
+      mbar_init(sm.full(s), 1);
+      mbar_init(sm.empty(s), 1);
+    }
+    for (int w = 0; w < 2; ++w) {
+      mbar_init(sm.sfull(w), 1);
+      mbar_init(sm.pready(w), 4);  // one arrival per softmax warp
+      mbar_init(sm.odone(w), 1);
+    }
+    for (int u = 0; u < kVRing; ++u) mbar_init(sm.vsafe(u), 2);
+    mbar_init(sm.drain(), 1);
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), kTmemCols);
+
+  // this thread's row (softmax threads), and what the rows of each tile see
+  const int stream = (warp >> 2) & 1, r = tid & (kTile - 1);
+  const int R = (PAIR ? (2 * m_block + stream) : m_block) * kTile + r;
+  const int token = R / a.G, head = h * a.G + R % a.G;
+  const bool valid = warp < kCopyWarp && token < a.tq;
+  Row row;
+  row.lo = row.hi = 0;
+  row.pos = 0.f;
+  row.slope = 0.f;
+  if (warp < kCopyWarp) {
+    if (valid) {
+      int len = a.tk;
+      row.hi = a.tk;
+      if (a.lens) len = row.hi = max(0, min(a.lens[b], a.tk));
+      if (a.spans) {
+        const int2 s = a.spans[(size_t)b * a.tq + token];
+        row.lo = max(s.x, 0);
+        row.hi = min(s.y, a.tk);
+      } else if (a.causal) {
+        row.hi = (int)min((long long)a.tk, max(0ll, (long long)a.q_start + token + 1));
+      }
+      if constexpr (BIAS) {
+        row.pos = (float)(a.pos ? a.pos[(size_t)b * a.tq + token] : a.pos_at_len ? len : a.q_start + token);
+        row.slope = a.slopes[head] * kLog2e;
+      }
+      if (row.hi <= row.lo) row.lo = row.hi = 0;
+    }
+    const bool sees = row.hi > row.lo;
+    const int lo = __reduce_min_sync(0xffffffffu, sees ? row.lo : INT_MAX);
+    const int hi = __reduce_max_sync(0xffffffffu, row.hi);
+    const int all_lo = __reduce_max_sync(0xffffffffu, !valid ? 0 : sees ? row.lo : INT_MAX);
+    const int all_hi = __reduce_min_sync(0xffffffffu, !valid ? INT_MAX : row.hi);
+    if (lane == 0) {
+      s_range[warp][0] = lo;
+      s_range[warp][1] = hi;
+      s_range[warp][2] = all_lo;
+      s_range[warp][3] = all_hi;
+    }
+  }
+  tcgen05_before_sync();
+  __syncthreads();
+  tcgen05_after_sync();
+  const uint32_t tmem = s_tmem;
+  // per stream: key tiles [t0, t1) that some row sees, keys [all_lo, all_hi) that every row sees
+  int t0[2], t1[2], all_lo[2], all_hi[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    int lo = INT_MAX, hi = 0;
+    all_lo[w] = 0;
+    all_hi[w] = INT_MAX;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo = min(lo, s_range[4 * w + i][0]);
+      hi = max(hi, s_range[4 * w + i][1]);
+      all_lo[w] = max(all_lo[w], s_range[4 * w + i][2]);
+      all_hi[w] = min(all_hi[w], s_range[4 * w + i][3]);
+    }
+    t0[w] = hi > 0 ? lo / kTile : INT_MAX;
+    t1[w] = (hi + kTile - 1) / kTile;
+  }
+  // this CTA's share of the union of both streams' tiles
+  int T0 = min(t0[0], t0[1]), T1 = max(t1[0], t1[1]);
+  if (T1 == 0) T0 = 0;
+  if (p.n_splits > 1) {
+    const int chunk = (T1 - T0 + p.n_splits - 1) / p.n_splits;
+    T0 = min(T1, T0 + split * chunk);
+    T1 = min(T1, T0 + chunk);
+  }
+  const int n = T1 - T0;
+  const int n_w[2] = {(n + 1) / 2, n / 2};  // !PAIR: tiles of each stream
+  auto active = [&](int w, int j) { return j >= t0[w] && j < t1[w]; };
+  auto cut = [&](int w, int j) { return j * kTile < all_lo[w] || (j + 1) * kTile > all_hi[w]; };
+  auto guarded = [&](int j) { return PAIR ? (active(0, j) && cut(0, j)) || (active(1, j) && cut(1, j)) : cut(0, j); };
+
+  if (warp == kCopyWarp) {
+    if (lane == 0 && n > 0) {
+      int last[L::kStages];
+      for (int s = 0; s < L::kStages; ++s) last[s] = -1;
+      mbar_arrive_expect_tx(sm.qfull(), L::kQ * kTileBytes);
+#pragma unroll
+      for (int m = 0; m < L::kQ; ++m) {
+        const int tok0 = (PAIR ? 2 * m_block + m : m_block) * (kTile / a.G);
+        tma_load_4d(sm.q(m), &p.map_q, 0, h * a.G, tok0, b, sm.qfull());
+        tma_load_4d(sm.q(m) + kHalfBytes, &p.map_q, 64, h * a.G, tok0, b, sm.qfull());
+      }
+      int c = 0;
+      auto load = [&](const CUtensorMap* map, int j, int hm, int bm) {
+        const int s = c % L::kStages;
+        if (c >= L::kStages && !mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail)) return false;
+        mbar_arrive_expect_tx(sm.full(s), kTileBytes);
+        tma_load_4d(sm.stage(s), map, 0, j * kTile, h * hm, b * bm, sm.full(s));
+        tma_load_4d(sm.stage(s) + kHalfBytes, map, 64, j * kTile, h * hm, b * bm, sm.full(s));
+        last[s] = c++;
+        return true;
+      };
+      auto load_k = [&](int j) { return load(&p.map_k, j, p.k_head, p.k_batch); };
+      auto load_v = [&](int j) { return load(&p.map_v, j, p.v_head, p.v_batch); };
+      bool ok = load_k(T1 - 1);
+      if constexpr (PAIR) {
+        for (int i = 0; ok && i < n; ++i) ok = load_v(T1 - 1 - i) && (i + 1 >= n || load_k(T1 - 2 - i));
+      } else {
+        if (ok && n > 1) ok = load_k(T1 - 2);
+        for (int i = 0; ok && i < n_w[0]; ++i)
+          for (int w = 0; ok && w < 2; ++w)
+            if (i < n_w[w]) {
+              const int j = T1 - 1 - (2 * i + w);
+              ok = load_v(j) && (i + 1 >= n_w[w] || load_k(j - 2));
+            }
+      }
+      if (*fail) {  // no copy may outlive the CTA
+        if (!mbar_wait(sm.qfull(), 0)) record_error(a.status, kErrDrainTimeout);
+        for (int s = 0; s < L::kStages; ++s)
+          if (last[s] >= 0 && !mbar_wait(sm.full(s), (last[s] / L::kStages) & 1)) record_error(a.status, kErrDrainTimeout);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    if (lane == 0 && n > 0) {
+      int done[2] = {0, 0};  // weights consumed per stream
+      auto wait_full = [&](int c) {
+        const bool ok = mbar_wait_role(sm.full(c % L::kStages), (c / L::kStages) & 1, fail);
+        tcgen05_after_sync();
+        return ok;
+      };
+      auto scores = [&](int w, int c) {
+        mma_scores<F16>(tmem + 128 * w, sm.q(PAIR ? w : 0), sm.stage(c % L::kStages));
+        umma_commit(sm.sfull(w));
+      };
+      auto values = [&](int w, int c) {
+        if (!mbar_wait_role(sm.pready(w), done[w] & 1, fail)) return false;
+        tcgen05_after_sync();
+        mma_values<F16>(tmem + 256 + 128 * w, tmem + 128 * w, sm.stage(c % L::kStages), done[w] > 0);
+        umma_commit(sm.odone(w));
+        ++done[w];
+        return true;
+      };
+      auto wait_safe = [&](int u) { return mbar_wait_role(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail); };
+      bool ok = mbar_wait_role(sm.qfull(), 0, fail) && wait_full(0);
+      if constexpr (PAIR) {
+        if (ok) {
+          for (int w = 0; w < 2; ++w)
+            if (active(w, T1 - 1)) scores(w, 0);
+          umma_commit(sm.empty(0));
+        }
+        for (int i = 0; ok && i < n; ++i) {
+          const int j = T1 - 1 - i, cv = 2 * i + 1, ck = cv + 1;
+          ok = wait_full(cv) && (!guarded(j) || wait_safe(i));
+          for (int w = 0; ok && w < 2; ++w) {
+            if (active(w, j)) ok = values(w, cv);
+            if (ok && i + 1 < n) {
+              if (w == 0) ok = wait_full(ck);
+              if (ok && active(w, j - 1)) scores(w, ck);
+            }
+          }
+          if (ok) {
+            umma_commit(sm.empty(cv % L::kStages));
+            if (i + 1 < n) umma_commit(sm.empty(ck % L::kStages));
+          }
+        }
+      } else {
+        int c = 0;
+        for (int w = 0; ok && w < 2; ++w)
+          if (w < n) {
+            if (w == 1) ok = wait_full(1);
+            if (ok) {
+              scores(w, c);
+              umma_commit(sm.empty(c));
+              ++c;
+            }
+          }
+        for (int i = 0; ok && i < n_w[0]; ++i)
+          for (int w = 0; ok && w < 2; ++w)
+            if (i < n_w[w]) {
+              ok = wait_full(c) && (!guarded(T1 - 1 - (2 * i + w)) || wait_safe(2 * i + w)) && values(w, c);
+              if (!ok) break;
+              umma_commit(sm.empty(c % L::kStages));
+              ++c;
+              if (i + 1 < n_w[w]) {
+                ok = wait_full(c);
+                if (!ok) break;
+                scores(w, c);
+                umma_commit(sm.empty(c % L::kStages));
+                ++c;
+              }
+            }
+      }
+      umma_commit(sm.drain());  // every MMA issued has completed once this arrives
+      if (!mbar_wait(sm.drain(), 0)) record_error(a.status, kErrDrainTimeout);
+    }
+  } else if (warp >= kGuardWarp) {
+    int c = PAIR ? 1 : min(n, 2);  // ring position of V tile u
+    for (int u = 0; u < n; ++u) {
+      const int s = c % L::kStages, j = T1 - 1 - u;
+      if (!__all_sync(0xffffffffu, mbar_wait_role(sm.full(s), (c / L::kStages) & 1, fail))) break;
+      if (guarded(j)) {
+        const int g = warp - kGuardWarp;
+        bool wrote = false;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          const int key = 64 * part + 32 * g + lane;
+          const uint32_t at = sm.stage(s) + key * 128;
+          bool bad = false;
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            bad = bad || any_nonfinite<F16>(lds128(at + (q >> 3) * kHalfBytes + (((q & 7) ^ (key & 7)) << 4)));
+          const uint32_t bits = __ballot_sync(0xffffffffu, bad);
+          if (bad) {
+            for (int q = 0; q < 16; ++q) sts128_zero(at + (q >> 3) * kHalfBytes + ((q & 7) << 4));
+            wrote = true;
+          }
+          if (lane == 0) s_bad[u % kVRing][2 * part + g] = bits;
+        }
+        if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
+      if (lane == 0) mbar_arrive(sm.vsafe(u % kVRing));
+      // to V tile u + 1: past the K tiles that are loaded between
+      c += PAIR ? 2 : 1 + (u / 2 + 1 < n_w[u & 1] ? 1 : 0);
+    }
+  } else {  // softmax warps
+    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+    const uint32_t ts = tmem + 128 * stream + lanes, to = tmem + 256 + 128 * stream + lanes;
+    Score sc;
+    sc.scale = CAP ? 2.f * kLog2e * (a.sm_scale / a.softcap) : a.sm_scale * kLog2e;
+    sc.cap = a.softcap * kLog2e;
+    float ref = -INFINITY, sum = 0.f;
+    bool bad_row = false, ok = true, exact_ref = false;
+    int it = 0;
+    for (int i = 0; i < (PAIR ? n : n_w[stream]); ++i) {
+      const int j = T1 - 1 - (PAIR ? i : 2 * i + stream);
+      if (PAIR && !active(stream, j)) continue;
+      const int k0 = j * kTile;
+      const bool masked = cut(PAIR ? stream : 0, j);
+      ok = __all_sync(0xffffffffu, mbar_wait_role(sm.sfull(stream), it & 1, fail));
+      if (!ok) break;
+      tcgen05_after_sync();
+      uint32_t w[64];
+      float tile_sum;
+      bool low = ref == -INFINITY;  // the row has no reference yet, or one that proved too low
+      for (bool again = false;; again = true) {
+        if (__any_sync(0xffffffffu, low)) {
+          float mx = -INFINITY;  // the row's largest score of this tile
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            float v[32];
+            tmem_ld32(ts + 32 * c, v);
+            tmem_wait_ld(v);
+            row_scores<CAP, BIAS>(v, sc, row, k0, 32 * c, 0.f, masked);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) mx = fmaxf(mx, v[e]);
+          }
+          const float next = low ? fmaxf(ref, mx - ref_drop<F16>()) : ref;
+          const bool moves = next != ref && ref != -INFINITY;
+          if (__any_sync(0xffffffffu, moves)) {
+            const float f = moves ? fast_exp2(ref - next) : 1.f;
+            if (it > 0) {
+              ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream), (it - 1) & 1, fail));
+              if (!ok) break;
+              tcgen05_after_sync();
+#pragma unroll 1
+              for (int c = 0; c < 4; ++c) {
+                float v[32];
+                tmem_ld32(to + 32 * c, v);
+                tmem_wait_ld(v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] *= f;
+                tmem_st32(to + 32 * c, reinterpret_cast<const uint32_t*>(v));
+              }
+            }
+            sum *= f;
+          }
+          ref = next;
+          exact_ref = fabsf(ref) > kRefExact && ref != -INFINITY;
+        }
+        const float rr = ref == -INFINITY || exact_ref ? 0.f : ref;
+        const bool some_exact = __any_sync(0xffffffffu, exact_ref);
+        uint64_t acc[2] = {0ull, 0ull};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float v[32];
+          tmem_ld32(ts + 32 * c, v);
+          tmem_wait_ld(v);
+          row_scores<CAP, BIAS>(v, sc, row, k0, 32 * c, rr, masked);
+          if (some_exact) {
+            const float rest = exact_ref ? ref : 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] -= rest;
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float x = fast_exp2(v[e]), y = fast_exp2(v[e + 1]);
+            acc[(e >> 1) & 1] = add_f32x2(acc[(e >> 1) & 1], f32x2(x, y));
+            w[16 * c + (e >> 1)] = pack16<F16>(x, y);
+          }
+        }
+        float s0, s1, s2, s3;
+        f32x2_split(acc[0], s0, s1);
+        f32x2_split(acc[1], s2, s3);
+        tile_sum = (s0 + s1) + (s2 + s3);
+        low = !(tile_sum <= sum_max<F16>());  // (stays so for a NaN: one more attempt, then it is kept)
+        if (again || !__any_sync(0xffffffffu, low)) break;
+      }
+      if (!ok) break;
+      sum += tile_sum;
+      tmem_st32(ts, w);
+      tmem_st32(ts + 32, w + 32);
+      if (guarded(j)) {
+        const int u = T1 - 1 - j;
+        ok = __all_sync(0xffffffffu, mbar_wait_role(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail));
+        if (!ok) break;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t bits = s_bad[u % kVRing][q];
+          while (bits) {
+            const int key = k0 + 32 * q + __ffs(bits) - 1;
+            bits &= bits - 1;
+            bad_row = bad_row || (key >= row.lo && key < row.hi);
+          }
+        }
+      }
+      tmem_wait_st();
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sm.pready(stream));
+      ++it;
+    }
+    if (ok && it > 0) {
+      ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream), (it - 1) & 1, fail));
+      tcgen05_after_sync();
+    }
+    float g0 = 1.f, g1 = 0.f;  // factors of this stream's and the other stream's O
+    const float* other = reinterpret_cast<const float*>(smem_raw + (sm.stage(0) - smem_u32(smem_raw))) + r;
+    if constexpr (!PAIR) {  // the second stream hands its part over through the (now unused) ring
+      named_bar_sync(1, kSoftThreads);  // every MMA of both streams is done
+      if (stream == 1) {
+        s_join[0][r] = it > 0 ? ref : -INFINITY;
+        s_join[1][r] = it > 0 ? sum : 0.f;
+        s_join_bad[r] = bad_row;
+        if (ok && it > 0) {
+          float* to_first = const_cast<float*>(other);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float v[32];
+            tmem_ld32(to + 32 * c, v);
+            tmem_wait_ld(v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) to_first[(32 * c + e) * kTile] = v[e];
+          }
+        }
+      }
+      named_bar_sync(1, kSoftThreads);
+      if (stream == 0) {
+        const float r1 = s_join[0][r], l1 = s_join[1][r];
+        bad_row = bad_row || s_join_bad[r];
+        const float top = fmaxf(ref, r1);
+        if (top > -INFINITY) {
+          g0 = fast_exp2(ref - top);
+          g1 = fast_exp2(r1 - top);
+        }
+        sum = sum * g0 + l1 * g1;
+        ref = top;
+      }
+    }
+    if ((PAIR || stream == 0) && ok && !*fail) {
+      const size_t out_row = ((size_t)b * a.tq + token) * a.heads_q + head;
+      float lse2 = sum == 0.f ? -INFINITY : ref + log2f(sum);
+      float f0 = sum == 0.f ? 0.f : 1.f / sum, f1 = 0.f;
+      const bool last = p.n_splits == 1;
+      if (last && a.own_out && valid) join_own(a, out_row, lse2, f0, f1);
+      if (bad_row) f0 = __int_as_float(0x7fffffff);
+      g0 *= f0;
+      g1 *= f0;
+      // (a row whose sum is 0 has seen nothing, or only scores of -inf: its O holds zeros or, never written, anything)
+      const bool blank = f0 == 0.f;
+      const bool other_ran = !PAIR && n_w[1] > 0;
+      char* dst = last ? static_cast<char*>(a.out) +
+                             (b * a.o_b + head * a.o_h + token * a.o_t) * (p.out_kind == 2 ? 4 : 2)
+                       : reinterpret_cast<char*>(p.part_o + ((size_t)split * p.part_rows + out_row) * kHeadDim);
+      const float* own = a.own_out + out_row * kHeadDim;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float v[32];
+        if (it > 0) {
+          tmem_ld32(to + 32 * c, v);
+          tmem_wait_ld(v);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          v[e] = blank ? 0.f : v[e] * g0;
+          if (other_ran && !blank) v[e] = fmaf(other[(32 * c + e) * kTile], g1, v[e]);
+        }
+        if (valid) {
+          if (f1 != 0.f) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 o = *reinterpret_cast<const float4*>(own + 32 * c + e);
+              v[e] = fmaf(o.x, f1, v[e]);
+              v[e + 1] = fmaf(o.y, f1, v[e + 1]);
+              v[e + 2] = fmaf(o.z, f1, v[e + 2]);
+              v[e + 3] = fmaf(o.w, f1, v[e + 3]);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) store_out8(dst, last ? p.out_kind : 2, 32 * c + e, v + e);
+        }
+      }
+      if (valid) {
+        if (last)
+          store_stat(a, b * a.s_b + head * a.s_h + token * a.s_t, lse2);
+        else
+          p.part_lse[(size_t)split * p.part_rows + out_row] = lse2;
+      }
+    }
+  }
+  tcgen05_before_sync();
+  __syncthreads();
+  if (s_fail && tid == 0) record_error(a.status, kErrFullTimeout);
+  if (warp == kMmaWarp) {
+    __syncwarp();
+    tcgen05_after_sync();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+template <bool F16, bool PAIR>
+cudaError_t launch_variant(const FlashKernelArgs& p, dim3 grid, cudaStream_t st) {
+  const bool cap = p.a.softcap > 0.f, bias = p.a.slopes != nullptr;
+  auto k = cap ? (bias ? flash_kernel<F16, PAIR, true, true> : flash_kernel<F16, PAIR, true, false>)
+               : (bias ? flash_kernel<F16, PAIR, false, true> : flash_kernel<F16, PAIR, false, false>);
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<PAIR>::kSmem);
+  if (e != cudaSuccess) return e;
+  k<<<grid, kThreads, Layout<PAIR>::kSmem, st>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace flash
+}  // namespace mikv

@@ -33,6 +33,19 @@ struct FlashArgs {
   int* status;
 };
 
+// What the tensor-core kernel takes: the problem, its tensor maps, and its share of the work plan.
+struct FlashKernelArgs {
+  CUtensorMap map_q;    // [batch][tokens][heads][128], box 64 channels x G heads x 128 / G tokens, 128B swizzle
+  CUtensorMap map_k, map_v;  // [batch][heads][keys][128], box 64 channels x 128 keys
+  FlashArgs a;
+  int k_batch, k_head, v_batch, v_head;  // 1, or 0 where the dimension is shared (zero stride)
+  int n_splits;         // CTAs that share a row tile's keys; their parts are merged
+  int out_kind;         // 0 bf16, 1 fp16, 2 fp32
+  float* part_o;        // [n_splits][part_rows][128] normalised outputs, row = (set * tq + token) * heads_q + head
+  float* part_lse;      // [n_splits][part_rows] log2 of the sum of 2^x (-inf: nothing seen)
+  long long part_rows;
+};
+
 size_t flash_workspace_bytes(int batch, int heads_kv, int G, int tq, int tk, int num_sms);
 cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, int num_sms, cudaStream_t st);
 
