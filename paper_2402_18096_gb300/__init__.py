@@ -87,6 +87,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     """Load libmikv.so (building it with nvcc first when it is missing or stale). With MIKV_DEBUG=1 in the
     environment the checked build (libmikv_debug.so, -DMIKV_DEBUG) is loaded instead."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             debug = os.environ.get("MIKV_DEBUG", "") == "1"

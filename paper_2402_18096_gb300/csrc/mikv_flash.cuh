@@ -34,6 +34,8 @@
 #include <limits.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "mikv_device.cuh"
 #include "mikv_flash.h"
 #include "mikv_tcgen05.cuh"
@@ -96,39 +98,81 @@ struct Row {
   float slope;       // slope of its head times log2 e
 };
 
-__device__ __forceinline__ float rcp_approx(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 struct Score {
   float scale;     // uncapped: sm_scale log2 e; capped: 2 log2 e sm_scale / cap
   float cap;       // cap log2 e
 };
 
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {  // NaN if either is
+  float y;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// The cap of four scores: cap tanh(y) + rest = (cap + rest) - 2 cap / (1 + e^2y). One reciprocal serves all four:
+// with p = (ac, bd) of the denominators a, b, c, d, 1 / a = bd c / (ac bd) and so on. 2^30 stands for larger
+// exponentials (tanh is then 1 to fp32 precision), which keeps the product of four inside fp32.
+__device__ __forceinline__ void cap_four(float* v, float scale, float cap, const float (&rest)[4]) {
+  const uint64_t s2 = f32x2(scale, scale), one = f32x2(1.f, 1.f), c2 = f32x2(-2.f * cap, -2.f * cap);
+  float y[4];
+  f32x2_split(mul_f32x2(f32x2(v[0], v[1]), s2), y[0], y[1]);
+  f32x2_split(mul_f32x2(f32x2(v[2], v[3]), s2), y[2], y[3]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = fast_exp2(min_nan(y[i], 30.f));
+  const uint64_t ab = add_f32x2(f32x2(y[0], y[1]), one), cd = add_f32x2(f32x2(y[2], y[3]), one);
+  float ac, bd;
+  f32x2_split(mul_f32x2(ab, cd), ac, bd);
+  const float r = rcp_approx(ac * bd);
+  const uint64_t s = mul_f32x2(f32x2(r, r), f32x2(bd, ac));
+  f32x2_split(fma_f32x2(mul_f32x2(s, cd), c2, f32x2(rest[0], rest[1])), v[0], v[1]);
+  f32x2_split(fma_f32x2(mul_f32x2(s, ab), c2, f32x2(rest[2], rest[3])), v[2], v[3]);
+}
+
 // 32 scores (columns col0 .. col0 + 31 of the tile at key k0) less `ref`, in place; masked ones become -inf.
+// side: every key of the tile lies at or before every position of the warp (-1), at or after them (1), or neither (0).
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ void row_scores(float (&v)[32], const Score& sc, const Row& row, int k0, int col0, float ref,
-                                           bool masked) {
-  if constexpr (!CAP && !BIAS) {
-    const uint64_t s2 = f32x2(sc.scale, sc.scale), r2 = f32x2(-ref, -ref);
+                                           bool masked, int side) {
+  const int first = row.lo - k0 - col0, n = row.hi - row.lo;
+  if constexpr (CAP) {
+    if (masked) {  // what a masked key holds must not reach its neighbours through the shared reciprocal
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) f32x2_split(fma_f32x2(f32x2(v[i], v[i + 1]), s2, r2), v[i], v[i + 1]);
+      for (int i = 0; i < 32; ++i)
+        if ((unsigned)(i - first) >= (unsigned)n) v[i] = 0.f;
+    }
+  }
+  const float rest = (CAP ? sc.cap : 0.f) - ref;
+  auto apply = [&](auto bias) {  // bias(i): the bias of column i, plus `rest`
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      const float b[4] = {bias(i), bias(i + 1), bias(i + 2), bias(i + 3)};
+      if constexpr (CAP) {
+        cap_four(v + i, sc.scale, sc.cap, b);
+      } else {
+        const uint64_t s2 = f32x2(sc.scale, sc.scale);
+        f32x2_split(fma_f32x2(f32x2(v[i], v[i + 1]), s2, f32x2(b[0], b[1])), v[i], v[i + 1]);
+        f32x2_split(fma_f32x2(f32x2(v[i + 2], v[i + 3]), s2, f32x2(b[2], b[3])), v[i + 2], v[i + 3]);
+      }
+    }
+  };
+  if constexpr (!BIAS) {
+    apply([&](int) { return rest; });
   } else {
     const float e0 = (float)(k0 + col0) - row.pos;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      float r = -ref;
-      if constexpr (BIAS) r = fmaf(-row.slope, fabsf(e0 + (float)i), -ref);
-      if constexpr (CAP)  // tanh(y) = 1 - 2 / (1 + e^2y)
-        v[i] = fmaf(fmaf(-2.f, rcp_approx(1.f + fast_exp2(v[i] * sc.scale)), 1.f), sc.cap, r);
-      else
-        v[i] = fmaf(v[i], sc.scale, r);
+    if (side != 0) {  // the bias is linear over the tile
+      const float sl = side < 0 ? row.slope : -row.slope;
+      const float base = fmaf(sl, e0, rest);
+      apply([&](int i) { return fmaf(sl, (float)i, base); });
+    } else {
+      apply([&](int i) { return fmaf(-row.slope, fabsf(e0 + (float)i), rest); });
     }
   }
   if (masked) {
-    const int first = row.lo - k0 - col0, n = row.hi - row.lo;
 #pragma unroll
     for (int i = 0; i < 32; ++i)
       if ((unsigned)(i - first) >= (unsigned)n) v[i] = -INFINITY;
@@ -255,6 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     fence_mbar_init();
   }
   if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), kTmemCols);
+  if (p.n_splits > 1) allow_dependent_launch();  // the merge may be scheduled; it waits for this grid's end
 
   // this thread's row (softmax threads), and what the rows of each tile see
   const int stream = (warp >> 2) & 1, r = tid & (kTile - 1);
@@ -265,7 +310,9 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   row.lo = row.hi = 0;
   row.pos = 0.f;
   row.slope = 0.f;
+  int warp_lo = INT_MAX, warp_hi = 0, warp_all_lo = 0, warp_all_hi = 0, pos_min = 0, pos_max = 0;
   if (warp < kCopyWarp) {
+    int at = 0;
     if (valid) {
       int len = a.tk;
       row.hi = a.tk;
@@ -278,21 +325,26 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         row.hi = (int)min((long long)a.tk, max(0ll, (long long)a.q_start + token + 1));
       }
       if constexpr (BIAS) {
-        row.pos = (float)(a.pos ? a.pos[(size_t)b * a.tq + token] : a.pos_at_len ? len : a.q_start + token);
+        at = a.pos ? a.pos[(size_t)b * a.tq + token] : a.pos_at_len ? len : a.q_start + token;
+        row.pos = (float)at;
         row.slope = a.slopes[head] * kLog2e;
       }
       if (row.hi <= row.lo) row.lo = row.hi = 0;
     }
     const bool sees = row.hi > row.lo;
-    const int lo = __reduce_min_sync(0xffffffffu, sees ? row.lo : INT_MAX);
-    const int hi = __reduce_max_sync(0xffffffffu, row.hi);
-    const int all_lo = __reduce_max_sync(0xffffffffu, !valid ? 0 : sees ? row.lo : INT_MAX);
-    const int all_hi = __reduce_min_sync(0xffffffffu, !valid ? INT_MAX : row.hi);
+    warp_lo = __reduce_min_sync(0xffffffffu, sees ? row.lo : INT_MAX);
+    warp_hi = __reduce_max_sync(0xffffffffu, row.hi);
+    warp_all_lo = __reduce_max_sync(0xffffffffu, !valid ? 0 : sees ? row.lo : INT_MAX);
+    warp_all_hi = __reduce_min_sync(0xffffffffu, !valid ? INT_MAX : row.hi);
+    if (BIAS) {
+      pos_min = __reduce_min_sync(0xffffffffu, valid ? at : INT_MAX);
+      pos_max = __reduce_max_sync(0xffffffffu, valid ? at : INT_MIN);
+    }
     if (lane == 0) {
-      s_range[warp][0] = lo;
-      s_range[warp][1] = hi;
-      s_range[warp][2] = all_lo;
-      s_range[warp][3] = all_hi;
+      s_range[warp][0] = warp_lo;
+      s_range[warp][1] = warp_hi;
+      s_range[warp][2] = warp_all_lo;
+      s_range[warp][3] = warp_all_hi;
     }
   }
   tcgen05_before_sync();
@@ -326,155 +378,161 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   }
   const int n = T1 - T0;
   const int n_w[2] = {(n + 1) / 2, n / 2};  // !PAIR: tiles of each stream
-  auto active = [&](int w, int j) { return j >= t0[w] && j < t1[w]; };
-  auto cut = [&](int w, int j) { return j * kTile < all_lo[w] || (j + 1) * kTile > all_hi[w]; };
+  auto of = [](const int(&x)[2], int w) { return w ? x[1] : x[0]; };
+  auto active = [&](int w, int j) { return j >= of(t0, w) && j < of(t1, w); };
+  auto cut = [&](int w, int j) { return j * kTile < of(all_lo, w) || (j + 1) * kTile > of(all_hi, w); };
   auto guarded = [&](int j) { return PAIR ? (active(0, j) && cut(0, j)) || (active(1, j) && cut(1, j)) : cut(0, j); };
 
-  if (warp == kCopyWarp) {
-    if (lane == 0 && n > 0) {
-      int last[L::kStages];
-      for (int s = 0; s < L::kStages; ++s) last[s] = -1;
-      mbar_arrive_expect_tx(sm.qfull(), L::kQ * kTileBytes);
+  // The softmax warps take the registers the other warpgroup does not need: 256 x 216 + 128 x 72 = 384 x 168.
+  if (warp >= kCopyWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == kCopyWarp) {
+      if (lane == 0 && n > 0) {
+        int last[L::kStages];
+        for (int s = 0; s < L::kStages; ++s) last[s] = -1;
+        mbar_arrive_expect_tx(sm.qfull(), L::kQ * kTileBytes);
 #pragma unroll
-      for (int m = 0; m < L::kQ; ++m) {
-        const int tok0 = (PAIR ? 2 * m_block + m : m_block) * (kTile / a.G);
-        tma_load_4d(sm.q(m), &p.map_q, 0, h * a.G, tok0, b, sm.qfull());
-        tma_load_4d(sm.q(m) + kHalfBytes, &p.map_q, 64, h * a.G, tok0, b, sm.qfull());
-      }
-      int c = 0;
-      auto load = [&](const CUtensorMap* map, int j, int hm, int bm) {
-        const int s = c % L::kStages;
-        if (c >= L::kStages && !mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail)) return false;
-        mbar_arrive_expect_tx(sm.full(s), kTileBytes);
-        tma_load_4d(sm.stage(s), map, 0, j * kTile, h * hm, b * bm, sm.full(s));
-        tma_load_4d(sm.stage(s) + kHalfBytes, map, 64, j * kTile, h * hm, b * bm, sm.full(s));
-        last[s] = c++;
-        return true;
-      };
-      auto load_k = [&](int j) { return load(&p.map_k, j, p.k_head, p.k_batch); };
-      auto load_v = [&](int j) { return load(&p.map_v, j, p.v_head, p.v_batch); };
-      bool ok = load_k(T1 - 1);
-      if constexpr (PAIR) {
-        for (int i = 0; ok && i < n; ++i) ok = load_v(T1 - 1 - i) && (i + 1 >= n || load_k(T1 - 2 - i));
-      } else {
-        if (ok && n > 1) ok = load_k(T1 - 2);
-        for (int i = 0; ok && i < n_w[0]; ++i)
-          for (int w = 0; ok && w < 2; ++w)
-            if (i < n_w[w]) {
-              const int j = T1 - 1 - (2 * i + w);
-              ok = load_v(j) && (i + 1 >= n_w[w] || load_k(j - 2));
-            }
-      }
-      if (*fail) {  // no copy may outlive the CTA
-        if (!mbar_wait(sm.qfull(), 0)) record_error(a.status, kErrDrainTimeout);
-        for (int s = 0; s < L::kStages; ++s)
-          if (last[s] >= 0 && !mbar_wait(sm.full(s), (last[s] / L::kStages) & 1)) record_error(a.status, kErrDrainTimeout);
-      }
-    }
-  } else if (warp == kMmaWarp) {
-    if (lane == 0 && n > 0) {
-      int done[2] = {0, 0};  // weights consumed per stream
-      auto wait_full = [&](int c) {
-        const bool ok = mbar_wait_role(sm.full(c % L::kStages), (c / L::kStages) & 1, fail);
-        tcgen05_after_sync();
-        return ok;
-      };
-      auto scores = [&](int w, int c) {
-        mma_scores<F16>(tmem + 128 * w, sm.q(PAIR ? w : 0), sm.stage(c % L::kStages));
-        umma_commit(sm.sfull(w));
-      };
-      auto values = [&](int w, int c) {
-        if (!mbar_wait_role(sm.pready(w), done[w] & 1, fail)) return false;
-        tcgen05_after_sync();
-        mma_values<F16>(tmem + 256 + 128 * w, tmem + 128 * w, sm.stage(c % L::kStages), done[w] > 0);
-        umma_commit(sm.odone(w));
-        ++done[w];
-        return true;
-      };
-      auto wait_safe = [&](int u) { return mbar_wait_role(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail); };
-      bool ok = mbar_wait_role(sm.qfull(), 0, fail) && wait_full(0);
-      if constexpr (PAIR) {
-        if (ok) {
-          for (int w = 0; w < 2; ++w)
-            if (active(w, T1 - 1)) scores(w, 0);
-          umma_commit(sm.empty(0));
+        for (int m = 0; m < L::kQ; ++m) {
+          const int tok0 = (PAIR ? 2 * m_block + m : m_block) * (kTile / a.G);
+          tma_load_4d(sm.q(m), &p.map_q, 0, h * a.G, tok0, b, sm.qfull());
+          tma_load_4d(sm.q(m) + kHalfBytes, &p.map_q, 64, h * a.G, tok0, b, sm.qfull());
         }
-        for (int i = 0; ok && i < n; ++i) {
-          const int j = T1 - 1 - i, cv = 2 * i + 1, ck = cv + 1;
-          ok = wait_full(cv) && (!guarded(j) || wait_safe(i));
-          for (int w = 0; ok && w < 2; ++w) {
-            if (active(w, j)) ok = values(w, cv);
-            if (ok && i + 1 < n) {
-              if (w == 0) ok = wait_full(ck);
-              if (ok && active(w, j - 1)) scores(w, ck);
-            }
-          }
-          if (ok) {
-            umma_commit(sm.empty(cv % L::kStages));
-            if (i + 1 < n) umma_commit(sm.empty(ck % L::kStages));
-          }
-        }
-      } else {
         int c = 0;
-        for (int w = 0; ok && w < 2; ++w)
-          if (w < n) {
-            if (w == 1) ok = wait_full(1);
+        auto load = [&](const CUtensorMap* map, int j, int hm, int bm) {
+          const int s = c % L::kStages;
+          if (c >= L::kStages && !mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail)) return false;
+          mbar_arrive_expect_tx(sm.full(s), kTileBytes);
+          tma_load_4d(sm.stage(s), map, 0, j * kTile, h * hm, b * bm, sm.full(s));
+          tma_load_4d(sm.stage(s) + kHalfBytes, map, 64, j * kTile, h * hm, b * bm, sm.full(s));
+          last[s] = c++;
+          return true;
+        };
+        auto load_k = [&](int j) { return load(&p.map_k, j, p.k_head, p.k_batch); };
+        auto load_v = [&](int j) { return load(&p.map_v, j, p.v_head, p.v_batch); };
+        bool ok = load_k(T1 - 1);
+        if constexpr (PAIR) {
+          for (int i = 0; ok && i < n; ++i) ok = load_v(T1 - 1 - i) && (i + 1 >= n || load_k(T1 - 2 - i));
+        } else {
+          if (ok && n > 1) ok = load_k(T1 - 2);
+          for (int i = 0; ok && i < n_w[0]; ++i)
+            for (int w = 0; ok && w < 2; ++w)
+              if (i < of(n_w, w)) {
+                const int j = T1 - 1 - (2 * i + w);
+                ok = load_v(j) && (i + 1 >= of(n_w, w) || load_k(j - 2));
+              }
+        }
+        if (*fail) {  // no copy may outlive the CTA
+          if (!mbar_wait(sm.qfull(), 0)) record_error(a.status, kErrDrainTimeout);
+          for (int s = 0; s < L::kStages; ++s)
+            if (last[s] >= 0 && !mbar_wait(sm.full(s), (last[s] / L::kStages) & 1)) record_error(a.status, kErrDrainTimeout);
+        }
+      }
+    } else if (warp == kMmaWarp) {
+      if (lane == 0 && n > 0) {
+        int done[2] = {0, 0};  // weights consumed per stream
+        auto wait_full = [&](int c) {
+          const bool ok = mbar_wait_role(sm.full(c % L::kStages), (c / L::kStages) & 1, fail);
+          tcgen05_after_sync();
+          return ok;
+        };
+        auto scores = [&](int w, int c) {
+          mma_scores<F16>(tmem + 128 * w, sm.q(PAIR ? w : 0), sm.stage(c % L::kStages));
+          umma_commit(sm.sfull(w));
+        };
+        auto values = [&](int w, int c) {
+          if (!mbar_wait_role(sm.pready(w), done[w] & 1, fail)) return false;
+          tcgen05_after_sync();
+          mma_values<F16>(tmem + 256 + 128 * w, tmem + 128 * w, sm.stage(c % L::kStages), done[w] > 0);
+          umma_commit(sm.odone(w));
+          ++done[w];
+          return true;
+        };
+        auto wait_safe = [&](int u) { return mbar_wait_role(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail); };
+        bool ok = mbar_wait_role(sm.qfull(), 0, fail) && wait_full(0);
+        if constexpr (PAIR) {
+          if (ok) {
+            for (int w = 0; w < 2; ++w)
+              if (active(w, T1 - 1)) scores(w, 0);
+            umma_commit(sm.empty(0));
+          }
+          for (int i = 0; ok && i < n; ++i) {
+            const int j = T1 - 1 - i, cv = 2 * i + 1, ck = cv + 1;
+            ok = wait_full(cv) && (!guarded(j) || wait_safe(i));
+            for (int w = 0; ok && w < 2; ++w) {
+              if (active(w, j)) ok = values(w, cv);
+              if (ok && i + 1 < n) {
+                if (w == 0) ok = wait_full(ck);
+                if (ok && active(w, j - 1)) scores(w, ck);
+              }
+            }
             if (ok) {
-              scores(w, c);
-              umma_commit(sm.empty(c));
-              ++c;
+              umma_commit(sm.empty(cv % L::kStages));
+              if (i + 1 < n) umma_commit(sm.empty(ck % L::kStages));
             }
           }
-        for (int i = 0; ok && i < n_w[0]; ++i)
+        } else {
+          int c = 0;
           for (int w = 0; ok && w < 2; ++w)
-            if (i < n_w[w]) {
-              ok = wait_full(c) && (!guarded(T1 - 1 - (2 * i + w)) || wait_safe(2 * i + w)) && values(w, c);
-              if (!ok) break;
-              umma_commit(sm.empty(c % L::kStages));
-              ++c;
-              if (i + 1 < n_w[w]) {
-                ok = wait_full(c);
-                if (!ok) break;
+            if (w < n) {
+              if (w == 1) ok = wait_full(1);
+              if (ok) {
                 scores(w, c);
-                umma_commit(sm.empty(c % L::kStages));
+                umma_commit(sm.empty(c));
                 ++c;
               }
             }
-      }
-      umma_commit(sm.drain());  // every MMA issued has completed once this arrives
-      if (!mbar_wait(sm.drain(), 0)) record_error(a.status, kErrDrainTimeout);
-    }
-  } else if (warp >= kGuardWarp) {
-    int c = PAIR ? 1 : min(n, 2);  // ring position of V tile u
-    for (int u = 0; u < n; ++u) {
-      const int s = c % L::kStages, j = T1 - 1 - u;
-      if (!__all_sync(0xffffffffu, mbar_wait_role(sm.full(s), (c / L::kStages) & 1, fail))) break;
-      if (guarded(j)) {
-        const int g = warp - kGuardWarp;
-        bool wrote = false;
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          const int key = 64 * part + 32 * g + lane;
-          const uint32_t at = sm.stage(s) + key * 128;
-          bool bad = false;
-#pragma unroll
-          for (int q = 0; q < 16; ++q)
-            bad = bad || any_nonfinite<F16>(lds128(at + (q >> 3) * kHalfBytes + (((q & 7) ^ (key & 7)) << 4)));
-          const uint32_t bits = __ballot_sync(0xffffffffu, bad);
-          if (bad) {
-            for (int q = 0; q < 16; ++q) sts128_zero(at + (q >> 3) * kHalfBytes + ((q & 7) << 4));
-            wrote = true;
-          }
-          if (lane == 0) s_bad[u % kVRing][2 * part + g] = bits;
+          for (int i = 0; ok && i < n_w[0]; ++i)
+            for (int w = 0; ok && w < 2; ++w)
+              if (i < of(n_w, w)) {
+                ok = wait_full(c) && (!guarded(T1 - 1 - (2 * i + w)) || wait_safe(2 * i + w)) && values(w, c);
+                if (!ok) break;
+                umma_commit(sm.empty(c % L::kStages));
+                ++c;
+                if (i + 1 < of(n_w, w)) {
+                  ok = wait_full(c);
+                  if (!ok) break;
+                  scores(w, c);
+                  umma_commit(sm.empty(c % L::kStages));
+                  ++c;
+                }
+              }
         }
-        if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
+        umma_commit(sm.drain());  // every MMA issued has completed once this arrives
+        if (!mbar_wait(sm.drain(), 0)) record_error(a.status, kErrDrainTimeout);
       }
-      if (lane == 0) mbar_arrive(sm.vsafe(u % kVRing));
-      // to V tile u + 1: past the K tiles that are loaded between
-      c += PAIR ? 2 : 1 + (u / 2 + 1 < n_w[u & 1] ? 1 : 0);
+    } else {  // guard warps
+      int c = PAIR ? 1 : min(n, 2);  // ring position of V tile u
+      for (int u = 0; u < n; ++u) {
+        const int s = c % L::kStages, j = T1 - 1 - u;
+        if (!__all_sync(0xffffffffu, mbar_wait_role(sm.full(s), (c / L::kStages) & 1, fail))) break;
+        if (guarded(j)) {
+          const int g = warp - kGuardWarp;
+          bool wrote = false;
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {
+            const int key = 64 * part + 32 * g + lane;
+            const uint32_t at = sm.stage(s) + key * 128;
+            bool bad = false;
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+              bad = bad || any_nonfinite<F16>(lds128(at + (q >> 3) * kHalfBytes + (((q & 7) ^ (key & 7)) << 4)));
+            const uint32_t bits = __ballot_sync(0xffffffffu, bad);
+            if (bad) {
+              for (int q = 0; q < 16; ++q) sts128_zero(at + (q >> 3) * kHalfBytes + ((q & 7) << 4));
+              wrote = true;
+            }
+            if (lane == 0) s_bad[u % kVRing][2 * part + g] = bits;
+          }
+          if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        if (lane == 0) mbar_arrive(sm.vsafe(u % kVRing));
+        // to V tile u + 1: past the K tiles that are loaded between
+        c += PAIR ? 2 : 1 + (u / 2 + 1 < of(n_w, u & 1) ? 1 : 0);
+      }
     }
   } else {  // softmax warps
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t ts = tmem + 128 * stream + lanes, to = tmem + 256 + 128 * stream + lanes;
     Score sc;
@@ -482,15 +540,32 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     sc.cap = a.softcap * kLog2e;
     float ref = -INFINITY, sum = 0.f;
     bool bad_row = false, ok = true, exact_ref = false;
+    const bool any_valid = __any_sync(0xffffffffu, valid);
     int it = 0;
-    for (int i = 0; i < (PAIR ? n : n_w[stream]); ++i) {
+    for (int i = 0; i < (PAIR ? n : of(n_w, stream)); ++i) {
       const int j = T1 - 1 - (PAIR ? i : 2 * i + stream);
       if (PAIR && !active(stream, j)) continue;
       const int k0 = j * kTile;
-      const bool masked = cut(PAIR ? stream : 0, j);
       ok = __all_sync(0xffffffffu, mbar_wait_role(sm.sfull(stream), it & 1, fail));
       if (!ok) break;
       tcgen05_after_sync();
+      if (k0 >= warp_hi || k0 + kTile <= warp_lo) {  // no row of this warp sees the tile
+        if (any_valid) {  // (rows past the last token may hold anything)
+          uint32_t zero[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) zero[e] = 0u;
+          tmem_st32(ts, zero);
+          tmem_st32(ts + 32, zero);
+          tmem_wait_st();
+        }
+        tcgen05_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sm.pready(stream));
+        ++it;
+        continue;
+      }
+      const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
+      const int side = !BIAS ? 0 : k0 + kTile - 1 <= pos_min ? -1 : k0 >= pos_max ? 1 : 0;
       uint32_t w[64];
       float tile_sum;
       bool low = ref == -INFINITY;  // the row has no reference yet, or one that proved too low
@@ -502,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             float v[32];
             tmem_ld32(ts + 32 * c, v);
             tmem_wait_ld(v);
-            row_scores<CAP, BIAS>(v, sc, row, k0, 32 * c, 0.f, masked);
+            row_scores<CAP, BIAS>(v, sc, row, k0, 32 * c, 0.f, masked, side);
 #pragma unroll
             for (int e = 0; e < 32; ++e) mx = fmaxf(mx, v[e]);
           }
@@ -532,12 +607,14 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         const float rr = ref == -INFINITY || exact_ref ? 0.f : ref;
         const bool some_exact = __any_sync(0xffffffffu, exact_ref);
         uint64_t acc[2] = {0ull, 0ull};
+        float buf[2][32];
+        tmem_ld32(ts, buf[0]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          float v[32];
-          tmem_ld32(ts + 32 * c, v);
+          float(&v)[32] = buf[c & 1];
           tmem_wait_ld(v);
-          row_scores<CAP, BIAS>(v, sc, row, k0, 32 * c, rr, masked);
+          if (c < 3) tmem_ld32(ts + 32 * (c + 1), buf[(c + 1) & 1]);
+          row_scores<CAP, BIAS>(v, sc, row, k0, 32 * c, rr, masked, side);
           if (some_exact) {
             const float rest = exact_ref ? ref : 0.f;
 #pragma unroll
@@ -684,8 +761,17 @@ cudaError_t launch_variant(const FlashKernelArgs& p, dim3 grid, cudaStream_t st)
   const bool cap = p.a.softcap > 0.f, bias = p.a.slopes != nullptr;
   auto k = cap ? (bias ? flash_kernel<F16, PAIR, true, true> : flash_kernel<F16, PAIR, true, false>)
                : (bias ? flash_kernel<F16, PAIR, false, true> : flash_kernel<F16, PAIR, false, false>);
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<PAIR>::kSmem);
+  static std::atomic<uint64_t> configured[4];  // per variant: one bit per device
+  std::atomic<uint64_t>& done = configured[2 * cap + bias];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev > 63 || !(done.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<PAIR>::kSmem);
+    if (e != cudaSuccess) return e;
+    done.fetch_or(bit, std::memory_order_relaxed);
+  }
   k<<<grid, kThreads, Layout<PAIR>::kSmem, st>>>(p);
   return cudaGetLastError();
 }

@@ -6,40 +6,56 @@ token-major rows are passed as ``x.transpose(1, 2)``.
 """
 from __future__ import annotations
 
-import ctypes
 import math
+import struct
 
 import torch
 
-from . import HEAD_DIM, _check, _PrefixDesc, _PromptDesc, _ptr, _RotaryDesc, _stream, _View, load
+from . import HEAD_DIM, _check, _ptr, load
 
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 LAYOUTS = {"half": 0, "interleaved": 1}
 
 
+# Descriptors and views are packed as bytes (ctypes passes their address): these calls are short enough that building
+# ctypes structures would take longer than the launches.
+_pack_view = struct.Struct("Pqqq").pack            # mikv_view
+_pack_rotary = struct.Struct("9if").pack           # mikv_rotary_desc
+_pack_prompt = struct.Struct("10iff").pack         # mikv_prompt_desc
+_pack_prefix = struct.Struct("8iff").pack          # mikv_prefix_desc
+
+
 def _dtype(t: torch.Tensor) -> int:
-    if t.dtype not in DTYPES:
+    code = DTYPES.get(t.dtype)
+    if code is None:
         raise ValueError(f"libmikv takes bfloat16, float16 or float32 tensors here, not {t.dtype}")
-    return DTYPES[t.dtype]
+    return code
 
 
-def _view(t: torch.Tensor, shape=None) -> _View:
-    if t.dim() != 4 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"expected a tensor of shape {shape or '[batch, heads, tokens, 128]'}, got {tuple(t.shape)}")
+def _view(t: torch.Tensor, shape) -> bytes:
+    """mikv_view of a [batch, heads, tokens, channels] tensor."""
+    if t.shape != shape or len(shape) != 4:
+        raise ValueError(f"expected a tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
     if not t.is_cuda:
         raise ValueError("libmikv takes device tensors")
-    if t.stride(3) != 1:
+    b, h, n, c = t.stride()
+    if c != 1:
         raise ValueError("the channels of a head must be contiguous")
-    return _View(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return _pack_view(t.data_ptr(), b, h, n)
 
 
 def _dense(t, shape, dtype, name):
     """Pointer of an optional dense tensor after checking what the library cannot see."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     return _ptr(t)
+
+
+def _raw_stream(stream, t: torch.Tensor) -> int:
+    """The given stream, or the current one of the tensor's device."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def mikv_rotary_phases(frequencies) -> torch.Tensor:
@@ -103,21 +119,25 @@ def mikv_rotary(table: RotaryTable, q, k=None, q_out=None, k_out=None, positions
     where they are None. positions: int32 [B, T], or token t stands at start + t. inverse: the transposed map.
     Returns (q_out, k_out)."""
     q_out = q if q_out is None else q_out
-    k_out = k if k_out is None else k_out
-    B, Hq, T, d = q.shape
-    kinds = {t.dtype for t in (q, q_out, k, k_out) if t is not None}
-    if len(kinds) != 1:
+    shape, dt = q.shape, q.dtype
+    B, Hq, T, d = shape
+    if q_out.dtype != dt:
         raise ValueError("rotary: inputs and outputs of one type")
-    views = [_view(q), _view(q_out, q.shape)]
-    Hk = 0
+    qi = _view(q, shape)
+    qo = qi if q_out is q else _view(q_out, shape)
+    Hk, ki, ko = 0, None, None
     if k is not None:
+        k_out = k if k_out is None else k_out
         Hk = k.shape[1]
-        views += [_view(k, (B, Hk, T, d)), _view(k_out, k.shape)]
-    desc = _RotaryDesc(_dtype(q), B, T, Hq, Hk, d, table.rot_dim, LAYOUTS[table.layout], int(inverse), table.amplitude)
-    refs = [ctypes.byref(v) for v in views] + [None] * (4 - len(views))
-    _check("mikv_rotary", load().mikv_rotary(
-        ctypes.byref(desc), *refs, _ptr(table.phases), _dense(positions, (B, T), torch.int32, "positions"), start,
-        _stream(stream)))
+        shape = (B, Hk, T, d)
+        if k.dtype != dt or k_out.dtype != dt:
+            raise ValueError("rotary: inputs and outputs of one type")
+        ki = _view(k, shape)
+        ko = ki if k_out is k else _view(k_out, shape)
+    desc = _pack_rotary(_dtype(q), B, T, Hq, Hk, d, table.rot_dim, LAYOUTS[table.layout], int(inverse), table.amplitude)
+    rc = load().mikv_rotary(desc, qi, qo, ki, ko, table.phases.data_ptr(),
+                            _dense(positions, (B, T), torch.int32, "positions"), start, _raw_stream(stream, q))
+    _check("mikv_rotary", rc)
     return q_out, k_out
 
 
@@ -134,21 +154,20 @@ def mikv_mask_spans(spans, tk: int, q_start: int = None, causal: bool = True, do
         _dense(docs, (B, n + 1), torch.int32, "docs"), n,
         _dense(prefix, (B,) if docs is None or (prefix is not None and prefix.dim() == 1 and n == 1) else (B, n),
                torch.int32, "prefix"),
-        _dense(key_len, (B,), torch.int32, "key_len"), _stream(stream)))
+        _dense(key_len, (B,), torch.int32, "key_len"), _raw_stream(stream, spans)))
 
 
-def _prompt_desc(q, k, out=None, causal=True, q_start=None, sm_scale=None, softcap=0.0) -> _PromptDesc:
+def _prompt_desc(q, k, out, causal, q_start, sm_scale, softcap) -> bytes:
     B, Hq, tq, d = q.shape
-    tk = k.shape[2]
-    out_dtype = _dtype(q if out is None else out)
-    return _PromptDesc(_dtype(q), out_dtype, B, Hq, k.shape[1], d, tq, tk, int(causal),
-                       tk - tq if q_start is None else q_start,
-                       1.0 / math.sqrt(d) if sm_scale is None else sm_scale, softcap)
+    Hkv, tk = k.shape[1:3]
+    return _pack_prompt(_dtype(q), _dtype(out), B, Hq, Hkv, d, tq, tk, 1 if causal else 0,
+                        tk - tq if q_start is None else q_start, 1.0 / math.sqrt(d) if sm_scale is None else sm_scale,
+                        softcap)
 
 
 def mikv_prompt_workspace_bytes(q, k) -> int:
     """Workspace of mikv_prompt_attention for q [B, Hq, Tq, d] and k [B, Hkv, Tk, d]."""
-    return int(load().mikv_prompt_workspace_bytes(ctypes.byref(_prompt_desc(q, k))))
+    return int(load().mikv_prompt_workspace_bytes(_prompt_desc(q, k, q, True, None, None, 0.0)))
 
 
 def mikv_prompt_attention(q, k, v, out, workspace, sm_scale: float = None, causal: bool = True, q_start: int = None,
@@ -156,26 +175,28 @@ def mikv_prompt_attention(q, k, v, out, workspace, sm_scale: float = None, causa
     """Attention of a prompt: q [B, Hq, Tq, d] over k, v [B, Hkv, Tk, d] into out [B, Hq, Tq, d] (the inputs' type or
     float32). spans (mikv_mask_spans) or causal says which keys a query sees; softcap caps the scores, slopes
     float32 [Hq] add a distance bias; lse float32 [B, Hq, Tq] takes the log of each row's sum."""
-    B, Hq, tq, d = q.shape
+    shape, ks = q.shape, k.shape
+    B, Hq, tq, d = shape
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("prompt attention: q, k and v of one type")
-    desc = _prompt_desc(q, k, out, causal, q_start, sm_scale, softcap)
-    views = (_view(q), _view(k, (B, k.shape[1], desc.tk, d)), _view(v, k.shape), _view(out, q.shape))
-    _check("mikv_prompt_attention", load().mikv_prompt_attention(
-        ctypes.byref(desc), *(ctypes.byref(x) for x in views), _dense(spans, (B, tq, 2), torch.int32, "spans"),
+    rc = load().mikv_prompt_attention(
+        _prompt_desc(q, k, out, causal, q_start, sm_scale, softcap), _view(q, shape), _view(k, (B, ks[1], ks[2], d)),
+        _view(v, ks), _view(out, shape), _dense(spans, (B, tq, 2), torch.int32, "spans"),
         _dense(slopes, (Hq,), torch.float32, "slopes"), _dense(lse, (B, Hq, tq), torch.float32, "lse"),
-        _ptr(workspace), workspace.numel(), _stream(stream)))
+        _ptr(workspace), workspace.nbytes, _raw_stream(stream, q))
+    _check("mikv_prompt_attention", rc)
 
 
-def _prefix_desc(q, k, out=None, sm_scale=None, softcap=0.0) -> _PrefixDesc:
+def _prefix_desc(q, k, out, sm_scale, softcap) -> bytes:
     B, Hq, d = q.shape
-    return _PrefixDesc(_dtype(q), _dtype(q if out is None else out), B, k.shape[0], Hq, k.shape[1], d, k.shape[2],
-                       1.0 / math.sqrt(d) if sm_scale is None else sm_scale, softcap)
+    n, Hkv, P, _ = k.shape
+    return _pack_prefix(_dtype(q), _dtype(out), B, n, Hq, Hkv, d, P,
+                        1.0 / math.sqrt(d) if sm_scale is None else sm_scale, softcap)
 
 
 def mikv_prefix_workspace_bytes(q, k) -> int:
     """Workspace of mikv_prefix_attention for q [B, Hq, d] and k [groups, Hkv, P, d]."""
-    return int(load().mikv_prefix_workspace_bytes(ctypes.byref(_prefix_desc(q, k))))
+    return int(load().mikv_prefix_workspace_bytes(_prefix_desc(q, k, q, None, 0.0)))
 
 
 def mikv_prefix_attention(q, k, v, out, workspace, lens=None, q_pos=None, sm_scale: float = None,
@@ -184,15 +205,15 @@ def mikv_prefix_attention(q, k, v, out, workspace, lens=None, q_pos=None, sm_sca
     each, into out [B, Hq, d]; lens int32 [groups] their lengths, q_pos int32 [B] the queries' positions. own_out
     float32 [B, Hq, d] and own_ml float32 [B, Hq, 2] (from mikv_decode_attention) join each request's own cache;
     ml float32 [B, Hq, 2] takes the joint (log-sum-exp, 1)."""
-    B, Hq, d = q.shape
-    n = k.shape[0]
+    shape, ks = q.shape, k.shape
+    B, Hq, d = shape
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("prefix attention: q, k and v of one type")
-    desc = _prefix_desc(q, k, out, sm_scale, softcap)
-    views = (_view(k), _view(v, k.shape))
-    _check("mikv_prefix_attention", load().mikv_prefix_attention(
-        ctypes.byref(desc), _ptr(q), *(ctypes.byref(x) for x in views), _dense(lens, (n,), torch.int32, "lens"),
-        _dense(q_pos, (B,), torch.int32, "q_pos"), _dense(slopes, (Hq,), torch.float32, "slopes"),
-        _dense(own_out, (B, Hq, d), torch.float32, "own_out"), _dense(own_ml, (B, Hq, 2), torch.float32, "own_ml"),
-        _dense(out, (B, Hq, d), out.dtype, "out"), _dense(ml, (B, Hq, 2), torch.float32, "ml"),
-        _ptr(workspace), workspace.numel(), _stream(stream)))
+    stat = (B, Hq, 2)
+    rc = load().mikv_prefix_attention(
+        _prefix_desc(q, k, out, sm_scale, softcap), _ptr(q), _view(k, (ks[0], ks[1], ks[2], d)), _view(v, ks),
+        _dense(lens, ks[:1], torch.int32, "lens"), _dense(q_pos, (B,), torch.int32, "q_pos"),
+        _dense(slopes, (Hq,), torch.float32, "slopes"), _dense(own_out, shape, torch.float32, "own_out"),
+        _dense(own_ml, stat, torch.float32, "own_ml"), _dense(out, shape, out.dtype, "out"),
+        _dense(ml, stat, torch.float32, "ml"), _ptr(workspace), workspace.nbytes, _raw_stream(stream, q))
+    _check("mikv_prefix_attention", rc)
