@@ -68,13 +68,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   }
 }
 
-// Bounded wait of one role of a specialised CTA: also gives up as soon as another role has failed.
+// Bounded wait of one role of a specialised CTA: also gives up as soon as another role has failed. The limit is counted
+// in SM clocks, which are cheap to read (the global timer takes longer than most waits of a full pipeline).
+constexpr long long kWaitLimitClocks = 4000000000ll;  // about 2 s
+
 __device__ __forceinline__ bool mbar_wait_role(uint32_t bar, uint32_t parity, volatile int* fail) {
   if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = global_timer_ns();
+  const long long t0 = clock64();
   for (uint32_t i = 1;; ++i) {
     if (mbar_try_wait(bar, parity)) return true;
-    if ((i & 63u) == 0 && (*fail || global_timer_ns() - t0 > kWaitLimitNs)) {
+    if ((i & 63u) == 0 && (*fail || clock64() - t0 > kWaitLimitClocks)) {
       *fail = 1;
       return false;
     }
