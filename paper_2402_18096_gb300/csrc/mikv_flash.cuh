@@ -79,16 +79,19 @@ struct Layout {
   __device__ uint32_t drain() const { return bar(kBars - 1); }
 };
 
-// What the weights may grow to before the reference moves, and how far below the first tile's largest score the
-// reference starts (log2). bf16 weights have fp32's range, so the reference is that largest score and the sums
-// may grow far; fp16 weights hold 2^-24 .. 2^16, so they start at 2^8 and move before the sum can pass 2^16.
+// What the weights may grow to before the reference moves, and how far below a tile's largest score the reference is
+// put (log2). bf16 weights have fp32's range, so the reference is that largest score and the sums may grow
+// far; fp16 weights hold 2^-24 .. 2^16, so they start at 2^8 and move before the sum of a tile can pass 2^16.
 template <bool F16>
 __device__ constexpr float ref_drop() { return F16 ? 8.f : 0.f; }
 template <bool F16>
 __device__ constexpr float sum_max() { return F16 ? 0x1.fep15f : 0x1p20f; }
+// A largest score this far above the reference may stay: 128 weights of 2^it are below sum_max.
+template <bool F16>
+__device__ constexpr float ref_slack() { return F16 ? 8.5f : 12.f; }
 
-// Above this size of the reference, scores are rounded before it is taken off: the fused form keeps the product's
-// rounding error, up to 2^-24 of it, which would be a factor of the weights.
+// Above this size of the reference, scores are rounded before it is taken off (the slow path): the fused form keeps
+// the product's rounding error, up to 2^-24 of it, which would be a factor of the weights.
 constexpr float kRefExact = 0x1p22f;
 
 // The scores of one row in log2 units: x = cap(v * scale) - slope |pos - j|, times log2 e.
@@ -133,23 +136,21 @@ __device__ __forceinline__ void cap_four(float* v, float scale, float cap, const
   f32x2_split(fma_f32x2(mul_f32x2(s, ab), c2, f32x2(rest[2], rest[3])), v[2], v[3]);
 }
 
-// 32 scores (columns col0 .. col0 + 31 of the tile at key k0) less `ref`, in place; masked ones become -inf.
+__device__ __forceinline__ float max3(float a, float b, float c) {  // NaN operands are passed over
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
+// N scores (columns col0 .. of the tile at key k0) less `ref`, in place.
 // side: every key of the tile lies at or before every position of the warp (-1), at or after them (1), or neither (0).
-template <bool CAP, bool BIAS>
-__device__ __forceinline__ void row_scores(float (&v)[32], const Score& sc, const Row& row, int k0, int col0, float ref,
-                                           bool masked, int side) {
-  const int first = row.lo - k0 - col0, n = row.hi - row.lo;
-  if constexpr (CAP) {
-    if (masked) {  // what a masked key holds must not reach its neighbours through the shared reciprocal
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if ((unsigned)(i - first) >= (unsigned)n) v[i] = 0.f;
-    }
-  }
+template <bool CAP, bool BIAS, int N>
+__device__ __forceinline__ void row_scores(float* v, const Score& sc, const Row& row, int k0, int col0, float ref,
+                                           int side) {
   const float rest = (CAP ? sc.cap : 0.f) - ref;
   auto apply = [&](auto bias) {  // bias(i): the bias of column i, plus `rest`
 #pragma unroll
-    for (int i = 0; i < 32; i += 4) {
+    for (int i = 0; i < N; i += 4) {
       const float b[4] = {bias(i), bias(i + 1), bias(i + 2), bias(i + 3)};
       if constexpr (CAP) {
         cap_four(v + i, sc.scale, sc.cap, b);
@@ -172,11 +173,16 @@ __device__ __forceinline__ void row_scores(float (&v)[32], const Score& sc, cons
       apply([&](int i) { return fmaf(-row.slope, fabsf(e0 + (float)i), rest); });
     }
   }
-  if (masked) {
+}
+
+// Scores outside the row's span, replaced by x.
+template <int N>
+__device__ __forceinline__ void mask_scores(float* v, const Row& row, int first_key, float x) {
+  const int first = row.lo - first_key;
+  const unsigned n = row.hi - row.lo;
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if ((unsigned)(i - first) >= (unsigned)n) v[i] = -INFINITY;
-  }
+  for (int i = 0; i < N; ++i)
+    if ((unsigned)(i - first) >= n) v[i] = x;
 }
 
 template <bool F16>
@@ -515,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             bool bad = false;
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-              bad = bad || any_nonfinite<F16>(lds128(at + (q >> 3) * kHalfBytes + (((q & 7) ^ (key & 7)) << 4)));
+              bad |= any_nonfinite<F16>(lds128(at + (q >> 3) * kHalfBytes + (((q & 7) ^ (key & 7)) << 4)));
             const uint32_t bits = __ballot_sync(0xffffffffu, bad);
             if (bad) {
               for (int q = 0; q < 16; ++q) sts128_zero(at + (q >> 3) * kHalfBytes + ((q & 7) << 4));
@@ -538,8 +544,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     Score sc;
     sc.scale = CAP ? 2.f * kLog2e * (a.sm_scale / a.softcap) : a.sm_scale * kLog2e;
     sc.cap = a.softcap * kLog2e;
-    float ref = -INFINITY, sum = 0.f;
-    bool bad_row = false, ok = true, exact_ref = false;
+    // (a row that sees nothing, or past the last token, needs no reference: its weights are 0 or never used)
+    float ref = row.hi > row.lo ? -INFINITY : 0.f, sum = 0.f;
+    bool bad_row = false, ok = true;
+    bool careful = true;  // some row of the warp has no reference yet, or one beyond kRefExact
     const bool any_valid = __any_sync(0xffffffffu, valid);
     int it = 0;
     for (int i = 0; i < (PAIR ? n : of(n_w, stream)); ++i) {
@@ -567,74 +575,93 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
       const int side = !BIAS ? 0 : k0 + kTile - 1 <= pos_min ? -1 : k0 >= pos_max ? 1 : 0;
       uint32_t w[64];
-      float tile_sum;
-      bool low = ref == -INFINITY;  // the row has no reference yet, or one that proved too low
-      for (bool again = false;; again = true) {
-        if (__any_sync(0xffffffffu, low)) {
-          float mx = -INFINITY;  // the row's largest score of this tile
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            float v[32];
-            tmem_ld32(ts + 32 * c, v);
-            tmem_wait_ld(v);
-            row_scores<CAP, BIAS>(v, sc, row, k0, 32 * c, 0.f, masked, side);
+      float tile_sum = 0.f;
+      // 64 columns at a time: the weights of v[0 .. 63] (scores less the reference), packed, and their sums
+      auto pack_half = [&](const float (&v)[64], uint32_t* dst, uint64_t (&acc)[4]) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) mx = fmaxf(mx, v[e]);
-          }
-          const float next = low ? fmaxf(ref, mx - ref_drop<F16>()) : ref;
-          const bool moves = next != ref && ref != -INFINITY;
-          if (__any_sync(0xffffffffu, moves)) {
-            const float f = moves ? fast_exp2(ref - next) : 1.f;
-            if (it > 0) {
-              ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream), (it - 1) & 1, fail));
-              if (!ok) break;
-              tcgen05_after_sync();
-#pragma unroll 1
-              for (int c = 0; c < 4; ++c) {
-                float v[32];
-                tmem_ld32(to + 32 * c, v);
-                tmem_wait_ld(v);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] *= f;
-                tmem_st32(to + 32 * c, reinterpret_cast<const uint32_t*>(v));
-              }
-            }
-            sum *= f;
-          }
-          ref = next;
-          exact_ref = fabsf(ref) > kRefExact && ref != -INFINITY;
+        for (int e = 0; e < 64; e += 2) {
+          const float x = fast_exp2(v[e]), y = fast_exp2(v[e + 1]);
+          acc[(e >> 1) & 3] = add_f32x2(acc[(e >> 1) & 3], f32x2(x, y));
+          dst[e >> 1] = pack16<F16>(x, y);
         }
-        const float rr = ref == -INFINITY || exact_ref ? 0.f : ref;
-        const bool some_exact = __any_sync(0xffffffffu, exact_ref);
-        uint64_t acc[2] = {0ull, 0ull};
-        float buf[2][32];
-        tmem_ld32(ts, buf[0]);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float(&v)[32] = buf[c & 1];
-          tmem_wait_ld(v);
-          if (c < 3) tmem_ld32(ts + 32 * (c + 1), buf[(c + 1) & 1]);
-          row_scores<CAP, BIAS>(v, sc, row, k0, 32 * c, rr, masked, side);
-          if (some_exact) {
-            const float rest = exact_ref ? ref : 0.f;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] -= rest;
-          }
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const float x = fast_exp2(v[e]), y = fast_exp2(v[e + 1]);
-            acc[(e >> 1) & 1] = add_f32x2(acc[(e >> 1) & 1], f32x2(x, y));
-            w[16 * c + (e >> 1)] = pack16<F16>(x, y);
-          }
-        }
+      };
+      auto total = [](const uint64_t (&acc)[4]) {
         float s0, s1, s2, s3;
-        f32x2_split(acc[0], s0, s1);
-        f32x2_split(acc[1], s2, s3);
-        tile_sum = (s0 + s1) + (s2 + s3);
-        low = !(tile_sum <= sum_max<F16>());  // (stays so for a NaN: one more attempt, then it is kept)
-        if (again || !__any_sync(0xffffffffu, low)) break;
+        f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
+        f32x2_split(add_f32x2(acc[2], acc[3]), s2, s3);
+        return (s0 + s1) + (s2 + s3);
+      };
+      // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards.
+      bool slow = masked || careful;
+      if (!slow) {
+        float v[2][64];
+        uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
+        tmem_ld32(ts, v[0]);
+        tmem_ld32(ts + 32, v[0] + 32);
+        tmem_wait_ld(v[0]);
+        reg_fence(v[0] + 32);
+        tmem_ld32(ts + 64, v[1]);
+        tmem_ld32(ts + 96, v[1] + 32);
+        row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
+        pack_half(v[0], w, acc);
+        tmem_wait_ld(v[1]);
+        reg_fence(v[1] + 32);
+        row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
+        pack_half(v[1], w + 32, acc);
+        tile_sum = total(acc);
+        slow = __any_sync(0xffffffffu, !(tile_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
       }
-      if (!ok) break;
+      if (slow) {
+        float v[2][64];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(ts + 32 * c, v[c >> 1] + 32 * (c & 1));
+        tmem_wait_ld(v[0]);
+        reg_fence(v[0] + 32);
+        reg_fence(v[1]);
+        reg_fence(v[1] + 32);
+        float mx = -INFINITY;  // the row's largest score of this tile
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (CAP && masked) mask_scores<64>(v[c], row, k0 + 64 * c, 0.f);  // (they share a reciprocal)
+          row_scores<CAP, BIAS, 64>(v[c], sc, row, k0, 64 * c, 0.f, side);
+          if (masked) mask_scores<64>(v[c], row, k0 + 64 * c, -INFINITY);
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) mx = max3(mx, v[c][e], v[c][e + 1]);
+        }
+        const float next = mx > ref + ref_slack<F16>() ? mx - ref_drop<F16>() : ref;
+        const bool moves = next != ref && ref != -INFINITY;
+        if (__any_sync(0xffffffffu, moves)) {
+          const float f = moves ? fast_exp2(ref - next) : 1.f;
+          if (it > 0) {
+            ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream), (it - 1) & 1, fail));
+            if (!ok) break;
+            tcgen05_after_sync();
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+              float o[16];
+              tmem_ld16(to + 16 * c, o);
+              tmem_wait_ld16(o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] *= f;
+              tmem_st16(to + 16 * c, reinterpret_cast<const uint32_t*>(o));
+            }
+          }
+          sum *= f;
+        }
+        ref = next;
+        careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
+        const float rr = ref == -INFINITY ? 0.f : ref;
+        const uint64_t r2 = f32x2(-rr, -rr);
+        uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int e = 0; e < 64; e += 2)
+            f32x2_split(add_f32x2(f32x2(v[c][e], v[c][e + 1]), r2), v[c][e], v[c][e + 1]);
+          pack_half(v[c], w + 32 * c, acc);
+        }
+        tile_sum = total(acc);
+      }
       sum += tile_sum;
       tmem_st32(ts, w);
       tmem_st32(ts + 32, w + 32);
