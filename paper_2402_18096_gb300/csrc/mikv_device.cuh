@@ -84,6 +84,19 @@ __device__ __forceinline__ bool mbar_wait_role(uint32_t bar, uint32_t parity, vo
   }
 }
 
+// The same for a converged warp: every lane waits, and all leave together with one answer.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* fail) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  const long long t0 = clock64();
+  for (uint32_t i = 1;; ++i) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if ((i & 63u) == 0 && __any_sync(0xffffffffu, *fail || clock64() - t0 > kWaitLimitClocks)) {
+      *fail = 1;
+      return false;
+    }
+  }
+}
+
 // ------------------------------------------------------------------ TMA
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w,

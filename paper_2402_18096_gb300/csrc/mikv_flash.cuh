@@ -62,7 +62,7 @@ template <bool PAIR>
 struct Layout {
   static constexpr int kQ = PAIR ? 2 : 1;          // query tiles in shared memory
   static constexpr int kStages = PAIR ? 5 : 6;     // K / V tiles in the ring
-  static constexpr int kBars = 1 + 2 * kStages + 3 * 2 + kVRing + 1;
+  static constexpr int kBars = 1 + 2 * kStages + 5 * 2 + kVRing + 1;
   static constexpr int kSmem = 1024 + (kQ + kStages) * kTileBytes + 8 * kBars;
   static_assert(kSmem <= 227 * 1024, "shared memory of one CTA");
   uint32_t base;
@@ -73,9 +73,10 @@ struct Layout {
   __device__ uint32_t full(int s) const { return bar(1 + s); }               // a copy landed
   __device__ uint32_t empty(int s) const { return bar(1 + kStages + s); }    // its MMAs have read it
   __device__ uint32_t sfull(int w) const { return bar(1 + 2 * kStages + w); }       // scores of stream w
-  __device__ uint32_t pready(int w) const { return bar(1 + 2 * kStages + 2 + w); }  // weights written (and O rescaled)
-  __device__ uint32_t odone(int w) const { return bar(1 + 2 * kStages + 4 + w); }   // O += P V done
-  __device__ uint32_t vsafe(int u) const { return bar(1 + 2 * kStages + 6 + u); }   // V tile u looked through
+  // of half a tile (64 keys): weights written (and O rescaled for them); O += P V done
+  __device__ uint32_t pready(int w, int half) const { return bar(1 + 2 * kStages + 2 + 2 * w + half); }
+  __device__ uint32_t odone(int w, int half) const { return bar(1 + 2 * kStages + 6 + 2 * w + half); }
+  __device__ uint32_t vsafe(int u) const { return bar(1 + 2 * kStages + 10 + u); }  // V tile u looked through
   __device__ uint32_t drain() const { return bar(kBars - 1); }
 };
 
@@ -220,14 +221,16 @@ __device__ __forceinline__ void mma_scores(uint32_t d, uint32_t q, uint32_t k) {
   }
 }
 
-// O (128 x 128) += P (TMEM, 128 x 128) x V tile.
+// O (128 x 128) += P (TMEM, 128 x 128) x V tile, 64 of the keys.
 template <bool F16>
-__device__ __forceinline__ void mma_values(uint32_t d, uint32_t p, uint32_t v, bool accumulate) {
+__device__ __forceinline__ void mma_values(uint32_t d, uint32_t p, uint32_t v, int half, bool accumulate) {
   constexpr uint32_t idesc = umma_idesc_16(F16, kTile, kTile, true);
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks)
+  for (int i = 0; i < 4; ++i) {
+    const int ks = 4 * half + i;
     umma_16_ts(d, p + 8 * ks, umma_desc_rows_sw128(v + ks * 16 * 128, kHalfBytes), idesc,
                (ks > 0 || accumulate) ? 1u : 0u);
+  }
 }
 
 // Four packed outputs at element i of an output row (16-byte stores for a caller that walks 8 / 4 elements).
@@ -277,12 +280,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   __shared__ int s_fail;
   __shared__ int s_range[8][4];
   __shared__ uint32_t s_bad[kVRing][4];  // keys of a guarded V tile that hold infinities or NaN
-  __shared__ float s_join[2][kTile];     // !PAIR: the second stream's reference and sum
-  __shared__ int s_join_bad[kTile];
   volatile int* fail = &s_fail;
   L sm;
   sm.base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int h = blockIdx.y, b = blockIdx.z;
   const int split = blockIdx.x % p.n_splits;
   const int m_blocks = gridDim.x / p.n_splits;
@@ -297,8 +298,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     }
     for (int w = 0; w < 2; ++w) {
       mbar_init(sm.sfull(w), 1);
-      mbar_init(sm.pready(w), 4);  // one arrival per softmax warp
-      mbar_init(sm.odone(w), 1);
+      mbar_init(sm.pready(w, 0), 4);  // one arrival per softmax warp
+      mbar_init(sm.pready(w, 1), 4);
+      mbar_init(sm.odone(w, 0), 1);
+      mbar_init(sm.odone(w, 1), 1);
     }
     for (int u = 0; u < kVRing; ++u) mbar_init(sm.vsafe(u), 2);
     mbar_init(sm.drain(), 1);
@@ -371,8 +374,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       all_lo[w] = max(all_lo[w], s_range[4 * w + i][2]);
       all_hi[w] = min(all_hi[w], s_range[4 * w + i][3]);
     }
-    t0[w] = hi > 0 ? lo / kTile : INT_MAX;
-    t1[w] = (hi + kTile - 1) / kTile;
+    t0[w] = __shfl_sync(0xffffffffu, hi > 0 ? lo / kTile : INT_MAX, 0);  // (the same in every lane: a uniform value)
+    t1[w] = __shfl_sync(0xffffffffu, (hi + kTile - 1) / kTile, 0);
+    all_lo[w] = __shfl_sync(0xffffffffu, all_lo[w], 0);
+    all_hi[w] = __shfl_sync(0xffffffffu, all_hi[w], 0);
   }
   // this CTA's share of the union of both streams' tiles
   int T0 = min(t0[0], t0[1]), T1 = max(t1[0], t1[1]);
@@ -434,77 +439,99 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         }
       }
     } else if (warp == kMmaWarp) {
-      if (lane == 0 && n > 0) {
+      if (n > 0) {  // the whole warp, converged; one lane issues
+        const bool leader = elect_one();
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         int done[2] = {0, 0};  // weights consumed per stream
+        auto commit = [&](uint32_t bar) {
+          if (leader) umma_commit(bar);
+        };
         auto wait_full = [&](int c) {
-          const bool ok = mbar_wait_role(sm.full(c % L::kStages), (c / L::kStages) & 1, fail);
+          const bool ok = mbar_wait_warp(sm.full(c % L::kStages), (c / L::kStages) & 1, fail);
           tcgen05_after_sync();
           return ok;
         };
         auto scores = [&](int w, int c) {
-          mma_scores<F16>(tmem + 128 * w, sm.q(PAIR ? w : 0), sm.stage(c % L::kStages));
-          umma_commit(sm.sfull(w));
+          const uint32_t q = sm.q(PAIR ? w : 0), k = sm.stage(c % L::kStages);
+          if (leader) {
+            mma_scores<F16>(tm + 128 * w, q, k);
+            umma_commit(sm.sfull(w));
+          }
         };
         auto values = [&](int w, int c) {
-          if (!mbar_wait_role(sm.pready(w), done[w] & 1, fail)) return false;
-          tcgen05_after_sync();
-          mma_values<F16>(tmem + 256 + 128 * w, tmem + 128 * w, sm.stage(c % L::kStages), done[w] > 0);
-          umma_commit(sm.odone(w));
-          ++done[w];
+          const uint32_t v = sm.stage(c % L::kStages);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            if (!mbar_wait_warp(sm.pready(w, half), of(done, w) & 1, fail)) return false;
+            tcgen05_after_sync();
+            if (leader) {
+              mma_values<F16>(tm + 256 + 128 * w, tm + 128 * w, v, half, of(done, w) > 0);
+              umma_commit(sm.odone(w, half));
+            }
+          }
+          done[w ? 1 : 0] += 1;
           return true;
         };
-        auto wait_safe = [&](int u) { return mbar_wait_role(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail); };
-        bool ok = mbar_wait_role(sm.qfull(), 0, fail) && wait_full(0);
+        auto wait_safe = [&](int u) { return mbar_wait_warp(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail); };
+        bool ok = mbar_wait_warp(sm.qfull(), 0, fail) && wait_full(0);
         if constexpr (PAIR) {
           if (ok) {
+#pragma unroll
             for (int w = 0; w < 2; ++w)
               if (active(w, T1 - 1)) scores(w, 0);
-            umma_commit(sm.empty(0));
+            commit(sm.empty(0));
           }
           for (int i = 0; ok && i < n; ++i) {
             const int j = T1 - 1 - i, cv = 2 * i + 1, ck = cv + 1;
             ok = wait_full(cv) && (!guarded(j) || wait_safe(i));
-            for (int w = 0; ok && w < 2; ++w) {
-              if (active(w, j)) ok = values(w, cv);
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              if (ok && active(w, j)) ok = values(w, cv);
               if (ok && i + 1 < n) {
                 if (w == 0) ok = wait_full(ck);
                 if (ok && active(w, j - 1)) scores(w, ck);
               }
             }
             if (ok) {
-              umma_commit(sm.empty(cv % L::kStages));
-              if (i + 1 < n) umma_commit(sm.empty(ck % L::kStages));
+              commit(sm.empty(cv % L::kStages));
+              if (i + 1 < n) commit(sm.empty(ck % L::kStages));
             }
           }
         } else {
           int c = 0;
-          for (int w = 0; ok && w < 2; ++w)
-            if (w < n) {
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+            if (ok && w < n) {
               if (w == 1) ok = wait_full(1);
               if (ok) {
                 scores(w, c);
-                umma_commit(sm.empty(c));
+                commit(sm.empty(c));
                 ++c;
               }
             }
-          for (int i = 0; ok && i < n_w[0]; ++i)
-            for (int w = 0; ok && w < 2; ++w)
-              if (i < of(n_w, w)) {
+          for (int i = 0; ok && i < of(n_w, 0); ++i) {
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+              if (ok && i < of(n_w, w)) {
                 ok = wait_full(c) && (!guarded(T1 - 1 - (2 * i + w)) || wait_safe(2 * i + w)) && values(w, c);
-                if (!ok) break;
-                umma_commit(sm.empty(c % L::kStages));
-                ++c;
-                if (i + 1 < of(n_w, w)) {
-                  ok = wait_full(c);
-                  if (!ok) break;
-                  scores(w, c);
-                  umma_commit(sm.empty(c % L::kStages));
+                if (ok) {
+                  commit(sm.empty(c % L::kStages));
                   ++c;
                 }
+                if (ok && i + 1 < of(n_w, w)) {
+                  ok = wait_full(c);
+                  if (ok) {
+                    scores(w, c);
+                    commit(sm.empty(c % L::kStages));
+                    ++c;
+                  }
+                }
               }
+          }
         }
-        umma_commit(sm.drain());  // every MMA issued has completed once this arrives
-        if (!mbar_wait(sm.drain(), 0)) record_error(a.status, kErrDrainTimeout);
+        commit(sm.drain());  // every MMA issued has completed once this arrives
+        if (!mbar_wait(sm.drain(), 0) && lane == 0) record_error(a.status, kErrDrainTimeout);
+        __syncwarp();
       }
     } else {  // guard warps
       int c = PAIR ? 1 : min(n, 2);  // ring position of V tile u
@@ -557,6 +584,12 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       ok = __all_sync(0xffffffffu, mbar_wait_role(sm.sfull(stream), it & 1, fail));
       if (!ok) break;
       tcgen05_after_sync();
+      auto arrive = [&](int half) {
+        tmem_wait_st();
+        tcgen05_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sm.pready(stream, half));
+      };
       if (k0 >= warp_hi || k0 + kTile <= warp_lo) {  // no row of this warp sees the tile
         if (any_valid) {  // (rows past the last token may hold anything)
           uint32_t zero[32];
@@ -564,107 +597,14 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           for (int e = 0; e < 32; ++e) zero[e] = 0u;
           tmem_st32(ts, zero);
           tmem_st32(ts + 32, zero);
-          tmem_wait_st();
         }
-        tcgen05_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sm.pready(stream));
+        arrive(0);
+        arrive(1);
         ++it;
         continue;
       }
       const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
       const int side = !BIAS ? 0 : k0 + kTile - 1 <= pos_min ? -1 : k0 >= pos_max ? 1 : 0;
-      uint32_t w[64];
-      float tile_sum = 0.f;
-      // 64 columns at a time: the weights of v[0 .. 63] (scores less the reference), packed, and their sums
-      auto pack_half = [&](const float (&v)[64], uint32_t* dst, uint64_t (&acc)[4]) {
-#pragma unroll
-        for (int e = 0; e < 64; e += 2) {
-          const float x = fast_exp2(v[e]), y = fast_exp2(v[e + 1]);
-          acc[(e >> 1) & 3] = add_f32x2(acc[(e >> 1) & 3], f32x2(x, y));
-          dst[e >> 1] = pack16<F16>(x, y);
-        }
-      };
-      auto total = [](const uint64_t (&acc)[4]) {
-        float s0, s1, s2, s3;
-        f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
-        f32x2_split(add_f32x2(acc[2], acc[3]), s2, s3);
-        return (s0 + s1) + (s2 + s3);
-      };
-      // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards.
-      bool slow = masked || careful;
-      if (!slow) {
-        float v[2][64];
-        uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
-        tmem_ld32(ts, v[0]);
-        tmem_ld32(ts + 32, v[0] + 32);
-        tmem_wait_ld(v[0]);
-        reg_fence(v[0] + 32);
-        tmem_ld32(ts + 64, v[1]);
-        tmem_ld32(ts + 96, v[1] + 32);
-        row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
-        pack_half(v[0], w, acc);
-        tmem_wait_ld(v[1]);
-        reg_fence(v[1] + 32);
-        row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
-        pack_half(v[1], w + 32, acc);
-        tile_sum = total(acc);
-        slow = __any_sync(0xffffffffu, !(tile_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
-      }
-      if (slow) {
-        float v[2][64];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(ts + 32 * c, v[c >> 1] + 32 * (c & 1));
-        tmem_wait_ld(v[0]);
-        reg_fence(v[0] + 32);
-        reg_fence(v[1]);
-        reg_fence(v[1] + 32);
-        float mx = -INFINITY;  // the row's largest score of this tile
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          if (CAP && masked) mask_scores<64>(v[c], row, k0 + 64 * c, 0.f);  // (they share a reciprocal)
-          row_scores<CAP, BIAS, 64>(v[c], sc, row, k0, 64 * c, 0.f, side);
-          if (masked) mask_scores<64>(v[c], row, k0 + 64 * c, -INFINITY);
-#pragma unroll
-          for (int e = 0; e < 64; e += 2) mx = max3(mx, v[c][e], v[c][e + 1]);
-        }
-        const float next = mx > ref + ref_slack<F16>() ? mx - ref_drop<F16>() : ref;
-        const bool moves = next != ref && ref != -INFINITY;
-        if (__any_sync(0xffffffffu, moves)) {
-          const float f = moves ? fast_exp2(ref - next) : 1.f;
-          if (it > 0) {
-            ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream), (it - 1) & 1, fail));
-            if (!ok) break;
-            tcgen05_after_sync();
-#pragma unroll 1
-            for (int c = 0; c < 8; ++c) {
-              float o[16];
-              tmem_ld16(to + 16 * c, o);
-              tmem_wait_ld16(o);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] *= f;
-              tmem_st16(to + 16 * c, reinterpret_cast<const uint32_t*>(o));
-            }
-          }
-          sum *= f;
-        }
-        ref = next;
-        careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
-        const float rr = ref == -INFINITY ? 0.f : ref;
-        const uint64_t r2 = f32x2(-rr, -rr);
-        uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-#pragma unroll
-          for (int e = 0; e < 64; e += 2)
-            f32x2_split(add_f32x2(f32x2(v[c][e], v[c][e + 1]), r2), v[c][e], v[c][e + 1]);
-          pack_half(v[c], w + 32 * c, acc);
-        }
-        tile_sum = total(acc);
-      }
-      sum += tile_sum;
-      tmem_st32(ts, w);
-      tmem_st32(ts + 32, w + 32);
       if (guarded(j)) {
         const int u = T1 - 1 - j;
         ok = __all_sync(0xffffffffu, mbar_wait_role(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail));
@@ -679,24 +619,107 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           }
         }
       }
-      tmem_wait_st();
-      tcgen05_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(sm.pready(stream));
+      // The weights of 64 columns, packed, and their sum: v holds the scores less the reference.
+      auto pack_half = [&](const float (&v)[64], uint32_t (&w)[32]) {
+        uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+        for (int e = 0; e < 64; e += 2) {
+          const float x = fast_exp2(v[e]), y = fast_exp2(v[e + 1]);
+          acc[(e >> 1) & 3] = add_f32x2(acc[(e >> 1) & 3], f32x2(x, y));
+          w[e >> 1] = pack16<F16>(x, y);
+        }
+        float s0, s1, s2, s3;
+        f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
+        f32x2_split(add_f32x2(acc[2], acc[3]), s2, s3);
+        return (s0 + s1) + (s2 + s3);
+      };
+      auto load_half = [&](int half, float (&v)[64]) {
+        tmem_ld32(ts + 64 * half, v);
+        tmem_ld32(ts + 64 * half + 32, v + 32);
+      };
+      auto loaded = [](float (&v)[64]) {
+        tmem_wait_ld(v);
+        reg_fence(v + 32);
+      };
+      float ahead[64];
+      load_half(0, ahead);
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        uint32_t w[32];
+        float half_sum = 0.f;
+        // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards.
+        bool slow = masked || careful;
+        loaded(ahead);
+        if (!slow) {
+          row_scores<CAP, BIAS, 64>(ahead, sc, row, k0, 64 * half, ref, side);
+          half_sum = pack_half(ahead, w);
+          slow = __any_sync(0xffffffffu, !(half_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
+        }
+        if (slow) {
+          float v[64];
+          load_half(half, v);
+          loaded(v);
+          if (CAP && masked) mask_scores<64>(v, row, k0 + 64 * half, 0.f);  // (four share a reciprocal)
+          row_scores<CAP, BIAS, 64>(v, sc, row, k0, 64 * half, 0.f, side);
+          if (masked) mask_scores<64>(v, row, k0 + 64 * half, -INFINITY);
+          float mx = -INFINITY, mx2 = -INFINITY;  // the row's largest score
+#pragma unroll
+          for (int e = 0; e < 64; e += 4) {
+            mx = max3(mx, v[e], v[e + 1]);
+            mx2 = max3(mx2, v[e + 2], v[e + 3]);
+          }
+          mx = fmaxf(mx, mx2);
+          const float next = mx > ref + ref_slack<F16>() ? mx - ref_drop<F16>() : ref;
+          const bool moves = next != ref && ref != -INFINITY;
+          if (__any_sync(0xffffffffu, moves)) {
+            const float f = moves ? fast_exp2(ref - next) : 1.f;
+            if (it + half > 0) {  // O holds the products up to the half before this one
+              ok = __all_sync(0xffffffffu,
+                              mbar_wait_role(sm.odone(stream, half ^ 1), (half ? it : it - 1) & 1, fail));
+              if (!ok) break;
+              tcgen05_after_sync();
+#pragma unroll 1
+              for (int c = 0; c < 8; ++c) {
+                float o[16];
+                tmem_ld16(to + 16 * c, o);
+                tmem_wait_ld16(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] *= f;
+                tmem_st16(to + 16 * c, reinterpret_cast<const uint32_t*>(o));
+              }
+            }
+            sum *= f;
+          }
+          ref = next;
+          careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
+          const float rr = ref == -INFINITY ? 0.f : ref;
+          const uint64_t r2 = f32x2(-rr, -rr);
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) f32x2_split(add_f32x2(f32x2(v[e], v[e + 1]), r2), v[e], v[e + 1]);
+          half_sum = pack_half(v, w);
+        }
+        if (half == 0) load_half(1, ahead);  // (its own columns: the weights of the first half lie over S's first 32)
+        sum += half_sum;
+        tmem_st32(ts + 32 * half, w);
+        arrive(half);
+      }
+      if (!ok) break;
       ++it;
     }
     if (ok && it > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream), (it - 1) & 1, fail));
+      ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, 1), (it - 1) & 1, fail));
       tcgen05_after_sync();
     }
     float g0 = 1.f, g1 = 0.f;  // factors of this stream's and the other stream's O
     const float* other = reinterpret_cast<const float*>(smem_raw + (sm.stage(0) - smem_u32(smem_raw))) + r;
+    // !PAIR: behind that O, the second stream's references, sums and marks
+    float* other_ref = reinterpret_cast<float*>(smem_raw + (sm.stage(2) - smem_u32(smem_raw))) + r;
     if constexpr (!PAIR) {  // the second stream hands its part over through the (now unused) ring
       named_bar_sync(1, kSoftThreads);  // every MMA of both streams is done
       if (stream == 1) {
-        s_join[0][r] = it > 0 ? ref : -INFINITY;
-        s_join[1][r] = it > 0 ? sum : 0.f;
-        s_join_bad[r] = bad_row;
+        other_ref[0] = it > 0 ? ref : -INFINITY;
+        other_ref[kTile] = it > 0 ? sum : 0.f;
+        other_ref[2 * kTile] = bad_row ? 1.f : 0.f;
         if (ok && it > 0) {
           float* to_first = const_cast<float*>(other);
 #pragma unroll
@@ -711,8 +734,8 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       }
       named_bar_sync(1, kSoftThreads);
       if (stream == 0) {
-        const float r1 = s_join[0][r], l1 = s_join[1][r];
-        bad_row = bad_row || s_join_bad[r];
+        const float r1 = other_ref[0], l1 = other_ref[kTile];
+        bad_row = bad_row || other_ref[2 * kTile] != 0.f;
         const float top = fmaxf(ref, r1);
         if (top > -INFINITY) {
           g0 = fast_exp2(ref - top);
