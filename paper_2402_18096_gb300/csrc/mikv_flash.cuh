@@ -54,7 +54,7 @@ constexpr int kSoftThreads = 256;
 constexpr int kCopyWarp = 8, kMmaWarp = 9, kGuardWarp = 10;
 constexpr int kThreads = 384;
 constexpr int kTmemCols = 512;                 // S0, S1, O0, O1
-constexpr int kVRing = 8;                      // guard results in flight (more than V tiles can be in the ring)
+constexpr int kSafeRing = 4;                   // guard results in flight (more than V tiles of a stream in the ring)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -62,7 +62,9 @@ template <bool PAIR>
 struct Layout {
   static constexpr int kQ = PAIR ? 2 : 1;          // query tiles in shared memory
   static constexpr int kStages = PAIR ? 5 : 6;     // K / V tiles in the ring
-  static constexpr int kBars = 1 + 2 * kStages + 5 * 2 + kVRing + 1;
+  // Loads: the first kLead K tiles, then V tile u and K tile u + kLead for u = 0, 1, ... (from the last key tile on).
+  static constexpr int kLead = PAIR ? 1 : 2;
+  static constexpr int kBars = 1 + 2 * kStages + 5 * 2 + 2 * kSafeRing + 1;
   static constexpr int kSmem = 1024 + (kQ + kStages) * kTileBytes + 8 * kBars;
   static_assert(kSmem <= 227 * 1024, "shared memory of one CTA");
   uint32_t base;
@@ -71,12 +73,13 @@ struct Layout {
   __device__ uint32_t bar(int i) const { return base + (kQ + kStages) * kTileBytes + 8 * i; }
   __device__ uint32_t qfull() const { return bar(0); }
   __device__ uint32_t full(int s) const { return bar(1 + s); }               // a copy landed
-  __device__ uint32_t empty(int s) const { return bar(1 + kStages + s); }    // its MMAs have read it
+  __device__ uint32_t empty(int s) const { return bar(1 + kStages + s); }    // it is not needed any more
   __device__ uint32_t sfull(int w) const { return bar(1 + 2 * kStages + w); }       // scores of stream w
   // of half a tile (64 keys): weights written (and O rescaled for them); O += P V done
   __device__ uint32_t pready(int w, int half) const { return bar(1 + 2 * kStages + 2 + 2 * w + half); }
   __device__ uint32_t odone(int w, int half) const { return bar(1 + 2 * kStages + 6 + 2 * w + half); }
-  __device__ uint32_t vsafe(int u) const { return bar(1 + 2 * kStages + 10 + u); }  // V tile u looked through
+  // guarded V tile looked through (PAIR: set 0 serves both streams)
+  __device__ uint32_t vsafe(int w, int g) const { return bar(1 + 2 * kStages + 10 + kSafeRing * w + g % kSafeRing); }
   __device__ uint32_t drain() const { return bar(kBars - 1); }
 };
 
@@ -279,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
   __shared__ int s_range[8][4];
-  __shared__ uint32_t s_bad[kVRing][4];  // keys of a guarded V tile that hold infinities or NaN
+  __shared__ uint32_t s_bad[2][kSafeRing][4];  // keys of a guarded V tile that hold infinities or NaN
   volatile int* fail = &s_fail;
   L sm;
   sm.base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     mbar_init(sm.qfull(), 1);
     for (int s = 0; s < L::kStages; ++s) {
       mbar_init(sm.full(s), 1);
-      mbar_init(sm.empty(s), 1);
+      mbar_init(sm.empty(s), 3);  // its MMAs, and both guard warps
     }
     for (int w = 0; w < 2; ++w) {
       mbar_init(sm.sfull(w), 1);
@@ -303,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       mbar_init(sm.odone(w, 0), 1);
       mbar_init(sm.odone(w, 1), 1);
     }
-    for (int u = 0; u < kVRing; ++u) mbar_init(sm.vsafe(u), 2);
+    for (int u = 0; u < 2 * kSafeRing; ++u) mbar_init(sm.vsafe(u / kSafeRing, u % kSafeRing), 2);
     mbar_init(sm.drain(), 1);
     fence_mbar_init();
   }
@@ -420,23 +423,13 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         };
         auto load_k = [&](int j) { return load(&p.map_k, j, p.k_head, p.k_batch); };
         auto load_v = [&](int j) { return load(&p.map_v, j, p.v_head, p.v_batch); };
-        bool ok = load_k(T1 - 1);
-        if constexpr (PAIR) {
-          for (int i = 0; ok && i < n; ++i) ok = load_v(T1 - 1 - i) && (i + 1 >= n || load_k(T1 - 2 - i));
-        } else {
-          if (ok && n > 1) ok = load_k(T1 - 2);
-          for (int i = 0; ok && i < n_w[0]; ++i)
-            for (int w = 0; ok && w < 2; ++w)
-              if (i < of(n_w, w)) {
-                const int j = T1 - 1 - (2 * i + w);
-                ok = load_v(j) && (i + 1 >= of(n_w, w) || load_k(j - 2));
-              }
-        }
-        if (*fail) {  // no copy may outlive the CTA
-          if (!mbar_wait(sm.qfull(), 0)) record_error(a.status, kErrDrainTimeout);
-          for (int s = 0; s < L::kStages; ++s)
-            if (last[s] >= 0 && !mbar_wait(sm.full(s), (last[s] / L::kStages) & 1)) record_error(a.status, kErrDrainTimeout);
-        }
+        bool ok = true;
+        for (int u = 0; ok && u < min(n, L::kLead); ++u) ok = load_k(T1 - 1 - u);
+        for (int u = 0; ok && u < n; ++u) ok = load_v(T1 - 1 - u) && (u + L::kLead >= n || load_k(T1 - 1 - u - L::kLead));
+        // no copy may outlive the CTA, whatever became of the other roles
+        if (!mbar_wait(sm.qfull(), 0)) record_error(a.status, kErrDrainTimeout);
+        for (int s = 0; s < L::kStages; ++s)
+          if (last[s] >= 0 && !mbar_wait(sm.full(s), (last[s] / L::kStages) & 1)) record_error(a.status, kErrDrainTimeout);
       }
     } else if (warp == kMmaWarp) {
       if (n > 0) {  // the whole warp, converged; one lane issues
@@ -472,7 +465,12 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           done[w ? 1 : 0] += 1;
           return true;
         };
-        auto wait_safe = [&](int u) { return mbar_wait_warp(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail); };
+        int checked[2] = {0, 0};  // guarded tiles so far (PAIR: in checked[0])
+        auto wait_safe = [&](int w) {
+          const int g = of(checked, w);
+          checked[w ? 1 : 0] += 1;
+          return mbar_wait_warp(sm.vsafe(w, g), (g / kSafeRing) & 1, fail);
+        };
         bool ok = mbar_wait_warp(sm.qfull(), 0, fail) && wait_full(0);
         if constexpr (PAIR) {
           if (ok) {
@@ -483,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           }
           for (int i = 0; ok && i < n; ++i) {
             const int j = T1 - 1 - i, cv = 2 * i + 1, ck = cv + 1;
-            ok = wait_full(cv) && (!guarded(j) || wait_safe(i));
+            ok = wait_full(cv) && (!guarded(j) || wait_safe(0));
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
               if (ok && active(w, j)) ok = values(w, cv);
@@ -513,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
 #pragma unroll
             for (int w = 0; w < 2; ++w)
               if (ok && i < of(n_w, w)) {
-                ok = wait_full(c) && (!guarded(T1 - 1 - (2 * i + w)) || wait_safe(2 * i + w)) && values(w, c);
+                ok = wait_full(c) && (!guarded(T1 - 1 - (2 * i + w)) || wait_safe(w)) && values(w, c);
                 if (ok) {
                   commit(sm.empty(c % L::kStages));
                   ++c;
@@ -533,18 +531,31 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         if (!mbar_wait(sm.drain(), 0) && lane == 0) record_error(a.status, kErrDrainTimeout);
         __syncwarp();
       }
-    } else {  // guard warps
-      int c = PAIR ? 1 : min(n, 2);  // ring position of V tile u
-      for (int u = 0; u < n; ++u) {
-        const int s = c % L::kStages, j = T1 - 1 - u;
-        if (!__all_sync(0xffffffffu, mbar_wait_role(sm.full(s), (c / L::kStages) & 1, fail))) break;
+    } else {  // guard warps: they see every load in order and release it too (a wait that left out phases of a barrier
+              // would take an earlier phase of the same parity for its own)
+      int checked[2] = {0, 0}, c = 0;
+      auto landed = [&]() { return mbar_wait_warp(sm.full(c % L::kStages), (c / L::kStages) & 1, fail); };
+      auto release = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sm.empty(c % L::kStages));
+        ++c;
+      };
+      bool ok = true;
+      for (int u = 0; ok && u < min(n, L::kLead); ++u) {
+        ok = landed();
+        if (ok) release();
+      }
+      for (int u = 0; ok && u < n; ++u) {
+        const int j = T1 - 1 - u, w = PAIR ? 0 : u & 1;
+        ok = landed();
+        if (!ok) break;
         if (guarded(j)) {
-          const int g = warp - kGuardWarp;
+          const int g = of(checked, w);
           bool wrote = false;
-#pragma unroll
-          for (int part = 0; part < 2; ++part) {
-            const int key = 64 * part + 32 * g + lane;
-            const uint32_t at = sm.stage(s) + key * 128;
+#pragma unroll 1
+          for (int part = warp - kGuardWarp; part < 4; part += 2) {
+            const int key = 32 * part + lane;
+            const uint32_t at = sm.stage(c % L::kStages) + key * 128;
             bool bad = false;
 #pragma unroll
             for (int q = 0; q < 16; ++q)
@@ -554,14 +565,18 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               for (int q = 0; q < 16; ++q) sts128_zero(at + (q >> 3) * kHalfBytes + ((q & 7) << 4));
               wrote = true;
             }
-            if (lane == 0) s_bad[u % kVRing][2 * part + g] = bits;
+            if (lane == 0) s_bad[w][g % kSafeRing][part] = bits;
           }
           if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
+          if (lane == 0) mbar_arrive(sm.vsafe(w, g));
+          checked[w ? 1 : 0] += 1;
         }
-        if (lane == 0) mbar_arrive(sm.vsafe(u % kVRing));
-        // to V tile u + 1: past the K tiles that are loaded between
-        c += PAIR ? 2 : 1 + (u / 2 + 1 < of(n_w, u & 1) ? 1 : 0);
+        release();
+        if (u + L::kLead < n) {
+          ok = landed();
+          if (ok) release();
+        }
       }
     }
   } else {  // softmax warps
@@ -576,9 +591,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     bool bad_row = false, ok = true;
     bool careful = true;  // some row of the warp has no reference yet, or one beyond kRefExact
     const bool any_valid = __any_sync(0xffffffffu, valid);
-    int it = 0;
+    int it = 0, guards = 0;  // tiles done, guarded tiles met
     for (int i = 0; i < (PAIR ? n : of(n_w, stream)); ++i) {
       const int j = T1 - 1 - (PAIR ? i : 2 * i + stream);
+      if (guarded(j)) ++guards;
       if (PAIR && !active(stream, j)) continue;
       const int k0 = j * kTile;
       ok = __all_sync(0xffffffffu, mbar_wait_role(sm.sfull(stream), it & 1, fail));
@@ -606,12 +622,12 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
       const int side = !BIAS ? 0 : k0 + kTile - 1 <= pos_min ? -1 : k0 >= pos_max ? 1 : 0;
       if (guarded(j)) {
-        const int u = T1 - 1 - j;
-        ok = __all_sync(0xffffffffu, mbar_wait_role(sm.vsafe(u % kVRing), (u / kVRing) & 1, fail));
+        const int g = guards - 1, ws = PAIR ? 0 : stream;
+        ok = __all_sync(0xffffffffu, mbar_wait_role(sm.vsafe(ws, g), (g / kSafeRing) & 1, fail));
         if (!ok) break;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          uint32_t bits = s_bad[u % kVRing][q];
+          uint32_t bits = s_bad[ws][g % kSafeRing][q];
           while (bits) {
             const int key = k0 + 32 * q + __ffs(bits) - 1;
             bits &= bits - 1;
@@ -641,21 +657,39 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         tmem_wait_ld(v);
         reg_fence(v + 32);
       };
-      float ahead[64];
-      load_half(0, ahead);
-#pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        uint32_t w[32];
-        float half_sum = 0.f;
-        // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards.
-        bool slow = masked || careful;
-        loaded(ahead);
+      // Fast path: no mask, a reference in every row. Straight-line code for the whole tile, checked by the sum
+      // afterwards; nothing is stored before the check.
+      bool slow = masked || careful;
+      if (!slow) {
+        float v[2][64];
+        uint32_t w[2][32];
+        load_half(0, v[0]);
+        loaded(v[0]);
+        load_half(1, v[1]);
+        row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
+        float tile_sum = pack_half(v[0], w[0]);
+        loaded(v[1]);
+        row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
+        tile_sum += pack_half(v[1], w[1]);
+        slow = __any_sync(0xffffffffu, !(tile_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
         if (!slow) {
-          row_scores<CAP, BIAS, 64>(ahead, sc, row, k0, 64 * half, ref, side);
-          half_sum = pack_half(ahead, w);
-          slow = __any_sync(0xffffffffu, !(half_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
+          sum += tile_sum;
+          tmem_st32(ts, w[0]);
+          tmem_st32(ts + 32, w[1]);
+          tmem_wait_st();
+          tcgen05_before_sync();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(sm.pready(stream, 0));
+            mbar_arrive(sm.pready(stream, 1));
+          }
         }
-        if (slow) {
+      }
+      // Slow path, 64 columns at a time: the largest score first, then the weights.
+      if (slow) {
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          uint32_t w[32];
           float v[64];
           load_half(half, v);
           loaded(v);
@@ -696,12 +730,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           const uint64_t r2 = f32x2(-rr, -rr);
 #pragma unroll
           for (int e = 0; e < 64; e += 2) f32x2_split(add_f32x2(f32x2(v[e], v[e + 1]), r2), v[e], v[e + 1]);
-          half_sum = pack_half(v, w);
+          sum += pack_half(v, w);
+          tmem_st32(ts + 32 * half, w);  // (over columns of S that both halves have left)
+          arrive(half);
         }
-        if (half == 0) load_half(1, ahead);  // (its own columns: the weights of the first half lie over S's first 32)
-        sum += half_sum;
-        tmem_st32(ts + 32 * half, w);
-        arrive(half);
       }
       if (!ok) break;
       ++it;
