@@ -69,7 +69,9 @@ mikv_status attn_common(int32_t dtype, int32_t out_dtype, int32_t batch, int32_t
   if (head_dim != kHeadDim) return MIKV_ERR_UNSUPPORTED;
   const int G = heads_q / heads_kv;
   if (G != 1 && G != 2 && G != 4 && G != 8) return MIKV_ERR_UNSUPPORTED;
-  if (batch > 65535 || heads_q > 65535 || tk > INT_MAX - 512 || tq > INT_MAX / 8 - 512) return MIKV_ERR_UNSUPPORTED;
+  if (batch > 65535 || heads_q > 65535 || tk > INT_MAX - 512 || tq > INT_MAX / 8 - 512 ||
+      !flash_fits(batch, heads_kv, G, tq))
+    return MIKV_ERR_UNSUPPORTED;
   return MIKV_OK;
 }
 

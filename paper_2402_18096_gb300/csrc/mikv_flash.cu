@@ -53,14 +53,19 @@ struct Plan {
   int m_blocks, n_splits;
 };
 
-// Splits a row block's key tiles may be cut into: enough that two rounds of CTAs could be filled, at least two tiles
-// each (so that both streams of a CTA have one).
+// Splits a row block's key tiles may be cut into: up to three rounds of CTAs (four splits at least, for lengths that
+// turn out ragged), and at least two tiles each, so that both streams of a CTA have one. Grows with `tiles` only, so
+// a workspace sized for the longest keys serves shorter ones.
 int most_splits(long long base, int tiles, int num_sms) {
-  const long long by_sms = 2ll * num_sms / base;
-  const long long s = by_sms < tiles / 2 ? by_sms : tiles / 2;
+  if (base >= 2ll * num_sms) return 1;
+  long long s = 3ll * num_sms / base;
+  s = s < 4 ? 4 : s;
+  s = s < tiles / 2 ? s : tiles / 2;
   return s < 1 ? 1 : (int)s;
 }
 
+// The number of splits that an estimate of the time makes shortest: rounds of items over the SMs, each a start and end
+// plus its key tiles, and for split rows the merge. The constants are measured (nanoseconds on an otherwise idle GB300).
 Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
   Plan p;
   const long long rows = (long long)tq * G;
@@ -68,12 +73,16 @@ Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
   p.m_blocks = (int)(p.pair ? (rows + 2 * kTile - 1) / (2 * kTile) : 1);
   const long long base = (long long)batch * heads_kv * p.m_blocks;
   const int tiles = (int)(((long long)tk + kTile - 1) / kTile);
-  // rounds of CTAs times the length of one: its tiles plus about four tiles' time of start and end
   p.n_splits = 1;
   double best = 1e300;
   for (int s = 1; s <= most_splits(base, tiles, num_sms); ++s) {
-    const double rounds = (double)((base * s + num_sms - 1) / num_sms);
-    const double cost = rounds * ((tiles + s - 1) / s + 4.0 + (s > 1 ? 1.0 : 0.0));
+    const long long items = base * s;
+    const double rounds = (double)((items + num_sms - 1) / num_sms);
+    const double busy = (double)(items < num_sms ? items : num_sms);
+    // a tile: the products and softmax, or its 64 KB at the SM's share of HBM
+    const double tile = p.pair ? 1650.0 : 9.7 * busy > 750.0 ? 9.7 * busy : 750.0;
+    const double merge = s > 1 ? 4500.0 + (double)s * rows * batch * heads_kv * kHeadDim * 8.0 / 5000.0 : 0.0;
+    const double cost = rounds * ((tiles + s - 1) / s * tile + 2500.0) + merge;
     if (cost < best) best = cost, p.n_splits = s;
   }
   return p;
@@ -94,22 +103,40 @@ __global__ void __launch_bounds__(128) merge_parts_kernel(const __grid_constant_
   const int lane = threadIdx.x & 31;
   grid_dependency_wait();
   if (row >= m.part_rows) return;
-  float top = -INFINITY;
-  for (int s = lane; s < m.n_splits; s += 32) top = fmaxf(top, m.part_lse[s * m.part_rows + row]);
+  float top = -INFINITY, mine = -INFINITY;  // lane s holds the sum of part s (of 32 at a time)
+  for (int s0 = 0; s0 < m.n_splits; s0 += 32) {
+    const float e = s0 + lane < m.n_splits ? m.part_lse[(s0 + lane) * m.part_rows + row] : -INFINITY;
+    if (s0 == 0) mine = e;
+    top = fmaxf(top, e);
+  }
 #pragma unroll
   for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   float sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < m.n_splits; ++s) {
-    const float e = m.part_lse[s * m.part_rows + row];
-    if (e == -INFINITY) continue;  // nothing seen
-    const float w = fast_exp2(e - top);
-    const float4 o = reinterpret_cast<const float4*>(m.part_o + (s * m.part_rows + row) * kHeadDim)[lane];
-    sum += w;
-    acc.x = fmaf(o.x, w, acc.x);
-    acc.y = fmaf(o.y, w, acc.y);
-    acc.z = fmaf(o.z, w, acc.z);
-    acc.w = fmaf(o.w, w, acc.w);
+  for (int s0 = 0; s0 < m.n_splits; s0 += 32) {
+    if (s0 > 0) mine = s0 + lane < m.n_splits ? m.part_lse[(s0 + lane) * m.part_rows + row] : -INFINITY;
+    const float w_mine = mine == -INFINITY ? 0.f : fast_exp2(mine - top);
+    const int n = min(32, m.n_splits - s0);
+    const float4* part = reinterpret_cast<const float4*>(m.part_o + (s0 * m.part_rows + row) * kHeadDim) + lane;
+    for (int s = 0; s < n; s += 8) {  // eight parts' loads in flight
+      float4 o[8];
+      float w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[i] = __shfl_sync(0xffffffffu, w_mine, min(s + i, 31));
+        if (s + i >= n) w[i] = 0.f;
+        // (the output of a part that has seen nothing may be anything)
+        o[i] = w[i] != 0.f ? __ldcs(part + (s + i) * m.part_rows * (kHeadDim / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sum += w[i];
+        acc.x = fmaf(o[i].x, w[i], acc.x);
+        acc.y = fmaf(o[i].y, w[i], acc.y);
+        acc.z = fmaf(o[i].z, w[i], acc.z);
+        acc.w = fmaf(o[i].w, w[i], acc.w);
+      }
+    }
   }
   float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
   float f0 = sum == 0.f ? 0.f : 1.f / sum, f1 = 0.f;
@@ -146,6 +173,11 @@ size_t flash_workspace_bytes(int batch, int heads_kv, int G, int tq, int tk, int
   return kWsHeader + (s > 1 ? (size_t)s * rows * (kHeadDim + 1) * sizeof(float) : 0);
 }
 
+bool flash_fits(int batch, int heads_kv, int G, int tq) {  // (with up to eight rounds of splits and a round of slack)
+  const double blocks = ((double)tq * G + 2 * kTile - 1) / (2 * kTile);
+  return (double)batch * heads_kv * blocks < 2.0e9 && (double)batch * tq * heads_kv * G < 8.0e9;
+}
+
 cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, int num_sms, cudaStream_t st) {
   const Plan plan = plan_flash(a.batch, a.heads_kv, a.G, a.tq, a.tk, num_sms);
   FlashKernelArgs p;
@@ -164,7 +196,15 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
         !encode_rows(&p.map_v, f16, a.v, {a.tk, a.heads_kv, a.batch}, {a.v_t, a.v_h, a.v_b}, box_k))
       return cudaErrorInvalidValue;
   }
-  const dim3 grid(plan.m_blocks * plan.n_splits, a.heads_kv, a.batch);
+  const int heads = a.batch * a.heads_kv;
+  p.m_blocks = plan.m_blocks;
+  p.n_items = heads * plan.m_blocks * plan.n_splits;
+  // heads worked on together: as many as have their keys and values in half of L2, and enough to occupy every SM
+  const long long l2_heads = (64ll << 20) / ((long long)a.tk * kHeadDim * 4 + 1) + 1;
+  const long long busy_heads = (num_sms + (long long)plan.m_blocks * plan.n_splits - 1) / ((long long)plan.m_blocks * plan.n_splits);
+  const long long group = l2_heads > busy_heads ? l2_heads : busy_heads;
+  p.group_heads = group < heads ? (int)group : heads;
+  const int grid = p.n_items < num_sms ? p.n_items : num_sms;
   cudaError_t e = f16 ? launch_flash_kernel<true>(p, plan.pair, grid, st) : launch_flash_kernel<false>(p, plan.pair, grid, st);
   if (e != cudaSuccess || plan.n_splits == 1) return e;
   const MergePartsArgs m = {a, p.part_o, p.part_lse, p.part_rows, plan.n_splits, p.out_kind};

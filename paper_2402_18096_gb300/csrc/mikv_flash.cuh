@@ -6,7 +6,12 @@
 // its positions, a shared prefix's tokens are its requests). The tq * G query rows of one KV head are packed into
 // tiles of 128 rows, row R = token * G + head, so that all heads and tokens that share keys share their loads.
 //
-// One CTA works on two streams, each with a score tile S (128 x 128 fp32) and an output tile O (128 x 128 fp32) in
+// Work. An item is a row tile (pair) of one KV head and set of keys, or one of n_splits shares of its key tiles; the
+// parts of split rows are merged by a second kernel. A persistent CTA per SM takes items in turn, and its roles run
+// ahead of one another across items: the next item's tiles are loaded and its first scores computed while the softmax
+// warps still write the last item's output. (Measured against a CTA per item: see the plan in mikv_flash.cu.)
+//
+// A CTA has two streams, each with a score tile S (128 x 128 fp32) and an output tile O (128 x 128 fp32) in
 // TMEM, over 128-key tiles of K and V that TMA stages in a ring:
 //   PAIR    two row tiles (256 rows) over the same key tiles: a K or V tile is loaded once for both.
 //   !PAIR   one row tile (up to 128 rows) over alternating key tiles; the streams' results are joined at the end.
@@ -14,7 +19,11 @@
 // Roles: warps 0-3 and 4-7 are the streams' softmax warpgroups (thread = row = TMEM lane), warp 8 issues the copies,
 // warp 9 the MMAs, warps 10-11 guard masked tiles (below). Per stream and tile: S = Q K^T (8 MMAs of K = 16), softmax
 // to P (16-bit, written over S in TMEM), O += P V (8 MMAs with A in TMEM). The MMA warp alternates streams, so one
-// stream's softmax runs under the other's products.
+// stream's softmax runs under the other's products. P lies over S and one warp issues all MMAs, which execute in the
+// order of issue: the next tile's scores may be issued right behind the product that reads P.
+//
+// Barriers. Every role that waits on a barrier sees each of its phases in order (a wait that left phases out would
+// take an earlier one of the same parity for its own); counters run on from item to item.
 //
 // Softmax. Weights are 2^(x - r) with x the score in log2 units and r a reference of the row: the largest x of the
 // first tile the row sees (less kRefDrop), moved only when a tile's sum of weights passes kSumMax, which rescales O. The
@@ -43,7 +52,7 @@
 namespace mikv {
 
 template <bool F16>
-cudaError_t launch_flash_kernel(const FlashKernelArgs& p, bool pair, dim3 grid, cudaStream_t st);
+cudaError_t launch_flash_kernel(const FlashKernelArgs& p, bool pair, int grid, cudaStream_t st);
 
 namespace flash {
 
@@ -60,26 +69,28 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 template <bool PAIR>
 struct Layout {
-  static constexpr int kQ = PAIR ? 2 : 1;          // query tiles in shared memory
-  static constexpr int kStages = PAIR ? 5 : 6;     // K / V tiles in the ring
-  // Loads: the first kLead K tiles, then V tile u and K tile u + kLead for u = 0, 1, ... (from the last key tile on).
+  static constexpr int kQ = PAIR ? 2 : 1;  // query tiles in shared memory
+  static constexpr int kStages = 5;        // K / V tiles in the ring
+  // Loads of an item: the first kLead K tiles, then V tile u and K tile u + kLead for u = 0, 1, ... (from the last
+  // key tile on).
   static constexpr int kLead = PAIR ? 1 : 2;
-  static constexpr int kBars = 1 + 2 * kStages + 5 * 2 + 2 * kSafeRing + 1;
+  static constexpr int kBars = 2 + 2 * kStages + 5 * 2 + 2 * kSafeRing + 1;
   static constexpr int kSmem = 1024 + (kQ + kStages) * kTileBytes + 8 * kBars;
-  static_assert(kSmem <= 227 * 1024, "shared memory of one CTA");
+  static_assert(kSmem <= 224 * 1024 + 2048, "shared memory of one CTA");
   uint32_t base;
   __device__ uint32_t q(int m) const { return base + m * kTileBytes; }
   __device__ uint32_t stage(int s) const { return base + (kQ + s) * kTileBytes; }
   __device__ uint32_t bar(int i) const { return base + (kQ + kStages) * kTileBytes + 8 * i; }
-  __device__ uint32_t qfull() const { return bar(0); }
-  __device__ uint32_t full(int s) const { return bar(1 + s); }               // a copy landed
-  __device__ uint32_t empty(int s) const { return bar(1 + kStages + s); }    // it is not needed any more
-  __device__ uint32_t sfull(int w) const { return bar(1 + 2 * kStages + w); }       // scores of stream w
+  __device__ uint32_t qfull() const { return bar(0); }                       // an item's queries landed
+  __device__ uint32_t qfree() const { return bar(1); }                       // its last scores have read them
+  __device__ uint32_t full(int s) const { return bar(2 + s); }               // a copy landed
+  __device__ uint32_t empty(int s) const { return bar(2 + kStages + s); }    // it is not needed any more
+  __device__ uint32_t sfull(int w) const { return bar(2 + 2 * kStages + w); }  // scores of stream w
   // of half a tile (64 keys): weights written (and O rescaled for them); O += P V done
-  __device__ uint32_t pready(int w, int half) const { return bar(1 + 2 * kStages + 2 + 2 * w + half); }
-  __device__ uint32_t odone(int w, int half) const { return bar(1 + 2 * kStages + 6 + 2 * w + half); }
+  __device__ uint32_t pready(int w, int half) const { return bar(4 + 2 * kStages + 2 * w + half); }
+  __device__ uint32_t odone(int w, int half) const { return bar(8 + 2 * kStages + 2 * w + half); }
   // guarded V tile looked through (PAIR: set 0 serves both streams)
-  __device__ uint32_t vsafe(int w, int g) const { return bar(1 + 2 * kStages + 10 + kSafeRing * w + g % kSafeRing); }
+  __device__ uint32_t vsafe(int w, int g) const { return bar(12 + 2 * kStages + kSafeRing * w + g % kSafeRing); }
   __device__ uint32_t drain() const { return bar(kBars - 1); }
 };
 
@@ -274,6 +285,120 @@ __device__ __forceinline__ void join_own(const FlashArgs& a, size_t row, float& 
   lse2 = top + log2f(w0 + w1);
 }
 
+// The keys that the tokens [tok0, tok1) of a set see: their union [lo, hi) (hi = 0: none), and what all of them see.
+struct Range {
+  int lo, hi, all_lo, all_hi;
+};
+
+// Whole warp, the same answer in every lane.
+__device__ __forceinline__ Range token_range(const FlashArgs& a, int b, int tok0, int tok1, int lane) {
+  Range r = {INT_MAX, 0, 0, INT_MAX};
+  if (tok0 >= tok1) return r;
+  int first = a.tk, last = a.tk;  // without spans: every token sees [0, its end), and the ends do not fall
+  if (a.spans) {
+    for (int t = tok0 + lane; t < tok1; t += 32) {
+      const int2 s = a.spans[(size_t)b * a.tq + t];
+      const int lo = max(s.x, 0), hi = min(s.y, a.tk);
+      const bool sees = hi > lo;
+      r.lo = min(r.lo, sees ? lo : INT_MAX);
+      r.hi = max(r.hi, sees ? hi : 0);
+      r.all_lo = max(r.all_lo, sees ? lo : INT_MAX);
+      r.all_hi = min(r.all_hi, sees ? hi : 0);
+    }
+    r.lo = __reduce_min_sync(0xffffffffu, r.lo);
+    r.hi = __reduce_max_sync(0xffffffffu, r.hi);
+    r.all_lo = __reduce_max_sync(0xffffffffu, r.all_lo);
+    r.all_hi = __reduce_min_sync(0xffffffffu, r.all_hi);
+    return r;
+  }
+  if (a.lens) first = last = max(0, min(a.lens[b], a.tk));
+  if (a.causal) {
+    first = (int)min((long long)first, max(0ll, (long long)a.q_start + tok0 + 1));
+    last = (int)min((long long)last, max(0ll, (long long)a.q_start + tok1));
+  }
+  r.lo = last > 0 ? 0 : INT_MAX;
+  r.hi = last;
+  r.all_lo = first > 0 ? 0 : INT_MAX;
+  r.all_hi = first;
+  return r;
+}
+
+// One item of work: its place, per stream the key tiles [t0, t1) that some row sees and the keys that every row sees, and
+// this item's share [T0, T1) of the union of both streams' tiles.
+template <bool PAIR>
+struct Item {
+  int b, h, m_block, split;
+  int t0[2], t1[2], all_lo[2], all_hi[2];
+  int T0, T1, n;
+  __device__ static int of(const int (&x)[2], int w) { return w ? x[1] : x[0]; }
+  __device__ bool active(int w, int j) const { return !PAIR || (j >= of(t0, w) && j < of(t1, w)); }
+  __device__ bool cut(int w, int j) const { return j * kTile < of(all_lo, w) || (j + 1) * kTile > of(all_hi, w); }
+  __device__ bool guarded(int j) const {
+    return PAIR ? (active(0, j) && cut(0, j)) || (active(1, j) && cut(1, j)) : cut(0, j);
+  }
+  __device__ int tiles_of(int w) const { return PAIR ? n : w ? n / 2 : (n + 1) / 2; }  // visited by stream w
+};
+
+// Item number `index` (whole warp). Heads go in groups whose keys fit in L2 together; within a group a causal prompt's
+// longest rows come first.
+template <bool PAIR>
+__device__ __forceinline__ Item<PAIR> item_at(const FlashKernelArgs& p, int index, int lane) {
+  const FlashArgs& a = p.a;
+  Item<PAIR> x;
+  const int heads = a.batch * a.heads_kv, per_group = p.group_heads * p.m_blocks * p.n_splits;
+  const int group = index / per_group;
+  int rest = index - group * per_group;
+  const int here = min(p.group_heads, heads - group * p.group_heads) * p.n_splits;
+  const int rank = rest / here;
+  rest -= rank * here;
+  const int bh = group * p.group_heads + rest / p.n_splits;
+  x.split = rest % p.n_splits;
+  x.b = bh / a.heads_kv;
+  x.h = bh - x.b * a.heads_kv;
+  x.m_block = p.m_blocks - 1 - rank;
+  const int toks = kTile / a.G;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    if (!PAIR && w == 1) {
+      x.t0[1] = x.t0[0], x.t1[1] = x.t1[0], x.all_lo[1] = x.all_lo[0], x.all_hi[1] = x.all_hi[0];
+      continue;
+    }
+    const int tok0 = (PAIR ? 2 * x.m_block + w : x.m_block) * toks;
+    const Range g = token_range(a, x.b, tok0, min(tok0 + toks, a.tq), lane);
+    x.t0[w] = __shfl_sync(0xffffffffu, g.hi > 0 ? g.lo / kTile : INT_MAX, 0);  // (shuffled: known to be uniform)
+    x.t1[w] = __shfl_sync(0xffffffffu, (g.hi + kTile - 1) / kTile, 0);
+    x.all_lo[w] = __shfl_sync(0xffffffffu, g.all_lo, 0);
+    x.all_hi[w] = __shfl_sync(0xffffffffu, g.all_hi, 0);
+  }
+  x.T0 = min(x.t0[0], x.t0[1]);
+  x.T1 = max(x.t1[0], x.t1[1]);
+  if (x.T1 == 0) x.T0 = 0;
+  if (p.n_splits > 1) {
+    const int chunk = (x.T1 - x.T0 + p.n_splits - 1) / p.n_splits;
+    x.T0 = min(x.T1, x.T0 + x.split * chunk);
+    x.T1 = min(x.T1, x.T0 + chunk);
+  }
+  x.n = x.T1 - x.T0;
+  return x;
+}
+
+// Items of this CTA: one of every gridDim.x, alternately from the front and from the back of a round, which evens out
+// the lengths of a causal prompt's rows.
+__device__ __forceinline__ int item_index(int round) {
+  return round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+}
+
+// Barrier of the softmax warps that tells all of them whether one of them (or another role) has failed.
+__device__ __forceinline__ bool softmax_sync(bool failed) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)failed), "n"(kSoftThreads)
+      : "memory");
+  return any != 0;
+}
+
 template <bool F16, bool PAIR, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constant__ FlashKernelArgs p) {
   using L = Layout<PAIR>;
@@ -281,30 +406,28 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
-  __shared__ int s_range[8][4];
   __shared__ uint32_t s_bad[2][kSafeRing][4];  // keys of a guarded V tile that hold infinities or NaN
+  __shared__ float s_part[2][2][kTile];        // !PAIR: references and sums of both streams
+  __shared__ uint8_t s_mark[2][kTile];         // !PAIR: rows that saw an infinity or NaN
   volatile int* fail = &s_fail;
   L sm;
   sm.base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int h = blockIdx.y, b = blockIdx.z;
-  const int split = blockIdx.x % p.n_splits;
-  const int m_blocks = gridDim.x / p.n_splits;
-  const int m_block = m_blocks - 1 - (int)(blockIdx.x / p.n_splits);  // a causal prompt's longest rows first
 
   if (tid == 0) {
     s_fail = 0;
     mbar_init(sm.qfull(), 1);
+    mbar_init(sm.qfree(), 1);
     for (int s = 0; s < L::kStages; ++s) {
       mbar_init(sm.full(s), 1);
       mbar_init(sm.empty(s), 3);  // its MMAs, and both guard warps
     }
     for (int w = 0; w < 2; ++w) {
       mbar_init(sm.sfull(w), 1);
-      mbar_init(sm.pready(w, 0), 4);  // one arrival per softmax warp
-      mbar_init(sm.pready(w, 1), 4);
-      mbar_init(sm.odone(w, 0), 1);
-      mbar_init(sm.odone(w, 1), 1);
+      for (int half = 0; half < 2; ++half) {
+        mbar_init(sm.pready(w, half), 4);  // one arrival per softmax warp
+        mbar_init(sm.odone(w, half), 1);
+      }
     }
     for (int u = 0; u < 2 * kSafeRing; ++u) mbar_init(sm.vsafe(u / kSafeRing, u % kSafeRing), 2);
     mbar_init(sm.drain(), 1);
@@ -312,228 +435,188 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   }
   if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), kTmemCols);
   if (p.n_splits > 1) allow_dependent_launch();  // the merge may be scheduled; it waits for this grid's end
-
-  // this thread's row (softmax threads), and what the rows of each tile see
-  const int stream = (warp >> 2) & 1, r = tid & (kTile - 1);
-  const int R = (PAIR ? (2 * m_block + stream) : m_block) * kTile + r;
-  const int token = R / a.G, head = h * a.G + R % a.G;
-  const bool valid = warp < kCopyWarp && token < a.tq;
-  Row row;
-  row.lo = row.hi = 0;
-  row.pos = 0.f;
-  row.slope = 0.f;
-  int warp_lo = INT_MAX, warp_hi = 0, warp_all_lo = 0, warp_all_hi = 0, pos_min = 0, pos_max = 0;
-  if (warp < kCopyWarp) {
-    int at = 0;
-    if (valid) {
-      int len = a.tk;
-      row.hi = a.tk;
-      if (a.lens) len = row.hi = max(0, min(a.lens[b], a.tk));
-      if (a.spans) {
-        const int2 s = a.spans[(size_t)b * a.tq + token];
-        row.lo = max(s.x, 0);
-        row.hi = min(s.y, a.tk);
-      } else if (a.causal) {
-        row.hi = (int)min((long long)a.tk, max(0ll, (long long)a.q_start + token + 1));
-      }
-      if constexpr (BIAS) {
-        at = a.pos ? a.pos[(size_t)b * a.tq + token] : a.pos_at_len ? len : a.q_start + token;
-        row.pos = (float)at;
-        row.slope = a.slopes[head] * kLog2e;
-      }
-      if (row.hi <= row.lo) row.lo = row.hi = 0;
-    }
-    const bool sees = row.hi > row.lo;
-    warp_lo = __reduce_min_sync(0xffffffffu, sees ? row.lo : INT_MAX);
-    warp_hi = __reduce_max_sync(0xffffffffu, row.hi);
-    warp_all_lo = __reduce_max_sync(0xffffffffu, !valid ? 0 : sees ? row.lo : INT_MAX);
-    warp_all_hi = __reduce_min_sync(0xffffffffu, !valid ? INT_MAX : row.hi);
-    if (BIAS) {
-      pos_min = __reduce_min_sync(0xffffffffu, valid ? at : INT_MAX);
-      pos_max = __reduce_max_sync(0xffffffffu, valid ? at : INT_MIN);
-    }
-    if (lane == 0) {
-      s_range[warp][0] = warp_lo;
-      s_range[warp][1] = warp_hi;
-      s_range[warp][2] = warp_all_lo;
-      s_range[warp][3] = warp_all_hi;
-    }
-  }
   tcgen05_before_sync();
   __syncthreads();
   tcgen05_after_sync();
-  const uint32_t tmem = s_tmem;
-  // per stream: key tiles [t0, t1) that some row sees, keys [all_lo, all_hi) that every row sees
-  int t0[2], t1[2], all_lo[2], all_hi[2];
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    int lo = INT_MAX, hi = 0;
-    all_lo[w] = 0;
-    all_hi[w] = INT_MAX;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lo = min(lo, s_range[4 * w + i][0]);
-      hi = max(hi, s_range[4 * w + i][1]);
-      all_lo[w] = max(all_lo[w], s_range[4 * w + i][2]);
-      all_hi[w] = min(all_hi[w], s_range[4 * w + i][3]);
-    }
-    t0[w] = __shfl_sync(0xffffffffu, hi > 0 ? lo / kTile : INT_MAX, 0);  // (the same in every lane: a uniform value)
-    t1[w] = __shfl_sync(0xffffffffu, (hi + kTile - 1) / kTile, 0);
-    all_lo[w] = __shfl_sync(0xffffffffu, all_lo[w], 0);
-    all_hi[w] = __shfl_sync(0xffffffffu, all_hi[w], 0);
-  }
-  // this CTA's share of the union of both streams' tiles
-  int T0 = min(t0[0], t0[1]), T1 = max(t1[0], t1[1]);
-  if (T1 == 0) T0 = 0;
-  if (p.n_splits > 1) {
-    const int chunk = (T1 - T0 + p.n_splits - 1) / p.n_splits;
-    T0 = min(T1, T0 + split * chunk);
-    T1 = min(T1, T0 + chunk);
-  }
-  const int n = T1 - T0;
-  const int n_w[2] = {(n + 1) / 2, n / 2};  // !PAIR: tiles of each stream
-  auto of = [](const int(&x)[2], int w) { return w ? x[1] : x[0]; };
-  auto active = [&](int w, int j) { return j >= of(t0, w) && j < of(t1, w); };
-  auto cut = [&](int w, int j) { return j * kTile < of(all_lo, w) || (j + 1) * kTile > of(all_hi, w); };
-  auto guarded = [&](int j) { return PAIR ? (active(0, j) && cut(0, j)) || (active(1, j) && cut(1, j)) : cut(0, j); };
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
 
   // The softmax warps take the registers the other warpgroup does not need: 256 x 216 + 128 x 72 = 384 x 168.
   if (warp >= kCopyWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    int c = 0;        // loads so far
+    int running = 0;  // items with key tiles so far
     if (warp == kCopyWarp) {
-      if (lane == 0 && n > 0) {
-        int last[L::kStages];
-        for (int s = 0; s < L::kStages; ++s) last[s] = -1;
-        mbar_arrive_expect_tx(sm.qfull(), L::kQ * kTileBytes);
+      int last[L::kStages];  // the last load of each stage
 #pragma unroll
-        for (int m = 0; m < L::kQ; ++m) {
-          const int tok0 = (PAIR ? 2 * m_block + m : m_block) * (kTile / a.G);
-          tma_load_4d(sm.q(m), &p.map_q, 0, h * a.G, tok0, b, sm.qfull());
-          tma_load_4d(sm.q(m) + kHalfBytes, &p.map_q, 64, h * a.G, tok0, b, sm.qfull());
+      for (int s = 0; s < L::kStages; ++s) last[s] = -1;
+      bool ok = true;
+      for (int round = 0; ok; ++round) {
+        const int index = item_index(round);
+        if (index >= p.n_items) break;
+        const Item<PAIR> x = item_at<PAIR>(p, index, lane);
+        if (x.n == 0) continue;
+        if (lane == 0) {
+          auto load = [&](const CUtensorMap* map, int j, int hm, int bm) {
+            const int s = c % L::kStages;
+            if (c >= L::kStages && !mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail)) return false;
+            mbar_arrive_expect_tx(sm.full(s), kTileBytes);
+            tma_load_4d(sm.stage(s), map, 0, j * kTile, x.h * hm, x.b * bm, sm.full(s));
+            tma_load_4d(sm.stage(s) + kHalfBytes, map, 64, j * kTile, x.h * hm, x.b * bm, sm.full(s));
+#pragma unroll
+            for (int q = 0; q < L::kStages; ++q)
+              if (q == s) last[q] = c;
+            ++c;
+            return true;
+          };
+          auto load_k = [&](int j) { return load(&p.map_k, j, p.k_head, p.k_batch); };
+          auto load_v = [&](int j) { return load(&p.map_v, j, p.v_head, p.v_batch); };
+          for (int u = 0; ok && u < min(x.n, L::kLead); ++u) ok = load_k(x.T1 - 1 - u);
+          if (ok && running > 0) ok = mbar_wait_role(sm.qfree(), (running - 1) & 1, fail);
+          if (ok) {
+            mbar_arrive_expect_tx(sm.qfull(), L::kQ * kTileBytes);
+#pragma unroll
+            for (int m = 0; m < L::kQ; ++m) {
+              const int tok0 = (PAIR ? 2 * x.m_block + m : x.m_block) * (kTile / a.G);
+              tma_load_4d(sm.q(m), &p.map_q, 0, x.h * a.G, tok0, x.b, sm.qfull());
+              tma_load_4d(sm.q(m) + kHalfBytes, &p.map_q, 64, x.h * a.G, tok0, x.b, sm.qfull());
+            }
+            ++running;
+          }
+          for (int u = 0; ok && u < x.n; ++u)
+            ok = load_v(x.T1 - 1 - u) && (u + L::kLead >= x.n || load_k(x.T1 - 1 - u - L::kLead));
         }
-        int c = 0;
-        auto load = [&](const CUtensorMap* map, int j, int hm, int bm) {
-          const int s = c % L::kStages;
-          if (c >= L::kStages && !mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail)) return false;
-          mbar_arrive_expect_tx(sm.full(s), kTileBytes);
-          tma_load_4d(sm.stage(s), map, 0, j * kTile, h * hm, b * bm, sm.full(s));
-          tma_load_4d(sm.stage(s) + kHalfBytes, map, 64, j * kTile, h * hm, b * bm, sm.full(s));
-          last[s] = c++;
-          return true;
-        };
-        auto load_k = [&](int j) { return load(&p.map_k, j, p.k_head, p.k_batch); };
-        auto load_v = [&](int j) { return load(&p.map_v, j, p.v_head, p.v_batch); };
-        bool ok = true;
-        for (int u = 0; ok && u < min(n, L::kLead); ++u) ok = load_k(T1 - 1 - u);
-        for (int u = 0; ok && u < n; ++u) ok = load_v(T1 - 1 - u) && (u + L::kLead >= n || load_k(T1 - 1 - u - L::kLead));
-        // no copy may outlive the CTA, whatever became of the other roles
-        if (!mbar_wait(sm.qfull(), 0)) record_error(a.status, kErrDrainTimeout);
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+      }
+      if (lane == 0) {  // no copy may outlive the CTA, whatever became of the other roles
+        if (running > 0 && !mbar_wait(sm.qfull(), (running - 1) & 1)) record_error(a.status, kErrDrainTimeout);
+#pragma unroll
         for (int s = 0; s < L::kStages; ++s)
           if (last[s] >= 0 && !mbar_wait(sm.full(s), (last[s] / L::kStages) & 1)) record_error(a.status, kErrDrainTimeout);
       }
-    } else if (warp == kMmaWarp) {
-      if (n > 0) {  // the whole warp, converged; one lane issues
-        const bool leader = elect_one();
-        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-        int done[2] = {0, 0};  // weights consumed per stream
-        auto commit = [&](uint32_t bar) {
-          if (leader) umma_commit(bar);
-        };
-        auto wait_full = [&](int c) {
-          const bool ok = mbar_wait_warp(sm.full(c % L::kStages), (c / L::kStages) & 1, fail);
-          tcgen05_after_sync();
-          return ok;
-        };
-        auto scores = [&](int w, int c) {
-          const uint32_t q = sm.q(PAIR ? w : 0), k = sm.stage(c % L::kStages);
-          if (leader) {
-            mma_scores<F16>(tm + 128 * w, q, k);
-            umma_commit(sm.sfull(w));
-          }
-        };
-        auto values = [&](int w, int c) {
-          const uint32_t v = sm.stage(c % L::kStages);
+      __syncwarp();
+    } else if (warp == kMmaWarp) {  // the whole warp, converged; one lane issues
+      const bool leader = elect_one();
+      int tiles[2] = {0, 0};    // tiles of each stream whose weights were consumed
+      int checked[2] = {0, 0};  // guarded tiles (PAIR: in checked[0])
+      auto of = [](const int(&x)[2], int w) { return w ? x[1] : x[0]; };
+      auto commit = [&](uint32_t bar) {
+        if (leader) umma_commit(bar);
+      };
+      auto wait_full = [&](int load) {
+        const bool ok = mbar_wait_warp(sm.full(load % L::kStages), (load / L::kStages) & 1, fail);
+        tcgen05_after_sync();
+        return ok;
+      };
+      auto release = [&](int load) { commit(sm.empty(load % L::kStages)); };
+      auto scores = [&](int w, int load) {
+        const uint32_t q = sm.q(PAIR ? w : 0), k = sm.stage(load % L::kStages);
+        if (leader) {
+          mma_scores<F16>(tmem + 128 * w, q, k);
+          umma_commit(sm.sfull(w));
+        }
+      };
+      auto values = [&](int w, int load, bool first) {
+        const uint32_t v = sm.stage(load % L::kStages);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            if (!mbar_wait_warp(sm.pready(w, half), of(done, w) & 1, fail)) return false;
-            tcgen05_after_sync();
-            if (leader) {
-              mma_values<F16>(tm + 256 + 128 * w, tm + 128 * w, v, half, of(done, w) > 0);
-              umma_commit(sm.odone(w, half));
-            }
+        for (int half = 0; half < 2; ++half) {
+          if (!mbar_wait_warp(sm.pready(w, half), of(tiles, w) & 1, fail)) return false;
+          tcgen05_after_sync();
+          if (leader) {
+            mma_values<F16>(tmem + 256 + 128 * w, tmem + 128 * w, v, half, !first);
+            umma_commit(sm.odone(w, half));
           }
-          done[w ? 1 : 0] += 1;
-          return true;
-        };
-        int checked[2] = {0, 0};  // guarded tiles so far (PAIR: in checked[0])
-        auto wait_safe = [&](int w) {
-          const int g = of(checked, w);
-          checked[w ? 1 : 0] += 1;
-          return mbar_wait_warp(sm.vsafe(w, g), (g / kSafeRing) & 1, fail);
-        };
-        bool ok = mbar_wait_warp(sm.qfull(), 0, fail) && wait_full(0);
+        }
+        tiles[w ? 1 : 0] += 1;
+        return true;
+      };
+      auto wait_safe = [&](int w) {
+        const int g = of(checked, w);
+        checked[w ? 1 : 0] += 1;
+        return mbar_wait_warp(sm.vsafe(w, g), (g / kSafeRing) & 1, fail);
+      };
+      bool ok = true;
+      for (int round = 0; ok; ++round) {
+        const int index = item_index(round);
+        if (index >= p.n_items) break;
+        const Item<PAIR> x = item_at<PAIR>(p, index, lane);
+        const int n = x.n;
+        if (n == 0) continue;
+        ok = mbar_wait_warp(sm.qfull(), running & 1, fail);
+        ++running;
+        bool fresh[2] = {true, true};  // the stream's O holds nothing of this item yet
         if constexpr (PAIR) {
+          ok = ok && wait_full(c);
           if (ok) {
 #pragma unroll
             for (int w = 0; w < 2; ++w)
-              if (active(w, T1 - 1)) scores(w, 0);
-            commit(sm.empty(0));
+              if (x.active(w, x.T1 - 1)) scores(w, c);
+            release(c);
+            if (n == 1) commit(sm.qfree());
           }
           for (int i = 0; ok && i < n; ++i) {
-            const int j = T1 - 1 - i, cv = 2 * i + 1, ck = cv + 1;
-            ok = wait_full(cv) && (!guarded(j) || wait_safe(0));
+            const int j = x.T1 - 1 - i, cv = c + 1, ck = c + 2;
+            ok = wait_full(cv) && (!x.guarded(j) || wait_safe(0));
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-              if (ok && active(w, j)) ok = values(w, cv);
+              if (ok && x.active(w, j)) {
+                ok = values(w, cv, fresh[w]);
+                fresh[w] = false;
+              }
               if (ok && i + 1 < n) {
                 if (w == 0) ok = wait_full(ck);
-                if (ok && active(w, j - 1)) scores(w, ck);
+                if (ok && x.active(w, j - 1)) scores(w, ck);
               }
             }
             if (ok) {
-              commit(sm.empty(cv % L::kStages));
-              if (i + 1 < n) commit(sm.empty(ck % L::kStages));
+              release(cv);
+              if (i + 1 < n) release(ck);
+              if (i + 2 == n) commit(sm.qfree());
             }
+            c += 2;
           }
         } else {
-          int c = 0;
 #pragma unroll
           for (int w = 0; w < 2; ++w)
             if (ok && w < n) {
-              if (w == 1) ok = wait_full(1);
+              ok = wait_full(c);
               if (ok) {
                 scores(w, c);
-                commit(sm.empty(c));
+                release(c);
+                if (w + 1 == n) commit(sm.qfree());
                 ++c;
               }
             }
-          for (int i = 0; ok && i < of(n_w, 0); ++i) {
+          for (int i = 0; ok && 2 * i < n; ++i) {
 #pragma unroll
-            for (int w = 0; w < 2; ++w)
-              if (ok && i < of(n_w, w)) {
-                ok = wait_full(c) && (!guarded(T1 - 1 - (2 * i + w)) || wait_safe(w)) && values(w, c);
+            for (int w = 0; w < 2; ++w) {
+              const int u = 2 * i + w;
+              if (ok && u < n) {
+                ok = wait_full(c) && (!x.guarded(x.T1 - 1 - u) || wait_safe(w)) && values(w, c, fresh[w]);
+                fresh[w] = false;
                 if (ok) {
-                  commit(sm.empty(c % L::kStages));
+                  release(c);
                   ++c;
                 }
-                if (ok && i + 1 < of(n_w, w)) {
+                if (ok && u + 2 < n) {
                   ok = wait_full(c);
                   if (ok) {
                     scores(w, c);
-                    commit(sm.empty(c % L::kStages));
+                    release(c);
                     ++c;
                   }
                 }
+                if (ok && u + 3 == n) commit(sm.qfree());  // (the last scores were those of tile n - 1)
               }
+            }
           }
         }
-        commit(sm.drain());  // every MMA issued has completed once this arrives
-        if (!mbar_wait(sm.drain(), 0) && lane == 0) record_error(a.status, kErrDrainTimeout);
-        __syncwarp();
       }
-    } else {  // guard warps: they see every load in order and release it too (a wait that left out phases of a barrier
-              // would take an earlier phase of the same parity for its own)
-      int checked[2] = {0, 0}, c = 0;
+      commit(sm.drain());  // every MMA issued has completed once this arrives
+      if (!mbar_wait(sm.drain(), 0) && lane == 0) record_error(a.status, kErrDrainTimeout);
+      __syncwarp();
+    } else {  // guard warps: they see every load in order, look through guarded V tiles and release each load too
+      int checked[2] = {0, 0};
+      auto of = [](const int(&x)[2], int w) { return w ? x[1] : x[0]; };
       auto landed = [&]() { return mbar_wait_warp(sm.full(c % L::kStages), (c / L::kStages) & 1, fail); };
       auto release = [&]() {
         __syncwarp();
@@ -541,275 +624,325 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         ++c;
       };
       bool ok = true;
-      for (int u = 0; ok && u < min(n, L::kLead); ++u) {
-        ok = landed();
-        if (ok) release();
-      }
-      for (int u = 0; ok && u < n; ++u) {
-        const int j = T1 - 1 - u, w = PAIR ? 0 : u & 1;
-        ok = landed();
-        if (!ok) break;
-        if (guarded(j)) {
-          const int g = of(checked, w);
-          bool wrote = false;
-#pragma unroll 1
-          for (int part = warp - kGuardWarp; part < 4; part += 2) {
-            const int key = 32 * part + lane;
-            const uint32_t at = sm.stage(c % L::kStages) + key * 128;
-            bool bad = false;
-#pragma unroll
-            for (int q = 0; q < 16; ++q)
-              bad |= any_nonfinite<F16>(lds128(at + (q >> 3) * kHalfBytes + (((q & 7) ^ (key & 7)) << 4)));
-            const uint32_t bits = __ballot_sync(0xffffffffu, bad);
-            if (bad) {
-              for (int q = 0; q < 16; ++q) sts128_zero(at + (q >> 3) * kHalfBytes + ((q & 7) << 4));
-              wrote = true;
-            }
-            if (lane == 0) s_bad[w][g % kSafeRing][part] = bits;
-          }
-          if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(sm.vsafe(w, g));
-          checked[w ? 1 : 0] += 1;
-        }
-        release();
-        if (u + L::kLead < n) {
+      for (int round = 0; ok; ++round) {
+        const int index = item_index(round);
+        if (index >= p.n_items) break;
+        const Item<PAIR> x = item_at<PAIR>(p, index, lane);
+        const int n = x.n;
+        for (int u = 0; ok && u < min(n, L::kLead); ++u) {
           ok = landed();
           if (ok) release();
+        }
+        for (int u = 0; ok && u < n; ++u) {
+          const int j = x.T1 - 1 - u, w = PAIR ? 0 : u & 1;
+          ok = landed();
+          if (!ok) break;
+          if (x.guarded(j)) {
+            const int g = of(checked, w);
+            bool wrote = false;
+#pragma unroll 1
+            for (int part = warp - kGuardWarp; part < 4; part += 2) {
+              const int key = 32 * part + lane;
+              const uint32_t at = sm.stage(c % L::kStages) + key * 128;
+              bool bad = false;
+#pragma unroll
+              for (int q = 0; q < 16; ++q)
+                bad |= any_nonfinite<F16>(lds128(at + (q >> 3) * kHalfBytes + (((q & 7) ^ (key & 7)) << 4)));
+              const uint32_t bits = __ballot_sync(0xffffffffu, bad);
+              if (bad) {
+                for (int q = 0; q < 16; ++q) sts128_zero(at + (q >> 3) * kHalfBytes + ((q & 7) << 4));
+                wrote = true;
+              }
+              if (lane == 0) s_bad[w][g % kSafeRing][part] = bits;
+            }
+            if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sm.vsafe(w, g));
+            checked[w ? 1 : 0] += 1;
+          }
+          release();
+          if (u + L::kLead < n) {
+            ok = landed();
+            if (ok) release();
+          }
         }
       }
     }
   } else {  // softmax warps
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const int stream = warp >> 2, r = tid & (kTile - 1);
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t ts = tmem + 128 * stream + lanes, to = tmem + 256 + 128 * stream + lanes;
     Score sc;
     sc.scale = CAP ? 2.f * kLog2e * (a.sm_scale / a.softcap) : a.sm_scale * kLog2e;
     sc.cap = a.softcap * kLog2e;
-    // (a row that sees nothing, or past the last token, needs no reference: its weights are 0 or never used)
-    float ref = row.hi > row.lo ? -INFINITY : 0.f, sum = 0.f;
-    bool bad_row = false, ok = true;
-    bool careful = true;  // some row of the warp has no reference yet, or one beyond kRefExact
-    const bool any_valid = __any_sync(0xffffffffu, valid);
-    int it = 0, guards = 0;  // tiles done, guarded tiles met
-    for (int i = 0; i < (PAIR ? n : of(n_w, stream)); ++i) {
-      const int j = T1 - 1 - (PAIR ? i : 2 * i + stream);
-      if (guarded(j)) ++guards;
-      if (PAIR && !active(stream, j)) continue;
-      const int k0 = j * kTile;
-      ok = __all_sync(0xffffffffu, mbar_wait_role(sm.sfull(stream), it & 1, fail));
-      if (!ok) break;
-      tcgen05_after_sync();
-      auto arrive = [&](int half) {
-        tmem_wait_st();
-        tcgen05_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sm.pready(stream, half));
-      };
-      if (k0 >= warp_hi || k0 + kTile <= warp_lo) {  // no row of this warp sees the tile
-        if (any_valid) {  // (rows past the last token may hold anything)
-          uint32_t zero[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) zero[e] = 0u;
-          tmem_st32(ts, zero);
-          tmem_st32(ts + 32, zero);
+    int tiles = 0, guards = 0;  // tiles done and guarded tiles met, over all items
+    for (int round = 0;; ++round) {
+      const int index = item_index(round);
+      if (index >= p.n_items) break;
+      const Item<PAIR> x = item_at<PAIR>(p, index, lane);
+      // this thread's row
+      const int R = (PAIR ? 2 * x.m_block + stream : x.m_block) * kTile + r;
+      const int token = R / a.G, head = x.h * a.G + R % a.G;
+      const bool valid = token < a.tq;
+      Row row;
+      row.lo = row.hi = 0;
+      row.pos = 0.f;
+      row.slope = 0.f;
+      int at = 0;
+      if (valid) {
+        int len = a.tk;
+        row.hi = a.tk;
+        if (a.lens) len = row.hi = max(0, min(a.lens[x.b], a.tk));
+        if (a.spans) {
+          const int2 s = a.spans[(size_t)x.b * a.tq + token];
+          row.lo = max(s.x, 0);
+          row.hi = min(s.y, a.tk);
+        } else if (a.causal) {
+          row.hi = (int)min((long long)a.tk, max(0ll, (long long)a.q_start + token + 1));
         }
-        arrive(0);
-        arrive(1);
-        ++it;
-        continue;
+        if constexpr (BIAS) {
+          at = a.pos ? a.pos[(size_t)x.b * a.tq + token] : a.pos_at_len ? len : a.q_start + token;
+          row.pos = (float)at;
+          row.slope = a.slopes[head] * kLog2e;
+        }
+        if (row.hi <= row.lo) row.lo = row.hi = 0;
       }
-      const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
-      const int side = !BIAS ? 0 : k0 + kTile - 1 <= pos_min ? -1 : k0 >= pos_max ? 1 : 0;
-      if (guarded(j)) {
-        const int g = guards - 1, ws = PAIR ? 0 : stream;
-        ok = __all_sync(0xffffffffu, mbar_wait_role(sm.vsafe(ws, g), (g / kSafeRing) & 1, fail));
+      const bool sees = row.hi > row.lo;
+      const int warp_lo = __reduce_min_sync(0xffffffffu, sees ? row.lo : INT_MAX);
+      const int warp_hi = __reduce_max_sync(0xffffffffu, row.hi);
+      const int warp_all_lo = __reduce_max_sync(0xffffffffu, !valid ? 0 : sees ? row.lo : INT_MAX);
+      const int warp_all_hi = __reduce_min_sync(0xffffffffu, !valid ? INT_MAX : row.hi);
+      int pos_min = 0, pos_max = 0;
+      if (BIAS) {
+        pos_min = __reduce_min_sync(0xffffffffu, valid ? at : INT_MAX);
+        pos_max = __reduce_max_sync(0xffffffffu, valid ? at : INT_MIN);
+      }
+      const bool any_valid = __any_sync(0xffffffffu, valid);
+      // (a row that sees nothing, or past the last token, needs no reference: its weights are 0 or never used)
+      float ref = sees ? -INFINITY : 0.f, sum = 0.f;
+      bool bad_row = false, ok = true;
+      bool careful = true;  // some row of the warp has no reference yet, or one beyond kRefExact
+      int it = 0;           // tiles of this item done
+      for (int i = 0; i < x.tiles_of(stream); ++i) {
+        const int j = x.T1 - 1 - (PAIR ? i : 2 * i + stream);
+        const bool guarded = x.guarded(j);
+        if (guarded) ++guards;
+        if (!x.active(stream, j)) continue;
+        const int k0 = j * kTile;
+        ok = __all_sync(0xffffffffu, mbar_wait_role(sm.sfull(stream), tiles & 1, fail));
         if (!ok) break;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t bits = s_bad[ws][g % kSafeRing][q];
-          while (bits) {
-            const int key = k0 + 32 * q + __ffs(bits) - 1;
-            bits &= bits - 1;
-            bad_row = bad_row || (key >= row.lo && key < row.hi);
-          }
-        }
-      }
-      // The weights of 64 columns, packed, and their sum: v holds the scores less the reference.
-      auto pack_half = [&](const float (&v)[64], uint32_t (&w)[32]) {
-        uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
-#pragma unroll
-        for (int e = 0; e < 64; e += 2) {
-          const float x = fast_exp2(v[e]), y = fast_exp2(v[e + 1]);
-          acc[(e >> 1) & 3] = add_f32x2(acc[(e >> 1) & 3], f32x2(x, y));
-          w[e >> 1] = pack16<F16>(x, y);
-        }
-        float s0, s1, s2, s3;
-        f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
-        f32x2_split(add_f32x2(acc[2], acc[3]), s2, s3);
-        return (s0 + s1) + (s2 + s3);
-      };
-      auto load_half = [&](int half, float (&v)[64]) {
-        tmem_ld32(ts + 64 * half, v);
-        tmem_ld32(ts + 64 * half + 32, v + 32);
-      };
-      auto loaded = [](float (&v)[64]) {
-        tmem_wait_ld(v);
-        reg_fence(v + 32);
-      };
-      // Fast path: no mask, a reference in every row. Straight-line code for the whole tile, checked by the sum
-      // afterwards; nothing is stored before the check.
-      bool slow = masked || careful;
-      if (!slow) {
-        float v[2][64];
-        uint32_t w[2][32];
-        load_half(0, v[0]);
-        loaded(v[0]);
-        load_half(1, v[1]);
-        row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
-        float tile_sum = pack_half(v[0], w[0]);
-        loaded(v[1]);
-        row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
-        tile_sum += pack_half(v[1], w[1]);
-        slow = __any_sync(0xffffffffu, !(tile_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
-        if (!slow) {
-          sum += tile_sum;
-          tmem_st32(ts, w[0]);
-          tmem_st32(ts + 32, w[1]);
+        tcgen05_after_sync();
+        auto arrive = [&](int first, int n) {
           tmem_wait_st();
           tcgen05_before_sync();
           __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(sm.pready(stream, 0));
-            mbar_arrive(sm.pready(stream, 1));
+          if (lane == 0)
+            for (int half = first; half < first + n; ++half) mbar_arrive(sm.pready(stream, half));
+        };
+        if (k0 >= warp_hi || k0 + kTile <= warp_lo) {  // no row of this warp sees the tile
+          if (any_valid) {  // (rows past the last token may hold anything)
+            uint32_t zero[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) zero[e] = 0u;
+            tmem_st32(ts, zero);
+            tmem_st32(ts + 32, zero);
+          }
+          arrive(0, 2);
+          ++it;
+          ++tiles;
+          continue;
+        }
+        const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
+        const int side = !BIAS ? 0 : k0 + kTile - 1 <= pos_min ? -1 : k0 >= pos_max ? 1 : 0;
+        if (guarded) {
+          const int g = guards - 1, ws = PAIR ? 0 : stream;
+          ok = __all_sync(0xffffffffu, mbar_wait_role(sm.vsafe(ws, g), (g / kSafeRing) & 1, fail));
+          if (!ok) break;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint32_t bits = s_bad[ws][g % kSafeRing][q];
+            while (bits) {
+              const int key = k0 + 32 * q + __ffs(bits) - 1;
+              bits &= bits - 1;
+              bad_row = bad_row || (key >= row.lo && key < row.hi);
+            }
           }
         }
-      }
-      // Slow path, 64 columns at a time: the largest score first, then the weights.
-      if (slow) {
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          uint32_t w[32];
-          float v[64];
-          load_half(half, v);
-          loaded(v);
-          if (CAP && masked) mask_scores<64>(v, row, k0 + 64 * half, 0.f);  // (four share a reciprocal)
-          row_scores<CAP, BIAS, 64>(v, sc, row, k0, 64 * half, 0.f, side);
-          if (masked) mask_scores<64>(v, row, k0 + 64 * half, -INFINITY);
-          float mx = -INFINITY, mx2 = -INFINITY;  // the row's largest score
+        // The weights of 64 columns, packed, and their sum: v holds the scores less the reference.
+        auto pack_half = [&](const float (&v)[64], uint32_t (&w)[32]) {
+          uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-          for (int e = 0; e < 64; e += 4) {
-            mx = max3(mx, v[e], v[e + 1]);
-            mx2 = max3(mx2, v[e + 2], v[e + 3]);
+          for (int e = 0; e < 64; e += 2) {
+            const float y0 = fast_exp2(v[e]), y1 = fast_exp2(v[e + 1]);
+            acc[(e >> 1) & 3] = add_f32x2(acc[(e >> 1) & 3], f32x2(y0, y1));
+            w[e >> 1] = pack16<F16>(y0, y1);
           }
-          mx = fmaxf(mx, mx2);
-          const float next = mx > ref + ref_slack<F16>() ? mx - ref_drop<F16>() : ref;
-          const bool moves = next != ref && ref != -INFINITY;
-          if (__any_sync(0xffffffffu, moves)) {
-            const float f = moves ? fast_exp2(ref - next) : 1.f;
-            if (it + half > 0) {  // O holds the products up to the half before this one
-              ok = __all_sync(0xffffffffu,
-                              mbar_wait_role(sm.odone(stream, half ^ 1), (half ? it : it - 1) & 1, fail));
-              if (!ok) break;
-              tcgen05_after_sync();
+          float s0, s1, s2, s3;
+          f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
+          f32x2_split(add_f32x2(acc[2], acc[3]), s2, s3);
+          return (s0 + s1) + (s2 + s3);
+        };
+        auto load_half = [&](int half, float (&v)[64]) {
+          tmem_ld32(ts + 64 * half, v);
+          tmem_ld32(ts + 64 * half + 32, v + 32);
+        };
+        auto loaded = [](float (&v)[64]) {
+          tmem_wait_ld(v);
+          reg_fence(v + 32);
+        };
+        // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards; nothing is
+        // stored before the check. Without a cap the whole tile is handed over at once; with one, whose arithmetic
+        // takes longer, each half as it is ready, so that its product runs under the next half.
+        bool slow = masked || careful;
+        if (!CAP && !slow) {
+          float v[2][64];
+          uint32_t w[2][32];
+          load_half(0, v[0]);
+          loaded(v[0]);
+          load_half(1, v[1]);
+          row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
+          float tile_sum = pack_half(v[0], w[0]);
+          loaded(v[1]);
+          row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
+          tile_sum += pack_half(v[1], w[1]);
+          slow = __any_sync(0xffffffffu, !(tile_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
+          if (!slow) {
+            sum += tile_sum;
+            tmem_st32(ts, w[0]);
+            tmem_st32(ts + 32, w[1]);
+            arrive(0, 2);
+          }
+        }
+        if (CAP || slow) {
 #pragma unroll 1
-              for (int c = 0; c < 8; ++c) {
-                float o[16];
-                tmem_ld16(to + 16 * c, o);
-                tmem_wait_ld16(o);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] *= f;
-                tmem_st16(to + 16 * c, reinterpret_cast<const uint32_t*>(o));
+          for (int half = 0; half < 2; ++half) {
+            float v[64];
+            uint32_t w[32];
+            bool slow_half = slow || careful;
+            load_half(half, v);
+            loaded(v);
+            if (CAP && !slow_half) {
+              row_scores<CAP, BIAS, 64>(v, sc, row, k0, 64 * half, ref, side);
+              const float half_sum = pack_half(v, w);
+              slow_half = __any_sync(0xffffffffu, !(half_sum <= sum_max<F16>()));
+              if (slow_half) {
+                load_half(half, v);
+                loaded(v);
+              } else {
+                sum += half_sum;
               }
             }
-            sum *= f;
+            if (slow_half) {  // the largest score first, then the weights
+              if (CAP && masked) mask_scores<64>(v, row, k0 + 64 * half, 0.f);  // (four share a reciprocal)
+              row_scores<CAP, BIAS, 64>(v, sc, row, k0, 64 * half, 0.f, side);
+              if (masked) mask_scores<64>(v, row, k0 + 64 * half, -INFINITY);
+              float mx = -INFINITY, mx2 = -INFINITY;
+#pragma unroll
+              for (int e = 0; e < 64; e += 4) {
+                mx = max3(mx, v[e], v[e + 1]);
+                mx2 = max3(mx2, v[e + 2], v[e + 3]);
+              }
+              mx = fmaxf(mx, mx2);
+              const float next = mx > ref + ref_slack<F16>() ? mx - ref_drop<F16>() : ref;
+              const bool moves = next != ref && ref != -INFINITY;
+              if (__any_sync(0xffffffffu, moves)) {
+                const float f = moves ? fast_exp2(ref - next) : 1.f;
+                if (it + half > 0) {  // O holds the products up to the half before this one
+                  ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, half ^ 1),
+                                                              (half ? tiles : tiles - 1) & 1, fail));
+                  if (!ok) break;
+                  tcgen05_after_sync();
+#pragma unroll 1
+                  for (int q = 0; q < 8; ++q) {
+                    float o[16];
+                    tmem_ld16(to + 16 * q, o);
+                    tmem_wait_ld16(o);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] *= f;
+                    tmem_st16(to + 16 * q, reinterpret_cast<const uint32_t*>(o));
+                  }
+                }
+                sum *= f;
+              }
+              ref = next;
+              careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
+              const float rr = ref == -INFINITY ? 0.f : ref;
+              const uint64_t r2 = f32x2(-rr, -rr);
+#pragma unroll
+              for (int e = 0; e < 64; e += 2) f32x2_split(add_f32x2(f32x2(v[e], v[e + 1]), r2), v[e], v[e + 1]);
+              sum += pack_half(v, w);
+            }
+            tmem_st32(ts + 32 * half, w);  // (over columns of S that both halves have left)
+            arrive(half, 1);
           }
-          ref = next;
-          careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
-          const float rr = ref == -INFINITY ? 0.f : ref;
-          const uint64_t r2 = f32x2(-rr, -rr);
-#pragma unroll
-          for (int e = 0; e < 64; e += 2) f32x2_split(add_f32x2(f32x2(v[e], v[e + 1]), r2), v[e], v[e + 1]);
-          sum += pack_half(v, w);
-          tmem_st32(ts + 32 * half, w);  // (over columns of S that both halves have left)
-          arrive(half);
         }
+        if (!ok) break;
+        ++it;
+        ++tiles;
       }
-      if (!ok) break;
-      ++it;
-    }
-    if (ok && it > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, 1), (it - 1) & 1, fail));
-      tcgen05_after_sync();
-    }
-    float g0 = 1.f, g1 = 0.f;  // factors of this stream's and the other stream's O
-    const float* other = reinterpret_cast<const float*>(smem_raw + (sm.stage(0) - smem_u32(smem_raw))) + r;
-    // !PAIR: behind that O, the second stream's references, sums and marks
-    float* other_ref = reinterpret_cast<float*>(smem_raw + (sm.stage(2) - smem_u32(smem_raw))) + r;
-    if constexpr (!PAIR) {  // the second stream hands its part over through the (now unused) ring
-      named_bar_sync(1, kSoftThreads);  // every MMA of both streams is done
-      if (stream == 1) {
-        other_ref[0] = it > 0 ? ref : -INFINITY;
-        other_ref[kTile] = it > 0 ? sum : 0.f;
-        other_ref[2 * kTile] = bad_row ? 1.f : 0.f;
-        if (ok && it > 0) {
-          float* to_first = const_cast<float*>(other);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float v[32];
-            tmem_ld32(to + 32 * c, v);
-            tmem_wait_ld(v);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) to_first[(32 * c + e) * kTile] = v[e];
-          }
-        }
+      if (ok && it > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, 1), (tiles - 1) & 1, fail));
+        tcgen05_after_sync();
       }
-      named_bar_sync(1, kSoftThreads);
-      if (stream == 0) {
-        const float r1 = other_ref[0], l1 = other_ref[kTile];
-        bad_row = bad_row || other_ref[2 * kTile] != 0.f;
-        const float top = fmaxf(ref, r1);
-        if (top > -INFINITY) {
-          g0 = fast_exp2(ref - top);
-          g1 = fast_exp2(r1 - top);
-        }
-        sum = sum * g0 + l1 * g1;
+      // Output. PAIR: each thread its row of O. !PAIR: the streams hold two parts of the same rows, in the same
+      // TMEM lanes; each warpgroup joins one half of the channels.
+      float g0 = 1.f, g1 = 0.f;  // factors of the first (PAIR: its own) and the second stream's O
+      if constexpr (!PAIR) {
+        s_part[stream][0][r] = it > 0 ? ref : -INFINITY;
+        s_part[stream][1][r] = it > 0 ? sum : 0.f;
+        s_mark[stream][r] = bad_row;
+        tcgen05_before_sync();
+        if (softmax_sync(!ok || *fail)) break;  // (both streams' products are done)
+        tcgen05_after_sync();
+        const float r0 = s_part[0][0][r], r1 = s_part[1][0][r], l0 = s_part[0][1][r], l1 = s_part[1][1][r];
+        bad_row = s_mark[0][r] || s_mark[1][r];
+        const float top = fmaxf(r0, r1);
+        g0 = top == -INFINITY ? 0.f : fast_exp2(r0 - top);
+        g1 = top == -INFINITY ? 0.f : fast_exp2(r1 - top);
+        sum = l0 * g0 + l1 * g1;
         ref = top;
+      } else if (!ok) {
+        break;
       }
-    }
-    if ((PAIR || stream == 0) && ok && !*fail) {
-      const size_t out_row = ((size_t)b * a.tq + token) * a.heads_q + head;
+      const size_t out_row = ((size_t)x.b * a.tq + token) * a.heads_q + head;
       float lse2 = sum == 0.f ? -INFINITY : ref + log2f(sum);
       float f0 = sum == 0.f ? 0.f : 1.f / sum, f1 = 0.f;
-      const bool last = p.n_splits == 1;
-      if (last && a.own_out && valid) join_own(a, out_row, lse2, f0, f1);
+      const bool whole = p.n_splits == 1;
+      if (whole && a.own_out && valid) join_own(a, out_row, lse2, f0, f1);
       if (bad_row) f0 = __int_as_float(0x7fffffff);
-      g0 *= f0;
-      g1 *= f0;
       // (a row whose sum is 0 has seen nothing, or only scores of -inf: its O holds zeros or, never written, anything)
       const bool blank = f0 == 0.f;
-      const bool other_ran = !PAIR && n_w[1] > 0;
-      char* dst = last ? static_cast<char*>(a.out) +
-                             (b * a.o_b + head * a.o_h + token * a.o_t) * (p.out_kind == 2 ? 4 : 2)
-                       : reinterpret_cast<char*>(p.part_o + ((size_t)split * p.part_rows + out_row) * kHeadDim);
+      g0 *= f0;
+      g1 *= f0;
+      const uint32_t o0 = PAIR ? to : tmem + 256 + lanes;
+      const bool has0 = PAIR ? it > 0 : x.n > 0, has1 = !PAIR && x.n > 1;
+      char* dst = whole ? static_cast<char*>(a.out) +
+                              (x.b * a.o_b + head * a.o_h + token * a.o_t) * (p.out_kind == 2 ? 4 : 2)
+                        : reinterpret_cast<char*>(p.part_o + ((size_t)x.split * p.part_rows + out_row) * kHeadDim);
       const float* own = a.own_out + out_row * kHeadDim;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int q = 0; q < (PAIR ? 4 : 2); ++q) {
+        const int ch = 32 * (PAIR ? q : 2 * stream + q);
         float v[32];
-        if (it > 0) {
-          tmem_ld32(to + 32 * c, v);
+        if (has0) {
+          tmem_ld32(o0 + ch, v);
           tmem_wait_ld(v);
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          v[e] = blank ? 0.f : v[e] * g0;
-          if (other_ran && !blank) v[e] = fmaf(other[(32 * c + e) * kTile], g1, v[e]);
+        for (int e = 0; e < 32; ++e) v[e] = blank || !has0 ? 0.f : v[e] * g0;
+        if (has1) {
+          float v1[32];
+          tmem_ld32(o0 + 128 + ch, v1);
+          tmem_wait_ld(v1);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = blank ? 0.f : fmaf(v1[e], g1, v[e]);
         }
         if (valid) {
           if (f1 != 0.f) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
-              const float4 o = *reinterpret_cast<const float4*>(own + 32 * c + e);
+              const float4 o = *reinterpret_cast<const float4*>(own + ch + e);
               v[e] = fmaf(o.x, f1, v[e]);
               v[e + 1] = fmaf(o.y, f1, v[e + 1]);
               v[e + 2] = fmaf(o.z, f1, v[e + 2]);
@@ -817,14 +950,18 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             }
           }
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) store_out8(dst, last ? p.out_kind : 2, 32 * c + e, v + e);
+          for (int e = 0; e < 32; e += 8) store_out8(dst, whole ? p.out_kind : 2, ch + e, v + e);
         }
       }
-      if (valid) {
-        if (last)
-          store_stat(a, b * a.s_b + head * a.s_h + token * a.s_t, lse2);
+      if (valid && (PAIR || stream == 0)) {
+        if (whole)
+          store_stat(a, x.b * a.s_b + head * a.s_h + token * a.s_t, lse2);
         else
-          p.part_lse[(size_t)split * p.part_rows + out_row] = lse2;
+          p.part_lse[(size_t)x.split * p.part_rows + out_row] = lse2;
+      }
+      if constexpr (!PAIR) {  // both warpgroups have read both O before the next item's products overwrite them
+        tcgen05_before_sync();
+        if (softmax_sync(*fail)) break;
       }
     }
   }
@@ -839,7 +976,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
 }
 
 template <bool F16, bool PAIR>
-cudaError_t launch_variant(const FlashKernelArgs& p, dim3 grid, cudaStream_t st) {
+cudaError_t launch_variant(const FlashKernelArgs& p, int grid, cudaStream_t st) {
   const bool cap = p.a.softcap > 0.f, bias = p.a.slopes != nullptr;
   auto k = cap ? (bias ? flash_kernel<F16, PAIR, true, true> : flash_kernel<F16, PAIR, true, false>)
                : (bias ? flash_kernel<F16, PAIR, false, true> : flash_kernel<F16, PAIR, false, false>);

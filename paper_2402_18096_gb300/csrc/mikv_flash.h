@@ -39,7 +39,10 @@ struct FlashKernelArgs {
   CUtensorMap map_k, map_v;  // [batch][heads][keys][128], box 64 channels x 128 keys
   FlashArgs a;
   int k_batch, k_head, v_batch, v_head;  // 1, or 0 where the dimension is shared (zero stride)
-  int n_splits;         // CTAs that share a row tile's keys; their parts are merged
+  int n_splits;         // items that share a row tile's keys; their parts are merged
+  int m_blocks;         // row tiles (pairs) of one KV head
+  int n_items;          // batch * heads_kv * m_blocks * n_splits
+  int group_heads;      // (set, KV head) combinations whose items are worked on together
   int out_kind;         // 0 bf16, 1 fp16, 2 fp32
   float* part_o;        // [n_splits][part_rows][128] normalised outputs, row = (set * tq + token) * heads_q + head
   float* part_lse;      // [n_splits][part_rows] log2 of the sum of 2^x (-inf: nothing seen)
@@ -47,6 +50,7 @@ struct FlashKernelArgs {
 };
 
 size_t flash_workspace_bytes(int batch, int heads_kv, int G, int tq, int tk, int num_sms);
+bool flash_fits(int batch, int heads_kv, int G, int tq);  // the number of items stays in range
 cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, int num_sms, cudaStream_t st);
 
 }  // namespace mikv

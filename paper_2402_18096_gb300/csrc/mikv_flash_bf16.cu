@@ -4,7 +4,7 @@
 namespace mikv {
 
 template <>
-cudaError_t launch_flash_kernel<false>(const FlashKernelArgs& p, bool pair, dim3 grid, cudaStream_t st) {
+cudaError_t launch_flash_kernel<false>(const FlashKernelArgs& p, bool pair, int grid, cudaStream_t st) {
   return pair ? flash::launch_variant<false, true>(p, grid, st) : flash::launch_variant<false, false>(p, grid, st);
 }
 
