@@ -80,9 +80,9 @@ Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
     const double rounds = (double)((items + num_sms - 1) / num_sms);
     const double busy = (double)(items < num_sms ? items : num_sms);
     // a tile: the products and softmax, or its 64 KB at the SM's share of HBM
-    const double tile = p.pair ? 1650.0 : 9.7 * busy > 750.0 ? 9.7 * busy : 750.0;
+    const double tile = p.pair ? 1650.0 : 9.7 * busy > 950.0 ? 9.7 * busy : 950.0;
     const double merge = s > 1 ? 4500.0 + (double)s * rows * batch * heads_kv * kHeadDim * 8.0 / 5000.0 : 0.0;
-    const double cost = rounds * ((tiles + s - 1) / s * tile + 2500.0) + merge;
+    const double cost = rounds * ((tiles + s - 1) / s * tile + 2000.0) + merge;
     if (cost < best) best = cost, p.n_splits = s;
   }
   return p;
@@ -204,6 +204,13 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   const long long busy_heads = (num_sms + (long long)plan.m_blocks * plan.n_splits - 1) / ((long long)plan.m_blocks * plan.n_splits);
   const long long group = l2_heads > busy_heads ? l2_heads : busy_heads;
   p.group_heads = group < heads ? (int)group : heads;
+  p.log2_G = a.G == 1 ? 0 : a.G == 2 ? 1 : a.G == 4 ? 2 : 3;
+  const int over = heads % p.group_heads;
+  p.by_group.set(p.group_heads * plan.m_blocks * plan.n_splits);
+  p.by_rank.set(p.group_heads * plan.n_splits);
+  p.by_last.set((over ? over : p.group_heads) * plan.n_splits);
+  p.by_split.set(plan.n_splits);
+  p.by_head.set(a.heads_kv);
   const int grid = p.n_items < num_sms ? p.n_items : num_sms;
   cudaError_t e = f16 ? launch_flash_kernel<true>(p, plan.pair, grid, st) : launch_flash_kernel<false>(p, plan.pair, grid, st);
   if (e != cudaSuccess || plan.n_splits == 1) return e;

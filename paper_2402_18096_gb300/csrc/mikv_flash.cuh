@@ -17,7 +17,7 @@
 //   !PAIR   one row tile (up to 128 rows) over alternating key tiles; the streams' results are joined at the end.
 //           The second stream's loads and softmax overlap the first's, which keeps HBM busy when rows are few.
 // Roles: warps 0-3 and 4-7 are the streams' softmax warpgroups (thread = row = TMEM lane), warp 8 issues the copies,
-// warp 9 the MMAs, warps 10-11 guard masked tiles (below). Per stream and tile: S = Q K^T (8 MMAs of K = 16), softmax
+// warp 9 the MMAs, warp 10 guards masked tiles (below), warp 11 works out the coming items. Per stream and tile: S = Q K^T (8 MMAs of K = 16), softmax
 // to P (16-bit, written over S in TMEM), O += P V (8 MMAs with A in TMEM). The MMA warp alternates streams, so one
 // stream's softmax runs under the other's products. P lies over S and one warp issues all MMAs, which execute in the
 // order of issue: the next tile's scores may be issued right behind the product that reads P.
@@ -34,7 +34,7 @@
 //
 // Masks. Every row sees one span of keys [lo, hi). Tiles outside the union of the CTA's spans are not visited; tiles
 // inside every span are not masked. In the tiles between, a weight of 0 does not stop an infinity or NaN in V from
-// entering O (0 * inf), so the guard warps look through the V tile first: rows with such a value are set to 0 and
+// entering O (0 * inf), so the guard warp looks through the V tile first: rows with such a value are set to 0 and
 // their keys reported to the softmax threads, which mark the output rows that do see them.
 #pragma once
 
@@ -60,7 +60,9 @@ constexpr int kTile = 128;                     // query rows of a tile, keys of 
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kHalfBytes = kTileBytes / 2;     // one 64-channel box
 constexpr int kSoftThreads = 256;
-constexpr int kCopyWarp = 8, kMmaWarp = 9, kGuardWarp = 10;
+constexpr int kCopyWarp = 8, kMmaWarp = 9, kGuardWarp = 10, kItemWarp = 11;
+constexpr int kItemRing = 4;                   // items described ahead
+constexpr int kItemReaders = 11;               // warps that read an item's description: all but the one that writes it
 constexpr int kThreads = 384;
 constexpr int kTmemCols = 512;                 // S0, S1, O0, O1
 constexpr int kSafeRing = 4;                   // guard results in flight (more than V tiles of a stream in the ring)
@@ -74,7 +76,7 @@ struct Layout {
   // Loads of an item: the first kLead K tiles, then V tile u and K tile u + kLead for u = 0, 1, ... (from the last
   // key tile on).
   static constexpr int kLead = PAIR ? 1 : 2;
-  static constexpr int kBars = 2 + 2 * kStages + 5 * 2 + 2 * kSafeRing + 1;
+  static constexpr int kBars = 2 + 2 * kStages + 5 * 2 + 2 * kSafeRing + 2 * kItemRing + 1;
   static constexpr int kSmem = 1024 + (kQ + kStages) * kTileBytes + 8 * kBars;
   static_assert(kSmem <= 224 * 1024 + 2048, "shared memory of one CTA");
   uint32_t base;
@@ -91,7 +93,17 @@ struct Layout {
   __device__ uint32_t odone(int w, int half) const { return bar(8 + 2 * kStages + 2 * w + half); }
   // guarded V tile looked through (PAIR: set 0 serves both streams)
   __device__ uint32_t vsafe(int w, int g) const { return bar(12 + 2 * kStages + kSafeRing * w + g % kSafeRing); }
+  // an item's description written; read by every role
+  __device__ uint32_t itemfull(int i) const { return bar(12 + 2 * kStages + 2 * kSafeRing + i % kItemRing); }
+  __device__ uint32_t itemfree(int i) const { return bar(12 + 2 * kStages + 2 * kSafeRing + kItemRing + i % kItemRing); }
   __device__ uint32_t drain() const { return bar(kBars - 1); }
+  // Arrivals that complete a phase of barrier i.
+  __device__ static constexpr int arrivals(int i) {
+    if (i >= 2 + kStages && i < 2 + 2 * kStages) return 2;           // empty: its MMAs and the guard warp
+    if (i >= 4 + 2 * kStages && i < 8 + 2 * kStages) return 4;       // pready: the softmax warps of the stream
+    if (i >= 12 + 2 * kStages + 2 * kSafeRing + kItemRing && i < kBars - 1) return kItemReaders;  // itemfree
+    return 1;
+  }
 };
 
 // What the weights may grow to before the reference moves, and how far below a tile's largest score the reference is
@@ -247,18 +259,36 @@ __device__ __forceinline__ void mma_values(uint32_t d, uint32_t p, uint32_t v, i
   }
 }
 
-// Four packed outputs at element i of an output row (16-byte stores for a caller that walks 8 / 4 elements).
-__device__ __forceinline__ void store_out8(void* row, int out_kind, int i, const float* v) {
-  if (out_kind == 2) {
-    float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + i);
-    o[0] = make_float4(v[0], v[1], v[2], v[3]);
-    o[1] = make_float4(v[4], v[5], v[6], v[7]);
-  } else if (out_kind == 1) {
-    *reinterpret_cast<uint4*>(static_cast<__half*>(row) + i) =
-        make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+// 32 outputs at element i of an output row, in stores of a whole 32-byte sector where the row is aligned for it.
+__device__ __forceinline__ void store32(void* at, const uint32_t (&v)[8], bool aligned32) {
+  if (aligned32) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
   } else {
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(row) + i) =
-        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    static_cast<uint4*>(at)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    static_cast<uint4*>(at)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
+}
+__device__ __forceinline__ void store_out32(char* row, int out_kind, int i, const float (&v)[32]) {
+  const bool al = (reinterpret_cast<uintptr_t>(row) & 31) == 0;
+  uint32_t u[8];
+  if (out_kind == 2) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = __float_as_uint(v[8 * q + e]);
+      store32(row + 4 * (i + 8 * q), u, al);
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        u[e] = out_kind == 1 ? pack_f16(v[16 * q + 2 * e], v[16 * q + 2 * e + 1])
+                             : pack_bf16(v[16 * q + 2 * e], v[16 * q + 2 * e + 1]);
+      store32(row + 2 * (i + 16 * q), u, al);
+    }
   }
 }
 
@@ -285,51 +315,19 @@ __device__ __forceinline__ void join_own(const FlashArgs& a, size_t row, float& 
   lse2 = top + log2f(w0 + w1);
 }
 
-// The keys that the tokens [tok0, tok1) of a set see: their union [lo, hi) (hi = 0: none), and what all of them see.
-struct Range {
-  int lo, hi, all_lo, all_hi;
+// One item of work: its place, per stream the key tiles [t0, t1) that some row sees and the keys that every row sees, and
+// this item's share [T0, T1) of the union of both streams' tiles. As it lies in shared memory.
+struct alignas(16) ItemData {
+  int b, h, m_block, split;
+  int t0[2], t1[2];
+  int all_lo[2], all_hi[2];
+  int T0, T1;
+  int valid, unused;
 };
 
-// Whole warp, the same answer in every lane.
-__device__ __forceinline__ Range token_range(const FlashArgs& a, int b, int tok0, int tok1, int lane) {
-  Range r = {INT_MAX, 0, 0, INT_MAX};
-  if (tok0 >= tok1) return r;
-  int first = a.tk, last = a.tk;  // without spans: every token sees [0, its end), and the ends do not fall
-  if (a.spans) {
-    for (int t = tok0 + lane; t < tok1; t += 32) {
-      const int2 s = a.spans[(size_t)b * a.tq + t];
-      const int lo = max(s.x, 0), hi = min(s.y, a.tk);
-      const bool sees = hi > lo;
-      r.lo = min(r.lo, sees ? lo : INT_MAX);
-      r.hi = max(r.hi, sees ? hi : 0);
-      r.all_lo = max(r.all_lo, sees ? lo : INT_MAX);
-      r.all_hi = min(r.all_hi, sees ? hi : 0);
-    }
-    r.lo = __reduce_min_sync(0xffffffffu, r.lo);
-    r.hi = __reduce_max_sync(0xffffffffu, r.hi);
-    r.all_lo = __reduce_max_sync(0xffffffffu, r.all_lo);
-    r.all_hi = __reduce_min_sync(0xffffffffu, r.all_hi);
-    return r;
-  }
-  if (a.lens) first = last = max(0, min(a.lens[b], a.tk));
-  if (a.causal) {
-    first = (int)min((long long)first, max(0ll, (long long)a.q_start + tok0 + 1));
-    last = (int)min((long long)last, max(0ll, (long long)a.q_start + tok1));
-  }
-  r.lo = last > 0 ? 0 : INT_MAX;
-  r.hi = last;
-  r.all_lo = first > 0 ? 0 : INT_MAX;
-  r.all_hi = first;
-  return r;
-}
-
-// One item of work: its place, per stream the key tiles [t0, t1) that some row sees and the keys that every row sees, and
-// this item's share [T0, T1) of the union of both streams' tiles.
 template <bool PAIR>
-struct Item {
-  int b, h, m_block, split;
-  int t0[2], t1[2], all_lo[2], all_hi[2];
-  int T0, T1, n;
+struct Item : ItemData {
+  int n;
   __device__ static int of(const int (&x)[2], int w) { return w ? x[1] : x[0]; }
   __device__ bool active(int w, int j) const { return !PAIR || (j >= of(t0, w) && j < of(t1, w)); }
   __device__ bool cut(int w, int j) const { return j * kTile < of(all_lo, w) || (j + 1) * kTile > of(all_hi, w); }
@@ -339,46 +337,90 @@ struct Item {
   __device__ int tiles_of(int w) const { return PAIR ? n : w ? n / 2 : (n + 1) / 2; }  // visited by stream w
 };
 
-// Item number `index` (whole warp). Heads go in groups whose keys fit in L2 together; within a group a causal prompt's
-// longest rows come first.
+// Item number `index`, worked out by a whole warp (the same in every lane). Heads go in groups whose keys fit in L2
+// together; within a group a causal prompt's longest rows come first.
 template <bool PAIR>
-__device__ __forceinline__ Item<PAIR> item_at(const FlashKernelArgs& p, int index, int lane) {
+__device__ __forceinline__ ItemData item_at(const FlashKernelArgs& p, int index, int lane) {
   const FlashArgs& a = p.a;
-  Item<PAIR> x;
-  const int heads = a.batch * a.heads_kv, per_group = p.group_heads * p.m_blocks * p.n_splits;
-  const int group = index / per_group;
-  int rest = index - group * per_group;
-  const int here = min(p.group_heads, heads - group * p.group_heads) * p.n_splits;
-  const int rank = rest / here;
-  rest -= rank * here;
-  const int bh = group * p.group_heads + rest / p.n_splits;
-  x.split = rest % p.n_splits;
-  x.b = bh / a.heads_kv;
+  ItemData x;
+  const int group = p.by_group.div(index);
+  int rest = index - group * p.by_group.d;
+  const bool last = (group + 1) * p.group_heads > a.batch * a.heads_kv;  // (a smaller group)
+  const int rank = last ? p.by_last.div(rest) : p.by_rank.div(rest);
+  rest -= rank * (last ? p.by_last.d : p.by_rank.d);
+  const int in_group = p.by_split.div(rest);
+  x.split = rest - in_group * p.n_splits;
+  const int bh = group * p.group_heads + in_group;
+  x.b = p.by_head.div(bh);
   x.h = bh - x.b * a.heads_kv;
   x.m_block = p.m_blocks - 1 - rank;
+  x.valid = 1;
+  x.unused = 0;
   const int toks = kTile / a.G;
+  constexpr int W = PAIR ? 2 : 1;
+  // what the tokens of each tile see: their union [lo, hi) (hi = 0: none), and what all of them see
+  int lo[W], hi[W], all_lo[W], all_hi[W];
+  if (a.spans) {
+    int2 s[W][4];  // up to 128 tokens of a tile, four to a lane; all loads in flight
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = lane + 32 * i, t = (PAIR ? 2 * x.m_block + w : x.m_block) * toks + at;
+        if (at < toks && t < a.tq) s[w][i] = __ldg(a.spans + (size_t)x.b * a.tq + t);
+      }
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      lo[w] = INT_MAX, hi[w] = 0, all_lo[w] = 0, all_hi[w] = INT_MAX;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = lane + 32 * i;
+        if (at >= toks || (PAIR ? 2 * x.m_block + w : x.m_block) * toks + at >= a.tq) continue;
+        const int l = max(s[w][i].x, 0), h = min(s[w][i].y, a.tk);
+        const bool sees = h > l;
+        lo[w] = min(lo[w], sees ? l : INT_MAX);
+        hi[w] = max(hi[w], sees ? h : 0);
+        all_lo[w] = max(all_lo[w], sees ? l : INT_MAX);
+        all_hi[w] = min(all_hi[w], sees ? h : 0);
+      }
+      lo[w] = __reduce_min_sync(0xffffffffu, lo[w]);
+      hi[w] = __reduce_max_sync(0xffffffffu, hi[w]);
+      all_lo[w] = __reduce_max_sync(0xffffffffu, all_lo[w]);
+      all_hi[w] = __reduce_min_sync(0xffffffffu, all_hi[w]);
+    }
+  } else {
+    const int len = a.lens ? max(0, min(a.lens[x.b], a.tk)) : a.tk;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {  // every token sees [0, its end), and the ends do not fall
+      const int tok0 = (PAIR ? 2 * x.m_block + w : x.m_block) * toks, tok1 = min(tok0 + toks, a.tq);
+      int first = len, end = len;
+      if (a.causal) {
+        first = (int)min((long long)len, max(0ll, (long long)a.q_start + tok0 + 1));
+        end = (int)min((long long)len, max(0ll, (long long)a.q_start + tok1));
+      }
+      const bool any = tok0 < tok1;
+      lo[w] = any && end > 0 ? 0 : INT_MAX;
+      hi[w] = any ? end : 0;
+      all_lo[w] = any && first == 0 ? INT_MAX : 0;
+      all_hi[w] = any ? first : INT_MAX;
+    }
+  }
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    if (!PAIR && w == 1) {
-      x.t0[1] = x.t0[0], x.t1[1] = x.t1[0], x.all_lo[1] = x.all_lo[0], x.all_hi[1] = x.all_hi[0];
-      continue;
-    }
-    const int tok0 = (PAIR ? 2 * x.m_block + w : x.m_block) * toks;
-    const Range g = token_range(a, x.b, tok0, min(tok0 + toks, a.tq), lane);
-    x.t0[w] = __shfl_sync(0xffffffffu, g.hi > 0 ? g.lo / kTile : INT_MAX, 0);  // (shuffled: known to be uniform)
-    x.t1[w] = __shfl_sync(0xffffffffu, (g.hi + kTile - 1) / kTile, 0);
-    x.all_lo[w] = __shfl_sync(0xffffffffu, g.all_lo, 0);
-    x.all_hi[w] = __shfl_sync(0xffffffffu, g.all_hi, 0);
+    const int v = w < W ? w : 0;
+    x.t0[w] = hi[v] > 0 ? lo[v] / kTile : INT_MAX;
+    x.t1[w] = (hi[v] + kTile - 1) / kTile;
+    x.all_lo[w] = all_lo[v];
+    x.all_hi[w] = all_hi[v];
   }
   x.T0 = min(x.t0[0], x.t0[1]);
   x.T1 = max(x.t1[0], x.t1[1]);
   if (x.T1 == 0) x.T0 = 0;
   if (p.n_splits > 1) {
-    const int chunk = (x.T1 - x.T0 + p.n_splits - 1) / p.n_splits;
+    const int chunk = p.by_split.div(x.T1 - x.T0 + p.n_splits - 1);
     x.T0 = min(x.T1, x.T0 + x.split * chunk);
     x.T1 = min(x.T1, x.T0 + chunk);
   }
-  x.n = x.T1 - x.T0;
   return x;
 }
 
@@ -406,6 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
+  __shared__ ItemData s_item[kItemRing];
   __shared__ uint32_t s_bad[2][kSafeRing][4];  // keys of a guarded V tile that hold infinities or NaN
   __shared__ float s_part[2][2][kTile];        // !PAIR: references and sums of both streams
   __shared__ uint8_t s_mark[2][kTile];         // !PAIR: rows that saw an infinity or NaN
@@ -414,31 +457,32 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   sm.base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
-  if (tid == 0) {
-    s_fail = 0;
-    mbar_init(sm.qfull(), 1);
-    mbar_init(sm.qfree(), 1);
-    for (int s = 0; s < L::kStages; ++s) {
-      mbar_init(sm.full(s), 1);
-      mbar_init(sm.empty(s), 3);  // its MMAs, and both guard warps
-    }
-    for (int w = 0; w < 2; ++w) {
-      mbar_init(sm.sfull(w), 1);
-      for (int half = 0; half < 2; ++half) {
-        mbar_init(sm.pready(w, half), 4);  // one arrival per softmax warp
-        mbar_init(sm.odone(w, half), 1);
-      }
-    }
-    for (int u = 0; u < 2 * kSafeRing; ++u) mbar_init(sm.vsafe(u / kSafeRing, u % kSafeRing), 2);
-    mbar_init(sm.drain(), 1);
-    fence_mbar_init();
-  }
+  if (tid < L::kBars) mbar_init(sm.bar(tid), L::arrivals(tid));
+  if (tid == 0) s_fail = 0;
+  fence_mbar_init();
   if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), kTmemCols);
+  if (tid == 32 * kCopyWarp) {
+    prefetch_tensormap(&p.map_q);
+    prefetch_tensormap(&p.map_k);
+    prefetch_tensormap(&p.map_v);
+  }
   if (p.n_splits > 1) allow_dependent_launch();  // the merge may be scheduled; it waits for this grid's end
   tcgen05_before_sync();
   __syncthreads();
   tcgen05_after_sync();
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+  // The description of the item of a round (uniform); false when a wait gave up.
+  auto next_item = [&](int round, Item<PAIR>& x) {
+    const bool ok = mbar_wait_warp(sm.itemfull(round), (round / kItemRing) & 1, fail);
+    const int* d = reinterpret_cast<const int*>(&s_item[round % kItemRing]);
+    int* to = reinterpret_cast<int*>(static_cast<ItemData*>(&x));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(ItemData) / 4); ++i) to[i] = __shfl_sync(0xffffffffu, d[i], 0);
+    x.n = x.T1 - x.T0;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(sm.itemfree(round));
+    return ok;
+  };
 
   // The softmax warps take the registers the other warpgroup does not need: 256 x 216 + 128 x 72 = 384 x 168.
   if (warp >= kCopyWarp) {
@@ -450,10 +494,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
 #pragma unroll
       for (int s = 0; s < L::kStages; ++s) last[s] = -1;
       bool ok = true;
+      Item<PAIR> x;
       for (int round = 0; ok; ++round) {
-        const int index = item_index(round);
-        if (index >= p.n_items) break;
-        const Item<PAIR> x = item_at<PAIR>(p, index, lane);
+        ok = next_item(round, x);
+        if (!ok || !x.valid) break;
         if (x.n == 0) continue;
         if (lane == 0) {
           auto load = [&](const CUtensorMap* map, int j, int hm, int bm) {
@@ -535,10 +579,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         return mbar_wait_warp(sm.vsafe(w, g), (g / kSafeRing) & 1, fail);
       };
       bool ok = true;
+      Item<PAIR> x;
       for (int round = 0; ok; ++round) {
-        const int index = item_index(round);
-        if (index >= p.n_items) break;
-        const Item<PAIR> x = item_at<PAIR>(p, index, lane);
+        ok = next_item(round, x);
+        if (!ok || !x.valid) break;
         const int n = x.n;
         if (n == 0) continue;
         ok = mbar_wait_warp(sm.qfull(), running & 1, fail);
@@ -614,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       commit(sm.drain());  // every MMA issued has completed once this arrives
       if (!mbar_wait(sm.drain(), 0) && lane == 0) record_error(a.status, kErrDrainTimeout);
       __syncwarp();
-    } else {  // guard warps: they see every load in order, look through guarded V tiles and release each load too
+    } else if (warp == kGuardWarp) {  // it sees every load in order, looks through guarded V tiles, releases each load too
       int checked[2] = {0, 0};
       auto of = [](const int(&x)[2], int w) { return w ? x[1] : x[0]; };
       auto landed = [&]() { return mbar_wait_warp(sm.full(c % L::kStages), (c / L::kStages) & 1, fail); };
@@ -624,10 +668,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         ++c;
       };
       bool ok = true;
+      Item<PAIR> x;
       for (int round = 0; ok; ++round) {
-        const int index = item_index(round);
-        if (index >= p.n_items) break;
-        const Item<PAIR> x = item_at<PAIR>(p, index, lane);
+        ok = next_item(round, x);
+        if (!ok || !x.valid) break;
         const int n = x.n;
         for (int u = 0; ok && u < min(n, L::kLead); ++u) {
           ok = landed();
@@ -641,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             const int g = of(checked, w);
             bool wrote = false;
 #pragma unroll 1
-            for (int part = warp - kGuardWarp; part < 4; part += 2) {
+            for (int part = 0; part < 4; ++part) {
               const int key = 32 * part + lane;
               const uint32_t at = sm.stage(c % L::kStages) + key * 128;
               bool bad = false;
@@ -667,6 +711,19 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           }
         }
       }
+    } else {  // the coming items, up to kItemRing ahead, and the end
+      for (int round = 0;; ++round) {
+        const int index = item_index(round);
+        ItemData x = {};
+        if (index < p.n_items) x = item_at<PAIR>(p, index, lane);
+        if (round >= kItemRing && !mbar_wait_warp(sm.itemfree(round), ((round / kItemRing) & 1) ^ 1, fail)) break;
+        if (lane == 0) {
+          s_item[round % kItemRing] = x;
+          mbar_arrive(sm.itemfull(round));
+        }
+        __syncwarp();
+        if (index >= p.n_items) break;
+      }
     }
   } else {  // softmax warps
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
@@ -677,34 +734,47 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     sc.scale = CAP ? 2.f * kLog2e * (a.sm_scale / a.softcap) : a.sm_scale * kLog2e;
     sc.cap = a.softcap * kLog2e;
     int tiles = 0, guards = 0;  // tiles done and guarded tiles met, over all items
-    for (int round = 0;; ++round) {
-      const int index = item_index(round);
-      if (index >= p.n_items) break;
-      const Item<PAIR> x = item_at<PAIR>(p, index, lane);
-      // this thread's row
+    Item<PAIR> x;
+    // What the thread's row of an item needs from memory, asked for ahead of its use.
+    int token = 0, head = 0;
+    int2 span = make_int2(0, 0);
+    int length = 0, at = 0;
+    float slope = 0.f;
+    auto load_row = [&]() {
       const int R = (PAIR ? 2 * x.m_block + stream : x.m_block) * kTile + r;
-      const int token = R / a.G, head = x.h * a.G + R % a.G;
+      token = R >> p.log2_G;
+      head = x.h * a.G + (R & (a.G - 1));
+      if (token >= a.tq) return;
+      if (a.lens) length = a.lens[x.b];
+      if (a.spans) span = a.spans[(size_t)x.b * a.tq + token];
+      if constexpr (BIAS) {
+        if (a.pos) at = a.pos[(size_t)x.b * a.tq + token];
+        slope = a.slopes[head];
+      }
+    };
+    bool ok = next_item(0, x);
+    if (ok && x.valid) load_row();
+    if (!PAIR) ok = !softmax_sync(!ok);  // (all of them go on, or none)
+    for (int round = 0; ok && x.valid; ++round) {
       const bool valid = token < a.tq;
       Row row;
       row.lo = row.hi = 0;
       row.pos = 0.f;
       row.slope = 0.f;
-      int at = 0;
+      int pos = 0;
       if (valid) {
-        int len = a.tk;
-        row.hi = a.tk;
-        if (a.lens) len = row.hi = max(0, min(a.lens[x.b], a.tk));
+        const int len = a.lens ? max(0, min(length, a.tk)) : a.tk;
+        row.hi = len;
         if (a.spans) {
-          const int2 s = a.spans[(size_t)x.b * a.tq + token];
-          row.lo = max(s.x, 0);
-          row.hi = min(s.y, a.tk);
+          row.lo = max(span.x, 0);
+          row.hi = min(span.y, a.tk);
         } else if (a.causal) {
-          row.hi = (int)min((long long)a.tk, max(0ll, (long long)a.q_start + token + 1));
+          row.hi = (int)min((long long)len, max(0ll, (long long)a.q_start + token + 1));
         }
         if constexpr (BIAS) {
-          at = a.pos ? a.pos[(size_t)x.b * a.tq + token] : a.pos_at_len ? len : a.q_start + token;
-          row.pos = (float)at;
-          row.slope = a.slopes[head] * kLog2e;
+          pos = a.pos ? at : a.pos_at_len ? len : a.q_start + token;
+          row.pos = (float)pos;
+          row.slope = slope * kLog2e;
         }
         if (row.hi <= row.lo) row.lo = row.hi = 0;
       }
@@ -715,13 +785,13 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       const int warp_all_hi = __reduce_min_sync(0xffffffffu, !valid ? INT_MAX : row.hi);
       int pos_min = 0, pos_max = 0;
       if (BIAS) {
-        pos_min = __reduce_min_sync(0xffffffffu, valid ? at : INT_MAX);
-        pos_max = __reduce_max_sync(0xffffffffu, valid ? at : INT_MIN);
+        pos_min = __reduce_min_sync(0xffffffffu, valid ? pos : INT_MAX);
+        pos_max = __reduce_max_sync(0xffffffffu, valid ? pos : INT_MIN);
       }
       const bool any_valid = __any_sync(0xffffffffu, valid);
       // (a row that sees nothing, or past the last token, needs no reference: its weights are 0 or never used)
       float ref = sees ? -INFINITY : 0.f, sum = 0.f;
-      bool bad_row = false, ok = true;
+      bool bad_row = false;
       bool careful = true;  // some row of the warp has no reference yet, or one beyond kRefExact
       int it = 0;           // tiles of this item done
       for (int i = 0; i < x.tiles_of(stream); ++i) {
@@ -755,11 +825,12 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         }
         const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
         const int side = !BIAS ? 0 : k0 + kTile - 1 <= pos_min ? -1 : k0 >= pos_max ? 1 : 0;
-        if (guarded) {
+        // The keys that the guard warp has found: rows that see one are marked (before the last weights are handed over,
+        // which lets the tile's results be overwritten).
+        auto mark = [&]() {
           const int g = guards - 1, ws = PAIR ? 0 : stream;
-          ok = __all_sync(0xffffffffu, mbar_wait_role(sm.vsafe(ws, g), (g / kSafeRing) & 1, fail));
-          if (!ok) break;
-#pragma unroll
+          if (!__all_sync(0xffffffffu, mbar_wait_role(sm.vsafe(ws, g), (g / kSafeRing) & 1, fail))) return false;
+#pragma unroll 1
           for (int q = 0; q < 4; ++q) {
             uint32_t bits = s_bad[ws][g % kSafeRing][q];
             while (bits) {
@@ -768,7 +839,8 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               bad_row = bad_row || (key >= row.lo && key < row.hi);
             }
           }
-        }
+          return true;
+        };
         // The weights of 64 columns, packed, and their sum: v holds the scores less the reference.
         auto pack_half = [&](const float (&v)[64], uint32_t (&w)[32]) {
           uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
@@ -795,6 +867,8 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         // stored before the check. Without a cap the whole tile is handed over at once; with one, whose arithmetic
         // takes longer, each half as it is ready, so that its product runs under the next half.
         bool slow = masked || careful;
+        if (guarded && !masked) ok = mark();
+        if (!ok) break;
         if (!CAP && !slow) {
           float v[2][64];
           uint32_t w[2][32];
@@ -874,6 +948,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               sum += pack_half(v, w);
             }
             tmem_st32(ts + 32 * half, w);  // (over columns of S that both halves have left)
+            if (half == 1 && guarded && masked) {
+              ok = mark();
+              if (!ok) break;
+            }
             arrive(half, 1);
           }
         }
@@ -881,6 +959,17 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         ++it;
         ++tiles;
       }
+      // where the row goes; the next item's row is asked for before this one is written
+      const size_t out_row = ((size_t)x.b * a.tq + token) * a.heads_q + head;
+      const bool whole = p.n_splits == 1;
+      char* dst = whole ? static_cast<char*>(a.out) +
+                              (x.b * a.o_b + head * a.o_h + token * a.o_t) * (p.out_kind == 2 ? 4 : 2)
+                        : reinterpret_cast<char*>(p.part_o + ((size_t)x.split * p.part_rows + out_row) * kHeadDim);
+      const long long stat_at = whole ? x.b * a.s_b + head * a.s_h + token * a.s_t
+                                      : (long long)x.split * p.part_rows + (long long)out_row;
+      const int n = x.n;
+      if (ok) ok = next_item(round + 1, x);
+      if (ok && x.valid) load_row();
       if (ok && it > 0) {
         ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, 1), (tiles - 1) & 1, fail));
         tcgen05_after_sync();
@@ -905,10 +994,8 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       } else if (!ok) {
         break;
       }
-      const size_t out_row = ((size_t)x.b * a.tq + token) * a.heads_q + head;
       float lse2 = sum == 0.f ? -INFINITY : ref + log2f(sum);
       float f0 = sum == 0.f ? 0.f : 1.f / sum, f1 = 0.f;
-      const bool whole = p.n_splits == 1;
       if (whole && a.own_out && valid) join_own(a, out_row, lse2, f0, f1);
       if (bad_row) f0 = __int_as_float(0x7fffffff);
       // (a row whose sum is 0 has seen nothing, or only scores of -inf: its O holds zeros or, never written, anything)
@@ -916,10 +1003,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       g0 *= f0;
       g1 *= f0;
       const uint32_t o0 = PAIR ? to : tmem + 256 + lanes;
-      const bool has0 = PAIR ? it > 0 : x.n > 0, has1 = !PAIR && x.n > 1;
-      char* dst = whole ? static_cast<char*>(a.out) +
-                              (x.b * a.o_b + head * a.o_h + token * a.o_t) * (p.out_kind == 2 ? 4 : 2)
-                        : reinterpret_cast<char*>(p.part_o + ((size_t)x.split * p.part_rows + out_row) * kHeadDim);
+      const bool has0 = PAIR ? it > 0 : n > 0, has1 = !PAIR && n > 1;
       const float* own = a.own_out + out_row * kHeadDim;
 #pragma unroll
       for (int q = 0; q < (PAIR ? 4 : 2); ++q) {
@@ -949,15 +1033,14 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               v[e + 3] = fmaf(o.w, f1, v[e + 3]);
             }
           }
-#pragma unroll
-          for (int e = 0; e < 32; e += 8) store_out8(dst, whole ? p.out_kind : 2, ch + e, v + e);
+          store_out32(dst, whole ? p.out_kind : 2, ch, v);
         }
       }
       if (valid && (PAIR || stream == 0)) {
         if (whole)
-          store_stat(a, x.b * a.s_b + head * a.s_h + token * a.s_t, lse2);
+          store_stat(a, stat_at, lse2);
         else
-          p.part_lse[(size_t)x.split * p.part_rows + out_row] = lse2;
+          p.part_lse[stat_at] = lse2;
       }
       if constexpr (!PAIR) {  // both warpgroups have read both O before the next item's products overwrite them
         tcgen05_before_sync();

@@ -33,6 +33,24 @@ struct FlashArgs {
   int* status;
 };
 
+// Division of 0 <= n < 2^31 by d > 0 through a multiplication: with s = ceil(log2 d) and mul = ceil(2^(31 + s) / d),
+// mul exceeds 2^(31 + s) / d by less than 1, so n mul / 2^(31 + s) exceeds n / d by less than 2^-s <= 1 / d.
+struct FastDiv {
+  int d;
+  unsigned mul, shift;
+  void set(int by) {
+    d = by;
+    shift = 0;
+    while ((1ll << shift) < by) ++shift;
+    mul = (unsigned)(((1ull << (31 + shift)) + by - 1) / by);
+  }
+#ifdef __CUDACC__
+  __device__ __forceinline__ int div(int n) const {
+    return (int)(((unsigned long long)(unsigned)n * mul) >> (31 + shift));
+  }
+#endif
+};
+
 // What the tensor-core kernel takes: the problem, its tensor maps, and its share of the work plan.
 struct FlashKernelArgs {
   CUtensorMap map_q;    // [batch][tokens][heads][128], box 64 channels x G heads x 128 / G tokens, 128B swizzle
@@ -43,6 +61,9 @@ struct FlashKernelArgs {
   int m_blocks;         // row tiles (pairs) of one KV head
   int n_items;          // batch * heads_kv * m_blocks * n_splits
   int group_heads;      // (set, KV head) combinations whose items are worked on together
+  int log2_G;
+  // an item's number taken apart: by group, by rank within a full or the last group, by split, and a head into its set
+  FastDiv by_group, by_rank, by_last, by_split, by_head;
   int out_kind;         // 0 bf16, 1 fp16, 2 fp32
   float* part_o;        // [n_splits][part_rows][128] normalised outputs, row = (set * tq + token) * heads_q + head
   float* part_lse;      // [n_splits][part_rows] log2 of the sum of 2^x (-inf: nothing seen)
