@@ -49,7 +49,7 @@ bool encode_rows(CUtensorMap* map, bool f16, const void* data, const long long (
 }
 
 struct Plan {
-  bool pair;
+  int mode;  // flash::Mode
   int m_blocks, n_splits;
 };
 
@@ -69,8 +69,9 @@ int most_splits(long long base, int tiles, int num_sms) {
 Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
   Plan p;
   const long long rows = (long long)tq * G;
-  p.pair = rows > kTile;
-  p.m_blocks = (int)(p.pair ? (rows + 2 * kTile - 1) / (2 * kTile) : 1);
+  const bool pair = rows > kTile;
+  p.mode = pair ? flash::kPair : rows > flash::Layout<flash::kFew>::kRows ? flash::kOne : flash::kFew;
+  p.m_blocks = (int)(pair ? (rows + 2 * kTile - 1) / (2 * kTile) : 1);
   const long long base = (long long)batch * heads_kv * p.m_blocks;
   const int tiles = (int)(((long long)tk + kTile - 1) / kTile);
   p.n_splits = 1;
@@ -80,7 +81,7 @@ Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
     const double rounds = (double)((items + num_sms - 1) / num_sms);
     const double busy = (double)(items < num_sms ? items : num_sms);
     // a tile: the products and softmax, or its 64 KB at the SM's share of HBM
-    const double tile = p.pair ? 1650.0 : 9.7 * busy > 950.0 ? 9.7 * busy : 950.0;
+    const double tile = pair ? 1650.0 : 9.7 * busy > 950.0 ? 9.7 * busy : 950.0;
     const double merge = s > 1 ? 4500.0 + (double)s * rows * batch * heads_kv * kHeadDim * 8.0 / 5000.0 : 0.0;
     const double cost = rounds * ((tiles + s - 1) / s * tile + 2000.0) + merge;
     if (cost < best) best = cost, p.n_splits = s;
@@ -190,7 +191,8 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   p.part_lse = p.part_o + (size_t)plan.n_splits * p.part_rows * kHeadDim;
   if (a.tk > 0) {
     p.k_batch = a.k_b != 0, p.k_head = a.k_h != 0, p.v_batch = a.v_b != 0, p.v_head = a.v_h != 0;
-    const uint32_t box_q[3] = {(uint32_t)a.G, (uint32_t)(kTile / a.G), 1}, box_k[3] = {(uint32_t)kTile, 1, 1};
+    const uint32_t box_q[3] = {(uint32_t)a.G, (uint32_t)((plan.mode == flash::kFew ? flash::Layout<flash::kFew>::kRows : kTile) / a.G), 1},
+                   box_k[3] = {(uint32_t)kTile, 1, 1};
     if (!encode_rows(&p.map_q, f16, a.q, {a.heads_q, a.tq, a.batch}, {a.q_h, a.q_t, a.q_b}, box_q) ||
         !encode_rows(&p.map_k, f16, a.k, {a.tk, a.heads_kv, a.batch}, {a.k_t, a.k_h, a.k_b}, box_k) ||
         !encode_rows(&p.map_v, f16, a.v, {a.tk, a.heads_kv, a.batch}, {a.v_t, a.v_h, a.v_b}, box_k))
@@ -212,7 +214,7 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   p.by_split.set(plan.n_splits);
   p.by_head.set(a.heads_kv);
   const int grid = p.n_items < num_sms ? p.n_items : num_sms;
-  cudaError_t e = f16 ? launch_flash_kernel<true>(p, plan.pair, grid, st) : launch_flash_kernel<false>(p, plan.pair, grid, st);
+  cudaError_t e = f16 ? launch_flash_kernel<true>(p, plan.mode, grid, st) : launch_flash_kernel<false>(p, plan.mode, grid, st);
   if (e != cudaSuccess || plan.n_splits == 1) return e;
   const MergePartsArgs m = {a, p.part_o, p.part_lse, p.part_rows, plan.n_splits, p.out_kind};
   return launch_chained(merge_parts_kernel, dim3((unsigned)((p.part_rows + 3) / 4)), dim3(128), 0, st, m);

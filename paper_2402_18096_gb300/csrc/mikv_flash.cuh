@@ -13,9 +13,13 @@
 //
 // A CTA has two streams, each with a score tile S (128 x 128 fp32) and an output tile O (128 x 128 fp32) in
 // TMEM, over 128-key tiles of K and V that TMA stages in a ring:
-//   PAIR    two row tiles (256 rows) over the same key tiles: a K or V tile is loaded once for both.
-//   !PAIR   one row tile (up to 128 rows) over alternating key tiles; the streams' results are joined at the end.
+//   kPair   two row tiles (256 rows) over the same key tiles: a K or V tile is loaded once for both.
+//   kOne    one row tile (up to 128 rows) over alternating key tiles; the streams' results are joined at the end.
 //           The second stream's loads and softmax overlap the first's, which keeps HBM busy when rows are few.
+//   kFew    like kOne for up to 32 rows, which stand in the tile four times: each softmax warp then weighs a quarter
+//           of a tile's keys for all rows (the others' weights are 0 in its copy), and the four copies of both streams
+//           are joined at the end. One warp that weighs whole tiles takes longer than HBM takes to deliver them: with
+//           capped and biased scores of 4 rows 5700 clocks for two tiles against 2700 a tile.
 // Roles: warps 0-3 and 4-7 are the streams' softmax warpgroups (thread = row = TMEM lane), warp 8 issues the copies,
 // warp 9 the MMAs, warp 10 guards masked tiles (below), warp 11 works out the coming items. Per stream and tile: S = Q K^T (8 MMAs of K = 16), softmax
 // to P (16-bit, written over S in TMEM), O += P V (8 MMAs with A in TMEM). The MMA warp alternates streams, so one
@@ -52,7 +56,7 @@
 namespace mikv {
 
 template <bool F16>
-cudaError_t launch_flash_kernel(const FlashKernelArgs& p, bool pair, int grid, cudaStream_t st);
+cudaError_t launch_flash_kernel(const FlashKernelArgs& p, int mode, int grid, cudaStream_t st);
 
 namespace flash {
 
@@ -61,6 +65,7 @@ constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kHalfBytes = kTileBytes / 2;     // one 64-channel box
 constexpr int kSoftThreads = 256;
 constexpr int kCopyWarp = 8, kMmaWarp = 9, kGuardWarp = 10, kItemWarp = 11;
+constexpr int kExPitch = 20;                   // floats of a row's 16 channels in the exchange (padded against conflicts)
 constexpr int kItemRing = 4;                   // items described ahead
 constexpr int kItemReaders = 11;               // warps that read an item's description: all but the one that writes it
 constexpr int kThreads = 384;
@@ -69,20 +74,29 @@ constexpr int kSafeRing = 4;                   // guard results in flight (more 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-template <bool PAIR>
+__host__ __device__ constexpr int align16(int x) { return (x + 15) & ~15; }
+
+enum Mode { kPair = 0, kOne = 1, kFew = 2 };
+
+template <int MODE>
 struct Layout {
+  static constexpr bool PAIR = MODE == kPair;
+  static constexpr int kCopies = MODE == kFew ? 4 : 1;   // of the rows in a tile
+  static constexpr int kRows = kTile / kCopies;          // rows of a tile
+  static constexpr int kExchange = MODE == kFew ? 8 * 32 * kExPitch * 4 : 0;  // for joining the copies
   static constexpr int kQ = PAIR ? 2 : 1;  // query tiles in shared memory
   static constexpr int kStages = 5;        // K / V tiles in the ring
   // Loads of an item: the first kLead K tiles, then V tile u and K tile u + kLead for u = 0, 1, ... (from the last
   // key tile on).
   static constexpr int kLead = PAIR ? 1 : 2;
   static constexpr int kBars = 2 + 2 * kStages + 5 * 2 + 2 * kSafeRing + 2 * kItemRing + 1;
-  static constexpr int kSmem = 1024 + (kQ + kStages) * kTileBytes + 8 * kBars;
+  static constexpr int kSmem = 1024 + (kQ + kStages) * kTileBytes + align16(8 * kBars) + kExchange;
   static_assert(kSmem <= 224 * 1024 + 2048, "shared memory of one CTA");
   uint32_t base;
   __device__ uint32_t q(int m) const { return base + m * kTileBytes; }
   __device__ uint32_t stage(int s) const { return base + (kQ + s) * kTileBytes; }
   __device__ uint32_t bar(int i) const { return base + (kQ + kStages) * kTileBytes + 8 * i; }
+  __device__ uint32_t exchange() const { return base + (kQ + kStages) * kTileBytes + align16(8 * kBars); }
   __device__ uint32_t qfull() const { return bar(0); }                       // an item's queries landed
   __device__ uint32_t qfree() const { return bar(1); }                       // its last scores have read them
   __device__ uint32_t full(int s) const { return bar(2 + s); }               // a copy landed
@@ -339,8 +353,9 @@ struct Item : ItemData {
 
 // Item number `index`, worked out by a whole warp (the same in every lane). Heads go in groups whose keys fit in L2
 // together; within a group a causal prompt's longest rows come first.
-template <bool PAIR>
+template <int MODE>
 __device__ __forceinline__ ItemData item_at(const FlashKernelArgs& p, int index, int lane) {
+  constexpr bool PAIR = MODE == kPair;
   const FlashArgs& a = p.a;
   ItemData x;
   const int group = p.by_group.div(index);
@@ -356,7 +371,7 @@ __device__ __forceinline__ ItemData item_at(const FlashKernelArgs& p, int index,
   x.m_block = p.m_blocks - 1 - rank;
   x.valid = 1;
   x.unused = 0;
-  const int toks = kTile / a.G;
+  const int toks = Layout<MODE>::kRows / a.G;
   constexpr int W = PAIR ? 2 : 1;
   // what the tokens of each tile see: their union [lo, hi) (hi = 0: none), and what all of them see
   int lo[W], hi[W], all_lo[W], all_hi[W];
@@ -441,17 +456,19 @@ __device__ __forceinline__ bool softmax_sync(bool failed) {
   return any != 0;
 }
 
-template <bool F16, bool PAIR, bool CAP, bool BIAS>
+template <bool F16, int MODE, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constant__ FlashKernelArgs p) {
-  using L = Layout<PAIR>;
+  using L = Layout<MODE>;
+  constexpr bool PAIR = L::PAIR;
   const FlashArgs& a = p.a;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
   __shared__ ItemData s_item[kItemRing];
   __shared__ uint32_t s_bad[2][kSafeRing][4];  // keys of a guarded V tile that hold infinities or NaN
-  __shared__ float s_part[2][2][kTile];        // !PAIR: references and sums of both streams
-  __shared__ uint8_t s_mark[2][kTile];         // !PAIR: rows that saw an infinity or NaN
+  // !PAIR: reference and sum of each part of a row, and whether it saw an infinity or NaN. Part: stream and copy.
+  __shared__ float s_part[2 * L::kCopies][2][L::kRows];
+  __shared__ uint8_t s_mark[2 * L::kCopies][L::kRows];
   volatile int* fail = &s_fail;
   L sm;
   sm.base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -521,8 +538,12 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
 #pragma unroll
             for (int m = 0; m < L::kQ; ++m) {
               const int tok0 = (PAIR ? 2 * x.m_block + m : x.m_block) * (kTile / a.G);
-              tma_load_4d(sm.q(m), &p.map_q, 0, x.h * a.G, tok0, x.b, sm.qfull());
-              tma_load_4d(sm.q(m) + kHalfBytes, &p.map_q, 64, x.h * a.G, tok0, x.b, sm.qfull());
+#pragma unroll
+              for (int copy = 0; copy < L::kCopies; ++copy) {
+                const uint32_t to = sm.q(m) + copy * L::kRows * 128;
+                tma_load_4d(to, &p.map_q, 0, x.h * a.G, tok0, x.b, sm.qfull());
+                tma_load_4d(to + kHalfBytes, &p.map_q, 64, x.h * a.G, tok0, x.b, sm.qfull());
+              }
             }
             ++running;
           }
@@ -715,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       for (int round = 0;; ++round) {
         const int index = item_index(round);
         ItemData x = {};
-        if (index < p.n_items) x = item_at<PAIR>(p, index, lane);
+        if (index < p.n_items) x = item_at<MODE>(p, index, lane);
         if (round >= kItemRing && !mbar_wait_warp(sm.itemfree(round), ((round / kItemRing) & 1) ^ 1, fail)) break;
         if (lane == 0) {
           s_item[round % kItemRing] = x;
@@ -727,7 +748,8 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     }
   } else {  // softmax warps
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    const int stream = warp >> 2, r = tid & (kTile - 1);
+    const int stream = warp >> 2, r = tid & (L::kRows - 1);
+    const int part = MODE == kFew ? warp : stream;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t ts = tmem + 128 * stream + lanes, to = tmem + 256 + 128 * stream + lanes;
     Score sc;
@@ -741,7 +763,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     int length = 0, at = 0;
     float slope = 0.f;
     auto load_row = [&]() {
-      const int R = (PAIR ? 2 * x.m_block + stream : x.m_block) * kTile + r;
+      const int R = (PAIR ? 2 * x.m_block + stream : x.m_block) * L::kRows + r;
       token = R >> p.log2_G;
       head = x.h * a.G + (R & (a.G - 1));
       if (token >= a.tq) return;
@@ -824,7 +846,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           continue;
         }
         const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
-        const int side = !BIAS ? 0 : k0 + kTile - 1 <= pos_min ? -1 : k0 >= pos_max ? 1 : 0;
+        auto side_of = [&](int key, int n) {
+          return !BIAS ? 0 : key + n - 1 <= pos_min ? -1 : key >= pos_max ? 1 : 0;
+        };
+        const int side = side_of(k0, kTile);
         // The keys that the guard warp has found: rows that see one are marked (before the last weights are handed over,
         // which lets the tile's results be overwritten).
         auto mark = [&]() {
@@ -841,11 +866,13 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           }
           return true;
         };
-        // The weights of 64 columns, packed, and their sum: v holds the scores less the reference.
-        auto pack_half = [&](const float (&v)[64], uint32_t (&w)[32]) {
+        // The weights of N columns, packed, and their sum: v holds the scores less the reference.
+        auto pack = [&](const auto& v, auto& w) {
+          constexpr int N = sizeof(v) / sizeof(float);
+          static_assert(sizeof(w) == 2 * N, "two weights to a word");
           uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-          for (int e = 0; e < 64; e += 2) {
+          for (int e = 0; e < N; e += 2) {
             const float y0 = fast_exp2(v[e]), y1 = fast_exp2(v[e + 1]);
             acc[(e >> 1) & 3] = add_f32x2(acc[(e >> 1) & 3], f32x2(y0, y1));
             w[e >> 1] = pack16<F16>(y0, y1);
@@ -855,104 +882,148 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           f32x2_split(add_f32x2(acc[2], acc[3]), s2, s3);
           return (s0 + s1) + (s2 + s3);
         };
-        auto load_half = [&](int half, float (&v)[64]) {
-          tmem_ld32(ts + 64 * half, v);
-          tmem_ld32(ts + 64 * half + 32, v + 32);
+        auto load = [&](int col, auto& v) {
+          constexpr int N = sizeof(v) / sizeof(float);
+#pragma unroll
+          for (int q = 0; q < N; q += 32) tmem_ld32(ts + col + q, v + q);
         };
-        auto loaded = [](float (&v)[64]) {
+        auto loaded = [](auto& v) {
           tmem_wait_ld(v);
-          reg_fence(v + 32);
+          if constexpr (sizeof(v) == 64 * sizeof(float)) reg_fence(v + 32);
+        };
+        // The slow path for the N raw scores of columns col ..: masks (by 32 columns, where a row of the warp needs
+        // them), the largest score, a moved reference with O rescaled (o_half, o_phase: the last product in O, if any),
+        // the weights. False when a wait gave up.
+        auto slow_weights = [&](auto& v, auto& w, int col, bool in_o, int o_half, int o_phase) {
+          constexpr int N = sizeof(v) / sizeof(float);
+          float mx = -INFINITY, mx2 = -INFINITY;
+#pragma unroll
+          for (int q = 0; q < N; q += 32) {
+            const int key = k0 + col + q;
+            const bool cut = key < warp_all_lo || key + 32 > warp_all_hi;
+            if (CAP && cut) mask_scores<32>(v + q, row, key, 0.f);  // (four share a reciprocal)
+            row_scores<CAP, BIAS, 32>(v + q, sc, row, k0, col + q, 0.f, side_of(key, 32));
+            if (cut) mask_scores<32>(v + q, row, key, -INFINITY);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              mx = max3(mx, v[q + e], v[q + e + 1]);
+              mx2 = max3(mx2, v[q + e + 2], v[q + e + 3]);
+            }
+          }
+          mx = fmaxf(mx, mx2);
+          const float next = mx > ref + ref_slack<F16>() ? mx - ref_drop<F16>() : ref;
+          const bool moves = next != ref && ref != -INFINITY;
+          if (__any_sync(0xffffffffu, moves)) {
+            const float f = moves ? fast_exp2(ref - next) : 1.f;
+            if (in_o) {
+              if (!__all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, o_half), o_phase & 1, fail))) return false;
+              tcgen05_after_sync();
+#pragma unroll 1
+              for (int q = 0; q < 8; ++q) {
+                float o[16];
+                tmem_ld16(to + 16 * q, o);
+                tmem_wait_ld16(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] *= f;
+                tmem_st16(to + 16 * q, reinterpret_cast<const uint32_t*>(o));
+              }
+            }
+            sum *= f;
+          }
+          ref = next;
+          careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
+          const float rr = ref == -INFINITY ? 0.f : ref;
+          const uint64_t r2 = f32x2(-rr, -rr);
+#pragma unroll
+          for (int e = 0; e < N; e += 2) f32x2_split(add_f32x2(f32x2(v[e], v[e + 1]), r2), v[e], v[e + 1]);
+          sum += pack(v, w);
+          return true;
         };
         // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards; nothing is
-        // stored before the check. Without a cap the whole tile is handed over at once; with one, whose arithmetic
-        // takes longer, each half as it is ready, so that its product runs under the next half.
+        // stored before the check.
         bool slow = masked || careful;
         if (guarded && !masked) ok = mark();
         if (!ok) break;
-        if (!CAP && !slow) {
-          float v[2][64];
-          uint32_t w[2][32];
-          load_half(0, v[0]);
-          loaded(v[0]);
-          load_half(1, v[1]);
-          row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
-          float tile_sum = pack_half(v[0], w[0]);
-          loaded(v[1]);
-          row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
-          tile_sum += pack_half(v[1], w[1]);
-          slow = __any_sync(0xffffffffu, !(tile_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
-          if (!slow) {
-            sum += tile_sum;
-            tmem_st32(ts, w[0]);
-            tmem_st32(ts + 32, w[1]);
-            arrive(0, 2);
-          }
-        }
-        if (CAP || slow) {
-#pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            float v[64];
-            uint32_t w[32];
-            bool slow_half = slow || careful;
-            load_half(half, v);
+        if constexpr (MODE == kFew) {  // this warp's quarter of the keys
+          const int quarter = warp & 3, col = 32 * quarter;
+          uint32_t w[16], zero[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w[e] = zero[e] = 0u;
+          if (k0 + col < warp_hi && k0 + col + 32 > warp_lo) {
+            float v[32];
+            load(col, v);
             loaded(v);
-            if (CAP && !slow_half) {
-              row_scores<CAP, BIAS, 64>(v, sc, row, k0, 64 * half, ref, side);
-              const float half_sum = pack_half(v, w);
-              slow_half = __any_sync(0xffffffffu, !(half_sum <= sum_max<F16>()));
-              if (slow_half) {
-                load_half(half, v);
+            slow = careful || k0 + col < warp_all_lo || k0 + col + 32 > warp_all_hi;
+            if (!slow) {
+              row_scores<CAP, BIAS, 32>(v, sc, row, k0, col, ref, side_of(k0 + col, 32));
+              const float quarter_sum = pack(v, w);
+              slow = __any_sync(0xffffffffu, !(quarter_sum <= sum_max<F16>()));
+              if (slow) {
+                load(col, v);
                 loaded(v);
               } else {
-                sum += half_sum;
+                sum += quarter_sum;
               }
             }
-            if (slow_half) {  // the largest score first, then the weights
-              if (CAP && masked) mask_scores<64>(v, row, k0 + 64 * half, 0.f);  // (four share a reciprocal)
-              row_scores<CAP, BIAS, 64>(v, sc, row, k0, 64 * half, 0.f, side);
-              if (masked) mask_scores<64>(v, row, k0 + 64 * half, -INFINITY);
-              float mx = -INFINITY, mx2 = -INFINITY;
+            if (slow) ok = slow_weights(v, w, col, it > 0, 1, tiles - 1);
+            if (!ok) break;
+          }
 #pragma unroll
-              for (int e = 0; e < 64; e += 4) {
-                mx = max3(mx, v[e], v[e + 1]);
-                mx2 = max3(mx2, v[e + 2], v[e + 3]);
-              }
-              mx = fmaxf(mx, mx2);
-              const float next = mx > ref + ref_slack<F16>() ? mx - ref_drop<F16>() : ref;
-              const bool moves = next != ref && ref != -INFINITY;
-              if (__any_sync(0xffffffffu, moves)) {
-                const float f = moves ? fast_exp2(ref - next) : 1.f;
-                if (it + half > 0) {  // O holds the products up to the half before this one
-                  ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, half ^ 1),
-                                                              (half ? tiles : tiles - 1) & 1, fail));
-                  if (!ok) break;
-                  tcgen05_after_sync();
+          for (int q = 1; q < 4; ++q) tmem_st16(ts + 16 * ((quarter + q) & 3), zero);
+          tmem_st16(ts + 16 * quarter, w);
+          if (guarded && masked) ok = mark();
+          if (!ok) break;
+          arrive(0, 2);
+        } else {
+          // Without a cap the whole tile is handed over at once; with one, whose arithmetic takes longer, each half as
+          // it is ready, so that its product runs under the next half.
+          if (!CAP && !slow) {
+            float v[2][64];
+            uint32_t w[2][32];
+            load(0, v[0]);
+            loaded(v[0]);
+            load(64, v[1]);
+            row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
+            float tile_sum = pack(v[0], w[0]);
+            loaded(v[1]);
+            row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
+            tile_sum += pack(v[1], w[1]);
+            slow = __any_sync(0xffffffffu, !(tile_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
+            if (!slow) {
+              sum += tile_sum;
+              tmem_st32(ts, w[0]);
+              tmem_st32(ts + 32, w[1]);
+              arrive(0, 2);
+            }
+          }
+          if (CAP || slow) {
 #pragma unroll 1
-                  for (int q = 0; q < 8; ++q) {
-                    float o[16];
-                    tmem_ld16(to + 16 * q, o);
-                    tmem_wait_ld16(o);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] *= f;
-                    tmem_st16(to + 16 * q, reinterpret_cast<const uint32_t*>(o));
-                  }
+            for (int half = 0; half < 2; ++half) {
+              float v[64];
+              uint32_t w[32];
+              bool slow_half = slow || careful;
+              load(64 * half, v);
+              loaded(v);
+              if (CAP && !slow_half) {
+                row_scores<CAP, BIAS, 64>(v, sc, row, k0, 64 * half, ref, side);
+                const float half_sum = pack(v, w);
+                slow_half = __any_sync(0xffffffffu, !(half_sum <= sum_max<F16>()));
+                if (slow_half) {
+                  load(64 * half, v);
+                  loaded(v);
+                } else {
+                  sum += half_sum;
                 }
-                sum *= f;
               }
-              ref = next;
-              careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
-              const float rr = ref == -INFINITY ? 0.f : ref;
-              const uint64_t r2 = f32x2(-rr, -rr);
-#pragma unroll
-              for (int e = 0; e < 64; e += 2) f32x2_split(add_f32x2(f32x2(v[e], v[e + 1]), r2), v[e], v[e + 1]);
-              sum += pack_half(v, w);
-            }
-            tmem_st32(ts + 32 * half, w);  // (over columns of S that both halves have left)
-            if (half == 1 && guarded && masked) {
-              ok = mark();
+              if (slow_half) ok = slow_weights(v, w, 64 * half, it + half > 0, half ^ 1, half ? tiles : tiles - 1);
               if (!ok) break;
+              tmem_st32(ts + 32 * half, w);  // (over columns of S that both halves have left)
+              if (half == 1 && guarded && masked) {
+                ok = mark();
+                if (!ok) break;
+              }
+              arrive(half, 1);
             }
-            arrive(half, 1);
           }
         }
         if (!ok) break;
@@ -967,41 +1038,119 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
                         : reinterpret_cast<char*>(p.part_o + ((size_t)x.split * p.part_rows + out_row) * kHeadDim);
       const long long stat_at = whole ? x.b * a.s_b + head * a.s_h + token * a.s_t
                                       : (long long)x.split * p.part_rows + (long long)out_row;
-      const int n = x.n;
+      const int n = x.n, set = x.b, head0 = x.h * a.G, split = x.split;
       if (ok) ok = next_item(round + 1, x);
       if (ok && x.valid) load_row();
       if (ok && it > 0) {
         ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, 1), (tiles - 1) & 1, fail));
         tcgen05_after_sync();
       }
-      // Output. PAIR: each thread its row of O. !PAIR: the streams hold two parts of the same rows, in the same
-      // TMEM lanes; each warpgroup joins one half of the channels.
-      float g0 = 1.f, g1 = 0.f;  // factors of the first (PAIR: its own) and the second stream's O
+      // Output. kPair: each thread its row of O. kOne: the streams hold two parts of the same rows, in the same TMEM
+      // lanes; each warpgroup joins one half of the channels. kFew: eight parts, joined through shared memory.
       if constexpr (!PAIR) {
-        s_part[stream][0][r] = it > 0 ? ref : -INFINITY;
-        s_part[stream][1][r] = it > 0 ? sum : 0.f;
-        s_mark[stream][r] = bad_row;
+        s_part[part][0][r] = it > 0 ? ref : -INFINITY;
+        s_part[part][1][r] = it > 0 ? sum : 0.f;
+        s_mark[part][r] = bad_row;
         tcgen05_before_sync();
         if (softmax_sync(!ok || *fail)) break;  // (both streams' products are done)
         tcgen05_after_sync();
-        const float r0 = s_part[0][0][r], r1 = s_part[1][0][r], l0 = s_part[0][1][r], l1 = s_part[1][1][r];
-        bad_row = s_mark[0][r] || s_mark[1][r];
-        const float top = fmaxf(r0, r1);
-        g0 = top == -INFINITY ? 0.f : fast_exp2(r0 - top);
-        g1 = top == -INFINITY ? 0.f : fast_exp2(r1 - top);
-        sum = l0 * g0 + l1 * g1;
-        ref = top;
       } else if (!ok) {
         break;
       }
-      float lse2 = sum == 0.f ? -INFINITY : ref + log2f(sum);
-      float f0 = sum == 0.f ? 0.f : 1.f / sum, f1 = 0.f;
-      if (whole && a.own_out && valid) join_own(a, out_row, lse2, f0, f1);
-      if (bad_row) f0 = __int_as_float(0x7fffffff);
+      // A row's parts taken together: the largest reference, log2 of the sum, factors of the parts (times 2^(reference of
+      // the part - top)) and of the request's own output.
+      struct Joined {
+        float top, lse2, f0, f1;
+      };
+      auto join = [&](int row_in_tile, bool there, size_t at_row) {
+        Joined q;
+        float total = sum;
+        bool marked = bad_row;
+        q.top = ref;
+        if constexpr (!PAIR) {
+          q.top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 2 * L::kCopies; ++i) q.top = fmaxf(q.top, s_part[i][0][row_in_tile]);
+          total = 0.f;
+          marked = false;
+#pragma unroll
+          for (int i = 0; i < 2 * L::kCopies; ++i) {
+            const float g = q.top == -INFINITY ? 0.f : fast_exp2(s_part[i][0][row_in_tile] - q.top);
+            total = fmaf(s_part[i][1][row_in_tile], g, total);
+            marked = marked || s_mark[i][row_in_tile];
+          }
+        }
+        q.lse2 = total == 0.f ? -INFINITY : q.top + log2f(total);
+        q.f0 = total == 0.f ? 0.f : 1.f / total;
+        q.f1 = 0.f;
+        if (whole && a.own_out && there) join_own(a, at_row, q.lse2, q.f0, q.f1);
+        if (marked) q.f0 = __int_as_float(0x7fffffff);
+        return q;
+      };
+      const Joined jn = join(r, valid, out_row);
       // (a row whose sum is 0 has seen nothing, or only scores of -inf: its O holds zeros or, never written, anything)
-      const bool blank = f0 == 0.f;
-      g0 *= f0;
-      g1 *= f0;
+      const bool blank = jn.f0 == 0.f;
+      const float f1 = jn.f1;
+      auto part_factor = [&](int i) { return jn.f0 * (jn.top == -INFINITY ? 0.f : fast_exp2(s_part[i][0][r] - jn.top)); };
+      if constexpr (MODE == kFew) {
+        // 16 channels at a time: every part scaled into shared memory, then summed (thread: two channels of a row)
+        float* ex = reinterpret_cast<float*>(smem_raw + (sm.exchange() - smem_u32(smem_raw)));
+        const float g = blank || it == 0 ? 0.f : part_factor(part);
+        const int orow = tid >> 3, oc = 2 * (tid & 7);
+        const int otoken = orow >> p.log2_G, ohead = head0 + (orow & (a.G - 1));
+        const bool othere = otoken < a.tq;
+        const size_t orow_out = ((size_t)set * a.tq + otoken) * a.heads_q + ohead;
+        const Joined jo = join(orow, othere, orow_out);
+        char* odst = whole ? static_cast<char*>(a.out) +
+                                 (set * a.o_b + ohead * a.o_h + otoken * a.o_t) * (p.out_kind == 2 ? 4 : 2)
+                           : reinterpret_cast<char*>(p.part_o + ((size_t)split * p.part_rows + orow_out) * kHeadDim);
+        const int kind = whole ? p.out_kind : 2;
+#pragma unroll 1
+        for (int q = 0; q < 8; ++q) {
+          float v[16];
+          if (it > 0) {
+            tmem_ld16(to + 16 * q, v);
+            tmem_wait_ld16(v);
+          }
+          float4* mine = reinterpret_cast<float4*>(ex + (part * 32 + lane) * kExPitch);
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            mine[e / 4] = g != 0.f ? make_float4(v[e] * g, v[e + 1] * g, v[e + 2] * g, v[e + 3] * g)
+                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+          softmax_sync(false);
+          if (othere) {
+            float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float2 z = *reinterpret_cast<const float2*>(ex + (i * 32 + orow) * kExPitch + oc);
+              y0 += z.x;
+              y1 += z.y;
+            }
+            const int ch = 16 * q + oc;
+            if (jo.f1 != 0.f) {
+              const float2 o = *reinterpret_cast<const float2*>(a.own_out + orow_out * kHeadDim + ch);
+              y0 = fmaf(o.x, jo.f1, y0);
+              y1 = fmaf(o.y, jo.f1, y1);
+            }
+            if (kind == 2)
+              reinterpret_cast<float2*>(odst)[ch / 2] = make_float2(y0, y1);
+            else
+              reinterpret_cast<uint32_t*>(odst)[ch / 2] = kind == 1 ? pack_f16(y0, y1) : pack_bf16(y0, y1);
+          }
+          softmax_sync(false);
+        }
+        if (othere && oc == 0) {
+          if (whole)
+            store_stat(a, set * a.s_b + ohead * a.s_h + otoken * a.s_t, jo.lse2);
+          else
+            p.part_lse[(long long)split * p.part_rows + (long long)orow_out] = jo.lse2;
+        }
+        tcgen05_before_sync();
+        if (softmax_sync(*fail)) break;
+        continue;
+      }
+      const float lse2 = jn.lse2;
+      const float g0 = PAIR ? jn.f0 : part_factor(0), g1 = PAIR ? 0.f : part_factor(1);
       const uint32_t o0 = PAIR ? to : tmem + 256 + lanes;
       const bool has0 = PAIR ? it > 0 : n > 0, has1 = !PAIR && n > 1;
       const float* own = a.own_out + out_row * kHeadDim;
@@ -1058,11 +1207,11 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
   }
 }
 
-template <bool F16, bool PAIR>
+template <bool F16, int MODE>
 cudaError_t launch_variant(const FlashKernelArgs& p, int grid, cudaStream_t st) {
   const bool cap = p.a.softcap > 0.f, bias = p.a.slopes != nullptr;
-  auto k = cap ? (bias ? flash_kernel<F16, PAIR, true, true> : flash_kernel<F16, PAIR, true, false>)
-               : (bias ? flash_kernel<F16, PAIR, false, true> : flash_kernel<F16, PAIR, false, false>);
+  auto k = cap ? (bias ? flash_kernel<F16, MODE, true, true> : flash_kernel<F16, MODE, true, false>)
+               : (bias ? flash_kernel<F16, MODE, false, true> : flash_kernel<F16, MODE, false, false>);
   static std::atomic<uint64_t> configured[4];  // per variant: one bit per device
   std::atomic<uint64_t>& done = configured[2 * cap + bias];
   int dev = 0;
@@ -1070,11 +1219,11 @@ cudaError_t launch_variant(const FlashKernelArgs& p, int grid, cudaStream_t st) 
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (dev > 63 || !(done.load(std::memory_order_relaxed) & bit)) {
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<PAIR>::kSmem);
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<MODE>::kSmem);
     if (e != cudaSuccess) return e;
     done.fetch_or(bit, std::memory_order_relaxed);
   }
-  k<<<grid, kThreads, Layout<PAIR>::kSmem, st>>>(p);
+  k<<<grid, kThreads, Layout<MODE>::kSmem, st>>>(p);
   return cudaGetLastError();
 }
 

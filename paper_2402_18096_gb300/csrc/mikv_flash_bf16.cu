@@ -4,8 +4,13 @@
 namespace mikv {
 
 template <>
-cudaError_t launch_flash_kernel<false>(const FlashKernelArgs& p, bool pair, int grid, cudaStream_t st) {
-  return pair ? flash::launch_variant<false, true>(p, grid, st) : flash::launch_variant<false, false>(p, grid, st);
+cudaError_t launch_flash_kernel<false>(const FlashKernelArgs& p, int mode, int grid, cudaStream_t st) {
+  switch (mode) {
+    case flash::kPair: return flash::launch_variant<false, flash::kPair>(p, grid, st);
+    case flash::kOne: return flash::launch_variant<false, flash::kOne>(p, grid, st);
+    case flash::kFew: return flash::launch_variant<false, flash::kFew>(p, grid, st);
+  }
+  return cudaErrorInvalidValue;
 }
 
 }  // namespace mikv

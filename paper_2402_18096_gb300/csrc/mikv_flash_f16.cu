@@ -4,8 +4,13 @@
 namespace mikv {
 
 template <>
-cudaError_t launch_flash_kernel<true>(const FlashKernelArgs& p, bool pair, int grid, cudaStream_t st) {
-  return pair ? flash::launch_variant<true, true>(p, grid, st) : flash::launch_variant<true, false>(p, grid, st);
+cudaError_t launch_flash_kernel<true>(const FlashKernelArgs& p, int mode, int grid, cudaStream_t st) {
+  switch (mode) {
+    case flash::kPair: return flash::launch_variant<true, flash::kPair>(p, grid, st);
+    case flash::kOne: return flash::launch_variant<true, flash::kOne>(p, grid, st);
+    case flash::kFew: return flash::launch_variant<true, flash::kFew>(p, grid, st);
+  }
+  return cudaErrorInvalidValue;
 }
 
 }  // namespace mikv
