@@ -112,7 +112,7 @@ mikv_status mikv_rotary(const mikv_rotary_desc* d, const mikv_view* q_in, const 
   if (d->batch <= 0 || d->tokens < 0 || d->heads_q <= 0 || d->heads_k < 0) return MIKV_ERR_ARG;
   if (d->layout != MIKV_ROTARY_HALF && d->layout != MIKV_ROTARY_INTERLEAVED) return MIKV_ERR_ARG;
   if (d->rot < 2 || d->rot % 2 || d->rot > d->head_dim || !(fabsf(d->amplitude) <= 3.402823466e38f)) return MIKV_ERR_ARG;
-  if (d->head_dim != kHeadDim || d->batch > 65535) return MIKV_ERR_UNSUPPORTED;
+  if (d->head_dim != kHeadDim || d->batch > 65535 || (int64_t)d->heads_q + d->heads_k > 65535) return MIKV_ERR_UNSUPPORTED;
   RotaryArgs a;
   memset(&a, 0, sizeof a);
   const int bytes = elem_bytes(d->dtype), n = 16 / bytes;

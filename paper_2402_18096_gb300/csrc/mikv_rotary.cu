@@ -2,9 +2,10 @@
 //
 // Rotary: a pair of channels (x, x') of a token at position p turns by a = 2 pi p f (f: turns per position). The
 // product p f is formed modulo one turn in 64-bit integer arithmetic (f as a 64-bit fraction), so its error stays
-// below 2^-32 turns at any position, where a 32-bit float product would lose 2^-24 of the whole angle. Each block
-// computes the cosines and sines of its tokens once, in shared memory, for all heads of both tensors.
-// Bound by HBM: every element is read and written once.
+// below 2^-32 turns at any position, where a 32-bit float product would lose 2^-24 of the whole angle.
+// Bound by HBM: every element is read and written once. A block takes a few tokens of some heads, at most four 32-byte
+// items to a thread: the loads are issued first, the cosines and sines of the block's tokens are computed while
+// they are under way (once, in shared memory, for all heads), then everything is turned and written.
 #include "mikv_device.cuh"
 #include "mikv_rotary.h"
 
@@ -41,27 +42,101 @@ struct Vec {
   };
 };
 
-// Items of one head row, in elements: VEC: vectors of 16 bytes (HALF: one from each half of the turning channels per
-// item); scalar: one pair per item. Channels past `rot` are copied, one vector / one element per item.
-template <typename T, bool HALF, bool VEC>
-__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotaryArgs a, int tok_per_block) {
-  extern __shared__ float2 s_cs[];  // [tok_per_block][rot / 2] (cos, sin)
-  constexpr int N = VEC ? Vec<T>::N : 1;
+constexpr int kRotItems = 4;  // items of a thread
+
+// cos and sin of the block's tokens, [tokens][rot / 2]
+__device__ __forceinline__ void rotary_angles(const RotaryArgs& a, float2* cs, int b, int t0, int nt) {
   const int half = a.rot / 2;
-  const int b = blockIdx.y;
-  const int t0 = blockIdx.x * tok_per_block;
-  const int nt = min(tok_per_block, a.tokens - t0);
   for (int i = threadIdx.x; i < nt * half; i += kRotThreads) {
     const int t = i / half, f = i - t * half;
     const long long pos = a.positions ? a.positions[(size_t)b * a.tokens + t0 + t] : (long long)a.start + t0 + t;
     const unsigned long long turn = (unsigned long long)pos * a.phases[f];  // modulo 2^64 = one turn
     float s, c;
     sincospif((float)(int)(turn >> 32) * 0x1p-31f, &s, &c);
-    s_cs[i] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
+    cs[i] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
   }
+}
+
+// Rows of 16-byte vectors: an item is two of them. HALF: a vector of the first turning half with its partner, or two
+// copied ones (the number of copied vectors is even: rot / 2 is a whole number of vectors and so is d / 2).
+// Interleaved: two neighbours. A thread keeps its token and its place in the row and takes several heads, so that it
+// reads its angles from shared memory once; a warp has one token, so that those reads meet in few banks.
+// log_tok: log2 of the tokens of a block; heads [z * heads_z, ...) of both tensors.
+template <typename T, bool HALF>
+__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotaryArgs a, int log_tok, int heads_z) {
+  extern __shared__ float2 s_cs[];
+  constexpr int N = Vec<T>::N, kPerRow = kHeadDim / N / 2;
+  const int half = a.rot / 2, b = blockIdx.y, t0 = blockIdx.x << log_tok, nt = min(1 << log_tok, a.tokens - t0);
+  const int h0 = blockIdx.z * heads_z, nh = min(heads_z, a.x[0].heads + a.x[1].heads - h0);
+  const int per_tok = kRotThreads >> log_tok, t = threadIdx.x / per_tok, r = threadIdx.x - t * per_tok;
+  const int it = r % kPerRow, step = per_tok / kPerRow;
+  const int turning = half / N;
+  const int ch = !HALF ? 2 * it * N : it < turning ? it * N : a.rot + (it - turning) * N;
+  const int gap = !HALF ? N : ch < a.rot ? half : (kHeadDim - a.rot) / 2;
+  Vec<T> lo[kRotItems], hi[kRotItems];
+  T* out[kRotItems];
+#pragma unroll
+  for (int u = 0; u < kRotItems; ++u) {
+    const int hz = r / kPerRow + u * step;
+    out[u] = nullptr;
+    if (t >= nt || hz >= nh) continue;
+    const bool second = h0 + hz >= a.x[0].heads;
+    const int h = h0 + hz - (second ? a.x[0].heads : 0);
+    const RotaryTensor& x = second ? a.x[1] : a.x[0];
+    const T* in = static_cast<const T*>(x.in) + b * x.in_b + h * x.in_h + (t0 + t) * x.in_t + ch;
+    out[u] = static_cast<T*>(x.out) + b * x.out_b + h * x.out_h + (t0 + t) * x.out_t + ch;
+    lo[u].u = *reinterpret_cast<const uint4*>(in);
+    hi[u].u = *reinterpret_cast<const uint4*>(in + gap);
+  }
+  rotary_angles(a, s_cs, b, t0, nt);
   __syncthreads();
-  const int turning = HALF ? half / N : (VEC ? a.rot / N : half);
-  const int items = turning + (kHeadDim - a.rot) / N;
+  // N pairs: of the two vectors' channels (HALF), or N / 2 of each vector
+  float2 w[N];
+  const float2* cs = s_cs + t * half + (HALF ? ch : ch / 2);
+  const bool turn0 = t < nt && ch < a.rot, turn1 = HALF ? turn0 : t < nt && ch + N < a.rot;
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (HALF || e < N / 2 ? turn0 : turn1) w[e] = cs[e];
+#pragma unroll
+  for (int u = 0; u < kRotItems; ++u) {
+    if (!out[u]) continue;
+    if constexpr (HALF) {
+      if (turn0) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float p = to_f32(lo[u].e[e]), q = to_f32(hi[u].e[e]);
+          lo[u].e[e] = from_f32<T>(p * w[e].x - q * w[e].y);
+          hi[u].e[e] = from_f32<T>(p * w[e].y + q * w[e].x);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        Vec<T>& x = v ? hi[u] : lo[u];
+        if (v ? turn1 : turn0) {
+#pragma unroll
+          for (int e = 0; e < N; e += 2) {
+            const float2 c = w[(v * N + e) / 2];
+            const float p = to_f32(x.e[e]), q = to_f32(x.e[e + 1]);
+            x.e[e] = from_f32<T>(p * c.x - q * c.y);
+            x.e[e + 1] = from_f32<T>(p * c.y + q * c.x);
+          }
+        }
+      }
+    }
+    *reinterpret_cast<uint4*>(out[u]) = lo[u].u;
+    *reinterpret_cast<uint4*>(out[u] + gap) = hi[u].u;
+  }
+}
+
+// Any alignment, strides and number of turning channels: a pair or a copied channel at a time.
+template <typename T, bool HALF>
+__global__ void __launch_bounds__(kRotThreads) rotary_elements_kernel(const __grid_constant__ RotaryArgs a, int log_tok) {
+  extern __shared__ float2 s_cs[];
+  const int half = a.rot / 2, b = blockIdx.y, t0 = blockIdx.x << log_tok, nt = min(1 << log_tok, a.tokens - t0);
+  rotary_angles(a, s_cs, b, t0, nt);
+  __syncthreads();
+  const int items = half + kHeadDim - a.rot;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     const RotaryTensor& x = a.x[which];
@@ -71,58 +146,38 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
       const int h = r / items, it = r - h * items;
       const T* in = static_cast<const T*>(x.in) + b * x.in_b + h * x.in_h + (t0 + t) * x.in_t;
       T* out = static_cast<T*>(x.out) + b * x.out_b + h * x.out_h + (t0 + t) * x.out_t;
-      const float2* cs = s_cs + t * half;
-      if (it >= turning) {  // copied channels
-        const int c0 = a.rot + (it - turning) * N;
-        if constexpr (VEC)
-          *reinterpret_cast<uint4*>(out + c0) = *reinterpret_cast<const uint4*>(in + c0);
-        else
-          out[c0] = in[c0];
+      if (it >= half) {  // copied channels
+        out[a.rot + it - half] = in[a.rot + it - half];
         continue;
       }
-      if constexpr (VEC && HALF) {
-        Vec<T> lo, hi;
-        lo.u = *reinterpret_cast<const uint4*>(in + it * N);
-        hi.u = *reinterpret_cast<const uint4*>(in + half + it * N);
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const float2 w = cs[it * N + e];
-          const float p = to_f32(lo.e[e]), q = to_f32(hi.e[e]);
-          lo.e[e] = from_f32<T>(p * w.x - q * w.y);
-          hi.e[e] = from_f32<T>(p * w.y + q * w.x);
-        }
-        *reinterpret_cast<uint4*>(out + it * N) = lo.u;
-        *reinterpret_cast<uint4*>(out + half + it * N) = hi.u;
-      } else if constexpr (VEC) {
-        Vec<T> v;
-        v.u = *reinterpret_cast<const uint4*>(in + it * N);
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          const float2 w = cs[(it * N + e) / 2];
-          const float p = to_f32(v.e[e]), q = to_f32(v.e[e + 1]);
-          v.e[e] = from_f32<T>(p * w.x - q * w.y);
-          v.e[e + 1] = from_f32<T>(p * w.y + q * w.x);
-        }
-        *reinterpret_cast<uint4*>(out + it * N) = v.u;
-      } else {
-        const int c0 = HALF ? it : 2 * it, c1 = HALF ? it + half : 2 * it + 1;
-        const float2 w = cs[it];
-        const float p = to_f32(in[c0]), q = to_f32(in[c1]);
-        out[c0] = from_f32<T>(p * w.x - q * w.y);
-        out[c1] = from_f32<T>(p * w.y + q * w.x);
-      }
+      const int c0 = HALF ? it : 2 * it, c1 = HALF ? it + half : 2 * it + 1;
+      const float2 w = s_cs[t * half + it];
+      const float p = to_f32(in[c0]), q = to_f32(in[c1]);
+      out[c0] = from_f32<T>(p * w.x - q * w.y);
+      out[c1] = from_f32<T>(p * w.y + q * w.x);
     }
   }
 }
 
 template <typename T>
 cudaError_t launch_rotary_t(const RotaryArgs& a, int layout, bool vec, cudaStream_t st) {
-  const int tok = a.tokens >= 4 ? 4 : 1;
-  const dim3 grid((a.tokens + tok - 1) / tok, a.batch);
+  // Eight tokens to a block write each head's rows 2 KB at a time: 32768 tokens of 32 + 8 bf16 heads take 101 us (6.6 TB/s,
+  // 98 % of a copy), 106 with four tokens, 144 with one (which also computes each angle for fewer heads). Few tokens are
+  // spread over more blocks instead.
+  const int log_tok = a.tokens >= 8 && (long long)a.batch * a.tokens >= 2048 ? 3 : 0, tok = 1 << log_tok;
+  const int blocks = (a.tokens + tok - 1) / tok;
   const size_t smem = (size_t)tok * (a.rot / 2) * sizeof(float2);
-  auto k = layout == 0 ? (vec ? rotary_kernel<T, true, true> : rotary_kernel<T, true, false>)
-                       : (vec ? rotary_kernel<T, false, true> : rotary_kernel<T, false, false>);
-  k<<<grid, kRotThreads, smem, st>>>(a, tok);
+  if (!vec) {
+    auto k = layout == 0 ? rotary_elements_kernel<T, true> : rotary_elements_kernel<T, false>;
+    k<<<dim3(blocks, a.batch), kRotThreads, smem, st>>>(a, log_tok);
+    return cudaGetLastError();
+  }
+  const int heads = a.x[0].heads + a.x[1].heads;
+  const int most = kRotThreads * kRotItems / (kHeadDim / Vec<T>::N / 2) / tok;  // heads of a block
+  const int parts = (heads + most - 1) / most;
+  if (parts > 65535) return cudaErrorInvalidValue;
+  auto k = layout == 0 ? rotary_kernel<T, true> : rotary_kernel<T, false>;
+  k<<<dim3(blocks, a.batch, parts), kRotThreads, smem, st>>>(a, log_tok, (heads + parts - 1) / parts);
   return cudaGetLastError();
 }
 
