@@ -7,6 +7,8 @@ This is the flow a serving stack runs around the library (Fig. 4 of arxiv 2402.1
               precision important set, Sec. 3.3), quantize the rest into the retained set
               (mikv_quantize_pack, Eq. 1 with Eq. 3 key balancing)
   decode   -> per token: insert, attend, update importance, demote the least important (mikv_decode_step)
+Requests that share a long prompt prefix keep it once, in bf16, beside a mixed-precision cache of their own tokens
+(SharedPrefixLayer): rotary positions, prompt attention, and decode steps whose attention joins both.
 Every step runs in the library's kernels; this module only orders the calls and owns the buffers.
 """
 from __future__ import annotations
@@ -15,9 +17,11 @@ import math
 
 import torch
 
-from . import (LayerCache, Shape, WS_BALANCER, WS_PREFILL, WS_STEP, mikv_compute_balancer, mikv_decode_attention,
-               mikv_decode_step, mikv_gather_hi, mikv_prefill_scores, mikv_quantize_pack, mikv_select_demote,
-               mikv_workspace_bytes)
+from . import (LayerCache, RotaryTable, Shape, WS_ATTENTION, WS_BALANCER, WS_PREFILL, WS_STEP, mikv_compute_balancer,
+               mikv_decode_attention, mikv_decode_step, mikv_gather_hi, mikv_insert_token, mikv_mask_spans,
+               mikv_prefill_scores, mikv_prefix_attention, mikv_prefix_workspace_bytes, mikv_prompt_attention,
+               mikv_prompt_workspace_bytes, mikv_quantize_pack, mikv_rotary, mikv_select_demote,
+               mikv_update_importance, mikv_workspace_bytes)
 
 
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:
@@ -78,6 +82,75 @@ class MixedPrecisionLayer:
         if self.shape.bits:
             self.n_lo += 1
         self.pos += 1
+
+
+class SharedPrefixLayer:
+    """One layer for a batch of requests whose prompts begin with the same tokens. The prefix's keys and values stay in
+    bf16 and are read once per step for all requests; every request's own tokens live in a mixed-precision cache
+    (bf16 important set). Queries and keys come in as projected, without positions; tensors are [B, H, T, d] views."""
+
+    def __init__(self, own: MixedPrecisionLayer, k_prefix, v_prefix, table: RotaryTable):
+        s = own.shape
+        if s.hi_coded:
+            raise ValueError("SharedPrefixLayer: the important set of the own cache is bf16")
+        dev = k_prefix.device
+        self.own, self.table = own, table
+        self.k_prefix, self.v_prefix = k_prefix, v_prefix  # [1, Hkv, P, d], positions applied
+        self.prefix = k_prefix.shape[2]
+        like = torch.empty(s.batch, s.heads_q, s.head_dim, dtype=torch.bfloat16, device=dev)
+        f = dict(dtype=torch.float32, device=dev)
+        self.own_out = torch.empty(s.batch, s.heads_q, s.head_dim, **f)
+        self.own_ml = torch.empty(s.batch, s.heads_q, 2, **f)
+        self.ml = torch.empty(s.batch, s.heads_q, 2, **f)
+        self.logits = torch.empty(s.batch, s.heads_q, s.hi_stride, **f)
+        self.demoted = torch.empty(s.batch, s.heads_kv, 1, dtype=torch.int32, device=dev)
+        self.ws_own = workspace(mikv_workspace_bytes(s, WS_ATTENTION, s.lo_cap), dev)
+        self.ws_prefix = workspace(mikv_prefix_workspace_bytes(like, k_prefix), dev)
+
+    @classmethod
+    def from_prompts(cls, shape: Shape, table: RotaryTable, prefix, own, out_prefix, out_own, key_len=None):
+        """The prompts of a batch: prefix = (q, k, v) of the shared tokens ([1, H, P, d], bf16), own = (q, k, v) of each
+        request's own tokens ([B, H, T, d]). Turns q and k (in place), attends the prefix (into out_prefix) and the
+        own tokens over prefix and own keys (into out_own; key_len int32 [B]: keys of each request, P + its own
+        tokens, the rest being padding), and builds the own cache by accumulated attention. shape is the own cache's
+        (shape_for_context with context = T)."""
+        q0, k0, v0 = prefix
+        q, k, v = own
+        B, Hkv, T, d = k.shape
+        P = k0.shape[2]
+        mikv_rotary(table, q0, k0)
+        mikv_rotary(table, q, k, start=P)
+        ws = workspace(mikv_prompt_workspace_bytes(q0, k0), k.device)
+        mikv_prompt_attention(q0, k0, v0, out_prefix, ws)
+        keys = torch.cat([k0.expand(B, Hkv, P, d), k], dim=2)
+        values = torch.cat([v0.expand(B, Hkv, P, d), v], dim=2)
+        spans = None
+        if key_len is not None:
+            spans = torch.empty(B, T, 2, dtype=torch.int32, device=k.device)
+            mikv_mask_spans(spans, P + T, key_len=key_len)
+        ws = workspace(mikv_prompt_workspace_bytes(q, keys), k.device)
+        mikv_prompt_attention(q, keys, values, out_own, ws, spans=spans)
+        layer = MixedPrecisionLayer.from_prefill(shape, k.contiguous(), v.contiguous(), None, q.contiguous(),
+                                                 device=k.device)
+        return cls(layer, k0.contiguous(), v0.contiguous(), table)
+
+    def step(self, q, k_new, v_new, out):
+        """One decode step: q [B, Hq, d], k_new, v_new [B, Hkv, d] of the new token as projected (q and k_new are turned
+        in place) into out [B, Hq, d]. The importance update takes the weights of the softmax over both parts."""
+        o, c = self.own, self.own.cache
+        s = o.shape
+        mikv_rotary(self.table, q[:, :, None], k_new[:, :, None], start=self.prefix + o.pos)
+        mikv_insert_token(c, k_new, v_new, o.pos, o.slots)
+        mikv_decode_attention(c, o.n_lo, q, o.sm_scale, self.own_out, self.ws_own, hi_logits=self.logits, ml=self.own_ml)
+        mikv_prefix_attention(q, self.k_prefix, self.v_prefix, out, self.ws_prefix, own_out=self.own_out,
+                              own_ml=self.own_ml, ml=self.ml)
+        mikv_update_importance(c, self.logits, self.ml)
+        mikv_select_demote(c.acc, s.hi_cap, 1, self.demoted, ids=c.hi_tok)
+        if s.bits:
+            mikv_quantize_pack(c, c.k_hi, c.v_hi, self.demoted, o.n_lo, src_tok=c.hi_tok)
+            o.n_lo += 1
+        o.slots.copy_(self.demoted[:, :, 0])
+        o.pos += 1
 
 
 def oracle_eviction_attention(k, v, q, budget: int, sm_scale: float, out, device="cuda"):
