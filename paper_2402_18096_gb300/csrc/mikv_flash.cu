@@ -97,46 +97,67 @@ struct MergePartsArgs {
   int n_splits, out_kind;
 };
 
-// One warp per output row: the parts weighted by 2^(lse - largest), then the join with the request's own part.
+// The parts of an output row weighted by 2^(lse - largest), then the join with the request's own part. W warps share a
+// row (more than eight parts: four), each with up to eight parts at a time; their sums and outputs are asked for
+// together (a part that has seen nothing holds anything: it is left out by its sum).
+template <int W>
 __global__ void __launch_bounds__(128) merge_parts_kernel(const __grid_constant__ MergePartsArgs m) {
   const FlashArgs& a = m.a;
-  const long long row = blockIdx.x * 4ll + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long row = W == 1 ? blockIdx.x * 4ll + warp : (long long)blockIdx.x;
+  const int first = W == 1 ? 0 : warp;
+  __shared__ float s_top[4], s_sum[4];
+  __shared__ float4 s_acc[4][32];
   grid_dependency_wait();
-  if (row >= m.part_rows) return;
-  float top = -INFINITY, mine = -INFINITY;  // lane s holds the sum of part s (of 32 at a time)
-  for (int s0 = 0; s0 < m.n_splits; s0 += 32) {
-    const float e = s0 + lane < m.n_splits ? m.part_lse[(s0 + lane) * m.part_rows + row] : -INFINITY;
-    if (s0 == 0) mine = e;
-    top = fmaxf(top, e);
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  float sum = 0.f;
+  if (W == 1 && row >= m.part_rows) return;
+  float top = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s0 = 0; s0 < m.n_splits; s0 += 32) {
-    if (s0 > 0) mine = s0 + lane < m.n_splits ? m.part_lse[(s0 + lane) * m.part_rows + row] : -INFINITY;
-    const float w_mine = mine == -INFINITY ? 0.f : fast_exp2(mine - top);
-    const int n = min(32, m.n_splits - s0);
-    const float4* part = reinterpret_cast<const float4*>(m.part_o + (s0 * m.part_rows + row) * kHeadDim) + lane;
-    for (int s = 0; s < n; s += 8) {  // eight parts' loads in flight
-      float4 o[8];
-      float w[8];
+  const float4* part = reinterpret_cast<const float4*>(m.part_o + row * kHeadDim) + lane;
+  for (int s0 = first; s0 < m.n_splits; s0 += 8 * W) {
+    float e[8];
+    float4 o[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        w[i] = __shfl_sync(0xffffffffu, w_mine, min(s + i, 31));
-        if (s + i >= n) w[i] = 0.f;
-        // (the output of a part that has seen nothing may be anything)
-        o[i] = w[i] != 0.f ? __ldcs(part + (s + i) * m.part_rows * (kHeadDim / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int s = s0 + W * i;
+      e[i] = s < m.n_splits ? m.part_lse[s * m.part_rows + row] : -INFINITY;
+      o[i] = s < m.n_splits ? __ldcs(part + s * m.part_rows * (kHeadDim / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    float next = top;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        sum += w[i];
-        acc.x = fmaf(o[i].x, w[i], acc.x);
-        acc.y = fmaf(o[i].y, w[i], acc.y);
-        acc.z = fmaf(o[i].z, w[i], acc.z);
-        acc.w = fmaf(o[i].w, w[i], acc.w);
-      }
+    for (int i = 0; i < 8; ++i) next = fmaxf(next, e[i]);
+    const float c = top == -INFINITY ? 0.f : fast_exp2(top - next);
+    sum *= c;
+    acc.x *= c, acc.y *= c, acc.z *= c, acc.w *= c;
+    top = next;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (e[i] == -INFINITY) continue;
+      const float w = fast_exp2(e[i] - top);
+      sum += w;
+      acc.x = fmaf(o[i].x, w, acc.x);
+      acc.y = fmaf(o[i].y, w, acc.y);
+      acc.z = fmaf(o[i].z, w, acc.z);
+      acc.w = fmaf(o[i].w, w, acc.w);
+    }
+  }
+  if constexpr (W > 1) {
+    if (lane == 0) s_top[warp] = top, s_sum[warp] = sum;
+    s_acc[warp][lane] = acc;
+    __syncthreads();
+    if (warp > 0) return;
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    sum = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if (s_top[i] == -INFINITY && s_sum[i] == 0.f) continue;
+      const float w = fast_exp2(s_top[i] - top);
+      const float4 o = s_acc[i][lane];
+      sum = fmaf(s_sum[i], w, sum);
+      acc.x = fmaf(o.x, w, acc.x);
+      acc.y = fmaf(o.y, w, acc.y);
+      acc.z = fmaf(o.z, w, acc.z);
+      acc.w = fmaf(o.w, w, acc.w);
     }
   }
   float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
@@ -217,7 +238,8 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   cudaError_t e = f16 ? launch_flash_kernel<true>(p, plan.mode, grid, st) : launch_flash_kernel<false>(p, plan.mode, grid, st);
   if (e != cudaSuccess || plan.n_splits == 1) return e;
   const MergePartsArgs m = {a, p.part_o, p.part_lse, p.part_rows, plan.n_splits, p.out_kind};
-  return launch_chained(merge_parts_kernel, dim3((unsigned)((p.part_rows + 3) / 4)), dim3(128), 0, st, m);
+  if (plan.n_splits > 8) return launch_chained(merge_parts_kernel<4>, dim3((unsigned)p.part_rows), dim3(128), 0, st, m);
+  return launch_chained(merge_parts_kernel<1>, dim3((unsigned)((p.part_rows + 3) / 4)), dim3(128), 0, st, m);
 }
 
 }  // namespace mikv
