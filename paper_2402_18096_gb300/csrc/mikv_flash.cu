@@ -1,5 +1,6 @@
 // mikv_flash.cu — attention over bf16 / fp16 keys: work plan, tensor maps, merge of split parts and dispatch (the
 // kernels are in mikv_flash.cuh).
+#include <limits.h>
 #include <string.h>
 
 #include <mutex>
@@ -50,51 +51,51 @@ bool encode_rows(CUtensorMap* map, bool f16, const void* data, const long long (
 
 struct Plan {
   int mode;  // flash::Mode
-  int m_blocks, n_splits;
+  int m_blocks, item_rows;
+  int shares;  // CTAs that share the key tiles out among them; 0: whole row tiles
 };
 
-// Splits a row block's key tiles may be cut into: up to three rounds of CTAs (four splits at least, for lengths that
-// turn out ragged), and at least two tiles each, so that both streams of a CTA have one. Grows with `tiles` only, so
-// a workspace sized for the longest keys serves shorter ones.
-int most_splits(long long base, int tiles, int num_sms) {
-  if (base >= 2ll * num_sms) return 1;
-  long long s = 3ll * num_sms / base;
-  s = s < 4 ? 4 : s;
-  s = s < tiles / 2 ? s : tiles / 2;
-  return s < 1 ? 1 : (int)s;
-}
+// Row tiles below this number may be shared out (above it the SMs are busy without, and parts would only cost traffic).
+long long most_shared(int num_sms) { return 2ll * num_sms; }
 
-// The number of splits that an estimate of the time makes shortest: rounds of items over the SMs, each a start and end
-// plus its key tiles, and for split rows the merge. The constants are measured (nanoseconds on an otherwise idle GB300).
+// Whole row tiles or shares, and for how many CTAs: what an estimate of the time makes shortest. A CTA has its tiles and
+// a start and end per item; shares add the merge, whose time is mostly the traffic of the parts. The constants
+// (nanoseconds) are measured on an otherwise idle GB300.
 Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
   Plan p;
   const long long rows = (long long)tq * G;
   const bool pair = rows > kTile;
   p.mode = pair ? flash::kPair : rows > flash::Layout<flash::kFew>::kRows ? flash::kOne : flash::kFew;
-  p.m_blocks = (int)(pair ? (rows + 2 * kTile - 1) / (2 * kTile) : 1);
+  p.item_rows = pair ? 2 * kTile : p.mode == flash::kOne ? kTile : flash::Layout<flash::kFew>::kRows;
+  p.m_blocks = (int)((rows + p.item_rows - 1) / p.item_rows);
   const long long base = (long long)batch * heads_kv * p.m_blocks;
-  const int tiles = (int)(((long long)tk + kTile - 1) / kTile);
-  p.n_splits = 1;
-  double best = 1e300;
-  for (int s = 1; s <= most_splits(base, tiles, num_sms); ++s) {
-    const long long items = base * s;
-    const double rounds = (double)((items + num_sms - 1) / num_sms);
-    const double busy = (double)(items < num_sms ? items : num_sms);
-    // a tile: the products and softmax, or its 64 KB at the SM's share of HBM
-    const double tile = pair ? 1650.0 : 9.7 * busy > 950.0 ? 9.7 * busy : 950.0;
-    const double merge = s > 1 ? 4500.0 + (double)s * rows * batch * heads_kv * kHeadDim * 8.0 / 5000.0 : 0.0;
-    const double cost = rounds * ((tiles + s - 1) / s * tile + 2000.0) + merge;
-    if (cost < best) best = cost, p.n_splits = s;
-  }
+  const long long tiles = ((long long)tk + kTile - 1) / kTile, units = base * tiles;
+  p.shares = 0;
+  if (base >= most_shared(num_sms) || units >= INT_MAX - 4 * num_sms) return p;
+  // a tile: the products and softmax, or its 64 KB at the SM's share of HBM
+  auto tile_ns = [&](double busy) { return pair ? 1600.0 : 9.7 * busy > 1150.0 ? 9.7 * busy : 1150.0; };
+  constexpr double kItem = 5000.0;  // start and end of an item
+  const double rounds = (double)((base + num_sms - 1) / num_sms);
+  double best = rounds * (tiles * tile_ns(base < num_sms ? base : num_sms) + kItem);
+  const double part_rows = rows < p.item_rows ? rows : p.item_rows;
+  auto consider = [&](int c) {
+    if (c < 1 || c > num_sms || c <= base / 2 || 2 * (long long)c > units) return;  // (a tile for each stream at least)
+    const double items = c % base == 0 ? 1.0 : 2.0 + (double)(base / c);  // the most that a share holds
+    const double cost = (double)((units + c - 1) / c) * tile_ns(c) + kItem * items + 5000.0 +
+                        ((double)c + base) * part_rows * kHeadDim * 4.0 / 3000.0;
+    if (cost < best) best = cost, p.shares = c;
+  };
+  for (int eighths = 1; eighths <= 8; ++eighths) consider(num_sms * eighths / 8);
+  for (long long c = 2 * base; c <= num_sms; c += base) consider((int)c);
   return p;
 }
 
 struct MergePartsArgs {
   FlashArgs a;
+  const int2* table;
   const float* part_o;
   const float* part_lse;
-  long long part_rows;
-  int n_splits, out_kind;
+  int rows, m_blocks, log2_item_rows, log2_G, out_kind;
 };
 
 // The parts of an output row weighted by 2^(lse - largest), then the join with the request's own part. W warps share a
@@ -104,23 +105,29 @@ template <int W>
 __global__ void __launch_bounds__(128) merge_parts_kernel(const __grid_constant__ MergePartsArgs m) {
   const FlashArgs& a = m.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long row = W == 1 ? blockIdx.x * 4ll + warp : (long long)blockIdx.x;
+  const int row = W == 1 ? blockIdx.x * 4 + warp : blockIdx.x;  // (set * tq + token) * heads_q + head
   const int first = W == 1 ? 0 : warp;
   __shared__ float s_top[4], s_sum[4];
   __shared__ float4 s_acc[4][32];
+  const int bt = row / a.heads_q, head = row - bt * a.heads_q, b = bt / a.tq, token = bt - b * a.tq;
+  const int kv = head >> m.log2_G, in_head = (token << m.log2_G) + (head & (a.G - 1));
+  const int tile = (b * a.heads_kv + kv) * m.m_blocks + (in_head >> m.log2_item_rows);
   grid_dependency_wait();
-  if (W == 1 && row >= m.part_rows) return;
+  if (W == 1 && row >= m.rows) return;
+  const int2 share = m.table[tile];
+  const long long at0 = ((long long)(share.x + tile) << m.log2_item_rows) + (in_head & ((1 << m.log2_item_rows) - 1));
   float top = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float4* part = reinterpret_cast<const float4*>(m.part_o + row * kHeadDim) + lane;
-  for (int s0 = first; s0 < m.n_splits; s0 += 8 * W) {
+  for (int s0 = first; s0 < share.y; s0 += 8 * W) {
     float e[8];
     float4 o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int s = s0 + W * i;
-      e[i] = s < m.n_splits ? m.part_lse[s * m.part_rows + row] : -INFINITY;
-      o[i] = s < m.n_splits ? __ldcs(part + s * m.part_rows * (kHeadDim / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const long long at = at0 + ((long long)s << m.log2_item_rows);
+      e[i] = s < share.y ? m.part_lse[at] : -INFINITY;
+      o[i] = s < share.y ? __ldcs(reinterpret_cast<const float4*>(m.part_o + at * kHeadDim) + lane)
+                         : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     float next = top;
 #pragma unroll
@@ -171,9 +178,6 @@ __global__ void __launch_bounds__(128) merge_parts_kernel(const __grid_constant_
     v[2] = fmaf(o.z, f1, v[2]);
     v[3] = fmaf(o.w, f1, v[3]);
   }
-  const int head = (int)(row % a.heads_q);
-  const long long bt = row / a.heads_q;
-  const int token = (int)(bt % a.tq), b = (int)(bt / a.tq);
   const long long at = b * a.o_b + head * a.o_h + token * a.o_t + 4 * lane;
   if (m.out_kind == 2)
     *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
@@ -186,16 +190,16 @@ __global__ void __launch_bounds__(128) merge_parts_kernel(const __grid_constant_
 
 }  // namespace
 
+// Room for the parts of every plan that keys up to tk may get: it depends on the row tiles alone.
 size_t flash_workspace_bytes(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
-  const Plan p = plan_flash(batch, heads_kv, G, tq, tk, num_sms);
+  const Plan p = plan_flash(batch, heads_kv, G, tq, 0, num_sms);
   const long long base = (long long)batch * heads_kv * p.m_blocks;
-  const int tiles = (int)(((long long)tk + kTile - 1) / kTile);
-  const int s = most_splits(base, tiles, num_sms);
-  const size_t rows = (size_t)batch * tq * heads_kv * G;
-  return kWsHeader + (s > 1 ? (size_t)s * rows * (kHeadDim + 1) * sizeof(float) : 0);
+  if (base >= most_shared(num_sms) || tk == 0) return kWsHeader;
+  const size_t slots = (size_t)(base + num_sms);
+  return kWsHeader + (base * sizeof(int2) + 255) / 256 * 256 + slots * p.item_rows * (kHeadDim + 1) * sizeof(float);
 }
 
-bool flash_fits(int batch, int heads_kv, int G, int tq) {  // (with up to eight rounds of splits and a round of slack)
+bool flash_fits(int batch, int heads_kv, int G, int tq) {
   const double blocks = ((double)tq * G + 2 * kTile - 1) / (2 * kTile);
   return (double)batch * heads_kv * blocks < 2.0e9 && (double)batch * tq * heads_kv * G < 8.0e9;
 }
@@ -205,11 +209,27 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   FlashKernelArgs p;
   memset(&p, 0, sizeof p);
   p.a = a;
-  p.n_splits = plan.n_splits;
   p.out_kind = out_f32 ? 2 : f16 ? 1 : 0;
-  p.part_rows = (long long)a.batch * a.tq * a.heads_q;
-  p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + kWsHeader);
-  p.part_lse = p.part_o + (size_t)plan.n_splits * p.part_rows * kHeadDim;
+  const int heads = a.batch * a.heads_kv;
+  const int base = heads * plan.m_blocks;
+  p.m_blocks = plan.m_blocks;
+  p.n_items = base;
+  p.log2_G = a.G == 1 ? 0 : a.G == 2 ? 1 : a.G == 4 ? 2 : 3;
+  if (plan.shares) {
+    const size_t slots = (size_t)base + num_sms;
+    p.shares = plan.shares;
+    p.by_length = a.lens && !a.spans && !a.causal;
+    p.units = (int)(((long long)a.tk + kTile - 1) / kTile);
+    p.share_each = (int)((long long)base * p.units / p.shares);
+    p.share_extra = (int)((long long)base * p.units % p.shares);
+    p.by_units.set(p.units);
+    p.by_set.set(a.heads_kv * plan.m_blocks);
+    p.by_block.set(plan.m_blocks);
+    char* at = static_cast<char*>(ws) + kWsHeader;
+    p.part_table = reinterpret_cast<int2*>(at);
+    p.part_o = reinterpret_cast<float*>(at + ((size_t)base * sizeof(int2) + 255) / 256 * 256);
+    p.part_lse = p.part_o + slots * plan.item_rows * kHeadDim;
+  }
   if (a.tk > 0) {
     p.k_batch = a.k_b != 0, p.k_head = a.k_h != 0, p.v_batch = a.v_b != 0, p.v_head = a.v_h != 0;
     const uint32_t box_q[3] = {(uint32_t)a.G, (uint32_t)((plan.mode == flash::kFew ? flash::Layout<flash::kFew>::kRows : kTile) / a.G), 1},
@@ -219,27 +239,25 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
         !encode_rows(&p.map_v, f16, a.v, {a.tk, a.heads_kv, a.batch}, {a.v_t, a.v_h, a.v_b}, box_k))
       return cudaErrorInvalidValue;
   }
-  const int heads = a.batch * a.heads_kv;
-  p.m_blocks = plan.m_blocks;
-  p.n_items = heads * plan.m_blocks * plan.n_splits;
   // heads worked on together: as many as have their keys and values in half of L2, and enough to occupy every SM
   const long long l2_heads = (64ll << 20) / ((long long)a.tk * kHeadDim * 4 + 1) + 1;
-  const long long busy_heads = (num_sms + (long long)plan.m_blocks * plan.n_splits - 1) / ((long long)plan.m_blocks * plan.n_splits);
+  const long long busy_heads = (num_sms + (long long)plan.m_blocks - 1) / plan.m_blocks;
   const long long group = l2_heads > busy_heads ? l2_heads : busy_heads;
   p.group_heads = group < heads ? (int)group : heads;
-  p.log2_G = a.G == 1 ? 0 : a.G == 2 ? 1 : a.G == 4 ? 2 : 3;
   const int over = heads % p.group_heads;
-  p.by_group.set(p.group_heads * plan.m_blocks * plan.n_splits);
-  p.by_rank.set(p.group_heads * plan.n_splits);
-  p.by_last.set((over ? over : p.group_heads) * plan.n_splits);
-  p.by_split.set(plan.n_splits);
+  p.by_group.set(p.group_heads * plan.m_blocks);
+  p.by_rank.set(p.group_heads);
+  p.by_last.set(over ? over : p.group_heads);
   p.by_head.set(a.heads_kv);
-  const int grid = p.n_items < num_sms ? p.n_items : num_sms;
+  const int grid = p.shares ? p.shares : p.n_items < num_sms ? p.n_items : num_sms;
   cudaError_t e = f16 ? launch_flash_kernel<true>(p, plan.mode, grid, st) : launch_flash_kernel<false>(p, plan.mode, grid, st);
-  if (e != cudaSuccess || plan.n_splits == 1) return e;
-  const MergePartsArgs m = {a, p.part_o, p.part_lse, p.part_rows, plan.n_splits, p.out_kind};
-  if (plan.n_splits > 8) return launch_chained(merge_parts_kernel<4>, dim3((unsigned)p.part_rows), dim3(128), 0, st, m);
-  return launch_chained(merge_parts_kernel<1>, dim3((unsigned)((p.part_rows + 3) / 4)), dim3(128), 0, st, m);
+  if (e != cudaSuccess || !p.shares) return e;
+  MergePartsArgs m = {a, p.part_table, p.part_o, p.part_lse, a.batch * a.tq * a.heads_q, plan.m_blocks, 0, p.log2_G, p.out_kind};
+  while ((1 << m.log2_item_rows) < plan.item_rows) ++m.log2_item_rows;
+  // (four warps to a row pay where rows are few and parts many)
+  if (p.shares > 8 * base && m.rows <= 4096)
+    return launch_chained(merge_parts_kernel<4>, dim3(m.rows), dim3(128), 0, st, m);
+  return launch_chained(merge_parts_kernel<1>, dim3((m.rows + 3) / 4), dim3(128), 0, st, m);
 }
 
 }  // namespace mikv

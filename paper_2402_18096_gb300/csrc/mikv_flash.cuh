@@ -6,8 +6,9 @@
 // its positions, a shared prefix's tokens are its requests). The tq * G query rows of one KV head are packed into
 // tiles of 128 rows, row R = token * G + head, so that all heads and tokens that share keys share their loads.
 //
-// Work. An item is a row tile (pair) of one KV head and set of keys, or one of n_splits shares of its key tiles; the
-// parts of split rows are merged by a second kernel. A persistent CTA per SM takes items in turn, and its roles run
+// Work. An item is a row tile (pair) of one KV head and set of keys. Where there are few of them, their key tiles are laid
+// end to end and every CTA gets an equal run of them (a share): an item is then the part of a row tile's keys that
+// lies in a CTA's share, and the parts are merged by a second kernel. A persistent CTA per SM takes items in turn, and its roles run
 // ahead of one another across items: the next item's tiles are loaded and its first scores computed while the softmax
 // warps still write the last item's output. (Measured against a CTA per item: see the plan in mikv_flash.cu.)
 //
@@ -83,6 +84,7 @@ struct Layout {
   static constexpr bool PAIR = MODE == kPair;
   static constexpr int kCopies = MODE == kFew ? 4 : 1;   // of the rows in a tile
   static constexpr int kRows = kTile / kCopies;          // rows of a tile
+  static constexpr int kItemRows = (PAIR ? 2 : 1) * kRows;  // rows of an item
   static constexpr int kExchange = MODE == kFew ? 8 * 32 * kExPitch * 4 : 0;  // for joining the copies
   static constexpr int kQ = PAIR ? 2 : 1;  // query tiles in shared memory
   static constexpr int kStages = 5;        // K / V tiles in the ring
@@ -332,7 +334,7 @@ __device__ __forceinline__ void join_own(const FlashArgs& a, size_t row, float& 
 // One item of work: its place, per stream the key tiles [t0, t1) that some row sees and the keys that every row sees, and
 // this item's share [T0, T1) of the union of both streams' tiles. As it lies in shared memory.
 struct alignas(16) ItemData {
-  int b, h, m_block, split;
+  int b, h, m_block, slot;  // slot: where the part of a share goes
   int t0[2], t1[2];
   int all_lo[2], all_hi[2];
   int T0, T1;
@@ -351,26 +353,29 @@ struct Item : ItemData {
   __device__ int tiles_of(int w) const { return PAIR ? n : w ? n / 2 : (n + 1) / 2; }  // visited by stream w
 };
 
-// Item number `index`, worked out by a whole warp (the same in every lane). Heads go in groups whose keys fit in L2
-// together; within a group a causal prompt's longest rows come first.
-template <int MODE>
-__device__ __forceinline__ ItemData item_at(const FlashKernelArgs& p, int index, int lane) {
-  constexpr bool PAIR = MODE == kPair;
+// Place of item number `index` among whole row tiles. Heads go in groups whose keys fit in L2 together; within a group a
+// causal prompt's longest rows come first.
+__device__ __forceinline__ ItemData place_at(const FlashKernelArgs& p, int index) {
   const FlashArgs& a = p.a;
-  ItemData x;
+  ItemData x = {};
   const int group = p.by_group.div(index);
   int rest = index - group * p.by_group.d;
   const bool last = (group + 1) * p.group_heads > a.batch * a.heads_kv;  // (a smaller group)
   const int rank = last ? p.by_last.div(rest) : p.by_rank.div(rest);
   rest -= rank * (last ? p.by_last.d : p.by_rank.d);
-  const int in_group = p.by_split.div(rest);
-  x.split = rest - in_group * p.n_splits;
-  const int bh = group * p.group_heads + in_group;
+  const int bh = group * p.group_heads + rest;
   x.b = p.by_head.div(bh);
   x.h = bh - x.b * a.heads_kv;
   x.m_block = p.m_blocks - 1 - rank;
+  return x;
+}
+
+// The key tiles of an item whose place is known, worked out by a whole warp (the same in every lane).
+template <int MODE>
+__device__ __forceinline__ void item_tiles(const FlashKernelArgs& p, ItemData& x, int lane) {
+  constexpr bool PAIR = MODE == kPair;
+  const FlashArgs& a = p.a;
   x.valid = 1;
-  x.unused = 0;
   const int toks = Layout<MODE>::kRows / a.G;
   constexpr int W = PAIR ? 2 : 1;
   // what the tokens of each tile see: their union [lo, hi) (hi = 0: none), and what all of them see
@@ -431,12 +436,22 @@ __device__ __forceinline__ ItemData item_at(const FlashKernelArgs& p, int index,
   x.T0 = min(x.t0[0], x.t0[1]);
   x.T1 = max(x.t1[0], x.t1[1]);
   if (x.T1 == 0) x.T0 = 0;
-  if (p.n_splits > 1) {
-    const int chunk = p.by_split.div(x.T1 - x.T0 + p.n_splits - 1);
-    x.T0 = min(x.T1, x.T0 + x.split * chunk);
-    x.T1 = min(x.T1, x.T0 + chunk);
+}
+
+// Units (key tiles) are numbered set by set, head by head, row block by row block; CTA c has the units [first(c),
+// first(c + 1)), one more for the first `extra` CTAs.
+struct Shares {
+  int each, extra;
+  __device__ int first(int c) const { return c * each + min(c, extra); }
+  __device__ int owner(int u) const {
+    const int big = extra * (each + 1);
+    return u < big ? u / (each + 1) : extra + (u - big) / each;
   }
-  return x;
+};
+// Units of every row block of set b: its key tiles where they follow from the set's length, else those of all keys (and a
+// part takes the same fraction of the tiles that the row block really has).
+__device__ __forceinline__ int units_of(const FlashKernelArgs& p, int b) {
+  return p.by_length ? (max(0, min(p.a.lens[b], p.a.tk)) + kTile - 1) / kTile : p.units;
 }
 
 // Items of this CTA: one of every gridDim.x, alternately from the front and from the back of a round, which evens out
@@ -483,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     prefetch_tensormap(&p.map_k);
     prefetch_tensormap(&p.map_v);
   }
-  if (p.n_splits > 1) allow_dependent_launch();  // the merge may be scheduled; it waits for this grid's end
+  if (p.shares) allow_dependent_launch();  // the merge may be scheduled; it waits for this grid's end
   tcgen05_before_sync();
   __syncthreads();
   tcgen05_after_sync();
@@ -733,17 +748,110 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         }
       }
     } else {  // the coming items, up to kItemRing ahead, and the end
-      for (int round = 0;; ++round) {
-        const int index = item_index(round);
-        ItemData x = {};
-        if (index < p.n_items) x = item_at<MODE>(p, index, lane);
-        if (round >= kItemRing && !mbar_wait_warp(sm.itemfree(round), ((round / kItemRing) & 1) ^ 1, fail)) break;
+      int round = 0;
+      auto publish = [&](const ItemData& x) {
+        if (round >= kItemRing && !mbar_wait_warp(sm.itemfree(round), ((round / kItemRing) & 1) ^ 1, fail)) return false;
         if (lane == 0) {
           s_item[round % kItemRing] = x;
           mbar_arrive(sm.itemfull(round));
         }
         __syncwarp();
-        if (index >= p.n_items) break;
+        ++round;
+        return true;
+      };
+      bool ok = true;
+      if (!p.shares) {
+        for (int index = item_index(0); ok && index < p.n_items; index = item_index(round)) {
+          ItemData x = place_at(p, index);
+          item_tiles<MODE>(p, x, lane);
+          ok = publish(x);
+        }
+        if (ok) publish(ItemData{});
+      } else {
+        const int c = blockIdx.x, per_set = a.heads_kv * p.m_blocks;
+        Shares sh = {p.share_each, p.share_extra};
+        // the first row block of this share: set b, number `in_set` in it, first unit `start`
+        int b = 0, in_set = 0, start = 0, lo, hi;
+        if (!p.by_length) {
+          lo = sh.first(c), hi = sh.first(c + 1);
+          const int m = p.by_units.div(lo);
+          b = p.by_set.div(m);
+          in_set = m - b * per_set;
+          start = m * p.units;
+        } else {
+          auto scan = [&](int b0, int& mine) {  // units of the sets b0 .. b0 + lane, and of this lane's
+            mine = b0 + lane < a.batch ? units_of(p, b0 + lane) * per_set : 0;
+            int sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+              const int y = __shfl_up_sync(0xffffffffu, sum, o);
+              if (lane >= o) sum += y;
+            }
+            return sum;
+          };
+          int mine, sum = scan(0, mine), all = __shfl_sync(0xffffffffu, sum, 31);
+          for (int b0 = 32; b0 < a.batch; b0 += 32) {
+            int other;
+            all += __shfl_sync(0xffffffffu, scan(b0, other), 31);
+          }
+          sh.each = all / (int)gridDim.x;
+          sh.extra = all - sh.each * gridDim.x;
+          lo = sh.first(c), hi = sh.first(c + 1);
+          int before = 0;
+          for (int b0 = 0; lo < hi && b0 < a.batch; b0 += 32) {
+            if (b0 > 0) sum = scan(b0, mine);
+            const int total = __shfl_sync(0xffffffffu, sum, 31);
+            if (lo < before + total) {
+              const int at = __ffs(__ballot_sync(0xffffffffu, before + sum > lo)) - 1;
+              b = b0 + at;
+              start = before + __shfl_sync(0xffffffffu, sum - mine, at);
+              const int t = __shfl_sync(0xffffffffu, mine, at) / per_set;
+              in_set = (lo - start) / t;
+              start += in_set * t;
+              break;
+            }
+            before += total;
+          }
+        }
+        for (int u = lo; ok && u < hi;) {
+          const int t = units_of(p, b), from = u - start, end = min(hi - start, t);
+          ItemData x = {};
+          x.b = b;
+          x.h = p.by_block.div(in_set);
+          x.m_block = in_set - x.h * p.m_blocks;
+          x.slot = c + b * per_set + in_set;
+          item_tiles<MODE>(p, x, lane);
+          const int n = x.T1 - x.T0;
+          if (!p.by_length) {
+            x.T1 = x.T0 + (int)((long long)n * end / t);
+            x.T0 += (int)((long long)n * from / t);
+          } else {
+            x.T1 = x.T0 + end;
+            x.T0 += from;
+          }
+          ok = publish(x);
+          u = start + end;
+          if (end == t) {  // on to the next row block that has units
+            start += t;
+            if (++in_set == per_set) {
+              in_set = 0;
+              do ++b;
+              while (b < a.batch && units_of(p, b) == 0);
+            }
+          }
+        }
+        if (ok) publish(ItemData{});
+        if (c == 0) {  // for the merge: the first CTA of each row block, and how many share it
+          int unit = 0;
+          for (int set = 0; set < a.batch; ++set) {
+            const int t = units_of(p, set);
+            for (int i = lane; i < per_set; i += 32) {
+              const int u0 = unit + i * t, first = t > 0 ? sh.owner(u0) : 0;
+              p.part_table[set * per_set + i] = make_int2(first, t > 0 ? sh.owner(u0 + t - 1) - first + 1 : 0);
+            }
+            unit += per_set * t;
+          }
+        }
       }
     }
   } else {  // softmax warps
@@ -939,6 +1047,24 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           sum += pack(v, w);
           return true;
         };
+        // A row without a reference takes one from 32 columns of its first tile, where no mask is in the way: any finite
+        // one will do that the sums do not outgrow, and the fast path checks that.
+        if (careful && !masked && __any_sync(0xffffffffu, ref == -INFINITY)) {
+          const int col = MODE == kFew ? 32 * (warp & 3) : 0;
+          float v[32];
+          load(col, v);
+          loaded(v);
+          row_scores<CAP, BIAS, 32>(v, sc, row, k0, col, 0.f, side_of(k0 + col, 32));
+          float mx = -INFINITY, mx2 = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            mx = max3(mx, v[e], v[e + 1]);
+            mx2 = max3(mx2, v[e + 2], v[e + 3]);
+          }
+          mx = fmaxf(mx, mx2);
+          if (ref == -INFINITY && mx > -INFINITY) ref = mx - ref_drop<F16>();
+          careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
+        }
         // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards; nothing is
         // stored before the check.
         bool slow = masked || careful;
@@ -1032,13 +1158,13 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       }
       // where the row goes; the next item's row is asked for before this one is written
       const size_t out_row = ((size_t)x.b * a.tq + token) * a.heads_q + head;
-      const bool whole = p.n_splits == 1;
+      const bool whole = !p.shares;
+      const long long part_at = (long long)x.slot * L::kItemRows + (PAIR ? stream * kTile : 0) + r;
       char* dst = whole ? static_cast<char*>(a.out) +
                               (x.b * a.o_b + head * a.o_h + token * a.o_t) * (p.out_kind == 2 ? 4 : 2)
-                        : reinterpret_cast<char*>(p.part_o + ((size_t)x.split * p.part_rows + out_row) * kHeadDim);
-      const long long stat_at = whole ? x.b * a.s_b + head * a.s_h + token * a.s_t
-                                      : (long long)x.split * p.part_rows + (long long)out_row;
-      const int n = x.n, set = x.b, head0 = x.h * a.G, split = x.split;
+                        : reinterpret_cast<char*>(p.part_o + part_at * kHeadDim);
+      const long long stat_at = whole ? x.b * a.s_b + head * a.s_h + token * a.s_t : part_at;
+      const int n = x.n, set = x.b, head0 = x.h * a.G, slot = x.slot;
       if (ok) ok = next_item(round + 1, x);
       if (ok && x.valid) load_row();
       if (ok && it > 0) {
@@ -1103,7 +1229,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         const Joined jo = join(orow, othere, orow_out);
         char* odst = whole ? static_cast<char*>(a.out) +
                                  (set * a.o_b + ohead * a.o_h + otoken * a.o_t) * (p.out_kind == 2 ? 4 : 2)
-                           : reinterpret_cast<char*>(p.part_o + ((size_t)split * p.part_rows + orow_out) * kHeadDim);
+                           : reinterpret_cast<char*>(p.part_o + ((size_t)slot * L::kItemRows + orow) * kHeadDim);
         const int kind = whole ? p.out_kind : 2;
 #pragma unroll 1
         for (int q = 0; q < 8; ++q) {
@@ -1143,7 +1269,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           if (whole)
             store_stat(a, set * a.s_b + ohead * a.s_h + otoken * a.s_t, jo.lse2);
           else
-            p.part_lse[(long long)split * p.part_rows + (long long)orow_out] = jo.lse2;
+            p.part_lse[(size_t)slot * L::kItemRows + orow] = jo.lse2;
         }
         tcgen05_before_sync();
         if (softmax_sync(*fail)) break;

@@ -57,17 +57,22 @@ struct FlashKernelArgs {
   CUtensorMap map_k, map_v;  // [batch][heads][keys][128], box 64 channels x 128 keys
   FlashArgs a;
   int k_batch, k_head, v_batch, v_head;  // 1, or 0 where the dimension is shared (zero stride)
-  int n_splits;         // items that share a row tile's keys; their parts are merged
   int m_blocks;         // row tiles (pairs) of one KV head
-  int n_items;          // batch * heads_kv * m_blocks * n_splits
+  int n_items;          // batch * heads_kv * m_blocks
   int group_heads;      // (set, KV head) combinations whose items are worked on together
   int log2_G;
-  // an item's number taken apart: by group, by rank within a full or the last group, by split, and a head into its set
-  FastDiv by_group, by_rank, by_last, by_split, by_head;
+  // an item's number taken apart: by group, by rank within a full or the last group, and a head into its set
+  FastDiv by_group, by_rank, by_last, by_head;
   int out_kind;         // 0 bf16, 1 fp16, 2 fp32
-  float* part_o;        // [n_splits][part_rows][128] normalised outputs, row = (set * tq + token) * heads_q + head
-  float* part_lse;      // [n_splits][part_rows] log2 of the sum of 2^x (-inf: nothing seen)
-  long long part_rows;
+  // Shares: the key tiles of all row tiles, end to end, in equal runs for the CTAs.
+  int shares;           // 0: whole row tiles
+  int by_length;        // units of a row tile: the tiles of its set's length (lens), else `units`
+  int units;
+  int share_each, share_extra;         // (not by_length) units of a CTA, and how many CTAs have one more
+  FastDiv by_units, by_set, by_block;  // a unit into its row tile, a row tile into its set, and into its head
+  int2* part_table;     // [batch * heads_kv * m_blocks]: first CTA of a row tile, and the number of its parts
+  float* part_o;        // [slots][rows of an item][128] normalised outputs, slot = CTA + row tile
+  float* part_lse;      // [slots][rows of an item] log2 of the sum of 2^x (-inf: nothing seen)
 };
 
 size_t flash_workspace_bytes(int batch, int heads_kv, int G, int tq, int tk, int num_sms);

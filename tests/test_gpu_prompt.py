@@ -393,6 +393,41 @@ def test_prefix_ragged_capped_biased_joined(shape, cap, bias, joined, out_dtype)
     check_prefix(q, k, v, out, ml, lens, q_pos, cap, sl, own_out, own_ml)
 
 
+@pytest.mark.parametrize("n,Hkv,P", [(70, 2, 1500), (33, 4, 700), (150, 1, 300)])
+def test_prefix_many_lengths(n, Hkv, P):
+    """More sets of keys than a warp has lanes, lengths from nothing to all, several of them empty in a row: every set
+    gets its share of the CTAs."""
+    g = gen(n)
+    lens = torch.randint(0, P + 1, (n,), generator=g, device="cuda", dtype=torch.int32)
+    lens[::7] = 0
+    lens[30:34] = 0
+    lens[-1] = P
+    q = torch.randn(n, 4 * Hkv, 128, generator=g, device="cuda").to(BF)
+    k, v = make(g, (n, Hkv, P, 128), BF), make(g, (n, Hkv, P, 128), BF)
+    out, ml = prefix(q, k, v, lens=lens)
+    check_prefix(q, k, v, out, ml, lens)
+    lens.zero_()
+    out, ml = prefix(q, k, v, lens=lens)
+    assert bool((out == 0).all()) and bool((ml[..., 1] == 0).all())
+
+
+@pytest.mark.parametrize("shape", [(1, 8, 2, 64, 9000), (2, 4, 1, 130, 5000), (1, 1, 1, 300, 7000), (1, 4, 4, 20, 3000)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_keys_shared_out(shape):
+    """Few queries on long keys: the row tiles' keys are cut for many CTAs, at places that masks make ragged (spans,
+    causal)."""
+    B, Hq, Hkv, tq, tk = shape
+    g = gen(tk)
+    q, k, v = make(g, (B, Hq, tq, 128), BF), make(g, (B, Hkv, tk, 128), BF), make(g, (B, Hkv, tk, 128), BF)
+    sl = slopes_of(Hq)
+    out, lse = prompt(q, k, v, slopes=sl)
+    check_prompt(q, k, v, out, lse, causal_spans(B, tq, tk, tk - tq), slopes=sl, q_start=tk - tq)
+    a = torch.randint(0, tk, (B, tq, 2), generator=g, device="cuda", dtype=torch.int32).sort(dim=2).values.contiguous()
+    a[:, ::5] = 0
+    out, lse = prompt(q, k, v, spans=a, softcap=20.0)
+    check_prompt(q, k, v, out, lse, a, cap=20.0)
+
+
 def test_prefix_empty_everywhere():
     q = torch.randn(2, 4, 128, device="cuda").to(BF)
     k = torch.full((1, 2, 64, 128), math.nan, dtype=BF, device="cuda")
