@@ -49,6 +49,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "mikv_device.cuh"
 #include "mikv_flash.h"
@@ -218,14 +219,20 @@ __device__ __forceinline__ void row_scores(float* v, const Score& sc, const Row&
   }
 }
 
-// Scores outside the row's span, replaced by x.
-template <int N>
-__device__ __forceinline__ void mask_scores(float* v, const Row& row, int first_key, float x) {
-  const int first = row.lo - first_key;
-  const unsigned n = row.hi - row.lo;
+// 32 scores outside the row's span, replaced by x; below and above: whether any row of the warp needs that side.
+__device__ __forceinline__ void mask_scores(float* v, const Row& row, int first_key, bool below, bool above, float x) {
+  if (above) {
+    const int end = row.hi - first_key;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if ((unsigned)(i - first) >= n) v[i] = x;
+    for (int i = 0; i < 32; ++i)
+      if (i >= end) v[i] = x;
+  }
+  if (below) {
+    const int first = row.lo - first_key;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < first) v[i] = x;
+  }
 }
 
 template <bool F16>
@@ -975,9 +982,8 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           return true;
         };
         // The weights of N columns, packed, and their sum: v holds the scores less the reference.
-        auto pack = [&](const auto& v, auto& w) {
-          constexpr int N = sizeof(v) / sizeof(float);
-          static_assert(sizeof(w) == 2 * N, "two weights to a word");
+        auto pack_n = [&](const float* v, uint32_t* w, auto count) {
+          constexpr int N = decltype(count)::value;
           uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
           for (int e = 0; e < N; e += 2) {
@@ -989,6 +995,9 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
           f32x2_split(add_f32x2(acc[2], acc[3]), s2, s3);
           return (s0 + s1) + (s2 + s3);
+        };
+        auto pack = [&](const auto& v, auto& w) {
+          return pack_n(v, w, std::integral_constant<int, sizeof(v) / sizeof(float)>());
         };
         auto load = [&](int col, auto& v) {
           constexpr int N = sizeof(v) / sizeof(float);
@@ -1004,22 +1013,22 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         // the weights. False when a wait gave up.
         auto slow_weights = [&](auto& v, auto& w, int col, bool in_o, int o_half, int o_phase) {
           constexpr int N = sizeof(v) / sizeof(float);
-          float mx = -INFINITY, mx2 = -INFINITY;
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          bool seen[N / 32];  // by some row of the warp
 #pragma unroll
           for (int q = 0; q < N; q += 32) {
             const int key = k0 + col + q;
-            const bool cut = key < warp_all_lo || key + 32 > warp_all_hi;
-            if (CAP && cut) mask_scores<32>(v + q, row, key, 0.f);  // (four share a reciprocal)
+            seen[q / 32] = key < warp_hi && key + 32 > warp_lo;
+            if (!seen[q / 32]) continue;
+            const bool below = key < warp_all_lo, above = key + 32 > warp_all_hi;
+            if (CAP && (below || above)) mask_scores(v + q, row, key, below, above, 0.f);  // (four share a reciprocal)
             row_scores<CAP, BIAS, 32>(v + q, sc, row, k0, col + q, 0.f, side_of(key, 32));
-            if (cut) mask_scores<32>(v + q, row, key, -INFINITY);
+            if (below || above) mask_scores(v + q, row, key, below, above, -INFINITY);
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              mx = max3(mx, v[q + e], v[q + e + 1]);
-              mx2 = max3(mx2, v[q + e + 2], v[q + e + 3]);
-            }
+            for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[q + e], v[q + e + 1]);
           }
-          mx = fmaxf(mx, mx2);
-          const float next = mx > ref + ref_slack<F16>() ? mx - ref_drop<F16>() : ref;
+          const float largest = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+          const float next = largest > ref + ref_slack<F16>() ? largest - ref_drop<F16>() : ref;
           const bool moves = next != ref && ref != -INFINITY;
           if (__any_sync(0xffffffffu, moves)) {
             const float f = moves ? fast_exp2(ref - next) : 1.f;
@@ -1043,8 +1052,16 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           const float rr = ref == -INFINITY ? 0.f : ref;
           const uint64_t r2 = f32x2(-rr, -rr);
 #pragma unroll
-          for (int e = 0; e < N; e += 2) f32x2_split(add_f32x2(f32x2(v[e], v[e + 1]), r2), v[e], v[e + 1]);
-          sum += pack(v, w);
+          for (int q = 0; q < N; q += 32) {
+            if (seen[q / 32]) {
+#pragma unroll
+              for (int e = q; e < q + 32; e += 2) f32x2_split(add_f32x2(f32x2(v[e], v[e + 1]), r2), v[e], v[e + 1]);
+              sum += pack_n(v + q, w + q / 2, std::integral_constant<int, 32>());
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) w[q / 2 + e] = 0u;
+            }
+          }
           return true;
         };
         // A row without a reference takes one from 32 columns of its first tile, where no mask is in the way: any finite
@@ -1101,8 +1118,9 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           if (!ok) break;
           arrive(0, 2);
         } else {
-          // Without a cap the whole tile is handed over at once; with one, whose arithmetic takes longer, each half as
-          // it is ready, so that its product runs under the next half.
+          // Each half of a tile is handed over as it is ready, so that its product runs under the next half. Without a
+          // cap the second half's arithmetic starts before the first half's hand-over has gone through.
+          int first_half = 0;
           if (!CAP && !slow) {
             float v[2][64];
             uint32_t w[2][32];
@@ -1110,21 +1128,29 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             loaded(v[0]);
             load(64, v[1]);
             row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
-            float tile_sum = pack(v[0], w[0]);
-            loaded(v[1]);
-            row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
-            tile_sum += pack(v[1], w[1]);
-            slow = __any_sync(0xffffffffu, !(tile_sum <= sum_max<F16>()));  // a reference is too low (or a score NaN)
+            const float sum0 = pack(v[0], w[0]);
+            slow = __any_sync(0xffffffffu, !(sum0 <= sum_max<F16>()));  // a reference is too low (or a score NaN)
             if (!slow) {
-              sum += tile_sum;
+              sum += sum0;
+              first_half = 1;
               tmem_st32(ts, w[0]);
-              tmem_st32(ts + 32, w[1]);
-              arrive(0, 2);
+              loaded(v[1]);
+              row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
+              arrive(0, 1);
+              const float sum1 = pack(v[1], w[1]);
+              slow = __any_sync(0xffffffffu, !(sum1 <= sum_max<F16>()));
+              if (!slow) {
+                sum += sum1;
+                tmem_st32(ts + 32, w[1]);
+                arrive(1, 1);
+              }
+            } else {
+              loaded(v[1]);
             }
           }
           if (CAP || slow) {
 #pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
+            for (int half = first_half; half < 2; ++half) {
               float v[64];
               uint32_t w[32];
               bool slow_half = slow || careful;
