@@ -416,7 +416,8 @@ typedef struct {
   int32_t tq;         /* queries per row of the batch */
   int32_t tk;         /* keys per row of the batch */
   int32_t causal;     /* without spans: 1 = query i sees the keys up to its own position, 0 = all keys */
-  int32_t q_start;    /* position of query 0 among the keys (tk - tq when the queries are the last tokens) */
+  int32_t q_start;    /* position of query 0 among the keys (tk - tq when the queries are the last tokens); at most
+                         2^30 either way */
   float sm_scale;     /* > 0 */
   float softcap;      /* 0 = none; c > 0: scores become c tanh(score / c) */
 } mikv_prompt_desc;
@@ -427,9 +428,10 @@ typedef struct {
  *   out_i = sum_j softmax_j(s_i) v_j over the keys j that query i sees,  lse_i = ln sum_j exp(s_ij)
  * with p_i = q_start + i. A query that sees no key gives out = 0 and lse = -inf. Keys that no query sees may hold
  * any bits. A query that sees an infinity or NaN in V gets NaN in the channels concerned (in tiles that a mask
- * cuts, in all channels); other queries are not touched by it.
- * Scores and sums are fp32 (exact products, fp32 accumulation); the probabilities enter the product with V rounded
- * to the input type.
+ * cuts, in all channels); other queries are not touched by it (beyond the rounding of their own sums).
+ * Scores and sums are fp32 (exact products, fp32 accumulation; the cap within 2^-20 of its size, distances exact to
+ * 2^24); the probabilities enter the product with V rounded to the input type. Results do not depend on what else
+ * runs, and repeat bit for bit.
  *   q, k, v, out  views; 16-byte aligned data, strides multiples of 16 bytes. k and v may have a zero batch or head
  *                 stride (one set of keys for several)
  *   spans     int32 [batch][tq][2] from mikv_mask_spans, or NULL (then `causal` decides); lo < 0 counts as 0 and

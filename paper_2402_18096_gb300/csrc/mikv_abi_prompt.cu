@@ -77,6 +77,7 @@ mikv_status attn_common(int32_t dtype, int32_t out_dtype, int32_t batch, int32_t
 
 mikv_status prompt_ok(const mikv_prompt_desc* d) {
   if (!d) return MIKV_ERR_ARG;
+  if (d->q_start > (1 << 30) || d->q_start < -(1 << 30)) return MIKV_ERR_UNSUPPORTED;  // (positions stay in 32 bits)
   return attn_common(d->dtype, d->out_dtype, d->batch, d->heads_q, d->heads_kv, d->head_dim, d->tq, d->tk, d->sm_scale,
                      d->softcap);
 }

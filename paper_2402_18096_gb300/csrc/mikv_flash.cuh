@@ -141,7 +141,7 @@ constexpr float kRefExact = 0x1p22f;
 // The scores of one row in log2 units: x = cap(v * scale) - slope |pos - j|, times log2 e.
 struct Row {
   int lo, hi;        // keys the row sees
-  float pos;         // its position, as far as the bias needs it (exact below 2^24)
+  int pos;           // its position
   float slope;       // slope of its head times log2 e
 };
 
@@ -161,23 +161,27 @@ __device__ __forceinline__ float min_nan(float a, float b) {  // NaN if either i
   return y;
 }
 
-// The cap of four scores: cap tanh(y) + rest = (cap + rest) - 2 cap / (1 + e^2y). One reciprocal serves all four:
-// with p = (ac, bd) of the denominators a, b, c, d, 1 / a = bd c / (ac bd) and so on. 2^30 stands for larger
-// exponentials (tanh is then 1 to fp32 precision), which keeps the product of four inside fp32.
+// The cap of four scores: cap tanh(y) + rest = cap (e - 1) / (e + 1) + rest with e = e^2y. One reciprocal serves all
+// four: with p = (ac, bd) of the denominators a, b, c, d, 1 / a = bd c / (ac bd) and so on. 2^30 stands for larger
+// exponentials (tanh is then 1 to fp32 precision), which keeps the product of four inside fp32. For small y, e - 1 is
+// exact and the quotient's roundings are relative to it: only the exponential's own error, 2^-23 of cap, remains.
 __device__ __forceinline__ void cap_four(float* v, float scale, float cap, const float (&rest)[4]) {
-  const uint64_t s2 = f32x2(scale, scale), one = f32x2(1.f, 1.f), c2 = f32x2(-2.f * cap, -2.f * cap);
+  const uint64_t s2 = f32x2(scale, scale), one = f32x2(1.f, 1.f), less = f32x2(-1.f, -1.f), c2 = f32x2(cap, cap);
   float y[4];
   f32x2_split(mul_f32x2(f32x2(v[0], v[1]), s2), y[0], y[1]);
   f32x2_split(mul_f32x2(f32x2(v[2], v[3]), s2), y[2], y[3]);
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[i] = fast_exp2(min_nan(y[i], 30.f));
-  const uint64_t ab = add_f32x2(f32x2(y[0], y[1]), one), cd = add_f32x2(f32x2(y[2], y[3]), one);
+  const uint64_t e0 = f32x2(y[0], y[1]), e1 = f32x2(y[2], y[3]);
+  const uint64_t ab = add_f32x2(e0, one), cd = add_f32x2(e1, one);
   float ac, bd;
   f32x2_split(mul_f32x2(ab, cd), ac, bd);
   const float r = rcp_approx(ac * bd);
   const uint64_t s = mul_f32x2(f32x2(r, r), f32x2(bd, ac));
-  f32x2_split(fma_f32x2(mul_f32x2(s, cd), c2, f32x2(rest[0], rest[1])), v[0], v[1]);
-  f32x2_split(fma_f32x2(mul_f32x2(s, ab), c2, f32x2(rest[2], rest[3])), v[2], v[3]);
+  const uint64_t t0 = mul_f32x2(mul_f32x2(s, cd), add_f32x2(e0, less));
+  const uint64_t t1 = mul_f32x2(mul_f32x2(s, ab), add_f32x2(e1, less));
+  f32x2_split(fma_f32x2(t0, c2, f32x2(rest[0], rest[1])), v[0], v[1]);
+  f32x2_split(fma_f32x2(t1, c2, f32x2(rest[2], rest[3])), v[2], v[3]);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN operands are passed over
@@ -191,7 +195,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN opera
 template <bool CAP, bool BIAS, int N>
 __device__ __forceinline__ void row_scores(float* v, const Score& sc, const Row& row, int k0, int col0, float ref,
                                            int side) {
-  const float rest = (CAP ? sc.cap : 0.f) - ref;
+  const float rest = -ref;
   auto apply = [&](auto bias) {  // bias(i): the bias of column i, plus `rest`
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
@@ -208,7 +212,7 @@ __device__ __forceinline__ void row_scores(float* v, const Score& sc, const Row&
   if constexpr (!BIAS) {
     apply([&](int) { return rest; });
   } else {
-    const float e0 = (float)(k0 + col0) - row.pos;
+    const float e0 = (float)(int)((unsigned)(k0 + col0) - (unsigned)row.pos);  // (exact up to distances of 2^24)
     if (side != 0) {  // the bias is linear over the tile
       const float sl = side < 0 ? row.slope : -row.slope;
       const float base = fmaf(sl, e0, rest);
@@ -896,7 +900,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       const bool valid = token < a.tq;
       Row row;
       row.lo = row.hi = 0;
-      row.pos = 0.f;
+      row.pos = 0;
       row.slope = 0.f;
       int pos = 0;
       if (valid) {
@@ -910,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         }
         if constexpr (BIAS) {
           pos = a.pos ? at : a.pos_at_len ? len : a.q_start + token;
-          row.pos = (float)pos;
+          row.pos = pos;
           row.slope = slope * kLog2e;
         }
         if (row.hi <= row.lo) row.lo = row.hi = 0;
@@ -965,6 +969,12 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           return !BIAS ? 0 : key + n - 1 <= pos_min ? -1 : key >= pos_max ? 1 : 0;
         };
         const int side = side_of(k0, kTile);
+        // the bias (log2) of the nearest of the keys [key, key + n)
+        auto near_bias = [&](int key, int n) {
+          if (!BIAS) return 0.f;
+          const float e = (float)(int)((unsigned)key - (unsigned)row.pos);
+          return -row.slope * fmaxf(0.f, fmaxf(e, -(e + (float)(n - 1))));
+        };
         // The keys that the guard warp has found: rows that see one are marked (before the last weights are handed over,
         // which lets the tile's results be overwritten).
         auto mark = [&]() {
@@ -1015,6 +1025,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           constexpr int N = sizeof(v) / sizeof(float);
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
           bool seen[N / 32];  // by some row of the warp
+          // The scores are taken less `base`, close to the largest, where that is the fused form's to give: a distance
+          // bias of thousands then costs them no bits. Large references of other kinds: see kRefExact.
+          float base = ref == -INFINITY ? near_bias(k0 + col, N) : ref;
+          if (!(fabsf(base) <= kRefExact)) base = 0.f;
 #pragma unroll
           for (int q = 0; q < N; q += 32) {
             const int key = k0 + col + q;
@@ -1022,13 +1036,14 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             if (!seen[q / 32]) continue;
             const bool below = key < warp_all_lo, above = key + 32 > warp_all_hi;
             if (CAP && (below || above)) mask_scores(v + q, row, key, below, above, 0.f);  // (four share a reciprocal)
-            row_scores<CAP, BIAS, 32>(v + q, sc, row, k0, col + q, 0.f, side_of(key, 32));
+            row_scores<CAP, BIAS, 32>(v + q, sc, row, k0, col + q, base, side_of(key, 32));
             if (below || above) mask_scores(v + q, row, key, below, above, -INFINITY);
 #pragma unroll
             for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[q + e], v[q + e + 1]);
           }
           const float largest = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-          const float next = largest > ref + ref_slack<F16>() ? largest - ref_drop<F16>() : ref;
+          const float have = ref - base;  // (relative to the base)
+          const float next = largest > have + ref_slack<F16>() ? base + (largest - ref_drop<F16>()) : ref;
           const bool moves = next != ref && ref != -INFINITY;
           if (__any_sync(0xffffffffu, moves)) {
             const float f = moves ? fast_exp2(ref - next) : 1.f;
@@ -1049,7 +1064,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           }
           ref = next;
           careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
-          const float rr = ref == -INFINITY ? 0.f : ref;
+          const float rr = ref == -INFINITY ? 0.f : ref - base;
           const uint64_t r2 = f32x2(-rr, -rr);
 #pragma unroll
           for (int q = 0; q < N; q += 32) {
@@ -1071,7 +1086,8 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           float v[32];
           load(col, v);
           loaded(v);
-          row_scores<CAP, BIAS, 32>(v, sc, row, k0, col, 0.f, side_of(k0 + col, 32));
+          const float near = near_bias(k0 + col, 32);
+          row_scores<CAP, BIAS, 32>(v, sc, row, k0, col, near, side_of(k0 + col, 32));
           float mx = -INFINITY, mx2 = -INFINITY;
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
@@ -1079,7 +1095,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             mx2 = max3(mx2, v[e + 2], v[e + 3]);
           }
           mx = fmaxf(mx, mx2);
-          if (ref == -INFINITY && mx > -INFINITY) ref = mx - ref_drop<F16>();
+          if (ref == -INFINITY && mx > -INFINITY) ref = near + (mx - ref_drop<F16>());
           careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
         }
         // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards; nothing is

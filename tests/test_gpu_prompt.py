@@ -428,6 +428,23 @@ def test_keys_shared_out(shape):
     check_prompt(q, k, v, out, lse, a, cap=20.0)
 
 
+def test_bias_at_far_positions():
+    """A bias of far queries differs from that of near ones by a constant per row, which the softmax does not see: with
+    exact distances the output stays within the near queries' bounds, through masked tiles and unmasked ones."""
+    B, Hq, Hkv, tq, tk = 1, 4, 2, 70, 700
+    g = gen(23)
+    q, k, v = make(g, (B, Hq, tq, 128), BF), make(g, (B, Hkv, tk, 128), BF), make(g, (B, Hkv, tk, 128), BF)
+    sl = slopes_of(Hq)
+    spans = torch.empty(B, tq, 2, dtype=torch.int32, device="cuda")
+    spans[..., 0] = 3
+    spans[..., 1] = tk - 5 - torch.arange(tq, device="cuda") % 40
+    full = torch.tensor([0, tk], device="cuda").expand(B, tq, 2)
+    for q_start in (tk, 2 ** 17, 2 ** 20):
+        for s, kw in ((spans, dict(spans=spans)), (full, dict(causal=False))):
+            out, _ = prompt(q, k, v, q_start=q_start, slopes=sl, **kw)
+            check_prompt(q, k, v, out, None, s, slopes=sl, q_start=tk)
+
+
 def test_prefix_empty_everywhere():
     q = torch.randn(2, 4, 128, device="cuda").to(BF)
     k = torch.full((1, 2, 64, 128), math.nan, dtype=BF, device="cuda")
