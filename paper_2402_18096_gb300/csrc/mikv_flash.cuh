@@ -6,11 +6,11 @@
 // its positions, a shared prefix's tokens are its requests). The tq * G query rows of one KV head are packed into
 // tiles of 128 rows, row R = token * G + head, so that all heads and tokens that share keys share their loads.
 //
-// Work. An item is a row tile (pair) of one KV head and set of keys. Where there are few of them, their key tiles are laid
-// end to end and every CTA gets an equal run of them (a share): an item is then the part of a row tile's keys that
-// lies in a CTA's share, and the parts are merged by a second kernel. A persistent CTA per SM takes items in turn, and its roles run
-// ahead of one another across items: the next item's tiles are loaded and its first scores computed while the softmax
-// warps still write the last item's output. (Measured against a CTA per item: see the plan in mikv_flash.cu.)
+// Work. An item is a row tile (pair) of one KV head and set of keys. Where there are few of them, their key tiles are
+// laid end to end and every CTA gets an equal run of them (a share): an item is then the part of a row tile's keys that
+// lies in a CTA's share, and the parts are merged by a second kernel. A persistent CTA per SM takes items in turn, and
+// its roles run ahead of one another across items: the next item's tiles are loaded and its first scores computed while
+// the softmax warps still write the last item's output.
 //
 // A CTA has two streams, each with a score tile S (128 x 128 fp32) and an output tile O (128 x 128 fp32) in
 // TMEM, over 128-key tiles of K and V that TMA stages in a ring:
@@ -22,10 +22,12 @@
 //           are joined at the end. One warp that weighs whole tiles takes longer than HBM takes to deliver them: with
 //           capped and biased scores of 4 rows 5700 clocks for two tiles against 2700 a tile.
 // Roles: warps 0-3 and 4-7 are the streams' softmax warpgroups (thread = row = TMEM lane), warp 8 issues the copies,
-// warp 9 the MMAs, warp 10 guards masked tiles (below), warp 11 works out the coming items. Per stream and tile: S = Q K^T (8 MMAs of K = 16), softmax
-// to P (16-bit, written over S in TMEM), O += P V (8 MMAs with A in TMEM). The MMA warp alternates streams, so one
-// stream's softmax runs under the other's products. P lies over S and one warp issues all MMAs, which execute in the
-// order of issue: the next tile's scores may be issued right behind the product that reads P.
+// warp 9 the MMAs, warp 10 guards masked tiles (below), warp 11 works out the coming items. Per stream and tile:
+// S = Q K^T (8 MMAs of K = 16), softmax to P (16-bit, written over S in TMEM), O += P V (8 MMAs with A in TMEM). The MMA
+// warp alternates streams, so one stream's softmax runs under the other's products. P lies over S and one warp
+// issues all MMAs, which execute in the order of issue: the next tile's scores may be issued right behind the product
+// that reads P. The MMA warp stays converged (elect_one) so that its operands stay in uniform registers: issuing from one
+// lane's branch cost 80 clocks an MMA and a third of the rate.
 //
 // Barriers. Every role that waits on a barrier sees each of its phases in order (a wait that left phases out would
 // take an earlier one of the same parity for its own); counters run on from item to item.
@@ -37,10 +39,17 @@
 // tend to come first. Sums are fp32 over the unrounded weights; rounding the weights to 16 bits is what the tensor
 // cores take, and perturbs each weight by at most half a unit in its last place.
 //
-// Masks. Every row sees one span of keys [lo, hi). Tiles outside the union of the CTA's spans are not visited; tiles
+// Masks. Every row sees one span of keys [lo, hi). Tiles outside the union of an item's spans are not visited; tiles
 // inside every span are not masked. In the tiles between, a weight of 0 does not stop an infinity or NaN in V from
 // entering O (0 * inf), so the guard warp looks through the V tile first: rows with such a value are set to 0 and
 // their keys reported to the softmax threads, which mark the output rows that do see them.
+//
+// Bounds. Two row tiles take at least 2068 clocks of the tensor cores per key tile (4 x 128^3 at 517 each, measured alone)
+// and about 2900 in the kernel: what is left is the chain of one stream (scores -> softmax, about 1200 clocks -> product
+// and next scores, 1034, and two hand-overs), which two streams in 512 TMEM columns cannot hide altogether. Causal, T 8192,
+// 32 query and 8 KV heads: 345 us, 1.59 PFLOP/s. A cap adds an exponential and a quarter of a reciprocal per score
+// (1.00 PFLOP/s at the same size), a distance bias two fp32 operations (1.30). With one row tile a set's keys pass once:
+// HBM. 8 requests of 32 heads with 4096 keys of their own: 87 us, 6.2 TB/s (91 % of a copy).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -66,7 +75,7 @@ constexpr int kTile = 128;                     // query rows of a tile, keys of 
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kHalfBytes = kTileBytes / 2;     // one 64-channel box
 constexpr int kSoftThreads = 256;
-constexpr int kCopyWarp = 8, kMmaWarp = 9, kGuardWarp = 10, kItemWarp = 11;
+constexpr int kCopyWarp = 8, kMmaWarp = 9, kGuardWarp = 10;  // 11: the items'
 constexpr int kExPitch = 20;                   // floats of a row's 16 channels in the exchange (padded against conflicts)
 constexpr int kItemRing = 4;                   // items described ahead
 constexpr int kItemReaders = 11;               // warps that read an item's description: all but the one that writes it
