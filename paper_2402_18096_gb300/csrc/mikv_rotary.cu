@@ -7,6 +7,7 @@
 // items to a thread: the loads are issued first, the cosines and sines of the block's tokens are computed while
 // they are under way (once, in shared memory, for all heads), then everything is turned and written.
 #include "mikv_device.cuh"
+#include "mikv_internal.h"
 #include "mikv_rotary.h"
 
 namespace mikv {
@@ -75,6 +76,8 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
   const int gap = !HALF ? N : ch < a.rot ? half : (kHeadDim - a.rot) / 2;
   Vec<T> lo[kRotItems], hi[kRotItems];
   T* out[kRotItems];
+  grid_dependency_wait();
+  allow_dependent_launch();
 #pragma unroll
   for (int u = 0; u < kRotItems; ++u) {
     const int hz = r / kPerRow + u * step;
@@ -134,6 +137,8 @@ template <typename T, bool HALF>
 __global__ void __launch_bounds__(kRotThreads) rotary_elements_kernel(const __grid_constant__ RotaryArgs a, int log_tok) {
   extern __shared__ float2 s_cs[];
   const int half = a.rot / 2, b = blockIdx.y, t0 = blockIdx.x << log_tok, nt = min(1 << log_tok, a.tokens - t0);
+  grid_dependency_wait();
+  allow_dependent_launch();
   rotary_angles(a, s_cs, b, t0, nt);
   __syncthreads();
   const int items = half + kHeadDim - a.rot;
@@ -169,21 +174,22 @@ cudaError_t launch_rotary_t(const RotaryArgs& a, int layout, bool vec, cudaStrea
   const size_t smem = (size_t)tok * (a.rot / 2) * sizeof(float2);
   if (!vec) {
     auto k = layout == 0 ? rotary_elements_kernel<T, true> : rotary_elements_kernel<T, false>;
-    k<<<dim3(blocks, a.batch), kRotThreads, smem, st>>>(a, log_tok);
-    return cudaGetLastError();
+    return launch_chained(k, dim3(blocks, a.batch), dim3(kRotThreads), smem, st, a, log_tok);
   }
   const int heads = a.x[0].heads + a.x[1].heads;
   const int most = kRotThreads * kRotItems / (kHeadDim / Vec<T>::N / 2) / tok;  // heads of a block
   const int parts = (heads + most - 1) / most;
   if (parts > 65535) return cudaErrorInvalidValue;
   auto k = layout == 0 ? rotary_kernel<T, true> : rotary_kernel<T, false>;
-  k<<<dim3(blocks, a.batch, parts), kRotThreads, smem, st>>>(a, log_tok, (heads + parts - 1) / parts);
-  return cudaGetLastError();
+  return launch_chained(k, dim3(blocks, a.batch, parts), dim3(kRotThreads), smem, st, a, log_tok,
+                        (heads + parts - 1) / parts);
 }
 
 // One thread per query: the document that holds its position by binary search.
 __global__ void __launch_bounds__(256) mask_spans_kernel(const SpanArgs a) {
   const int i = blockIdx.x * 256 + threadIdx.x, b = blockIdx.y;
+  grid_dependency_wait();
+  allow_dependent_launch();
   if (i >= a.tq) return;
   const long long p = (long long)a.q_start + i;
   long long lo = 0, hi = a.causal ? p + 1 : a.tk;
@@ -222,8 +228,7 @@ cudaError_t launch_rotary(const RotaryArgs& a, int dtype, int layout, bool vec, 
 }
 
 cudaError_t launch_mask_spans(const SpanArgs& a, cudaStream_t st) {
-  mask_spans_kernel<<<dim3((a.tq + 255) / 256, a.batch), 256, 0, st>>>(a);
-  return cudaGetLastError();
+  return launch_chained(mask_spans_kernel, dim3((a.tq + 255) / 256, a.batch), dim3(256), 0, st, a);
 }
 
 }  // namespace mikv
