@@ -6,7 +6,6 @@
 #include <mutex>
 
 #include "mikv_flash.cuh"
-#include "mikv_internal.h"
 
 namespace mikv {
 namespace {
@@ -95,7 +94,7 @@ struct MergePartsArgs {
   const int2* table;
   const float* part_o;
   const float* part_lse;
-  int rows, m_blocks, log2_item_rows, log2_G, out_kind;
+  int rows, m_blocks, log2_item_rows, log2_G, out_kind;  // (out_kind: 0 bf16, 1 fp16, 2 fp32)
 };
 
 // The parts of an output row weighted by 2^(lse - largest), then the join with the request's own part. W warps share a
@@ -209,7 +208,7 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   FlashKernelArgs p;
   memset(&p, 0, sizeof p);
   p.a = a;
-  p.out_kind = out_f32 ? 2 : f16 ? 1 : 0;
+  p.out_f32 = out_f32;
   const int heads = a.batch * a.heads_kv;
   const int base = heads * plan.m_blocks;
   p.m_blocks = plan.m_blocks;
@@ -252,7 +251,7 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   const int grid = p.shares ? p.shares : p.n_items < num_sms ? p.n_items : num_sms;
   cudaError_t e = f16 ? launch_flash_kernel<true>(p, plan.mode, grid, st) : launch_flash_kernel<false>(p, plan.mode, grid, st);
   if (e != cudaSuccess || !p.shares) return e;
-  MergePartsArgs m = {a, p.part_table, p.part_o, p.part_lse, a.batch * a.tq * a.heads_q, plan.m_blocks, 0, p.log2_G, p.out_kind};
+  MergePartsArgs m = {a, p.part_table, p.part_o, p.part_lse, a.batch * a.tq * a.heads_q, plan.m_blocks, 0, p.log2_G, out_f32 ? 2 : f16 ? 1 : 0};
   while ((1 << m.log2_item_rows) < plan.item_rows) ++m.log2_item_rows;
   // (four warps to a row pay where rows are few and parts many)
   if (p.shares > 8 * base && m.rows <= 4096)

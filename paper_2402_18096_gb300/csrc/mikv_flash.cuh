@@ -62,6 +62,7 @@
 
 #include "mikv_device.cuh"
 #include "mikv_flash.h"
+#include "mikv_internal.h"
 #include "mikv_tcgen05.cuh"
 
 namespace mikv {
@@ -174,7 +175,7 @@ __device__ __forceinline__ float min_nan(float a, float b) {  // NaN if either i
 // four: with p = (ac, bd) of the denominators a, b, c, d, 1 / a = bd c / (ac bd) and so on. 2^30 stands for larger
 // exponentials (tanh is then 1 to fp32 precision), which keeps the product of four inside fp32. For small y, e - 1 is
 // exact and the quotient's roundings are relative to it: only the exponential's own error, 2^-23 of cap, remains.
-__device__ __forceinline__ void cap_four(float* v, float scale, float cap, const float (&rest)[4]) {
+__device__ __forceinline__ void cap_four(float* v, float scale, float cap, uint64_t rest0, uint64_t rest1) {
   const uint64_t s2 = f32x2(scale, scale), one = f32x2(1.f, 1.f), less = f32x2(-1.f, -1.f), c2 = f32x2(cap, cap);
   float y[4];
   f32x2_split(mul_f32x2(f32x2(v[0], v[1]), s2), y[0], y[1]);
@@ -189,8 +190,8 @@ __device__ __forceinline__ void cap_four(float* v, float scale, float cap, const
   const uint64_t s = mul_f32x2(f32x2(r, r), f32x2(bd, ac));
   const uint64_t t0 = mul_f32x2(mul_f32x2(s, cd), add_f32x2(e0, less));
   const uint64_t t1 = mul_f32x2(mul_f32x2(s, ab), add_f32x2(e1, less));
-  f32x2_split(fma_f32x2(t0, c2, f32x2(rest[0], rest[1])), v[0], v[1]);
-  f32x2_split(fma_f32x2(t1, c2, f32x2(rest[2], rest[3])), v[2], v[3]);
+  f32x2_split(fma_f32x2(t0, c2, rest0), v[0], v[1]);
+  f32x2_split(fma_f32x2(t1, c2, rest1), v[2], v[3]);
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN operands are passed over
@@ -200,52 +201,54 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN opera
 }
 
 // N scores (columns col0 .. of the tile at key k0) less `ref`, in place.
-// side: every key of the tile lies at or before every position of the warp (-1), at or after them (1), or neither (0).
-template <bool CAP, bool BIAS, int N>
+// LINEAR: all the keys lie on one side of the row's position, and the bias is slope times (key - position).
+template <bool CAP, bool BIAS, int N, bool LINEAR>
 __device__ __forceinline__ void row_scores(float* v, const Score& sc, const Row& row, int k0, int col0, float ref,
-                                           int side) {
+                                           float slope) {
   const float rest = -ref;
-  auto apply = [&](auto bias) {  // bias(i): the bias of column i, plus `rest`
+  auto apply = [&](auto bias) {  // bias(i): the biases of columns i and i + 1, plus `rest`
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-      const float b[4] = {bias(i), bias(i + 1), bias(i + 2), bias(i + 3)};
+      const uint64_t b0 = bias(i), b1 = bias(i + 2);
       if constexpr (CAP) {
-        cap_four(v + i, sc.scale, sc.cap, b);
+        cap_four(v + i, sc.scale, sc.cap, b0, b1);
       } else {
         const uint64_t s2 = f32x2(sc.scale, sc.scale);
-        f32x2_split(fma_f32x2(f32x2(v[i], v[i + 1]), s2, f32x2(b[0], b[1])), v[i], v[i + 1]);
-        f32x2_split(fma_f32x2(f32x2(v[i + 2], v[i + 3]), s2, f32x2(b[2], b[3])), v[i + 2], v[i + 3]);
+        f32x2_split(fma_f32x2(f32x2(v[i], v[i + 1]), s2, b0), v[i], v[i + 1]);
+        f32x2_split(fma_f32x2(f32x2(v[i + 2], v[i + 3]), s2, b1), v[i + 2], v[i + 3]);
       }
     }
   };
   if constexpr (!BIAS) {
-    apply([&](int) { return rest; });
+    apply([&](int) { return f32x2(rest, rest); });
   } else {
     const float e0 = (float)(int)((unsigned)(k0 + col0) - (unsigned)row.pos);  // (exact up to distances of 2^24)
-    if (side != 0) {  // the bias is linear over the tile
-      const float sl = side < 0 ? row.slope : -row.slope;
-      const float base = fmaf(sl, e0, rest);
-      apply([&](int i) { return fmaf(sl, (float)i, base); });
+    if constexpr (LINEAR) {
+      uint64_t near[4];  // within eight columns, which share a base
+#pragma unroll
+      for (int k = 0; k < 4; ++k) near[k] = f32x2(slope * (2.f * k), slope * (2.f * k + 1.f));
+      apply([&](int i) {
+        const float base = fmaf(slope, e0 + (float)(i & ~7), rest);
+        return add_f32x2(f32x2(base, base), near[(i & 7) / 2]);
+      });
     } else {
-      apply([&](int i) { return fmaf(-row.slope, fabsf(e0 + (float)i), rest); });
+      apply([&](int i) {
+        return f32x2(fmaf(-slope, fabsf(e0 + (float)i), rest), fmaf(-slope, fabsf(e0 + (float)(i + 1)), rest));
+      });
     }
   }
 }
 
-// 32 scores outside the row's span, replaced by x; below and above: whether any row of the warp needs that side.
-__device__ __forceinline__ void mask_scores(float* v, const Row& row, int first_key, bool below, bool above, float x) {
-  if (above) {
-    const int end = row.hi - first_key;
+// The keys of [first_key, first_key + 32) that the row sees, a bit each.
+__device__ __forceinline__ uint32_t seen_keys(const Row& row, int first_key) {
+  const int end = min(max(row.hi - first_key, 0), 32), first = min(max(row.lo - first_key, 0), 32);
+  return (uint32_t)((1ull << end) - 1) & ~(uint32_t)((1ull << first) - 1);
+}
+// 32 scores, replaced by x where the row does not see the key (a test of a bit and a move each).
+__device__ __forceinline__ void mask_scores(float* v, uint32_t seen, float x) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i >= end) v[i] = x;
-  }
-  if (below) {
-    const int first = row.lo - first_key;
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < first) v[i] = x;
-  }
+  for (int i = 0; i < 32; ++i)
+    if (!(seen & (1u << i))) v[i] = x;
 }
 
 template <bool F16>
@@ -306,10 +309,11 @@ __device__ __forceinline__ void store32(void* at, const uint32_t (&v)[8], bool a
     static_cast<uint4*>(at)[1] = make_uint4(v[4], v[5], v[6], v[7]);
   }
 }
-__device__ __forceinline__ void store_out32(char* row, int out_kind, int i, const float (&v)[32]) {
+template <bool F16>
+__device__ __forceinline__ void store_out32(char* row, bool f32, int i, const float (&v)[32]) {
   const bool al = (reinterpret_cast<uintptr_t>(row) & 31) == 0;
   uint32_t u[8];
-  if (out_kind == 2) {
+  if (f32) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
 #pragma unroll
@@ -321,8 +325,7 @@ __device__ __forceinline__ void store_out32(char* row, int out_kind, int i, cons
     for (int q = 0; q < 2; ++q) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        u[e] = out_kind == 1 ? pack_f16(v[16 * q + 2 * e], v[16 * q + 2 * e + 1])
-                             : pack_bf16(v[16 * q + 2 * e], v[16 * q + 2 * e + 1]);
+        u[e] = pack16<F16>(v[16 * q + 2 * e], v[16 * q + 2 * e + 1]);
       store32(row + 2 * (i + 16 * q), u, al);
     }
   }
@@ -518,11 +521,12 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
     prefetch_tensormap(&p.map_k);
     prefetch_tensormap(&p.map_v);
   }
-  if (p.shares) allow_dependent_launch();  // the merge may be scheduled; it waits for this grid's end
   tcgen05_before_sync();
   __syncthreads();
   tcgen05_after_sync();
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+  grid_dependency_wait();
+  if (p.shares) allow_dependent_launch();  // (the merge; CTAs of the next grid that wait on freed SMs slow the rest of whole tiles)
   // The description of the item of a round (uniform); false when a wait gave up.
   auto next_item = [&](int round, Item<PAIR>& x) {
     const bool ok = mbar_wait_warp(sm.itemfull(round), (round / kItemRing) & 1, fail);
@@ -974,10 +978,9 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           continue;
         }
         const bool masked = k0 < warp_all_lo || k0 + kTile > warp_all_hi;
-        auto side_of = [&](int key, int n) {
-          return !BIAS ? 0 : key + n - 1 <= pos_min ? -1 : key >= pos_max ? 1 : 0;
-        };
-        const int side = side_of(k0, kTile);
+        // every key of the tile lies at or before every position of the warp, or at or after them
+        const bool before = !BIAS || k0 + kTile - 1 <= pos_min, after = BIAS && k0 >= pos_max;
+        const float slope_to = before ? row.slope : -row.slope;
         // the bias (log2) of the nearest of the keys [key, key + n)
         auto near_bias = [&](int key, int n) {
           if (!BIAS) return 0.f;
@@ -1043,10 +1046,11 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             const int key = k0 + col + q;
             seen[q / 32] = key < warp_hi && key + 32 > warp_lo;
             if (!seen[q / 32]) continue;
-            const bool below = key < warp_all_lo, above = key + 32 > warp_all_hi;
-            if (CAP && (below || above)) mask_scores(v + q, row, key, below, above, 0.f);  // (four share a reciprocal)
-            row_scores<CAP, BIAS, 32>(v + q, sc, row, k0, col + q, base, side_of(key, 32));
-            if (below || above) mask_scores(v + q, row, key, below, above, -INFINITY);
+            const bool cut = key < warp_all_lo || key + 32 > warp_all_hi;
+            const uint32_t keys = seen_keys(row, key);
+            if (CAP && cut) mask_scores(v + q, keys, 0.f);  // (four share a reciprocal)
+            row_scores<CAP, BIAS, 32, false>(v + q, sc, row, k0, col + q, base, row.slope);
+            if (cut) mask_scores(v + q, keys, -INFINITY);
 #pragma unroll
             for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[q + e], v[q + e + 1]);
           }
@@ -1096,7 +1100,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           load(col, v);
           loaded(v);
           const float near = near_bias(k0 + col, 32);
-          row_scores<CAP, BIAS, 32>(v, sc, row, k0, col, near, side_of(k0 + col, 32));
+          row_scores<CAP, BIAS, 32, false>(v, sc, row, k0, col, near, row.slope);
           float mx = -INFINITY, mx2 = -INFINITY;
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
@@ -1107,9 +1111,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           if (ref == -INFINITY && mx > -INFINITY) ref = near + (mx - ref_drop<F16>());
           careful = __any_sync(0xffffffffu, ref == -INFINITY || fabsf(ref) > kRefExact);
         }
-        // Fast path: no mask, a reference in every row. Straight-line code, checked by the sum afterwards; nothing is
-        // stored before the check.
-        bool slow = masked || careful;
+        // Fast path: no mask, a reference in every row, the bias linear. Straight-line code, checked by the sum afterwards;
+        // nothing is stored before the check.
+        const bool bent = !before && !after;
+        bool slow = masked || careful || bent;
         if (guarded && !masked) ok = mark();
         if (!ok) break;
         if constexpr (MODE == kFew) {  // this warp's quarter of the keys
@@ -1121,9 +1126,9 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             float v[32];
             load(col, v);
             loaded(v);
-            slow = careful || k0 + col < warp_all_lo || k0 + col + 32 > warp_all_hi;
+            slow = careful || bent || k0 + col < warp_all_lo || k0 + col + 32 > warp_all_hi;
             if (!slow) {
-              row_scores<CAP, BIAS, 32>(v, sc, row, k0, col, ref, side_of(k0 + col, 32));
+              row_scores<CAP, BIAS, 32, true>(v, sc, row, k0, col, ref, slope_to);
               const float quarter_sum = pack(v, w);
               slow = __any_sync(0xffffffffu, !(quarter_sum <= sum_max<F16>()));
               if (slow) {
@@ -1152,7 +1157,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             load(0, v[0]);
             loaded(v[0]);
             load(64, v[1]);
-            row_scores<CAP, BIAS, 64>(v[0], sc, row, k0, 0, ref, side);
+            row_scores<CAP, BIAS, 64, true>(v[0], sc, row, k0, 0, ref, slope_to);
             const float sum0 = pack(v[0], w[0]);
             slow = __any_sync(0xffffffffu, !(sum0 <= sum_max<F16>()));  // a reference is too low (or a score NaN)
             if (!slow) {
@@ -1160,7 +1165,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               first_half = 1;
               tmem_st32(ts, w[0]);
               loaded(v[1]);
-              row_scores<CAP, BIAS, 64>(v[1], sc, row, k0, 64, ref, side);
+              row_scores<CAP, BIAS, 64, true>(v[1], sc, row, k0, 64, ref, slope_to);
               arrive(0, 1);
               const float sum1 = pack(v[1], w[1]);
               slow = __any_sync(0xffffffffu, !(sum1 <= sum_max<F16>()));
@@ -1182,7 +1187,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               load(64 * half, v);
               loaded(v);
               if (CAP && !slow_half) {
-                row_scores<CAP, BIAS, 64>(v, sc, row, k0, 64 * half, ref, side);
+                row_scores<CAP, BIAS, 64, true>(v, sc, row, k0, 64 * half, ref, slope_to);
                 const float half_sum = pack(v, w);
                 slow_half = __any_sync(0xffffffffu, !(half_sum <= sum_max<F16>()));
                 if (slow_half) {
@@ -1212,7 +1217,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       const bool whole = !p.shares;
       const long long part_at = (long long)x.slot * L::kItemRows + (PAIR ? stream * kTile : 0) + r;
       char* dst = whole ? static_cast<char*>(a.out) +
-                              (x.b * a.o_b + head * a.o_h + token * a.o_t) * (p.out_kind == 2 ? 4 : 2)
+                              (x.b * a.o_b + head * a.o_h + token * a.o_t) * (p.out_f32 ? 4 : 2)
                         : reinterpret_cast<char*>(p.part_o + part_at * kHeadDim);
       const long long stat_at = whole ? x.b * a.s_b + head * a.s_h + token * a.s_t : part_at;
       const int n = x.n, set = x.b, head0 = x.h * a.G, slot = x.slot;
@@ -1279,9 +1284,9 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         const size_t orow_out = ((size_t)set * a.tq + otoken) * a.heads_q + ohead;
         const Joined jo = join(orow, othere, orow_out);
         char* odst = whole ? static_cast<char*>(a.out) +
-                                 (set * a.o_b + ohead * a.o_h + otoken * a.o_t) * (p.out_kind == 2 ? 4 : 2)
+                                 (set * a.o_b + ohead * a.o_h + otoken * a.o_t) * (p.out_f32 ? 4 : 2)
                            : reinterpret_cast<char*>(p.part_o + ((size_t)slot * L::kItemRows + orow) * kHeadDim);
-        const int kind = whole ? p.out_kind : 2;
+        const bool f32 = !whole || p.out_f32;
 #pragma unroll 1
         for (int q = 0; q < 8; ++q) {
           float v[16];
@@ -1309,10 +1314,10 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               y0 = fmaf(o.x, jo.f1, y0);
               y1 = fmaf(o.y, jo.f1, y1);
             }
-            if (kind == 2)
+            if (f32)
               reinterpret_cast<float2*>(odst)[ch / 2] = make_float2(y0, y1);
             else
-              reinterpret_cast<uint32_t*>(odst)[ch / 2] = kind == 1 ? pack_f16(y0, y1) : pack_bf16(y0, y1);
+              reinterpret_cast<uint32_t*>(odst)[ch / 2] = pack16<F16>(y0, y1);
           }
           softmax_sync(false);
         }
@@ -1331,7 +1336,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       const uint32_t o0 = PAIR ? to : tmem + 256 + lanes;
       const bool has0 = PAIR ? it > 0 : n > 0, has1 = !PAIR && n > 1;
       const float* own = a.own_out + out_row * kHeadDim;
-#pragma unroll
+#pragma unroll 1
       for (int q = 0; q < (PAIR ? 4 : 2); ++q) {
         const int ch = 32 * (PAIR ? q : 2 * stream + q);
         float v[32];
@@ -1359,7 +1364,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               v[e + 3] = fmaf(o.w, f1, v[e + 3]);
             }
           }
-          store_out32(dst, whole ? p.out_kind : 2, ch, v);
+          store_out32<F16>(dst, !whole || p.out_f32, ch, v);
         }
       }
       if (valid && (PAIR || stream == 0)) {
@@ -1400,8 +1405,7 @@ cudaError_t launch_variant(const FlashKernelArgs& p, int grid, cudaStream_t st) 
     if (e != cudaSuccess) return e;
     done.fetch_or(bit, std::memory_order_relaxed);
   }
-  k<<<grid, kThreads, Layout<MODE>::kSmem, st>>>(p);
-  return cudaGetLastError();
+  return launch_chained(k, dim3(grid), dim3(kThreads), Layout<MODE>::kSmem, st, p);
 }
 
 }  // namespace flash

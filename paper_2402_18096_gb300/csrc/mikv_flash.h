@@ -63,7 +63,7 @@ struct FlashKernelArgs {
   int log2_G;
   // an item's number taken apart: by group, by rank within a full or the last group, and a head into its set
   FastDiv by_group, by_rank, by_last, by_head;
-  int out_kind;         // 0 bf16, 1 fp16, 2 fp32
+  int out_f32;          // the output is fp32; else of the keys' type
   // Shares: the key tiles of all row tiles, end to end, in equal runs for the CTAs.
   int shares;           // 0: whole row tiles
   int by_length;        // units of a row tile: the tiles of its set's length (lens), else `units`
