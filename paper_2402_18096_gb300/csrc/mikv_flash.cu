@@ -221,6 +221,7 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
     p.units = (int)(((long long)a.tk + kTile - 1) / kTile);
     p.share_each = (int)((long long)base * p.units / p.shares);
     p.share_extra = (int)((long long)base * p.units % p.shares);
+    p.inv_units = 1.f / (float)p.units;
     p.by_units.set(p.units);
     p.by_set.set(a.heads_kv * plan.m_blocks);
     p.by_block.set(plan.m_blocks);

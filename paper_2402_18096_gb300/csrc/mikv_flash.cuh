@@ -556,28 +556,13 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         if (!ok || !x.valid) break;
         if (x.n == 0) continue;
         if (lane == 0) {
-          auto load = [&](const CUtensorMap* map, int j, int hm, int bm) {
-            const int s = c % L::kStages;
-            if (c >= L::kStages && !mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail)) return false;
-            mbar_arrive_expect_tx(sm.full(s), kTileBytes);
-            tma_load_4d(sm.stage(s), map, 0, j * kTile, x.h * hm, x.b * bm, sm.full(s));
-            tma_load_4d(sm.stage(s) + kHalfBytes, map, 64, j * kTile, x.h * hm, x.b * bm, sm.full(s));
-#pragma unroll
-            for (int q = 0; q < L::kStages; ++q)
-              if (q == s) last[q] = c;
-            ++c;
-            return true;
-          };
-          auto load_k = [&](int j) { return load(&p.map_k, j, p.k_head, p.k_batch); };
-          auto load_v = [&](int j) { return load(&p.map_v, j, p.v_head, p.v_batch); };
-          for (int u = 0; ok && u < min(x.n, L::kLead); ++u) ok = load_k(x.T1 - 1 - u);
-          if (ok && running > 0) ok = mbar_wait_role(sm.qfree(), (running - 1) & 1, fail);
-          if (ok) {
+          auto load_q = [&]() {
+            if (running > 0 && !mbar_wait_role(sm.qfree(), (running - 1) & 1, fail)) return false;
             mbar_arrive_expect_tx(sm.qfull(), L::kQ * kTileBytes);
 #pragma unroll
             for (int m = 0; m < L::kQ; ++m) {
               const int tok0 = (PAIR ? 2 * x.m_block + m : x.m_block) * (kTile / a.G);
-#pragma unroll
+#pragma unroll 1
               for (int copy = 0; copy < L::kCopies; ++copy) {
                 const uint32_t to = sm.q(m) + copy * L::kRows * 128;
                 tma_load_4d(to, &p.map_q, 0, x.h * a.G, tok0, x.b, sm.qfull());
@@ -585,9 +570,28 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
               }
             }
             ++running;
+            return true;
+          };
+          // V tile u, then K tile u + kLead; the first kLead K tiles and the queries before them
+#pragma unroll 1
+          for (int i = -2 * L::kLead; ok && i < 2 * x.n; ++i) {
+            const int u = i >> 1;
+            const bool keys = i & 1;
+            if (i == 0) ok = load_q();
+            if (keys ? u + L::kLead >= x.n : u < 0) continue;
+            const int s = c % L::kStages, j = (x.T1 - 1 - u - (keys ? L::kLead : 0)) * kTile;
+            const CUtensorMap* map = keys ? &p.map_k : &p.map_v;
+            const int h = x.h * (keys ? p.k_head : p.v_head), b = x.b * (keys ? p.k_batch : p.v_batch);
+            ok = ok && (c < L::kStages || mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail));
+            if (!ok) break;
+            mbar_arrive_expect_tx(sm.full(s), kTileBytes);
+            tma_load_4d(sm.stage(s), map, 0, j, h, b, sm.full(s));
+            tma_load_4d(sm.stage(s) + kHalfBytes, map, 64, j, h, b, sm.full(s));
+#pragma unroll
+            for (int q = 0; q < L::kStages; ++q)
+              if (q == s) last[q] = c;
+            ++c;
           }
-          for (int u = 0; ok && u < x.n; ++u)
-            ok = load_v(x.T1 - 1 - u) && (u + L::kLead >= x.n || load_k(x.T1 - 1 - u - L::kLead));
         }
         ok = __shfl_sync(0xffffffffu, ok, 0);
       }
@@ -630,12 +634,12 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             umma_commit(sm.odone(w, half));
           }
         }
-        tiles[w ? 1 : 0] += 1;
+        (w ? tiles[1] : tiles[0]) += 1;
         return true;
       };
       auto wait_safe = [&](int w) {
         const int g = of(checked, w);
-        checked[w ? 1 : 0] += 1;
+        (w ? checked[1] : checked[0]) += 1;
         return mbar_wait_warp(sm.vsafe(w, g), (g / kSafeRing) & 1, fail);
       };
       bool ok = true;
@@ -647,8 +651,8 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         if (n == 0) continue;
         ok = mbar_wait_warp(sm.qfull(), running & 1, fail);
         ++running;
-        bool fresh[2] = {true, true};  // the stream's O holds nothing of this item yet
         if constexpr (PAIR) {
+          bool fresh[2] = {true, true};  // the stream's O holds nothing of this item yet
           ok = ok && wait_full(c);
           if (ok) {
 #pragma unroll
@@ -678,38 +682,24 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             }
             c += 2;
           }
-        } else {
-#pragma unroll
-          for (int w = 0; w < 2; ++w)
-            if (ok && w < n) {
+        } else {  // step u: the product of tile u (from 0 on), then the scores of tile u + 2; streams in turn
+#pragma unroll 1
+          for (int u = -2; ok && u < n; ++u) {
+            const int w = u & 1;
+            if (u >= 0) {
+              ok = wait_full(c) && (!x.guarded(x.T1 - 1 - u) || wait_safe(w)) && values(w, c, u < 2);
+              if (ok) {
+                release(c);
+                ++c;
+              }
+            }
+            if (ok && u + 2 < n) {
               ok = wait_full(c);
               if (ok) {
                 scores(w, c);
                 release(c);
-                if (w + 1 == n) commit(sm.qfree());
                 ++c;
-              }
-            }
-          for (int i = 0; ok && 2 * i < n; ++i) {
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const int u = 2 * i + w;
-              if (ok && u < n) {
-                ok = wait_full(c) && (!x.guarded(x.T1 - 1 - u) || wait_safe(w)) && values(w, c, fresh[w]);
-                fresh[w] = false;
-                if (ok) {
-                  release(c);
-                  ++c;
-                }
-                if (ok && u + 2 < n) {
-                  ok = wait_full(c);
-                  if (ok) {
-                    scores(w, c);
-                    release(c);
-                    ++c;
-                  }
-                }
-                if (ok && u + 3 == n) commit(sm.qfree());  // (the last scores were those of tile n - 1)
+                if (u + 3 == n) commit(sm.qfree());
               }
             }
           }
@@ -771,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
           }
         }
       }
-    } else {  // the coming items, up to kItemRing ahead, and the end
+    } else {  // the coming items, up to kItemRing ahead, and the end (little code: every launch fetches it anew)
       int round = 0;
       auto publish = [&](const ItemData& x) {
         if (round >= kItemRing && !mbar_wait_warp(sm.itemfree(round), ((round / kItemRing) & 1) ^ 1, fail)) return false;
@@ -783,77 +773,80 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
         ++round;
         return true;
       };
-      bool ok = true;
-      if (!p.shares) {
-        for (int index = item_index(0); ok && index < p.n_items; index = item_index(round)) {
-          ItemData x = place_at(p, index);
-          item_tiles<MODE>(p, x, lane);
-          ok = publish(x);
-        }
-        if (ok) publish(ItemData{});
-      } else {
-        const int c = blockIdx.x, per_set = a.heads_kv * p.m_blocks;
-        Shares sh = {p.share_each, p.share_extra};
-        // the first row block of this share: set b, number `in_set` in it, first unit `start`
-        int b = 0, in_set = 0, start = 0, lo, hi;
-        if (!p.by_length) {
-          lo = sh.first(c), hi = sh.first(c + 1);
-          const int m = p.by_units.div(lo);
-          b = p.by_set.div(m);
-          in_set = m - b * per_set;
-          start = m * p.units;
-        } else {
-          auto scan = [&](int b0, int& mine) {  // units of the sets b0 .. b0 + lane, and of this lane's
-            mine = b0 + lane < a.batch ? units_of(p, b0 + lane) * per_set : 0;
-            int sum = mine;
+      // Shares: this CTA's units [lo, hi); the row block that holds the next unit `u`: set b, number `in_set` in it, first
+      // unit `start`.
+      const int per_set = a.heads_kv * p.m_blocks;
+      Shares sh = {p.share_each, p.share_extra};
+      int b = 0, in_set = 0, start = 0, u = 0, hi = 0;
+      if (p.shares && !p.by_length) {
+        u = sh.first(blockIdx.x), hi = sh.first(blockIdx.x + 1);
+        const int m = p.by_units.div(u);
+        b = p.by_set.div(m);
+        in_set = m - b * per_set;
+        start = m * p.units;
+      } else if (p.shares) {
+        auto scan = [&](int b0, int& mine) {  // units of the sets b0 .. b0 + lane, and of this lane's
+          mine = b0 + lane < a.batch ? units_of(p, b0 + lane) * per_set : 0;
+          int sum = mine;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-              const int y = __shfl_up_sync(0xffffffffu, sum, o);
-              if (lane >= o) sum += y;
-            }
-            return sum;
-          };
-          int mine, sum = scan(0, mine), all = __shfl_sync(0xffffffffu, sum, 31);
-          for (int b0 = 32; b0 < a.batch; b0 += 32) {
-            int other;
-            all += __shfl_sync(0xffffffffu, scan(b0, other), 31);
+          for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += y;
           }
-          sh.each = all / (int)gridDim.x;
-          sh.extra = all - sh.each * gridDim.x;
-          lo = sh.first(c), hi = sh.first(c + 1);
-          int before = 0;
-          for (int b0 = 0; lo < hi && b0 < a.batch; b0 += 32) {
-            if (b0 > 0) sum = scan(b0, mine);
-            const int total = __shfl_sync(0xffffffffu, sum, 31);
-            if (lo < before + total) {
-              const int at = __ffs(__ballot_sync(0xffffffffu, before + sum > lo)) - 1;
-              b = b0 + at;
-              start = before + __shfl_sync(0xffffffffu, sum - mine, at);
-              const int t = __shfl_sync(0xffffffffu, mine, at) / per_set;
-              in_set = (lo - start) / t;
-              start += in_set * t;
-              break;
-            }
-            before += total;
+          return sum;
+        };
+        int all = 0, mine, sum;
+#pragma unroll 1
+        for (int b0 = 0; b0 < a.batch; b0 += 32) all += __shfl_sync(0xffffffffu, scan(b0, mine), 31);
+        sh.each = all / (int)gridDim.x;
+        sh.extra = all - sh.each * gridDim.x;
+        u = sh.first(blockIdx.x), hi = sh.first(blockIdx.x + 1);
+        int before = 0;
+#pragma unroll 1
+        for (int b0 = 0; u < hi && b0 < a.batch; b0 += 32) {
+          sum = scan(b0, mine);
+          const int total = __shfl_sync(0xffffffffu, sum, 31);
+          if (u < before + total) {
+            const int at = __ffs(__ballot_sync(0xffffffffu, before + sum > u)) - 1;
+            b = b0 + at;
+            start = before + __shfl_sync(0xffffffffu, sum - mine, at);
+            const int t = units_of(p, b);
+            in_set = (u - start) / t;
+            start += in_set * t;
+            break;
           }
+          before += total;
         }
-        for (int u = lo; ok && u < hi;) {
-          const int t = units_of(p, b), from = u - start, end = min(hi - start, t);
-          ItemData x = {};
+      }
+      bool ok = true;
+#pragma unroll 1
+      while (ok) {
+        ItemData x = {};
+        int t = 0;  // units of the row block
+        if (!p.shares) {
+          const int index = item_index(round);
+          if (index >= p.n_items) break;
+          x = place_at(p, index);
+        } else {
+          if (u >= hi) break;
+          t = units_of(p, b);
           x.b = b;
           x.h = p.by_block.div(in_set);
           x.m_block = in_set - x.h * p.m_blocks;
-          x.slot = c + b * per_set + in_set;
-          item_tiles<MODE>(p, x, lane);
-          const int n = x.T1 - x.T0;
-          if (!p.by_length) {
-            x.T1 = x.T0 + (int)((long long)n * end / t);
-            x.T0 += (int)((long long)n * from / t);
+          x.slot = blockIdx.x + b * per_set + in_set;
+        }
+        item_tiles<MODE>(p, x, lane);
+        if (p.shares) {
+          const int from = u - start, end = min(hi - start, t);
+          if (!p.by_length) {  // units to tiles: a rising function, the same for the part before and the one behind
+            const int n = x.T1 - x.T0;
+            auto tile = [&](int unit) { return unit == t ? n : min(n, (int)((float)n * (float)unit * p.inv_units)); };
+            x.T1 = x.T0 + tile(end);
+            x.T0 += tile(from);
           } else {
             x.T1 = x.T0 + end;
             x.T0 += from;
           }
-          ok = publish(x);
           u = start + end;
           if (end == t) {  // on to the next row block that has units
             start += t;
@@ -864,17 +857,20 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
             }
           }
         }
-        if (ok) publish(ItemData{});
-        if (c == 0) {  // for the merge: the first CTA of each row block, and how many share it
-          int unit = 0;
-          for (int set = 0; set < a.batch; ++set) {
-            const int t = units_of(p, set);
-            for (int i = lane; i < per_set; i += 32) {
-              const int u0 = unit + i * t, first = t > 0 ? sh.owner(u0) : 0;
-              p.part_table[set * per_set + i] = make_int2(first, t > 0 ? sh.owner(u0 + t - 1) - first + 1 : 0);
-            }
-            unit += per_set * t;
+        ok = publish(x);
+      }
+      if (ok) publish(ItemData{});
+      if (p.shares && blockIdx.x == 0) {  // for the merge: the first CTA of each row block, and how many share it
+        int unit = 0;
+#pragma unroll 1
+        for (int set = 0; set < a.batch; ++set) {
+          const int t = units_of(p, set);
+#pragma unroll 1
+          for (int i = lane; i < per_set; i += 32) {
+            const int u0 = unit + i * t, first = t > 0 ? sh.owner(u0) : 0;
+            p.part_table[set * per_set + i] = make_int2(first, t > 0 ? sh.owner(u0 + t - 1) - first + 1 : 0);
           }
+          unit += per_set * t;
         }
       }
     }

@@ -69,6 +69,7 @@ struct FlashKernelArgs {
   int by_length;        // units of a row tile: the tiles of its set's length (lens), else `units`
   int units;
   int share_each, share_extra;         // (not by_length) units of a CTA, and how many CTAs have one more
+  float inv_units;                     // 1 / units
   FastDiv by_units, by_set, by_block;  // a unit into its row tile, a row tile into its set, and into its head
   int2* part_table;     // [batch * heads_kv * m_blocks]: first CTA of a row tile, and the number of its parts
   float* part_o;        // [slots][rows of an item][128] normalised outputs, slot = CTA + row tile
