@@ -48,8 +48,12 @@
 // and about 2900 in the kernel: what is left is the chain of one stream (scores -> softmax, about 1200 clocks -> product
 // and next scores, 1034, and two hand-overs), which two streams in 512 TMEM columns cannot hide altogether. Causal, T 8192,
 // 32 query and 8 KV heads: 345 us, 1.59 PFLOP/s. A cap adds an exponential and a quarter of a reciprocal per score
-// (1.00 PFLOP/s at the same size), a distance bias two fp32 operations (1.30). With one row tile a set's keys pass once:
+// (1.00 PFLOP/s at the same size), a distance bias an addition (1.47). With one row tile a set's keys pass once:
 // HBM. 8 requests of 32 heads with 4096 keys of their own: 87 us, 6.2 TB/s (91 % of a copy).
+//
+// Code that runs once per item or launch is bound by fetching its instructions (traces: 2 us from the start of a CTA to its
+// first item, 2.5 us for the output of one), so such code is kept in loops, and each path has one form: a kernel of 131 KB
+// of code took 88 us where its 88 KB form took 84 (four prompts of other lengths, 16 requests, cap and bias).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -77,7 +81,7 @@ constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kHalfBytes = kTileBytes / 2;     // one 64-channel box
 constexpr int kSoftThreads = 256;
 constexpr int kCopyWarp = 8, kMmaWarp = 9, kGuardWarp = 10;  // 11: the items'
-constexpr int kExPitch = 20;                   // floats of a row's 16 channels in the exchange (padded against conflicts)
+constexpr int kExPitch = 68;                   // floats of a row's 64 channels in the exchange (padded against conflicts)
 constexpr int kItemRing = 4;                   // items described ahead
 constexpr int kItemReaders = 11;               // warps that read an item's description: all but the one that writes it
 constexpr int kThreads = 384;
@@ -96,7 +100,7 @@ struct Layout {
   static constexpr int kCopies = MODE == kFew ? 4 : 1;   // of the rows in a tile
   static constexpr int kRows = kTile / kCopies;          // rows of a tile
   static constexpr int kItemRows = (PAIR ? 2 : 1) * kRows;  // rows of an item
-  static constexpr int kExchange = MODE == kFew ? 8 * 32 * kExPitch * 4 : 0;  // for joining the copies
+  static constexpr int kExchange = MODE == kFew ? 8 * 8 * kExPitch * 4 : 0;  // for joining the copies
   static constexpr int kQ = PAIR ? 2 : 1;  // query tiles in shared memory
   static constexpr int kStages = 5;        // K / V tiles in the ring
   // Loads of an item: the first kLead K tiles, then V tile u and K tile u + kLead for u = 0, 1, ... (from the last
@@ -1271,57 +1275,64 @@ __global__ void __launch_bounds__(kThreads, 1) flash_kernel(const __grid_constan
       const float f1 = jn.f1;
       auto part_factor = [&](int i) { return jn.f0 * (jn.top == -INFINITY ? 0.f : fast_exp2(s_part[i][0][r] - jn.top)); };
       if constexpr (MODE == kFew) {
-        // 16 channels at a time: every part scaled into shared memory, then summed (thread: two channels of a row)
+        // 8 rows and 64 channels at a time: every part scaled into shared memory, then summed (thread: two channels of the
+        // row `warp` of the eight). Few rows, few rounds: one decoded token's take two.
         float* ex = reinterpret_cast<float*>(smem_raw + (sm.exchange() - smem_u32(smem_raw)));
         const float g = blank || it == 0 ? 0.f : part_factor(part);
-        const int orow = tid >> 3, oc = 2 * (tid & 7);
-        const int otoken = orow >> p.log2_G, ohead = head0 + (orow & (a.G - 1));
-        const bool othere = otoken < a.tq;
-        const size_t orow_out = ((size_t)set * a.tq + otoken) * a.heads_q + ohead;
-        const Joined jo = join(orow, othere, orow_out);
-        char* odst = whole ? static_cast<char*>(a.out) +
-                                 (set * a.o_b + ohead * a.o_h + otoken * a.o_t) * (p.out_f32 ? 4 : 2)
-                           : reinterpret_cast<char*>(p.part_o + ((size_t)slot * L::kItemRows + orow) * kHeadDim);
         const bool f32 = !whole || p.out_f32;
 #pragma unroll 1
-        for (int q = 0; q < 8; ++q) {
-          float v[16];
-          if (it > 0) {
-            tmem_ld16(to + 16 * q, v);
-            tmem_wait_ld16(v);
+        for (int row0 = 0; row0 < a.tq * a.G; row0 += 8) {
+          const int orow = row0 + warp, otoken = orow >> p.log2_G, ohead = head0 + (orow & (a.G - 1));
+          const bool othere = otoken < a.tq;
+          const size_t orow_out = ((size_t)set * a.tq + otoken) * a.heads_q + ohead;
+          const Joined jo = join(orow, othere, orow_out);
+          char* odst = whole ? static_cast<char*>(a.out) +
+                                   (set * a.o_b + ohead * a.o_h + otoken * a.o_t) * (p.out_f32 ? 4 : 2)
+                             : reinterpret_cast<char*>(p.part_o + ((size_t)slot * L::kItemRows + orow) * kHeadDim);
+#pragma unroll 1
+          for (int ch0 = 0; ch0 < kHeadDim; ch0 += 64) {
+            float v[64];
+            if (it > 0) {
+              tmem_ld32(to + ch0, v);
+              tmem_ld32(to + ch0 + 32, v + 32);
+              tmem_wait_ld(v);
+              reg_fence(v + 32);
+            }
+            if ((lane & 24) == row0) {
+              float4* mine = reinterpret_cast<float4*>(ex + (part * 8 + (lane & 7)) * kExPitch);
+#pragma unroll
+              for (int e = 0; e < 64; e += 4)
+                mine[e / 4] = g != 0.f ? make_float4(v[e] * g, v[e + 1] * g, v[e + 2] * g, v[e + 3] * g)
+                                       : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            softmax_sync(false);
+            if (othere) {
+              float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float2 z = *reinterpret_cast<const float2*>(ex + (i * 8 + warp) * kExPitch + 2 * lane);
+                y0 += z.x;
+                y1 += z.y;
+              }
+              const int ch = ch0 + 2 * lane;
+              if (jo.f1 != 0.f) {
+                const float2 o = *reinterpret_cast<const float2*>(a.own_out + orow_out * kHeadDim + ch);
+                y0 = fmaf(o.x, jo.f1, y0);
+                y1 = fmaf(o.y, jo.f1, y1);
+              }
+              if (f32)
+                reinterpret_cast<float2*>(odst)[ch / 2] = make_float2(y0, y1);
+              else
+                reinterpret_cast<uint32_t*>(odst)[ch / 2] = pack16<F16>(y0, y1);
+            }
+            softmax_sync(false);
           }
-          float4* mine = reinterpret_cast<float4*>(ex + (part * 32 + lane) * kExPitch);
-#pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            mine[e / 4] = g != 0.f ? make_float4(v[e] * g, v[e + 1] * g, v[e + 2] * g, v[e + 3] * g)
-                                   : make_float4(0.f, 0.f, 0.f, 0.f);
-          softmax_sync(false);
-          if (othere) {
-            float y0 = 0.f, y1 = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float2 z = *reinterpret_cast<const float2*>(ex + (i * 32 + orow) * kExPitch + oc);
-              y0 += z.x;
-              y1 += z.y;
-            }
-            const int ch = 16 * q + oc;
-            if (jo.f1 != 0.f) {
-              const float2 o = *reinterpret_cast<const float2*>(a.own_out + orow_out * kHeadDim + ch);
-              y0 = fmaf(o.x, jo.f1, y0);
-              y1 = fmaf(o.y, jo.f1, y1);
-            }
-            if (f32)
-              reinterpret_cast<float2*>(odst)[ch / 2] = make_float2(y0, y1);
+          if (othere && lane == 0) {
+            if (whole)
+              store_stat(a, set * a.s_b + ohead * a.s_h + otoken * a.s_t, jo.lse2);
             else
-              reinterpret_cast<uint32_t*>(odst)[ch / 2] = pack16<F16>(y0, y1);
+              p.part_lse[(size_t)slot * L::kItemRows + orow] = jo.lse2;
           }
-          softmax_sync(false);
-        }
-        if (othere && oc == 0) {
-          if (whole)
-            store_stat(a, set * a.s_b + ohead * a.s_h + otoken * a.s_t, jo.lse2);
-          else
-            p.part_lse[(size_t)slot * L::kItemRows + orow] = jo.lse2;
         }
         tcgen05_before_sync();
         if (softmax_sync(*fail)) break;
