@@ -49,7 +49,7 @@
 // and next scores, 1034, and two hand-overs), which two streams in 512 TMEM columns cannot hide altogether. Causal, T 8192,
 // 32 query and 8 KV heads: 345 us, 1.59 PFLOP/s. A cap adds an exponential and a quarter of a reciprocal per score
 // (1.00 PFLOP/s at the same size), a distance bias an addition (1.47). With one row tile a set's keys pass once:
-// HBM. 8 requests of 32 heads with 4096 keys of their own: 87 us, 6.2 TB/s (91 % of a copy).
+// HBM. 8 requests of 32 heads with 4096 keys of their own: 86 us, 6.3 TB/s (92 % of a copy).
 //
 // Code that runs once per item or launch is bound by fetching its instructions (traces: 2 us from the start of a CTA to its
 // first item, 2.5 us for the output of one), so such code is kept in loops, and each path has one form: a kernel of 131 KB
