@@ -18,7 +18,7 @@ import math
 import torch
 
 from . import (LayerCache, RotaryTable, Shape, WS_ATTENTION, WS_BALANCER, WS_PREFILL, WS_STEP, mikv_compute_balancer,
-               mikv_decode_attention, mikv_decode_step, mikv_gather_hi, mikv_insert_token, mikv_mask_spans,
+               mikv_decode_attention, mikv_decode_step, mikv_gather_hi, mikv_insert_token,
                mikv_prefill_scores, mikv_prefix_attention, mikv_prefix_workspace_bytes, mikv_prompt_attention,
                mikv_prompt_workspace_bytes, mikv_quantize_pack, mikv_rotary, mikv_select_demote,
                mikv_update_importance, mikv_workspace_bytes)
@@ -111,9 +111,13 @@ class SharedPrefixLayer:
     def from_prompts(cls, shape: Shape, table: RotaryTable, prefix, own, out_prefix, out_own, key_len=None):
         """The prompts of a batch: prefix = (q, k, v) of the shared tokens ([1, H, P, d], bf16), own = (q, k, v) of each
         request's own tokens ([B, H, T, d]). Turns q and k (in place), attends the prefix (into out_prefix) and the
-        own tokens over prefix and own keys (into out_own; key_len int32 [B]: keys of each request, P + its own
-        tokens, the rest being padding), and builds the own cache by accumulated attention. shape is the own cache's
-        (shape_for_context with context = T)."""
+        own tokens over prefix and own keys (into out_own), and builds the own cache by accumulated attention. shape is
+        the own cache's (shape_for_context with context = T).
+        Every request has all T own tokens: key_len is refused. The cache holds the same number of slots and rows for
+        every request and its attention weighs all of them, so the padding of a shorter one would be kept, attended and
+        counted, and its next token would stand at a wrong position. Requests of other lengths go into other layers."""
+        if key_len is not None:
+            raise ValueError("SharedPrefixLayer: key_len (own tokens of several lengths) is not supported by the own cache")
         q0, k0, v0 = prefix
         q, k, v = own
         B, Hkv, T, d = k.shape
@@ -124,12 +128,8 @@ class SharedPrefixLayer:
         mikv_prompt_attention(q0, k0, v0, out_prefix, ws)
         keys = torch.cat([k0.expand(B, Hkv, P, d), k], dim=2)
         values = torch.cat([v0.expand(B, Hkv, P, d), v], dim=2)
-        spans = None
-        if key_len is not None:
-            spans = torch.empty(B, T, 2, dtype=torch.int32, device=k.device)
-            mikv_mask_spans(spans, P + T, key_len=key_len)
         ws = workspace(mikv_prompt_workspace_bytes(q, keys), k.device)
-        mikv_prompt_attention(q, keys, values, out_own, ws, spans=spans)
+        mikv_prompt_attention(q, keys, values, out_own, ws)
         layer = MixedPrecisionLayer.from_prefill(shape, k.contiguous(), v.contiguous(), None, q.contiguous(),
                                                  device=k.device)
         return cls(layer, k0.contiguous(), v0.contiguous(), table)
