@@ -181,6 +181,19 @@ mikv_status mikv_prefill_scores(const mikv_shape* shape, const void* q_pre, cons
                                 float sm_scale, float* scores, void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * The same sums where the queries attend to more than these keys (a prefix that requests share stands before them): the
+ * weights are those of the whole softmax, whose log-sum-exp per query is given (mikv_prompt_attention's lse,
+ * mikv_prefix_attention's ml):
+ *   scores[b][h][t] = sum over the G query heads j of KV head h and the queries i >= t of exp(s_it - lse[b][hG+j][i])
+ * A query whose lse is infinite weighs nothing. One tensor-core pass.
+ *   lse        fp32 [B][Hq][T]
+ *   the others as in mikv_prefill_scores
+ */
+mikv_status mikv_prefill_scores_lse(const mikv_shape* shape, const void* q_pre, const void* k_pre, int32_t T,
+                                    float sm_scale, const float* lse, float* scores, void* workspace, size_t ws_bytes,
+                                    void* stream);
+
+/*
  * Single-token decode attention over the mixed-precision cache (Eq. 3-4; Sec. 3.4):
  *   s_i = sm_scale * q . k_hi[i]                  for the hi_cap important slots (bf16 keys)
  *   s_t = sm_scale * (q / balancer) . k_hat[t]    for retained rows t < n_lo, k_hat = alpha*code+beta

@@ -120,6 +120,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
                 "mikv_debug_enabled": (I, []),
                 "mikv_debug_check": (I, [P]),
                 "mikv_prefill_scores": (I, [SP, P, P, I, F, P, P, Z, P]),
+                "mikv_prefill_scores_lse": (I, [SP, P, P, I, F, P, P, P, Z, P]),
                 "mikv_cache_fraction": (ctypes.c_double, [I, I, ctypes.c_double, I]),
                 "mikv_retained_row_bytes": (Z, [I, I, I]),
                 "mikv_rotary_phases": (I, [P, I, P]),
@@ -345,11 +346,19 @@ def mikv_decode_step(cache: LayerCache, n_lo: int, q, k_new, v_new, tok: int, sl
         _ptr(slots), float(sm_scale), _ptr(out), out_dtype, _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
-def mikv_prefill_scores(shape: Shape, q_pre, k_pre, scores, workspace, sm_scale: float = None, stream=None):
+def mikv_prefill_scores(shape: Shape, q_pre, k_pre, scores, workspace, sm_scale: float = None, stream=None, lse=None):
     """Initial importance of the prefill tokens into scores [B, Hkv, T] (fp32) from q_pre [B, Hq, T, d] and
-    k_pre [B, Hkv, T, d] (bf16); workspace of mikv_workspace_bytes(shape, WS_PREFILL, T) bytes."""
+    k_pre [B, Hkv, T, d] (bf16); workspace of mikv_workspace_bytes(shape, WS_PREFILL, T) bytes. Queries that attend to
+    more than these keys give the log of their whole sums as lse float32 [B, Hq, T] (mikv_prefill_scores_lse)."""
     T = k_pre.shape[2]
     scale = 1.0 / math.sqrt(shape.head_dim) if sm_scale is None else sm_scale
+    if lse is not None:
+        if lse.shape != q_pre.shape[:3] or lse.dtype != torch.float32:
+            raise ValueError(f"lse: expected float32 {tuple(q_pre.shape[:3])}, got {lse.dtype} {tuple(lse.shape)}")
+        _check("mikv_prefill_scores_lse", load().mikv_prefill_scores_lse(
+            ctypes.byref(shape.c()), _ptr(q_pre), _ptr(k_pre), T, float(scale), _ptr(lse), _ptr(scores),
+            _ptr(workspace), workspace.numel(), _stream(stream)))
+        return
     _check("mikv_prefill_scores", load().mikv_prefill_scores(
         ctypes.byref(shape.c()), _ptr(q_pre), _ptr(k_pre), T, float(scale), _ptr(scores), _ptr(workspace),
         workspace.numel(), _stream(stream)))

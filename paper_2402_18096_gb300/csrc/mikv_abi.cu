@@ -371,9 +371,13 @@ mikv_status mikv_quantize_pack(const mikv_shape* shape, const mikv_cache* cache,
                                           static_cast<cudaStream_t>(stream)));
 }
 
-mikv_status mikv_prefill_scores(const mikv_shape* shape, const void* q_pre, const void* k_pre, int32_t T,
-                                float sm_scale, float* scores, void* workspace, size_t ws_bytes, void* stream) {
-  MIKV_CALL_RANGE();
+}  // extern "C"
+
+namespace {
+
+// Both forms: lse nullptr takes the normalisers from the rows themselves.
+mikv_status prefill_scores(const mikv_shape* shape, const void* q_pre, const void* k_pre, int32_t T, float sm_scale,
+                           const float* lse, float* scores, void* workspace, size_t ws_bytes, void* stream) {
   mikv_status st = shape_supported(shape);
   if (st != MIKV_OK) return st;
   if (!q_pre || !k_pre || !scores || T <= 0) return MIKV_ERR_ARG;
@@ -405,7 +409,25 @@ mikv_status mikv_prefill_scores(const mikv_shape* shape, const void* q_pre, cons
   a.T = T;
   a.T_pad = prefill_padded(T);
   a.scale_log2 = sm_scale * 1.4426950408889634f;
-  return cuda_status(launch_prefill(a, shape->batch, static_cast<cudaStream_t>(stream)));
+  return cuda_status(launch_prefill(a, shape->batch, lse, static_cast<cudaStream_t>(stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+mikv_status mikv_prefill_scores(const mikv_shape* shape, const void* q_pre, const void* k_pre, int32_t T,
+                                float sm_scale, float* scores, void* workspace, size_t ws_bytes, void* stream) {
+  MIKV_CALL_RANGE();
+  return prefill_scores(shape, q_pre, k_pre, T, sm_scale, nullptr, scores, workspace, ws_bytes, stream);
+}
+
+mikv_status mikv_prefill_scores_lse(const mikv_shape* shape, const void* q_pre, const void* k_pre, int32_t T,
+                                    float sm_scale, const float* lse, float* scores, void* workspace, size_t ws_bytes,
+                                    void* stream) {
+  MIKV_CALL_RANGE();
+  if (!lse || !aligned(lse, 4)) return MIKV_ERR_ARG;
+  return prefill_scores(shape, q_pre, k_pre, T, sm_scale, lse, scores, workspace, ws_bytes, stream);
 }
 
 mikv_status mikv_decode_attention(const mikv_shape* shape, const mikv_cache* cache, int32_t n_lo, const void* q,

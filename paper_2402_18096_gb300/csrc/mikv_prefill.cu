@@ -8,6 +8,7 @@
 //   1. rows:    per query i, the log2 of its softmax normaliser, c_i = log2 sum_{t <= i} 2^(s_it log2 e)
 //               (accumulated online against a reference, as in flash attention, without values);
 //   2. columns: per key t, sum over the G query heads and the queries i >= t of 2^(s_it log2 e - c_i).
+// Where the queries' normalisers are given (they attend to more keys than these), a copy of them replaces pass 1.
 // A CTA owns one 128-token tile of its fixed operand (queries in pass 1, keys in pass 2: the M side, so that
 // epilogue thread r owns accumulator row r = TMEM lane r) and streams 64-token tiles of the other operand.
 // Its warps specialise: warp 8 issues the TMA copies (the fixed tile, then a four-stage ring of 128B-swizzled
@@ -291,6 +292,17 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_rows_kernel(const __gri
   }
 }
 
+// Normalisers that are given, in place of pass 1: log2 units, +inf (weighs nothing) for padding queries and for queries
+// without a finite sum. Bound by its launch: 8 bytes per query, beside pass 2's 256 bytes of each query row.
+__global__ void __launch_bounds__(256) prefill_given_kernel(float* stats, const float* lse, int rows, int T, int T_pad) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (size_t)rows * T_pad) return;
+  const size_t row = i / T_pad;
+  const int q = (int)(i - row * T_pad);
+  const float c = q < T ? lse[row * T + q] * 1.4426950408889634f : INFINITY;
+  stats[i] = c == -INFINITY ? INFINITY : c;
+}
+
 // ------------------------------------------------------------------------------ pass 2: column sums
 
 __global__ void __launch_bounds__(kPfThreads, 2) prefill_cols_kernel(const __grid_constant__ PrefillArgs a) {
@@ -343,7 +355,7 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_cols_kernel(const __gri
 
 }  // namespace
 
-cudaError_t launch_prefill(const PrefillArgs& a, int batch, cudaStream_t st) {
+cudaError_t launch_prefill(const PrefillArgs& a, int batch, const float* lse, cudaStream_t st) {
   static bool configured = false;
   if (!configured) {
     cudaError_t e = cudaFuncSetAttribute(prefill_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
@@ -353,7 +365,12 @@ cudaError_t launch_prefill(const PrefillArgs& a, int batch, cudaStream_t st) {
     configured = true;
   }
   const int nt = (a.T + kPfTile - 1) / kPfTile;
-  prefill_rows_kernel<<<dim3(nt, batch * a.heads_q), kPfThreads, kPfSmem, st>>>(a);
+  if (lse) {
+    const size_t n = (size_t)batch * a.heads_q * a.T_pad;
+    prefill_given_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(a.stats, lse, batch * a.heads_q, a.T, a.T_pad);
+  } else {
+    prefill_rows_kernel<<<dim3(nt, batch * a.heads_q), kPfThreads, kPfSmem, st>>>(a);
+  }
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   prefill_cols_kernel<<<dim3(nt, batch * a.heads_kv), kPfThreads, kPfSmem, st>>>(a);

@@ -33,6 +33,7 @@ inline size_t prefill_workspace_bytes(int batch, int heads_q, int T) {
   return kWsHeader + (stats + 255) / 256 * 256;
 }
 
-cudaError_t launch_prefill(const PrefillArgs& a, int batch, cudaStream_t st);
+// lse: log of each query's whole sum, [B][Hq][T], or nullptr = the sums over these keys (pass 1).
+cudaError_t launch_prefill(const PrefillArgs& a, int batch, const float* lse, cudaStream_t st);
 
 }  // namespace mikv

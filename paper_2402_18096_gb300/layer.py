@@ -111,8 +111,9 @@ class SharedPrefixLayer:
     def from_prompts(cls, shape: Shape, table: RotaryTable, prefix, own, out_prefix, out_own, key_len=None):
         """The prompts of a batch: prefix = (q, k, v) of the shared tokens ([1, H, P, d], bf16), own = (q, k, v) of each
         request's own tokens ([B, H, T, d]). Turns q and k (in place), attends the prefix (into out_prefix) and the
-        own tokens over prefix and own keys (into out_own), and builds the own cache by accumulated attention. shape is
-        the own cache's (shape_for_context with context = T).
+        own tokens over prefix and own keys (into out_own), and builds the own cache by accumulated attention: the
+        weights of the softmax over prefix and own keys, as in step. shape is the own cache's (shape_for_context with
+        context = T).
         Every request has all T own tokens: key_len is refused. The cache holds the same number of slots and rows for
         every request and its attention weighs all of them, so the padding of a shorter one would be kept, attended and
         counted, and its next token would stand at a wrong position. Requests of other lengths go into other layers."""
@@ -129,9 +130,13 @@ class SharedPrefixLayer:
         keys = torch.cat([k0.expand(B, Hkv, P, d), k], dim=2)
         values = torch.cat([v0.expand(B, Hkv, P, d), v], dim=2)
         ws = workspace(mikv_prompt_workspace_bytes(q, keys), k.device)
-        mikv_prompt_attention(q, keys, values, out_own, ws)
-        layer = MixedPrecisionLayer.from_prefill(shape, k.contiguous(), v.contiguous(), None, q.contiguous(),
-                                                 device=k.device)
+        lse = torch.empty(B, q.shape[1], T, dtype=torch.float32, device=k.device)
+        mikv_prompt_attention(q, keys, values, out_own, ws, lse=lse)
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        scores = torch.empty(B, Hkv, T, dtype=torch.float32, device=k.device)
+        ws = workspace(mikv_workspace_bytes(shape, WS_PREFILL, T), k.device)
+        mikv_prefill_scores(shape, q, k, scores, ws, lse=lse)
+        layer = MixedPrecisionLayer.from_prefill(shape, k, v, scores, q, device=k.device)
         return cls(layer, k0.contiguous(), v0.contiguous(), table)
 
     def step(self, q, k_new, v_new, out):

@@ -1,0 +1,112 @@
+"""The own cache of a shared-prefix layer: importance under the softmax over prefix and own tokens."""
+import math
+
+import pytest
+import torch
+
+import paper_2402_18096_gb300 as pkg
+from paper_2402_18096_gb300.layer import SharedPrefixLayer, workspace
+import _attn_ref as ref
+from _cases import bits16
+from test_gpu_prefill import prefill_rtol
+
+pytestmark = pytest.mark.gpu
+
+SCALE = 1 / math.sqrt(128)
+
+
+def make(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda").to(torch.bfloat16)
+
+
+def given_scores(q, k, lse):
+    """fp32 [B, Hkv, T] of the library for own rows q [B, Hq, T, d], k [B, Hkv, T, d] and given log-sum-exps."""
+    B, Hq, T, _ = q.shape
+    Hkv = k.shape[1]
+    shape = pkg.Shape(B, Hq, Hkv, 2, 32, 1, 16)
+    out = torch.full((B, Hkv, T), math.nan, device="cuda")
+    ws = workspace(pkg.mikv_workspace_bytes(shape, pkg.WS_PREFILL, T))
+    pkg.mikv_prefill_scores(shape, q, k, out, ws, lse=lse)
+    pkg.mikv_workspace_check(ws)
+    return out
+
+
+def summed_weights(q, k, lse):
+    """The same in 64 bits: sum over query heads and queries i >= t of exp(s_it - lse_i)."""
+    B, Hq, T, _ = q.shape
+    Hkv = k.shape[1]
+    past = torch.ones(T, T, dtype=torch.bool, device="cuda").tril()
+    out = torch.zeros(B, Hkv, T, dtype=torch.float64, device="cuda")
+    for b in range(B):
+        for h in range(Hq):
+            kv = h // (Hq // Hkv)
+            s = SCALE * q[b, h].double() @ k[b, kv].double().T
+            w = torch.exp(s - lse[b, h].double()[:, None])
+            w[torch.isinf(lse[b, h])] = 0  # (a query without a finite sum weighs nothing)
+            out[b, kv] += torch.where(past, w, 0.0).sum(dim=0)
+    return out
+
+
+def given_rtol(q, k, lse):
+    """prefill_rtol with the given normaliser in place of the kernel's own: it is turned into log2 units by one fp32
+    product with a rounded constant, 2^-23 of its size, which is an absolute error of the exponent."""
+    size = float(torch.where(torch.isinf(lse), 0.0, lse).abs().max()) * math.log2(math.e)
+    return prefill_rtol(bits16(q), bits16(k), q.shape[2], q.shape[1] // k.shape[1]) + 2 * math.log(2) * 2.0 ** -23 * size
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,T", [(1, 2, 2, 1), (2, 8, 2, 130), (1, 4, 1, 700), (3, 8, 1, 64)])
+def test_scores_with_given_normalisers(B, Hq, Hkv, T):
+    g = torch.Generator(device="cuda").manual_seed(T)
+    q, k = make(g, B, Hq, T, 128), make(g, B, Hkv, T, 128)
+    k[..., 5] *= 5
+    lse = 4 + 3 * torch.randn(B, Hq, T, generator=g, device="cuda")
+    if T > 1:
+        lse[0, 0, T // 2] = -math.inf  # a query that saw nothing
+        lse[-1, -1, T - 1] = math.inf
+    got, want = given_scores(q, k, lse).double(), summed_weights(q, k, lse)
+    assert bool(((got - want).abs() <= given_rtol(q, k, lse) * want).all())
+
+
+def prompts(g, B, Hq, Hkv, P, T, ratio, steps, bits=2, group=32):
+    """A layer from random prompts, with its turned queries and keys."""
+    table = pkg.RotaryTable()
+    q0, k0, v0 = (make(g, 1, h, P, 128) for h in (Hq, Hkv, Hkv))
+    q, k, v = (make(g, B, h, T, 128) for h in (Hq, Hkv, Hkv))
+    k0 *= 1.5  # the prefix holds most of the weight
+    shape = pkg.shape_for_context(B, Hq, Hkv, bits, group, T, ratio, steps)
+    out0 = torch.empty(1, Hq, P, 128, dtype=torch.bfloat16, device="cuda")
+    out1 = torch.empty(B, Hq, T, 128, dtype=torch.bfloat16, device="cuda")
+    layer = SharedPrefixLayer.from_prompts(shape, table, (q0, k0, v0), (q, k, v), out0, out1)
+    return layer, table, (k0, v0), (q, k, v)
+
+
+def joint_lse(q, k0, k):
+    """Log of each own query's sum over prefix and own keys, in 64 bits, and the bound on the kernels' value."""
+    B, Hq, T, _ = q.shape
+    P, G = k0.shape[2], Hq // k.shape[1]
+    lse = torch.empty(B, Hq, T, dtype=torch.float64, device="cuda")
+    bound = 0.0
+    mask = torch.arange(P + T, device="cuda") <= P + torch.arange(T, device="cuda")[:, None]
+    for b in range(B):
+        for h in range(Hq):
+            keys = torch.cat([k0[0, h // G], k[b, h // G]])
+            _, lse[b, h], _, eb = ref.attention(q[b, h], keys, keys, mask, SCALE)
+            bound = max(bound, float(eb.max()))
+    return lse, bound
+
+
+def test_prompt_importance_is_that_of_the_whole_softmax():
+    """The scores that the own cache starts with are sums of weights over prefix and own keys; the kept tokens are the
+    largest of them."""
+    B, Hq, Hkv, P, T = 2, 8, 2, 700, 150
+    layer, _, (k0, _), (q, k, _) = prompts(torch.Generator(device="cuda").manual_seed(5), B, Hq, Hkv, P, T, 0.2, 4)
+    lse, bound = joint_lse(q, k0, k)
+    want = summed_weights(q, k, lse)
+    # (both statistics of a weight are off: the scores' own bound, twice the bound of the log-sum-exp with its margin)
+    rtol = given_rtol(q, k, lse) + 2 * math.expm1(2 * bound)
+    n = layer.own.shape.hi_cap - 1
+    tok = layer.own.cache.hi_tok[:, :, :n].long()
+    at = torch.gather(want, 2, tok)
+    assert bool(((layer.own.cache.acc[:, :, :n].double() - at).abs() <= rtol * at).all())
+    edge = want.sort(dim=2, descending=True).values[:, :, n - 1:n]
+    assert bool((at >= edge * (1 - 2 * rtol)).all())

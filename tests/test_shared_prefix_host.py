@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2402_18096_gb300 as pkg
+import test_nvtx_ranges as ranges
 from paper_2402_18096_gb300.layer import SharedPrefixLayer
 
 
@@ -19,3 +20,25 @@ def test_key_lengths_are_refused():
                                        torch.empty_like(own[0]),
                                        key_len=torch.tensor([P + T, P + 2], dtype=torch.int32))
     assert all(bool((x == 1).all()) for x in prefix + own)
+
+
+def test_given_normalisers_refused():
+    """mikv_prefill_scores_lse: what is checked before anything is launched."""
+    lib, p = pkg.load(), 0x10000  # never dereferenced
+    shape = pkg.Shape(2, 8, 2, 2, 32, 1, 16)
+
+    def rc(q=p, k=p, T=64, lse=p, scores=p, ws=p, n=1 << 30, s=shape):
+        return lib.mikv_prefill_scores_lse(s.c(), q, k, T, 0.1, lse, scores, ws, n, None)
+
+    assert rc(lse=None) == 1 and rc(lse=p + 2) == 1
+    assert rc(q=None) == 1 and rc(k=p + 8) == 1 and rc(scores=None) == 1 and rc(T=0) == 1
+    assert rc(s=pkg.Shape(2, 7, 2, 2, 32, 1, 16)) != 0
+    assert rc(ws=None) == 5 and rc(n=16) == 5
+    q = torch.zeros(2, 8, 64, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="lse"):
+        pkg.mikv_prefill_scores(shape, q, q[:, :2], torch.zeros(2, 2, 64), q, lse=torch.zeros(2, 8, 63))
+
+
+def test_range_of_the_given_form(tmp_path, monkeypatch):
+    monkeypatch.setattr(ranges, "CALLS", {"mikv_prefill_scores_lse": (None, None, None, 0, 1.0, None, None, None, 0, None)})
+    ranges.test_every_entry_point_has_one_balanced_range(tmp_path)
