@@ -1,13 +1,16 @@
-"""The own cache of a shared-prefix layer: importance under the softmax over prefix and own tokens."""
+"""The own cache of a shared-prefix layer: importance under the softmax over prefix and own tokens, from the prompt on
+and over decode steps whose cache holds retained (quantised) tokens beside the prefix."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
+import oracle
 import paper_2402_18096_gb300 as pkg
 from paper_2402_18096_gb300.layer import SharedPrefixLayer, workspace
 import _attn_ref as ref
-from _cases import bits16
+from _cases import bits16, logit_bounds, softmax_stat_bounds
 from test_gpu_prefill import prefill_rtol
 
 pytestmark = pytest.mark.gpu
@@ -110,3 +113,63 @@ def test_prompt_importance_is_that_of_the_whole_softmax():
     assert bool(((layer.own.cache.acc[:, :, :n].double() - at).abs() <= rtol * at).all())
     edge = want.sort(dim=2, descending=True).values[:, :, n - 1:n]
     assert bool((at >= edge * (1 - 2 * rtol)).all())
+
+
+def snapshot(layer):
+    """The own cache as the oracle's arrays."""
+    c, s = layer.own.cache, layer.own.shape
+    hi = {x: bits16(getattr(c, x)[:, :, :s.hi_cap].contiguous().cpu()) for x in ("k_hi", "v_hi")}
+    hi.update({x: getattr(c, x)[:, :, :s.hi_cap].contiguous().cpu().numpy() for x in ("hi_tok", "acc")})
+    lo = {x: getattr(c, x).cpu().numpy().copy() for x in ("k_codes", "v_codes", "lo_tok")}
+    lo.update({x: getattr(c, x).cpu().numpy().view(np.uint16).copy() for x in ("k_params", "v_params")})
+    return {**hi, **lo}, c.balancer.cpu().numpy()
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,P,T,bits", [(2, 8, 2, 700, 150, 2), (3, 4, 4, 130, 200, 4)])
+def test_steps_over_prefix_and_retained_tokens(B, Hq, Hkv, P, T, bits):
+    """Every step against the oracle on the cache as it stood before the step (its own insertion, attention over slots and
+    retained rows, quantiser), joined in 64 bits with attention over the prefix."""
+    steps = 4
+    g = torch.Generator(device="cuda").manual_seed(6)
+    layer, table, (k0, v0), (_, _, v_own) = prompts(g, B, Hq, Hkv, P, T, 0.2, steps, bits)
+    o, G = layer.own, Hq // Hkv
+    vmax = max(float(v0.abs().max()), float(v_own.abs().max()))
+    full = torch.ones(G, P, dtype=torch.bool, device="cuda")
+    for i in range(steps):
+        q, k, v = (make(g, B, h, 128) for h in (Hq, Hkv, Hkv))
+        tq, tk = q.clone(), k.clone()
+        vmax = max(vmax, float(v.abs().max()))
+        pkg.mikv_rotary(table, tq[:, :, None], tk[:, :, None], start=P + T + i)
+        c, bal = snapshot(layer)
+        n_lo, slots = o.n_lo, o.slots.cpu().numpy()
+        out = torch.empty(B, Hq, 128, device="cuda")
+        layer.step(q, k, v, out)
+        oracle.insert_token(c, bits16(tk.cpu()), bits16(v.cpu()), T + i, slots)
+        own, logits, ml = oracle.decode_attention(c, bits16(tq.cpu()), n_lo, SCALE, balancer_=bal)
+        acc = torch.as_tensor(c["acc"]).double()
+        rel = 0.0
+        for b in range(B):
+            for h in range(Hkv):
+                hs = slice(h * G, (h + 1) * G)
+                one = {x: c[x][b:b + 1, h:h + 1] for x in c}
+                hi, lo = logit_bounds(one, bits16(tq[b:b + 1, hs].cpu()), bal[h], bits, 32, n_lo, SCALE)
+                E, l_rtol = softmax_stat_bounds(hi, lo, o.shape.hi_cap + n_lo)
+                mine = torch.as_tensor(E + l_rtol).cuda()
+                po, pe, pb, peb = ref.attention(tq[b, hs], k0[0, h], v0[0, h], full, SCALE, out_dtype=torch.float32)
+                jo, je, jb, jeb = ref.join(po, pe, pb, peb + mine, torch.as_tensor(own[b, hs]).cuda(),
+                                           torch.as_tensor(ml[b, hs]).cuda(), torch.float32)
+                # (the own part's documented bound is 2e-3 of the largest value)
+                assert bool(((out[b, hs].double() - jo).abs() <= jb + 2e-3 * vmax).all())
+                assert bool(((layer.ml[b, hs, 0].double() - je).abs() <= jeb).all())
+                w = torch.exp(torch.as_tensor(logits[b, hs]) - je.cpu()[:, None]).sum(dim=0)
+                acc[b, h] += w
+                rel = max(rel, math.expm1(2 * float(jeb.max()) + 2 * float(hi.max())))
+        got = o.cache.acc[:, :, :o.shape.hi_cap].cpu()
+        assert bool(((got.double() - acc).abs() <= rel * acc + 2.0 ** -20 * acc).all())
+        victim, _ = oracle.select_demote(got.numpy(), 1, ids=c["hi_tok"])
+        assert np.array_equal(o.slots.cpu().numpy(), victim[:, :, 0])
+        oracle.quantize_pack(c, c["k_hi"], c["v_hi"], victim, n_lo, src_tok=c["hi_tok"], balancer_=bal)
+        after, _ = snapshot(layer)
+        for x in ("k_codes", "v_codes", "k_params", "v_params", "lo_tok"):
+            assert np.array_equal(after[x][:, :, :n_lo + 1], c[x][:, :, :n_lo + 1]), x
+    assert o.n_lo == n_lo + 1 and o.pos == T + steps
