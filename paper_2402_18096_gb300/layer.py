@@ -122,21 +122,32 @@ class SharedPrefixLayer:
         q0, k0, v0 = prefix
         q, k, v = own
         B, Hkv, T, d = k.shape
-        P = k0.shape[2]
+        Hq, P, dev = q.shape[1], k0.shape[2], k.device
         mikv_rotary(table, q0, k0)
         mikv_rotary(table, q, k, start=P)
-        ws = workspace(mikv_prompt_workspace_bytes(q0, k0), k.device)
+        rows = q.transpose(1, 2).contiguous().view(B * T, Hq, d)  # every own token a request of the prefix
+        ws = workspace(max(mikv_prompt_workspace_bytes(q0, k0), mikv_prompt_workspace_bytes(q, k),
+                           mikv_prefix_workspace_bytes(rows, k0), mikv_workspace_bytes(shape, WS_PREFILL, T)), dev)
         mikv_prompt_attention(q0, k0, v0, out_prefix, ws)
-        keys = torch.cat([k0.expand(B, Hkv, P, d), k], dim=2)
-        values = torch.cat([v0.expand(B, Hkv, P, d), v], dim=2)
-        ws = workspace(mikv_prompt_workspace_bytes(q, keys), k.device)
-        lse = torch.empty(B, q.shape[1], T, dtype=torch.float32, device=k.device)
-        mikv_prompt_attention(q, keys, values, out_own, ws, lse=lse)
+        # the own tokens over their own keys, joined with their attention over the prefix as it lies
+        own_out = torch.empty(B, T, Hq, d, dtype=torch.float32, device=dev)
+        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=dev)
+        mikv_prompt_attention(q, k, v, own_out.transpose(1, 2), ws, lse=lse)
+        own_ml = torch.stack([lse, torch.ones_like(lse)], dim=3).transpose(1, 2).reshape(B * T, Hq, 2)
+        ml = torch.empty_like(own_ml)
+        joined = out_own.transpose(1, 2)
+        if not joined.is_contiguous():
+            joined = torch.empty(B, T, Hq, d, dtype=out_own.dtype, device=dev)
+        mikv_prefix_attention(rows, k0, v0, joined.view(B * T, Hq, d), ws, own_out=own_out.view(B * T, Hq, d),
+                              own_ml=own_ml, ml=ml)
+        if joined.data_ptr() != out_own.data_ptr():
+            out_own.copy_(joined.transpose(1, 2))
+        lse.copy_(ml[:, :, 0].view(B, T, Hq).transpose(1, 2))
+        del rows, own_out, own_ml, joined
         q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
-        scores = torch.empty(B, Hkv, T, dtype=torch.float32, device=k.device)
-        ws = workspace(mikv_workspace_bytes(shape, WS_PREFILL, T), k.device)
+        scores = torch.empty(B, Hkv, T, dtype=torch.float32, device=dev)
         mikv_prefill_scores(shape, q, k, scores, ws, lse=lse)
-        layer = MixedPrecisionLayer.from_prefill(shape, k, v, scores, q, device=k.device)
+        layer = MixedPrecisionLayer.from_prefill(shape, k, v, scores, q, device=dev)
         return cls(layer, k0.contiguous(), v0.contiguous(), table)
 
     def step(self, q, k_new, v_new, out):

@@ -115,6 +115,45 @@ def test_prompt_importance_is_that_of_the_whole_softmax():
     assert bool((at >= edge * (1 - 2 * rtol)).all())
 
 
+def test_the_prefix_is_not_copied_for_each_request():
+    """What from_prompts allocates stays well below the prefix's keys and values once per request."""
+    B, Hq, Hkv, P, T = 128, 8, 2, 2048, 8
+    g = torch.Generator(device="cuda").manual_seed(7)
+    q0, k0, v0 = (make(g, 1, h, P, 128) for h in (Hq, Hkv, Hkv))
+    q, k, v = (make(g, B, h, T, 128) for h in (Hq, Hkv, Hkv))
+    out0, out1 = torch.empty_like(q0), torch.empty_like(q)
+    shape = pkg.shape_for_context(B, Hq, Hkv, 2, 32, T, 0.5, 2)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    layer = SharedPrefixLayer.from_prompts(shape, pkg.RotaryTable(), (q0, k0, v0), (q, k, v), out0, out1)
+    assert torch.cuda.max_memory_allocated() - before < B * (k0.nbytes + v0.nbytes) // 2
+    assert torch.equal(layer.k_prefix, k0)
+
+
+@pytest.mark.parametrize("major", [False, True])
+def test_prompt_outputs_in_either_layout(major):
+    """Own tokens over prefix and own keys against 64 bits, written head-major or token-major, from views of one
+    projection."""
+    B, Hq, Hkv, P, T = 2, 8, 2, 333, 77
+    g = torch.Generator(device="cuda").manual_seed(8)
+    table = pkg.RotaryTable()
+    q0, k0, v0 = (make(g, 1, h, P, 128) for h in (Hq, Hkv, Hkv))
+    own = make(g, B, T, Hq + 2 * Hkv, 128)
+    q, k, v = (own[:, :, a:b].transpose(1, 2) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    out0 = torch.empty_like(q0)
+    out1 = torch.full((B, T, Hq, 128) if major else (B, Hq, T, 128), math.nan, dtype=torch.bfloat16, device="cuda")
+    out1 = out1.transpose(1, 2) if major else out1
+    shape = pkg.shape_for_context(B, Hq, Hkv, 2, 32, T, 0.3, 2)
+    SharedPrefixLayer.from_prompts(shape, table, (q0, k0, v0), (q, k, v), out0, out1)
+    mask = torch.arange(P + T, device="cuda") <= P + torch.arange(T, device="cuda")[:, None]
+    for b in range(B):
+        for h in range(Hq):
+            keys, vals = torch.cat([k0[0, h // 4], k[b, h // 4]]), torch.cat([v0[0, h // 4], v[b, h // 4]])
+            o, _, bound, _ = ref.attention(q[b, h], keys, vals, mask, SCALE)
+            assert bool(((out1[b, h].double() - o).abs() <= bound).all())
+
+
 def snapshot(layer):
     """The own cache as the oracle's arrays."""
     c, s = layer.own.cache, layer.own.shape
