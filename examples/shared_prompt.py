@@ -45,8 +45,7 @@ def run(requests=32, prefix=8192, own=512, steps=8, heads_q=32, heads_kv=8, bits
         layer.step(q, k, v, outs[i])
     last.record()
     torch.cuda.synchronize()
-    for ws in (layer.ws_own, layer.ws_prefix):
-        pkg.mikv_workspace_check(ws)
+    layer.check()
     return outs, first.elapsed_time(last) * 1e3 / (steps - min(3, steps - 1))
 
 

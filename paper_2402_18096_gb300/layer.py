@@ -21,7 +21,7 @@ from . import (LayerCache, RotaryTable, Shape, WS_ATTENTION, WS_BALANCER, WS_PRE
                mikv_decode_attention, mikv_decode_step, mikv_gather_hi, mikv_insert_token,
                mikv_prefill_scores, mikv_prefix_attention, mikv_prefix_workspace_bytes, mikv_prompt_attention,
                mikv_prompt_workspace_bytes, mikv_quantize_pack, mikv_rotary, mikv_select_demote,
-               mikv_update_importance, mikv_workspace_bytes)
+               mikv_update_importance, mikv_workspace_bytes, mikv_workspace_check)
 
 
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:
@@ -106,6 +106,7 @@ class SharedPrefixLayer:
         self.demoted = torch.empty(s.batch, s.heads_kv, 1, dtype=torch.int32, device=dev)
         self.ws_own = workspace(mikv_workspace_bytes(s, WS_ATTENTION, s.lo_cap), dev)
         self.ws_prefix = workspace(mikv_prefix_workspace_bytes(like, k_prefix), dev)
+        self.prompt_status = None  # the status words that the prompts' calls left (from_prompts)
 
     @classmethod
     def from_prompts(cls, shape: Shape, table: RotaryTable, prefix, own, out_prefix, out_own, key_len=None):
@@ -148,7 +149,15 @@ class SharedPrefixLayer:
         scores = torch.empty(B, Hkv, T, dtype=torch.float32, device=dev)
         mikv_prefill_scores(shape, q, k, scores, ws, lse=lse)
         layer = MixedPrecisionLayer.from_prefill(shape, k, v, scores, q, device=dev)
-        return cls(layer, k0.contiguous(), v0.contiguous(), table)
+        layer = cls(layer, k0.contiguous(), v0.contiguous(), table)
+        layer.prompt_status = ws[:256].clone()  # (the workspace itself is not kept)
+        return layer
+
+    def check(self, stream=None):
+        """Raise MikvError (MIKV_ERR_DEVICE) if a kernel of the prompts or of a step so far gave up; synchronises."""
+        for ws in (self.prompt_status, self.ws_prefix, self.ws_own):
+            if ws is not None:
+                mikv_workspace_check(ws, stream)
 
     def step(self, q, k_new, v_new, out):
         """One decode step: q [B, Hq, d], k_new, v_new [B, Hkv, d] of the new token as projected (q and k_new are turned

@@ -154,6 +154,33 @@ def test_prompt_outputs_in_either_layout(major):
             assert bool(((out1[b, h].double() - o).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("call,at", [(None, 0), ("mikv_prompt_attention", 4), ("mikv_prefix_attention", 4),
+                                     ("mikv_prefill_scores", 4)])
+def test_check_reports_failures_of_the_prompts(monkeypatch, call, at):
+    """A status word that one of the prompts' calls leaves (written by the host here) is still seen after the layer is
+    built; without one nothing is reported."""
+    from paper_2402_18096_gb300 import layer as module
+
+    if call:
+        real = getattr(module, call)
+
+        def failing(*args, **kw):
+            real(*args, **kw)
+            args[at].view(torch.int32)[0] = 1
+
+        monkeypatch.setattr(module, call, failing)
+    layer = prompts(torch.Generator(device="cuda").manual_seed(9), 2, 4, 2, 60, 20, 0.5, 2)[0]
+    monkeypatch.undo()
+    out = torch.empty(2, 4, 128, dtype=torch.bfloat16, device="cuda")
+    layer.step(*(torch.ones(2, h, 128, dtype=torch.bfloat16, device="cuda") for h in (4, 2, 2)), out)
+    if call:
+        with pytest.raises(pkg.MikvError) as e:
+            layer.check()
+        assert e.value.code == 6
+    else:
+        layer.check()
+
+
 def snapshot(layer):
     """The own cache as the oracle's arrays."""
     c, s = layer.own.cache, layer.own.shape
