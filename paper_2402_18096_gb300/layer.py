@@ -17,7 +17,7 @@ import math
 
 import torch
 
-from . import (LayerCache, RotaryTable, Shape, WS_ATTENTION, WS_BALANCER, WS_PREFILL, WS_STEP, mikv_compute_balancer,
+from . import (LayerCache, MikvError, RotaryTable, Shape, WS_ATTENTION, WS_BALANCER, WS_PREFILL, WS_STEP, mikv_compute_balancer,
                mikv_decode_attention, mikv_decode_step, mikv_gather_hi, mikv_insert_token,
                mikv_prefill_scores, mikv_prefix_attention, mikv_prefix_workspace_bytes, mikv_prompt_attention,
                mikv_prompt_workspace_bytes, mikv_quantize_pack, mikv_rotary, mikv_select_demote,
@@ -161,9 +161,18 @@ class SharedPrefixLayer:
 
     def step(self, q, k_new, v_new, out):
         """One decode step: q [B, Hq, d], k_new, v_new [B, Hkv, d] of the new token as projected (q and k_new are turned
-        in place) into out [B, Hq, d]. The importance update takes the weights of the softmax over both parts."""
+        in place) into out [B, Hq, d] (bf16 or fp32). The importance update takes the weights of the softmax over both
+        parts. A call that is refused has changed nothing."""
         o, c = self.own, self.own.cache
         s = o.shape
+        for name, t, heads, types in (("q", q, s.heads_q, (torch.bfloat16,)), ("k_new", k_new, s.heads_kv, (torch.bfloat16,)),
+                                      ("v_new", v_new, s.heads_kv, (torch.bfloat16,)),
+                                      ("out", out, s.heads_q, (torch.bfloat16, torch.float32))):
+            if t.shape != (s.batch, heads, s.head_dim) or t.dtype not in types or not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"{name}: expected a dense device tensor of shape {(s.batch, heads, s.head_dim)} and type "
+                                 f"{' or '.join(str(x) for x in types)}, got {t.dtype} {tuple(t.shape)}")
+        if s.bits and o.n_lo >= s.lo_cap:
+            raise MikvError("SharedPrefixLayer.step", 3)  # MIKV_ERR_CAPACITY: no row is left for the demoted token
         mikv_rotary(self.table, q[:, :, None], k_new[:, :, None], start=self.prefix + o.pos)
         mikv_insert_token(c, k_new, v_new, o.pos, o.slots)
         mikv_decode_attention(c, o.n_lo, q, o.sm_scale, self.own_out, self.ws_own, hi_logits=self.logits, ml=self.own_ml)

@@ -181,6 +181,34 @@ def test_check_reports_failures_of_the_prompts(monkeypatch, call, at):
         layer.check()
 
 
+def test_refused_steps_change_nothing():
+    """A full retained set and wrong arguments are refused before the new token is turned, inserted or counted."""
+    B, Hq, Hkv = 2, 4, 2
+    g = torch.Generator(device="cuda").manual_seed(10)
+    layer = prompts(g, B, Hq, Hkv, 60, 20, 0.5, 2)[0]
+    o, out = layer.own, torch.zeros(B, Hq, 128, dtype=torch.bfloat16, device="cuda")
+
+    def refused(error, *args):
+        c = o.cache
+        state = [x for x in (c.k_hi, c.v_hi, c.hi_tok, c.acc, c.lo_tok, o.slots, *args)]
+        before, counts = [x.clone() for x in state], (o.n_lo, o.pos)
+        with pytest.raises(error) as e:
+            layer.step(*args)
+        assert all(torch.equal(x, y) for x, y in zip(state, before)) and counts == (o.n_lo, o.pos)
+        return e.value
+
+    q, k, v = (make(g, B, h, 128) for h in (Hq, Hkv, Hkv))
+    refused(ValueError, q, k, v.float(), out)
+    refused(ValueError, q, k, v[:1], out)
+    refused(ValueError, q.float(), k, v, out)
+    refused(ValueError, q, k.transpose(0, 1).contiguous().transpose(0, 1), v, out)
+    refused(ValueError, q, k, v, out[:, :2])
+    refused(ValueError, q, k, v, torch.zeros(B, Hq, 128, dtype=torch.float16, device="cuda"))
+    while o.n_lo < o.shape.lo_cap:
+        layer.step(*(make(g, B, h, 128) for h in (Hq, Hkv, Hkv)), out)
+    assert refused(pkg.MikvError, q, k, v, out).code == 3
+
+
 def snapshot(layer):
     """The own cache as the oracle's arrays."""
     c, s = layer.own.cache, layer.own.shape
