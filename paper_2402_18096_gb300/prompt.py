@@ -135,7 +135,7 @@ def mikv_rotary(table: RotaryTable, q, k=None, q_out=None, k_out=None, positions
         ki = _view(k, shape)
         ko = ki if k_out is k else _view(k_out, shape)
     desc = _pack_rotary(_dtype(q), B, T, Hq, Hk, d, table.rot_dim, LAYOUTS[table.layout], int(inverse), table.amplitude)
-    rc = load().mikv_rotary(desc, qi, qo, ki, ko, table.phases.data_ptr(),
+    rc = load().mikv_rotary(desc, qi, qo, ki, ko, _ptr(table.phases),
                             _dense(positions, (B, T), torch.int32, "positions"), start, _raw_stream(stream, q))
     _check("mikv_rotary", rc)
     return q_out, k_out

@@ -5,6 +5,7 @@ import torch
 
 import paper_2402_18096_gb300 as pkg
 import test_nvtx_ranges as ranges
+from paper_2402_18096_gb300 import prompt
 from paper_2402_18096_gb300.layer import SharedPrefixLayer
 
 
@@ -42,3 +43,23 @@ def test_given_normalisers_refused():
 def test_range_of_the_given_form(tmp_path, monkeypatch):
     monkeypatch.setattr(ranges, "CALLS", {"mikv_prefill_scores_lse": (None, None, None, 0, 1.0, None, None, None, 0, None)})
     ranges.test_every_entry_point_has_one_balanced_range(tmp_path)
+
+
+def test_phases_on_the_host_are_refused(monkeypatch):
+    """The kernel reads the phases: a table on the host must not reach it (as with every other pointer)."""
+    calls = []
+
+    class Library:
+        def mikv_rotary(self, *args):
+            calls.append(args)
+            return 0
+
+    monkeypatch.setattr(prompt, "load", Library)
+    monkeypatch.setattr(prompt, "_view", lambda t, shape: b"")
+    monkeypatch.setattr(prompt, "_raw_stream", lambda stream, t: 0)
+    table = pkg.RotaryTable.__new__(pkg.RotaryTable)
+    table.rot_dim, table.layout, table.amplitude = 128, "half", 1.0
+    table.phases = torch.zeros(64, dtype=torch.int64)
+    with pytest.raises(ValueError, match="device"):
+        prompt.mikv_rotary(table, torch.zeros(1, 1, 1, 128))
+    assert not calls
