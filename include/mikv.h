@@ -399,6 +399,7 @@ mikv_status mikv_rotary_phases(const double* freq, int32_t n, uint64_t* phases);
  *   phases     uint64 [rot / 2] (device), see mikv_rotary_phases
  *   positions  int32 [batch][tokens] (device), or NULL: token t has position `start` + t. Negative positions turn
  *              the other way.
+ * With no tokens nothing is launched and no view is looked at.
  */
 mikv_status mikv_rotary(const mikv_rotary_desc* desc, const mikv_view* q_in, const mikv_view* q_out,
                         const mikv_view* k_in, const mikv_view* k_out, const uint64_t* phases,
@@ -413,7 +414,7 @@ mikv_status mikv_rotary(const mikv_rotary_desc* desc, const mikv_view* q_in, con
  *           `docs`) are seen by all of its queries
  *   key_len int32 [batch] or NULL: keys from key_len[b] on are seen by nobody
  * An empty span is written as [0, 0). One launch; the result serves every layer of the batch.
- *   spans   int32 [batch][tq][2] (device), 8-byte aligned
+ *   spans   int32 [batch][tq][2] (device), 8-byte aligned; may be NULL with no queries
  */
 mikv_status mikv_mask_spans(int32_t* spans, int32_t batch, int32_t tq, int32_t tk, int32_t q_start, int32_t causal,
                             const int32_t* docs, int32_t n_docs, const int32_t* prefix, const int32_t* key_len,

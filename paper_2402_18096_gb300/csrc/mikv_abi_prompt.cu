@@ -114,6 +114,7 @@ mikv_status mikv_rotary(const mikv_rotary_desc* d, const mikv_view* q_in, const 
   if (d->layout != MIKV_ROTARY_HALF && d->layout != MIKV_ROTARY_INTERLEAVED) return MIKV_ERR_ARG;
   if (d->rot < 2 || d->rot % 2 || d->rot > d->head_dim || !(fabsf(d->amplitude) <= 3.402823466e38f)) return MIKV_ERR_ARG;
   if (d->head_dim != kHeadDim || d->batch > 65535 || (int64_t)d->heads_q + d->heads_k > 65535) return MIKV_ERR_UNSUPPORTED;
+  if (d->tokens == 0) return MIKV_OK;  // (an empty tensor may have no address)
   RotaryArgs a;
   memset(&a, 0, sizeof a);
   const int bytes = elem_bytes(d->dtype), n = 16 / bytes;
@@ -134,7 +135,6 @@ mikv_status mikv_rotary(const mikv_rotary_desc* d, const mikv_view* q_in, const 
     vec = vec && aligned(x.in, 16) && aligned(x.out, 16);
     for (int j = 0; j < 3; ++j) vec = vec && s[j] % n == 0 && o[j] % n == 0;
   }
-  if (d->tokens == 0) return MIKV_OK;
   a.phases = reinterpret_cast<const unsigned long long*>(phases);
   a.positions = positions;
   a.start = start;
@@ -150,10 +150,11 @@ mikv_status mikv_mask_spans(int32_t* spans, int32_t batch, int32_t tq, int32_t t
                             const int32_t* docs, int32_t n_docs, const int32_t* prefix, const int32_t* key_len,
                             void* stream) {
   MIKV_CALL_RANGE();
-  if (!spans || !aligned(spans, 8) || batch <= 0 || tq < 0 || tk < 0 || (docs && n_docs <= 0)) return MIKV_ERR_ARG;
+  if (!aligned(spans, 8) || batch <= 0 || tq < 0 || tk < 0 || (docs && n_docs <= 0)) return MIKV_ERR_ARG;
   if (!aligned(docs, 4) || !aligned(prefix, 4) || !aligned(key_len, 4)) return MIKV_ERR_ARG;
   if (batch > 65535 || n_docs == INT_MAX) return MIKV_ERR_UNSUPPORTED;
-  if (tq == 0) return MIKV_OK;
+  if (tq == 0) return MIKV_OK;  // (an empty tensor may have no address)
+  if (!spans) return MIKV_ERR_ARG;
   const SpanArgs a = {reinterpret_cast<int2*>(spans), docs, prefix, key_len, batch, tq, tk, q_start, causal, n_docs};
   return cuda_status(launch_mask_spans(a, static_cast<cudaStream_t>(stream)));
 }

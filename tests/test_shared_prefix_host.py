@@ -1,5 +1,7 @@
 """Host side of the shared-prefix layer and of the rotary binding (no GPU): what they refuse before anything is
 launched."""
+import ctypes
+
 import pytest
 import torch
 
@@ -21,6 +23,27 @@ def test_key_lengths_are_refused():
                                        torch.empty_like(own[0]),
                                        key_len=torch.tensor([P + T, P + 2], dtype=torch.int32))
     assert all(bool((x == 1).all()) for x in prefix + own)
+
+
+def test_no_tokens_need_no_arrays():
+    """Empty tensors have no address: with no tokens nothing is launched and no pointer is asked for."""
+    lib = pkg.load()
+    view = pkg._View(None, 0, 0, 0)
+    args = [ctypes.byref(view)] * 4
+
+    def rotary(tokens, **kw):
+        d = dict(dtype=0, batch=2, tokens=tokens, heads_q=4, heads_k=2, head_dim=128, rot=128, layout=0, inverse=0,
+                 amplitude=1.0)
+        d.update(kw)
+        return lib.mikv_rotary(ctypes.byref(pkg._RotaryDesc(*[d[n] for n, _ in pkg._RotaryDesc._fields_])), *args,
+                               0x10000, None, 0, None)
+
+    assert rotary(0) == 0
+    assert rotary(1) == 1 and rotary(-1) == 1
+    assert rotary(0, rot=3) == 1 and rotary(0, dtype=7) == 1 and rotary(0, head_dim=64, rot=64) == 2
+    assert lib.mikv_mask_spans(None, 2, 0, 5, 0, 1, None, 0, None, None, None) == 0
+    assert lib.mikv_mask_spans(None, 2, 1, 5, 0, 1, None, 0, None, None, None) == 1
+    assert lib.mikv_mask_spans(None, 0, 0, 5, 0, 1, None, 0, None, None, None) == 1
 
 
 def test_given_normalisers_refused():
