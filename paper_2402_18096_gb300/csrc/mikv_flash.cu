@@ -54,12 +54,19 @@ struct Plan {
   int shares;  // CTAs that share the key tiles out among them; 0: whole row tiles
 };
 
-// Row tiles below this number may be shared out (above it the SMs are busy without, and parts would only cost traffic).
+// Row tiles below this number may be shared out: above it a share would hold more than two row tiles' worth of keys, and
+// whole row tiles leave little idle. 280 row tiles of few rows with 8000 keys: 170 us shared, 164 whole; 300: 182 and
+// 174; 310, where a third round begins: 187 and 217; 400: 238 and 233. With 1000 keys whole tiles win from 200 on (28
+// and 27 us; 288: 34 and 29).
 long long most_shared(int num_sms) { return 2ll * num_sms; }
 
 // Whole row tiles or shares, and for how many CTAs: what an estimate of the time makes shortest. A CTA has its tiles and
-// a start and end per item; shares add the merge, whose time is mostly the traffic of the parts. The constants
-// (nanoseconds) are measured on an otherwise idle GB300.
+// a start and end per item; shares add the merge, whose time is mostly the traffic of the parts, and its table, which the
+// first CTA writes set by set beside its items. The constants are nanoseconds on an idle GB300: those of a tile and of the
+// table are measured, kItem is an estimate (2500 and 3500 choose alike). Against fixed numbers of CTAs (0, eighths and
+// multiples of the row tiles up to 152) the choice was within 4 % of the best on twenty shapes: 32 requests on 32768
+// keys of 8 heads 128 CTAs 32.3 us (whole 223, 152 CTAs 34.1); one request on 4096 keys 128 CTAs 12.0 (whole 30.0, 64
+// CTAs 12.4); 160 row tiles of 8000 keys 133 CTAs 103 (whole 138); 240 of 1000 keys whole 27 (152 CTAs 31).
 Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
   Plan p;
   const long long rows = (long long)tq * G;
@@ -74,14 +81,16 @@ Plan plan_flash(int batch, int heads_kv, int G, int tq, int tk, int num_sms) {
   // a tile: the products and softmax, or its 64 KB at the SM's share of HBM
   auto tile_ns = [&](double busy) { return pair ? 1600.0 : 9.7 * busy > 1150.0 ? 9.7 * busy : 1150.0; };
   constexpr double kItem = 5000.0;  // start and end of an item
+  // 160 sets of one head and 1000 keys: 55 us shared, 26 whole; 40 sets of four: 24 and 26
+  const double table = 4000.0 + 350.0 * batch;
   const double rounds = (double)((base + num_sms - 1) / num_sms);
   double best = rounds * (tiles * tile_ns(base < num_sms ? base : num_sms) + kItem);
   const double part_rows = rows < p.item_rows ? rows : p.item_rows;
   auto consider = [&](int c) {
     if (c < 1 || c > num_sms || c <= base / 2 || 2 * (long long)c > units) return;  // (a tile for each stream at least)
     const double items = c % base == 0 ? 1.0 : 2.0 + (double)(base / c);  // the most that a share holds
-    const double cost = (double)((units + c - 1) / c) * tile_ns(c) + kItem * items + 5000.0 +
-                        ((double)c + base) * part_rows * kHeadDim * 4.0 / 3000.0;
+    const double run = (double)((units + c - 1) / c) * tile_ns(c) + kItem * items;
+    const double cost = (run > table ? run : table) + 5000.0 + ((double)c + base) * part_rows * kHeadDim * 4.0 / 3000.0;
     if (cost < best) best = cost, p.shares = c;
   };
   for (int eighths = 1; eighths <= 8; ++eighths) consider(num_sms * eighths / 8);
@@ -254,8 +263,10 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   if (e != cudaSuccess || !p.shares) return e;
   MergePartsArgs m = {a, p.part_table, p.part_o, p.part_lse, a.batch * a.tq * a.heads_q, plan.m_blocks, 0, p.log2_G, out_f32 ? 2 : f16 ? 1 : 0};
   while ((1 << m.log2_item_rows) < plan.item_rows) ++m.log2_item_rows;
-  // (four warps to a row pay where rows are few and parts many)
-  if (p.shares > 8 * base && m.rows <= 4096)
+  // Four warps to a row where parts are many and rows few (one warp / four warps, whole call): 4 rows of 32 parts 14.7 /
+  // 12.0 us, 1024 rows of 16 parts 33.9 / 32.1, 2048 rows of 19 parts 44.1 / 42.4; but 3072 rows of 9 parts 57.0 / 58.6,
+  // 4096 rows 60.9 / 64.3, and 128 rows of 5 parts 44.8 / 46.0.
+  if (p.shares > 8 * base && m.rows <= 2048)
     return launch_chained(merge_parts_kernel<4>, dim3(m.rows), dim3(128), 0, st, m);
   return launch_chained(merge_parts_kernel<1>, dim3((m.rows + 3) / 4), dim3(128), 0, st, m);
 }
