@@ -378,7 +378,8 @@ typedef struct {
   int32_t head_dim;   /* d, must be 128 */
   int32_t rot;        /* channels that turn, even, 2 <= rot <= d; the others are copied */
   int32_t layout;     /* MIKV_ROTARY_HALF or MIKV_ROTARY_INTERLEAVED */
-  int32_t inverse;    /* 0: turn by the angle; 1: by minus the angle (the transposed map: the gradient's) */
+  int32_t inverse;    /* 0: turn by the angle; 1: by minus the angle: the transposed map (turns stored keys back; it is
+                         also the map of gradients) */
   float amplitude;    /* factor on the turned channels (1 unless long-context scaling asks for one) */
 } mikv_rotary_desc;
 
@@ -441,11 +442,13 @@ typedef struct {
  *   s_ij = sm_scale * q_i . k_j;  softcap c: s_ij = c tanh(s_ij / c);  slopes: s_ij -= slope_h |p_i - j|
  *   out_i = sum_j softmax_j(s_i) v_j over the keys j that query i sees,  lse_i = ln sum_j exp(s_ij)
  * with p_i = q_start + i. A query that sees no key gives out = 0 and lse = -inf. Keys that no query sees may hold
- * any bits. A query that sees an infinity or NaN in V gets NaN in the channels concerned (in tiles that a mask
- * cuts, in all channels); other queries are not touched by it (beyond the rounding of their own sums).
+ * any bits. A query that sees an infinity or NaN in V gets an infinity or NaN in the channels concerned (in tiles of 128
+ * keys that a mask cuts for it or for a query worked on with it, NaN in all channels; which of the two an infinity
+ * gives depends on its weight and on the number of queries); other queries are not touched by it (beyond the rounding
+ * of their own sums).
  * Scores and sums are fp32 (exact products, fp32 accumulation; the cap within 2^-20 of its size, distances exact to
- * 2^24); the probabilities enter the product with V rounded to the input type. Results do not depend on what else
- * runs, and repeat bit for bit.
+ * 2^24); the probabilities enter the product with V rounded to the input type, whatever out_dtype is. Results do not
+ * depend on what else runs, and repeat bit for bit.
  *   q, k, v, out  views; 16-byte aligned data, strides multiples of 16 bytes. k and v may have a zero batch or head
  *                 stride (one set of keys for several)
  *   spans     int32 [batch][tq][2] from mikv_mask_spans, or NULL (then `causal` decides); lo < 0 counts as 0 and
@@ -477,7 +480,9 @@ typedef struct {
  * its requests and their query heads. groups = batch gives each request keys of its own (a plain bf16 / fp16
  * cache); groups = 1 one prefix for all. Scores as in mikv_prompt_attention with p = q_pos[b].
  * With own_out and own_ml the result is joined with attention over other keys of the same query, as
- * mikv_decode_attention leaves it for the request's own cache (fp32 output, (max, sum)): the softmax runs over both.
+ * mikv_decode_attention leaves it for the request's own cache (fp32 output, (max, sum)): the softmax runs over both. Own
+ * parts have to come from scores of the same form: mikv_decode_attention has neither cap nor bias, so with those the own
+ * part is another call's (this one's, with groups = batch, over a 16-bit cache of the request).
  *   q         [batch][heads_q][d] dense, 16-byte aligned
  *   k, v      views [groups][heads_kv][length][d] as in mikv_prompt_attention
  *   lens      int32 [groups] (device) or NULL: keys of each prefix, 0 <= lens <= length; later rows may hold any bits

@@ -32,8 +32,9 @@
 // Barriers. Every role that waits on a barrier sees each of its phases in order (a wait that left phases out would
 // take an earlier one of the same parity for its own); counters run on from item to item.
 //
-// Softmax. Weights are 2^(x - r) with x the score in log2 units and r a reference of the row: the largest x of the
-// first tile the row sees (less kRefDrop), moved only when a tile's sum of weights passes kSumMax, which rescales O. The
+// Softmax. Weights are 2^(x - r) with x the score in log2 units and r a reference of the row: the largest x of 32 columns
+// of its first tile, or of what it sees there where a mask cuts it (less ref_drop), moved only when a sum of weights
+// passes sum_max, which rescales O. The
 // weights' 16-bit types hold that range without loss of relative precision, so most tiles need no maximum at all. Key
 // tiles are visited from the last to the first: with a causal mask or a distance bias the largest scores then
 // tend to come first. Sums are fp32 over the unrounded weights; rounding the weights to 16 bits is what the tensor
@@ -42,7 +43,9 @@
 // Masks. Every row sees one span of keys [lo, hi). Tiles outside the union of an item's spans are not visited; tiles
 // inside every span are not masked. In the tiles between, a weight of 0 does not stop an infinity or NaN in V from
 // entering O (0 * inf), so the guard warp looks through the V tile first: rows with such a value are set to 0 and
-// their keys reported to the softmax threads, which mark the output rows that do see them.
+// their keys reported to the softmax threads, which mark the output rows that do see them. In tiles that no mask cuts an
+// infinity reaches the rows as the products give it: infinite, or NaN where its weight rounds to 0 (as in kFew, whose
+// copies weigh three quarters of the keys by 0).
 //
 // Bounds. Two row tiles take at least 2068 clocks of the tensor cores per key tile (4 x 128^3 at 517 each, measured alone)
 // and about 2900 in the kernel: what is left is the chain of one stream (scores -> softmax, about 1200 clocks -> product

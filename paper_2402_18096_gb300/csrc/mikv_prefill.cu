@@ -293,7 +293,8 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_rows_kernel(const __gri
 }
 
 // Normalisers that are given, in place of pass 1: log2 units, +inf (weighs nothing) for padding queries and for queries
-// without a finite sum. Bound by its launch: 8 bytes per query, beside pass 2's 256 bytes of each query row.
+// without a finite sum. Bound by its launch: 8 bytes per query, beside pass 2's 256 bytes of each query row. Both kernels
+// take 683 us where the two passes take 1239 (2 x 8192 tokens, 32 / 8 heads), 71 and 154 for 32 x 512.
 __global__ void __launch_bounds__(256) prefill_given_kernel(float* stats, const float* lse, int rows, int T, int T_pad) {
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= (size_t)rows * T_pad) return;

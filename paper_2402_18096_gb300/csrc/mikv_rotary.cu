@@ -1,8 +1,9 @@
 // mikv_rotary.cu — rotary positions and the visible-key spans of a prompt (sm_103a).
 //
 // Rotary: a pair of channels (x, x') of a token at position p turns by a = 2 pi p f (f: turns per position). The
-// product p f is formed modulo one turn in 64-bit integer arithmetic (f as a 64-bit fraction), so its error stays
-// below 2^-32 turns at any position, where a 32-bit float product would lose 2^-24 of the whole angle.
+// product p f is formed modulo one turn in 64-bit integer arithmetic (f as a 64-bit fraction), where a 32-bit float
+// product would lose 2^-24 of the whole angle. The angle is off by at most |p| 2^-55 turns (the fraction comes from doubles:
+// frequencies up to 1 radian per position), 2^-32 (the bits kept) and 2^-26 (their rounding to fp32).
 // Bound by HBM: every element is read and written once. A block takes a few tokens of some heads, at most four 32-byte
 // items to a thread: the loads are issued first, the cosines and sines of the block's tokens are computed while
 // they are under way (once, in shared memory, for all heads), then everything is turned and written.
@@ -132,7 +133,10 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
   }
 }
 
-// Any alignment, strides and number of turning channels: a pair or a copied channel at a time.
+// Any alignment, strides and number of turning channels: a pair or a copied channel at a time. Bound by instructions (two
+// divisions and two 2- or 4-byte accesses each way per pair): 8192 tokens of 40 heads in rows of 131 elements take 124 us
+// in bf16 (1.4 TB/s, 20 % of a copy) and 132 in fp32 (38 %), with 10 turning channels 197 and 218; aligned 27 and 51 us in
+// rotary_kernel. Whole models have aligned rows; this form is there so that no view is refused.
 template <typename T, bool HALF>
 __global__ void __launch_bounds__(kRotThreads) rotary_elements_kernel(const __grid_constant__ RotaryArgs a, int log_tok) {
   extern __shared__ float2 s_cs[];
@@ -166,9 +170,11 @@ __global__ void __launch_bounds__(kRotThreads) rotary_elements_kernel(const __gr
 
 template <typename T>
 cudaError_t launch_rotary_t(const RotaryArgs& a, int layout, bool vec, cudaStream_t st) {
-  // Eight tokens to a block write each head's rows 2 KB at a time: 32768 tokens of 32 + 8 bf16 heads take 101 us (6.6 TB/s,
-  // 98 % of a copy), 106 with four tokens, 144 with one (which also computes each angle for fewer heads). Few tokens are
-  // spread over more blocks instead.
+  // Eight tokens to a block write each head's rows 2 KB at a time: 32768 tokens of 32 + 8 bf16 heads take 97 us in a graph (104
+  // call by call, 95 % of a copy), 100 with two or four tokens, 135 with one (which also computes each angle for fewer
+  // heads). Few tokens are spread over more blocks instead (one / eight tokens to a block): 128 tokens of 32 + 8 bf16 heads
+  // 2.0 / 2.7 us, of 40 + 40 fp32 heads 2.8 / 3.4; 2048 tokens 11.0 / 9.1 and 25.8 / 26.6. Between, 512 and 1024 tokens of
+  // 32 + 8 bf16 heads would gain from eight (4.4 / 3.6, 7.0 / 5.6), fp32 would lose (4.9 / 5.8, 8.1 / 8.1).
   const int log_tok = a.tokens >= 8 && (long long)a.batch * a.tokens >= 2048 ? 3 : 0, tok = 1 << log_tok;
   const int blocks = (a.tokens + tok - 1) / tok;
   const size_t smem = (size_t)tok * (a.rot / 2) * sizeof(float2);
