@@ -126,10 +126,12 @@ class SharedPrefixLayer:
         Hq, P, dev = q.shape[1], k0.shape[2], k.device
         mikv_rotary(table, q0, k0)
         mikv_rotary(table, q, k, start=P)
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
         rows = q.transpose(1, 2).contiguous().view(B * T, Hq, d)  # every own token a request of the prefix
         ws = workspace(max(mikv_prompt_workspace_bytes(q0, k0), mikv_prompt_workspace_bytes(q, k),
                            mikv_prefix_workspace_bytes(rows, k0), mikv_workspace_bytes(shape, WS_PREFILL, T)), dev)
-        mikv_prompt_attention(q0, k0, v0, out_prefix, ws)
+        if P > 0:
+            mikv_prompt_attention(q0, k0, v0, out_prefix, ws)
         # the own tokens over their own keys, joined with their attention over the prefix as it lies
         own_out = torch.empty(B, T, Hq, d, dtype=torch.float32, device=dev)
         lse = torch.empty(B, Hq, T, dtype=torch.float32, device=dev)
@@ -145,7 +147,6 @@ class SharedPrefixLayer:
             out_own.copy_(joined.transpose(1, 2))
         lse.copy_(ml[:, :, 0].view(B, T, Hq).transpose(1, 2))
         del rows, own_out, own_ml, joined
-        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
         scores = torch.empty(B, Hkv, T, dtype=torch.float32, device=dev)
         mikv_prefill_scores(shape, q, k, scores, ws, lse=lse)
         layer = MixedPrecisionLayer.from_prefill(shape, k, v, scores, q, device=dev)

@@ -154,6 +154,29 @@ def test_prompt_outputs_in_either_layout(major):
             assert bool(((out1[b, h].double() - o).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("P", [0, 1, 129])
+def test_short_prefixes_and_rows_of_any_alignment(P):
+    """Prefixes of no and of one token; own rows that start and step at odd elements."""
+    B, Hq, Hkv, T = 2, 4, 2, 33
+    g = torch.Generator(device="cuda").manual_seed(11)
+    table = pkg.RotaryTable()
+    q0, k0, v0 = (make(g, 1, h, P, 128) for h in (Hq, Hkv, Hkv))
+    q, k, v = (make(g, B, h, T, 131)[..., 1:129] for h in (Hq, Hkv, Hkv))
+    out0, out1 = torch.empty_like(q0), torch.full((B, Hq, T, 128), math.nan, dtype=torch.bfloat16, device="cuda")
+    layer = SharedPrefixLayer.from_prompts(pkg.shape_for_context(B, Hq, Hkv, 2, 32, T, 1.0, 2), table, (q0, k0, v0),
+                                           (q, k, v), out0, out1)
+    mask = torch.arange(P + T, device="cuda") <= P + torch.arange(T, device="cuda")[:, None]
+    for b in range(B):
+        for h in range(Hq):
+            keys, vals = torch.cat([k0[0, h // 2], k[b, h // 2]]), torch.cat([v0[0, h // 2], v[b, h // 2]])
+            o, _, bound, _ = ref.attention(q[b, h], keys, vals, mask, SCALE)
+            assert bool(((out1[b, h].double() - o).abs() <= bound).all())
+    out = torch.empty(B, Hq, 128, device="cuda")
+    layer.step(*(make(g, B, h, 128) for h in (Hq, Hkv, Hkv)), out)
+    layer.check()
+    assert bool(torch.isfinite(out).all()) and layer.prefix == P
+
+
 @pytest.mark.parametrize("call,at", [(None, 0), ("mikv_prompt_attention", 4), ("mikv_prefix_attention", 4),
                                      ("mikv_prefill_scores", 4)])
 def test_check_reports_failures_of_the_prompts(monkeypatch, call, at):
