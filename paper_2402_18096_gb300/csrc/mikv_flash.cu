@@ -264,8 +264,8 @@ cudaError_t launch_flash(const FlashArgs& a, bool f16, bool out_f32, void* ws, i
   MergePartsArgs m = {a, p.part_table, p.part_o, p.part_lse, a.batch * a.tq * a.heads_q, plan.m_blocks, 0, p.log2_G, out_f32 ? 2 : f16 ? 1 : 0};
   while ((1 << m.log2_item_rows) < plan.item_rows) ++m.log2_item_rows;
   // Four warps to a row where parts are many and rows few (one warp / four warps, whole call): 4 rows of 32 parts 14.7 /
-  // 12.0 us, 1024 rows of 16 parts 33.9 / 32.1, 2048 rows of 19 parts 44.1 / 42.4; but 3072 rows of 9 parts 57.0 / 58.6,
-  // 4096 rows 60.9 / 64.3, and 128 rows of 5 parts 44.8 / 46.0.
+  // 12.0 us, 1024 rows of 16 parts 33.9 / 32.1, 2048 rows of 19 parts 44.1 / 42.4; but 4096 rows of 9 parts 60.9 / 64.3,
+  // and 240 rows of 4 parts 44.8 / 46.0.
   if (p.shares > 8 * base && m.rows <= 2048)
     return launch_chained(merge_parts_kernel<4>, dim3(m.rows), dim3(128), 0, st, m);
   return launch_chained(merge_parts_kernel<1>, dim3((m.rows + 3) / 4), dim3(128), 0, st, m);
