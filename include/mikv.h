@@ -500,6 +500,126 @@ mikv_status mikv_prefix_attention(const mikv_prefix_desc* desc, const void* q, c
                                   const float* slopes, const float* own_out, const float* own_ml, void* out,
                                   float* ml, void* workspace, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------ drafted tokens: trees, commits, copies of requests
+ *
+ * Several tokens of a request at once (speculative decoding): a tree of drafted tokens attends the request's
+ * mixed-precision cache and, among the drafted tokens, its own ancestors; the accepted path then enters the cache.
+ * Requests of one cache may hold different numbers of tokens. These entry points take caches with a bf16 important set
+ * (hi_bits 0 or 16) and per-token retained keys (k_channel_group 0), or none (bits 0); mikv_copy_requests takes all. */
+
+/* What each request of a cache holds (device arrays, any of them may be NULL). The slots [0, n_hi[b]) of its important
+ * arrays are in use, slots[b][h] of them free (the slot that mikv_decode_step leaves for the next token); retained rows
+ * [0, n_lo[b]) are in use. A request with n_hi[b] = n_lo[b] = 0 holds nothing. Kernels take n_hi[b] within
+ * [0, hi_cap] and n_lo[b] within [0, n_lo_max]; a free slot outside [0, n_hi[b]) is no slot. Slots and rows that are not
+ * in use may hold any bits. */
+typedef struct {
+  int32_t* n_hi;     /* int32 [B], or NULL: hi_cap slots of every request */
+  int32_t* n_lo;     /* int32 [B], or NULL: n_lo_max rows of every request */
+  int32_t* slots;    /* int32 [B][Hkv], or NULL: no slot in use is free */
+  int32_t n_lo_max;  /* most retained rows of any request, <= lo_cap (on the host) */
+} mikv_lengths;
+
+/* Drafted tokens of a request at most (one tile of keys, four words of a mask). */
+#define MIKV_TREE_NODES 128
+
+/*
+ * Trees of drafted tokens: what each one sees of the others, and where it stands.
+ *   parents    int32 [batch][nodes] (device): the node before it, 0 <= parents[b][i] < i, or -1: it follows the cached
+ *              tokens. Any other value, and a parent that is itself none, makes i no node (padding)
+ *   masks      uint32 [batch][nodes][4] (device): bit j of node i's 128 bits: j is i or one of its ancestors; 0 for padding
+ *   positions  int32 [batch][nodes] (device) or NULL: first[b] (or `start` where first is NULL) plus the number of i's
+ *              ancestors; padding gets first[b]. For mikv_rotary
+ *   first      int32 [batch] (device) or NULL
+ * One launch; the result serves every layer. 1 <= nodes <= MIKV_TREE_NODES.
+ */
+mikv_status mikv_tree_masks(uint32_t* masks, int32_t* positions, const int32_t* parents, int32_t batch, int32_t nodes,
+                            const int32_t* first, int32_t start, void* stream);
+
+typedef struct {
+  int32_t nodes;     /* N, drafted tokens per request, 1 .. MIKV_TREE_NODES */
+  int32_t out_dtype; /* MIKV_BF16 or MIKV_F32 */
+  float sm_scale;    /* > 0 */
+} mikv_tree_desc;
+
+/*
+ * Attention of drafted tokens over the mixed-precision cache and their ancestors. For node i of request b, query head j,
+ * KV head h = j div G:
+ *   x_s = sm_scale * q . k_hi[s]                     important slots s in use and not free
+ *   x_t = sm_scale * (q / balancer) . k_hat[t]       retained rows t < n_lo[b], k_hat = alpha * code + beta
+ *   x_m = sm_scale * q . k[m]                        nodes m in i's mask (itself among them)
+ *   out = sum softmax(x) v (v_hat = alpha * code + beta for retained rows),  lse = ln sum exp(x)
+ * A padding node (mask without its own bit) gives out = 0 and lse = -inf, and its key and value may hold any bits. Scores
+ * and sums are fp32. Retained values (alpha * code + beta) enter the product rounded to fp16, as do retained keys divided
+ * by the balancer, alpha * code / b + beta / b, whose magnitude has to stay below 65504; the probabilities enter
+ * rounded to fp16 (retained) or bf16 (important slots, nodes), whatever out_dtype is. Queries are taken exactly, in fp16
+ * after a power of two per row: elements below 2^-24 of a row's largest are lost. A node whose value holds an infinity
+ * or NaN gives NaN in all channels to the nodes that see it, and touches no other; in the cache such values reach all
+ * nodes of the request. Results do not depend on what else runs, and repeat bit for bit.
+ *   masks      uint32 [B][N][4], 16-byte aligned
+ *   q, out     views [B][Hq][N][d];  k, v  views [B][Hkv][N][d] (bf16; 16-byte aligned data and strides; out of out_dtype)
+ *   lens       what the requests hold, or NULL: hi_cap slots and no retained rows
+ *   lse        fp32 [B][Hq][N] or NULL
+ *   workspace  >= mikv_tree_workspace_bytes(shape, nodes) bytes, 256-byte aligned, status word as above
+ */
+size_t mikv_tree_workspace_bytes(const mikv_shape* shape, int32_t nodes);
+mikv_status mikv_tree_attention(const mikv_shape* shape, const mikv_cache* cache, const mikv_tree_desc* desc,
+                                const uint32_t* masks, const mikv_view* q, const mikv_view* k, const mikv_view* v,
+                                const mikv_view* out, const mikv_lengths* lens, float* lse, void* workspace,
+                                size_t ws_bytes, void* stream);
+
+/*
+ * The importance that an accepted path hands out (the accumulated attention of mikv_update_importance, for its nodes'
+ * queries together). A path is its nodes from the root on: the entries of path[b] up to the first that is no node number
+ * in [0, nodes). With A of them accepted, p_0 .. p_(A-1):
+ *   acc[b][h][s] += sum over a < A and the G query heads j of KV head h of exp(x_s - lse[b][j][p_a])   slots in use, not free
+ *   gained[b][h][a] = sum over c = a .. A - 1 and the heads j of exp(sm_scale * q_(p_c) . k_(p_a) - lse[b][j][p_c])
+ * and gained = 0 from A on. A query whose lse is infinite weighs nothing. fp32 sums in a fixed order.
+ *   path    int32 [B][steps] (device), 1 <= steps <= MIKV_TREE_NODES
+ *   q, k    views [B][Hq][nodes][d], [B][Hkv][nodes][d] as in mikv_tree_attention;  lse  fp32 [B][Hq][nodes]
+ *   gained  fp32 [B][Hkv][steps]
+ */
+mikv_status mikv_path_importance(const mikv_shape* shape, const mikv_cache* cache, int32_t nodes, float sm_scale,
+                                 const int32_t* path, int32_t steps, const mikv_view* q, const mikv_view* k,
+                                 const float* lse, const mikv_lengths* lens, float* gained, void* stream);
+
+/*
+ * Entry of an accepted path into the cache: the A nodes of path[b] (as in mikv_path_importance), tokens first[b],
+ * first[b] + 1, ..., join the important set with the scores gained[b][h][a]. Where it then holds more than its budget
+ * (hi_cap, or hi_cap - 1 with `slots`: the free slot stays free), the surplus least important of all, by (score, id)
+ * ascending (ties: the slot first, then path order), are demoted: quantized as by mikv_quantize_pack into the retained rows n_lo[b],
+ * n_lo[b] + 1, ... in that order (bits 0: dropped). New tokens that stay take the slots of demoted ones in that order, then
+ * slots n_hi[b], n_hi[b] + 1, ....
+ *   k, v     views [B][Hkv][nodes][d]; first  int32 [B];  gained  fp32 [B][Hkv][steps] (no NaN)
+ *   lens     what the requests hold. A request with n_hi[b] = 0 is left alone
+ *   lens_out n_hi and n_lo after the commit (either or the struct may be NULL; may be those of lens; slots is not written)
+ *   next     int32 [B] or NULL: first[b] plus the tokens that entered; may be `first`
+ *   workspace >= mikv_commit_workspace_bytes(shape, steps) bytes, 256-byte aligned. A request whose retained rows would
+ *            pass lo_cap keeps its state and lengths, and mikv_workspace_check then gives MIKV_ERR_DEVICE; so does a KV head
+ *            whose free slot is no slot in use, which is left alone while the request's lengths go on.
+ */
+size_t mikv_commit_workspace_bytes(const mikv_shape* shape, int32_t steps);
+mikv_status mikv_commit_path(const mikv_shape* shape, const mikv_cache* cache, int32_t nodes, const int32_t* path,
+                             int32_t steps, const mikv_view* k, const mikv_view* v, const float* gained,
+                             const int32_t* first, const mikv_lengths* lens, const mikv_lengths* lens_out,
+                             int32_t* next, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Copies of whole requests (forks for several samples, compaction of a batch, growth into a larger cache): for every pair
+ * (from, to), row `to` of `to_cache` becomes what row `from` of `cache` holds: the slots in use and the retained rows in
+ * use with their codes, parameters, scores and ids (and, with per-channel keys, the staged rows), n_hi, n_lo and
+ * slots where both lengths have them. What lies behind stays as it was.
+ *   pairs     int32 [n][2] on the HOST (read before the call returns). 0 <= n; rows of the two batches; no row is the
+ *             target of two pairs, and in one cache (to_cache->k_hi == cache->k_hi) none is source and target:
+ *             MIKV_ERR_ARG
+ *   shapes    equal heads, dimensions and precisions; to_shape->hi_cap >= shape->hi_cap (equal where k_channel_group is
+ *             set or hi_cap slots are in use without n_hi) and to_shape->lo_cap >= lens->n_lo_max: MIKV_ERR_CAPACITY. All
+ *             arrays 16-byte aligned
+ *   lens, to_lens  as above; to_lens may be NULL. The balancer is the layer's, not copied
+ */
+mikv_status mikv_copy_requests(const mikv_shape* shape, const mikv_cache* cache, const mikv_shape* to_shape,
+                               const mikv_cache* to_cache, const int32_t* pairs, int32_t n, const mikv_lengths* lens,
+                               const mikv_lengths* to_lens, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

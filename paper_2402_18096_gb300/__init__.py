@@ -26,6 +26,8 @@ __all__ = [
     "mikv_budget", "shape_for_context", "mikv_debug_check", "debug_build",
     "RotaryTable", "mikv_rotary_phases", "mikv_rotary", "mikv_mask_spans", "mikv_prompt_workspace_bytes",
     "mikv_prompt_attention", "mikv_prefix_workspace_bytes", "mikv_prefix_attention",
+    "Lengths", "TREE_NODES", "mikv_tree_masks", "mikv_tree_workspace_bytes", "mikv_tree_attention",
+    "mikv_path_importance", "mikv_commit_workspace_bytes", "mikv_commit_path", "mikv_copy_requests",
     "WS_ATTENTION", "WS_BALANCER", "WS_STEP", "WS_PREFILL", "OUT_BF16", "OUT_F32", "HEAD_DIM",
 ]
 
@@ -65,6 +67,14 @@ class _RotaryDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("dtype", "batch", "tokens", "heads_q", "heads_k", "head_dim", "rot", "layout", "inverse")]
     _fields_ += [("amplitude", ctypes.c_float)]
+
+
+class _Lengths(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("n_hi", "n_lo", "slots")] + [("n_lo_max", ctypes.c_int32)]
+
+
+class _TreeDesc(ctypes.Structure):
+    _fields_ = [("nodes", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("sm_scale", ctypes.c_float)]
 
 
 class _PromptDesc(ctypes.Structure):
@@ -130,6 +140,13 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
                 "mikv_prompt_attention": (I, [P, P, P, P, P, P, P, P, P, Z, P]),
                 "mikv_prefix_workspace_bytes": (Z, [P]),
                 "mikv_prefix_attention": (I, [P, P, P, P, P, P, P, P, P, P, P, P, Z, P]),
+                "mikv_tree_masks": (I, [P, P, P, I, I, P, I, P]),
+                "mikv_tree_workspace_bytes": (Z, [P, I]),
+                "mikv_tree_attention": (I, [P, P, P, P, P, P, P, P, P, P, P, Z, P]),
+                "mikv_path_importance": (I, [P, P, I, F, P, I, P, P, P, P, P, P]),
+                "mikv_commit_workspace_bytes": (Z, [P, I]),
+                "mikv_commit_path": (I, [P, P, I, P, I, P, P, P, P, P, P, P, P, Z, P]),
+                "mikv_copy_requests": (I, [P, P, P, P, P, I, P, P, P]),
             }
             for name, (res, args) in sig.items():
                 fn = getattr(lib, name)
@@ -230,6 +247,35 @@ class LayerCache:
         self.lo_tok = torch.zeros(B, H, s.lo_cap, dtype=torch.int32, **z)
         self.balancer = balancer
         self.n_lo = 0
+
+    @classmethod
+    def of(cls, shape: Shape, k_hi, v_hi, hi_tok, acc, k_codes=None, v_codes=None, k_params=None, v_params=None,
+           lo_tok=None, balancer=None, k_hi_params=None, v_hi_params=None) -> "LayerCache":
+        """A cache around arrays that the caller owns (layouts of mikv_cache; the retained arrays may be None with
+        bits = 0)."""
+        s, d = shape, shape.head_dim
+        hi, lo = (s.batch, s.heads_kv, s.hi_stride), (s.batch, s.heads_kv, s.lo_cap)
+        hi_row = ((16 * s.hi_bits,), torch.uint8) if s.hi_coded else ((d,), torch.bfloat16)
+        par = (d // s.group, 2) if s.bits else (0, 2)
+        key_par = (*lo[:2], s.lo_cap // s.k_channel_group, d, 2) if s.k_channel_group else (*lo, *par)
+        want = {"k_hi": (k_hi, (*hi, *hi_row[0]), hi_row[1]), "v_hi": (v_hi, (*hi, *hi_row[0]), hi_row[1]),
+                "hi_tok": (hi_tok, hi, torch.int32), "acc": (acc, hi, torch.float32),
+                "k_codes": (k_codes, (*lo, 16 * s.bits), torch.uint8), "v_codes": (v_codes, (*lo, 16 * s.bits), torch.uint8),
+                "k_params": (k_params, key_par, torch.float16), "v_params": (v_params, (*lo, *par), torch.float16),
+                "lo_tok": (lo_tok, lo, torch.int32), "balancer": (balancer, (s.heads_kv, d), torch.float32),
+                "k_hi_params": (k_hi_params, (*hi, d // s.hi_group, 2), torch.float16),
+                "v_hi_params": (v_hi_params, (*hi, d // s.hi_group, 2), torch.float16)}
+        optional = {"balancer"} | (set() if s.bits else {"k_codes", "v_codes", "k_params", "v_params", "lo_tok"}) | \
+            (set() if s.hi_coded else {"k_hi_params", "v_hi_params"})
+        self = cls.__new__(cls)
+        self.shape, self.n_lo = shape, 0
+        for name, (t, dims, dtype) in want.items():
+            if t is None and name not in optional:
+                raise ValueError(f"LayerCache: {name} is missing")
+            if t is not None and (t.shape != dims or t.dtype != dtype or not t.is_contiguous()):
+                raise ValueError(f"{name}: expected dense {dtype} {dims}, got {t.dtype} {tuple(t.shape)}")
+            setattr(self, name, t)
+        return self
 
     def c(self) -> _Cache:
         return _Cache(*[_ptr(getattr(self, n)) for n in
@@ -384,3 +430,5 @@ def mikv_retained_row_bytes(bits: int, group: int, head_dim: int = HEAD_DIM) -> 
 from .prompt import (RotaryTable, mikv_mask_spans, mikv_prefix_attention,  # noqa: E402
                      mikv_prefix_workspace_bytes, mikv_prompt_attention, mikv_prompt_workspace_bytes, mikv_rotary,
                      mikv_rotary_phases)
+from .tree import (Lengths, TREE_NODES, mikv_commit_path, mikv_commit_workspace_bytes, mikv_copy_requests,  # noqa: E402
+                   mikv_path_importance, mikv_tree_attention, mikv_tree_masks, mikv_tree_workspace_bytes)

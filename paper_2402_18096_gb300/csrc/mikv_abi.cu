@@ -9,6 +9,7 @@
 
 #include <mutex>
 
+#include "mikv_checks.h"
 #include "mikv_device.cuh"
 #include "mikv_internal.h"
 #include "mikv_nvtx.h"
@@ -30,50 +31,11 @@ int* mikv::debug_status_word() { return nullptr; }
 
 namespace {
 
-mikv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MIKV_OK : MIKV_ERR_CUDA; }
-
 int num_sms() {
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 148;
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
   return n;
-}
-
-bool shape_ok(const mikv_shape* s) {
-  return s && s->batch > 0 && s->heads_q > 0 && s->heads_kv > 0 && s->heads_q % s->heads_kv == 0 &&
-         s->head_dim > 0 && s->bits >= 0 && (s->bits == 0 || s->group > 0) && s->hi_cap >= 0 &&
-         s->hi_stride >= s->hi_cap &&
-         s->hi_stride % 16 == 0 && s->lo_cap >= 0 && s->lo_cap % 16 == 0;
-}
-
-mikv_status shape_supported(const mikv_shape* s) {
-  if (!shape_ok(s)) return MIKV_ERR_ARG;
-  const int G = s->heads_q / s->heads_kv;
-  if (s->head_dim != kHeadDim) return MIKV_ERR_UNSUPPORTED;
-  if (s->bits != 0) {  // bits == 0: eviction, no retained set (its group is ignored)
-    if (s->bits < 2 || s->bits > 4) return MIKV_ERR_UNSUPPORTED;
-    if (s->group != 32 && s->group != 64 && s->group != 128) return MIKV_ERR_UNSUPPORTED;
-  }
-  if (G != 1 && G != 2 && G != 4 && G != 8) return MIKV_ERR_UNSUPPORTED;
-  const int hb = s->hi_bits;
-  if (hb != 0 && hb != 16 && hb != 8 && hb != 4 && hb != 2) return MIKV_ERR_UNSUPPORTED;
-  if (hb != 0 && hb != 16 && s->hi_group != kHiGroup) return MIKV_ERR_UNSUPPORTED;
-  if (s->k_channel_group != 0) {  // per-channel retained keys (App. C)
-    if (s->k_channel_group != kKchGroup || (hb != 0 && hb != 16) || s->bits == 0) return MIKV_ERR_UNSUPPORTED;
-    if (s->hi_stride < s->hi_cap + kKchGroup || s->lo_cap % kKchGroup) return MIKV_ERR_ARG;
-  }
-  return MIKV_OK;
-}
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-// The cache's arrays exist (and, for a coded important set, so do its parameter arrays, 16-byte aligned).
-bool cache_ok(const mikv_cache* c, const mikv_shape* s) {
-  if (!(c && c->k_hi && c->v_hi && c->hi_tok && c->acc)) return false;
-  if (!evicting(*s) && !(c->k_codes && c->v_codes && c->k_params && c->v_params && c->lo_tok)) return false;
-  if (hi_bits_of(*s) != 16)
-    return c->k_hi_params && c->v_hi_params && aligned(c->k_hi_params, 16) && aligned(c->v_hi_params, 16);
-  return true;
 }
 
 // ------------------------------------------------------------------ tensor maps

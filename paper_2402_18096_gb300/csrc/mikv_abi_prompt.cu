@@ -8,6 +8,7 @@
 #include <atomic>
 
 #include "../../include/mikv.h"
+#include "mikv_checks.h"
 #include "mikv_flash.h"
 #include "mikv_nvtx.h"
 #include "mikv_rotary.h"
@@ -15,8 +16,6 @@
 using namespace mikv;
 
 namespace {
-
-mikv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MIKV_OK : MIKV_ERR_CUDA; }
 
 // SMs of the current device (asked once per device).
 int num_sms() {
@@ -28,37 +27,6 @@ int num_sms() {
   if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
   return n;
 }
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-int elem_bytes(int dtype) { return dtype == MIKV_F32 ? 4 : 2; }
-
-constexpr int64_t kStrideMax = (int64_t)1 << 38;  // elements: a byte stride then fits a tensor map's 40 bits
-
-// Strides of the dimensions that are there lie in [least, kStrideMax); unused ones become 0.
-bool strides_of(const mikv_view* x, int64_t batch, int64_t heads, int64_t tokens, int64_t least, long long (&s)[3]) {
-  const int64_t n[3] = {batch, heads, tokens}, st[3] = {x->stride_batch, x->stride_head, x->stride_token};
-  for (int i = 0; i < 3; ++i) {
-    s[i] = n[i] == 1 ? 0 : st[i];
-    if (n[i] != 1 && (st[i] < least || st[i] >= kStrideMax)) return false;
-  }
-  return true;
-}
-
-// Attention operands: 16-byte aligned data and strides; a zero batch or head stride only where `shared` allows it.
-mikv_status attn_view(const mikv_view* x, int64_t batch, int64_t heads, int64_t tokens, int bytes, bool shared,
-                      long long (&s)[3]) {
-  if (!x || !x->data || !aligned(x->data, 16)) return MIKV_ERR_ARG;
-  if (!strides_of(x, batch, heads, tokens, 0, s)) return MIKV_ERR_ARG;
-  const int64_t n[3] = {batch, heads, tokens};
-  for (int i = 0; i < 3; ++i) {
-    if (s[i] * bytes % 16) return MIKV_ERR_ARG;
-    if (n[i] != 1 && s[i] == 0 && !(shared && i < 2)) return MIKV_ERR_ARG;
-  }
-  return MIKV_OK;
-}
-
-bool positive(float x) { return x > 0.f && x <= 3.402823466e38f; }
 
 mikv_status attn_common(int32_t dtype, int32_t out_dtype, int32_t batch, int32_t heads_q, int32_t heads_kv,
                         int32_t head_dim, int32_t tq, int32_t tk, float sm_scale, float softcap) {

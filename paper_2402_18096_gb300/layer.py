@@ -9,6 +9,8 @@ This is the flow a serving stack runs around the library (Fig. 4 of arxiv 2402.1
   decode   -> per token: insert, attend, update importance, demote the least important (mikv_decode_step)
 Requests that share a long prompt prefix keep it once, in bf16, beside a mixed-precision cache of their own tokens
 (SharedPrefixLayer): rotary positions, prompt attention, and decode steps whose attention joins both.
+Requests that decode several drafted tokens at a time, each request at its own length (DraftedLayer): the tree's attention over
+cache and ancestors, the accepted path's entry into the cache, copies of requests for several samples.
 Every step runs in the library's kernels; this module only orders the calls and owns the buffers.
 """
 from __future__ import annotations
@@ -17,11 +19,11 @@ import math
 
 import torch
 
-from . import (LayerCache, MikvError, RotaryTable, Shape, WS_ATTENTION, WS_BALANCER, WS_PREFILL, WS_STEP, mikv_compute_balancer,
-               mikv_decode_attention, mikv_decode_step, mikv_gather_hi, mikv_insert_token,
-               mikv_prefill_scores, mikv_prefix_attention, mikv_prefix_workspace_bytes, mikv_prompt_attention,
-               mikv_prompt_workspace_bytes, mikv_quantize_pack, mikv_rotary, mikv_select_demote,
-               mikv_update_importance, mikv_workspace_bytes, mikv_workspace_check)
+from . import (LayerCache, Lengths, MikvError, RotaryTable, Shape, WS_ATTENTION, WS_BALANCER, WS_PREFILL, WS_STEP, mikv_compute_balancer,
+               mikv_commit_path, mikv_commit_workspace_bytes, mikv_copy_requests, mikv_decode_attention, mikv_decode_step,
+               mikv_gather_hi, mikv_insert_token, mikv_path_importance, mikv_prefill_scores, mikv_prefix_attention, mikv_prefix_workspace_bytes, mikv_prompt_attention,
+               mikv_prompt_workspace_bytes, mikv_quantize_pack, mikv_rotary, mikv_select_demote, mikv_tree_attention,
+               mikv_tree_masks, mikv_tree_workspace_bytes, mikv_update_importance, mikv_workspace_bytes, mikv_workspace_check)
 
 
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:
@@ -186,6 +188,76 @@ class SharedPrefixLayer:
             o.n_lo += 1
         o.slots.copy_(self.demoted[:, :, 0])
         o.pos += 1
+
+
+class DraftedLayer:
+    """One layer whose requests decode trees of drafted tokens over their mixed-precision caches (bf16 important set), each
+    request at its own length. attend() runs a tree, commit() takes the accepted path into the cache."""
+
+    def __init__(self, cache: LayerCache, table: RotaryTable, nodes: int, steps: int, n_hi, n_lo, slots, tokens,
+                 n_lo_max: int = None):
+        """nodes, steps: most drafted and most accepted tokens of a step. n_hi, n_lo, tokens int32 [B] (slots in use,
+        retained rows, tokens so far) and slots int32 [B, Hkv] (the free slots) are kept and updated in place; n_lo_max
+        bounds n_lo."""
+        s, dev = cache.shape, cache.k_hi.device
+        self.cache, self.table, self.nodes, self.steps = cache, table, nodes, steps
+        self.lens, self.tokens = Lengths(n_hi, n_lo, slots), tokens
+        self.n_lo_max = int(n_lo.max()) if n_lo_max is None else n_lo_max
+        i = dict(dtype=torch.int32, device=dev)
+        self.masks = torch.empty(s.batch, nodes, 4, **i)
+        self.positions = torch.empty(s.batch, nodes, **i)
+        self.lse = torch.empty(s.batch, s.heads_q, nodes, dtype=torch.float32, device=dev)
+        self.gained = torch.empty(s.batch, s.heads_kv, steps, dtype=torch.float32, device=dev)
+        self.ws_tree = workspace(mikv_tree_workspace_bytes(s, nodes), dev)
+        self.ws_commit = workspace(mikv_commit_workspace_bytes(s, steps), dev)
+        self.drafted = None  # (q, k, v) of the tree attended last
+
+    @classmethod
+    def of(cls, layer: MixedPrecisionLayer, table: RotaryTable, nodes: int, steps: int) -> "DraftedLayer":
+        """Goes on from a layer whose requests have all come to the same length (its cache is taken over)."""
+        s, dev = layer.shape, layer.cache.k_hi.device
+        full = lambda x: torch.full((s.batch,), x, dtype=torch.int32, device=dev)  # noqa: E731
+        return cls(layer.cache, table, nodes, steps, full(s.hi_cap), full(layer.n_lo), layer.slots, full(layer.pos),
+                   layer.n_lo)
+
+    def attend(self, q, k, v, parents, out):
+        """Attention of drafted tokens as projected: q [B, Hq, nodes, d] and k, v [B, Hkv, nodes, d] (views; q and k are turned
+        in place) with parents int32 [B, nodes], into out [B, Hq, nodes, d]. The next commit() takes its path from them."""
+        mikv_tree_masks(self.masks, parents, positions=self.positions, first=self.tokens)
+        mikv_rotary(self.table, q, k, positions=self.positions)
+        mikv_tree_attention(self.cache, self.masks, q, k, v, out, self.ws_tree, lens=self.lens, lse=self.lse)
+        self.drafted = (q, k, v)
+
+    def commit(self, path):
+        """The accepted nodes path int32 [B, steps] (root first, -1 behind the last) of the tree attended last: they hand out
+        importance, enter the cache, and what it holds above its budget is demoted. A call that is refused has changed
+        nothing."""
+        if self.drafted is None:
+            raise ValueError("DraftedLayer.commit: no tree was attended since the last commit")
+        s = self.cache.shape
+        if s.bits and self.n_lo_max + self.steps > s.lo_cap:  # (the bound is of commits with every step accepted)
+            self.n_lo_max = int(self.lens.n_lo.max())
+            if self.n_lo_max + self.steps > s.lo_cap:
+                raise MikvError("DraftedLayer.commit", 3)  # MIKV_ERR_CAPACITY
+        q, k, v = self.drafted
+        mikv_path_importance(self.cache, path, q, k, self.lse, self.gained, lens=self.lens)
+        mikv_commit_path(self.cache, path, k, v, self.gained, self.tokens, self.ws_commit, lens=self.lens,
+                         lens_out=self.lens, next=self.tokens)
+        self.drafted = None
+        self.n_lo_max += self.steps if s.bits else 0
+
+    def fork(self, pairs):
+        """Requests copied to other rows of the batch, (from, to) each: their caches, lengths and tokens so far."""
+        mikv_copy_requests(self.cache, self.cache, pairs, lens=self.lens, to_lens=self.lens)
+        if pairs:
+            src, dst = torch.tensor(pairs, device=self.tokens.device).T
+            self.tokens[dst] = self.tokens[src]
+        self.drafted = None
+
+    def check(self, stream=None):
+        """Raise MikvError (MIKV_ERR_DEVICE) if a kernel of a tree or a commit so far gave up; synchronises."""
+        for ws in (self.ws_tree, self.ws_commit):
+            mikv_workspace_check(ws, stream)
 
 
 def oracle_eviction_attention(k, v, q, budget: int, sm_scale: float, out, device="cuda"):
