@@ -1,9 +1,11 @@
 // mikv_tree.cu — drafted tokens: what the nodes of a tree see of one another, and their attention over the
 // mixed-precision cache.
 #include <math.h>
+#include <string.h>
 
-#include "mikv_quant_rows.cuh"
-#include "mikv_tree.h"
+#include <mutex>
+
+#include "mikv_tree_kernel.cuh"
 
 namespace mikv {
 namespace {
@@ -38,101 +40,116 @@ __global__ void __launch_bounds__(kTreeNodes) tree_masks_kernel(uint4* masks, in
   if (positions) positions[(size_t)b * nodes + i] = (first ? first[b] : start) + max(depth, 0);
 }
 
-// The code of channel c in a packed row.
-__device__ __forceinline__ int code_at(const uint8_t* row, int bits, int c) {
-  const uint16_t* units = reinterpret_cast<const uint16_t*>(row);
-  int unit, bit;
-  field_pos(c, bits == 3 ? 2 : bits, unit, bit);
-  int code = (units[unit] >> bit) & (bits == 4 ? 15 : 3);
-  if (bits == 3) {
-    field_pos(c, 1, unit, bit);
-    code |= ((units[16 + unit] >> bit) & 1) << 2;
-  }
-  return code;
-}
+using tree::Runs;
+using tree::Tiles;
 
-__device__ __forceinline__ void bf16x4(const __nv_bfloat16* p, float (&x)[4]) {
-  const uint2 r = *reinterpret_cast<const uint2*>(p);
-  x[0] = __uint_as_float(r.x << 16);
-  x[1] = __uint_as_float(r.x & 0xffff0000u);
-  x[2] = __uint_as_float(r.y << 16);
-  x[3] = __uint_as_float(r.y & 0xffff0000u);
-}
+struct TreeMergeArgs {
+  TreeArgs a;
+  const long long* prefix;
+  const float *part_o, *part_lse;
+  int m_blocks, log2_G, item_rows, ctas;
+};
 
-// One block per (node, query head, request), a key to a warp at a time, all in fp32.
-__global__ void __launch_bounds__(128) tree_rows_kernel(const TreeArgs a) {
-  __shared__ float s_o[4][kHeadDim], s_m[4], s_l[4];
-  __shared__ int s_bad;
-  const int node = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int h = hq / a.G, bh = b * a.heads_kv + h;
-  const uint4 mw = a.masks[(size_t)b * a.nodes + node];
-  const uint32_t mask[4] = {mw.x, mw.y, mw.z, mw.w};
-  const bool real = mask[node >> 5] >> (node & 31) & 1;
-  const int n_hi = a.held.hi(b), n_lo = a.held.lo(b), free_slot = a.held.free_slot(bh, n_hi);
-  float q[4], qb[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  bf16x4(static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + hq * a.q.h + node * a.q.t + 4 * lane, q);
+// The parts of an output row, weighted by 2^(lse - largest): a warp to a row. Rows whose item one CTA had are written.
+__global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__ TreeMergeArgs m) {
+  const TreeArgs& a = m.a;
+  const int lane = threadIdx.x & 31;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);  // (request * nodes + node) * heads_q + head
+  grid_dependency_wait();
+  const long long bn = row / a.heads_q;
+  const int head = (int)(row - bn * a.heads_q), b = (int)(bn / a.nodes), node = (int)(bn - (long long)b * a.nodes);
+  if (b >= a.batch) return;
+  const int h = head >> m.log2_G, in_head = (node << m.log2_G) + (head & (a.G - 1));
+  const int block = in_head / m.item_rows, in_item = in_head - block * m.item_rows;
+  const Tiles tl(a.held, b);
+  const Runs runs(m.prefix[a.batch], m.ctas);
+  const long long start = m.prefix[b] + (long long)(h * m.m_blocks + block) * tl.cost();
+  const int c0 = runs.owner(start), c1 = runs.owner(start + tl.before(tl.count() - 1));
+  if (c0 == c1) return;
+  float top = -INFINITY, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int first = c0; first <= c1; first += 32) {
+    const int c = first + lane;
+    const long long at = (long long)(2 * c + (c == c0)) * m.item_rows + in_item;
+    bool part = c <= c1;
+    if (part) part = tl.first(runs.first(c) - start) < tl.first(runs.first(c + 1) - start);
+    const float e = part ? m.part_lse[at] : -INFINITY;
+    float next = fmaxf(top, e);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) qb[e] = a.balancer ? q[e] / a.balancer[h * kHeadDim + 4 * lane + e] : q[e];
-  if (threadIdx.x == 0) s_bad = 0;
-  __syncthreads();
-  for (int t = warp; real && t < n_hi + n_lo + a.nodes; t += 4) {
-    float k[4], v[4];
-    const float* x = q;
-    if (t < n_hi) {
-      if (t == free_slot) continue;
-      const size_t row = ((size_t)bh * a.hi_stride + t) * kHeadDim + 4 * lane;
-      bf16x4(a.k_hi + row, k);
-      bf16x4(a.v_hi + row, v);
-    } else if (t < n_hi + n_lo) {
-      const size_t row = (size_t)bh * a.lo_cap + (t - n_hi);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = 4 * lane + e;
-        const float2 kp = __half22float2(a.k_params[row * (kHeadDim / a.group) + c / a.group]);
-        const float2 vp = __half22float2(a.v_params[row * (kHeadDim / a.group) + c / a.group]);
-        k[e] = fmaf(kp.x, (float)code_at(a.k_codes + row * 16 * a.bits, a.bits, c), kp.y);
-        v[e] = fmaf(vp.x, (float)code_at(a.v_codes + row * 16 * a.bits, a.bits, c), vp.y);
-      }
-      x = qb;
-    } else {
-      const int j = t - n_hi - n_lo;
-      if (!(mask[j >> 5] >> (j & 31) & 1)) continue;
-      bf16x4(static_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + h * a.k.h + j * a.k.t + 4 * lane, k);
-      bf16x4(static_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + h * a.v.h + j * a.v.t + 4 * lane, v);
-      if (!(isfinite(v[0]) && isfinite(v[1]) && isfinite(v[2]) && isfinite(v[3]))) s_bad = 1;
+    for (int o = 16; o > 0; o >>= 1) next = fmaxf(next, __shfl_xor_sync(0xffffffffu, next, o));
+    const float old = top == -INFINITY ? 0.f : fast_exp2(top - next);
+    sum *= old;
+    acc.x *= old, acc.y *= old, acc.z *= old, acc.w *= old;
+    top = next;
+    const float w = e == -INFINITY ? 0.f : fast_exp2(e - top);
+    uint32_t parts = __ballot_sync(0xffffffffu, part && e != -INFINITY);
+    while (parts) {
+      const int i = __ffs(parts) - 1;
+      parts &= parts - 1;
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      const float4 o = reinterpret_cast<const float4*>(m.part_o + ((long long)(2 * (first + i) + (first + i == c0)) * m.item_rows + in_item) * kHeadDim)[lane];
+      sum += wi;
+      acc.x = fmaf(o.x, wi, acc.x);
+      acc.y = fmaf(o.y, wi, acc.y);
+      acc.z = fmaf(o.z, wi, acc.z);
+      acc.w = fmaf(o.w, wi, acc.w);
     }
-    float s = x[0] * k[0] + x[1] * k[1] + x[2] * k[2] + x[3] * k[3];
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    s *= a.sm_scale;
-    const float top = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - top), w = s == -INFINITY ? 0.f : expf(s - top);
-    l = l * f + w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = o[e] * f + w * v[e];
-    m = top;
   }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) s_o[warp][4 * lane + e] = o[e];
-  if (lane == 0) s_m[warp] = m, s_l[warp] = l;
-  __syncthreads();
-  const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  float total = 0.f, y = 0.f;
-  const int c = threadIdx.x;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float f = s_m[i] == -INFINITY ? 0.f : expf(s_m[i] - top);
-    total += s_l[i] * f;
-    y += f == 0.f ? 0.f : s_o[i][c] * f;
-  }
-  y = !real ? 0.f : s_bad ? __int_as_float(0x7fffffff) : y / total;
-  const long long at = b * a.out.b + hq * a.out.h + node * a.out.t + c;
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  const long long to = b * a.out.b + head * a.out.h + node * a.out.t + 4 * lane;
   if (a.out_f32)
-    static_cast<float*>(a.out.p)[at] = y;
+    *reinterpret_cast<float4*>(static_cast<float*>(a.out.p) + to) = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
   else
-    static_cast<__nv_bfloat16*>(a.out.p)[at] = __float2bfloat16(y);
-  if (a.lse && c == 0)
-    a.lse[((size_t)b * a.heads_q + hq) * a.nodes + node] = real ? top + logf(total) : -INFINITY;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out.p) + to) =
+        make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
+  if (a.lse && lane == 0)
+    a.lse[((size_t)b * a.heads_q + head) * a.nodes + node] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * flash::kLn2;
 }
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeTiledFn>(p);
+  });
+  return fn;
+}
+
+// Map of a bf16 tensor of 128 channels and up to three more dimensions (element strides; 0 where a dimension has one
+// entry), box 64 channels x 128 entries of the next dimension.
+bool encode_rows(CUtensorMap* map, const void* data, int dims, const long long (&n)[3], const long long (&stride)[3]) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return false;
+  cuuint64_t size[4] = {kHeadDim, 1, 1, 1}, strides[3];
+  const cuuint32_t box[4] = {64, tree::kTile, 1, 1}, one[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 3; ++i) {
+    size[i + 1] = (cuuint64_t)n[i];
+    strides[i] = stride[i] ? 2 * (cuuint64_t)stride[i] : 2 * kHeadDim;
+  }
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dims, const_cast<void*>(data), size, strides, box, one,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Sizes {
+  bool pair;
+  int rows, item_rows, m_blocks;
+  Sizes(int G, int nodes) : rows(G * nodes) {
+    pair = rows > tree::kTile;
+    item_rows = pair ? 2 * tree::kTile : tree::kTile;
+    m_blocks = (rows + item_rows - 1) / item_rows;
+  }
+};
+
+size_t prefix_bytes(int batch) { return ((batch + 1) * sizeof(long long) + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -142,11 +159,38 @@ cudaError_t launch_tree_masks(uint4* masks, int32_t* positions, const int32_t* p
                         start);
 }
 
-size_t tree_workspace_bytes(const mikv_shape&, int, int) { return kWsHeader; }
+size_t tree_workspace_bytes(const mikv_shape& s, int nodes, int num_sms) {
+  const Sizes z(s.heads_q / s.heads_kv, nodes);
+  return kWsHeader + prefix_bytes(s.batch) + (size_t)2 * num_sms * z.item_rows * (kHeadDim + 1) * sizeof(float);
+}
 
-cudaError_t launch_tree(const TreeArgs& a, void*, int, cudaStream_t st) {
-  tree_rows_kernel<<<dim3(a.nodes, a.heads_q, a.batch), 128, 0, st>>>(a);
-  return cudaGetLastError();
+cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t st) {
+  const Sizes z(a.G, a.nodes);
+  TreeKernelArgs p;
+  memset(&p, 0, sizeof p);
+  p.a = a;
+  p.rows = z.rows;
+  p.m_blocks = z.m_blocks;
+  p.log2_G = a.G == 1 ? 0 : a.G == 2 ? 1 : a.G == 4 ? 2 : 3;
+  char* at = static_cast<char*>(ws) + kWsHeader;
+  p.prefix = reinterpret_cast<long long*>(at);
+  p.part_o = reinterpret_cast<float*>(at + prefix_bytes(a.batch));
+  p.part_lse = p.part_o + (size_t)2 * num_sms * z.item_rows * kHeadDim;
+  const long long rows = (long long)a.batch * a.heads_kv * a.hi_stride;
+  if (rows >= 1ll << 31) return cudaErrorInvalidValue;  // (row numbers of the copies)
+  if (rows > 0 && (!encode_rows(&p.map_k_hi, a.k_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0}) ||
+                   !encode_rows(&p.map_v_hi, a.v_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0})))
+    return cudaErrorInvalidValue;
+  if (!encode_rows(&p.map_k, a.k.p, 4, {a.nodes, a.heads_kv, a.batch}, {a.k.t, a.k.h, a.k.b}) ||
+      !encode_rows(&p.map_v, a.v.p, 4, {a.nodes, a.heads_kv, a.batch}, {a.v.t, a.v.h, a.v.b}))
+    return cudaErrorInvalidValue;
+  cudaError_t e = a.bits == 2   ? launch_tree_kernel<2>(p, z.pair, num_sms, st)
+                  : a.bits == 3 ? launch_tree_kernel<3>(p, z.pair, num_sms, st)
+                                : launch_tree_kernel<4>(p, z.pair, num_sms, st);
+  if (e != cudaSuccess) return e;
+  const TreeMergeArgs m = {a, p.prefix, p.part_o, p.part_lse, z.m_blocks, p.log2_G, z.item_rows, num_sms};
+  const long long out_rows = (long long)a.batch * a.nodes * a.heads_q;
+  return launch_chained(tree_merge_kernel, dim3((unsigned)((out_rows + 3) / 4)), dim3(128), 0, st, m);
 }
 
 }  // namespace mikv

@@ -1,0 +1,11 @@
+// mikv_tree_b3.cu — the attention of drafted tokens (mikv_tree_kernel.cuh) over 3-bit retained codes.
+#include "mikv_tree_kernel.cuh"
+
+namespace mikv {
+
+template <>
+cudaError_t launch_tree_kernel<3>(const TreeKernelArgs& p, bool pair, int grid, cudaStream_t st) {
+  return pair ? tree::launch_variant<3, true>(p, grid, st) : tree::launch_variant<3, false>(p, grid, st);
+}
+
+}  // namespace mikv
