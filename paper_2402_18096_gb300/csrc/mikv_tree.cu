@@ -171,6 +171,7 @@ cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t s
   p.a = a;
   p.rows = z.rows;
   p.m_blocks = z.m_blocks;
+  p.twin = z.rows <= tree::kTile / 2;
   p.log2_G = a.G == 1 ? 0 : a.G == 2 ? 1 : a.G == 4 ? 2 : 3;
   char* at = static_cast<char*>(ws) + kWsHeader;
   p.prefix = reinterpret_cast<long long*>(at);

@@ -38,6 +38,7 @@ struct TreeKernelArgs {
   CUtensorMap map_k, map_v;        // bf16 [batch][heads][nodes][128], box 64 channels x 128 nodes
   TreeArgs a;
   int rows, m_blocks, log2_G;      // rows of a KV head; row tiles (pairs)
+  int twin;                        // the rows of a tile (up to 64) stand in it twice
   long long* prefix;               // [batch + 1] costs of all items before each request (for the merge)
   float* part_o;                   // [2 * CTAs][rows of an item][128]
   float* part_lse;                 // [2 * CTAs][rows of an item], log2
@@ -58,11 +59,13 @@ constexpr int kSoftThreads = 256, kCodeThreads = 256, kThreads = 640;
 constexpr int kCodeWarp = 8, kCopyWarp = 16, kMmaWarp = 17, kPlanWarp = 18;
 constexpr int kItemRing = 4, kItemReaders = 18, kBadRing = 8;
 constexpr int kTmemCols = 512;  // S0, S1, O0, O1
+constexpr int kExPitch = 33;    // floats of a row's 32 channels in the exchange (padded against conflicts)
 
 // Costs of tiles, for the runs.
 constexpr int kCostNodes = 2, kCostHi = 2, kCostLo = 1;
 constexpr int kLeastRun = 2;       // cost of a run at least
 constexpr int kFineRows = 1024;    // requests with up to this many retained rows have their keys in two tiles
+constexpr int kAhead = 6;          // tiles of codes asked for ahead (L2)
 
 template <bool PAIR_>
 struct Layout {
@@ -73,16 +76,19 @@ struct Layout {
   // Loads of an item: the first kLead K tiles, then V tile u and K tile u + kLead for u = 0, 1, ...
   static constexpr int kLead = PAIR ? 1 : 2;
   static constexpr int kBars = 3 * kStages + 10 + 2 + 2 * kItemRing + 1;
-  static constexpr int kTables = 8 * kBars + 2 * kHeadDim * 4 + (PAIR ? 0 : 4 * kTile * 4);
+  static constexpr int kParts = PAIR ? 0 : 4 * kTile * 4, kExchange = PAIR ? 0 : 2 * (kTile / 2) * kExPitch * 4;
+  static constexpr int kTables = 8 * kBars + 8 + 2 * kHeadDim * 4 + kParts + kExchange;
   static constexpr int kSmem = 1024 + (kQ + kStages) * kTileBytes + kTables;
   static_assert(kSmem <= 227 * 1024 - 512, "shared memory of one CTA");
   uint32_t base;
   __device__ uint32_t q(int m, bool f16) const { return base + (2 * m + (f16 ? 1 : 0)) * kTileBytes; }
   __device__ uint32_t stage(int s) const { return base + (kQ + s) * kTileBytes; }
   __device__ uint32_t bar(int i) const { return base + (kQ + kStages) * kTileBytes + 8 * i; }
-  __device__ uint32_t inverse(int round) const { return bar(kBars) + (round & 1) * kHeadDim * 4; }  // 1 / balancer
-  __device__ uint32_t parts() const { return bar(kBars) + 2 * kHeadDim * 4; }
-  __device__ uint32_t full(int s) const { return bar(s); }                  // a bf16 tile landed
+  // 1 / balancer of an item's channels: in fp32 or, of 8 channels each, the fp16 nearest to it and to what that leaves
+  __device__ uint32_t inverse(int round) const { return base + (kQ + kStages) * kTileBytes + (8 * kBars + 15) / 16 * 16 + (round & 1) * kHeadDim * 4; }
+  __device__ uint32_t parts() const { return inverse(0) + 2 * kHeadDim * 4; }
+  __device__ uint32_t exchange(int w) const { return parts() + kParts + w * (kTile / 2) * kExPitch * 4; }
+  __device__ uint32_t full(int s) const { return bar(s); }                  // a bf16 tile landed; a code tile may be written
   __device__ uint32_t ready(int s) const { return bar(kStages + s); }       // a tile may be multiplied
   __device__ uint32_t empty(int s) const { return bar(2 * kStages + s); }   // it is not needed any more
   __device__ uint32_t sfull(int w) const { return bar(3 * kStages + w); }   // scores of stream w
@@ -157,7 +163,17 @@ __device__ __forceinline__ bool group_sync(bool failed) {
 }
 
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w));
+}
+__device__ __forceinline__ void sts32(uint32_t addr, uint32_t x) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(x) : "memory");
+}
+__device__ __forceinline__ void sts16(uint32_t addr, uint16_t x) {
+  asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(x) : "memory");
+}
+// Asks for `bytes` at p (both multiples of 16) to be brought into L2.
+__device__ __forceinline__ void prefetch_l2_bulk(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -186,43 +202,68 @@ template <int BITS>
 struct Codes {
   static constexpr int kWords = BITS == 4 ? 8 : 4;
   uint32_t w[kWords], top[BITS == 3 ? 4 : 1], pair[4];
-  __device__ __forceinline__ void load(const uint8_t* codes, const __half2* params, size_t row, int j, int group, bool live) {
+  // codes, params: those of row 0
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint32_t* params, uint32_t row, int j, int group) {
     auto get = [](const void* p) { return __ldg(static_cast<const uint4*>(p)); };
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    const uint8_t* at = codes + row * (16 * BITS) + 16 * j;
-    const uint4 x = live ? get(at) : zero;
+    const uint8_t* at = codes + (uint64_t)row * (16 * BITS);
+    const uint4 x = get(at + 16 * j);
     w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
     if constexpr (BITS == 4) {
-      const uint4 y = live ? get(at + 32) : zero;
+      const uint4 y = get(at + 16 * j + 32);
       w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
     }
     if constexpr (BITS == 3) {
-      const uint4 y = live ? get(codes + row * 48 + 32) : zero;
-      top[0] = y.x >> j, top[1] = y.y >> j, top[2] = y.z >> j, top[3] = y.w >> j;
+      const uint4 y = get(at + 32);
+      top[0] = y.x, top[1] = y.y, top[2] = y.z, top[3] = y.w;
     }
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(params);
     if (group == 32) {
-      const uint4 y = live ? get(p + 4 * row) : zero;
+      const uint4 y = get(params + 4 * (uint64_t)row);
       pair[0] = y.x, pair[1] = y.y, pair[2] = y.z, pair[3] = y.w;
     } else if (group == 64) {
-      const uint2 y = live ? __ldg(reinterpret_cast<const uint2*>(p + 2 * row)) : make_uint2(0u, 0u);
+      const uint2 y = __ldg(reinterpret_cast<const uint2*>(params + 2 * (uint64_t)row));
       pair[0] = pair[1] = y.x, pair[2] = pair[3] = y.y;
     } else {
-      pair[0] = pair[1] = pair[2] = pair[3] = live ? __ldg(p + row) : 0u;
+      pair[0] = pair[1] = pair[2] = pair[3] = __ldg(params + row);
     }
   }
-  // The codes of channels 16 m + 8 j + 2 q and the next, as exact fp16 numbers (a code under the exponent of 1024).
-  __device__ __forceinline__ __half2 code(int m, int q) const {
+  // The same codes (channels 16 m + 8 j + 2 q and the next) as Fields gives them, for any m at run time.
+  __device__ __forceinline__ __half2 code(int m, int q, int j) const {
     uint32_t x;
     if constexpr (BITS == 4) {
-      x = and_or(w[4 * (m >> 2) + q] >> (4 * (m & 3)), 0x000F000Fu, 0x64006400u);
+      x = and_or((m < 4 ? w[q] : w[4 + q]) >> (4 * (m & 3)), 0x000F000Fu, 0x64006400u);
     } else {
       x = and_or(w[q] >> (2 * m), 0x00030003u, 0x64006400u);
-      if constexpr (BITS == 3) x = and_or(m == 0 ? top[q] << 2 : top[q] >> (2 * m - 2), 0x00040004u, x);
+      if constexpr (BITS == 3) x |= ((top[q] >> (2 * m + j)) & 0x00010001u) << 2;
     }
     return __hsub2(u32_as_h2(x), u32_as_h2(0x64006400u));
   }
-  __device__ __forceinline__ float2 params(int m) const { return __half22float2(u32_as_h2(pair[m >> 1])); }
+};
+
+// The codes of channels 16 m + 8 j + 2 q and the next of a row, as exact fp16 numbers: the field's bits stay where they are
+// (bit s of each 16-bit unit, after one shift of the word for the upper fields) under the exponent that makes bit s count
+// 1, which is then taken off.
+template <int BITS>
+struct Fields {
+  static constexpr int kShift = BITS == 2 ? 10 : 8, kUpper = BITS == 2 ? 5 : BITS == 3 ? 4 : 2;  // from field kUpper on
+  uint32_t lo[BITS == 4 ? 8 : 4], up[BITS == 4 ? 8 : 4], lo_top[BITS == 3 ? 4 : 1], up_top[BITS == 3 ? 4 : 1];
+  __device__ __forceinline__ Fields(const Codes<BITS>& c, int j) {
+#pragma unroll
+    for (int i = 0; i < Codes<BITS>::kWords; ++i) lo[i] = c.w[i], up[i] = c.w[i] >> kShift;
+    if constexpr (BITS == 3) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lo_top[i] = (c.top[i] >> j) << 2, up_top[i] = (c.top[i] >> j) >> 6;
+    }
+  }
+  __device__ __forceinline__ __half2 code(int m, int q) const {
+    const int f = BITS == 4 ? m & 3 : m, width = BITS == 4 ? 4 : 2;
+    const bool upper = f >= kUpper;
+    const int s = width * f - (upper ? kShift : 0);
+    const uint32_t magic = 0x64006400u - 0x04000400u * s, mask = BITS == 4 ? 0x000F000Fu : 0x00030003u;
+    const int i = BITS == 4 ? 4 * (m >> 2) + q : q;
+    uint32_t x = and_or(upper ? up[i] : lo[i], mask << s, magic);
+    if constexpr (BITS == 3) x = and_or(upper ? up_top[q] : lo_top[q], 0x00040004u << s, x);
+    return __hsub2(u32_as_h2(x), u32_as_h2(magic));
+  }
 };
 
 // Where chunk `c` (8 channels) of a key lies in a tile.
@@ -272,27 +313,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     if (lane == 0) mbar_arrive(sm.itemfree(round));
     return ok;
   };
-  // The loads of an item in the order of the ring: f(tile, values, second), `second` for the rounding errors of a key tile.
-  auto for_loads = [&](const ItemData& x, auto f) {
-    const int n = x.n();
-#pragma unroll 1
-    for (int i = -2 * L::kLead; i < 2 * n; ++i) {
-      const int u = i >> 1;
-      const bool keys = i & 1;
-      if (keys ? u + L::kLead >= n : u < 0) continue;
-      const int t = x.t0 + u + (keys ? L::kLead : 0);
-      if (!f(t, !keys, false)) return false;
-      if (keys && x.fine && x.codes(t) && !f(t, false, true)) return false;
-    }
-    return true;
-  };
-
-  // Registers go to the softmax warps: 256 x 144 + 256 x 72 + 128 x 48 = 640 x 96.
+  // Registers go to the softmax warps: 256 x 128 + 256 x 88 + 128 x 48 = 640 x 96.
   if (warp >= kCopyWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == kCopyWarp) {
       int c = 0;  // loads so far
-      uint32_t copies = 0, filled = 0;  // per stage: parity of the next copy into it; whether there was one
+      int last[L::kStages];  // the last copy into each stage
+#pragma unroll
+      for (int s = 0; s < L::kStages; ++s) last[s] = -1;
       bool ok = true;
       ItemData x = {};
       for (int round = 0; ok; ++round) {
@@ -300,33 +328,64 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         if (!ok || !x.valid) break;
         if (lane == 0) {
           const int bh = x.b * a.heads_kv + x.h;
-          ok = for_loads(x, [&](int t, bool values, bool) {
-            const int s = c % L::kStages;
-            if (c >= L::kStages && !mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail)) return false;
-            ++c;
-            if (x.codes(t)) return true;
-            mbar_arrive_expect_tx(sm.full(s), kTileBytes);
-            if (t == 0) {
-              const CUtensorMap* map = values ? &p.map_v : &p.map_k;
-              tma_load_4d(sm.stage(s), map, 0, 0, x.h, x.b, sm.full(s));
-              tma_load_4d(sm.stage(s) + kHalfBytes, map, 64, 0, x.h, x.b, sm.full(s));
-            } else {
-              const CUtensorMap* map = values ? &p.map_v_hi : &p.map_k_hi;
-              const int row = bh * a.hi_stride + (t - 1) * kTile;
-              tma_load_2d(sm.stage(s), map, 0, row, sm.full(s));
-              tma_load_2d(sm.stage(s) + kHalfBytes, map, 64, row, sm.full(s));
+          const int row_bytes = 4 * (kHeadDim / a.group);
+          auto ask = [&](int t, bool values) {  // the codes and parameters of tile t into L2
+            const int r = (t - 1 - x.hi_tiles) * kTile, rows = min(kTile, x.n_lo - r);
+            if (t >= x.t1 || rows <= 0) return;
+            const size_t row = (size_t)bh * a.lo_cap + r;
+            prefetch_l2_bulk((values ? a.v_codes : a.k_codes) + row * 16 * BITS, rows * 16 * BITS);
+            prefetch_l2_bulk(reinterpret_cast<const char*>(values ? a.v_params : a.k_params) + row * row_bytes,
+                             (rows * row_bytes + 15) & ~15);
+          };
+          int asked = max(x.t0, 1 + x.hi_tiles);  // tiles asked for, two at a time
+          const int n = x.n();
+          // V tile u, then K tile u + kLead. Every stage passes through here in its turn, those that the code warps write
+          // too: a role that waited for some phases of a barrier only could take another of the same parity for its own.
+#pragma unroll 1
+          for (int i = -2 * L::kLead; ok && i < 2 * n; ++i) {
+            const bool values = !(i & 1);
+            const int u = (i >> 1) + (values ? 0 : L::kLead), t = x.t0 + u;
+            if (values ? i < 0 : u >= n) continue;
+            const bool code = x.codes(t);
+            for (int part = code && x.fine && !values ? 2 : 1; ok && part > 0; --part) {
+              const int s = c % L::kStages;
+              ok = c < L::kStages || mbar_wait_role(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail);
+              if (!ok) break;
+              if (code) {
+                mbar_arrive(sm.full(s));
+#pragma unroll
+                for (int q = 0; q < L::kStages; ++q)
+                  if (q == s) last[q] = -1;  // (what was copied here has been multiplied)
+              } else {
+                mbar_arrive_expect_tx(sm.full(s), kTileBytes);
+                const CUtensorMap* map = t == 0 ? (values ? &p.map_v : &p.map_k) : (values ? &p.map_v_hi : &p.map_k_hi);
+                const int row = bh * a.hi_stride + (t - 1) * kTile;
+#pragma unroll
+                for (int ch = 0; ch < kHeadDim; ch += 64) {
+                  const uint32_t to = sm.stage(s) + (ch ? kHalfBytes : 0);
+                  if (t == 0)
+                    tma_load_4d(to, map, ch, 0, x.h, x.b, sm.full(s));
+                  else
+                    tma_load_2d(to, map, ch, row, sm.full(s));
+                }
+#pragma unroll
+                for (int q = 0; q < L::kStages; ++q)
+                  if (q == s) last[q] = c;
+              }
+              ++c;
             }
-            copies ^= 1u << s;
-            filled |= 1u << s;
-            return true;
-          });
+            for (int k = 0; k < 2 && asked < min(x.t1, t + 1 + kAhead); ++k, ++asked) {
+              ask(asked, false);
+              ask(asked, true);
+            }
+          }
         }
         ok = __shfl_sync(0xffffffffu, ok, 0);
       }
       if (lane == 0) {  // no copy may outlive the CTA, whatever became of the other roles
 #pragma unroll
         for (int s = 0; s < L::kStages; ++s)
-          if ((filled >> s & 1) && !mbar_wait(sm.full(s), (copies >> s & 1) ^ 1)) record_error(a.status, kErrDrainTimeout);
+          if (last[s] >= 0 && !mbar_wait(sm.full(s), (last[s] / L::kStages) & 1)) record_error(a.status, kErrDrainTimeout);
       }
       __syncwarp();
     } else if (warp == kMmaWarp) {  // the whole warp, converged; one lane issues
@@ -511,75 +570,83 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       if (ok) publish(ItemData{});
     }
   } else if (warp >= kCodeWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     // The thread's place in a tile: a key and half of its channels. Eight lanes that store together have keys of one
     // parity, so that their chunks fall on different banks; a warp reads 16 rows as they lie.
     const int w = warp - kCodeWarp, quarter = lane >> 3, j = lane & 1;
     const int key = 16 * w + 8 * (quarter >> 1) + (quarter & 1) + 2 * ((lane & 7) >> 1);
     int c = 0;
-    uint32_t copies = 0;  // per stage: parity of the next copy into it
     bool ok = true;
     ItemData x = {};
     for (int round = 0;; ++round) {
       if (ok) ok = next_item(round, x);
+      bool wide = false;  // a balancer too far from 1 for fp16 arithmetic
       if (ok && x.valid) {
         const int ct = tid - 32 * kCodeWarp;
         if (ct < kHeadDim) {
           const float inv = a.balancer ? 1.f / a.balancer[x.h * kHeadDim + ct] : 1.f;
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(sm.inverse(round) + 4 * ct), "f"(inv) : "memory");
+          wide = !(inv >= 0x1p-4f && inv <= 0x1p10f);
+          sts32(sm.inverse(round) + 4 * ct, __float_as_uint(inv));
         }
       }
       if (group_sync<2, kCodeThreads>(!ok) || !x.valid) break;
-      const size_t row0 = (size_t)(x.b * a.heads_kv + x.h) * a.lo_cap;
-      const uint32_t inverse = sm.inverse(round) + 32 * j;
-      ok = for_loads(x, [&](int t, bool values, bool second) {
-        const int s = c % L::kStages;
-        if (c >= L::kStages && !mbar_wait_warp(sm.empty(s), ((c / L::kStages) & 1) ^ 1, fail)) return false;
-        const uint32_t tile = sm.stage(s);
-        if (x.codes(t)) {
-          Codes<BITS> q;
-          const int r = (t - 1 - x.hi_tiles) * kTile + key;
-          q.load(values ? a.v_codes : a.k_codes, values ? a.v_params : a.k_params, row0 + r, j, a.group, r < x.n_lo);
-          if (values) {
-#pragma unroll
-            for (int m = 0; m < 8; ++m) {
-              const __half2 pr = u32_as_h2(q.pair[m >> 1]), al = __low2half2(pr), be = __high2half2(pr);
-              uint32_t y[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) y[i] = h2_as_u32(__hfma2(q.code(m, i), al, be));
-              sts128(chunk_at(tile, key, 2 * m + j), y[0], y[1], y[2], y[3]);
-            }
-          } else {
-#pragma unroll
-            for (int m = 0; m < 8; ++m) {
-              const float2 pr = q.params(m);
-              uint32_t y[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                float2 inv;
-                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(inv.x), "=f"(inv.y) : "r"(inverse + 64 * m + 8 * i));
-                const float2 cd = __half22float2(q.code(m, i));
-                const float k0 = fmaf(pr.x, cd.x, pr.y) * inv.x, k1 = fmaf(pr.x, cd.y, pr.y) * inv.y;
-                y[i] = pack_f16(k0, k1);
-                if (second) {
-                  const float2 h = __half22float2(u32_as_h2(y[i]));
-                  y[i] = pack_f16(k0 - h.x, k1 - h.y);
-                }
-              }
-              sts128(chunk_at(tile, key, 2 * m + j), y[0], y[1], y[2], y[3]);
-            }
-          }
-          fence_async();
-        } else {
-          if (!mbar_wait_warp(sm.full(s), copies >> s & 1, fail)) return false;
-          copies ^= 1u << s;
+      const bool exact = group_sync<2, kCodeThreads>(wide) || x.fine;  // keys in fp32 arithmetic
+      const uint32_t inverse = sm.inverse(round);
+      if (!exact) {  // in place: of chunk c (8 channels) 16 bytes of the fp16 nearest to 1 / b, 16 of what that leaves
+        const int ct = tid - 32 * kCodeWarp;
+        uint32_t bits = 0;
+        if (ct < kHeadDim) {
+          const float inv = __uint_as_float(lds32(inverse + 4 * ct));
+          const __half h = __float2half_rn(inv);
+          bits = h2_as_u32(__halves2half2(h, __float2half_rn(inv - __half2float(h))));
+        }
+        if (group_sync<2, kCodeThreads>(false)) break;
+        if (ct < kHeadDim) {
+          sts16(inverse + 32 * (ct >> 3) + 2 * (ct & 7), (uint16_t)bits);
+          sts16(inverse + 32 * (ct >> 3) + 16 + 2 * (ct & 7), (uint16_t)(bits >> 16));
+        }
+        if (group_sync<2, kCodeThreads>(false)) break;
+      }
+      // Rows past the last one repeat it: their keys are masked, and their weights of 0 need finite values only where the
+      // last row's are.
+      const size_t row0 = (size_t)(x.b * a.heads_kv + x.h) * a.lo_cap, pair0 = row0 * (kHeadDim / a.group);
+      const uint32_t* params[2] = {reinterpret_cast<const uint32_t*>(a.k_params) + pair0,
+                                   reinterpret_cast<const uint32_t*>(a.v_params) + pair0};
+      const uint8_t* codes[2] = {a.k_codes + row0 * (16 * BITS), a.v_codes + row0 * (16 * BITS)};
+      const int first_codes = max(x.t0, 1 + x.hi_tiles);
+      // The codes of the next key tile and of the next value tile are on their way while the last ones are worked on.
+      Codes<BITS> next_k, next_v;
+      auto row_of = [&](int t) { return (uint32_t)min((t - 1 - x.hi_tiles) * kTile + key, x.n_lo - 1); };
+      if (first_codes < x.t1) {
+        next_k.load(codes[0], params[0], row_of(first_codes), j, a.group);
+        next_v.load(codes[1], params[1], row_of(first_codes), j, a.group);
+      }
+      const int n = x.n();
+      auto landed = [&](int load) {  // or, for codes, the stage is free
+        return mbar_wait_warp(sm.full(load % L::kStages), (load / L::kStages) & 1, fail);
+      };
+      auto done = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sm.ready(c % L::kStages));
+        ++c;
+      };
+      // V tile u, then K tile u + kLead
+#pragma unroll 1
+      for (int i = -2 * L::kLead; ok && i < 2 * n; ++i) {
+        const bool values = !(i & 1);
+        const int u = (i >> 1) + (values ? 0 : L::kLead), t = x.t0 + u;
+        if (values ? i < 0 : u >= n) continue;
+        ok = landed(c);
+        if (!ok) break;
+        const uint32_t tile = sm.stage(c % L::kStages);
+        if (!x.codes(t)) {
           if (values) {  // rows that hold no token may hold any bits
             bool blank, bad = false;
             if (t == 0) {
               const uint4 mw = key < a.nodes ? __ldg(a.masks + (size_t)x.b * a.nodes + key) : make_uint4(0u, 0u, 0u, 0u);
               const uint32_t word = key < 64 ? (key < 32 ? mw.x : mw.y) : (key < 96 ? mw.z : mw.w);
               blank = !(word >> (key & 31) & 1);
-#pragma unroll
+#pragma unroll 1
               for (int m = 0; m < 8; ++m) bad |= flash::any_nonfinite<false>(flash::lds128(chunk_at(tile, key, 2 * m + j)));
               bad = bad && !blank;
               bad |= __shfl_xor_sync(0xffffffffu, bad, 1);  // the other half of the channels
@@ -587,9 +654,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
               const uint32_t bits = __ballot_sync(0xffffffffu, bad && j == 0);
               uint32_t sorted = 0;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {  // the lane of key i (j = 0)
-                const int of = 8 * (2 * (i >> 3) + (i & 1)) + 2 * ((i & 7) >> 1);
-                sorted |= (bits >> of & 1u) << i;
+              for (int k = 0; k < 16; ++k) {  // the lane of key k (j = 0)
+                const int of = 8 * (2 * (k >> 3) + (k & 1)) + 2 * ((k & 7) >> 1);
+                sorted |= (bits >> of & 1u) << k;
               }
               if (lane == 0) reinterpret_cast<uint16_t*>(s_bad[round % kBadRing])[w] = (uint16_t)sorted;
             } else {
@@ -597,22 +664,79 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
               blank = slot >= x.n_hi || slot == x.free_slot;
             }
             if (blank || bad) {
-#pragma unroll
+#pragma unroll 1
               for (int m = 0; m < 8; ++m) flash::sts128_zero(chunk_at(tile, key, 2 * m + j));
               fence_async();
             }
           }
+          done();
+        } else if (values) {
+          const Fields<BITS> f(next_v, j);
+#pragma unroll
+          for (int m = 0; m < 8; ++m) {
+            const __half2 pr = u32_as_h2(next_v.pair[m >> 1]), al = __low2half2(pr), be = __high2half2(pr);
+            uint32_t y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = h2_as_u32(__hfma2(f.code(m, q), al, be));
+            sts128(chunk_at(tile, key, 2 * m + j), y[0], y[1], y[2], y[3]);
+          }
+          fence_async();
+          done();
+          // (behind the fence and the arrival, which wait for loads under way)
+          if (t + 1 < x.t1) next_v.load(codes[1], params[1], row_of(t + 1), j, a.group);
+        } else {
+          if (!exact) {
+            const Fields<BITS> f(next_k, j);
+            const uint4* table = reinterpret_cast<const uint4*>(smem_raw + (inverse - smem_u32(smem_raw)));
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+              const __half2 pr = u32_as_h2(next_k.pair[m >> 1]), al = __low2half2(pr), be = __high2half2(pr);
+              const uint4 n4 = table[2 * (2 * m + j)], r4 = table[2 * (2 * m + j) + 1];
+              const uint32_t near[4] = {n4.x, n4.y, n4.z, n4.w}, rest[4] = {r4.x, r4.y, r4.z, r4.w};
+              uint32_t y[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const __half2 k = __hfma2(f.code(m, q), al, be);
+                y[q] = h2_as_u32(__hfma2(k, u32_as_h2(near[q]), __hmul2(k, u32_as_h2(rest[q]))));
+              }
+              sts128(chunk_at(tile, key, 2 * m + j), y[0], y[1], y[2], y[3]);
+            }
+          } else {
+            if (x.fine) ok = landed(c + 1);
+            if (!ok) break;
+            const uint32_t second = sm.stage((c + 1) % L::kStages);
+#pragma unroll 1
+            for (int m = 0; m < 8; ++m) {
+              const float2 pr = __half22float2(u32_as_h2(m < 4 ? (m < 2 ? next_k.pair[0] : next_k.pair[1])
+                                                               : (m < 6 ? next_k.pair[2] : next_k.pair[3])));
+              uint32_t y[4], z[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const uint32_t at = inverse + 64 * m + 32 * j + 8 * q;
+                const float2 cd = __half22float2(next_k.code(m, q, j));
+                const float k0 = fmaf(pr.x, cd.x, pr.y) * __uint_as_float(lds32(at));
+                const float k1 = fmaf(pr.x, cd.y, pr.y) * __uint_as_float(lds32(at + 4));
+                y[q] = pack_f16(k0, k1);
+                const float2 h = __half22float2(u32_as_h2(y[q]));
+                z[q] = pack_f16(k0 - h.x, k1 - h.y);
+              }
+              sts128(chunk_at(tile, key, 2 * m + j), y[0], y[1], y[2], y[3]);
+              if (x.fine) sts128(chunk_at(second, key, 2 * m + j), z[0], z[1], z[2], z[3]);
+            }
+          }
+          fence_async();
+          done();
+          if (x.fine) done();
+          if (t + 1 < x.t1) next_k.load(codes[0], params[0], row_of(t + 1), j, a.group);
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sm.ready(s));
-        ++c;
-        return true;
-      });
+      }
     }
   } else {  // softmax warps
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     constexpr float kDrop = flash::ref_drop<true>(), kSlack = flash::ref_slack<true>(), kSumMax = flash::sum_max<true>();
     const int stream = warp >> 2, r = tid & (kTile - 1);
+    const bool twin = !PAIR && p.twin, upper = twin && (warp & 2);  // upper: the second copy of the rows
+    const int row = twin ? r & (kTile / 2 - 1) : r;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t ts = tmem + 128 * stream + lanes, to = tmem + 256 + 128 * stream + lanes;
     const float scale = a.sm_scale * kLog2e;
@@ -627,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     float scale16 = 0.f;
     // Stages the queries of an item (PAIR: both forms of the stream's row tile; else stream 0 bf16 and stream 1 fp16).
     auto stage_rows = [&](int round) {
-      const int R = (PAIR ? 2 * x.m_block + stream : x.m_block) * kTile + r;
+      const int R = (PAIR ? 2 * x.m_block + stream : x.m_block) * kTile + row;
       node = R >> p.log2_G;
       head = x.h * a.G + (R & (a.G - 1));
       real = false;
@@ -640,33 +764,34 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       }
       const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q.p) + x.b * a.q.b + head * a.q.h +
                                                       node * a.q.t);
-      uint4 raw[16];
-      float top = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) raw[i] = real ? __ldg(q + i) : make_uint4(0u, 0u, 0u, 0u);
       auto low = [](uint32_t v) { return __uint_as_float(v << 16); };
       auto high = [](uint32_t v) { return __uint_as_float(v & 0xffff0000u); };
+      auto chunk = [&](int i) { return real ? __ldg(q + i) : make_uint4(0u, 0u, 0u, 0u); };
+      if (round > 0 && !__all_sync(0xffffffffu, mbar_wait_role(sm.qfree(), (round - 1) & 1, fail))) return false;
+      float top = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < 16; i += 4) {
+        uint4 raw[4];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t v[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+        for (int k = 0; k < 4; ++k) raw[k] = chunk(i + k);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(low(v[e])), fabsf(high(v[e]))));
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t v[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+          if (PAIR || stream == 0) sts128(chunk_at(sm.q(PAIR ? stream : 0, false), r, i + k), v[0], v[1], v[2], v[3]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(low(v[e])), fabsf(high(v[e]))));
+        }
       }
       // 2^e with the largest element in [2^14, 2^15) 2^e
       const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 120) - 14;
       const float down = __uint_as_float((uint32_t)(127 - e) << 23);
       scale16 = scale * __uint_as_float((uint32_t)(127 + e) << 23);
-      if (round > 0 && !__all_sync(0xffffffffu, mbar_wait_role(sm.qfree(), (round - 1) & 1, fail))) return false;
-      if (PAIR || stream == 0) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sts128(chunk_at(sm.q(PAIR ? stream : 0, false), r, i), raw[i].x, raw[i].y, raw[i].z, raw[i].w);
-      }
       if (PAIR || stream == 1) {
-#pragma unroll
+#pragma unroll 4
         for (int i = 0; i < 16; ++i) {
+          const uint4 raw = chunk(i);
           auto h = [&](uint32_t v) { return pack_f16(low(v) * down, high(v) * down); };
-          sts128(chunk_at(sm.q(PAIR ? stream : 0, true), r, i), h(raw[i].x), h(raw[i].y), h(raw[i].z), h(raw[i].w));
+          sts128(chunk_at(sm.q(PAIR ? stream : 0, true), r, i), h(raw.x), h(raw.y), h(raw.z), h(raw.w));
         }
       }
       fence_async();
@@ -674,14 +799,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       if (lane == 0) mbar_arrive(sm.qfull());
       return true;
     };
-    bool ok = next_item(0, x);
-    if (ok && x.valid) ok = stage_rows(0);
-    if (!PAIR) ok = !group_sync<1, kSoftThreads>(!ok);  // (all of them go on, or none)
-    for (int round = 0; ok && x.valid; ++round) {
+    bool ok = true;
+    // Round -1 only stages the first item's queries.
+#pragma unroll 1
+    for (int round = -1; ok; ++round) {
+      if (round >= 0 && !x.valid) break;
+      const int n = round >= 0 ? x.n() : 0;
       float ref = real ? -INFINITY : 0.f, sum = 0.f;
       bool careful = true;  // some row of the warp has no reference yet
       int it = 0;           // tiles of this item done by this stream
-      const int n = x.n();
+      const bool idle = !__any_sync(0xffffffffu, real);  // no row of the warp needs weights
 #pragma unroll 1
       for (int u = PAIR ? 0 : stream; u < n; u += PAIR ? 1 : 2) {
         const int t = x.t0 + u;
@@ -689,6 +816,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         ok = __all_sync(0xffffffffu, mbar_wait_role(sm.sfull(stream), tiles & 1, fail));
         if (!ok) break;
         tcgen05_after_sync();
+        if (idle) {
+          tcgen05_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sm.pready(stream, 0)), mbar_arrive(sm.pready(stream, 1));
+          ++it;
+          ++tiles;
+          continue;
+        }
         const float sc = codes ? scale16 : scale;
         // keys of the tile that the row sees: all of them, or by the bits of `see`
         const int first = codes ? (t - 1 - x.hi_tiles) * kTile : (t - 1) * kTile;
@@ -701,8 +836,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           if (!codes && ((x.free_slot - first) >> 5) == word) bits &= ~(1u << ((x.free_slot - first) & 31));
           return bits;
         };
+        // Both halves of the keys or, where the rows stand twice, the copy's: its other weights are 0.
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
+        for (int half = upper ? 1 : 0; half < (twin && !upper ? 1 : 2); ++half) {
           float v[64];
           uint32_t w[32];
           auto load = [&]() {
@@ -712,7 +848,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             reg_fence(v + 32);
           };
           // weights of the scores in v, packed, and their sum
-          auto weigh = [&](float less) {
+          auto weigh_as = [&](float less, auto f16) {
             const uint64_t s2 = f32x2(sc, sc), r2 = f32x2(-less, -less);
             uint64_t acc[2] = {0ull, 0ull};
 #pragma unroll
@@ -721,62 +857,79 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
               f32x2_split(fma_f32x2(f32x2(v[i], v[i + 1]), s2, r2), y0, y1);
               y0 = fast_exp2(y0), y1 = fast_exp2(y1);
               acc[(i >> 1) & 1] = add_f32x2(acc[(i >> 1) & 1], f32x2(y0, y1));
-              w[i >> 1] = codes ? pack_f16(y0, y1) : pack_bf16(y0, y1);
+              w[i >> 1] = flash::pack16<decltype(f16)::value>(y0, y1);
             }
             float s0, s1;
             f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
             return s0 + s1;
           };
-          load();
+          auto weigh = [&](float less) {
+            return codes ? weigh_as(less, std::true_type{}) : weigh_as(less, std::false_type{});
+          };
+          // Without masks and with a reference in every row the weights come first and their sum tells whether a reference
+          // was too low (or a score NaN); then, or else at once: masks, the largest score, a moved reference with O rescaled.
           bool slow = masked || careful;
-          if (!slow) {
-            const float got = weigh(ref);
-            slow = __any_sync(0xffffffffu, !(got <= kSumMax));  // a reference is too low (or a score NaN)
-            if (!slow) sum += got;
-            else load();
-          }
-          if (slow) {  // masks, the largest score, a moved reference with O rescaled
-            if (masked) {
-              const uint32_t s0 = see(2 * half), s1 = see(2 * half + 1);
-              flash::mask_scores(v, s0, -INFINITY);
-              flash::mask_scores(v + 32, s1, -INFINITY);
-            }
-            float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-            for (int i = 0; i < 64; i += 4) {
-              mx[0] = flash::max3(mx[0], v[i], v[i + 1]);
-              mx[1] = flash::max3(mx[1], v[i + 2], v[i + 3]);
-            }
-            const float largest = fmaxf(mx[0], mx[1]) * sc;
-            const float next = largest > ref + kSlack ? largest - kDrop : ref;
-            const bool moves = next != ref && ref != -INFINITY;
-            if (__any_sync(0xffffffffu, moves)) {
-              const float f = moves ? fast_exp2(ref - next) : 1.f;
-              if (it + half > 0) {  // the last product in O: the other half of this tile or of the one before
-                ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, half ^ 1), (half ? tiles : tiles - 1) & 1, fail));
-                if (!ok) break;
-                tcgen05_after_sync();
 #pragma unroll 1
-                for (int q = 0; q < 8; ++q) {
-                  float o[16];
-                  tmem_ld16(to + 16 * q, o);
-                  tmem_wait_ld16(o);
-#pragma unroll
-                  for (int e = 0; e < 16; ++e) o[e] *= f;
-                  tmem_st16(to + 16 * q, reinterpret_cast<const uint32_t*>(o));
-                }
+          while (true) {
+            load();
+            if (slow) {
+              if (masked) {
+                const uint32_t s0 = see(2 * half), s1 = see(2 * half + 1);
+                flash::mask_scores(v, s0, -INFINITY);
+                flash::mask_scores(v + 32, s1, -INFINITY);
               }
-              sum *= f;
+              float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+              for (int i = 0; i < 64; i += 4) {
+                mx[0] = flash::max3(mx[0], v[i], v[i + 1]);
+                mx[1] = flash::max3(mx[1], v[i + 2], v[i + 3]);
+              }
+              const float largest = fmaxf(mx[0], mx[1]) * sc;
+              const float next = largest > ref + kSlack ? largest - kDrop : ref;
+              const bool moves = next != ref && ref != -INFINITY;
+              if (__any_sync(0xffffffffu, moves)) {
+                const float f = moves ? fast_exp2(ref - next) : 1.f;
+                const bool same = half && !twin;  // the last product in O: the first half of this tile, or the tile before
+                if (same || it > 0) {
+                  ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, same ? 0 : 1), (same ? tiles : tiles - 1) & 1, fail));
+                  if (!ok) break;
+                  tcgen05_after_sync();
+#pragma unroll 1
+                  for (int q = 0; q < 8; ++q) {
+                    float o[16];
+                    tmem_ld16(to + 16 * q, o);
+                    tmem_wait_ld16(o);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] *= f;
+                    tmem_st16(to + 16 * q, reinterpret_cast<const uint32_t*>(o));
+                  }
+                }
+                sum *= f;
+              }
+              ref = next;
+              careful = __any_sync(0xffffffffu, ref == -INFINITY);
             }
-            ref = next;
-            careful = __any_sync(0xffffffffu, ref == -INFINITY);
-            sum += weigh(ref == -INFINITY ? 0.f : ref);
+            const float got = weigh(ref == -INFINITY ? 0.f : ref);
+            if (slow || __all_sync(0xffffffffu, got <= kSumMax)) {
+              sum += got;
+              break;
+            }
+            slow = true;
           }
+          if (!ok) break;
           tmem_st32(ts + 32 * half, w);  // (over columns of S that both halves have left)
+          if (twin) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = 0u;
+            tmem_st32(ts + 32 * (half ^ 1), w);
+          }
           tmem_wait_st();
           tcgen05_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive(sm.pready(stream, half));
+          if (lane == 0) {
+            mbar_arrive(sm.pready(stream, half));
+            if (twin) mbar_arrive(sm.pready(stream, half ^ 1));
+          }
         }
         if (!ok) break;
         ++it;
@@ -784,8 +937,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       }
       // where the row goes; the next item's queries are staged before this one is written
       const bool live = real, whole = x.slot < 0;
-      const bool there = (PAIR ? 2 * x.m_block + stream : x.m_block) * kTile + r < p.rows;
-      const size_t part_at = (size_t)max(x.slot, 0) * L::kItemRows + (PAIR ? stream * kTile : 0) + r;
+      const bool there = !upper && (PAIR ? 2 * x.m_block + stream : x.m_block) * kTile + row < p.rows;
+      const size_t part_at = (size_t)max(x.slot, 0) * L::kItemRows + (PAIR ? stream * kTile : 0) + row;
       const long long out_at = x.b * a.out.b + head * a.out.h + node * a.out.t;
       const size_t lse_at = ((size_t)x.b * a.heads_q + head) * a.nodes + node;
       bool poisoned = false;
@@ -795,6 +948,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       for (int i = 0; i < 4; ++i) old_mask[i] = mask[i];
       if (ok) ok = next_item(round + 1, x);
       if (ok && x.valid) ok = stage_rows(round + 1);
+      if (round < 0) {
+        if (!PAIR) ok = !group_sync<1, kSoftThreads>(!ok);  // (all of them go on, or none)
+        continue;
+      }
       if (ok && it > 0) {
         ok = __all_sync(0xffffffffu, mbar_wait_role(sm.odone(stream, 1), (tiles - 1) & 1, fail));
         tcgen05_after_sync();
@@ -814,11 +971,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       }
       float top = ref, total = sum, g0 = 1.f, g1 = 0.f;
       if constexpr (!PAIR) {
+        const int other = twin ? r ^ (kTile / 2) : r;  // the row's other copy
         const float m0 = s_part[r], m1 = s_part[2 * kTile + r];
         top = fmaxf(m0, m1);
-        g0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - top);
-        g1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - top);
+        if (twin) top = fmaxf(top, fmaxf(s_part[other], s_part[2 * kTile + other]));
+        auto factor = [&](float m) { return m == -INFINITY ? 0.f : fast_exp2(m - top); };
+        g0 = factor(m0);
+        g1 = factor(m1);
         total = s_part[kTile + r] * g0 + s_part[3 * kTile + r] * g1;
+        // (added in the same order by both copies)
+        const float rest = s_part[kTile + other] * factor(s_part[other]) + s_part[3 * kTile + other] * factor(s_part[2 * kTile + other]);
+        if (twin) total = upper ? rest + total : total + rest;
       }
       const bool blank = !live || total == 0.f;
       const float lse2 = blank ? -INFINITY : top + log2f(total);
@@ -843,9 +1006,24 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = blank ? 0.f : fmaf(v1[e], g1, v[e]);
         }
+        if constexpr (!PAIR) {
+          if (twin) {  // the upper copy's part goes to the lower one's thread
+            float* ex = reinterpret_cast<float*>(smem_raw + (sm.exchange(stream) - smem_u32(smem_raw))) + row * kExPitch;
+            if (upper) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) ex[e] = v[e];
+            }
+            group_sync<1, kSoftThreads>(false);
+            if (!upper) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[e] += ex[e];
+            }
+            group_sync<1, kSoftThreads>(false);
+          }
+        }
         if (there) flash::store_out32<false>(dst, !whole || a.out_f32, ch, v);
       }
-      if (there && (PAIR || stream == 0)) {
+      if (there && (PAIR || stream == 0)) {  // (upper copies are not there)
         if (!whole)
           p.part_lse[part_at] = lse2;
         else if (a.lse)
