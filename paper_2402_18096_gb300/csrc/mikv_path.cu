@@ -1,5 +1,6 @@
 // mikv_path.cu — what follows the attention of drafted tokens: the importance that an accepted path hands out, its entry
 // into the cache with the demotions that follow, and copies of whole requests.
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -26,42 +27,103 @@ __device__ __forceinline__ int accepted(const int32_t* entries, int steps, int n
   return *count;
 }
 
-// acc and gained. Block (x, bh): x < gridDim.x - 1 takes kSlots slots, the last one the path's own nodes; a key to a warp
-// at a time, the path's queries in turn.
-constexpr int kSlots = 64;
-__global__ void __launch_bounds__(256) importance_kernel(float* acc, const __nv_bfloat16* k_hi, const PathArgs a, int Hq,
-                                                         int Hkv, int hi_stride) {
+// acc and gained on mma.sync: a warp holds kSteps * 16 keys as the A operand, straight from memory (a lane's 16 bytes of a
+// key are the k elements of two steps, in an order that the queries share), and goes through the path's rows (node, query
+// head) eight columns at a time. Bound by the keys' bytes (256 a slot): every key is read once, whatever the path's length,
+// and nothing is staged on its way; the rows are staged kRowChunk at a time. Block (x, bh): x < gridDim.x - 1 takes
+// kBlockKeys slots, the last one the path's own nodes.
+constexpr int kImpWarps = 8, kSteps = 2, kBlockKeys = kImpWarps * kSteps * 16, kRowChunk = 64, kRowPitch = 2 * kHeadDim + 16;
+__global__ void __launch_bounds__(32 * kImpWarps, 2) importance_kernel(float* acc, const __nv_bfloat16* k_hi,
+                                                                      const PathArgs a, int Hq, int Hkv, int hi_stride) {
   __shared__ int path[kTreeNodes], count;
+  __shared__ __align__(16) uint8_t s_q[kRowChunk * kRowPitch];
+  __shared__ float s_lse[kRowChunk];  // log2; +inf where a row weighs nothing
   const int bh = blockIdx.y, b = bh / Hkv, h = bh - b * Hkv, G = Hq / Hkv, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t = lane & 3;
+  grid_dependency_wait();
+  allow_dependent_launch();
   const int n = accepted(a.path + (size_t)b * a.steps, a.steps, a.nodes, path, &count);
   const bool slots = blockIdx.x + 1 < gridDim.x;
-  const int n_hi = a.held.hi(b), free_slot = a.held.free_slot(bh, n_hi);
-  const int first = slots ? blockIdx.x * kSlots : 0, last = slots ? min(n_hi, first + kSlots) : a.steps;
-  for (int s = first + warp; s < last; s += 8) {
-    if (slots && (s == free_slot || n == 0)) continue;
-    const __nv_bfloat16* key =
-        slots ? k_hi + ((size_t)bh * hi_stride + s) * kHeadDim
-              : static_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + h * a.k.h + (s < n ? path[s] : 0) * a.k.t;
-    float x[4], sum = 0.f;
-    row_values(*reinterpret_cast<const uint2*>(key + 4 * lane), nullptr, lane, x);
-    for (int c = slots ? 0 : s; c < n; ++c)
-      for (int j = h * G; j < (h + 1) * G; ++j) {
-        const __nv_bfloat16* query = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + j * a.q.h + path[c] * a.q.t;
-        const float lse = a.lse[((size_t)b * Hq + j) * a.nodes + path[c]];
-        float y[4];
-        row_values(*reinterpret_cast<const uint2*>(query + 4 * lane), nullptr, lane, y);
-        float d = x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3];
+  const int n_hi = a.held.hi(b), first = slots ? blockIdx.x * kBlockKeys : 0, last = slots ? n_hi : n;
+  float* gained = a.gained + (size_t)bh * a.steps;
+  if (!slots && threadIdx.x < a.steps && (int)threadIdx.x >= n) gained[threadIdx.x] = 0.f;
+  if (n == 0 || first >= last) return;
+  const int free_slot = slots ? a.held.free_slot(bh, n_hi) : -1;
+  // the keys of this warp: step i, rows g and g + 8; four chunks of 16 bytes of each
+  uint4 key[kSteps][2][4];
+  const int mine = first + warp * (kSteps * 16);
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
-        if (!isinf(lse)) sum += expf(d * a.sm_scale - lse);
+  for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int s = min(mine + 16 * i + 8 * r + g, last - 1);
+      const __nv_bfloat16* row = slots ? k_hi + ((size_t)bh * hi_stride + s) * kHeadDim
+                                       : static_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + h * a.k.h + path[s] * a.k.t;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) key[i][r][c] = __ldg(reinterpret_cast<const uint4*>(row + 32 * c) + t);
+    }
+  constexpr float kLog2e = 1.4426950408889634f;
+  const float scale = a.sm_scale * kLog2e;
+  const int rows = n * G;
+  float sum[kSteps][2] = {};
+  for (int r0 = 0; r0 < rows; r0 += kRowChunk) {
+    const int here = min(kRowChunk, rows - r0), padded = (here + 7) & ~7;
+    __syncthreads();
+    for (int i = threadIdx.x; i < padded * 16; i += 32 * kImpWarps) {
+      const int r = i >> 4, c = i & 15, node = path[min((r0 + r) / G, n - 1)], j = h * G + (r0 + r) % G;
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (r < here)
+        x = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + j * a.q.h + node * a.q.t) + c);
+      *reinterpret_cast<uint4*>(s_q + r * kRowPitch + 16 * c) = x;
+      if (c == 0) {
+        const float e = r < here ? a.lse[((size_t)b * Hq + j) * a.nodes + node] : INFINITY;
+        s_lse[r] = isinf(e) ? INFINITY : e * kLog2e;
       }
-    if (lane == 0) {
-      if (slots)
-        acc[(size_t)bh * hi_stride + s] += sum;
-      else
-        a.gained[(size_t)bh * a.steps + s] = sum;
+    }
+    __syncthreads();
+    if (mine >= last) continue;
+    for (int col = 0; col < padded; col += 8) {
+      float d[kSteps][4] = {};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {  // steps 2 c and 2 c + 1
+        const uint4 q = *reinterpret_cast<const uint4*>(s_q + (col + g) * kRowPitch + 64 * c + 16 * t);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          const uint4 x = key[i][0][c], y = key[i][1][c];
+          const uint32_t a0[4] = {x.x, y.x, x.y, y.y}, a1[4] = {x.z, y.z, x.w, y.w};
+          mma_bf16(d[i], a0, q.x, q.y);
+          mma_bf16(d[i], a1, q.z, q.w);
+        }
+      }
+      // columns 2 t and 2 t + 1 of this lane; a path's own node receives from itself and the later ones
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = col + 2 * t + e, step = slots ? INT_MAX : (r0 + r) / G;
+        const float lse = s_lse[r];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const bool sees = lse != INFINITY && step >= mine + 16 * i + 8 * k + g;
+            sum[i][k] += sees ? fast_exp2(fmaf(d[i][2 * k + e], scale, -lse)) : 0.f;
+          }
+      }
     }
   }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float x = sum[i][k];
+      x += __shfl_xor_sync(0xffffffffu, x, 1);
+      x += __shfl_xor_sync(0xffffffffu, x, 2);
+      const int s = mine + 16 * i + 8 * k + g;
+      if (t != 0 || s >= last || s == free_slot) continue;
+      if (slots)
+        acc[(size_t)bh * hi_stride + s] += x;
+      else
+        gained[s] = x;
+    }
 }
 
 // What a commit does to the lengths of a request.
@@ -81,6 +143,13 @@ __device__ __forceinline__ Commit commit_of(const PathArgs& a, int b, int count,
   return c;
 }
 
+__device__ __forceinline__ void write_lengths(const PathArgs& a, int b, const Commit& m, int bits) {
+  const int count = m.fits ? m.count : 0, gone = m.fits ? m.gone : 0;
+  if (a.n_hi_out) a.n_hi_out[b] = m.n_hi + count - gone;
+  if (a.n_lo_out) a.n_lo_out[b] = m.n_lo + (bits ? gone : 0);
+  if (a.next) a.next[b] = a.first[b] + count;
+}
+
 struct CommitArrays {
   __nv_bfloat16 *k_hi, *v_hi;
   int32_t* hi_tok;
@@ -93,15 +162,20 @@ struct CommitArrays {
 };
 
 // One block per KV head. The demoted entries are found one after another, the least (score, id, place) of those left
-// (places: the slots, then the path's nodes); a warp to a row quantizes them; then the tokens that stay are written.
-constexpr int kCommitThreads = 256;
+// (places: the slots, then the path's nodes); a warp to a row quantizes them; then the tokens that stay are written. Bound
+// by latency: the scores and ids are read once and stay in registers (kOwn entries a thread), a demotion costs two
+// reductions, and the rows of all demotions are in flight together.
+constexpr int kCommitThreads = 256, kOwn = 8;
 template <int BITS, int GROUP>
-__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArrays c, const PathArgs a) {
+__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArrays c, const PathArgs a, bool lengths) {
   __shared__ int path[kTreeNodes], count, victim[kTreeNodes], place[kTreeNodes];
   __shared__ unsigned long long s_key[kCommitThreads / 32];
   __shared__ int s_at[kCommitThreads / 32];
   const int bh = blockIdx.x, b = bh / c.Hkv, h = bh - b * c.Hkv, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  grid_dependency_wait();
+  allow_dependent_launch();
   const Commit m = commit_of(a, b, accepted(a.path + (size_t)b * a.steps, a.steps, a.nodes, path, &count), BITS, c.lo_cap);
+  if (lengths && h == 0 && tid == 0) write_lengths(a, b, m, BITS);
   if (m.count == 0) return;
   const int free_slot = a.held.free_slot(bh, m.n_hi);
   if (!m.fits || (a.held.slots && free_slot < 0)) {
@@ -114,32 +188,44 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArra
   auto key_of = [&](int e) {
     return e < m.n_hi ? order_key(c.acc[hi0 + e], c.hi_tok[hi0 + e]) : order_key(gained[e - m.n_hi], tok0 + e - m.n_hi);
   };
+  unsigned long long own[kOwn];  // entries tid, tid + kCommitThreads, ...; the highest key: none
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const int e = tid + i * kCommitThreads;
+    own[i] = m.gone > 0 && e < entries && e != free_slot ? key_of(e) : ~0ull;
+  }
   unsigned long long last_key = 0ull;  // the least entry found so far
   int last_at = -1;
   for (int j = 0; j < m.gone; ++j) {
     unsigned long long best = ~0ull;
     int at = entries;
-    for (int e = tid; e < entries; e += kCommitThreads) {
-      if (e == free_slot) continue;
-      const unsigned long long k = key_of(e);
+    auto consider = [&](unsigned long long k, int e) {
       const bool left = j == 0 || k > last_key || (k == last_key && e > last_at);
       if (left && (at == entries || k < best)) best = k, at = e;
-    }
+    };
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-      const unsigned long long k = __shfl_xor_sync(0xffffffffu, best, off);
-      const int e = __shfl_xor_sync(0xffffffffu, at, off);
-      if (k < best || (k == best && e < at)) best = k, at = e;
+    for (int i = 0; i < kOwn; ++i) {
+      const int e = tid + i * kCommitThreads;
+      if (e < entries && e != free_slot) consider(own[i], e);
     }
+    for (int e = tid + kOwn * kCommitThreads; e < entries; e += kCommitThreads)
+      if (e != free_slot) consider(key_of(e), e);
+    auto reduce = [&]() {
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) {
+        const unsigned long long k = __shfl_xor_sync(0xffffffffu, best, off);
+        const int e = __shfl_xor_sync(0xffffffffu, at, off);
+        if (k < best || (k == best && e < at)) best = k, at = e;
+      }
+    };
+    reduce();
     if (lane == 0) s_key[warp] = best, s_at[warp] = at;
     __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < kCommitThreads / 32; ++w)
-        if (s_key[w] < s_key[0] || (s_key[w] == s_key[0] && s_at[w] < s_at[0])) s_key[0] = s_key[w], s_at[0] = s_at[w];
-      victim[j] = s_at[0];
-    }
-    __syncthreads();
-    last_key = s_key[0], last_at = victim[j];
+    constexpr int W = kCommitThreads / 32;
+    best = s_key[lane & (W - 1)], at = s_at[lane & (W - 1)];
+    reduce();
+    last_key = best, last_at = at;
+    if (tid == 0) victim[j] = at;
     __syncthreads();
   }
   if (tid == 0) {  // where the path's nodes go: -1 demoted, else the slot
@@ -184,16 +270,14 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArra
   }
 }
 
-// The lengths after a commit, in a launch of its own: they may be written over those that the commit read.
+// The lengths after a commit, where they are written over those that it reads: a launch of its own.
 __global__ void __launch_bounds__(kTreeNodes) commit_lengths_kernel(const PathArgs a, int bits, int lo_cap) {
   __shared__ int path[kTreeNodes], count;
   const int b = blockIdx.x;
+  grid_dependency_wait();
+  allow_dependent_launch();
   const Commit m = commit_of(a, b, accepted(a.path + (size_t)b * a.steps, a.steps, a.nodes, path, &count), bits, lo_cap);
-  if (threadIdx.x) return;
-  const int count_in = m.fits ? m.count : 0, gone = m.fits ? m.gone : 0;
-  if (a.n_hi_out) a.n_hi_out[b] = m.n_hi + count_in - gone;
-  if (a.n_lo_out) a.n_lo_out[b] = m.n_lo + (bits ? gone : 0);
-  if (a.next) a.next[b] = a.first[b] + count_in;
+  if (threadIdx.x == 0) write_lengths(a, b, m, bits);
 }
 
 // Copies. An array of a cache, and which of a request's rows it keeps.
@@ -205,18 +289,20 @@ struct CopyArray {
   int from_row, to_row;  // first row
   int row_bytes, kind;
 };
-constexpr int kCopyArrays = 16, kCopyPairs = 256, kCopyThreads = 256, kCopyChunk = 64 * 1024;
+constexpr int kCopyArrays = 16, kCopyPairs = 256, kCopyThreads = 256, kInFlight = 8;
 struct CopyArgs {
   CopyArray x[kCopyArrays];
   int2 pair[kCopyPairs];
   CopyLengths len;
-  int arrays, heads, hi_cap, kch;
+  int arrays, heads, hi_cap, kch, chunk;
 };
 
 // Block (pair, chunk, head): its chunk of the bytes that the request keeps of this head, array after array. Pairs run
 // fastest, so that those of one source read it from L2.
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
   const int2 pair = a.pair[blockIdx.x];
+  grid_dependency_wait();
+  allow_dependent_launch();
   const int h = blockIdx.z;
   const int n_hi = a.len.n_hi ? max(0, min(a.len.n_hi[pair.x], a.hi_cap)) : a.hi_cap;
   const int n_lo = a.len.n_lo ? max(0, min(a.len.n_lo[pair.x], a.len.n_lo_max)) : a.len.n_lo_max;
@@ -227,7 +313,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
   }
   const int kept = a.kch ? n_lo / kKchGroup * kKchGroup : n_lo;
   for (int chunk = blockIdx.y;; chunk += gridDim.y) {
-    long long begin = (long long)chunk * kCopyChunk, end = begin + kCopyChunk;
+    long long begin = (long long)chunk * a.chunk, end = begin + a.chunk;
     for (int i = 0; i < a.arrays && end > 0; ++i) {
       const CopyArray& x = a.x[i];
       const int rows = x.kind == kHiRows ? n_hi : x.kind == kLoRows ? kept : x.kind == kGroups ? kept / kKchGroup : n_lo - kept;
@@ -235,7 +321,20 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
       const long long lo = max(begin, 0ll), hi = min(end, bytes);
       const char* from = x.from + (((size_t)pair.x * a.heads + h) * x.from_cap + x.from_row) * x.row_bytes;
       char* to = x.to + (((size_t)pair.y * a.heads + h) * x.to_cap + x.to_row) * x.row_bytes;
-      for (long long at = lo + 4 * threadIdx.x; at < hi; at += 4 * kCopyThreads)
+      // (ids and scores of staged rows may begin anywhere)
+      const bool wide = ((reinterpret_cast<uintptr_t>(from) | reinterpret_cast<uintptr_t>(to)) & 15) == 0;
+      const long long end16 = wide ? lo + ((hi - lo) & ~15ll) : lo;
+      long long at = lo + 16 * threadIdx.x;
+      for (; at + 16ll * kCopyThreads * (kInFlight - 1) < end16; at += 16ll * kCopyThreads * kInFlight) {
+        uint4 v[kInFlight];
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k) v[k] = __ldg(reinterpret_cast<const uint4*>(from + at + 16ll * kCopyThreads * k));
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k) __stcs(reinterpret_cast<uint4*>(to + at + 16ll * kCopyThreads * k), v[k]);
+      }
+      for (; at < end16; at += 16ll * kCopyThreads)
+        __stcs(reinterpret_cast<uint4*>(to + at), __ldg(reinterpret_cast<const uint4*>(from + at)));
+      for (at = end16 + 4 * threadIdx.x; at < hi; at += 4 * kCopyThreads)
         *reinterpret_cast<uint32_t*>(to + at) = *reinterpret_cast<const uint32_t*>(from + at);
       const long long whole = (bytes + 15) / 16 * 16;  // (the next array's pieces begin at a multiple of 16 bytes)
       begin -= whole;
@@ -248,10 +347,9 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
 }  // namespace
 
 cudaError_t launch_path_importance(const mikv_shape& s, const PathArgs& a, cudaStream_t st) {
-  const dim3 grid((s.hi_cap + kSlots - 1) / kSlots + 1, s.batch * s.heads_kv);
-  importance_kernel<<<grid, 256, 0, st>>>(a.cache->acc, static_cast<const __nv_bfloat16*>(a.cache->k_hi), a, s.heads_q,
-                                          s.heads_kv, s.hi_stride);
-  return cudaGetLastError();
+  const dim3 grid((s.hi_cap + kBlockKeys - 1) / kBlockKeys + 1, s.batch * s.heads_kv);
+  return launch_chained(importance_kernel, grid, dim3(32 * kImpWarps), 0, st, a.cache->acc,
+                        static_cast<const __nv_bfloat16*>(a.cache->k_hi), a, s.heads_q, s.heads_kv, s.hi_stride);
 }
 
 cudaError_t launch_commit(const mikv_shape& s, const PathArgs& a, cudaStream_t st) {
@@ -260,7 +358,8 @@ cudaError_t launch_commit(const mikv_shape& s, const PathArgs& a, cudaStream_t s
                           static_cast<uint8_t*>(k.k_codes), static_cast<uint8_t*>(k.v_codes),
                           static_cast<__half2*>(k.k_params), static_cast<__half2*>(k.v_params), k.lo_tok, k.balancer,
                           s.heads_kv, s.hi_stride, s.lo_cap};
-  void (*kernel)(const CommitArrays, const PathArgs) = nullptr;
+  void (*kernel)(const CommitArrays, const PathArgs, bool) = nullptr;
+  const bool over = (a.n_hi_out && a.n_hi_out == a.held.n_hi) || (a.n_lo_out && a.n_lo_out == a.held.n_lo) || (a.next && a.next == a.first);
   switch (s.bits == 0 ? 0 : 1000 * s.bits + s.group) {
     case 0: kernel = commit_kernel<0, 32>; break;
     case 2032: kernel = commit_kernel<2, 32>; break;
@@ -274,11 +373,9 @@ cudaError_t launch_commit(const mikv_shape& s, const PathArgs& a, cudaStream_t s
     case 4128: kernel = commit_kernel<4, 128>; break;
     default: return cudaErrorInvalidValue;
   }
-  kernel<<<s.batch * s.heads_kv, kCommitThreads, 0, st>>>(c, a);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || (!a.n_hi_out && !a.n_lo_out && !a.next)) return e;
-  commit_lengths_kernel<<<s.batch, kTreeNodes, 0, st>>>(a, s.bits, s.lo_cap);
-  return cudaGetLastError();
+  const cudaError_t e = launch_chained(kernel, dim3(s.batch * s.heads_kv), dim3(kCommitThreads), 0, st, c, a, !over);
+  if (e != cudaSuccess || !over) return e;
+  return launch_chained(commit_lengths_kernel, dim3(s.batch), dim3(kTreeNodes), 0, st, a, s.bits, s.lo_cap);
 }
 
 cudaError_t launch_copy_requests(const mikv_shape& s, const mikv_cache& c, const mikv_shape& ts, const mikv_cache& tc,
@@ -322,12 +419,15 @@ cudaError_t launch_copy_requests(const mikv_shape& s, const mikv_cache& c, const
   a.len = len;
   a.heads = s.heads_kv;
   a.hi_cap = s.hi_cap;
-  const int chunks = (int)std::min(std::max(1ll, (most + kCopyChunk - 1) / kCopyChunk), 65535ll);
+  // Pieces of 32 KB (what a block has in flight) to 128 KB: enough of them for every SM, and few of them empty where
+  // requests are shorter than the caches allow. 8 requests of 20 .. 8192 tokens, twice each: 32 KB 290 us, 128 KB 114.
+  const long long share = most * s.heads_kv * std::min(n, kCopyPairs) / (8 * 152);
+  a.chunk = (int)std::min(std::max(share & ~32767ll, 32768ll), 131072ll);
+  const int chunks = (int)std::min(std::max(1ll, (most + a.chunk - 1) / a.chunk), 65535ll);
   for (int first = 0; first < n; first += kCopyPairs) {
     const int count = std::min(kCopyPairs, n - first);
     for (int i = 0; i < count; ++i) a.pair[i] = make_int2(pairs[2 * (first + i)], pairs[2 * (first + i) + 1]);
-    copy_kernel<<<dim3(count, chunks, s.heads_kv), kCopyThreads, 0, st>>>(a);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_chained(copy_kernel, dim3(count, chunks, s.heads_kv), dim3(kCopyThreads), 0, st, a);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
