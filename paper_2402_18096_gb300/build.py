@@ -23,7 +23,8 @@ SOURCES = ["mikv_attn_h16.cu", "mikv_attn_h8.cu", "mikv_attn_h4.cu", "mikv_attn_
            "mikv_attention.cu",
            "mikv_quant.cu", "mikv_policy.cu", "mikv_step.cu", "mikv_prefill.cu", "mikv_abi.cu",
            "mikv_rotary.cu", "mikv_flash.cu", "mikv_flash_bf16.cu", "mikv_flash_f16.cu", "mikv_abi_prompt.cu",
-           "mikv_tree.cu", "mikv_tree_b2.cu", "mikv_tree_b3.cu", "mikv_tree_b4.cu", "mikv_path.cu", "mikv_abi_tree.cu"]
+           "mikv_tree.cu", "mikv_tree_b2.cu", "mikv_tree_b3.cu", "mikv_tree_b4.cu",
+           "mikv_tree_f2.cu", "mikv_tree_f3.cu", "mikv_tree_f4.cu", "mikv_path.cu", "mikv_abi_tree.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

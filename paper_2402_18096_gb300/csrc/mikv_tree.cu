@@ -5,7 +5,7 @@
 
 #include <mutex>
 
-#include "mikv_tree_kernel.cuh"
+#include "mikv_tree_few.cuh"
 
 namespace mikv {
 namespace {
@@ -47,10 +47,30 @@ struct TreeMergeArgs {
   TreeArgs a;
   const long long* prefix;
   const float *part_o, *part_lse;
-  int m_blocks, log2_G, item_rows, ctas;
+  int m_blocks, log2_G, item_rows, ctas, lo_rows;
+};
+
+// How an item's units lie in the runs: key tiles by their costs, or the units of few rows, one like another.
+struct TileRuns {
+  Tiles tl;
+  Runs runs;
+  __device__ TileRuns(const TreeMergeArgs& m, int b) : tl(m.a.held, b), runs(m.prefix[m.a.batch], m.ctas) {}
+  __device__ long long cost() const { return tl.cost(); }
+  __device__ long long last() const { return tl.before(tl.count() - 1); }
+  __device__ bool part(long long from, long long to) const { return tl.first(from) < tl.first(to); }
+};
+struct FewRuns {
+  int count;
+  Runs runs;
+  __device__ FewRuns(const TreeMergeArgs& m, int b)
+      : count(tree::FewUnits(m.a.held, m.a.nodes, b, m.lo_rows).count()), runs(m.prefix[m.a.batch], m.ctas, tree::kFewLeast) {}
+  __device__ long long cost() const { return count; }
+  __device__ long long last() const { return count - 1; }
+  __device__ bool part(long long from, long long to) const { return max(from, 0ll) < min(to, (long long)count); }
 };
 
 // The parts of an output row, weighted by 2^(lse - largest): a warp to a row. Rows whose item one CTA had are written.
+template <typename R>
 __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__ TreeMergeArgs m) {
   const TreeArgs& a = m.a;
   const int lane = threadIdx.x & 31;
@@ -61,10 +81,10 @@ __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__
   if (b >= a.batch) return;
   const int h = head >> m.log2_G, in_head = (node << m.log2_G) + (head & (a.G - 1));
   const int block = in_head / m.item_rows, in_item = in_head - block * m.item_rows;
-  const Tiles tl(a.held, b);
-  const Runs runs(m.prefix[a.batch], m.ctas);
-  const long long start = m.prefix[b] + (long long)(h * m.m_blocks + block) * tl.cost();
-  const int c0 = runs.owner(start), c1 = runs.owner(start + tl.before(tl.count() - 1));
+  const R item(m, b);
+  const Runs& runs = item.runs;
+  const long long start = m.prefix[b] + (long long)(h * m.m_blocks + block) * item.cost();
+  const int c0 = runs.owner(start), c1 = runs.owner(start + item.last());
   if (c0 == c1) return;
   float top = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -72,7 +92,7 @@ __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__
     const int c = first + lane;
     const long long at = (long long)(2 * c + (c == c0)) * m.item_rows + in_item;
     bool part = c <= c1;
-    if (part) part = tl.first(runs.first(c) - start) < tl.first(runs.first(c + 1) - start);
+    if (part) part = item.part(runs.first(c) - start, runs.first(c + 1) - start);
     const float e = part ? m.part_lse[at] : -INFINITY;
     float next = fmaxf(top, e);
 #pragma unroll
@@ -124,12 +144,13 @@ EncodeTiledFn encode_fn() {
 }
 
 // Map of a bf16 tensor of 128 channels and up to three more dimensions (element strides; 0 where a dimension has one
-// entry), box 64 channels x 128 entries of the next dimension.
-bool encode_rows(CUtensorMap* map, const void* data, int dims, const long long (&n)[3], const long long (&stride)[3]) {
+// entry), box 64 channels x `rows` entries of the next dimension.
+bool encode_rows(CUtensorMap* map, const void* data, int dims, const long long (&n)[3], const long long (&stride)[3],
+                 int rows = tree::kTile) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return false;
   cuuint64_t size[4] = {kHeadDim, 1, 1, 1}, strides[3];
-  const cuuint32_t box[4] = {64, tree::kTile, 1, 1}, one[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, one[4] = {1, 1, 1, 1};
   for (int i = 0; i < 3; ++i) {
     size[i + 1] = (cuuint64_t)n[i];
     strides[i] = stride[i] ? 2 * (cuuint64_t)stride[i] : 2 * kHeadDim;
@@ -139,14 +160,19 @@ bool encode_rows(CUtensorMap* map, const void* data, int dims, const long long (
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Which kernel: few rows stay in registers (mikv_tree_few.cuh), more go through tensor memory.
+constexpr int kFewMost = 16;
+
 struct Sizes {
-  bool pair;
+  bool few, pair;
   int rows, item_rows, m_blocks;
   Sizes(int G, int nodes) : rows(G * nodes) {
+    few = rows <= kFewMost;
     pair = rows > tree::kTile;
-    item_rows = pair ? 2 * tree::kTile : tree::kTile;
+    item_rows = few ? tree::kFewRows : pair ? 2 * tree::kTile : tree::kTile;
     m_blocks = (rows + item_rows - 1) / item_rows;
   }
+  size_t parts(int num_sms) const { return (size_t)2 * num_sms * (few ? tree::kFewWarps : 1); }
 };
 
 size_t prefix_bytes(int batch) { return ((batch + 1) * sizeof(long long) + 255) / 256 * 256; }
@@ -161,37 +187,62 @@ cudaError_t launch_tree_masks(uint4* masks, int32_t* positions, const int32_t* p
 
 size_t tree_workspace_bytes(const mikv_shape& s, int nodes, int num_sms) {
   const Sizes z(s.heads_q / s.heads_kv, nodes);
-  return kWsHeader + prefix_bytes(s.batch) + (size_t)2 * num_sms * z.item_rows * (kHeadDim + 1) * sizeof(float);
+  return kWsHeader + prefix_bytes(s.batch) + z.parts(num_sms) * z.item_rows * (kHeadDim + 1) * sizeof(float);
 }
 
 cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t st) {
   const Sizes z(a.G, a.nodes);
+  const int log2_G = a.G == 1 ? 0 : a.G == 2 ? 1 : a.G == 4 ? 2 : 3;
+  char* at = static_cast<char*>(ws) + kWsHeader;
+  long long* prefix = reinterpret_cast<long long*>(at);
+  float* part_o = reinterpret_cast<float*>(at + prefix_bytes(a.batch));
+  float* part_lse = part_o + z.parts(num_sms) * z.item_rows * kHeadDim;
+  const long long rows = (long long)a.batch * a.heads_kv * a.hi_stride;
+  if (rows >= 1ll << 31) return cudaErrorInvalidValue;  // (row numbers of the copies)
+  CUtensorMap k_hi, v_hi;
+  memset(&k_hi, 0, sizeof k_hi);
+  memset(&v_hi, 0, sizeof v_hi);
+  const int box = z.few ? 16 : tree::kTile;
+  if (rows > 0 && (!encode_rows(&k_hi, a.k_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0}, box) ||
+                   !encode_rows(&v_hi, a.v_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0}, box)))
+    return cudaErrorInvalidValue;
+  TreeMergeArgs m = {a, prefix, part_o, part_lse, z.m_blocks, log2_G, z.item_rows, num_sms, 0};
+  const long long out_rows = (long long)a.batch * a.nodes * a.heads_q;
+  const dim3 merge_grid((unsigned)((out_rows + 3) / 4));
+  if (z.few) {
+    TreeFewArgs p;
+    memset(&p, 0, sizeof p);
+    p.map_k_hi = k_hi, p.map_v_hi = v_hi;
+    p.a = a;
+    p.rows = z.rows, p.row_blocks = z.m_blocks, p.log2_G = log2_G;
+    p.prefix = prefix, p.part_o = part_o, p.part_lse = part_lse;
+    const cudaError_t e = a.bits == 2   ? launch_tree_few<2>(p, num_sms, st)
+                          : a.bits == 3 ? launch_tree_few<3>(p, num_sms, st)
+                                        : launch_tree_few<4>(p, num_sms, st);
+    if (e != cudaSuccess) return e;
+    m.ctas = num_sms * tree::kFewWarps;
+    m.lo_rows = 16 * (a.bits == 2   ? tree::FewUnit<2>(a.group).blocks
+                      : a.bits == 3 ? tree::FewUnit<3>(a.group).blocks
+                                    : tree::FewUnit<4>(a.group).blocks);
+    return launch_chained(tree_merge_kernel<FewRuns>, merge_grid, dim3(128), 0, st, m);
+  }
   TreeKernelArgs p;
   memset(&p, 0, sizeof p);
+  p.map_k_hi = k_hi, p.map_v_hi = v_hi;
   p.a = a;
   p.rows = z.rows;
   p.m_blocks = z.m_blocks;
   p.twin = z.rows <= tree::kTile / 2;
-  p.log2_G = a.G == 1 ? 0 : a.G == 2 ? 1 : a.G == 4 ? 2 : 3;
-  char* at = static_cast<char*>(ws) + kWsHeader;
-  p.prefix = reinterpret_cast<long long*>(at);
-  p.part_o = reinterpret_cast<float*>(at + prefix_bytes(a.batch));
-  p.part_lse = p.part_o + (size_t)2 * num_sms * z.item_rows * kHeadDim;
-  const long long rows = (long long)a.batch * a.heads_kv * a.hi_stride;
-  if (rows >= 1ll << 31) return cudaErrorInvalidValue;  // (row numbers of the copies)
-  if (rows > 0 && (!encode_rows(&p.map_k_hi, a.k_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0}) ||
-                   !encode_rows(&p.map_v_hi, a.v_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0})))
-    return cudaErrorInvalidValue;
+  p.log2_G = log2_G;
+  p.prefix = prefix, p.part_o = part_o, p.part_lse = part_lse;
   if (!encode_rows(&p.map_k, a.k.p, 4, {a.nodes, a.heads_kv, a.batch}, {a.k.t, a.k.h, a.k.b}) ||
       !encode_rows(&p.map_v, a.v.p, 4, {a.nodes, a.heads_kv, a.batch}, {a.v.t, a.v.h, a.v.b}))
     return cudaErrorInvalidValue;
-  cudaError_t e = a.bits == 2   ? launch_tree_kernel<2>(p, z.pair, num_sms, st)
-                  : a.bits == 3 ? launch_tree_kernel<3>(p, z.pair, num_sms, st)
-                                : launch_tree_kernel<4>(p, z.pair, num_sms, st);
+  const cudaError_t e = a.bits == 2   ? launch_tree_kernel<2>(p, z.pair, num_sms, st)
+                        : a.bits == 3 ? launch_tree_kernel<3>(p, z.pair, num_sms, st)
+                                      : launch_tree_kernel<4>(p, z.pair, num_sms, st);
   if (e != cudaSuccess) return e;
-  const TreeMergeArgs m = {a, p.prefix, p.part_o, p.part_lse, z.m_blocks, p.log2_G, z.item_rows, num_sms};
-  const long long out_rows = (long long)a.batch * a.nodes * a.heads_q;
-  return launch_chained(tree_merge_kernel, dim3((unsigned)((out_rows + 3) / 4)), dim3(128), 0, st, m);
+  return launch_chained(tree_merge_kernel<TileRuns>, merge_grid, dim3(128), 0, st, m);
 }
 
 }  // namespace mikv

@@ -1,0 +1,610 @@
+// mikv_tree_few.cuh — attention of drafted tokens over the mixed-precision cache where a KV head has few query rows: codes
+// go from shared memory through registers into mma.sync, without a tile of dequantized keys in between.
+// mikv_tree_f2.cu, mikv_tree_f3.cu and mikv_tree_f4.cu instantiate it for one code width each.
+//
+// Why not the tensor-memory kernel: its tiles have 128 rows, its codes are written to and read from shared memory as
+// fp16 (ten times their size), and 16 rows of 128 are an eighth of what its products cost. Here a key costs 330 / 16
+// instructions of a warp, whatever the rows up to 16, and HBM is nearer than the tensor cores' rate.
+//
+// Work. Rows r = node * G + head in blocks of 16 (the M side of the MMAs); an item is a row block of one KV head. Its units
+// are 16 nodes, 16 important slots, or as many blocks of 16 retained rows as fit a stage of 8 KB. All items' units are laid
+// end to end and every warp of the grid takes an equal run of them, as the CTAs do in mikv_tree_kernel.cuh; the same
+// second kernel merges what lies in several runs. A warp shares nothing with the others: two stages of its own, filled by
+// copies (bulk copies of code rows, swizzled boxes of bf16 rows) that it asks for one unit ahead.
+//
+// A block of 16 tokens: S (16 x 16) = Q K^T with keys dequantized into the B operand (fp16: alpha code + beta, one rounding),
+// P = 2^(x - r) packed from S as it lies into the A operand, O (16 x 128) += P V with values dequantized likewise. The query
+// is divided by the balancer and stands in two fp16 terms (22 bits): rounded to one it would be off alike for all keys,
+// 1e-5 of lse. Where few retained rows (kFineRows) average nothing out, the rounding errors of the keys follow as a third
+// product. Tokens 2 t and 2 t + 1 of an operand are rows t and t + 4 of their eight, so that eight lanes read four rows of
+// codes from different banks.
+#pragma once
+
+#include "mikv_tree_kernel.cuh"
+
+namespace mikv {
+
+struct TreeFewArgs {
+  CUtensorMap map_k_hi, map_v_hi;  // bf16 [batch * heads * hi_stride][128], box 64 channels x 16 rows, 128B swizzle
+  TreeArgs a;
+  int rows, row_blocks, log2_G;
+  long long* prefix;
+  float* part_o;    // [2 * warps][16][128]
+  float* part_lse;  // [2 * warps][16], log2
+};
+
+template <int BITS>
+cudaError_t launch_tree_few(const TreeFewArgs& p, int grid, cudaStream_t st);
+
+namespace tree {
+
+constexpr int kFewWarps = 8, kFewRows = 16, kFewStage = 8192, kFewStages = 3;
+constexpr int kFewLeast = 2;  // units of a run at least
+
+// Blocks of 16 retained rows in a unit, and where its arrays lie in a stage.
+template <int BITS>
+struct FewUnit {
+  int blocks, pairs, v, kp, vp, row_bytes;
+  __host__ __device__ explicit FewUnit(int group) : pairs(kHeadDim / group) {
+    const int block = 2 * 16 * (16 * BITS + 4 * pairs);
+    blocks = kFewStage / block < 5 ? kFewStage / block : 5;
+    row_bytes = 4 * pairs;
+    v = blocks * 16 * 16 * BITS;
+    kp = 2 * v;
+    vp = kp + blocks * 16 * row_bytes;
+  }
+};
+
+// Units of a request's items: nodes, slots, retained rows.
+struct FewUnits {
+  int nodes, hi, lo;
+  __device__ FewUnits() : nodes(0), hi(0), lo(0) {}
+  __device__ FewUnits(const HeldArgs& held, int n_nodes, int b, int lo_rows)
+      : nodes((n_nodes + 15) / 16), hi((held.hi(b) + 15) / 16), lo((held.lo(b) + lo_rows - 1) / lo_rows) {}
+  __device__ int count() const { return nodes + hi + lo; }
+};
+
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 r;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(addr));
+  return r;
+}
+__device__ __forceinline__ uint32_t lds32v(uint32_t addr) {
+  uint32_t r;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(addr));
+  return r;
+}
+
+// A code field of both 16-bit halves of a word as exact fp16 numbers; m: which field (compile time), up: the word shifted
+// for the upper fields.
+template <int BITS>
+struct FieldOf {
+  static constexpr int kShift = BITS == 2 ? 10 : 8, kUpper = BITS == 2 ? 5 : BITS == 3 ? 4 : 2;
+  // x, y: the word, and for 4 bits the second word (fields 4 ..), for 3 bits the word of the high bits (at bit 2 m)
+  uint32_t lo[2], up[2];
+  __device__ __forceinline__ FieldOf(uint32_t x, uint32_t y) {
+    lo[0] = x, up[0] = x >> kShift;
+    if constexpr (BITS == 4) lo[1] = y, up[1] = y >> kShift;
+    if constexpr (BITS == 3) lo[1] = y << 2, up[1] = y >> 6;
+  }
+  __device__ __forceinline__ __half2 code(int m) const {
+    const int f = BITS == 4 ? m & 3 : m, width = BITS == 4 ? 4 : 2;
+    const bool upper = f >= kUpper;
+    const int s = width * f - (upper ? kShift : 0), i = BITS == 4 ? m >> 2 : 0;
+    const uint32_t magic = 0x64006400u - 0x04000400u * s, mask = BITS == 4 ? 0x000F000Fu : 0x00030003u;
+    uint32_t x = and_or(upper ? up[i] : lo[i], mask << s, magic);
+    if constexpr (BITS == 3) x = and_or(upper ? up[1] : lo[1], 0x00040004u << s, x);
+    return __hsub2(u32_as_h2(x), u32_as_h2(magic));
+  }
+};
+
+// The parameters of a token.
+template <int PAIRS>
+__device__ __forceinline__ void load_pairs(uint32_t addr, uint32_t (&p)[PAIRS]) {
+  if constexpr (PAIRS == 4) {
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(p[0]), "=r"(p[1]), "=r"(p[2]), "=r"(p[3]) : "r"(addr));
+  } else if constexpr (PAIRS == 2) {
+    const uint2 x = lds64(addr);
+    p[0] = x.x, p[1] = x.y;
+  } else {
+    p[0] = lds32v(addr);
+  }
+}
+
+template <int BITS, int PAIRS>
+__global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __grid_constant__ TreeFewArgs p) {
+  const TreeArgs& a = p.a;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t s_bar[kFewWarps][kFewStages];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t stages = ((smem_u32(smem_raw) + 1023u) & ~1023u) + warp * (kFewStages * kFewStage);
+  const uint32_t bars = smem_u32(&s_bar[warp][0]);
+  if (lane < kFewStages) mbar_init(bars + 8 * lane, 1);
+  fence_mbar_init();
+  __syncwarp();
+  grid_dependency_wait();
+  allow_dependent_launch();
+  const FewUnit<BITS> U(kHeadDim / PAIRS);
+  constexpr int kOf = 8 / PAIRS;  // fields of 16 channels to a pair of parameters
+  const int lo_rows = 16 * U.blocks, per_set = a.heads_kv * p.row_blocks;
+  auto units_of = [&](int b) { return FewUnits(a.held, a.nodes, b, lo_rows); };
+
+  // This warp's run of all units.
+  auto scan = [&](int b0, long long& mine) {
+    mine = b0 + lane < a.batch ? (long long)units_of(b0 + lane).count() * per_set : 0;
+    long long sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    return sum;
+  };
+  const int me = blockIdx.x * kFewWarps + warp;
+  long long all = 0, mine;
+#pragma unroll 1
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    const long long sum = scan(b0, mine);
+    if (me == 0 && b0 + lane < a.batch) p.prefix[b0 + lane] = all + sum - mine;
+    all += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (me == 0 && lane == 0) p.prefix[a.batch] = all;
+  const Runs runs(all, gridDim.x * kFewWarps, kFewLeast);
+  if (me >= runs.n) return;
+  const long long from = runs.first(me), to = runs.first(me + 1);
+  long long start = 0;  // units before the item
+  int b = 0, in_set = 0;
+#pragma unroll 1
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    const long long sum = scan(b0, mine), total = __shfl_sync(0xffffffffu, sum, 31);
+    if (from < start + total) {
+      const int at = __ffs(__ballot_sync(0xffffffffu, start + sum > from)) - 1;
+      b = b0 + at;
+      start += __shfl_sync(0xffffffffu, sum - mine, at);
+      const int count = units_of(b).count();
+      in_set = (int)((from - start) / count);
+      start += (long long)in_set * count;
+      break;
+    }
+    start += total;
+  }
+
+  // The unit that is asked for next: its place, and the stage it goes to.
+  struct Place {
+    int b, in_set, u;
+    FewUnits n;
+  };
+  long long left_to_ask = to - from;
+  Place ask = {b, in_set, (int)(from - start), units_of(b)};
+  int ask_stage = 0, stage = 0;    // of the unit asked for next, of the one worked on next
+  uint32_t parity = 0, copies = 0; // per stage: of the copy taken next; whether the unit in it was copied
+  auto ask_next = [&]() {
+    if (left_to_ask == 0) return;
+    --left_to_ask;
+    const int s = ask_stage, bh = ask.b * a.heads_kv + ask.in_set / p.row_blocks;
+    ask_stage = s + 1 == kFewStages ? 0 : s + 1;
+    const uint32_t at = stages + s * kFewStage, bar = bars + 8 * s;
+    copies = (copies & ~(1u << s)) | (ask.u >= ask.n.nodes ? 1u << s : 0u);
+    if (lane == 0 && ask.u >= ask.n.nodes) {
+      if (ask.u < ask.n.nodes + ask.n.hi) {
+        const int row = bh * a.hi_stride + 16 * (ask.u - ask.n.nodes);
+        mbar_arrive_expect_tx(bar, kFewStage);
+        tma_load_2d(at, &p.map_k_hi, 0, row, bar);
+        tma_load_2d(at + 2048, &p.map_k_hi, 64, row, bar);
+        tma_load_2d(at + 4096, &p.map_v_hi, 0, row, bar);
+        tma_load_2d(at + 6144, &p.map_v_hi, 64, row, bar);
+      } else {
+        const int r0 = (ask.u - ask.n.nodes - ask.n.hi) * lo_rows;
+        const int rows = min(lo_rows, (a.held.lo(ask.b) - r0 + 15) & ~15);  // (a multiple of 16: lo_cap is one)
+        const size_t row = (size_t)bh * a.lo_cap + r0;
+        const uint32_t codes = rows * 16 * BITS, params = rows * U.row_bytes;
+        mbar_arrive_expect_tx(bar, 2 * (codes + params));
+        bulk_load(at, a.k_codes + row * 16 * BITS, codes, bar);
+        bulk_load(at + U.v, a.v_codes + row * 16 * BITS, codes, bar);
+        bulk_load(at + U.kp, reinterpret_cast<const char*>(a.k_params) + row * U.row_bytes, params, bar);
+        bulk_load(at + U.vp, reinterpret_cast<const char*>(a.v_params) + row * U.row_bytes, params, bar);
+      }
+    }
+    if (++ask.u == ask.n.count()) {
+      ask.u = 0;
+      if (++ask.in_set == per_set) {
+        ask.in_set = 0;
+        if (++ask.b < a.batch) ask.n = units_of(ask.b);
+      }
+    }
+  };
+#pragma unroll 1
+  for (int i = 1; i < kFewStages; ++i) ask_next();
+
+  constexpr float kDrop = flash::ref_drop<true>(), kSlack = flash::ref_slack<true>();
+  const float scale = a.sm_scale * kLog2e;
+  long long at_unit = from;
+  bool ok = true;
+#pragma unroll 1
+  while (ok && at_unit < to) {  // an item
+    const FewUnits n = units_of(b);
+    const int count = n.count(), u0 = (int)(at_unit - start), u1 = (int)min((long long)count, to - start);
+    const int h = in_set / p.row_blocks, block = in_set - h * p.row_blocks, bh = b * a.heads_kv + h;
+    const int n_hi = a.held.hi(b), n_lo = a.held.lo(b), free_slot = a.held.free_slot(bh, n_hi);
+    const bool fine = n_lo <= kFineRows;
+    // rows g and g + 8 of this lane
+    int node[2], head[2];
+    bool there[2], real[2];
+    const __nv_bfloat16* query[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int R = block * kFewRows + g + 8 * r;
+      there[r] = R < p.rows;
+      node[r] = there[r] ? R >> p.log2_G : 0;
+      head[r] = h * a.G + (R & (a.G - 1));
+      const uint32_t word = reinterpret_cast<const uint32_t*>(a.masks + (size_t)b * a.nodes + node[r])[node[r] >> 5];
+      real[r] = there[r] && (word >> (node[r] & 31) & 1);
+      query[r] = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + head[r] * a.q.h + node[r] * a.q.t;
+    }
+    float o[16][4], ref[2], sum[2] = {0.f, 0.f}, scale_lo[2] = {0.f, 0.f};
+    bool poisoned[2] = {false, false};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+    ref[0] = real[0] ? -INFINITY : 0.f, ref[1] = real[1] ? -INFINITY : 0.f;
+    uint32_t q[8][4], q2[8][4];  // the queries as A operands; the second terms (retained rows)
+    int form = -1;               // what q holds: 0 bf16 for nodes and slots, 1 fp16 for retained rows
+
+    // Weights of a block's scores s (columns: tokens 2 t, 2 t + 1 of both halves, for rows g and g + 8), packed as the A
+    // operand; see(i, row): whether the row sees the token of column i. A reference that is missing or too low moves.
+    auto weigh = [&](float (&s)[2][4], const float (&sc)[2], bool masked, auto see, uint32_t (&pk)[4], auto f16) {
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!see(2 * i + (e & 1), e >> 1)) s[i][e] = -INFINITY;
+      }
+      float top[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        top[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1])) * sc[r];
+      if (__any_sync(0xffffffffu, top[0] > ref[0] + kSlack || top[1] > ref[1] + kSlack)) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float x = top[r];
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+          const float next = x > ref[r] + kSlack ? x - kDrop : ref[r];
+          const float f = ref[r] == -INFINITY ? 0.f : fast_exp2(ref[r] - next);
+          sum[r] *= f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[i][2 * r] *= f, o[i][2 * r + 1] *= f;
+          ref[r] = next;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float less = ref[r] == -INFINITY ? 0.f : -ref[r];
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = fast_exp2(fmaf(s[i >> 1][2 * r + (i & 1)], sc[r], less));
+        sum[r] += (w[0] + w[1]) + (w[2] + w[3]);
+        pk[r] = flash::pack16<decltype(f16)::value>(w[0], w[1]);
+        pk[2 + r] = flash::pack16<decltype(f16)::value>(w[2], w[3]);
+      }
+    };
+
+#pragma unroll 1
+    for (int u = u0; ok && u < u1; ++u) {
+      ask_next();
+      const int s = stage;
+      stage = s + 1 == kFewStages ? 0 : s + 1;
+      const uint32_t at = stages + s * kFewStage;
+      if (copies >> s & 1) {
+        ok = mbar_wait(bars + 8 * s, parity >> s & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        parity ^= 1u << s;
+        if (!ok) break;
+      }
+      if (u < n.nodes + n.hi) {  // bf16 keys and values: [K | V][64 channels][16 rows of 128 bytes], swizzled
+        const bool is_node = u < n.nodes;
+        if (form != 0) {
+          form = 0;
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {  // 16 bytes: steps 2 i and 2 i + 1
+              uint4 x = make_uint4(0u, 0u, 0u, 0u);
+              if (real[r]) x = __ldg(reinterpret_cast<const uint4*>(query[r] + 64 * (i >> 1) + 8 * (2 * t + (i & 1))));
+              q[2 * i][r] = x.x, q[2 * i][2 + r] = x.y, q[2 * i + 1][r] = x.z, q[2 * i + 1][2 + r] = x.w;
+            }
+        }
+        const int first = 16 * (is_node ? u : u - n.nodes);
+        uint32_t seen[2] = {0xffffu, 0xffffu};  // of the 16 keys, by rows g and g + 8
+        bool masked = false;
+        if (is_node) {  // staged here: rows of padding as zeros, and those that hold an infinity or NaN
+          uint32_t bad = 0;
+          const int row = lane >> 1;  // two lanes to a node, eight chunks of 16 bytes of its key and of its value each
+          const int j = first + row;
+          bool node_real = false;
+          if (j < a.nodes)
+            node_real = reinterpret_cast<const uint32_t*>(a.masks + (size_t)b * a.nodes + j)[j >> 5] >> (j & 31) & 1;
+          uint4 x[8];
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            const TreeView& view = kv ? a.v : a.k;
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(view.p) + b * view.b + h * view.h + j * view.t) + 8 * (lane & 1);
+            bool is_bad = false;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) x[c] = node_real ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
+            if (kv) {
+#pragma unroll
+              for (int c = 0; c < 8; ++c) is_bad |= flash::any_nonfinite<false>(x[c]);
+              is_bad |= __shfl_xor_sync(0xffffffffu, (int)is_bad, 1) != 0;
+              bad = __ballot_sync(0xffffffffu, is_bad);  // two bits to a node
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              const uint4 y = is_bad ? make_uint4(0u, 0u, 0u, 0u) : x[c];
+              sts128(at + 4096 * kv + 2048 * (lane & 1) + row * 128 + ((c ^ (row & 7)) << 4), y.x, y.y, y.z, y.w);
+            }
+          }
+          asm volatile("" ::: "memory");
+          masked = true;
+          uint32_t bad16 = 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) bad16 |= (bad >> (2 * i) & 1u) << i;
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const uint32_t word = reinterpret_cast<const uint32_t*>(a.masks + (size_t)b * a.nodes + node[r])[u >> 1];
+            seen[r] = real[r] ? (word >> (16 * (u & 1))) & 0xffffu : 0u;
+            poisoned[r] |= (seen[r] & bad16) != 0u;
+          }
+        } else {
+          const int left = n_hi - first;
+          uint32_t live = left >= 16 ? 0xffffu : (1u << left) - 1u;
+          if (free_slot >= first && free_slot < first + 16) live &= ~(1u << (free_slot - first));
+          seen[0] = seen[1] = live;
+          masked = live != 0xffffu;
+          if (masked) {  // values of slots that hold nothing: any bits
+            const int row = lane >> 1;
+            if (!(live >> row & 1)) {
+#pragma unroll
+              for (int c = 0; c < 8; ++c) flash::sts128_zero(at + 4096 + 2048 * (lane & 1) + row * 128 + (c << 4));
+            }
+          }
+        }
+        __syncwarp();
+        float sc[2][4] = {}, sc2[2][4] = {};  // (chains of MMAs: an MMA waits 30 clocks for the one it adds to)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t k[4];
+            lds_vec(at + 2048 * (i >> 1) + (8 * half + g) * 128 + (((2 * t + (i & 1)) ^ g) << 4), k);
+            mma_bf16(sc[half], q[2 * i], k[0], k[1]);
+            mma_bf16(sc2[half], q[2 * i + 1], k[2], k[3]);
+          }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[half][e] += sc2[half][e];
+        uint32_t pk[4];
+        const float c2[2] = {scale, scale};
+        weigh(sc, c2, masked, [&](int i, int r) { return seen[r] >> (8 * (i >> 1) + 2 * t + (i & 1)) & 1; }, pk, std::false_type{});
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {  // 16 channels: two n-blocks
+          uint32_t v[4];
+          const int row = (lane & 7) + 8 * ((lane >> 3) & 1), c = 2 * i + (lane >> 4);
+          ldsm_x4_t(at + 4096 + 2048 * (c >> 3) + row * 128 + (((c & 7) ^ (row & 7)) << 4), v);
+          mma_bf16(o[2 * i], pk, v[0], v[1]);
+          mma_bf16(o[2 * i + 1], pk, v[2], v[3]);
+        }
+        if (masked) fence_async();  // (the stage was written here; a copy comes next)
+      } else {  // codes
+        if (form != 1) {
+          form = 1;
+          float x[2][8][4], top[2] = {0.f, 0.f};
+#pragma unroll
+          for (int m = 0; m < 8; ++m) {
+            float4 inv = make_float4(1.f, 1.f, 1.f, 1.f);
+            if (a.balancer) {
+              const float4 bal = __ldg(reinterpret_cast<const float4*>(a.balancer + h * kHeadDim + 16 * m + 4 * t));
+              inv = make_float4(1.f / bal.x, 1.f / bal.y, 1.f / bal.z, 1.f / bal.w);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              uint2 raw = make_uint2(0u, 0u);
+              if (real[r]) raw = __ldg(reinterpret_cast<const uint2*>(query[r] + 16 * m + 4 * t));
+              x[r][m][0] = __uint_as_float(raw.x << 16) * inv.x, x[r][m][1] = __uint_as_float(raw.x & 0xffff0000u) * inv.y;
+              x[r][m][2] = __uint_as_float(raw.y << 16) * inv.z, x[r][m][3] = __uint_as_float(raw.y & 0xffff0000u) * inv.w;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) top[r] = fmaxf(top[r], fabsf(x[r][m][e]));
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+            const int e2 = min(max((int)(__float_as_uint(top[r]) >> 23) - 127, -100), 120) - 14;
+            const float down = __uint_as_float((uint32_t)(127 - e2) << 23);
+            scale_lo[r] = scale * __uint_as_float((uint32_t)(127 + e2) << 23);
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float y0 = x[r][m][2 * e] * down, y1 = x[r][m][2 * e + 1] * down;
+                const __half2 near = __floats2half2_rn(y0, y1);
+                const float2 f = __half22float2(near);
+                q[m][2 * e + r] = h2_as_u32(near);
+                q2[m][2 * e + r] = pack_f16(y0 - f.x, y1 - f.y);
+              }
+          }
+        }
+        const int r0 = (u - n.nodes - n.hi) * lo_rows, blocks = min(U.blocks, (n_lo - r0 + 15) >> 4);
+        constexpr int kPitch = 16 * BITS;
+        // rows of a block in the order of the operand's columns: 2 t and 2 t + 1 are t and t + 4
+        const int krow = (g >> 1) + 4 * (g & 1);
+#pragma unroll 1
+        for (int blk = 0; blk < blocks; ++blk) {
+          const int valid = n_lo - (r0 + 16 * blk);  // rows of the block
+          const uint32_t kc = at + blk * 16 * kPitch, kp = at + U.kp + blk * 16 * U.row_bytes;
+          float sc[2][4] = {};
+          auto scores = [&](auto with_rest) {
+            float part[2][4][4] = {};  // chains of MMAs by the half, the query's term and the parity of m
+            uint2 x[2], y[2];
+            uint32_t pr[2][PAIRS];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const int row = 8 * half + krow;
+              x[half] = lds64(kc + row * kPitch + 8 * t);
+              y[half] = make_uint2(0u, 0u);
+              if constexpr (BITS == 4) y[half] = lds64(kc + row * kPitch + 32 + 8 * t);
+              if constexpr (BITS == 3) {
+                y[half] = lds64(kc + row * kPitch + 32 + 8 * (t & 1));
+                y[half].x >>= t >> 1, y[half].y >>= t >> 1;
+              }
+              load_pairs(kp + row * U.row_bytes, pr[half]);
+            }
+            const FieldOf<BITS> f[2][2] = {{FieldOf<BITS>(x[0].x, y[0].x), FieldOf<BITS>(x[0].y, y[0].y)},
+                                           {FieldOf<BITS>(x[1].x, y[1].x), FieldOf<BITS>(x[1].y, y[1].y)}};
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                const __half2 ab = u32_as_h2(pr[half][m / kOf]), al = __low2half2(ab), be = __high2half2(ab);
+                const __half2 c0 = f[half][0].code(m), c1 = f[half][1].code(m);
+                const uint32_t k0 = h2_as_u32(__hfma2(c0, al, be)), k1 = h2_as_u32(__hfma2(c1, al, be));
+                mma_f16(part[half][m & 1], q[m], k0, k1);
+                mma_f16(part[half][2 + (m & 1)], q2[m], k0, k1);
+                if constexpr (decltype(with_rest)::value) {
+                  const float2 af = __half22float2(ab), d0 = __half22float2(c0), d1 = __half22float2(c1);
+                  const float2 n0 = __half22float2(u32_as_h2(k0)), n1 = __half22float2(u32_as_h2(k1));
+                  mma_f16(part[half][2 + (m & 1)], q[m], pack_f16(fmaf(af.x, d0.x, af.y) - n0.x, fmaf(af.x, d0.y, af.y) - n0.y),
+                          pack_f16(fmaf(af.x, d1.x, af.y) - n1.x, fmaf(af.x, d1.y, af.y) - n1.y));
+                }
+              }
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                sc[half][e] = (part[half][0][e] + part[half][1][e]) + (part[half][2][e] + part[half][3][e]);
+          };
+          if (fine)
+            scores(std::true_type{});
+          else
+            scores(std::false_type{});
+          uint32_t pk[4];
+          const bool masked = valid < 16;
+          weigh(sc, scale_lo, masked, [&](int i, int) { return 8 * (i >> 1) + t + 4 * (i & 1) < valid; }, pk, std::true_type{});
+          // values: of tokens 2 t, 2 t + 1 of both halves, the channels 16 m + 8 jj + g
+          const uint32_t vc = at + U.v + blk * 16 * kPitch, vp = at + U.vp + blk * 16 * U.row_bytes;
+          __half2 al[2][PAIRS], be[2][PAIRS];  // of both tokens of an operand register, by its half
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t pa[PAIRS], pb[PAIRS];
+            const int ra = 8 * half + t, rb = ra + 4;
+            load_pairs(vp + ra * U.row_bytes, pa);
+            load_pairs(vp + rb * U.row_bytes, pb);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+              if (masked) pa[i] = ra < valid ? pa[i] : 0u, pb[i] = rb < valid ? pb[i] : 0u;  // (rows behind the last: any bits)
+              al[half][i] = u32_as_h2(prmt(pa[i], pb[i], 0x5410u));
+              be[half][i] = u32_as_h2(prmt(pa[i], pb[i], 0x7632u));
+            }
+          }
+          const uint32_t sel = g & 1 ? 0x7632u : 0x5410u, rows[4] = {vc + t * kPitch, vc + (t + 4) * kPitch,
+                                                                     vc + (t + 8) * kPitch, vc + (t + 12) * kPitch};
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj) {
+            const uint32_t wo = 16 * jj + 4 * (g >> 1), wt = 32 + 4 * (g >> 1);
+            auto words = [&](int half) {
+              const uint32_t ra = rows[2 * half], rb = rows[2 * half + 1];
+              const uint32_t x = prmt(lds32v(ra + wo), lds32v(rb + wo), sel);
+              uint32_t y = 0;
+              if constexpr (BITS == 4) y = prmt(lds32v(ra + 32 + wo), lds32v(rb + 32 + wo), sel);
+              if constexpr (BITS == 3) y = prmt(lds32v(ra + wt), lds32v(rb + wt), sel) >> jj;
+              return FieldOf<BITS>(x, y);
+            };
+            const FieldOf<BITS> f0 = words(0), f1 = words(1);
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+              mma_f16(o[2 * m + jj], pk, h2_as_u32(__hfma2(f0.code(m), al[0][m / kOf], be[0][m / kOf])),
+                      h2_as_u32(__hfma2(f1.code(m), al[1][m / kOf], be[1][m / kOf])));
+          }
+        }
+      }
+      __syncwarp();  // (the stage may be filled again)
+    }
+    if (!ok) break;
+
+    // Output: rows g and g + 8, channels 8 i + 2 t and the next of every n-block i.
+    const bool whole = u0 == 0 && u1 == count;
+    const int slot = 2 * me + (u0 == 0);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float total = sum[r];
+      total += __shfl_xor_sync(0xffffffffu, total, 1);
+      total += __shfl_xor_sync(0xffffffffu, total, 2);
+      const bool blank = !real[r] || total == 0.f;
+      const float lse2 = blank ? -INFINITY : ref[r] + log2f(total);
+      const float f = poisoned[r] ? __int_as_float(0x7fffffff) : 1.f / total;
+      if (!there[r]) continue;
+      if (whole) {
+        const long long out = b * a.out.b + head[r] * a.out.h + node[r] * a.out.t + 2 * t;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = blank ? 0.f : o[i][2 * r] * f, y = blank ? 0.f : o[i][2 * r + 1] * f;
+          if (a.out_f32)
+            *reinterpret_cast<float2*>(static_cast<float*>(a.out.p) + out + 8 * i) = make_float2(x, y);
+          else
+            *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.out.p) + out + 8 * i) = pack_bf16(x, y);
+        }
+        if (a.lse && t == 0) a.lse[((size_t)b * a.heads_q + head[r]) * a.nodes + node[r]] = lse2 * kLn2;
+      } else {
+        float* part = p.part_o + ((size_t)slot * kFewRows + g + 8 * r) * kHeadDim + 2 * t;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          *reinterpret_cast<float2*>(part + 8 * i) =
+              make_float2(blank ? 0.f : o[i][2 * r] * f, blank ? 0.f : o[i][2 * r + 1] * f);
+        if (t == 0) p.part_lse[(size_t)slot * kFewRows + g + 8 * r] = lse2;
+      }
+    }
+    at_unit = start + u1;
+    if (u1 == count) {
+      start += count;
+      if (++in_set == per_set) in_set = 0, ++b;
+    }
+  }
+  if (!ok && lane == 0) {
+    record_error(a.status, kErrFullTimeout);
+    // no copy may outlive the CTA
+    for (int s = 0; s < kFewStages; ++s)
+      if (copies >> s & 1) mbar_wait(bars + 8 * s, parity >> s & 1);
+  }
+}
+
+template <int BITS, int PAIRS>
+cudaError_t launch_few_pairs(const TreeFewArgs& p, int grid, cudaStream_t st) {
+  constexpr int kSmem = 1024 + kFewWarps * kFewStages * kFewStage;
+  static std::atomic<uint64_t> configured;  // one bit per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  auto kernel = tree_few_kernel<BITS, PAIRS>;
+  if (dev > 63 || !(configured.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    configured.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch_chained(kernel, dim3(grid), dim3(32 * kFewWarps), kSmem, st, p);
+}
+
+template <int BITS>
+cudaError_t launch_few_variant(const TreeFewArgs& p, int grid, cudaStream_t st) {
+  return p.a.group == 32   ? launch_few_pairs<BITS, 4>(p, grid, st)
+         : p.a.group == 64 ? launch_few_pairs<BITS, 2>(p, grid, st)
+                           : launch_few_pairs<BITS, 1>(p, grid, st);
+}
+
+}  // namespace tree
+}  // namespace mikv

@@ -128,11 +128,11 @@ struct Tiles {
   }
 };
 
-// CTA c has the costs [first(c), first(c + 1)) of all.
+// CTA (or warp) c has the costs [first(c), first(c + 1)) of all.
 struct Runs {
   long long total;
   int n;
-  __device__ Runs(long long total, int ctas) : total(total), n((int)max(1ll, min((long long)ctas, total / kLeastRun))) {}
+  __device__ Runs(long long total, int ctas, int least = kLeastRun) : total(total), n((int)max(1ll, min((long long)ctas, total / least))) {}
   __device__ long long first(int c) const { return total * c / n; }  // (total * n stays far below 2^63)
   __device__ int owner(long long x) const {
     int c = (int)min((long long)n - 1, x * n / total);
