@@ -47,7 +47,7 @@ struct TreeMergeArgs {
   TreeArgs a;
   const long long* prefix;
   const float *part_o, *part_lse;
-  int m_blocks, log2_G, item_rows, ctas, lo_rows;
+  int m_blocks, log2_G, item_rows, ctas, lo_blocks;
 };
 
 // How an item's units lie in the runs: key tiles by their costs, or the units of few rows, one like another.
@@ -60,13 +60,13 @@ struct TileRuns {
   __device__ bool part(long long from, long long to) const { return tl.first(from) < tl.first(to); }
 };
 struct FewRuns {
-  int count;
+  tree::FewUnits n;
   Runs runs;
   __device__ FewRuns(const TreeMergeArgs& m, int b)
-      : count(tree::FewUnits(m.a.held, m.a.nodes, b, m.lo_rows).count()), runs(m.prefix[m.a.batch], m.ctas, tree::kFewLeast) {}
-  __device__ long long cost() const { return count; }
-  __device__ long long last() const { return count - 1; }
-  __device__ bool part(long long from, long long to) const { return max(from, 0ll) < min(to, (long long)count); }
+      : n(m.a.held, m.a.nodes, b, m.lo_blocks), runs(m.prefix[m.a.batch], m.ctas, tree::kFewLeast) {}
+  __device__ long long cost() const { return n.cost(); }
+  __device__ long long last() const { return n.before(n.count() - 1); }
+  __device__ bool part(long long from, long long to) const { return n.first(from) < n.first(to); }
 };
 
 // The parts of an output row, weighted by 2^(lse - largest): a warp to a row. Rows whose item one CTA had are written.
@@ -221,9 +221,9 @@ cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t s
                                         : launch_tree_few<4>(p, num_sms, st);
     if (e != cudaSuccess) return e;
     m.ctas = num_sms * tree::kFewWarps;
-    m.lo_rows = 16 * (a.bits == 2   ? tree::FewUnit<2>(a.group).blocks
-                      : a.bits == 3 ? tree::FewUnit<3>(a.group).blocks
-                                    : tree::FewUnit<4>(a.group).blocks);
+    m.lo_blocks = a.bits == 2   ? tree::FewUnit<2>(a.group).blocks
+                  : a.bits == 3 ? tree::FewUnit<3>(a.group).blocks
+                                : tree::FewUnit<4>(a.group).blocks;
     return launch_chained(tree_merge_kernel<FewRuns>, merge_grid, dim3(128), 0, st, m);
   }
   TreeKernelArgs p;

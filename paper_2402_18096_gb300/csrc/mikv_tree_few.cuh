@@ -55,13 +55,21 @@ struct FewUnit {
   }
 };
 
-// Units of a request's items: nodes, slots, retained rows.
+// Units of a request's items: nodes, slots, retained rows; and their costs for the runs, one for 16 tokens of any kind (a
+// block of codes takes as many instructions as two of slots, which take three times its bytes from HBM).
 struct FewUnits {
-  int nodes, hi, lo;
-  __device__ FewUnits() : nodes(0), hi(0), lo(0) {}
-  __device__ FewUnits(const HeldArgs& held, int n_nodes, int b, int lo_rows)
-      : nodes((n_nodes + 15) / 16), hi((held.hi(b) + 15) / 16), lo((held.lo(b) + lo_rows - 1) / lo_rows) {}
+  int nodes, hi, lo, blocks;  // blocks: cost of a unit of retained rows
+  __device__ FewUnits(const HeldArgs& held, int n_nodes, int b, int lo_blocks)
+      : nodes((n_nodes + 15) / 16), hi((held.hi(b) + 15) / 16), lo((held.lo(b) + 16 * lo_blocks - 1) / (16 * lo_blocks)),
+        blocks(lo_blocks) {}
   __device__ int count() const { return nodes + hi + lo; }
+  __device__ long long before(int u) const { return (long long)min(u, nodes + hi) + (long long)blocks * max(0, u - nodes - hi); }
+  __device__ long long cost() const { return before(count()); }
+  // the first unit that begins at x or later
+  __device__ int first(long long x) const {
+    if (x <= 0) return 0;
+    return (int)min((long long)count(), x <= nodes + hi ? x : nodes + hi + (x - nodes - hi + blocks - 1) / blocks);
+  }
 };
 
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
@@ -127,11 +135,11 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
   const FewUnit<BITS> U(kHeadDim / PAIRS);
   constexpr int kOf = 8 / PAIRS;  // fields of 16 channels to a pair of parameters
   const int lo_rows = 16 * U.blocks, per_set = a.heads_kv * p.row_blocks;
-  auto units_of = [&](int b) { return FewUnits(a.held, a.nodes, b, lo_rows); };
+  auto units_of = [&](int b) { return FewUnits(a.held, a.nodes, b, U.blocks); };
 
   // This warp's run of all units.
   auto scan = [&](int b0, long long& mine) {
-    mine = b0 + lane < a.batch ? (long long)units_of(b0 + lane).count() * per_set : 0;
+    mine = b0 + lane < a.batch ? units_of(b0 + lane).cost() * per_set : 0;
     long long sum = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -152,7 +160,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
   const Runs runs(all, gridDim.x * kFewWarps, kFewLeast);
   if (me >= runs.n) return;
   const long long from = runs.first(me), to = runs.first(me + 1);
-  long long start = 0;  // units before the item
+  long long start = 0;  // costs before the item
   int b = 0, in_set = 0;
 #pragma unroll 1
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
@@ -161,9 +169,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
       const int at = __ffs(__ballot_sync(0xffffffffu, start + sum > from)) - 1;
       b = b0 + at;
       start += __shfl_sync(0xffffffffu, sum - mine, at);
-      const int count = units_of(b).count();
-      in_set = (int)((from - start) / count);
-      start += (long long)in_set * count;
+      const long long cost = units_of(b).cost();
+      in_set = (int)((from - start) / cost);
+      start += in_set * cost;
       break;
     }
     start += total;
@@ -174,13 +182,22 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
     int b, in_set, u;
     FewUnits n;
   };
-  long long left_to_ask = to - from;
-  Place ask = {b, in_set, (int)(from - start), units_of(b)};
+  long long ask_start = start;  // costs before its item
+  Place ask = {b, in_set, 0, units_of(b)};
+  ask.u = ask.n.first(from - start);
+  bool more = ask_start + ask.n.before(ask.u) < to;
   int ask_stage = 0, stage = 0;    // of the unit asked for next, of the one worked on next
   uint32_t parity = 0, copies = 0; // per stage: of the copy taken next; whether the unit in it was copied
+  auto next_ask_item = [&]() {
+    ask_start += ask.n.cost();
+    ask.u = 0;
+    if (++ask.in_set == per_set) {
+      ask.in_set = 0;
+      if (++ask.b < a.batch) ask.n = units_of(ask.b);
+    }
+  };
   auto ask_next = [&]() {
-    if (left_to_ask == 0) return;
-    --left_to_ask;
+    if (!more) return;
     const int s = ask_stage, bh = ask.b * a.heads_kv + ask.in_set / p.row_blocks;
     ask_stage = s + 1 == kFewStages ? 0 : s + 1;
     const uint32_t at = stages + s * kFewStage, bar = bars + 8 * s;
@@ -205,25 +222,28 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
         bulk_load(at + U.vp, reinterpret_cast<const char*>(a.v_params) + row * U.row_bytes, params, bar);
       }
     }
-    if (++ask.u == ask.n.count()) {
-      ask.u = 0;
-      if (++ask.in_set == per_set) {
-        ask.in_set = 0;
-        if (++ask.b < a.batch) ask.n = units_of(ask.b);
-      }
-    }
+    if (++ask.u == ask.n.count()) next_ask_item();
+    more = ask.b < a.batch && ask_start + ask.n.before(ask.u) < to;
   };
+  if (ask.u == ask.n.count()) {  // (the run begins within the item's last unit)
+    next_ask_item();
+    more = ask.b < a.batch && ask_start < to;
+  }
 #pragma unroll 1
   for (int i = 1; i < kFewStages; ++i) ask_next();
 
   constexpr float kDrop = flash::ref_drop<true>(), kSlack = flash::ref_slack<true>();
   const float scale = a.sm_scale * kLog2e;
-  long long at_unit = from;
   bool ok = true;
 #pragma unroll 1
-  while (ok && at_unit < to) {  // an item
+  for (; ok && start < to; ) {  // an item
     const FewUnits n = units_of(b);
-    const int count = n.count(), u0 = (int)(at_unit - start), u1 = (int)min((long long)count, to - start);
+    const int count = n.count(), u0 = n.first(from - start), u1 = n.first(to - start);
+    if (u0 == u1) {  // (none of its units begins in this run)
+      start += n.cost();
+      if (++in_set == per_set) in_set = 0, ++b;
+      continue;
+    }
     const int h = in_set / p.row_blocks, block = in_set - h * p.row_blocks, bh = b * a.heads_kv + h;
     const int n_hi = a.held.hi(b), n_lo = a.held.lo(b), free_slot = a.held.free_slot(bh, n_hi);
     const bool fine = n_lo <= kFineRows;
@@ -568,11 +588,8 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
         if (t == 0) p.part_lse[(size_t)slot * kFewRows + g + 8 * r] = lse2;
       }
     }
-    at_unit = start + u1;
-    if (u1 == count) {
-      start += count;
-      if (++in_set == per_set) in_set = 0, ++b;
-    }
+    start += n.cost();
+    if (++in_set == per_set) in_set = 0, ++b;
   }
   if (!ok && lane == 0) {
     record_error(a.status, kErrFullTimeout);
