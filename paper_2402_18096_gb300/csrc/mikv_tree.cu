@@ -164,15 +164,19 @@ bool encode_rows(CUtensorMap* map, const void* data, int dims, const long long (
 constexpr int kFewMost = 16;
 
 struct Sizes {
-  bool few, pair;
+  bool few, narrow, pair;
   int rows, item_rows, m_blocks;
   Sizes(int G, int nodes) : rows(G * nodes) {
     few = rows <= kFewMost;
+    narrow = rows <= 8;
     pair = rows > tree::kTile;
     item_rows = few ? tree::kFewRows : pair ? 2 * tree::kTile : tree::kTile;
     m_blocks = (rows + item_rows - 1) / item_rows;
   }
-  size_t parts(int num_sms) const { return (size_t)2 * num_sms * (few ? tree::kFewWarps : 1); }
+  int runs(int num_sms) const {
+    return num_sms * (!few ? 1 : narrow ? tree::FewShape<true>::kWarps : tree::FewShape<false>::kWarps);
+  }
+  size_t parts(int num_sms) const { return (size_t)2 * runs(num_sms); }
 };
 
 size_t prefix_bytes(int batch) { return ((batch + 1) * sizeof(long long) + 255) / 256 * 256; }
@@ -216,11 +220,11 @@ cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t s
     p.a = a;
     p.rows = z.rows, p.row_blocks = z.m_blocks, p.log2_G = log2_G;
     p.prefix = prefix, p.part_o = part_o, p.part_lse = part_lse;
-    const cudaError_t e = a.bits == 2   ? launch_tree_few<2>(p, num_sms, st)
-                          : a.bits == 3 ? launch_tree_few<3>(p, num_sms, st)
-                                        : launch_tree_few<4>(p, num_sms, st);
+    const cudaError_t e = a.bits == 2   ? launch_tree_few<2>(p, z.narrow, num_sms, st)
+                          : a.bits == 3 ? launch_tree_few<3>(p, z.narrow, num_sms, st)
+                                        : launch_tree_few<4>(p, z.narrow, num_sms, st);
     if (e != cudaSuccess) return e;
-    m.ctas = num_sms * tree::kFewWarps;
+    m.ctas = z.runs(num_sms);
     m.lo_blocks = a.bits == 2   ? tree::FewUnit<2>(a.group).blocks
                   : a.bits == 3 ? tree::FewUnit<3>(a.group).blocks
                                 : tree::FewUnit<4>(a.group).blocks;

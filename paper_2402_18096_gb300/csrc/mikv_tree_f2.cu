@@ -5,8 +5,8 @@
 namespace mikv {
 
 template <>
-cudaError_t launch_tree_few<2>(const TreeFewArgs& p, int grid, cudaStream_t st) {
-  return tree::launch_few_variant<2>(p, grid, st);
+cudaError_t launch_tree_few<2>(const TreeFewArgs& p, bool narrow, int grid, cudaStream_t st) {
+  return narrow ? tree::launch_few_variant<2, true>(p, grid, st) : tree::launch_few_variant<2, false>(p, grid, st);
 }
 
 }  // namespace mikv

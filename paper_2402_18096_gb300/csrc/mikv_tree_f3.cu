@@ -4,8 +4,8 @@
 namespace mikv {
 
 template <>
-cudaError_t launch_tree_few<3>(const TreeFewArgs& p, int grid, cudaStream_t st) {
-  return tree::launch_few_variant<3>(p, grid, st);
+cudaError_t launch_tree_few<3>(const TreeFewArgs& p, bool narrow, int grid, cudaStream_t st) {
+  return narrow ? tree::launch_few_variant<3, true>(p, grid, st) : tree::launch_few_variant<3, false>(p, grid, st);
 }
 
 }  // namespace mikv

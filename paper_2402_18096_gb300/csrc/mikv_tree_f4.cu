@@ -4,8 +4,8 @@
 namespace mikv {
 
 template <>
-cudaError_t launch_tree_few<4>(const TreeFewArgs& p, int grid, cudaStream_t st) {
-  return tree::launch_few_variant<4>(p, grid, st);
+cudaError_t launch_tree_few<4>(const TreeFewArgs& p, bool narrow, int grid, cudaStream_t st) {
+  return narrow ? tree::launch_few_variant<4, true>(p, grid, st) : tree::launch_few_variant<4, false>(p, grid, st);
 }
 
 }  // namespace mikv

@@ -34,11 +34,19 @@ struct TreeFewArgs {
 };
 
 template <int BITS>
-cudaError_t launch_tree_few(const TreeFewArgs& p, int grid, cudaStream_t st);
+cudaError_t launch_tree_few(const TreeFewArgs& p, bool narrow, int grid, cudaStream_t st);
 
 namespace tree {
 
-constexpr int kFewWarps = 8, kFewRows = 16, kFewStage = 8192, kFewStages = 3;
+constexpr int kFewRows = 16, kFewStage = 8192;  // rows of a part; bytes of a stage
+constexpr int kFewItem = 6;  // cost of an item beside its units (its queries, its output)
+
+// Narrow: up to 8 rows, which are the N side of the MMAs, and the tokens (scores) or channels (output) the M side. Half
+// the MMAs and half the registers of 16 rows as the M side, hence 12 warps on an SM and not 8.
+template <bool NARROW>
+struct FewShape {
+  static constexpr int kRows = NARROW ? 8 : 16, kWarps = NARROW ? 12 : 8, kStages = NARROW ? 2 : 3;
+};
 constexpr int kFewLeast = 2;  // units of a run at least
 
 // Blocks of 16 retained rows in a unit, and where its arrays lie in a stage.
@@ -63,11 +71,14 @@ struct FewUnits {
       : nodes((n_nodes + 15) / 16), hi((held.hi(b) + 15) / 16), lo((held.lo(b) + 16 * lo_blocks - 1) / (16 * lo_blocks)),
         blocks(lo_blocks) {}
   __device__ int count() const { return nodes + hi + lo; }
-  __device__ long long before(int u) const { return (long long)min(u, nodes + hi) + (long long)blocks * max(0, u - nodes - hi); }
+  __device__ long long before(int u) const {
+    return u == 0 ? 0 : kFewItem + (long long)min(u, nodes + hi) + (long long)blocks * max(0, u - nodes - hi);
+  }
   __device__ long long cost() const { return before(count()); }
   // the first unit that begins at x or later
   __device__ int first(long long x) const {
     if (x <= 0) return 0;
+    x = max(1ll, x - kFewItem);
     return (int)min((long long)count(), x <= nodes + hi ? x : nodes + hi + (x - nodes - hi + blocks - 1) / blocks);
   }
 };
@@ -119,8 +130,9 @@ __device__ __forceinline__ void load_pairs(uint32_t addr, uint32_t (&p)[PAIRS]) 
   }
 }
 
-template <int BITS, int PAIRS>
-__global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __grid_constant__ TreeFewArgs p) {
+template <int BITS, int PAIRS, bool NARROW>
+__global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_kernel(const __grid_constant__ TreeFewArgs p) {
+  constexpr int kFewWarps = FewShape<NARROW>::kWarps, kFewStages = FewShape<NARROW>::kStages, kRows = FewShape<NARROW>::kRows;
   const TreeArgs& a = p.a;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t s_bar[kFewWarps][kFewStages];
@@ -247,13 +259,14 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
     const int h = in_set / p.row_blocks, block = in_set - h * p.row_blocks, bh = b * a.heads_kv + h;
     const int n_hi = a.held.hi(b), n_lo = a.held.lo(b), free_slot = a.held.free_slot(bh, n_hi);
     const bool fine = n_lo <= kFineRows;
-    // rows g and g + 8 of this lane
+    // The lane's rows: g and g + 8, or (narrow) 2 t and 2 t + 1; the queries that it holds are those of rows g and g + 8, or
+    // (narrow) of row g alone.
     int node[2], head[2];
     bool there[2], real[2];
     const __nv_bfloat16* query[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int R = block * kFewRows + g + 8 * r;
+      const int R = block * kRows + (NARROW ? 2 * t + r : g + 8 * r);
       there[r] = R < p.rows;
       node[r] = there[r] ? R >> p.log2_G : 0;
       head[r] = h * a.G + (R & (a.G - 1));
@@ -261,53 +274,77 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
       real[r] = there[r] && (word >> (node[r] & 31) & 1);
       query[r] = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + head[r] * a.q.h + node[r] * a.q.t;
     }
-    float o[16][4], ref[2], sum[2] = {0.f, 0.f}, scale_lo[2] = {0.f, 0.f};
+    bool asks[2] = {real[0], real[1]};
+    if constexpr (NARROW) {
+      const int R = block * kRows + g, i = R < p.rows ? R >> p.log2_G : 0;
+      const uint32_t word = reinterpret_cast<const uint32_t*>(a.masks + (size_t)b * a.nodes + i)[i >> 5];
+      asks[0] = R < p.rows && (word >> (i & 31) & 1), asks[1] = false;
+      query[0] = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + (h * a.G + (R & (a.G - 1))) * a.q.h + i * a.q.t;
+    }
+    constexpr int kHeld = NARROW ? 1 : 2, kO = NARROW ? 8 : 16;
+    float o[kO][4], ref[2], sum[2] = {0.f, 0.f}, scale_lo[2] = {0.f, 0.f};
     bool poisoned[2] = {false, false};
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < kO; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
     ref[0] = real[0] ? -INFINITY : 0.f, ref[1] = real[1] ? -INFINITY : 0.f;
-    uint32_t q[8][4], q2[8][4];  // the queries as A operands; the second terms (retained rows)
+    uint32_t q[8][2 * kHeld], q2[8][2 * kHeld];  // the queries as operands; the second terms (retained rows)
     int form = -1;               // what q holds: 0 bf16 for nodes and slots, 1 fp16 for retained rows
 
-    // Weights of a block's scores s (columns: tokens 2 t, 2 t + 1 of both halves, for rows g and g + 8), packed as the A
-    // operand; see(i, row): whether the row sees the token of column i. A reference that is missing or too low moves.
+    // Weights of a block's scores s[half of the tokens][register], packed as the operand of the second product; see(half,
+    // parity, row): whether the row sees the token. The lane's tokens are 2 t + parity of a half, or (narrow) row g of a
+    // half. A reference that is missing or too low moves, and O with it.
     auto weigh = [&](float (&s)[2][4], const float (&sc)[2], bool masked, auto see, uint32_t (&pk)[4], auto f16) {
+      // (narrow: registers 0 and 1 are token g of the first half, rows 2 t and 2 t + 1; 2 and 3 token g of the second)
+      auto row_of = [](int half, int e) { return NARROW ? e & 1 : e >> 1; };
       if (masked) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < (NARROW ? 1 : 2); ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (!see(2 * i + (e & 1), e >> 1)) s[i][e] = -INFINITY;
+            if (!see(NARROW ? e >> 1 : i, e & 1, row_of(i, e))) s[i][e] = -INFINITY;
       }
       float top[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r)
-        top[r] = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1])) * sc[r];
+        top[r] = (NARROW ? fmaxf(s[0][r], s[0][2 + r])
+                         : fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1]))) * sc[r];
       if (__any_sync(0xffffffffu, top[0] > ref[0] + kSlack || top[1] > ref[1] + kSlack)) {
+        float f[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float x = top[r];
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-          const float next = x > ref[r] + kSlack ? x - kDrop : ref[r];
-          const float f = ref[r] == -INFINITY ? 0.f : fast_exp2(ref[r] - next);
-          sum[r] *= f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i][2 * r] *= f, o[i][2 * r + 1] *= f;
+          for (int off = NARROW ? 4 : 1; off < (NARROW ? 32 : 4); off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+          const float next = x > ref[r] + kSlack ? x - kDrop : ref[r];
+          f[r] = ref[r] == -INFINITY ? 0.f : fast_exp2(ref[r] - next);
+          sum[r] *= f[r];
           ref[r] = next;
         }
+#pragma unroll
+        for (int i = 0; i < kO; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][e] *= f[row_of(0, e)];
       }
+      float w[2][4];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float less = ref[r] == -INFINITY ? 0.f : -ref[r];
-        float w[4];
+        if constexpr (NARROW) {
+          w[0][r] = fast_exp2(fmaf(s[0][r], sc[r], less)), w[0][2 + r] = fast_exp2(fmaf(s[0][2 + r], sc[r], less));
+          sum[r] += w[0][r] + w[0][2 + r];
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = fast_exp2(fmaf(s[i >> 1][2 * r + (i & 1)], sc[r], less));
-        sum[r] += (w[0] + w[1]) + (w[2] + w[3]);
-        pk[r] = flash::pack16<decltype(f16)::value>(w[0], w[1]);
-        pk[2 + r] = flash::pack16<decltype(f16)::value>(w[2], w[3]);
+          for (int i = 0; i < 4; ++i) w[r][i] = fast_exp2(fmaf(s[i >> 1][2 * r + (i & 1)], sc[r], less));
+          sum[r] += (w[r][0] + w[r][1]) + (w[r][2] + w[r][3]);
+          pk[r] = flash::pack16<decltype(f16)::value>(w[r][0], w[r][1]);
+          pk[2 + r] = flash::pack16<decltype(f16)::value>(w[r][2], w[r][3]);
+        }
+      }
+      if constexpr (NARROW) {  // tokens g by rows 2 t, 2 t + 1, turned into rows g by tokens 2 t, 2 t + 1
+        pk[0] = movmatrix_t(flash::pack16<decltype(f16)::value>(w[0][0], w[0][1]));
+        pk[1] = movmatrix_t(flash::pack16<decltype(f16)::value>(w[0][2], w[0][3]));
       }
     };
 
@@ -328,12 +365,12 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
         if (form != 0) {
           form = 0;
 #pragma unroll
-          for (int r = 0; r < 2; ++r)
+          for (int r = 0; r < kHeld; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {  // 16 bytes: steps 2 i and 2 i + 1
               uint4 x = make_uint4(0u, 0u, 0u, 0u);
-              if (real[r]) x = __ldg(reinterpret_cast<const uint4*>(query[r] + 64 * (i >> 1) + 8 * (2 * t + (i & 1))));
-              q[2 * i][r] = x.x, q[2 * i][2 + r] = x.y, q[2 * i + 1][r] = x.z, q[2 * i + 1][2 + r] = x.w;
+              if (asks[r]) x = __ldg(reinterpret_cast<const uint4*>(query[r] + 64 * (i >> 1) + 8 * (2 * t + (i & 1))));
+              q[2 * i][r] = x.x, q[2 * i][kHeld + r] = x.y, q[2 * i + 1][r] = x.z, q[2 * i + 1][kHeld + r] = x.w;
             }
         }
         const int first = 16 * (is_node ? u : u - n.nodes);
@@ -395,12 +432,20 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
         float sc[2][4] = {}, sc2[2][4] = {};  // (chains of MMAs: an MMA waits 30 clocks for the one it adds to)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+          uint32_t k[2][4];
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t k[4];
-            lds_vec(at + 2048 * (i >> 1) + (8 * half + g) * 128 + (((2 * t + (i & 1)) ^ g) << 4), k);
-            mma_bf16(sc[half], q[2 * i], k[0], k[1]);
-            mma_bf16(sc2[half], q[2 * i + 1], k[2], k[3]);
+          for (int half = 0; half < 2; ++half)
+            lds_vec(at + 2048 * (i >> 1) + (8 * half + g) * 128 + (((2 * t + (i & 1)) ^ g) << 4), k[half]);
+          if constexpr (NARROW) {
+            const uint32_t k0[4] = {k[0][0], k[1][0], k[0][1], k[1][1]}, k1[4] = {k[0][2], k[1][2], k[0][3], k[1][3]};
+            mma_bf16(sc[0], k0, q[2 * i][0], q[2 * i][1]);
+            mma_bf16(sc2[0], k1, q[2 * i + 1][0], q[2 * i + 1][1]);
+          } else {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              mma_bf16(sc[half], q[2 * i], k[half][0], k[half][1]);
+              mma_bf16(sc2[half], q[2 * i + 1], k[half][2], k[half][3]);
+            }
           }
         }
 #pragma unroll
@@ -409,20 +454,26 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
           for (int e = 0; e < 4; ++e) sc[half][e] += sc2[half][e];
         uint32_t pk[4];
         const float c2[2] = {scale, scale};
-        weigh(sc, c2, masked, [&](int i, int r) { return seen[r] >> (8 * (i >> 1) + 2 * t + (i & 1)) & 1; }, pk, std::false_type{});
+        weigh(sc, c2, masked, [&](int half, int parity, int r) { return seen[r] >> (8 * half + (NARROW ? g : 2 * t + parity)) & 1; }, pk,
+              std::false_type{});
 #pragma unroll
         for (int i = 0; i < 8; ++i) {  // 16 channels: two n-blocks
           uint32_t v[4];
           const int row = (lane & 7) + 8 * ((lane >> 3) & 1), c = 2 * i + (lane >> 4);
           ldsm_x4_t(at + 4096 + 2048 * (c >> 3) + row * 128 + (((c & 7) ^ (row & 7)) << 4), v);
-          mma_bf16(o[2 * i], pk, v[0], v[1]);
-          mma_bf16(o[2 * i + 1], pk, v[2], v[3]);
+          if constexpr (NARROW) {
+            const uint32_t vt[4] = {v[0], v[2], v[1], v[3]};
+            mma_bf16(o[i], vt, pk[0], pk[1]);
+          } else {
+            mma_bf16(o[2 * i], pk, v[0], v[1]);
+            mma_bf16(o[2 * i + 1], pk, v[2], v[3]);
+          }
         }
         if (masked) fence_async();  // (the stage was written here; a copy comes next)
       } else {  // codes
         if (form != 1) {
           form = 1;
-          float x[2][8][4], top[2] = {0.f, 0.f};
+          float x[kHeld][8][4], top[2] = {0.f, 0.f};
 #pragma unroll
           for (int m = 0; m < 8; ++m) {
             float4 inv = make_float4(1.f, 1.f, 1.f, 1.f);
@@ -431,9 +482,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
               inv = make_float4(1.f / bal.x, 1.f / bal.y, 1.f / bal.z, 1.f / bal.w);
             }
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
+            for (int r = 0; r < kHeld; ++r) {
               uint2 raw = make_uint2(0u, 0u);
-              if (real[r]) raw = __ldg(reinterpret_cast<const uint2*>(query[r] + 16 * m + 4 * t));
+              if (asks[r]) raw = __ldg(reinterpret_cast<const uint2*>(query[r] + 16 * m + 4 * t));
               x[r][m][0] = __uint_as_float(raw.x << 16) * inv.x, x[r][m][1] = __uint_as_float(raw.x & 0xffff0000u) * inv.y;
               x[r][m][2] = __uint_as_float(raw.y << 16) * inv.z, x[r][m][3] = __uint_as_float(raw.y & 0xffff0000u) * inv.w;
 #pragma unroll
@@ -441,7 +492,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
             }
           }
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
+          for (int r = 0; r < kHeld; ++r) {
             top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
             top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
             const int e2 = min(max((int)(__float_as_uint(top[r]) >> 23) - 127, -100), 120) - 14;
@@ -454,9 +505,14 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
                 const float y0 = x[r][m][2 * e] * down, y1 = x[r][m][2 * e + 1] * down;
                 const __half2 near = __floats2half2_rn(y0, y1);
                 const float2 f = __half22float2(near);
-                q[m][2 * e + r] = h2_as_u32(near);
-                q2[m][2 * e + r] = pack_f16(y0 - f.x, y1 - f.y);
+                q[m][kHeld * e + r] = h2_as_u32(near);
+                q2[m][kHeld * e + r] = pack_f16(y0 - f.x, y1 - f.y);
               }
+          }
+          if constexpr (NARROW) {
+            const float mine = scale_lo[0];
+            scale_lo[0] = __shfl_sync(0xffffffffu, mine, 8 * t);
+            scale_lo[1] = __shfl_sync(0xffffffffu, mine, 8 * t + 4);
           }
         }
         const int r0 = (u - n.nodes - n.hi) * lo_rows, blocks = min(U.blocks, (n_lo - r0 + 15) >> 4);
@@ -469,7 +525,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
           const uint32_t kc = at + blk * 16 * kPitch, kp = at + U.kp + blk * 16 * U.row_bytes;
           float sc[2][4] = {};
           auto scores = [&](auto with_rest) {
-            float part[2][4][4] = {};  // chains of MMAs by the half, the query's term and the parity of m
+            float part[NARROW ? 1 : 2][4][4] = {};  // chains of MMAs by the half, the query's term and the parity of m
             uint2 x[2], y[2];
             uint32_t pr[2][PAIRS];
 #pragma unroll
@@ -487,23 +543,41 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
             const FieldOf<BITS> f[2][2] = {{FieldOf<BITS>(x[0].x, y[0].x), FieldOf<BITS>(x[0].y, y[0].y)},
                                            {FieldOf<BITS>(x[1].x, y[1].x), FieldOf<BITS>(x[1].y, y[1].y)}};
 #pragma unroll
-            for (int m = 0; m < 8; ++m)
+            for (int m = 0; m < 8; ++m) {
+              uint32_t k[2][2], rest[2][2];  // [half][register]; what their rounding leaves
 #pragma unroll
               for (int half = 0; half < 2; ++half) {
                 const __half2 ab = u32_as_h2(pr[half][m / kOf]), al = __low2half2(ab), be = __high2half2(ab);
-                const __half2 c0 = f[half][0].code(m), c1 = f[half][1].code(m);
-                const uint32_t k0 = h2_as_u32(__hfma2(c0, al, be)), k1 = h2_as_u32(__hfma2(c1, al, be));
-                mma_f16(part[half][m & 1], q[m], k0, k1);
-                mma_f16(part[half][2 + (m & 1)], q2[m], k0, k1);
-                if constexpr (decltype(with_rest)::value) {
-                  const float2 af = __half22float2(ab), d0 = __half22float2(c0), d1 = __half22float2(c1);
-                  const float2 n0 = __half22float2(u32_as_h2(k0)), n1 = __half22float2(u32_as_h2(k1));
-                  mma_f16(part[half][2 + (m & 1)], q[m], pack_f16(fmaf(af.x, d0.x, af.y) - n0.x, fmaf(af.x, d0.y, af.y) - n0.y),
-                          pack_f16(fmaf(af.x, d1.x, af.y) - n1.x, fmaf(af.x, d1.y, af.y) - n1.y));
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  const __half2 code = f[half][e].code(m);
+                  k[half][e] = h2_as_u32(__hfma2(code, al, be));
+                  if constexpr (decltype(with_rest)::value) {
+                    const float2 af = __half22float2(ab), d = __half22float2(code), n = __half22float2(u32_as_h2(k[half][e]));
+                    rest[half][e] = pack_f16(fmaf(af.x, d.x, af.y) - n.x, fmaf(af.x, d.y, af.y) - n.y);
+                  }
                 }
               }
+              if constexpr (NARROW) {
+                const uint32_t kt[4] = {k[0][0], k[1][0], k[0][1], k[1][1]};
+                mma_f16(part[0][m & 1], kt, q[m][0], q[m][1]);
+                mma_f16(part[0][2 + (m & 1)], kt, q2[m][0], q2[m][1]);
+                if constexpr (decltype(with_rest)::value) {
+                  const uint32_t rt[4] = {rest[0][0], rest[1][0], rest[0][1], rest[1][1]};
+                  mma_f16(part[0][2 + (m & 1)], rt, q[m][0], q[m][1]);
+                }
+              } else {
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+                for (int half = 0; half < 2; ++half) {
+                  mma_f16(part[half][m & 1], q[m], k[half][0], k[half][1]);
+                  mma_f16(part[half][2 + (m & 1)], q2[m], k[half][0], k[half][1]);
+                  if constexpr (decltype(with_rest)::value)
+                    mma_f16(part[half][2 + (m & 1)], q[m], rest[half][0], rest[half][1]);
+                }
+              }
+            }
+#pragma unroll
+            for (int half = 0; half < (NARROW ? 1 : 2); ++half)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 sc[half][e] = (part[half][0][e] + part[half][1][e]) + (part[half][2][e] + part[half][3][e]);
@@ -514,7 +588,8 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
             scores(std::false_type{});
           uint32_t pk[4];
           const bool masked = valid < 16;
-          weigh(sc, scale_lo, masked, [&](int i, int) { return 8 * (i >> 1) + t + 4 * (i & 1) < valid; }, pk, std::true_type{});
+          weigh(sc, scale_lo, masked, [&](int half, int parity, int) { return 8 * half + (NARROW ? krow : t + 4 * parity) < valid; }, pk,
+                std::true_type{});
           // values: of tokens 2 t, 2 t + 1 of both halves, the channels 16 m + 8 jj + g
           const uint32_t vc = at + U.v + blk * 16 * kPitch, vp = at + U.vp + blk * 16 * U.row_bytes;
           __half2 al[2][PAIRS], be[2][PAIRS];  // of both tokens of an operand register, by its half
@@ -533,22 +608,32 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
           }
           const uint32_t sel = g & 1 ? 0x7632u : 0x5410u, rows[4] = {vc + t * kPitch, vc + (t + 4) * kPitch,
                                                                      vc + (t + 8) * kPitch, vc + (t + 12) * kPitch};
+          // the codes of both tokens of an operand register, channels 16 m + 8 jj + g
+          auto words = [&](int half, int jj) {
+            const uint32_t ra = rows[2 * half], rb = rows[2 * half + 1], wo = 16 * jj + 4 * (g >> 1), wt = 32 + 4 * (g >> 1);
+            const uint32_t x = prmt(lds32v(ra + wo), lds32v(rb + wo), sel);
+            uint32_t y = 0;
+            if constexpr (BITS == 4) y = prmt(lds32v(ra + 32 + wo), lds32v(rb + 32 + wo), sel);
+            if constexpr (BITS == 3) y = prmt(lds32v(ra + wt), lds32v(rb + wt), sel) >> jj;
+            return FieldOf<BITS>(x, y);
+          };
+          if constexpr (NARROW) {
+            const FieldOf<BITS> f00 = words(0, 0), f01 = words(0, 1), f10 = words(1, 0), f11 = words(1, 1);
 #pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            const uint32_t wo = 16 * jj + 4 * (g >> 1), wt = 32 + 4 * (g >> 1);
-            auto words = [&](int half) {
-              const uint32_t ra = rows[2 * half], rb = rows[2 * half + 1];
-              const uint32_t x = prmt(lds32v(ra + wo), lds32v(rb + wo), sel);
-              uint32_t y = 0;
-              if constexpr (BITS == 4) y = prmt(lds32v(ra + 32 + wo), lds32v(rb + 32 + wo), sel);
-              if constexpr (BITS == 3) y = prmt(lds32v(ra + wt), lds32v(rb + wt), sel) >> jj;
-              return FieldOf<BITS>(x, y);
-            };
-            const FieldOf<BITS> f0 = words(0), f1 = words(1);
+            for (int m = 0; m < 8; ++m) {
+              auto value = [&](const FieldOf<BITS>& f, int half) { return h2_as_u32(__hfma2(f.code(m), al[half][m / kOf], be[half][m / kOf])); };
+              const uint32_t vt[4] = {value(f00, 0), value(f01, 0), value(f10, 1), value(f11, 1)};
+              mma_f16(o[m], vt, pk[0], pk[1]);
+            }
+          } else {
 #pragma unroll
-            for (int m = 0; m < 8; ++m)
-              mma_f16(o[2 * m + jj], pk, h2_as_u32(__hfma2(f0.code(m), al[0][m / kOf], be[0][m / kOf])),
-                      h2_as_u32(__hfma2(f1.code(m), al[1][m / kOf], be[1][m / kOf])));
+            for (int jj = 0; jj < 2; ++jj) {
+              const FieldOf<BITS> f0 = words(0, jj), f1 = words(1, jj);
+#pragma unroll
+              for (int m = 0; m < 8; ++m)
+                mma_f16(o[2 * m + jj], pk, h2_as_u32(__hfma2(f0.code(m), al[0][m / kOf], be[0][m / kOf])),
+                        h2_as_u32(__hfma2(f1.code(m), al[1][m / kOf], be[1][m / kOf])));
+            }
           }
         }
       }
@@ -556,36 +641,48 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
     }
     if (!ok) break;
 
-    // Output: rows g and g + 8, channels 8 i + 2 t and the next of every n-block i.
+    // Output: channels 8 i + 2 t and the next of every n-block i, or (narrow) 16 i + g and 8 on.
     const bool whole = u0 == 0 && u1 == count;
     const int slot = 2 * me + (u0 == 0);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       float total = sum[r];
-      total += __shfl_xor_sync(0xffffffffu, total, 1);
-      total += __shfl_xor_sync(0xffffffffu, total, 2);
+#pragma unroll
+      for (int off = NARROW ? 4 : 1; off < (NARROW ? 32 : 4); off <<= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
       const bool blank = !real[r] || total == 0.f;
       const float lse2 = blank ? -INFINITY : ref[r] + log2f(total);
       const float f = poisoned[r] ? __int_as_float(0x7fffffff) : 1.f / total;
       if (!there[r]) continue;
-      if (whole) {
-        const long long out = b * a.out.b + head[r] * a.out.h + node[r] * a.out.t + 2 * t;
+      const int row = NARROW ? 2 * t + r : g + 8 * r;
+      const long long out = b * a.out.b + head[r] * a.out.h + node[r] * a.out.t;
+      float* part = p.part_o + ((size_t)slot * kFewRows + row) * kHeadDim;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = blank ? 0.f : o[i][2 * r] * f, y = blank ? 0.f : o[i][2 * r + 1] * f;
-          if (a.out_f32)
-            *reinterpret_cast<float2*>(static_cast<float*>(a.out.p) + out + 8 * i) = make_float2(x, y);
+      for (int i = 0; i < kO; ++i) {
+        const float x = blank ? 0.f : o[i][NARROW ? r : 2 * r] * f, y = blank ? 0.f : o[i][NARROW ? 2 + r : 2 * r + 1] * f;
+        if constexpr (NARROW) {
+          const int c = 16 * i + g;
+          if (!whole)
+            part[c] = x, part[c + 8] = y;
+          else if (a.out_f32)
+            static_cast<float*>(a.out.p)[out + c] = x, static_cast<float*>(a.out.p)[out + c + 8] = y;
           else
-            *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.out.p) + out + 8 * i) = pack_bf16(x, y);
+            static_cast<__nv_bfloat16*>(a.out.p)[out + c] = __float2bfloat16(x),
+            static_cast<__nv_bfloat16*>(a.out.p)[out + c + 8] = __float2bfloat16(y);
+        } else {
+          const int c = 8 * i + 2 * t;
+          if (!whole)
+            *reinterpret_cast<float2*>(part + c) = make_float2(x, y);
+          else if (a.out_f32)
+            *reinterpret_cast<float2*>(static_cast<float*>(a.out.p) + out + c) = make_float2(x, y);
+          else
+            *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.out.p) + out + c) = pack_bf16(x, y);
         }
-        if (a.lse && t == 0) a.lse[((size_t)b * a.heads_q + head[r]) * a.nodes + node[r]] = lse2 * kLn2;
-      } else {
-        float* part = p.part_o + ((size_t)slot * kFewRows + g + 8 * r) * kHeadDim + 2 * t;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          *reinterpret_cast<float2*>(part + 8 * i) =
-              make_float2(blank ? 0.f : o[i][2 * r] * f, blank ? 0.f : o[i][2 * r + 1] * f);
-        if (t == 0) p.part_lse[(size_t)slot * kFewRows + g + 8 * r] = lse2;
+      }
+      if (NARROW ? g == 0 : t == 0) {
+        if (!whole)
+          p.part_lse[(size_t)slot * kFewRows + row] = lse2;
+        else if (a.lse)
+          a.lse[((size_t)b * a.heads_q + head[r]) * a.nodes + node[r]] = lse2 * kLn2;
       }
     }
     start += n.cost();
@@ -599,28 +696,29 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1) tree_few_kernel(const __gri
   }
 }
 
-template <int BITS, int PAIRS>
-cudaError_t launch_few_pairs(const TreeFewArgs& p, int grid, cudaStream_t st) {
-  constexpr int kSmem = 1024 + kFewWarps * kFewStages * kFewStage;
+template <int BITS, int PAIRS, bool NARROW>
+cudaError_t launch_few_shape(const TreeFewArgs& p, int grid, cudaStream_t st) {
+  using F = FewShape<NARROW>;
+  constexpr int kSmem = 1024 + F::kWarps * F::kStages * kFewStage;
   static std::atomic<uint64_t> configured;  // one bit per device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
-  auto kernel = tree_few_kernel<BITS, PAIRS>;
+  auto kernel = tree_few_kernel<BITS, PAIRS, NARROW>;
   if (dev > 63 || !(configured.load(std::memory_order_relaxed) & bit)) {
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     configured.fetch_or(bit, std::memory_order_relaxed);
   }
-  return launch_chained(kernel, dim3(grid), dim3(32 * kFewWarps), kSmem, st, p);
+  return launch_chained(kernel, dim3(grid), dim3(32 * F::kWarps), kSmem, st, p);
 }
 
-template <int BITS>
+template <int BITS, bool NARROW>
 cudaError_t launch_few_variant(const TreeFewArgs& p, int grid, cudaStream_t st) {
-  return p.a.group == 32   ? launch_few_pairs<BITS, 4>(p, grid, st)
-         : p.a.group == 64 ? launch_few_pairs<BITS, 2>(p, grid, st)
-                           : launch_few_pairs<BITS, 1>(p, grid, st);
+  return p.a.group == 32   ? launch_few_shape<BITS, 4, NARROW>(p, grid, st)
+         : p.a.group == 64 ? launch_few_shape<BITS, 2, NARROW>(p, grid, st)
+                           : launch_few_shape<BITS, 1, NARROW>(p, grid, st);
 }
 
 }  // namespace tree
