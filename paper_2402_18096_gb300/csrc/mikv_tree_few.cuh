@@ -3,21 +3,26 @@
 // mikv_tree_f2.cu, mikv_tree_f3.cu and mikv_tree_f4.cu instantiate it for one code width each.
 //
 // Why not the tensor-memory kernel: its tiles have 128 rows, its codes are written to and read from shared memory as
-// fp16 (ten times their size), and 16 rows of 128 are an eighth of what its products cost. Here a key costs 330 / 16
-// instructions of a warp, whatever the rows up to 16, and HBM is nearer than the tensor cores' rate.
+// fp16 (ten times their size), and 16 rows of 128 are an eighth of what its products cost.
 //
-// Work. Rows r = node * G + head in blocks of 16 (the M side of the MMAs); an item is a row block of one KV head. Its units
-// are 16 nodes, 16 important slots, or as many blocks of 16 retained rows as fit a stage of 8 KB. All items' units are laid
+// Work. Rows r = node * G + head in blocks of 8 or 16 (FewShape); an item is a row block of one KV head. Its units are 16
+// nodes, 16 important slots, or as many blocks of 16 retained rows as fit a stage of 8 KB. All items' units are laid
 // end to end and every warp of the grid takes an equal run of them, as the CTAs do in mikv_tree_kernel.cuh; the same
-// second kernel merges what lies in several runs. A warp shares nothing with the others: two stages of its own, filled by
-// copies (bulk copies of code rows, swizzled boxes of bf16 rows) that it asks for one unit ahead.
+// second kernel merges what lies in several runs. A warp shares nothing with the others: its own two or three stages,
+// filled by copies (bulk copies of code rows, swizzled boxes of bf16 rows) that it asks for one or two units ahead.
 //
-// A block of 16 tokens: S (16 x 16) = Q K^T with keys dequantized into the B operand (fp16: alpha code + beta, one rounding),
-// P = 2^(x - r) packed from S as it lies into the A operand, O (16 x 128) += P V with values dequantized likewise. The query
-// is divided by the balancer and stands in two fp16 terms (22 bits): rounded to one it would be off alike for all keys,
-// 1e-5 of lse. Where few retained rows (kFineRows) average nothing out, the rounding errors of the keys follow as a third
-// product. Tokens 2 t and 2 t + 1 of an operand are rows t and t + 4 of their eight, so that eight lanes read four rows of
-// codes from different banks.
+// A block of 16 tokens. Codes enter both products as they lie: a field's bits under a zero exponent are the fp16 number
+// code 2^(s - 24), s the field's place, exactly; one LOP3 makes a pair of operands.
+//   S = sum over the groups of alpha_g (sum over the group's channels of q^ code) + beta_g (sum of q^), q^ = q / balancer:
+//       a chain of MMAs per group, alpha and beta in fp32 afterwards. The keys are never rounded. q^ stands in two fp16
+//       terms (22 bits; rounded to one it would be off alike for all keys, 1e-5 of lse), scaled by 2^-s per field.
+//   O += (P alpha_g) code: P = 2^(x - r) in fp16 times the tokens' alpha, per group; what beta adds is P beta_g, one more MMA
+//       whose other side are the groups, added to the group's channels at the end. O of channels 16 m .. is kept in units of
+//       2^(s_m - 24) meanwhile, and of 2^ev for alphas far from 1.
+// With alpha and beta applied to every key and value in fp16 (two more instructions a pair) the same kernel took 182 us where
+// this one takes 149, 16 requests of 205 .. 8192 tokens, 40 heads, 3 bits.
+// Tokens 2 t and 2 t + 1 of an operand are rows t and t + 4 of their eight, so that eight lanes read four rows of codes from
+// different banks.
 #pragma once
 
 #include "mikv_tree_kernel.cuh"
@@ -71,15 +76,15 @@ struct FewUnits {
       : nodes((n_nodes + 15) / 16), hi((held.hi(b) + 15) / 16), lo((held.lo(b) + 16 * lo_blocks - 1) / (16 * lo_blocks)),
         blocks(lo_blocks) {}
   __device__ int count() const { return nodes + hi + lo; }
-  __device__ long long before(int u) const {
-    return u == 0 ? 0 : kFewItem + (long long)min(u, nodes + hi) + (long long)blocks * max(0, u - nodes - hi);
+  __device__ int before(int u) const {
+    return u == 0 ? 0 : kFewItem + min(u, nodes + hi) + blocks * max(0, u - nodes - hi);
   }
-  __device__ long long cost() const { return before(count()); }
+  __device__ int cost() const { return before(count()); }
   // the first unit that begins at x or later
-  __device__ int first(long long x) const {
+  __device__ int first(int x) const {
     if (x <= 0) return 0;
-    x = max(1ll, x - kFewItem);
-    return (int)min((long long)count(), x <= nodes + hi ? x : nodes + hi + (x - nodes - hi + blocks - 1) / blocks);
+    x = max(1, x - kFewItem);
+    return min(count(), x <= nodes + hi ? x : nodes + hi + (x - nodes - hi + blocks - 1) / blocks);
   }
 };
 
@@ -94,28 +99,30 @@ __device__ __forceinline__ uint32_t lds32v(uint32_t addr) {
   return r;
 }
 
-// A code field of both 16-bit halves of a word as exact fp16 numbers; m: which field (compile time), up: the word shifted
-// for the upper fields.
+// Code fields m of both 16-bit halves of a word: the fp16 numbers code 2^(place(m) - 24). A field has to lie in the 10 bits
+// of the mantissa, so the upper ones are read from the words shifted.
 template <int BITS>
 struct FieldOf {
-  static constexpr int kShift = BITS == 2 ? 10 : 8, kUpper = BITS == 2 ? 5 : BITS == 3 ? 4 : 2;
-  // x, y: the word, and for 4 bits the second word (fields 4 ..), for 3 bits the word of the high bits (at bit 2 m)
-  uint32_t lo[2], up[2];
+  static constexpr int kWords = BITS == 2 ? 1 : 2;
+  uint32_t lo[kWords], up[kWords];
+  // x, y: the word, and for 4 bits the second word (fields 4 ..), for 3 bits the word of the high bits (at bit 2 m): even
+  // and odd fields are brought together with their high bits, 4 bits to a field
   __device__ __forceinline__ FieldOf(uint32_t x, uint32_t y) {
-    lo[0] = x, up[0] = x >> kShift;
-    if constexpr (BITS == 4) lo[1] = y, up[1] = y >> kShift;
-    if constexpr (BITS == 3) lo[1] = y << 2, up[1] = y >> 6;
+    lo[0] = x;
+    if constexpr (BITS == 4) lo[1] = y;
+    if constexpr (BITS == 3) lo[0] = merge(x, y << 2), lo[1] = merge(x >> 2, y);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) up[i] = lo[i] >> 8;
   }
-  __device__ __forceinline__ __half2 code(int m) const {
-    const int f = BITS == 4 ? m & 3 : m, width = BITS == 4 ? 4 : 2;
-    const bool upper = f >= kUpper;
-    const int s = width * f - (upper ? kShift : 0), i = BITS == 4 ? m >> 2 : 0;
-    const uint32_t magic = 0x64006400u - 0x04000400u * s, mask = BITS == 4 ? 0x000F000Fu : 0x00030003u;
-    uint32_t x = and_or(upper ? up[i] : lo[i], mask << s, magic);
-    if constexpr (BITS == 3) x = and_or(upper ? up[1] : lo[1], 0x00040004u << s, x);
-    return __hsub2(u32_as_h2(x), u32_as_h2(magic));
+  static __device__ __forceinline__ uint32_t merge(uint32_t low, uint32_t high) { return (low & 0x33333333u) | (high & ~0x33333333u); }
+  static __host__ __device__ constexpr int field(int m) { return BITS == 2 ? m : BITS == 3 ? m >> 1 : m & 3; }  // in its word
+  static __host__ __device__ constexpr int place(int m) { return (BITS == 2 ? 2 : 4) * field(m) & 7; }
+  __device__ __forceinline__ uint32_t code(int m) const {
+    const int i = BITS == 2 ? 0 : BITS == 3 ? m & 1 : m >> 2, at = (BITS == 2 ? 2 : 4) * field(m);
+    return (at >= 8 ? up[i] : lo[i]) & (((1u << BITS) - 1u) * 0x10001u << place(m));
   }
 };
+__device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
 // The parameters of a token.
 template <int PAIRS>
@@ -136,6 +143,7 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
   const TreeArgs& a = p.a;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t s_bar[kFewWarps][kFewStages];
+  __shared__ float s_rel[kFewWarps][4][kRows];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const uint32_t stages = ((smem_u32(smem_raw) + 1023u) & ~1023u) + warp * (kFewStages * kFewStage);
   const uint32_t bars = smem_u32(&s_bar[warp][0]);
@@ -151,7 +159,7 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
 
   // This warp's run of all units.
   auto scan = [&](int b0, long long& mine) {
-    mine = b0 + lane < a.batch ? units_of(b0 + lane).cost() * per_set : 0;
+    mine = b0 + lane < a.batch ? (long long)units_of(b0 + lane).cost() * per_set : 0;
     long long sum = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -171,32 +179,35 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
   if (me == 0 && lane == 0) p.prefix[a.batch] = all;
   const Runs runs(all, gridDim.x * kFewWarps, kFewLeast);
   if (me >= runs.n) return;
-  const long long from = runs.first(me), to = runs.first(me + 1);
-  long long start = 0;  // costs before the item
+  const long long from = runs.first(me);
+  long long start64 = 0;  // costs before the item
   int b = 0, in_set = 0;
 #pragma unroll 1
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
     const long long sum = scan(b0, mine), total = __shfl_sync(0xffffffffu, sum, 31);
-    if (from < start + total) {
-      const int at = __ffs(__ballot_sync(0xffffffffu, start + sum > from)) - 1;
+    if (from < start64 + total) {
+      const int at = __ffs(__ballot_sync(0xffffffffu, start64 + sum > from)) - 1;
       b = b0 + at;
-      start += __shfl_sync(0xffffffffu, sum - mine, at);
+      start64 += __shfl_sync(0xffffffffu, sum - mine, at);
       const long long cost = units_of(b).cost();
-      in_set = (int)((from - start) / cost);
-      start += in_set * cost;
+      in_set = (int)((from - start64) / cost);
+      start64 += in_set * cost;
       break;
     }
-    start += total;
+    start64 += total;
   }
 
+  // from here on relative to the run's begin: an item's costs, and a run's, are inside 32 bits
+  int start = (int)(start64 - from);
+  const int to = (int)(runs.first(me + 1) - from);
   // The unit that is asked for next: its place, and the stage it goes to.
   struct Place {
     int b, in_set, u;
     FewUnits n;
   };
-  long long ask_start = start;  // costs before its item
+  int ask_start = start;  // costs before its item
   Place ask = {b, in_set, 0, units_of(b)};
-  ask.u = ask.n.first(from - start);
+  ask.u = ask.n.first(-start);
   bool more = ask_start + ask.n.before(ask.u) < to;
   int ask_stage = 0, stage = 0;    // of the unit asked for next, of the one worked on next
   uint32_t parity = 0, copies = 0; // per stage: of the copy taken next; whether the unit in it was copied
@@ -250,7 +261,7 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
 #pragma unroll 1
   for (; ok && start < to; ) {  // an item
     const FewUnits n = units_of(b);
-    const int count = n.count(), u0 = n.first(from - start), u1 = n.first(to - start);
+    const int count = n.count(), u0 = n.first(-start), u1 = n.first(to - start);
     if (u0 == u1) {  // (none of its units begins in this run)
       start += n.cost();
       if (++in_set == per_set) in_set = 0, ++b;
@@ -258,7 +269,6 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
     }
     const int h = in_set / p.row_blocks, block = in_set - h * p.row_blocks, bh = b * a.heads_kv + h;
     const int n_hi = a.held.hi(b), n_lo = a.held.lo(b), free_slot = a.held.free_slot(bh, n_hi);
-    const bool fine = n_lo <= kFineRows;
     // The lane's rows: g and g + 8, or (narrow) 2 t and 2 t + 1; the queries that it holds are those of rows g and g + 8, or
     // (narrow) of row g alone.
     int node[2], head[2];
@@ -282,6 +292,11 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
       query[0] = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + (h * a.G + (R & (a.G - 1))) * a.q.h + i * a.q.t;
     }
     constexpr int kHeld = NARROW ? 1 : 2, kO = NARROW ? 8 : 16;
+    float ob[4] = {0.f, 0.f, 0.f, 0.f};  // P beta: by groups g (narrow), or rows by groups 2 t, 2 t + 1
+    float qs[PAIRS][2];                  // sums of the groups' q^, in units of 2^24 products
+    bool spread = false;                 // 32 channels of q^ have a scale of their own (s_rel, beside the row's)
+    float alpha_most = -1.f;             // 2^(ev + 6): O is in units of 2^ev (retained rows)
+    __half2 unit = u32_as_h2(0u);        // 2^-ev
     float o[kO][4], ref[2], sum[2] = {0.f, 0.f}, scale_lo[2] = {0.f, 0.f};
     bool poisoned[2] = {false, false};
 #pragma unroll
@@ -326,6 +341,8 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
         for (int i = 0; i < kO; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[i][e] *= f[row_of(0, e)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ob[e] *= f[row_of(0, e)];
       }
       float w[2][4];
 #pragma unroll
@@ -473,7 +490,7 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
       } else {  // codes
         if (form != 1) {
           form = 1;
-          float x[kHeld][8][4], top[2] = {0.f, 0.f};
+          float x[kHeld][8][4], top[kHeld][4] = {};  // (by 32 channels)
 #pragma unroll
           for (int m = 0; m < 8; ++m) {
             float4 inv = make_float4(1.f, 1.f, 1.f, 1.f);
@@ -488,32 +505,66 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
               x[r][m][0] = __uint_as_float(raw.x << 16) * inv.x, x[r][m][1] = __uint_as_float(raw.x & 0xffff0000u) * inv.y;
               x[r][m][2] = __uint_as_float(raw.y << 16) * inv.z, x[r][m][3] = __uint_as_float(raw.y & 0xffff0000u) * inv.w;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) top[r] = fmaxf(top[r], fabsf(x[r][m][e]));
+              for (int e = 0; e < 4; ++e) top[r][m >> 1] = fmaxf(top[r][m >> 1], fabsf(x[r][m][e]));
             }
           }
+          // Their powers of two, 2^e for the row: the terms of a channel 2^-8 below the largest are as good as its own, so the
+          // row's is used for all 128 until 32 channels lie lower; then each 32 take their own.
+          auto exponent = [](float y) { return min(max((int)(__float_as_uint(y) >> 23) - 127, -100), 100) - 14; };
+          bool low = false;
+          float most[kHeld];
 #pragma unroll
           for (int r = 0; r < kHeld; ++r) {
-            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-            const int e2 = min(max((int)(__float_as_uint(top[r]) >> 23) - 127, -100), 120) - 14;
-            const float down = __uint_as_float((uint32_t)(127 - e2) << 23);
-            scale_lo[r] = scale * __uint_as_float((uint32_t)(127 + e2) << 23);
 #pragma unroll
-            for (int m = 0; m < 8; ++m)
+            for (int j = 0; j < 4; ++j) {
+              top[r][j] = fmaxf(top[r][j], __shfl_xor_sync(0xffffffffu, top[r][j], 1));
+              top[r][j] = fmaxf(top[r][j], __shfl_xor_sync(0xffffffffu, top[r][j], 2));
+            }
+            most[r] = fmaxf(fmaxf(top[r][0], top[r][1]), fmaxf(top[r][2], top[r][3]));
+            low |= fminf(fminf(top[r][0], top[r][1]), fminf(top[r][2], top[r][3])) < 0x1p-8f * most[r];
+          }
+          spread = __any_sync(0xffffffffu, low);
+          __syncwarp();
+#pragma unroll
+          for (int r = 0; r < kHeld; ++r) {
+            const int e2 = exponent(most[r]);
+            scale_lo[r] = scale * power2(e2) * 0x1p24f;
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+              float all = 0.f;
+#pragma unroll
+              for (int m = kOf * i; m < kOf * (i + 1); ++m) all += (x[r][m][0] + x[r][m][1]) + (x[r][m][2] + x[r][m][3]);
+              all += __shfl_xor_sync(0xffffffffu, all, 1);
+              all += __shfl_xor_sync(0xffffffffu, all, 2);
+              qs[i][r] = all * power2(-e2) * 0x1p-24f;
+            }
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+              const int ej = spread ? max(exponent(top[r][m >> 1]), e2 - 100) : e2;
+              if (spread && !(m & 1) && t == 0) s_rel[warp][m >> 1][g + 8 * r] = power2(ej - e2);
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                const float y0 = x[r][m][2 * e] * down, y1 = x[r][m][2 * e + 1] * down;
+                const float d = power2(-ej) * power2(-FieldOf<BITS>::place(m)), y0 = x[r][m][2 * e] * d, y1 = x[r][m][2 * e + 1] * d;
                 const __half2 near = __floats2half2_rn(y0, y1);
                 const float2 f = __half22float2(near);
                 q[m][kHeld * e + r] = h2_as_u32(near);
                 q2[m][kHeld * e + r] = pack_f16(y0 - f.x, y1 - f.y);
               }
+            }
           }
+          __syncwarp();
           if constexpr (NARROW) {
-            const float mine = scale_lo[0];
-            scale_lo[0] = __shfl_sync(0xffffffffu, mine, 8 * t);
-            scale_lo[1] = __shfl_sync(0xffffffffu, mine, 8 * t + 4);
+            auto turn = [&](float mine, float& r0, float& r1) {
+              r0 = __shfl_sync(0xffffffffu, mine, 8 * t), r1 = __shfl_sync(0xffffffffu, mine, 8 * t + 4);
+            };
+            turn(scale_lo[0], scale_lo[0], scale_lo[1]);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) turn(qs[i][0], qs[i][0], qs[i][1]);
           }
+#pragma unroll
+          for (int i = 0; i < kO; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][e] *= power2(FieldOf<BITS>::place(NARROW ? i : i >> 1) - 24);
         }
         const int r0 = (u - n.nodes - n.hi) * lo_rows, blocks = min(U.blocks, (n_lo - r0 + 15) >> 4);
         constexpr int kPitch = 16 * BITS;
@@ -523,11 +574,13 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
         for (int blk = 0; blk < blocks; ++blk) {
           const int valid = n_lo - (r0 + 16 * blk);  // rows of the block
           const uint32_t kc = at + blk * 16 * kPitch, kp = at + U.kp + blk * 16 * U.row_bytes;
+          const uint32_t vc = at + U.v + blk * 16 * kPitch, vp = at + U.vp + blk * 16 * U.row_bytes;
+          const bool masked = valid < 16;
+          // scores: codes of rows krow of both halves, channels 16 m + 4 t .. 4 t + 3
           float sc[2][4] = {};
-          auto scores = [&](auto with_rest) {
-            float part[NARROW ? 1 : 2][4][4] = {};  // chains of MMAs by the half, the query's term and the parity of m
+          {
+            float part[NARROW ? 1 : 2][4][4] = {};  // by 32 channels
             uint2 x[2], y[2];
-            uint32_t pr[2][PAIRS];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               const int row = 8 * half + krow;
@@ -538,73 +591,101 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
                 y[half] = lds64(kc + row * kPitch + 32 + 8 * (t & 1));
                 y[half].x >>= t >> 1, y[half].y >>= t >> 1;
               }
-              load_pairs(kp + row * U.row_bytes, pr[half]);
             }
             const FieldOf<BITS> f[2][2] = {{FieldOf<BITS>(x[0].x, y[0].x), FieldOf<BITS>(x[0].y, y[0].y)},
                                            {FieldOf<BITS>(x[1].x, y[1].x), FieldOf<BITS>(x[1].y, y[1].y)}};
 #pragma unroll
-            for (int m = 0; m < 8; ++m) {
-              uint32_t k[2][2], rest[2][2];  // [half][register]; what their rounding leaves
+            for (int odd = 0; odd < 2; ++odd)
 #pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const __half2 ab = u32_as_h2(pr[half][m / kOf]), al = __low2half2(ab), be = __high2half2(ab);
+              for (int term = 0; term < 2; ++term)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  const __half2 code = f[half][e].code(m);
-                  k[half][e] = h2_as_u32(__hfma2(code, al, be));
-                  if constexpr (decltype(with_rest)::value) {
-                    const float2 af = __half22float2(ab), d = __half22float2(code), n = __half22float2(u32_as_h2(k[half][e]));
-                    rest[half][e] = pack_f16(fmaf(af.x, d.x, af.y) - n.x, fmaf(af.x, d.y, af.y) - n.y);
+                for (int j = 0; j < 4; ++j) {
+                  const int m = 2 * j + odd;
+                  const uint32_t k[2][2] = {{f[0][0].code(m), f[0][1].code(m)}, {f[1][0].code(m), f[1][1].code(m)}};
+                  if constexpr (NARROW) {
+                    const uint32_t kt[4] = {k[0][0], k[1][0], k[0][1], k[1][1]};
+                    mma_f16(part[0][j], kt, term ? q2[m][0] : q[m][0], term ? q2[m][1] : q[m][1]);
+                  } else {
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) mma_f16(part[half][j], term ? q2[m] : q[m], k[half][0], k[half][1]);
                   }
                 }
-              }
-              if constexpr (NARROW) {
-                const uint32_t kt[4] = {k[0][0], k[1][0], k[0][1], k[1][1]};
-                mma_f16(part[0][m & 1], kt, q[m][0], q[m][1]);
-                mma_f16(part[0][2 + (m & 1)], kt, q2[m][0], q2[m][1]);
-                if constexpr (decltype(with_rest)::value) {
-                  const uint32_t rt[4] = {rest[0][0], rest[1][0], rest[0][1], rest[1][1]};
-                  mma_f16(part[0][2 + (m & 1)], rt, q[m][0], q[m][1]);
-                }
-              } else {
+            // alpha and beta of the lane's tokens: row krow of both halves, or (16 rows) the columns 2 t and 2 t + 1
+            if (spread) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                  mma_f16(part[half][m & 1], q[m], k[half][0], k[half][1]);
-                  mma_f16(part[half][2 + (m & 1)], q2[m], k[half][0], k[half][1]);
-                  if constexpr (decltype(with_rest)::value)
-                    mma_f16(part[half][2 + (m & 1)], q[m], rest[half][0], rest[half][1]);
+              for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                  const float f = s_rel[warp][j][NARROW ? 2 * t + r : g + 8 * r];
+#pragma unroll
+                  for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int half = 0; half < (NARROW ? 1 : 2); ++half) part[half][j][NARROW ? 2 * i + r : 2 * r + i] *= f;
+                }
+            }
+            if constexpr (PAIRS < 4) {
+#pragma unroll
+              for (int half = 0; half < (NARROW ? 1 : 2); ++half)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  part[half][0][e] += part[half][1][e];
+                  part[half][1][e] = part[half][2][e] + part[half][3][e];
+                  if constexpr (PAIRS == 1) part[half][0][e] += part[half][1][e];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < (NARROW ? 2 : 4); ++i) {  // token: half i (narrow), or half i >> 1 and column 2 t + (i & 1)
+              uint32_t pr[PAIRS];
+              load_pairs(kp + (NARROW ? 8 * i + krow : 8 * (i >> 1) + t + 4 * (i & 1)) * U.row_bytes, pr);
+#pragma unroll
+              for (int j = 0; j < PAIRS; ++j) {
+                const float2 ab = __half22float2(u32_as_h2(pr[j]));
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                  const int half = NARROW ? 0 : i >> 1, e = NARROW ? 2 * i + r : 2 * r + (i & 1);
+                  sc[half][e] = fmaf(ab.x, part[half][j][e], fmaf(ab.y, qs[j][r], sc[half][e]));
                 }
               }
             }
-#pragma unroll
-            for (int half = 0; half < (NARROW ? 1 : 2); ++half)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                sc[half][e] = (part[half][0][e] + part[half][1][e]) + (part[half][2][e] + part[half][3][e]);
-          };
-          if (fine)
-            scores(std::true_type{});
-          else
-            scores(std::false_type{});
+          }
           uint32_t pk[4];
-          const bool masked = valid < 16;
           weigh(sc, scale_lo, masked, [&](int half, int parity, int) { return 8 * half + (NARROW ? krow : t + 4 * parity) < valid; }, pk,
                 std::true_type{});
-          // values: of tokens 2 t, 2 t + 1 of both halves, the channels 16 m + 8 jj + g
-          const uint32_t vc = at + U.v + blk * 16 * kPitch, vp = at + U.vp + blk * 16 * U.row_bytes;
-          __half2 al[2][PAIRS], be[2][PAIRS];  // of both tokens of an operand register, by its half
+          // values: the parameters of tokens 2 t and 2 t + 1 of both halves; beta of group g to every lane g
+          __half2 al[2][PAIRS], most = u32_as_h2(0u);
+          uint32_t be[2];
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             uint32_t pa[PAIRS], pb[PAIRS];
-            const int ra = 8 * half + t, rb = ra + 4;
+            const int ra = 8 * half + t, rb = ra + 4, j = min(g, PAIRS - 1);
             load_pairs(vp + ra * U.row_bytes, pa);
             load_pairs(vp + rb * U.row_bytes, pb);
+            uint32_t ba = lds32v(vp + ra * U.row_bytes + 4 * j), bb = lds32v(vp + rb * U.row_bytes + 4 * j);
+            if (masked) {  // (rows behind the last: any bits)
+#pragma unroll
+              for (int i = 0; i < PAIRS; ++i) pa[i] = ra < valid ? pa[i] : 0u, pb[i] = rb < valid ? pb[i] : 0u;
+              ba = ra < valid ? ba : 0u, bb = rb < valid ? bb : 0u;
+            }
+            be[half] = g < PAIRS ? prmt(ba, bb, 0x7632u) : 0u;
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) {
-              if (masked) pa[i] = ra < valid ? pa[i] : 0u, pb[i] = rb < valid ? pb[i] : 0u;  // (rows behind the last: any bits)
               al[half][i] = u32_as_h2(prmt(pa[i], pb[i], 0x5410u));
-              be[half][i] = u32_as_h2(prmt(pa[i], pb[i], 0x7632u));
+              most = __hmax2(most, al[half][i]);
             }
+          }
+          // P is up to 2^8.5 and alpha up to 2^(ev + 6): their product is inside fp16. The first block chooses ev.
+          const float top_alpha = fmaxf(__low2float(most), __high2float(most));
+          if (__any_sync(0xffffffffu, top_alpha > alpha_most)) {
+            float x = top_alpha;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+            const int ev = min(max((int)(__float_as_uint(x) >> 23) - 127, -14), 15);
+            const float f = alpha_most < 0.f ? power2(-ev) : alpha_most * power2(-6 - ev);
+#pragma unroll
+            for (int i = 0; i < kO; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][e] *= f;
+            alpha_most = power2(ev + 6), unit = __float2half2_rn(power2(-ev));
           }
           const uint32_t sel = g & 1 ? 0x7632u : 0x5410u, rows[4] = {vc + t * kPitch, vc + (t + 4) * kPitch,
                                                                      vc + (t + 8) * kPitch, vc + (t + 12) * kPitch};
@@ -618,21 +699,32 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
             return FieldOf<BITS>(x, y);
           };
           if constexpr (NARROW) {
+            const uint32_t bt[4] = {be[0], 0u, be[1], 0u};
+            mma_f16(ob, bt, pk[0], pk[1]);
+            uint32_t pa[PAIRS][2];  // P alpha
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i)
+#pragma unroll
+              for (int half = 0; half < 2; ++half)
+                pa[i][half] = h2_as_u32(__hmul2(__hmul2(u32_as_h2(pk[half]), unit), al[half][i]));
             const FieldOf<BITS> f00 = words(0, 0), f01 = words(0, 1), f10 = words(1, 0), f11 = words(1, 1);
 #pragma unroll
             for (int m = 0; m < 8; ++m) {
-              auto value = [&](const FieldOf<BITS>& f, int half) { return h2_as_u32(__hfma2(f.code(m), al[half][m / kOf], be[half][m / kOf])); };
-              const uint32_t vt[4] = {value(f00, 0), value(f01, 0), value(f10, 1), value(f11, 1)};
-              mma_f16(o[m], vt, pk[0], pk[1]);
+              const uint32_t vt[4] = {f00.code(m), f01.code(m), f10.code(m), f11.code(m)};
+              mma_f16(o[m], vt, pa[m / kOf][0], pa[m / kOf][1]);
             }
           } else {
+            mma_f16(ob, pk, be[0], be[1]);
+            uint32_t pa[PAIRS][4];
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) pa[i][e] = h2_as_u32(__hmul2(__hmul2(u32_as_h2(pk[e]), unit), al[e >> 1][i]));
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
               const FieldOf<BITS> f0 = words(0, jj), f1 = words(1, jj);
 #pragma unroll
-              for (int m = 0; m < 8; ++m)
-                mma_f16(o[2 * m + jj], pk, h2_as_u32(__hfma2(f0.code(m), al[0][m / kOf], be[0][m / kOf])),
-                        h2_as_u32(__hfma2(f1.code(m), al[1][m / kOf], be[1][m / kOf])));
+              for (int m = 0; m < 8; ++m) mma_f16(o[2 * m + jj], pa[m / kOf], f0.code(m), f1.code(m));
             }
           }
         }
@@ -642,6 +734,21 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
     if (!ok) break;
 
     // Output: channels 8 i + 2 t and the next of every n-block i, or (narrow) 16 i + g and 8 on.
+    if (form == 1) {
+      float add[PAIRS][2];  // P beta of the groups, for the lane's rows
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          add[i][r] = NARROW ? __shfl_sync(0xffffffffu, ob[r], 4 * i + t) : __shfl_sync(0xffffffffu, ob[2 * r + (i & 1)], (lane & 28) + (i >> 1));
+#pragma unroll
+      for (int i = 0; i < kO; ++i) {
+        const int m = NARROW ? i : i >> 1;
+        const float f = alpha_most * power2(18 - FieldOf<BITS>::place(m));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][e] = fmaf(o[i][e], f, add[m / kOf][NARROW ? e & 1 : e >> 1]);
+      }
+    }
     const bool whole = u0 == 0 && u1 == count;
     const int slot = 2 * me + (u0 == 0);
 #pragma unroll
