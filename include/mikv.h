@@ -549,12 +549,20 @@ typedef struct {
  *   x_m = sm_scale * q . k[m]                        nodes m in i's mask (itself among them)
  *   out = sum softmax(x) v (v_hat = alpha * code + beta for retained rows),  lse = ln sum exp(x)
  * A padding node (mask without its own bit) gives out = 0 and lse = -inf, and its key and value may hold any bits. Scores
- * and sums are fp32. Retained values (alpha * code + beta) enter the product rounded to fp16, as do retained keys divided
- * by the balancer, alpha * code / b + beta / b, whose magnitude has to stay below 65504; the probabilities enter
- * rounded to fp16 (retained) or bf16 (important slots, nodes), whatever out_dtype is. Queries are taken exactly, in fp16
- * after a power of two per row: elements below 2^-24 of a row's largest are lost. A node whose value holds an infinity
- * or NaN gives NaN in all channels to the nodes that see it, and touches no other; in the cache such values reach all
- * nodes of the request. Results do not depend on what else runs, and repeat bit for bit.
+ * and sums are fp32; bf16 keys enter exactly. The probabilities enter rounded to fp16 (retained) or bf16 (important slots,
+ * nodes), whatever out_dtype is. What the retained rows are rounded to depends on the rows N * G, for caches of more than
+ * 2^18 tokens over all KV heads (smaller ones are as with more rows):
+ *   up to 16   codes enter exactly. q / balancer enters in two fp16 terms after a power of two for 32 channels or all
+ *              (22 bits of an element; those below 2^-19 of the largest of their 32 channels lose some); probabilities are
+ *              rounded to fp16 once more, times alpha. alpha and beta of the keys act in fp32
+ *   more       keys, alpha * code / b + beta / b, and values, alpha * code + beta, are rounded to fp16 (of requests with
+ *              at most 1024 retained rows the keys' remainder enters too); their magnitude has to stay below 65504.
+ *              Queries are taken exactly, in fp16 after a power of two per row: elements below 2^-24 of a row's largest
+ *              are lost
+ * A node whose value holds an infinity or NaN gives NaN in all channels to the nodes that see it, and touches no other; in
+ * the cache such values reach all nodes of the request. Results do not depend on what else runs, and repeat bit for bit.
+ * Errors: MIKV_ERR_UNSUPPORTED for batch * heads_kv * hi_stride or batch * heads_q * nodes of 2^31 or more, and for blocks of
+ * 16 tokens (with 32 for every 16 to 256 rows) of 2^32 or more in all.
  *   masks      uint32 [B][N][4], 16-byte aligned
  *   q, out     views [B][Hq][N][d];  k, v  views [B][Hkv][N][d] (bf16; 16-byte aligned data and strides; out of out_dtype)
  *   lens       what the requests hold, or NULL: hi_cap slots and no retained rows

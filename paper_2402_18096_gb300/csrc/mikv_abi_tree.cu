@@ -107,7 +107,7 @@ mikv_status mikv_tree_masks(uint32_t* masks, int32_t* positions, const int32_t* 
 }
 
 size_t mikv_tree_workspace_bytes(const mikv_shape* shape, int32_t nodes) {
-  if (drafts_supported(shape) != MIKV_OK || !nodes_ok(nodes)) return 0;
+  if (drafts_supported(shape) != MIKV_OK || !nodes_ok(nodes) || !tree_sizes_ok(*shape, nodes)) return 0;
   return tree_workspace_bytes(*shape, nodes, num_sms());
 }
 
@@ -122,7 +122,7 @@ mikv_status mikv_tree_attention(const mikv_shape* shape, const mikv_cache* cache
     return MIKV_ERR_ARG;
   if (d->nodes <= 0 || !positive(d->sm_scale) || (d->out_dtype != MIKV_BF16 && d->out_dtype != MIKV_F32))
     return MIKV_ERR_ARG;
-  if (!nodes_ok(d->nodes)) return MIKV_ERR_UNSUPPORTED;
+  if (!nodes_ok(d->nodes) || !tree_sizes_ok(*shape, d->nodes)) return MIKV_ERR_UNSUPPORTED;
   TreeArgs a;
   memset(&a, 0, sizeof a);
   if ((st = view_of(q, shape->batch, shape->heads_q, d->nodes, 2, a.q)) != MIKV_OK) return st;

@@ -45,9 +45,9 @@ using tree::Tiles;
 
 struct TreeMergeArgs {
   TreeArgs a;
-  const long long* prefix;
+  const uint32_t* prefix;
   const float *part_o, *part_lse;
-  int m_blocks, log2_G, item_rows, ctas, lo_blocks;
+  int m_blocks, log2_G, log2_rows, ctas, lo_blocks;
 };
 
 // How an item's units lie in the runs: key tiles by their costs, or the units of few rows, one like another.
@@ -55,18 +55,18 @@ struct TileRuns {
   Tiles tl;
   Runs runs;
   __device__ TileRuns(const TreeMergeArgs& m, int b) : tl(m.a.held, b), runs(m.prefix[m.a.batch], m.ctas) {}
-  __device__ long long cost() const { return tl.cost(); }
-  __device__ long long last() const { return tl.before(tl.count() - 1); }
-  __device__ bool part(long long from, long long to) const { return tl.first(from) < tl.first(to); }
+  __device__ int cost() const { return tl.cost(); }
+  __device__ int last() const { return tl.before(tl.count() - 1); }
+  __device__ bool part(int from, int to) const { return tl.first(from) < tl.first(to); }
 };
 struct FewRuns {
   tree::FewUnits n;
   Runs runs;
   __device__ FewRuns(const TreeMergeArgs& m, int b)
       : n(m.a.held, m.a.nodes, b, m.lo_blocks), runs(m.prefix[m.a.batch], m.ctas, tree::kFewLeast) {}
-  __device__ long long cost() const { return n.cost(); }
-  __device__ long long last() const { return n.before(n.count() - 1); }
-  __device__ bool part(long long from, long long to) const { return n.first(from) < n.first(to); }
+  __device__ int cost() const { return n.cost(); }
+  __device__ int last() const { return n.before(n.count() - 1); }
+  __device__ bool part(int from, int to) const { return n.first(from) < n.first(to); }
 };
 
 // The parts of an output row, weighted by 2^(lse - largest): a warp to a row. Rows whose item one CTA had are written.
@@ -74,25 +74,24 @@ template <typename R>
 __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__ TreeMergeArgs m) {
   const TreeArgs& a = m.a;
   const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);  // (request * nodes + node) * heads_q + head
+  const uint32_t row = blockIdx.x * 4u + (threadIdx.x >> 5), bn = row / a.heads_q;  // (request * nodes + node) * heads_q + head
   grid_dependency_wait();
-  const long long bn = row / a.heads_q;
-  const int head = (int)(row - bn * a.heads_q), b = (int)(bn / a.nodes), node = (int)(bn - (long long)b * a.nodes);
+  const int head = (int)(row - bn * a.heads_q), b = (int)(bn / a.nodes), node = (int)(bn - (uint32_t)b * a.nodes);
   if (b >= a.batch) return;
   const int h = head >> m.log2_G, in_head = (node << m.log2_G) + (head & (a.G - 1));
-  const int block = in_head / m.item_rows, in_item = in_head - block * m.item_rows;
+  const int block = in_head >> m.log2_rows, in_item = in_head & ((1 << m.log2_rows) - 1);
   const R item(m, b);
   const Runs& runs = item.runs;
-  const long long start = m.prefix[b] + (long long)(h * m.m_blocks + block) * item.cost();
+  const uint32_t start = m.prefix[b] + (uint32_t)(h * m.m_blocks + block) * item.cost();
   const int c0 = runs.owner(start), c1 = runs.owner(start + item.last());
   if (c0 == c1) return;
   float top = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int first = c0; first <= c1; first += 32) {
     const int c = first + lane;
-    const long long at = (long long)(2 * c + (c == c0)) * m.item_rows + in_item;
+    const long long at = ((long long)(2 * c + (c == c0)) << m.log2_rows) + in_item;
     bool part = c <= c1;
-    if (part) part = item.part(runs.first(c) - start, runs.first(c + 1) - start);
+    if (part) part = item.part((int)(runs.first(c) - start), (int)(runs.first(c + 1) - start));
     const float e = part ? m.part_lse[at] : -INFINITY;
     float next = fmaxf(top, e);
 #pragma unroll
@@ -104,15 +103,27 @@ __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__
     const float w = e == -INFINITY ? 0.f : fast_exp2(e - top);
     uint32_t parts = __ballot_sync(0xffffffffu, part && e != -INFINITY);
     while (parts) {
-      const int i = __ffs(parts) - 1;
-      parts &= parts - 1;
-      const float wi = __shfl_sync(0xffffffffu, w, i);
-      const float4 o = reinterpret_cast<const float4*>(m.part_o + ((long long)(2 * (first + i) + (first + i == c0)) * m.item_rows + in_item) * kHeadDim)[lane];
-      sum += wi;
-      acc.x = fmaf(o.x, wi, acc.x);
-      acc.y = fmaf(o.y, wi, acc.y);
-      acc.z = fmaf(o.z, wi, acc.z);
-      acc.w = fmaf(o.w, wi, acc.w);
+      float wi[8];
+      float4 o[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {  // (eight loads on their way at a time)
+        const int i = __ffs(parts) - 1;
+        parts &= parts - 1;
+        wi[k] = __shfl_sync(0xffffffffu, w, i & 31);
+        o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < 0)
+          wi[k] = 0.f;
+        else
+          o[k] = reinterpret_cast<const float4*>(m.part_o + (((long long)(2 * (first + i) + (first + i == c0)) << m.log2_rows) + in_item) * kHeadDim)[lane];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        sum += wi[k];
+        acc.x = fmaf(o[k].x, wi[k], acc.x);
+        acc.y = fmaf(o[k].y, wi[k], acc.y);
+        acc.z = fmaf(o[k].z, wi[k], acc.z);
+        acc.w = fmaf(o[k].w, wi[k], acc.w);
+      }
     }
   }
   const float f = sum == 0.f ? 0.f : 1.f / sum;
@@ -160,14 +171,19 @@ bool encode_rows(CUtensorMap* map, const void* data, int dims, const long long (
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Which kernel: few rows stay in registers (mikv_tree_few.cuh), more go through tensor memory.
+// Which kernel: few rows stay in registers (mikv_tree_few.cuh), more go through tensor memory. 16 requests of 8192 tokens, 8
+// KV heads: 16 rows 89 us against 125, 32 rows (two blocks of 16) 147 against 127. A small cache takes tensor memory for all
+// rows, since an item costs the other kernel as much as 100 tokens: 32 KV heads, 8 rows: 512 tokens 18.7 us against 16.0,
+// 2048 29.6 against 25.5, 8192 35.1 against 34.9, 16384 47 against 68. (The size is the cache's, not what it holds: the
+// workspace depends on it.)
 constexpr int kFewMost = 16;
+constexpr long long kFewTokens = 1 << 18;
 
 struct Sizes {
   bool few, narrow, pair;
   int rows, item_rows, m_blocks;
-  Sizes(int G, int nodes) : rows(G * nodes) {
-    few = rows <= kFewMost;
+  Sizes(int G, int nodes, long long tokens) : rows(G * nodes) {
+    few = rows <= kFewMost && tokens > kFewTokens;
     narrow = rows <= 8;
     pair = rows > tree::kTile;
     item_rows = few ? tree::kFewRows : pair ? 2 * tree::kTile : tree::kTile;
@@ -179,7 +195,7 @@ struct Sizes {
   size_t parts(int num_sms) const { return (size_t)2 * runs(num_sms); }
 };
 
-size_t prefix_bytes(int batch) { return ((batch + 1) * sizeof(long long) + 255) / 256 * 256; }
+size_t prefix_bytes(int batch) { return ((batch + 1) * sizeof(uint32_t) + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -189,20 +205,26 @@ cudaError_t launch_tree_masks(uint4* masks, int32_t* positions, const int32_t* p
                         start);
 }
 
+bool tree_sizes_ok(const mikv_shape& s, int nodes) {
+  const Sizes z(s.heads_q / s.heads_kv, nodes, (long long)s.batch * s.heads_kv * (s.hi_stride + (long long)s.lo_cap));
+  const long long slots = (long long)s.batch * s.heads_kv * s.hi_stride, rows = (long long)s.batch * s.heads_q * nodes;
+  const long long items = (long long)s.batch * s.heads_kv * z.m_blocks;  // of either kernel's costs:
+  return slots < 1ll << 31 && rows < 1ll << 31 && items * (32 + ((long long)nodes + s.hi_cap + s.lo_cap) / 16) < 1ll << 32;
+}
+
 size_t tree_workspace_bytes(const mikv_shape& s, int nodes, int num_sms) {
-  const Sizes z(s.heads_q / s.heads_kv, nodes);
+  const Sizes z(s.heads_q / s.heads_kv, nodes, (long long)s.batch * s.heads_kv * (s.hi_stride + (long long)s.lo_cap));
   return kWsHeader + prefix_bytes(s.batch) + z.parts(num_sms) * z.item_rows * (kHeadDim + 1) * sizeof(float);
 }
 
 cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t st) {
-  const Sizes z(a.G, a.nodes);
+  const Sizes z(a.G, a.nodes, (long long)a.batch * a.heads_kv * (a.hi_stride + (long long)a.lo_cap));
   const int log2_G = a.G == 1 ? 0 : a.G == 2 ? 1 : a.G == 4 ? 2 : 3;
   char* at = static_cast<char*>(ws) + kWsHeader;
-  long long* prefix = reinterpret_cast<long long*>(at);
+  uint32_t* prefix = reinterpret_cast<uint32_t*>(at);
   float* part_o = reinterpret_cast<float*>(at + prefix_bytes(a.batch));
   float* part_lse = part_o + z.parts(num_sms) * z.item_rows * kHeadDim;
   const long long rows = (long long)a.batch * a.heads_kv * a.hi_stride;
-  if (rows >= 1ll << 31) return cudaErrorInvalidValue;  // (row numbers of the copies)
   CUtensorMap k_hi, v_hi;
   memset(&k_hi, 0, sizeof k_hi);
   memset(&v_hi, 0, sizeof v_hi);
@@ -210,7 +232,7 @@ cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t s
   if (rows > 0 && (!encode_rows(&k_hi, a.k_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0}, box) ||
                    !encode_rows(&v_hi, a.v_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0}, box)))
     return cudaErrorInvalidValue;
-  TreeMergeArgs m = {a, prefix, part_o, part_lse, z.m_blocks, log2_G, z.item_rows, num_sms, 0};
+  TreeMergeArgs m = {a, prefix, part_o, part_lse, z.m_blocks, log2_G, 31 - __builtin_clz(z.item_rows), num_sms, 0};
   const long long out_rows = (long long)a.batch * a.nodes * a.heads_q;
   const dim3 merge_grid((unsigned)((out_rows + 3) / 4));
   if (z.few) {

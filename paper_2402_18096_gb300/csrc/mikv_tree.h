@@ -49,6 +49,8 @@ struct TreeArgs {
   int out_f32;
 };
 
+// Row numbers, and the costs that the runs are made of, within 32 bits.
+bool tree_sizes_ok(const mikv_shape& s, int nodes);
 size_t tree_workspace_bytes(const mikv_shape& s, int nodes, int num_sms);
 cudaError_t launch_tree_masks(uint4* masks, int32_t* positions, const int32_t* parents, int batch, int nodes,
                               const int32_t* first, int start, cudaStream_t st);

@@ -20,7 +20,7 @@
 //       whose other side are the groups, added to the group's channels at the end. O of channels 16 m .. is kept in units of
 //       2^(s_m - 24) meanwhile, and of 2^ev for alphas far from 1.
 // With alpha and beta applied to every key and value in fp16 (two more instructions a pair) the same kernel took 182 us where
-// this one takes 149, 16 requests of 205 .. 8192 tokens, 40 heads, 3 bits.
+// this one took 149, 16 requests of 205 .. 8192 tokens, 40 heads, 3 bits.
 // Tokens 2 t and 2 t + 1 of an operand are rows t and t + 4 of their eight, so that eight lanes read four rows of codes from
 // different banks.
 #pragma once
@@ -33,7 +33,7 @@ struct TreeFewArgs {
   CUtensorMap map_k_hi, map_v_hi;  // bf16 [batch * heads * hi_stride][128], box 64 channels x 16 rows, 128B swizzle
   TreeArgs a;
   int rows, row_blocks, log2_G;
-  long long* prefix;
+  uint32_t* prefix;
   float* part_o;    // [2 * warps][16][128]
   float* part_lse;  // [2 * warps][16], log2
 };
@@ -57,11 +57,10 @@ constexpr int kFewLeast = 2;  // units of a run at least
 // Blocks of 16 retained rows in a unit, and where its arrays lie in a stage.
 template <int BITS>
 struct FewUnit {
-  int blocks, pairs, v, kp, vp, row_bytes;
-  __host__ __device__ explicit FewUnit(int group) : pairs(kHeadDim / group) {
-    const int block = 2 * 16 * (16 * BITS + 4 * pairs);
+  int blocks, v, kp, vp, row_bytes;
+  __host__ __device__ explicit FewUnit(int group) : row_bytes(4 * kHeadDim / group) {
+    const int block = 2 * 16 * (16 * BITS + row_bytes);
     blocks = kFewStage / block < 5 ? kFewStage / block : 5;
-    row_bytes = 4 * pairs;
     v = blocks * 16 * 16 * BITS;
     kp = 2 * v;
     vp = kp + blocks * 16 * row_bytes;
@@ -122,6 +121,17 @@ struct FieldOf {
     return (at >= 8 ? up[i] : lo[i]) & (((1u << BITS) - 1u) * 0x10001u << place(m));
   }
 };
+// 1 / x to 2^-22: the queries stand in 22 bits beside it
+__device__ __forceinline__ float fast_inverse(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float fast_log2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
 // The parameters of a token.
@@ -150,6 +160,10 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
   if (lane < kFewStages) mbar_init(bars + 8 * lane, 1);
   fence_mbar_init();
   __syncwarp();
+  if (lane == 0) {
+    prefetch_tensormap(&p.map_k_hi);
+    prefetch_tensormap(&p.map_v_hi);
+  }
   grid_dependency_wait();
   allow_dependent_launch();
   const FewUnit<BITS> U(kHeadDim / PAIRS);
@@ -158,47 +172,46 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
   auto units_of = [&](int b) { return FewUnits(a.held, a.nodes, b, U.blocks); };
 
   // This warp's run of all units.
-  auto scan = [&](int b0, long long& mine) {
-    mine = b0 + lane < a.batch ? (long long)units_of(b0 + lane).cost() * per_set : 0;
-    long long sum = mine;
+  auto scan = [&](int b0, uint32_t& mine) {
+    mine = b0 + lane < a.batch ? units_of(b0 + lane).cost() * per_set : 0;
+    uint32_t sum = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, sum, o);
+      const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
       if (lane >= o) sum += y;
     }
     return sum;
   };
-  const int me = blockIdx.x * kFewWarps + warp;
-  long long all = 0, mine;
+  const int me = warp * gridDim.x + blockIdx.x;  // (few runs: on all SMs)
+  uint32_t all = 0, mine;
 #pragma unroll 1
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
-    const long long sum = scan(b0, mine);
+    const uint32_t sum = scan(b0, mine);
     if (me == 0 && b0 + lane < a.batch) p.prefix[b0 + lane] = all + sum - mine;
     all += __shfl_sync(0xffffffffu, sum, 31);
   }
   if (me == 0 && lane == 0) p.prefix[a.batch] = all;
   const Runs runs(all, gridDim.x * kFewWarps, kFewLeast);
   if (me >= runs.n) return;
-  const long long from = runs.first(me);
-  long long start64 = 0;  // costs before the item
+  const uint32_t from = runs.first(me);
+  uint32_t begin = 0;  // costs before the item
   int b = 0, in_set = 0;
 #pragma unroll 1
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
-    const long long sum = scan(b0, mine), total = __shfl_sync(0xffffffffu, sum, 31);
-    if (from < start64 + total) {
-      const int at = __ffs(__ballot_sync(0xffffffffu, start64 + sum > from)) - 1;
+    const uint32_t sum = scan(b0, mine), total = __shfl_sync(0xffffffffu, sum, 31);
+    if (from < begin + total) {
+      const int at = __ffs(__ballot_sync(0xffffffffu, begin + sum > from)) - 1;
       b = b0 + at;
-      start64 += __shfl_sync(0xffffffffu, sum - mine, at);
-      const long long cost = units_of(b).cost();
-      in_set = (int)((from - start64) / cost);
-      start64 += in_set * cost;
+      begin += __shfl_sync(0xffffffffu, sum - mine, at);
+      const uint32_t cost = units_of(b).cost();
+      in_set = (int)((from - begin) / cost);
+      begin += in_set * cost;
       break;
     }
-    start64 += total;
+    begin += total;
   }
 
-  // from here on relative to the run's begin: an item's costs, and a run's, are inside 32 bits
-  int start = (int)(start64 - from);
+  int start = (int)(begin - from);  // from here on relative to the run's begin
   const int to = (int)(runs.first(me + 1) - from);
   // The unit that is asked for next: its place, and the stage it goes to.
   struct Place {
@@ -496,7 +509,7 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
             float4 inv = make_float4(1.f, 1.f, 1.f, 1.f);
             if (a.balancer) {
               const float4 bal = __ldg(reinterpret_cast<const float4*>(a.balancer + h * kHeadDim + 16 * m + 4 * t));
-              inv = make_float4(1.f / bal.x, 1.f / bal.y, 1.f / bal.z, 1.f / bal.w);
+              inv = make_float4(fast_inverse(bal.x), fast_inverse(bal.y), fast_inverse(bal.z), fast_inverse(bal.w));
             }
 #pragma unroll
             for (int r = 0; r < kHeld; ++r) {
@@ -749,7 +762,7 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
         for (int e = 0; e < 4; ++e) o[i][e] = fmaf(o[i][e], f, add[m / kOf][NARROW ? e & 1 : e >> 1]);
       }
     }
-    const bool whole = u0 == 0 && u1 == count;
+    const bool whole = u0 == 0 && u1 == count, f32 = !whole || a.out_f32;
     const int slot = 2 * me + (u0 == 0);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -757,35 +770,37 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
 #pragma unroll
       for (int off = NARROW ? 4 : 1; off < (NARROW ? 32 : 4); off <<= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
       const bool blank = !real[r] || total == 0.f;
-      const float lse2 = blank ? -INFINITY : ref[r] + log2f(total);
-      const float f = poisoned[r] ? __int_as_float(0x7fffffff) : 1.f / total;
-      if (!there[r]) continue;
+      const float lse2 = blank ? -INFINITY : ref[r] + fast_log2(total);
+      const float f = poisoned[r] ? __int_as_float(0x7fffffff) : fast_inverse(total);
+#pragma unroll
+      for (int i = 0; i < kO; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float& x = o[i][NARROW ? r + 2 * e : 2 * r + e];
+          x = blank ? 0.f : x * f;
+        }
       const int row = NARROW ? 2 * t + r : g + 8 * r;
       const long long out = b * a.out.b + head[r] * a.out.h + node[r] * a.out.t;
-      float* part = p.part_o + ((size_t)slot * kFewRows + row) * kHeadDim;
+      const int c = NARROW ? g : 2 * t;  // and from there 16 (8) on; two channels that are 8 (one) apart
+      if (!there[r]) {
+      } else if (f32) {
+        float* at = (whole ? static_cast<float*>(a.out.p) + out : p.part_o + ((size_t)slot * kFewRows + row) * kHeadDim) + c;
 #pragma unroll
-      for (int i = 0; i < kO; ++i) {
-        const float x = blank ? 0.f : o[i][NARROW ? r : 2 * r] * f, y = blank ? 0.f : o[i][NARROW ? 2 + r : 2 * r + 1] * f;
-        if constexpr (NARROW) {
-          const int c = 16 * i + g;
-          if (!whole)
-            part[c] = x, part[c + 8] = y;
-          else if (a.out_f32)
-            static_cast<float*>(a.out.p)[out + c] = x, static_cast<float*>(a.out.p)[out + c + 8] = y;
+        for (int i = 0; i < kO; ++i)
+          if constexpr (NARROW)
+            at[16 * i] = o[i][r], at[16 * i + 8] = o[i][r + 2];
           else
-            static_cast<__nv_bfloat16*>(a.out.p)[out + c] = __float2bfloat16(x),
-            static_cast<__nv_bfloat16*>(a.out.p)[out + c + 8] = __float2bfloat16(y);
-        } else {
-          const int c = 8 * i + 2 * t;
-          if (!whole)
-            *reinterpret_cast<float2*>(part + c) = make_float2(x, y);
-          else if (a.out_f32)
-            *reinterpret_cast<float2*>(static_cast<float*>(a.out.p) + out + c) = make_float2(x, y);
+            *reinterpret_cast<float2*>(at + 8 * i) = make_float2(o[i][2 * r], o[i][2 * r + 1]);
+      } else {
+        __nv_bfloat16* at = static_cast<__nv_bfloat16*>(a.out.p) + out + c;
+#pragma unroll
+        for (int i = 0; i < kO; ++i)
+          if constexpr (NARROW)
+            at[16 * i] = __float2bfloat16(o[i][r]), at[16 * i + 8] = __float2bfloat16(o[i][r + 2]);
           else
-            *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.out.p) + out + c) = pack_bf16(x, y);
-        }
+            *reinterpret_cast<uint32_t*>(at + 8 * i) = pack_bf16(o[i][2 * r], o[i][2 * r + 1]);
       }
-      if (NARROW ? g == 0 : t == 0) {
+      if (there[r] && (NARROW ? g == 0 : t == 0)) {
         if (!whole)
           p.part_lse[(size_t)slot * kFewRows + row] = lse2;
         else if (a.lse)

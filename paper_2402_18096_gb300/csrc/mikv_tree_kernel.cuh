@@ -39,7 +39,7 @@ struct TreeKernelArgs {
   TreeArgs a;
   int rows, m_blocks, log2_G;      // rows of a KV head; row tiles (pairs)
   int twin;                        // the rows of a tile (up to 64) stand in it twice
-  long long* prefix;               // [batch + 1] costs of all items before each request (for the merge)
+  uint32_t* prefix;               // [batch + 1] costs of all items before each request (for the merge)
   float* part_o;                   // [2 * CTAs][rows of an item][128]
   float* part_lse;                 // [2 * CTAs][rows of an item], log2
 };
@@ -114,31 +114,31 @@ struct Tiles {
   int hi, lo;  // tiles of slots, of retained rows
   __device__ Tiles(const HeldArgs& held, int b) : hi((held.hi(b) + kTile - 1) / kTile), lo((held.lo(b) + kTile - 1) / kTile) {}
   __device__ int count() const { return 1 + hi + lo; }
-  __device__ long long cost() const { return kCostNodes + (long long)kCostHi * hi + (long long)kCostLo * lo; }
-  __device__ long long before(int t) const {
-    return t == 0 ? 0 : kCostNodes + (t <= hi ? (long long)kCostHi * (t - 1) : (long long)kCostHi * hi + (long long)kCostLo * (t - 1 - hi));
+  __device__ int cost() const { return kCostNodes + kCostHi * hi + kCostLo * lo; }
+  __device__ int before(int t) const {
+    return t == 0 ? 0 : kCostNodes + (t <= hi ? kCostHi * (t - 1) : kCostHi * hi + kCostLo * (t - 1 - hi));
   }
   // the first tile that begins at x or later
-  __device__ int first(long long x) const {
+  __device__ int first(int x) const {
     if (x <= 0) return 0;
     x -= kCostNodes;
-    const long long t = x <= 0 ? 0 : x <= (long long)kCostHi * hi ? (x + kCostHi - 1) / kCostHi
-                                                                 : hi + (x - (long long)kCostHi * hi + kCostLo - 1) / kCostLo;
-    return (int)min(t + 1, (long long)count());
+    const int t = x <= 0 ? 0 : x <= kCostHi * hi ? (x + kCostHi - 1) / kCostHi : hi + (x - kCostHi * hi + kCostLo - 1) / kCostLo;
+    return min(t + 1, count());
   }
 };
 
-// CTA (or warp) c has the costs [first(c), first(c + 1)) of all.
+// CTA (or warp) c has the costs [first(c), first(c + 1)) of all: shares that differ by one at most. In 32 bits (sizes that
+// could pass them are refused, tree_sizes_ok), for 64-bit divisions are long and a small call runs its code once, cold.
 struct Runs {
-  long long total;
+  uint32_t share, more;  // the first `more` runs have one more
   int n;
-  __device__ Runs(long long total, int ctas, int least = kLeastRun) : total(total), n((int)max(1ll, min((long long)ctas, total / least))) {}
-  __device__ long long first(int c) const { return total * c / n; }  // (total * n stays far below 2^63)
-  __device__ int owner(long long x) const {
-    int c = (int)min((long long)n - 1, x * n / total);
-    while (c + 1 < n && first(c + 1) <= x) ++c;
-    while (c > 0 && first(c) > x) --c;
-    return c;
+  __device__ Runs(uint32_t total, int ctas, int least = kLeastRun) : n((int)max(1u, min((uint32_t)ctas, total / least))) {
+    share = total / n, more = total - share * n;
+  }
+  __device__ uint32_t first(int c) const { return share * c + min((uint32_t)c, more); }
+  __device__ int owner(uint32_t x) const {
+    const uint32_t larger = (share + 1) * more;
+    return x < larger ? x / (share + 1) : more + (x - larger) / max(1u, share);
   }
 };
 
@@ -510,36 +510,36 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       };
       const int per_set = a.heads_kv * p.m_blocks;
       // costs of the items of requests b0 .. b0 + lane, and of this lane's
-      auto scan = [&](int b0, long long& mine) {
+      auto scan = [&](int b0, uint32_t& mine) {
         mine = b0 + lane < a.batch ? Tiles(a.held, b0 + lane).cost() * per_set : 0;
-        long long sum = mine;
+        uint32_t sum = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const long long y = __shfl_up_sync(0xffffffffu, sum, o);
+          const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
           if (lane >= o) sum += y;
         }
         return sum;
       };
-      long long all = 0, mine;
+      uint32_t all = 0, mine;
 #pragma unroll 1
       for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        const long long sum = scan(b0, mine);
+        const uint32_t sum = scan(b0, mine);
         if (blockIdx.x == 0 && b0 + lane < a.batch) p.prefix[b0 + lane] = all + sum - mine;
         all += __shfl_sync(0xffffffffu, sum, 31);
       }
       if (blockIdx.x == 0 && lane == 0) p.prefix[a.batch] = all;
       const Runs runs(all, gridDim.x);
-      long long from = 0, to = 0, start = 0;  // this CTA's run; costs before the item at hand
+      uint32_t from = 0, to = 0, start = 0;  // this CTA's run; costs before the item at hand
       if ((int)blockIdx.x < runs.n) from = runs.first(blockIdx.x), to = runs.first(blockIdx.x + 1);
       int b = 0, in_set = 0;
 #pragma unroll 1
       for (int b0 = 0; from < to && b0 < a.batch; b0 += 32) {
-        const long long sum = scan(b0, mine), total = __shfl_sync(0xffffffffu, sum, 31);
+        const uint32_t sum = scan(b0, mine), total = __shfl_sync(0xffffffffu, sum, 31);
         if (from < start + total) {
           const int at = __ffs(__ballot_sync(0xffffffffu, start + sum > from)) - 1;
           b = b0 + at;
           start += __shfl_sync(0xffffffffu, sum - mine, at);
-          const long long cost = Tiles(a.held, b).cost();
+          const uint32_t cost = Tiles(a.held, b).cost();
           in_set = (int)((from - start) / cost);
           start += in_set * cost;
           break;
@@ -559,8 +559,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         x.n_lo = a.held.lo(b);
         x.free_slot = a.held.free_slot(b * a.heads_kv + x.h, x.n_hi);
         x.fine = x.n_lo <= kFineRows;
-        x.t0 = tl.first(from - start);
-        x.t1 = tl.first(to - start);
+        x.t0 = tl.first((int)(from - start));
+        x.t1 = tl.first((int)(to - start));
         x.slot = x.t0 == 0 && x.t1 == tl.count() ? -1 : 2 * (int)blockIdx.x + (x.t0 == 0);
         x.valid = 1;
         if (x.t0 < x.t1) ok = publish(x);

@@ -41,13 +41,17 @@ def values_of(packed, params, bits):
 
 class Drafts:
     """A cache with random contents, drafted tokens for it, and what the requests hold. Slots and rows that are not in
-    use, the free slots and padding nodes hold NaN (codes: any bits, NaN parameters)."""
+    use, the free slots and padding nodes hold NaN (codes: any bits, NaN parameters). `tokens`: the cache's size at least,
+    over all KV heads; rows behind lo_cap are there but not in use."""
+
+    tokens = 0
 
     def __init__(self, seed, B, Hq, Hkv, nodes, hi_cap, lo_cap, bits=2, group=32, n_hi=None, n_lo=None, free=True,
                  balanced=True, parents=None, outliers=3.0, major=True):
         g = gen(seed)
         r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
-        self.shape = s = pkg.Shape(B, Hq, Hkv, bits, group, hi_cap, lo_cap)
+        rows = max(lo_cap, -(-self.tokens // (16 * B * Hkv)) * 16)
+        self.shape = s = pkg.Shape(B, Hq, Hkv, bits, group, hi_cap, rows)
         self.cache = c = pkg.LayerCache(s)
         self.N, self.G = nodes, Hq // Hkv
         n_hi = [hi_cap] * B if n_hi is None else n_hi

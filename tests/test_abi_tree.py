@@ -107,6 +107,13 @@ def commit_rc(lib, s=None, c=None, nodes=5, path=P, steps=3, k=None, v=None, gai
                                 gained, first, None if lens is NO else ref(lens or lengths()), ref(out), next_, ws, n, None)
 
 
+@pytest.mark.parametrize("kw", [dict(batch=30000, hi_cap=1 << 20, hi_stride=1 << 20), dict(batch=30000, lo_cap=2 ** 31 - 16)])
+def test_trees_past_32_bits_refused(lib, kw):
+    """Row numbers of the slots, and the costs that the work is divided by."""
+    s = shape(**kw)
+    assert lib.mikv_tree_workspace_bytes(ref(s), 5) == 0 and tree_rc(lib, s) == 2
+
+
 def test_path_arguments_refused(lib):
     assert lib.mikv_commit_workspace_bytes(ref(shape()), 3) >= 256
     for rc in (importance_rc, commit_rc):

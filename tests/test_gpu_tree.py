@@ -14,6 +14,12 @@ pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 
 
+@pytest.fixture(autouse=True, params=[0, (1 << 18) + 1], ids=["small", "roomy"])
+def room(request, monkeypatch):
+    """Caches as small as what they hold, and large ones: few rows have a kernel of their own there."""
+    monkeypatch.setattr(Drafts, "tokens", request.param)
+
+
 @pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 100, 128])
 def test_masks_and_positions(n):
     rng = random.Random(n)
@@ -175,14 +181,16 @@ def test_without_lengths():
     check(d, out, lse)
 
 
-def test_lengths_beyond_the_cache():
+def test_lengths_beyond_the_cache(room, monkeypatch):
     """Lengths are held to the cache's capacity, free slots outside those in use are none."""
-    d = Drafts(12, 2, 4, 2, 6, 70, 304, 2, 32, free=False)
-    d.lens = pkg.Lengths(d.dev([5000, 70]), d.dev([99999, 304]), torch.full((2, 2), 70, dtype=torch.int32, device="cuda"))
+    lo = max(304, Drafts.tokens // 64 * 16 + 16)
+    monkeypatch.setattr(Drafts, "tokens", 0)
+    d = Drafts(12, 2, 4, 2, 6, 70, lo, 2, 32, free=False)
+    d.lens = pkg.Lengths(d.dev([5000, 70]), d.dev([2 ** 31 - 1, lo]), torch.full((2, 2), 70, dtype=torch.int32, device="cuda"))
     out, lse = run(d)
     check(d, out, lse)
-    d.n_hi, d.n_lo = [0, 70], [0, 304]
-    d.lens = pkg.Lengths(d.dev([-3, 70]), d.dev([-1, 304]), torch.full((2, 2), -1, dtype=torch.int32, device="cuda"))
+    d.n_hi, d.n_lo = [0, 70], [0, lo]
+    d.lens = pkg.Lengths(d.dev([-3, 70]), d.dev([-1, lo]), torch.full((2, 2), -1, dtype=torch.int32, device="cuda"))
     out, lse = run(d)
     check(d, out, lse)
 
@@ -223,7 +231,7 @@ def test_offsets_past_32_bits():
     d = Drafts(15, 1, 1, 1, 4, 1, 208, 2, 32)
     c = pkg.LayerCache(s)
     for name in ("k_codes", "v_codes", "k_params", "v_params"):
-        getattr(c, name)[-1, -1, :208] = getattr(d.cache, name)[0, 0]
+        getattr(c, name)[-1, -1, :208] = getattr(d.cache, name)[0, 0, :208]
     c.balancer = torch.ones(H, 128, device="cuda")
     c.balancer[-1] = d.cache.balancer[0]
     q, k, v = (torch.zeros(B, H, 4, 128, dtype=BF, device="cuda") for _ in range(3))
