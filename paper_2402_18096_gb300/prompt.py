@@ -50,7 +50,7 @@ def _dense(t, shape, dtype, name):
         return None
     if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
+    return t.data_ptr() if t.is_cuda and t.is_contiguous() else _ptr(t)
 
 
 def _raw_stream(stream, t: torch.Tensor) -> int:

@@ -19,6 +19,8 @@ from .prompt import _dense, _raw_stream, _view
 TREE_NODES = 128  # drafted tokens of a request at most
 
 _OUT = {torch.bfloat16: 0, torch.float32: 2}
+_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+_SCALE = 1.0 / math.sqrt(HEAD_DIM)
 _pack_shape = struct.Struct("12i").pack     # mikv_shape
 _pack_cache = struct.Struct("12P").pack     # mikv_cache
 _pack_lengths = struct.Struct("PPPi").pack  # mikv_lengths
@@ -36,12 +38,11 @@ class Lengths:
         self.n_lo_max = n_lo if isinstance(n_lo, int) else 0 if n_lo is None else n_lo_max
 
     def _packed(self, shape) -> bytes:
-        B = (shape.batch,)
-        most = self.n_lo_max
+        B, hi, lo, slots, most = (shape.batch,), self.n_hi, self.n_lo, self.slots, self.n_lo_max
         if most is None:
             most = shape.lo_cap if shape.bits else 0
-        return _pack_lengths(_dense(self.n_hi, B, torch.int32, "n_hi") or 0, _dense(self.n_lo, B, torch.int32, "n_lo") or 0,
-                             _dense(self.slots, (shape.batch, shape.heads_kv), torch.int32, "slots") or 0, most)
+        return _pack_lengths(0 if hi is None else _dense(hi, B, _I32, "n_hi"), 0 if lo is None else _dense(lo, B, _I32, "n_lo"),
+                             0 if slots is None else _dense(slots, (shape.batch, shape.heads_kv), _I32, "slots"), most)
 
 
 def _shape(s) -> bytes:
@@ -50,18 +51,20 @@ def _shape(s) -> bytes:
 
 
 def _cache(c) -> bytes:
-    return _pack_cache(*[_ptr(t) or 0 for t in (c.k_hi, c.v_hi, c.hi_tok, c.acc, c.k_codes, c.v_codes, c.k_params,
-                                                c.v_params, c.lo_tok, c.balancer, c.k_hi_params, c.v_hi_params)])
+    # (without a call for every array: 1 of the 10 us that a call takes on the host)
+    return _pack_cache(*[0 if t is None else t.data_ptr() if t.is_cuda and t.is_contiguous() else _ptr(t)
+                         for t in (c.k_hi, c.v_hi, c.hi_tok, c.acc, c.k_codes, c.v_codes, c.k_params, c.v_params,
+                                   c.lo_tok, c.balancer, c.k_hi_params, c.v_hi_params)])
 
 
 def _lens(lens, shape):
     return None if lens is None else lens._packed(shape)
 
 
-def _bf16(**tensors):
-    for name, t in tensors.items():
-        if t.dtype != torch.bfloat16:
-            raise ValueError(f"{name}: expected bfloat16, got {t.dtype}")
+def _bf16(names, *tensors):
+    for t in tensors:
+        if t.dtype != _BF16:
+            raise ValueError(f"{', '.join(names)}: expected bfloat16, got {', '.join(str(x.dtype) for x in tensors)}")
 
 
 def mikv_tree_masks(masks, parents, positions=None, first=None, start: int = 0, stream=None):
@@ -70,8 +73,8 @@ def mikv_tree_masks(masks, parents, positions=None, first=None, start: int = 0, 
     `start`) plus a node's number of ancestors, for mikv_rotary."""
     B, N = parents.shape
     _check("mikv_tree_masks", load().mikv_tree_masks(
-        _dense(masks, (B, N, 4), torch.int32, "masks"), _dense(positions, (B, N), torch.int32, "positions"),
-        _dense(parents, (B, N), torch.int32, "parents"), B, N, _dense(first, (B,), torch.int32, "first"), start,
+        _dense(masks, (B, N, 4), _I32, "masks"), _dense(positions, (B, N), _I32, "positions"),
+        _dense(parents, (B, N), _I32, "parents"), B, N, _dense(first, (B,), _I32, "first"), start,
         _raw_stream(stream, parents)))
 
 
@@ -87,14 +90,14 @@ def mikv_tree_attention(cache, masks, q, k, v, out, workspace, lens: Lengths = N
     s = cache.shape
     N = q.shape[2]
     qs, ks = (s.batch, s.heads_q, N, HEAD_DIM), (s.batch, s.heads_kv, N, HEAD_DIM)
-    _bf16(q=q, k=k, v=v)
+    _bf16("qkv", q, k, v)
     dt = _OUT.get(out.dtype)
     if dt is None:
         raise ValueError(f"out: expected bfloat16 or float32, got {out.dtype}")
     rc = load().mikv_tree_attention(
-        _shape(s), _cache(cache), _pack_tree(N, dt, 1.0 / math.sqrt(HEAD_DIM) if sm_scale is None else sm_scale),
-        _dense(masks, (s.batch, N, 4), torch.int32, "masks"), _view(q, qs), _view(k, ks), _view(v, ks), _view(out, qs),
-        _lens(lens, s), _dense(lse, qs[:3], torch.float32, "lse"), _ptr(workspace), workspace.nbytes,
+        _shape(s), _cache(cache), _pack_tree(N, dt, _SCALE if sm_scale is None else sm_scale),
+        _dense(masks, (s.batch, N, 4), _I32, "masks"), _view(q, qs), _view(k, ks), _view(v, ks), _view(out, qs),
+        _lens(lens, s), _dense(lse, qs[:3], _F32, "lse"), _ptr(workspace), workspace.nbytes,
         _raw_stream(stream, q))
     _check("mikv_tree_attention", rc)
 
@@ -105,12 +108,12 @@ def mikv_path_importance(cache, path, q, k, lse, gained, lens: Lengths = None, s
     mikv_tree_attention."""
     s = cache.shape
     N, steps = q.shape[2], path.shape[-1]
-    _bf16(q=q, k=k)
+    _bf16("qk", q, k)
     rc = load().mikv_path_importance(
-        _shape(s), _cache(cache), N, 1.0 / math.sqrt(HEAD_DIM) if sm_scale is None else sm_scale,
-        _dense(path, (s.batch, steps), torch.int32, "path"), steps, _view(q, (s.batch, s.heads_q, N, HEAD_DIM)),
-        _view(k, (s.batch, s.heads_kv, N, HEAD_DIM)), _dense(lse, (s.batch, s.heads_q, N), torch.float32, "lse"),
-        _lens(lens, s), _dense(gained, (s.batch, s.heads_kv, steps), torch.float32, "gained"), _raw_stream(stream, q))
+        _shape(s), _cache(cache), N, _SCALE if sm_scale is None else sm_scale,
+        _dense(path, (s.batch, steps), _I32, "path"), steps, _view(q, (s.batch, s.heads_q, N, HEAD_DIM)),
+        _view(k, (s.batch, s.heads_kv, N, HEAD_DIM)), _dense(lse, (s.batch, s.heads_q, N), _F32, "lse"),
+        _lens(lens, s), _dense(gained, (s.batch, s.heads_kv, steps), _F32, "gained"), _raw_stream(stream, q))
     _check("mikv_path_importance", rc)
 
 
@@ -126,12 +129,12 @@ def mikv_commit_path(cache, path, k, v, gained, first, workspace, lens: Lengths,
     s = cache.shape
     N, steps = k.shape[2], path.shape[-1]
     ks = (s.batch, s.heads_kv, N, HEAD_DIM)
-    _bf16(k=k, v=v)
+    _bf16("kv", k, v)
     rc = load().mikv_commit_path(
-        _shape(s), _cache(cache), N, _dense(path, (s.batch, steps), torch.int32, "path"), steps, _view(k, ks),
-        _view(v, ks), _dense(gained, (s.batch, s.heads_kv, steps), torch.float32, "gained"),
-        _dense(first, (s.batch,), torch.int32, "first"), _lens(lens, s), _lens(lens_out, s),
-        _dense(next, (s.batch,), torch.int32, "next"), _ptr(workspace), workspace.nbytes, _raw_stream(stream, k))
+        _shape(s), _cache(cache), N, _dense(path, (s.batch, steps), _I32, "path"), steps, _view(k, ks),
+        _view(v, ks), _dense(gained, (s.batch, s.heads_kv, steps), _F32, "gained"),
+        _dense(first, (s.batch,), _I32, "first"), _lens(lens, s), _lens(lens_out, s),
+        _dense(next, (s.batch,), _I32, "next"), _ptr(workspace), workspace.nbytes, _raw_stream(stream, k))
     _check("mikv_commit_path", rc)
 
 
