@@ -325,15 +325,15 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
       const bool wide = ((reinterpret_cast<uintptr_t>(from) | reinterpret_cast<uintptr_t>(to)) & 15) == 0;
       const long long end16 = wide ? lo + ((hi - lo) & ~15ll) : lo;
       long long at = lo + 16 * threadIdx.x;
-      for (; at + 16ll * kCopyThreads * (kInFlight - 1) < end16; at += 16ll * kCopyThreads * kInFlight) {
+      for (; at < end16; at += 16ll * kCopyThreads * kInFlight) {
         uint4 v[kInFlight];
 #pragma unroll
-        for (int k = 0; k < kInFlight; ++k) v[k] = __ldg(reinterpret_cast<const uint4*>(from + at + 16ll * kCopyThreads * k));
+        for (int k = 0; k < kInFlight; ++k)
+          if (at + 16ll * kCopyThreads * k < end16) v[k] = __ldg(reinterpret_cast<const uint4*>(from + at + 16ll * kCopyThreads * k));
 #pragma unroll
-        for (int k = 0; k < kInFlight; ++k) __stcs(reinterpret_cast<uint4*>(to + at + 16ll * kCopyThreads * k), v[k]);
+        for (int k = 0; k < kInFlight; ++k)
+          if (at + 16ll * kCopyThreads * k < end16) __stcs(reinterpret_cast<uint4*>(to + at + 16ll * kCopyThreads * k), v[k]);
       }
-      for (; at < end16; at += 16ll * kCopyThreads)
-        __stcs(reinterpret_cast<uint4*>(to + at), __ldg(reinterpret_cast<const uint4*>(from + at)));
       for (at = end16 + 4 * threadIdx.x; at < hi; at += 4 * kCopyThreads)
         *reinterpret_cast<uint32_t*>(to + at) = *reinterpret_cast<const uint32_t*>(from + at);
       const long long whole = (bytes + 15) / 16 * 16;  // (the next array's pieces begin at a multiple of 16 bytes)
