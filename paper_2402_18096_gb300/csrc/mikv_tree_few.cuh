@@ -700,16 +700,15 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
               for (int e = 0; e < 4; ++e) o[i][e] *= f;
             alpha_most = power2(ev + 6), unit = __float2half2_rn(power2(-ev));
           }
-          const uint32_t sel = g & 1 ? 0x7632u : 0x5410u, rows[4] = {vc + t * kPitch, vc + (t + 4) * kPitch,
-                                                                     vc + (t + 8) * kPitch, vc + (t + 12) * kPitch};
-          // the codes of both tokens of an operand register, channels 16 m + 8 jj + g
+          // The codes of both tokens of an operand register, channels 16 m + 8 jj + g: 16-bit units 8 jj + g of their rows,
+          // transposed. The lane's address is that of row lane & 7 of matrix (half, jj).
+          uint32_t word[4], more[4] = {};
+          const uint32_t in8 = ((lane & 7) >> 1) + 4 * (lane & 1), from = vc + (8 * (lane >> 4) + in8) * kPitch + 16 * (lane >> 3 & 1);
+          ldsm_x4_t(from, word);
+          if constexpr (BITS == 4) ldsm_x4_t(from + 32, more);
+          if constexpr (BITS == 3) ldsm_x2_t(vc + (8 * (lane >> 3 & 1) + in8) * kPitch + 32, more[0], more[2]);
           auto words = [&](int half, int jj) {
-            const uint32_t ra = rows[2 * half], rb = rows[2 * half + 1], wo = 16 * jj + 4 * (g >> 1), wt = 32 + 4 * (g >> 1);
-            const uint32_t x = prmt(lds32v(ra + wo), lds32v(rb + wo), sel);
-            uint32_t y = 0;
-            if constexpr (BITS == 4) y = prmt(lds32v(ra + 32 + wo), lds32v(rb + 32 + wo), sel);
-            if constexpr (BITS == 3) y = prmt(lds32v(ra + wt), lds32v(rb + wt), sel) >> jj;
-            return FieldOf<BITS>(x, y);
+            return FieldOf<BITS>(word[2 * half + jj], BITS == 3 ? more[2 * half] >> jj : more[2 * half + jj]);
           };
           if constexpr (NARROW) {
             const uint32_t bt[4] = {be[0], 0u, be[1], 0u};
