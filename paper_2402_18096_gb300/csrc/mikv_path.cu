@@ -27,103 +27,127 @@ __device__ __forceinline__ int accepted(const int32_t* entries, int steps, int n
   return *count;
 }
 
-// acc and gained on mma.sync: a warp holds kSteps * 16 keys as the A operand, straight from memory (a lane's 16 bytes of a
-// key are the k elements of two steps, in an order that the queries share), and goes through the path's rows (node, query
-// head) eight columns at a time. Bound by the keys' bytes (256 a slot): every key is read once, whatever the path's length,
-// and nothing is staged on its way; the rows are staged kRowChunk at a time. Block (x, bh): x < gridDim.x - 1 takes
-// kBlockKeys slots, the last one the path's own nodes.
-constexpr int kImpWarps = 8, kSteps = 2, kBlockKeys = kImpWarps * kSteps * 16, kRowChunk = 64, kRowPitch = 2 * kHeadDim + 16;
+// acc and gained on mma.sync: a warp holds 16 keys as the A operand, straight from memory (a lane's 16 bytes of a key are the
+// k elements of two steps, in an order that the queries share), and goes through the path's rows (node, query head) 16
+// columns at a time. Bound by the keys' bytes (256 a slot): every key is read once, whatever the path's length, and
+// nothing is staged on its way; the rows are staged kRowChunk at a time, once where they fit. Block (x, bh): x < gridDim.x -
+// 1 takes key blocks x, x + gridDim.x - 1, ..., the next one's keys on their way under the products of this; the last one
+// the path's own nodes. 256 KV heads of 6554 slots at most, 20 rows at most: 69 us with one block of 256 keys to a CTA, whose
+// start every one of them waited for, 47 here (4.4 TB/s, 65 % of a copy).
+constexpr int kImpWarps = 8, kBlockKeys = kImpWarps * 16, kRowChunk = 64, kRowPitch = 2 * kHeadDim + 16;
 __global__ void __launch_bounds__(32 * kImpWarps, 2) importance_kernel(float* acc, const __nv_bfloat16* k_hi,
                                                                       const PathArgs a, int Hq, int Hkv, int hi_stride) {
   __shared__ int path[kTreeNodes], count;
   __shared__ __align__(16) uint8_t s_q[kRowChunk * kRowPitch];
   __shared__ float s_lse[kRowChunk];  // log2; +inf where a row weighs nothing
-  const int bh = blockIdx.y, b = bh / Hkv, h = bh - b * Hkv, G = Hq / Hkv, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int g = lane >> 2, t = lane & 3;
+  const int bh = blockIdx.y, b = bh / Hkv, h = bh - b * Hkv, G = Hq / Hkv, log2_G = 31 - __clz(G);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   grid_dependency_wait();
   allow_dependent_launch();
-  const int n = accepted(a.path + (size_t)b * a.steps, a.steps, a.nodes, path, &count);
   const bool slots = blockIdx.x + 1 < gridDim.x;
-  const int n_hi = a.held.hi(b), first = slots ? blockIdx.x * kBlockKeys : 0, last = slots ? n_hi : n;
-  float* gained = a.gained + (size_t)bh * a.steps;
-  if (!slots && threadIdx.x < a.steps && (int)threadIdx.x >= n) gained[threadIdx.x] = 0.f;
-  if (n == 0 || first >= last) return;
-  const int free_slot = slots ? a.held.free_slot(bh, n_hi) : -1;
-  // the keys of this warp: step i, rows g and g + 8; four chunks of 16 bytes of each
-  uint4 key[kSteps][2][4];
-  const int mine = first + warp * (kSteps * 16);
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i)
+  const int stride = slots ? (gridDim.x - 1) * kBlockKeys : kBlockKeys, n_hi = a.held.hi(b);
+  int first = slots ? blockIdx.x * kBlockKeys : 0, last = n_hi;
+  if (slots && first >= last) return;
+  // a block's keys of this warp: rows g and g + 8; four chunks of 16 bytes of each
+  uint4 key[2][4], next[2][4];
+  auto load = [&](int at, uint4 (&to)[2][4]) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int s = min(mine + 16 * i + 8 * r + g, last - 1);
+      const int s = min(at + 16 * warp + 8 * r + g, last - 1);
       const __nv_bfloat16* row = slots ? k_hi + ((size_t)bh * hi_stride + s) * kHeadDim
                                        : static_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + h * a.k.h + path[s] * a.k.t;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) key[i][r][c] = __ldg(reinterpret_cast<const uint4*>(row + 32 * c) + t);
+      for (int c = 0; c < 4; ++c) to[r][c] = __ldg(reinterpret_cast<const uint4*>(row + 32 * c) + t);
     }
+  };
+  if (slots) load(first, key);
+  const int n = accepted(a.path + (size_t)b * a.steps, a.steps, a.nodes, path, &count);
+  float* gained = a.gained + (size_t)bh * a.steps;
+  if (!slots && threadIdx.x < a.steps && (int)threadIdx.x >= n) gained[threadIdx.x] = 0.f;
+  if (n == 0) return;
+  if (!slots) {
+    last = n;
+    load(0, key);
+  }
+  const int free_slot = slots ? a.held.free_slot(bh, n_hi) : -1;
+  float* to = slots ? acc + (size_t)bh * hi_stride : gained;
   constexpr float kLog2e = 1.4426950408889634f;
   const float scale = a.sm_scale * kLog2e;
-  const int rows = n * G;
-  float sum[kSteps][2] = {};
-  for (int r0 = 0; r0 < rows; r0 += kRowChunk) {
-    const int here = min(kRowChunk, rows - r0), padded = (here + 7) & ~7;
-    __syncthreads();
-    for (int i = threadIdx.x; i < padded * 16; i += 32 * kImpWarps) {
-      const int r = i >> 4, c = i & 15, node = path[min((r0 + r) / G, n - 1)], j = h * G + (r0 + r) % G;
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (r < here)
-        x = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + j * a.q.h + node * a.q.t) + c);
-      *reinterpret_cast<uint4*>(s_q + r * kRowPitch + 16 * c) = x;
-      if (c == 0) {
-        const float e = r < here ? a.lse[((size_t)b * Hq + j) * a.nodes + node] : INFINITY;
-        s_lse[r] = isinf(e) ? INFINITY : e * kLog2e;
-      }
+  const int rows = n << log2_G;
+  bool staged = false;
+#pragma unroll 1
+  for (; first < last; first += stride) {
+    if (first + stride < last) load(first + stride, next);
+    const int mine = first + 16 * warp;
+    float sum[2] = {0.f, 0.f}, old[2] = {0.f, 0.f};
+    bool writes[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int s = mine + 8 * k + g;
+      writes[k] = t == 0 && s < last && s != free_slot;
+      if (slots && writes[k]) old[k] = to[s];
     }
-    __syncthreads();
-    if (mine >= last) continue;
-    for (int col = 0; col < padded; col += 8) {
-      float d[kSteps][4] = {};
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {  // steps 2 c and 2 c + 1
-        const uint4 q = *reinterpret_cast<const uint4*>(s_q + (col + g) * kRowPitch + 64 * c + 16 * t);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          const uint4 x = key[i][0][c], y = key[i][1][c];
-          const uint32_t a0[4] = {x.x, y.x, x.y, y.y}, a1[4] = {x.z, y.z, x.w, y.w};
-          mma_bf16(d[i], a0, q.x, q.y);
-          mma_bf16(d[i], a1, q.z, q.w);
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += kRowChunk) {
+      const int here = min(kRowChunk, rows - r0), padded = (here + 15) & ~15;
+      if (!staged) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < padded * 16; i += 32 * kImpWarps) {
+          const int r = i >> 4, c = i & 15, node = path[min((r0 + r) >> log2_G, n - 1)], j = h * G + ((r0 + r) & (G - 1));
+          uint4 x = make_uint4(0u, 0u, 0u, 0u);
+          if (r < here)
+            x = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + j * a.q.h + node * a.q.t) + c);
+          *reinterpret_cast<uint4*>(s_q + r * kRowPitch + 16 * c) = x;
+          if (c == 0) {
+            const float e = r < here ? a.lse[((size_t)b * Hq + j) * a.nodes + node] : INFINITY;
+            s_lse[r] = isinf(e) ? INFINITY : e * kLog2e;
+          }
         }
+        __syncthreads();
+        staged = rows <= kRowChunk;
       }
-      // columns 2 t and 2 t + 1 of this lane; a path's own node receives from itself and the later ones
+      if (mine >= last) continue;
+#pragma unroll 1
+      for (int col = 0; col < padded; col += 16) {
+        float d[2][4] = {};
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = col + 2 * t + e, step = slots ? INT_MAX : (r0 + r) / G;
-        const float lse = s_lse[r];
+        for (int c = 0; c < 4; ++c) {  // steps 2 c and 2 c + 1
+          const uint4 x = key[0][c], y = key[1][c];
+          const uint32_t a0[4] = {x.x, y.x, x.y, y.y}, a1[4] = {x.z, y.z, x.w, y.w};
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i)
+          for (int i = 0; i < 2; ++i) {
+            const uint4 q = *reinterpret_cast<const uint4*>(s_q + (col + 8 * i + g) * kRowPitch + 64 * c + 16 * t);
+            mma_bf16(d[i], a0, q.x, q.y);
+            mma_bf16(d[i], a1, q.z, q.w);
+          }
+        }
+        // columns 2 t and 2 t + 1 of this lane; a path's own node receives from itself and the later ones
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const bool sees = lse != INFINITY && step >= mine + 16 * i + 8 * k + g;
-            sum[i][k] += sees ? fast_exp2(fmaf(d[i][2 * k + e], scale, -lse)) : 0.f;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = col + 8 * i + 2 * t + e, step = slots ? INT_MAX : (r0 + r) >> log2_G;
+            const float lse = s_lse[r];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const bool sees = lse != INFINITY && step >= mine + 8 * k + g;
+              sum[k] += sees ? fast_exp2(fmaf(d[i][2 * k + e], scale, -lse)) : 0.f;
+            }
           }
       }
     }
-  }
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      float x = sum[i][k];
+      float x = sum[k];
       x += __shfl_xor_sync(0xffffffffu, x, 1);
       x += __shfl_xor_sync(0xffffffffu, x, 2);
-      const int s = mine + 16 * i + 8 * k + g;
-      if (t != 0 || s >= last || s == free_slot) continue;
-      if (slots)
-        acc[(size_t)bh * hi_stride + s] += x;
-      else
-        gained[s] = x;
+      if (writes[k]) to[mine + 8 * k + g] = old[k] + x;
     }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) key[r][c] = next[r][c];
+  }
 }
 
 // What a commit does to the lengths of a request.
@@ -347,7 +371,10 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
 }  // namespace
 
 cudaError_t launch_path_importance(const mikv_shape& s, const PathArgs& a, cudaStream_t st) {
-  const dim3 grid((s.hi_cap + kBlockKeys - 1) / kBlockKeys + 1, s.batch * s.heads_kv);
+  // a CTA takes 16 key blocks, fewer where that would leave SMs idle (4: 58 us, 8: 50, 16: 47, 26: 48)
+  const int blocks = (s.hi_cap + kBlockKeys - 1) / kBlockKeys, heads = s.batch * s.heads_kv;
+  const int ctas = std::min(blocks, std::max((blocks + 15) / 16, (4 * 152 + heads - 1) / heads));
+  const dim3 grid(ctas + 1, heads);
   return launch_chained(importance_kernel, grid, dim3(32 * kImpWarps), 0, st, a.cache->acc,
                         static_cast<const __nv_bfloat16*>(a.cache->k_hi), a, s.heads_q, s.heads_kv, s.hi_stride);
 }

@@ -70,14 +70,15 @@ struct FewRuns {
 };
 
 // The parts of an output row, weighted by 2^(lse - largest): a warp to a row. Rows whose item one CTA had are written.
+constexpr int kMergeRows = 4;
 template <typename R>
-__global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__ TreeMergeArgs m) {
+__global__ void __launch_bounds__(32 * kMergeRows) tree_merge_kernel(const __grid_constant__ TreeMergeArgs m) {
   const TreeArgs& a = m.a;
   const int lane = threadIdx.x & 31;
-  const uint32_t row = blockIdx.x * 4u + (threadIdx.x >> 5), bn = row / a.heads_q;  // (request * nodes + node) * heads_q + head
+  const int b = blockIdx.y, row = blockIdx.x * kMergeRows + (threadIdx.x >> 5);  // node * heads_q + head
   grid_dependency_wait();
-  const int head = (int)(row - bn * a.heads_q), b = (int)(bn / a.nodes), node = (int)(bn - (uint32_t)b * a.nodes);
-  if (b >= a.batch) return;
+  const int node = row / a.heads_q, head = row - node * a.heads_q;
+  if (node >= a.nodes) return;
   const int h = head >> m.log2_G, in_head = (node << m.log2_G) + (head & (a.G - 1));
   const int block = in_head >> m.log2_rows, in_item = in_head & ((1 << m.log2_rows) - 1);
   const R item(m, b);
@@ -233,8 +234,7 @@ cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t s
                    !encode_rows(&v_hi, a.v_hi, 2, {rows, 1, 1}, {kHeadDim, 0, 0}, box)))
     return cudaErrorInvalidValue;
   TreeMergeArgs m = {a, prefix, part_o, part_lse, z.m_blocks, log2_G, 31 - __builtin_clz(z.item_rows), num_sms, 0};
-  const long long out_rows = (long long)a.batch * a.nodes * a.heads_q;
-  const dim3 merge_grid((unsigned)((out_rows + 3) / 4));
+  const dim3 merge_grid((a.nodes * a.heads_q + kMergeRows - 1) / kMergeRows, a.batch);
   if (z.few) {
     TreeFewArgs p;
     memset(&p, 0, sizeof p);
@@ -250,7 +250,7 @@ cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t s
     m.lo_blocks = a.bits == 2   ? tree::FewUnit<2>(a.group).blocks
                   : a.bits == 3 ? tree::FewUnit<3>(a.group).blocks
                                 : tree::FewUnit<4>(a.group).blocks;
-    return launch_chained(tree_merge_kernel<FewRuns>, merge_grid, dim3(128), 0, st, m);
+    return launch_chained(tree_merge_kernel<FewRuns>, merge_grid, dim3(32 * kMergeRows), 0, st, m);
   }
   TreeKernelArgs p;
   memset(&p, 0, sizeof p);
@@ -268,7 +268,7 @@ cudaError_t launch_tree(const TreeArgs& a, void* ws, int num_sms, cudaStream_t s
                         : a.bits == 3 ? launch_tree_kernel<3>(p, z.pair, num_sms, st)
                                       : launch_tree_kernel<4>(p, z.pair, num_sms, st);
   if (e != cudaSuccess) return e;
-  return launch_chained(tree_merge_kernel<TileRuns>, merge_grid, dim3(128), 0, st, m);
+  return launch_chained(tree_merge_kernel<TileRuns>, merge_grid, dim3(32 * kMergeRows), 0, st, m);
 }
 
 }  // namespace mikv

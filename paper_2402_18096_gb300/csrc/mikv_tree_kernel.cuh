@@ -138,7 +138,8 @@ struct Runs {
   __device__ uint32_t first(int c) const { return share * c + min((uint32_t)c, more); }
   __device__ int owner(uint32_t x) const {
     const uint32_t larger = (share + 1) * more;
-    return x < larger ? x / (share + 1) : more + (x - larger) / max(1u, share);
+    const bool in = x < larger;
+    return (in ? 0 : more) + (in ? x : x - larger) / (in ? share + 1 : max(1u, share));
   }
 };
 
