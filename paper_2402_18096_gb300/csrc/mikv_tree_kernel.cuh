@@ -61,9 +61,11 @@ constexpr int kItemRing = 4, kItemReaders = 18, kBadRing = 8;
 constexpr int kTmemCols = 512;  // S0, S1, O0, O1
 constexpr int kExPitch = 33;    // floats of a row's 32 channels in the exchange (padded against conflicts)
 
-// Costs of tiles, for the runs.
-constexpr int kCostNodes = 2, kCostHi = 2, kCostLo = 1;
-constexpr int kLeastRun = 2;       // cost of a run at least
+// Costs of tiles, for the runs: the nodes (with the start and the end of an item), slots, retained rows, those of few
+// (kFineRows). With 2, 2, 1, 1 the same calls took 690 us in place of 642 (32 requests of up to 32768 tokens, 64 rows), 203 of
+// 173 (4 of 16384, 508 rows) and 104 of 85 (8 of 118 .. 4096 retained rows, 33 rows).
+constexpr int kCostNodes = 3, kCostHi = 1, kCostLo = 1, kCostFine = 2;
+constexpr int kLeastRun = 1;       // cost of a run at least
 constexpr int kFineRows = 1024;    // requests with up to this many retained rows have their keys in two tiles
 constexpr int kAhead = 6;          // tiles of codes asked for ahead (L2)
 
@@ -111,18 +113,21 @@ struct Layout {
 
 // The key tiles of a request's items, and the costs before each.
 struct Tiles {
-  int hi, lo;  // tiles of slots, of retained rows
-  __device__ Tiles(const HeldArgs& held, int b) : hi((held.hi(b) + kTile - 1) / kTile), lo((held.lo(b) + kTile - 1) / kTile) {}
+  int hi, lo, each;  // tiles of slots, of retained rows; cost of one of the latter
+  __device__ Tiles(const HeldArgs& held, int b) : hi((held.hi(b) + kTile - 1) / kTile) {
+    const int rows = held.lo(b);
+    lo = (rows + kTile - 1) / kTile, each = rows <= kFineRows ? kCostFine : kCostLo;
+  }
   __device__ int count() const { return 1 + hi + lo; }
-  __device__ int cost() const { return kCostNodes + kCostHi * hi + kCostLo * lo; }
+  __device__ int cost() const { return kCostNodes + kCostHi * hi + each * lo; }
   __device__ int before(int t) const {
-    return t == 0 ? 0 : kCostNodes + (t <= hi ? kCostHi * (t - 1) : kCostHi * hi + kCostLo * (t - 1 - hi));
+    return t == 0 ? 0 : kCostNodes + (t <= hi ? kCostHi * (t - 1) : kCostHi * hi + each * (t - 1 - hi));
   }
   // the first tile that begins at x or later
   __device__ int first(int x) const {
     if (x <= 0) return 0;
     x -= kCostNodes;
-    const int t = x <= 0 ? 0 : x <= kCostHi * hi ? (x + kCostHi - 1) / kCostHi : hi + (x - kCostHi * hi + kCostLo - 1) / kCostLo;
+    const int t = x <= 0 ? 0 : x <= kCostHi * hi ? (x + kCostHi - 1) / kCostHi : hi + (x - kCostHi * hi + each - 1) / each;
     return min(t + 1, count());
   }
 };
