@@ -65,7 +65,7 @@ constexpr int kExPitch = 33;    // floats of a row's 32 channels in the exchange
 // (kFineRows). With 2, 2, 1, 1 the same calls took 690 us in place of 642 (32 requests of up to 32768 tokens, 64 rows), 203 of
 // 173 (4 of 16384, 508 rows) and 104 of 85 (8 of 118 .. 4096 retained rows, 33 rows).
 constexpr int kCostNodes = 3, kCostHi = 1, kCostLo = 1, kCostFine = 2;
-constexpr int kLeastRun = 1;       // cost of a run at least
+constexpr int kLeastRun = 3;       // cost of a run at least (6: 29.7 us where 1, 3 and 4 take 23.4, 32 items of 2047 tokens)
 constexpr int kFineRows = 1024;    // requests with up to this many retained rows have their keys in two tiles
 constexpr int kAhead = 6;          // tiles of codes asked for ahead (L2)
 
