@@ -227,7 +227,18 @@ mikv_status mikv_copy_requests(const mikv_shape* shape, const mikv_cache* cache,
     return MIKV_ERR_ARG;
   if (y.hi_cap < x.hi_cap || (kch_of(x) && y.hi_cap != x.hi_cap) || (!evicting(x) && y.lo_cap < held.n_lo_max))
     return MIKV_ERR_CAPACITY;
-  const bool same = cache->k_hi == to_cache->k_hi;
+  // the caches are one or share nothing: of one, all arrays are the same
+  const void* from_all[] = {cache->k_hi, cache->v_hi, cache->hi_tok, cache->acc, cache->k_codes, cache->v_codes,
+                            cache->k_params, cache->v_params, cache->lo_tok, cache->k_hi_params, cache->v_hi_params};
+  const void* to_all[] = {to_cache->k_hi, to_cache->v_hi, to_cache->hi_tok, to_cache->acc, to_cache->k_codes,
+                          to_cache->v_codes, to_cache->k_params, to_cache->v_params, to_cache->lo_tok,
+                          to_cache->k_hi_params, to_cache->v_hi_params};
+  const int arrays = hi_bits_of(x) == 16 ? (evicting(x) ? 4 : 9) : 11;
+  int shared = 0, counted = 0;
+  for (int i = 0; i < arrays; ++i)
+    if (!evicting(x) || i < 4 || i > 8) ++counted, shared += from_all[i] == to_all[i];
+  if (shared != 0 && shared != counted) return MIKV_ERR_ARG;
+  const bool same = shared != 0;
   if (same && (x.hi_stride != y.hi_stride || x.lo_cap != y.lo_cap)) return MIKV_ERR_ARG;
   if ((st = pairs_ok(pairs, n, x.batch, y.batch, same)) != MIKV_OK) return st;
   if (n == 0) return MIKV_OK;

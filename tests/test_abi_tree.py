@@ -153,6 +153,12 @@ def test_copy_arguments_refused(lib):
     assert lib.mikv_copy_requests(None, None, None, None, None, 0, None, None, None) == 1
 
 
+def test_copies_between_caches_that_share_some_arrays_refused(lib):
+    for name in ("k_hi", "acc", "v_params", "lo_tok"):
+        assert copy_rc(lib, ((0, 0),), tc=cache(**{name: 2 * P})) == 1, name
+    assert copy_rc(lib, (), tc=cache(k_hi=2 * P)) == 1 and copy_rc(lib, (), tc=cache(**{n: 2 * P for n, _ in pkg._Cache._fields_})) == 0
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     s = pkg.Shape(1, 4, 2, 2, 32, 17, 32)
     arrays = [torch.zeros(1, 2, 32, 128, dtype=torch.bfloat16)] * 2 + \
