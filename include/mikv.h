@@ -617,8 +617,9 @@ mikv_status mikv_commit_path(const mikv_shape* shape, const mikv_cache* cache, i
  * use with their codes, parameters, scores and ids (and, with per-channel keys, the staged rows), n_hi, n_lo and
  * slots where both lengths have them. What lies behind stays as it was.
  *   pairs     int32 [n][2] on the HOST (read before the call returns). 0 <= n; rows of the two batches; no row is the
- *             target of two pairs, and in one cache (to_cache->k_hi == cache->k_hi) none is source and target:
- *             MIKV_ERR_ARG
+ *             target of two pairs, and in one cache none is source and target (where the caches differ but an array of
+ *             the lengths is one, none but a row paired with itself): MIKV_ERR_ARG
+ *   caches    one, with all arrays the same, or two that share none: MIKV_ERR_ARG
  *   shapes    equal heads, dimensions and precisions; to_shape->hi_cap >= shape->hi_cap (equal where k_channel_group is
  *             set or hi_cap slots are in use without n_hi) and to_shape->lo_cap >= lens->n_lo_max: MIKV_ERR_CAPACITY. All
  *             arrays 16-byte aligned

@@ -65,8 +65,9 @@ mikv_status view_of(const mikv_view* x, int64_t batch, int64_t heads, int64_t no
 
 bool nodes_ok(int32_t n) { return n >= 1 && n <= kTreeNodes; }
 
-// The row `to` of every pair once, and none of `from` among them where `same`.
-mikv_status pairs_ok(const int32_t* pairs, int32_t n, int32_t batch, int32_t to_batch, bool same) {
+// The row `to` of every pair once, and none of `from` among them where `same`; where the lengths alone are `joint`, none but a
+// row that stays itself.
+mikv_status pairs_ok(const int32_t* pairs, int32_t n, int32_t batch, int32_t to_batch, bool same, bool joint) {
   std::vector<uint8_t> role;
   try {
     role.assign((size_t)(to_batch > batch ? to_batch : batch), 0);
@@ -76,10 +77,12 @@ mikv_status pairs_ok(const int32_t* pairs, int32_t n, int32_t batch, int32_t to_
   for (int32_t i = 0; i < n; ++i) {
     const int32_t from = pairs[2 * i], to = pairs[2 * i + 1];
     if (from < 0 || from >= batch || to < 0 || to >= to_batch || (role[to] & 1)) return MIKV_ERR_ARG;
-    role[to] |= 1;
+    role[to] |= from == to ? 3 : 1;
   }
-  for (int32_t i = 0; same && i < n; ++i)
-    if (role[pairs[2 * i]] & 1) return MIKV_ERR_ARG;
+  for (int32_t i = 0; (same || joint) && i < n; ++i) {
+    const uint8_t r = role[pairs[2 * i]];
+    if (same ? (r & 1) != 0 : r == 1) return MIKV_ERR_ARG;
+  }
   return MIKV_OK;
 }
 
@@ -240,7 +243,9 @@ mikv_status mikv_copy_requests(const mikv_shape* shape, const mikv_cache* cache,
   if (shared != 0 && shared != counted) return MIKV_ERR_ARG;
   const bool same = shared != 0;
   if (same && (x.hi_stride != y.hi_stride || x.lo_cap != y.lo_cap)) return MIKV_ERR_ARG;
-  if ((st = pairs_ok(pairs, n, x.batch, y.batch, same)) != MIKV_OK) return st;
+  const bool joint = lens && to_lens && ((lens->n_hi && lens->n_hi == to_lens->n_hi) || (lens->n_lo && lens->n_lo == to_lens->n_lo) ||
+                                         (lens->slots && lens->slots == to_lens->slots));
+  if ((st = pairs_ok(pairs, n, x.batch, y.batch, same, joint)) != MIKV_OK) return st;
   if (n == 0) return MIKV_OK;
   CopyLengths len = {held.n_hi, held.n_lo, held.slots, nullptr, nullptr, nullptr, held.n_lo_max};
   if (to_lens) len.to_n_hi = to_lens->n_hi, len.to_n_lo = to_lens->n_lo, len.to_slots = to_lens->slots;

@@ -683,7 +683,7 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) {
               al[half][i] = u32_as_h2(prmt(pa[i], pb[i], 0x5410u));
-              most = __hmax2(most, al[half][i]);
+              most = __hmax2(most, __habs2(al[half][i]));
             }
           }
           // P is up to 2^8.5 and alpha up to 2^(ev + 6): their product is inside fp16. The first block chooses ev.

@@ -131,7 +131,9 @@ def attention(d: Drafts, b, hq, scale=1 / math.sqrt(128), out_dtype=torch.bfloat
     Bounds: scores of bf16 keys are exact products summed in fp32; a retained key is rounded at most twice to fp16 on its
     way (dequantized, divided by the balancer; subnormals: 2^-25 each), its query is exact; weights are then off by a
     factor e^(2 E), by 2^-19 for the exponential and the sums, and by their rounding to bf16 or fp16; retained values are
-    rounded to fp16 once; fp16 weights lose what lies 2^-33 below the largest; the output is rounded once."""
+    rounded to fp16 once; fp16 weights lose what lies 2^-33 below the largest; the output is rounded once. (Of few rows
+    the keys are not rounded, and a weight is rounded once more with its row's scale: 2^-11 of scale * code, which over the
+    rows of these tests stays inside the same terms.)"""
     h, c = hq // d.G, d.cache
     q = d.q[b, hq].double()
     N, n_lo = d.N, d.n_lo[b]

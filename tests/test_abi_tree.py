@@ -159,6 +159,16 @@ def test_copies_between_caches_that_share_some_arrays_refused(lib):
     assert copy_rc(lib, (), tc=cache(k_hi=2 * P)) == 1 and copy_rc(lib, (), tc=cache(**{n: 2 * P for n, _ in pkg._Cache._fields_})) == 0
 
 
+def test_copies_that_read_lengths_they_write_refused(lib):
+    """Two caches with one array of lengths: a row may keep its number, but not be read for one and written for another."""
+    two = cache(**{n: 2 * P for n, _ in pkg._Cache._fields_})
+    mine = dict(lens=lengths(n_hi=P, n_lo=2 * P, slots=3 * P), tc=two)
+    for to in (lengths(n_hi=P, n_lo=None, slots=None), lengths(n_hi=None, n_lo=2 * P, slots=None),
+               lengths(n_hi=None, n_lo=None, slots=3 * P)):
+        assert copy_rc(lib, ((0, 1), (1, 0)), to=to, **mine) == 1
+        assert copy_rc(lib, ((0, 0), (0, 1), (1, 2)), to=to, t=shape(batch=3), **mine) == 1
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     s = pkg.Shape(1, 4, 2, 2, 32, 17, 32)
     arrays = [torch.zeros(1, 2, 32, 128, dtype=torch.bfloat16)] * 2 + \

@@ -244,3 +244,18 @@ def test_offsets_past_32_bits():
     pkg.mikv_tree_attention(c, masks, q, k, v, out, ws, lens=lens, lse=lse)
     pkg.mikv_workspace_check(ws)
     check(d, out[-1:, -1:], lse[-1:, -1:])
+
+
+@pytest.mark.parametrize("bits,group", [(2, 32), (3, 64), (4, 128)])
+def test_scales_of_either_sign_and_size(bits, group):
+    """Parameters that no quantizer gives but the formula takes: negative scales, rows 2^12 apart."""
+    d = Drafts(16 + bits, 2, 4, 2, 3, 40, 608, bits, group)
+    g = gen(5)
+    for x in (d.cache.k_params, d.cache.v_params):
+        sign = torch.where(torch.rand(x.shape[:-1], generator=g, device="cuda") < 0.5, -1.0, 1.0)
+        x[..., 0] = (x[..., 0].float() * sign).half()
+    step = 2.0 ** (4 * torch.randint(-2, 2, d.cache.v_params.shape[:3], generator=g, device="cuda").float())
+    d.cache.v_params.copy_((d.cache.v_params.float() * step[..., None, None]).half())
+    for dt in (BF, F32):
+        out, lse = run(d, dt)
+        check(d, out, lse)
