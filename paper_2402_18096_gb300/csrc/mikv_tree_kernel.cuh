@@ -21,6 +21,11 @@
 //   warp 18         works out the coming items
 // All tiles pass one ring of shared memory in the order of their use.
 //
+// Bound by the chain of a key tile, about 2400 clocks with up to 64 rows: its codes to a tile of keys and one of values
+// (1450 each, eight warps), 16 MMAs (87 clocks each, most of them the operands' way out of shared memory) and the hand-overs
+// between the roles. 32 requests of up to 32768 tokens, 8 KV heads, 64 rows: 638 us (2.4 TB/s of codes); 4 requests of
+// 16384, 508 rows: 174 us (0.78 PFLOP/s).
+//
 // Precision. A retained key enters as alpha code / b + beta / b, rounded to fp16, so that the query enters as it is: its
 // bf16 elements are exact in fp16 once a power of two brings the row's largest to 2^14. (A query divided by the balancer
 // and rounded would be off alike for all keys, 1e-5 of lse; roundings of the keys average out.) Requests with few
@@ -39,7 +44,7 @@ struct TreeKernelArgs {
   TreeArgs a;
   int rows, m_blocks, log2_G;      // rows of a KV head; row tiles (pairs)
   int twin;                        // the rows of a tile (up to 64) stand in it twice
-  uint32_t* prefix;               // [batch + 1] costs of all items before each request (for the merge)
+  uint32_t* prefix;                // [batch + 1] costs of all items before each request (for the merge)
   float* part_o;                   // [2 * CTAs][rows of an item][128]
   float* part_lse;                 // [2 * CTAs][rows of an item], log2
 };
