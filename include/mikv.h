@@ -554,9 +554,12 @@ typedef struct {
  * 2^18 tokens over all KV heads (smaller ones are as with more rows):
  *   up to 16   codes enter exactly. q / balancer enters in two fp16 terms after a power of two for 32 channels or all
  *              (22 bits of an element; those below 2^-19 of the largest of their 32 channels lose some); probabilities are
- *              rounded to fp16 once more, times alpha. alpha and beta of the keys act in fp32
+ *              rounded to fp16 once more, times alpha, whatever the size of the values' scales (0 among them); of these
+ *              products those below 2^-22 of the largest probability times the largest scale lose some bits. alpha and
+ *              beta of the keys, and beta of the values, act unrounded
  *   more       keys, alpha * code / b + beta / b, and values, alpha * code + beta, are rounded to fp16 (of requests with
- *              at most 1024 retained rows the keys' remainder enters too); their magnitude has to stay below 65504.
+ *              at most 1024 retained rows the keys' remainder enters too); their magnitude has to stay below 65504, and
+ *              what is left of them below 2^-14 are multiples of 2^-24.
  *              Queries are taken exactly, in fp16 after a power of two per row: elements below 2^-24 of a row's largest
  *              are lost
  * A node whose value holds an infinity or NaN gives NaN in all channels to the nodes that see it, and touches no other; in

@@ -20,7 +20,7 @@
 //       whose other side are the groups, added to the group's channels at the end. O of channels 16 m .. is kept in units of
 //       2^(s_m - 24) meanwhile, and of 2^ev for alphas far from 1.
 // With alpha and beta applied to every key and value in fp16 (two more instructions a pair) the same kernel took 182 us where
-// this one took 149, 16 requests of 205 .. 8192 tokens, 40 heads, 3 bits. Now 127 (3.7 TB/s, 54 % of a copy): bound by the
+// this one took 149, 16 requests of 205 .. 8192 tokens, 40 heads, 3 bits. Now 128 (3.6 TB/s, 53 % of a copy): bound by the
 // instructions of a block (390, with three warps a scheduler that wait for their own results).
 // Tokens 2 t and 2 t + 1 of an operand are rows t and t + 4 of their eight, so that eight lanes read four rows of codes from
 // different banks.
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
     float qs[PAIRS][2];                  // sums of the groups' q^, in units of 2^24 products
     bool spread = false;                 // 32 channels of q^ have a scale of their own (s_rel, beside the row's)
     float alpha_most = -1.f;             // 2^(ev + 6): O is in units of 2^ev (retained rows)
-    __half2 unit = u32_as_h2(0u);        // 2^-ev
+    __half2 unit = u32_as_h2(0u);        // 2^-ev, 2^6 at most
     float o[kO][4], ref[2], sum[2] = {0.f, 0.f}, scale_lo[2] = {0.f, 0.f};
     bool poisoned[2] = {false, false};
 #pragma unroll
@@ -687,7 +687,9 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
               most = __hmax2(most, __habs2(al[half][i]));
             }
           }
-          // P is up to 2^8.5 and alpha up to 2^(ev + 6): their product is inside fp16. The first block chooses ev.
+          // P alpha 2^-ev enters, P up to 2^8.5 and alpha up to 2^(ev + 6); the first block chooses ev. The power has to lie
+          // on the factor that stays inside fp16: on P it brings P alpha down where ev > 0, and up to P 2^6 = 2^14.5; what is
+          // left of it goes to alpha, which stays below 1. Powers upwards are exact, and the product is rounded once.
           const float top_alpha = fmaxf(__low2float(most), __high2float(most));
           if (__any_sync(0xffffffffu, top_alpha > alpha_most)) {
             float x = top_alpha;
@@ -699,7 +701,14 @@ __global__ void __launch_bounds__(32 * FewShape<NARROW>::kWarps, 1) tree_few_ker
             for (int i = 0; i < kO; ++i)
 #pragma unroll
               for (int e = 0; e < 4; ++e) o[i][e] *= f;
-            alpha_most = power2(ev + 6), unit = __float2half2_rn(power2(-ev));
+            alpha_most = power2(ev + 6), unit = __float2half2_rn(power2(-max(ev, -6)));
+          }
+          if (alpha_most < 1.f) {  // 2^(-6 - ev), for all of the warp
+            const __half2 up = __float2half2_rn(__uint_as_float(0x7f000000u - __float_as_uint(alpha_most)));
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int i = 0; i < PAIRS; ++i) al[half][i] = __hmul2(al[half][i], up);
           }
           // The codes of both tokens of an operand register, channels 16 m + 8 jj + g: 16-bit units 8 jj + g of their rows,
           // transposed. The lane's address is that of row lane & 7 of matrix (half, jj).
