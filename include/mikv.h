@@ -555,8 +555,9 @@ typedef struct {
  *   up to 16   codes enter exactly. q / balancer enters in two fp16 terms after a power of two for 32 channels or all
  *              (22 bits of an element; those below 2^-19 of the largest of their 32 channels lose some); probabilities are
  *              rounded to fp16 once more, times alpha, whatever the size of the values' scales (0 among them); of these
- *              products those below 2^-22 of the largest probability times the largest scale lose some bits. alpha and
- *              beta of the keys, and beta of the values, act unrounded
+ *              products those below 2^-22 of the largest probability times the largest scale lose some bits, and so do
+ *              probabilities below 2^-22 S of the largest where the largest scale S is above 1. alpha and beta of the
+ *              keys, and beta of the values, act unrounded
  *   more       keys, alpha * code / b + beta / b, and values, alpha * code + beta, are rounded to fp16 (of requests with
  *              at most 1024 retained rows the keys' remainder enters too); their magnitude has to stay below 65504, and
  *              what is left of them below 2^-14 are multiples of 2^-24.
@@ -624,8 +625,8 @@ mikv_status mikv_commit_path(const mikv_shape* shape, const mikv_cache* cache, i
  *             the lengths is one, none but a row paired with itself): MIKV_ERR_ARG
  *   caches    one, with all arrays the same, or two that share none: MIKV_ERR_ARG
  *   shapes    equal heads, dimensions and precisions; to_shape->hi_cap >= shape->hi_cap (equal where k_channel_group is
- *             set or hi_cap slots are in use without n_hi) and to_shape->lo_cap >= lens->n_lo_max: MIKV_ERR_CAPACITY. All
- *             arrays 16-byte aligned
+ *             set, and where hi_cap slots are in use without n_hi unless to_lens has n_hi to take that number) and
+ *             to_shape->lo_cap >= lens->n_lo_max: MIKV_ERR_CAPACITY. All arrays 16-byte aligned
  *   lens, to_lens  as above; to_lens may be NULL. The balancer is the layer's, not copied
  */
 mikv_status mikv_copy_requests(const mikv_shape* shape, const mikv_cache* cache, const mikv_shape* to_shape,

@@ -228,7 +228,9 @@ mikv_status mikv_copy_requests(const mikv_shape* shape, const mikv_cache* cache,
   if ((st = held_of(lens, shape, held)) != MIKV_OK) return st;
   if (to_lens && (!aligned(to_lens->n_hi, 4) || !aligned(to_lens->n_lo, 4) || !aligned(to_lens->slots, 4)))
     return MIKV_ERR_ARG;
-  if (y.hi_cap < x.hi_cap || (kch_of(x) && y.hi_cap != x.hi_cap) || (!evicting(x) && y.lo_cap < held.n_lo_max))
+  const bool counted_hi = held.n_hi || (to_lens && to_lens->n_hi);  // else every slot of the target counts as in use
+  if (y.hi_cap < x.hi_cap || ((kch_of(x) || !counted_hi) && y.hi_cap != x.hi_cap) ||
+      (!evicting(x) && y.lo_cap < held.n_lo_max))
     return MIKV_ERR_CAPACITY;
   // the caches are one or share nothing: of one, all arrays are the same
   const void* from_all[] = {cache->k_hi, cache->v_hi, cache->hi_tok, cache->acc, cache->k_codes, cache->v_codes,

@@ -169,6 +169,20 @@ def test_copies_that_read_lengths_they_write_refused(lib):
         assert copy_rc(lib, ((0, 0), (0, 1), (1, 2)), to=to, t=shape(batch=3), **mine) == 1
 
 
+def test_copies_into_more_slots_than_are_counted_refused(lib):
+    """All hi_cap slots in use, into a cache of more: only where the target's n_hi takes their number."""
+    two = cache(**{n: 2 * P for n, _ in pkg._Cache._fields_})
+    larger = dict(t=shape(hi_cap=18), tc=two)
+    assert copy_rc(lib, (), lens=lengths(n_hi=None), **larger) == 3
+    assert copy_rc(lib, (), lens=lengths(n_hi=None), to=lengths(n_hi=None), **larger) == 3
+    none = lambda t, to: lib.mikv_copy_requests(ref(shape()), ref(cache()), ref(t), ref(two), (ctypes.c_int32 * 2)(), 0, None,  # noqa: E731
+                                                ref(to), None)
+    assert none(shape(hi_cap=18), None) == 3 and none(shape(), None) == 0
+    assert copy_rc(lib, (), lens=lengths(n_hi=None), tc=two) == 0  # as many slots
+    assert copy_rc(lib, (), lens=lengths(n_hi=None), to=lengths(n_hi=2 * P), **larger) == 0
+    assert copy_rc(lib, (), **larger) == 0
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     s = pkg.Shape(1, 4, 2, 2, 32, 17, 32)
     arrays = [torch.zeros(1, 2, 32, 128, dtype=torch.bfloat16)] * 2 + \
