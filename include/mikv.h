@@ -618,8 +618,9 @@ mikv_status mikv_commit_path(const mikv_shape* shape, const mikv_cache* cache, i
 /*
  * Copies of whole requests (forks for several samples, compaction of a batch, growth into a larger cache): for every pair
  * (from, to), row `to` of `to_cache` becomes what row `from` of `cache` holds: the slots in use and the retained rows in
- * use with their codes, parameters, scores and ids (and, with per-channel keys, the staged rows), n_hi, n_lo and
- * slots where both lengths have them. What lies behind stays as it was.
+ * use with their codes, parameters, scores and ids (and, with per-channel keys, the staged rows). The target's n_hi and n_lo,
+ * where it has them, take the numbers of slots and rows in use (hi_cap and n_lo_max of a source without the array), its slots
+ * the source's. What lies behind stays as it was.
  *   pairs     int32 [n][2] on the HOST (read before the call returns). 0 <= n; rows of the two batches; no row is the
  *             target of two pairs, and in one cache none is source and target (where the caches differ but an array of
  *             the lengths is one, none but a row paired with itself): MIKV_ERR_ARG
@@ -627,7 +628,8 @@ mikv_status mikv_commit_path(const mikv_shape* shape, const mikv_cache* cache, i
  *   shapes    equal heads, dimensions and precisions; to_shape->hi_cap >= shape->hi_cap (equal where k_channel_group is
  *             set, and where hi_cap slots are in use without n_hi unless to_lens has n_hi to take that number) and
  *             to_shape->lo_cap >= lens->n_lo_max: MIKV_ERR_CAPACITY. All arrays 16-byte aligned
- *   lens, to_lens  as above; to_lens may be NULL. The balancer is the layer's, not copied
+ *   lens, to_lens  as above; to_lens may be NULL. to_lens with slots and lens without: MIKV_ERR_ARG, for a source without
+ *             free slots has none to give. The balancer is the layer's, not copied
  */
 mikv_status mikv_copy_requests(const mikv_shape* shape, const mikv_cache* cache, const mikv_shape* to_shape,
                                const mikv_cache* to_cache, const int32_t* pairs, int32_t n, const mikv_lengths* lens,

@@ -226,7 +226,8 @@ mikv_status mikv_copy_requests(const mikv_shape* shape, const mikv_cache* cache,
   if (x.heads_kv > 65535) return MIKV_ERR_UNSUPPORTED;
   HeldArgs held;
   if ((st = held_of(lens, shape, held)) != MIKV_OK) return st;
-  if (to_lens && (!aligned(to_lens->n_hi, 4) || !aligned(to_lens->n_lo, 4) || !aligned(to_lens->slots, 4)))
+  if (to_lens && (!aligned(to_lens->n_hi, 4) || !aligned(to_lens->n_lo, 4) || !aligned(to_lens->slots, 4) ||
+                  (to_lens->slots && !held.slots)))
     return MIKV_ERR_ARG;
   const bool counted_hi = held.n_hi || (to_lens && to_lens->n_hi);  // else every slot of the target counts as in use
   if (y.hi_cap < x.hi_cap || ((kch_of(x) || !counted_hi) && y.hi_cap != x.hi_cap) ||

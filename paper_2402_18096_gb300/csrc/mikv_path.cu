@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
   const int n_hi = a.len.n_hi ? max(0, min(a.len.n_hi[pair.x], a.hi_cap)) : a.hi_cap;
   const int n_lo = a.len.n_lo ? max(0, min(a.len.n_lo[pair.x], a.len.n_lo_max)) : a.len.n_lo_max;
   if (blockIdx.y == 0 && threadIdx.x == 0) {
-    if (a.len.to_slots) a.len.to_slots[pair.y * a.heads + h] = a.len.slots ? a.len.slots[pair.x * a.heads + h] : -1;
+    if (a.len.to_slots) a.len.to_slots[pair.y * a.heads + h] = a.len.slots[pair.x * a.heads + h];
     if (h == 0 && a.len.to_n_hi) a.len.to_n_hi[pair.y] = n_hi;
     if (h == 0 && a.len.to_n_lo) a.len.to_n_lo[pair.y] = n_lo;
   }

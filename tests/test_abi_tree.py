@@ -183,6 +183,15 @@ def test_copies_into_more_slots_than_are_counted_refused(lib):
     assert copy_rc(lib, (), **larger) == 0
 
 
+def test_copies_of_free_slots_that_the_source_does_not_have_refused(lib):
+    two = cache(**{n: 2 * P for n, _ in pkg._Cache._fields_})
+    assert copy_rc(lib, (), lens=lengths(slots=None), to=lengths(), tc=two) == 1
+    assert lib.mikv_copy_requests(ref(shape()), ref(cache()), ref(shape()), ref(two), (ctypes.c_int32 * 2)(), 0, None,
+                                  ref(lengths()), None) == 1
+    assert copy_rc(lib, (), lens=lengths(slots=None), to=lengths(slots=None), tc=two) == 0
+    assert copy_rc(lib, (), lens=lengths(), to=lengths(slots=None), tc=two) == 0
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     s = pkg.Shape(1, 4, 2, 2, 32, 17, 32)
     arrays = [torch.zeros(1, 2, 32, 128, dtype=torch.bfloat16)] * 2 + \

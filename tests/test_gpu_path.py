@@ -262,6 +262,25 @@ def test_many_copies_and_none():
         same(got[:, :, :rows], src[:, :, :rows].expand(700, *src.shape[1:2], rows, *src.shape[3:]), x)
 
 
+def test_copies_of_uncounted_requests():
+    """A source whose lengths have no arrays: the target's take its slots and rows in use, its free slots are left alone."""
+    s, t = pkg.Shape(2, 2, 2, 2, 32, 20, 32), pkg.Shape(3, 2, 2, 2, 32, 33, 48)
+    a, b = random_cache(s, 5), random_cache(t, 6)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    to = pkg.Lengths(dev([7, 8, 9]), dev([1, 2, 3]), torch.full((3, 2), 5, dtype=torch.int32, device="cuda"))
+    with pytest.raises(pkg.MikvError) as e:
+        pkg.mikv_copy_requests(a, b, [(0, 2)], lens=pkg.Lengths(n_lo=30), to_lens=to)
+    assert e.value.status == "MIKV_ERR_ARG" and to.n_hi.tolist() == [7, 8, 9] and to.slots.tolist() == [[5, 5]] * 3
+    to.slots = None
+    old = {x: getattr(b, x).clone() for x in ARRAYS}
+    pkg.mikv_copy_requests(a, b, [(0, 2)], lens=pkg.Lengths(n_lo=30), to_lens=to)
+    assert to.n_hi.tolist() == [7, 8, 20] and to.n_lo.tolist() == [1, 2, 30]
+    for x in ARRAYS:
+        rows = 20 if x in ("k_hi", "v_hi", "hi_tok", "acc") else 30
+        old[x][2, :, :rows] = getattr(a, x)[0, :, :rows]
+        same(getattr(b, x), old[x], x)
+
+
 def test_drafts_run_together():
     """A prompt's cache, then trees, accepted paths, a fork, trees again: every tree is attended over what the caches hold
     then, every token is somewhere, in bf16 as it came or quantized from that, and the lengths add up."""
