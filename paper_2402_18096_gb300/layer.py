@@ -211,6 +211,7 @@ class DraftedLayer:
         self.ws_tree = workspace(mikv_tree_workspace_bytes(s, nodes), dev)
         self.ws_commit = workspace(mikv_commit_workspace_bytes(s, steps), dev)
         self.drafted = None  # (q, k, v) of the tree attended last
+        self.captured = False  # a commit was captured: replays move the lengths, and n_lo_max does not follow
 
     @classmethod
     def of(cls, layer: MixedPrecisionLayer, table: RotaryTable, nodes: int, steps: int) -> "DraftedLayer":
@@ -230,15 +231,23 @@ class DraftedLayer:
 
     def commit(self, path):
         """The accepted nodes path int32 [B, steps] (root first, -1 behind the last) of the tree attended last: they hand out
-        importance, enter the cache, and what it holds above its budget is demoted. A call that is refused has changed
-        nothing."""
+        importance, enter the cache, and what it holds above its budget is demoted.
+        Refused (MIKV_ERR_CAPACITY) where a request might not have the room, with every step accepted: the last steps - 1
+        rows of a cache may stay empty. A call that raises has changed nothing. The replay of a captured one cannot raise: a
+        request without the room then keeps its tokens and lengths, but its important tokens have taken the path's
+        importance, and check() says so. Under capture the bound n_lo_max decides alone; once a commit was captured, those
+        outside a capture read the lengths (the host waits for them)."""
         if self.drafted is None:
             raise ValueError("DraftedLayer.commit: no tree was attended since the last commit")
-        s = self.cache.shape
-        if s.bits and self.n_lo_max + self.steps > s.lo_cap:  # (the bound is of commits with every step accepted)
-            self.n_lo_max = int(self.lens.n_lo.max())
-            if self.n_lo_max + self.steps > s.lo_cap:
+        s, capturing = self.cache.shape, torch.cuda.is_current_stream_capturing()
+        if s.bits:
+            def full():
+                return self.n_lo_max + self.steps > s.lo_cap
+            if not capturing and (self.captured or full()):
+                self.n_lo_max = int(self.lens.n_lo.max())
+            if full():
                 raise MikvError("DraftedLayer.commit", 3)  # MIKV_ERR_CAPACITY
+        self.captured |= capturing
         q, k, v = self.drafted
         mikv_path_importance(self.cache, path, q, k, self.lse, self.gained, lens=self.lens)
         mikv_commit_path(self.cache, path, k, v, self.gained, self.tokens, self.ws_commit, lens=self.lens,

@@ -392,3 +392,52 @@ def test_a_step_in_a_graph():
                                                                          layer.tokens])
     for a, b in zip(*results):
         same(a, b, "graph")
+
+
+def full_soon(n_lo, steps=3):
+    """A layer of one request whose every accepted token demotes one, 16 retained rows, and a chain for it."""
+    d = drafts(31, B=1, N=3, hi=4, lo=16, n_lo=[n_lo])
+    layer = DraftedLayer(d.cache, pkg.RotaryTable(), 3, steps, d.dev(d.n_hi), d.dev(d.n_lo), d.free, d.dev([3 + n_lo]), n_lo)
+    out = torch.empty_like(d.q)
+    return d, layer, lambda: layer.attend(d.q, d.k, d.v, d.parents, out)
+
+
+def test_commits_after_replays_refuse_before_anything_changes():
+    """Replayed steps fill the cache; the next commit, call by call, is refused on the host."""
+    d, layer, attend = full_soon(4)
+    path = path_tensor([[0, 1, 2]], 3)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        attend()
+        layer.commit(path)
+    for _ in range(3):
+        g.replay()
+    attend()
+    layer.commit(path)  # the last that has room
+    layer.check()
+    assert layer.lens.n_lo.tolist() == [16] and layer.tokens.tolist() == [19]
+    attend()
+    old = {x: getattr(d.cache, x).clone() for x in ARRAYS}
+    with pytest.raises(pkg.MikvError) as e:
+        layer.commit(path)
+    assert e.value.status == "MIKV_ERR_CAPACITY"
+    for x in ARRAYS:
+        same(getattr(d.cache, x), old[x], x)
+    assert layer.lens.n_lo.tolist() == [16] and layer.tokens.tolist() == [19]
+    layer.check()  # no kernel refused anything
+
+
+def test_a_captured_commit_without_the_room_is_refused():
+    """As an error of the library's own, with the capture left whole."""
+    d, layer, attend = full_soon(14)
+    path = path_tensor([[0]], 3)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        attend()
+        with pytest.raises(pkg.MikvError) as e:
+            layer.commit(path)
+    assert e.value.status == "MIKV_ERR_CAPACITY" and layer.lens.n_lo.tolist() == [14]
+    g.replay()
+    layer.check()
