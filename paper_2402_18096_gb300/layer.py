@@ -196,10 +196,13 @@ class DraftedLayer:
 
     def __init__(self, cache: LayerCache, table: RotaryTable, nodes: int, steps: int, n_hi, n_lo, slots, tokens,
                  n_lo_max: int = None):
-        """nodes, steps: most drafted and most accepted tokens of a step. n_hi, n_lo, tokens int32 [B] (slots in use,
-        retained rows, tokens so far) and slots int32 [B, Hkv] (the free slots) are kept and updated in place; n_lo_max
-        bounds n_lo."""
+        """nodes, steps: the nodes of a tree and the entries of a path (smaller ones are padded: parents of -2, entries of
+        -1). n_hi, n_lo, tokens int32 [B] (slots in use, retained rows, tokens so far) and slots int32 [B, Hkv] (the free
+        slots) are kept and updated in place; n_lo_max bounds n_lo. Caches that mikv_tree_attention does not take are
+        refused (MIKV_ERR_UNSUPPORTED)."""
         s, dev = cache.shape, cache.k_hi.device
+        if not (mikv_tree_workspace_bytes(s, nodes) and mikv_commit_workspace_bytes(s, steps)):
+            raise MikvError("DraftedLayer", 2)  # MIKV_ERR_UNSUPPORTED
         self.cache, self.table, self.nodes, self.steps = cache, table, nodes, steps
         self.lens, self.tokens = Lengths(n_hi, n_lo, slots), tokens
         self.n_lo_max = int(n_lo.max()) if n_lo_max is None else n_lo_max
