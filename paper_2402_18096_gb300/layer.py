@@ -259,12 +259,13 @@ class DraftedLayer:
         self.n_lo_max += self.steps if s.bits else 0
 
     def fork(self, pairs):
-        """Requests copied to other rows of the batch, (from, to) each: their caches, lengths and tokens so far."""
+        """Requests copied to other rows of the batch, (from, to) each: their caches, lengths and tokens so far. A tree that
+        was attended and not committed is dropped, for those rows' tokens no longer follow from it."""
         mikv_copy_requests(self.cache, self.cache, pairs, lens=self.lens, to_lens=self.lens)
         if pairs:
             src, dst = torch.tensor(pairs, device=self.tokens.device).T
             self.tokens[dst] = self.tokens[src]
-        self.drafted = None
+            self.drafted = None
 
     def check(self, stream=None):
         """Raise MikvError (MIKV_ERR_DEVICE) if a kernel of a tree or a commit so far gave up; synchronises."""

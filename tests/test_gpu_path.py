@@ -441,3 +441,19 @@ def test_a_captured_commit_without_the_room_is_refused():
     assert e.value.status == "MIKV_ERR_CAPACITY" and layer.lens.n_lo.tolist() == [14]
     g.replay()
     layer.check()
+
+
+def test_forks_of_nothing_keep_the_tree():
+    """And forks of a request drop it: a commit then asks for another."""
+    d = drafts(32, hi=40, lo=64, n_hi=[40, 10, 40, 39], n_lo=[3, 0, 5, 20])
+    layer = DraftedLayer(d.cache, pkg.RotaryTable(), d.N, 4, d.dev(d.n_hi), d.dev(d.n_lo), d.free, d.dev([42, 9, 44, 58]))
+    layer.attend(d.q, d.k, d.v, d.parents, torch.empty_like(d.q))
+    layer.fork([])
+    layer.commit(path_tensor([[0]] * 4, 4))
+    assert layer.tokens.tolist() == [43, 10, 45, 59]
+    layer.attend(d.q, d.k, d.v, d.parents, torch.empty_like(d.q))
+    layer.fork([(0, 1)])
+    with pytest.raises(ValueError):
+        layer.commit(path_tensor([[0]] * 4, 4))
+    assert layer.tokens.tolist() == [43, 43, 45, 59]
+    layer.check()
