@@ -190,6 +190,15 @@ class SharedPrefixLayer:
         o.pos += 1
 
 
+def _check_operand(name: str, t, shape, types):
+    """What mikv_tree_attention asks of a [B, H, nodes, d] operand."""
+    size = t.element_size()
+    if t.shape != shape or t.dtype not in types or not t.is_cuda or t.stride(3) != 1 or t.data_ptr() % 16 or \
+            any(n > 1 and (s <= 0 or s * size % 16) for n, s in zip(shape[:3], t.stride())):
+        raise ValueError(f"{name}: expected a device tensor of shape {shape}, type {' or '.join(str(x) for x in types)} and "
+                         f"16-byte aligned rows, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+
+
 class DraftedLayer:
     """One layer whose requests decode trees of drafted tokens over their mixed-precision caches (bf16 important set), each
     request at its own length. attend() runs a tree, commit() takes the accepted path into the cache."""
@@ -226,7 +235,13 @@ class DraftedLayer:
 
     def attend(self, q, k, v, parents, out):
         """Attention of drafted tokens as projected: q [B, Hq, nodes, d] and k, v [B, Hkv, nodes, d] (views; q and k are turned
-        in place) with parents int32 [B, nodes], into out [B, Hq, nodes, d]. The next commit() takes its path from them."""
+        in place) with parents int32 [B, nodes], into out [B, Hq, nodes, d] (bf16 or fp32). The next commit() takes its path
+        from them. A call that is refused has turned nothing."""
+        s = self.cache.shape
+        qs, ks = (s.batch, s.heads_q, self.nodes, s.head_dim), (s.batch, s.heads_kv, self.nodes, s.head_dim)
+        for name, t, shape, types in (("q", q, qs, (torch.bfloat16,)), ("k", k, ks, (torch.bfloat16,)),
+                                      ("v", v, ks, (torch.bfloat16,)), ("out", out, qs, (torch.bfloat16, torch.float32))):
+            _check_operand(name, t, shape, types)
         mikv_tree_masks(self.masks, parents, positions=self.positions, first=self.tokens)
         mikv_rotary(self.table, q, k, positions=self.positions)
         mikv_tree_attention(self.cache, self.masks, q, k, v, out, self.ws_tree, lens=self.lens, lse=self.lse)

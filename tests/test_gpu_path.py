@@ -457,3 +457,23 @@ def test_forks_of_nothing_keep_the_tree():
         layer.commit(path_tensor([[0]] * 4, 4))
     assert layer.tokens.tolist() == [43, 43, 45, 59]
     layer.check()
+
+
+def test_trees_that_are_refused_turn_nothing():
+    """Operands that the attention does not take, though the rotary positions would: q and k are as they were, and the same
+    tree may come again."""
+    d = drafts(33, hi=40, lo=64, n_hi=[40, 10, 40, 39], n_lo=[3, 0, 5, 20])
+    layer = DraftedLayer(d.cache, pkg.RotaryTable(), d.N, 4, d.dev(d.n_hi), d.dev(d.n_lo), d.free, d.dev([42, 9, 44, 58]))
+    q0, k0, out = d.q.clone(), d.k.clone(), torch.empty_like(d.q)
+    room = torch.empty(d.v.numel() + 8, dtype=BF, device="cuda")
+    odd = room[1:1 + d.v.numel()].view(d.v.transpose(1, 2).shape).transpose(1, 2)  # rows off a 16-byte boundary
+    assert odd.data_ptr() % 16
+    pitch = torch.empty(4, d.N, 2, 132, dtype=BF, device="cuda")[..., :128].transpose(1, 2)  # and at strides of 264 bytes
+    for v, o in ((odd, out), (pitch, out), (d.v.float(), out), (d.v[:, :, 1:], out), (d.v, out.half()), (d.v, out[:, 1:]),
+                 (d.v[:1].expand(4, -1, -1, -1), out), (d.v.cpu(), out)):
+        with pytest.raises(ValueError):
+            layer.attend(d.q, d.k, v, d.parents, o)
+        same(d.q, q0, "q"), same(d.k, k0, "k")
+        assert layer.drafted is None
+    layer.attend(d.q, d.k, d.v, d.parents, out.float())
+    layer.check()
