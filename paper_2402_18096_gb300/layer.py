@@ -192,6 +192,10 @@ class SharedPrefixLayer:
 
 def _check_operand(name: str, t, shape, types):
     """What mikv_tree_attention asks of a [B, H, nodes, d] operand."""
+    if t.shape == shape and t.dtype in types and t.is_cuda:  # (nearly always, in a quarter of the time)
+        b, h, n, c = t.stride()
+        if c == 1 and b > 0 and h > 0 and n > 0 and not (t.data_ptr() | 2 * (b | h | n)) & 15:
+            return
     size = t.element_size()
     if t.shape != shape or t.dtype not in types or not t.is_cuda or t.stride(3) != 1 or t.data_ptr() % 16 or \
             any(n > 1 and (s <= 0 or s * size % 16) for n, s in zip(shape[:3], t.stride())):
