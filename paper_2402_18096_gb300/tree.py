@@ -141,9 +141,9 @@ def mikv_commit_path(cache, path, k, v, gained, first, workspace, lens: Lengths,
 def mikv_copy_requests(cache, to_cache, pairs, lens: Lengths = None, to_lens: Lengths = None, stream=None):
     """Whole requests copied: for every (from, to) of `pairs`, row `to` of to_cache takes what row `from` of cache holds
     (and to_lens its lengths). The two caches may be one, if no row is both source and target."""
-    flat = [int(x) for p in pairs for x in p]
-    if len(flat) != 2 * len(pairs):
+    if any(len(p) != 2 for p in pairs):
         raise ValueError("pairs: (from, to) each")
+    flat = [int(x) for p in pairs for x in p]
     rc = load().mikv_copy_requests(
         _shape(cache.shape), _cache(cache), _shape(to_cache.shape), _cache(to_cache),
         (ctypes.c_int32 * max(len(flat), 1))(*flat), len(pairs), _lens(lens, cache.shape),

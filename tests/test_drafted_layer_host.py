@@ -23,3 +23,10 @@ def test_caches_and_sizes_that_the_kernels_do_not_take_are_refused_at_once(kw):
 @pytest.mark.parametrize("kw", [dict(), dict(bits=0), dict(nodes=128, steps=128)])
 def test_others_are_taken(kw):
     assert make(**kw).drafted is None
+
+
+@pytest.mark.parametrize("pairs", [[(0,)], [(0, 1, 2), (3,)], [(), (0, 1, 2, 3)]])
+def test_pairs_of_other_lengths_are_refused(pairs):
+    c = pkg.LayerCache(pkg.Shape(4, 4, 2, 2, 32, 16, 64), device="cpu")
+    with pytest.raises(ValueError, match="from, to"):
+        pkg.mikv_copy_requests(c, c, pairs)
