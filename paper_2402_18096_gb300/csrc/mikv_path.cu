@@ -187,8 +187,10 @@ struct CommitArrays {
 
 // One block per KV head. The demoted entries are found one after another, the least (score, id, place) of those left
 // (places: the slots, then the path's nodes); a warp to a row quantizes them; then the tokens that stay are written. Bound
-// by latency: the scores and ids are read once and stay in registers (kOwn entries a thread), a demotion costs two
-// reductions, and the rows of all demotions are in flight together.
+// by latency: a demotion costs two reductions, and the rows of all demotions are in flight together. The scores and ids of
+// the first 2048 entries are read once and stay in registers (kOwn entries a thread); those behind are read again, from
+// L2, for every demotion. Eight demotions, us a call in a graph: 64 requests of up to 1025 slots, 32 KV heads 9.7; 32 of 2001, 8
+// KV heads 14.7, of 6555 33.6 (one demotion 10.9).
 constexpr int kCommitThreads = 256, kOwn = 8;
 template <int BITS, int GROUP>
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArrays c, const PathArgs a, bool lengths) {
@@ -322,7 +324,9 @@ struct CopyArgs {
 };
 
 // Block (pair, chunk, head): its chunk of the bytes that the request keeps of this head, array after array. Pairs run
-// fastest, so that those of one source read it from L2.
+// fastest, so that those of one source read it from L2. Long requests are bound by HBM (16 copies of up to 8192 tokens, 40
+// heads: 114 us, 82 % of a copy), short ones by the way through nine arrays (three of 512 tokens, 32 heads: 14.6 us in a
+// graph, 2.3 at a copy's rate).
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
   const int2 pair = a.pair[blockIdx.x];
   grid_dependency_wait();
